@@ -73,7 +73,8 @@ typedef enum {
     FSA_ERR_DTYPE = -3,   /* unknown fsa_dtype / fsa_itype                                */
     FSA_ERR_ALIGN = -4,   /* a pointer is not aligned to its element size                 */
     FSA_ERR_HIP = -5,     /* the HIP runtime refused the launch                           */
-    FSA_ERR_SCRATCH = -6  /* the call needs more scratch than the library's fixed array   */
+    FSA_ERR_SCRATCH = -6, /* the call needs more scratch than the library's fixed array   */
+    FSA_ERR_WORKSPACE = -7 /* the caller's workspace is smaller than the call needs        */
 } fsa_status;
 
 enum { FSA_KMAX = 64 };   /* largest fanout per hop (one wavefront lane per Floyd step)   */
@@ -360,6 +361,60 @@ int fsa_wmean_bwd_ws(const float* grad_out, const float* grad_h1,
                      int64_t B, int32_t k1, int32_t k2, int64_t D,
                      float* grad_x, int64_t num_nodes,
                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Losses over many classes: a row of h (what a model answers for a seed: fsa_sample_mean_fwd's out, or a layer on top of
+ * it) against every row of a class table w (labels, or the nodes of the graph themselves), without keeping the T x V
+ * scores.  With s = scale, or scale / temperature in the distillation:
+ *   z[t,v] = s * h[t,:] . w[v,:],   lse[t] = log sum_v exp z[t,v],   p[t,v] = exp(z[t,v] - lse[t])
+ *   fsa_xent     loss[t] = lse[t] - z[t, targets[t]]
+ *   fsa_distill  loss[t] = sum_j q[t,j] (log q[t,j] - log p[t, ids[t,j]]),  q[t,:] = softmax over the slots j of row t of
+ *                teacher_logits[t,j] / temperature: the divergence from a teacher of which the K best classes are known,
+ *                renormalised over those.  Cross entropy is the case of one slot with weight one.
+ * A negative target or ID is an empty slot and may appear anywhere; nothing that stands at it is used.  A row without a
+ * slot (or whose teacher logits are all -inf) has loss 0, lse 0, mean 0, a zero gradient, and adds nothing to grad_w,
+ * whatever its h, lse and grad_loss hold, NaN included.  An ID of V or more is not read: the row's loss is NaN, the
+ * gradients are as if its slot's class were none of the table's.  An ID named by two slots of a row counts twice.
+ *   h [T,D], w [V,D]   fsa_dtype `dtype`, rows `h_stride` and `w_stride` elements apart (>= D), at any alignment of an
+ *                      element;  0 <= T <= FSA_CLASS_TMAX, 1 <= V <= FSA_CLASS_VMAX, 1 <= D <= FSA_CLASS_DMAX
+ *   scale, temperature finite and positive
+ *   out_loss, out_lse  [T] fp32
+ *   out_mean           [T,D] fp32, the mean of w's rows under p; may be NULL.  The gradient of h is made of it.
+ *   grad_loss          [T] fp32: the gradient of every loss (its signs may differ)
+ *   lse, mean          as the forward wrote them; mean may be NULL (the backward then computes it again)
+ *   grad_h [T,D], grad_w [V,D]   `dtype`, contiguous, written whole; either may be NULL
+ *   workspace          device memory of the call's *_workspace_bytes, 16-byte aligned (else FSA_ERR_WORKSPACE,
+ *                      FSA_ERR_ALIGN); nothing in it is kept from one call to the next
+ * Sums, maxima and means are fp32.  Scores of 16-bit tables are fp32 sums of exact products; those of fp32 tables take
+ * 22 bits of every element (see the kernels); probabilities enter the gradients rounded to the table's 16-bit type, or to
+ * 22 bits.  Every result is a function of the arguments alone: no atomics whose order could change it (two slots of a row
+ * that name one class aside).
+ */
+enum { FSA_CLASS_TMAX = 1 << 23, FSA_CLASS_VMAX = 1 << 30, FSA_CLASS_DMAX = 256 };
+
+int64_t fsa_class_fwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_mean);
+/* with_mean: grad_h is wanted and no mean is given; with_grad_w: grad_w is wanted.  0 for sizes that the calls refuse. */
+int64_t fsa_class_bwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_mean, int with_grad_w);
+
+int fsa_xent_fwd(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
+                 int64_t T, int64_t V, int64_t D, float scale, const int32_t* targets,
+                 float* out_loss, float* out_lse, float* out_mean,
+                 void* workspace, int64_t workspace_bytes, void* stream);
+int fsa_xent_bwd(const float* grad_loss, const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
+                 int64_t T, int64_t V, int64_t D, float scale, const int32_t* targets,
+                 const float* lse, const float* mean, void* grad_h, void* grad_w,
+                 void* workspace, int64_t workspace_bytes, void* stream);
+/* teacher_ids [T,K] int32, teacher_logits [T,K] fsa_dtype `teacher_dtype`; 1 <= K <= FSA_KMAX */
+int fsa_distill_fwd(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
+                    int64_t T, int64_t V, int64_t D, float scale, float temperature,
+                    const int32_t* teacher_ids, const void* teacher_logits, int teacher_dtype, int32_t K,
+                    float* out_loss, float* out_lse, float* out_mean,
+                    void* workspace, int64_t workspace_bytes, void* stream);
+int fsa_distill_bwd(const float* grad_loss, const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
+                    int64_t T, int64_t V, int64_t D, float scale, float temperature,
+                    const int32_t* teacher_ids, const void* teacher_logits, int teacher_dtype, int32_t K,
+                    const float* lse, const float* mean, void* grad_h, void* grad_w,
+                    void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Static, never-freed description of a status code. */
 const char* fsa_status_string(int status);

@@ -104,3 +104,42 @@ def fused_sample_mean(x: torch.Tensor, indptr: torch.Tensor, indices: torch.Tens
     out, h1, ids1, ids2 = _FusedSampleMean.apply(x, indptr, indices, seeds, tuple(fanouts), int(seed),
                                                  bool(want_h1), bool(save_indices), master_grad, workspace)
     return (out, h1, ids1 if ids1 is not None and ids1.numel() else None, ids2 if ids2 is not None and ids2.numel() else None)
+
+
+class _ClassLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, h, w, ids, logits, temperature, scale, emit_mean):
+        if logits is None:
+            loss, lse, mean = binding.fsa_xent_fwd(h, w, ids, scale, emit_mean=emit_mean)
+        else:
+            loss, lse, mean = binding.fsa_distill_fwd(h, w, ids, logits, temperature, scale, emit_mean=emit_mean)
+        ctx.save_for_backward(h, w, ids, logits, lse, mean)
+        ctx.temperature, ctx.scale = temperature, scale
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        h, w, ids, logits, lse, mean = ctx.saved_tensors
+        want = dict(want_h=ctx.needs_input_grad[0], want_w=ctx.needs_input_grad[1])
+        g = grad_loss.contiguous()
+        if logits is None:
+            grads = binding.fsa_xent_bwd(g, h, w, ids, lse, mean, ctx.scale, **want)
+        else:
+            grads = binding.fsa_distill_bwd(g, h, w, ids, logits, lse, mean, ctx.temperature, ctx.scale, **want)
+        return (*grads, None, None, None, None, None)
+
+
+def fused_cross_entropy(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, *, scale: float = 1.0) -> torch.Tensor:
+    """Differentiable softmax cross entropy of rows h [T,D] against every class of w [V,D] (scores scale * h.w, never
+    kept), one loss a row, fp32.  targets [T] int32; a negative one leaves its row out (loss 0, no gradient)."""
+    return _ClassLoss.apply(h, w, targets, None, 1.0, float(scale), h.requires_grad and torch.is_grad_enabled())
+
+
+def fused_distillation(h: torch.Tensor, w: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, *,
+                       temperature: float = 1.0, scale: float = 1.0) -> torch.Tensor:
+    """Differentiable divergence of rows h [T,D] over every class of w [V,D] from a teacher of which the K best classes
+    are known: teacher_ids [T,K] int32 (negative: an empty slot) and teacher_logits [T,K].  `temperature` divides both
+    sides' scores; the loss is not multiplied by its square.  The teacher gets no gradient."""
+    return _ClassLoss.apply(h, w, teacher_ids, teacher_logits, float(temperature), float(scale),
+                            h.requires_grad and torch.is_grad_enabled())

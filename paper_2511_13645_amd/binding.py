@@ -38,7 +38,9 @@ EXPORTS = ("fsa_sample_mean_fwd", "fsa_mean_replay_fwd", "fsa_mean_bwd", "fsa_me
            "fsa_mean3_bwd_noalloc", "fsa_mean_bwd_ws", "fsa_mean_bwd_workspace_bytes",
            "fsa_bwd_workspace_bytes", "fsa_mean_bwd_lp_ws", "fsa_mean3_bwd_ws", "fsa_wmean_bwd_ws",
            "fsa_mean_bwd_dense", "fsa_mean_bwd_dense_workspace_bytes", "fsa_mean_bwd_dense_pays",
-           "fsa_sample_wmean_fwd", "fsa_wmean_replay_fwd", "fsa_wmean_bwd")
+           "fsa_sample_wmean_fwd", "fsa_wmean_replay_fwd", "fsa_wmean_bwd",
+           "fsa_class_fwd_workspace_bytes", "fsa_class_bwd_workspace_bytes",
+           "fsa_xent_fwd", "fsa_xent_bwd", "fsa_distill_fwd", "fsa_distill_bwd")
 
 _lib: Optional[ctypes.CDLL] = None
 _host = None                                    # the module _fsa_host, once the library is loaded; None without it
@@ -108,6 +110,19 @@ def lib() -> ctypes.CDLL:
         L.fsa_mean_bwd_dense_pays.restype = ci
         L.fsa_mean_bwd_dense.argtypes = [vp, vp, ci, vp, vp, i64, i32, i32, i64, vp, i64, vp, i64, vp]
         L.fsa_mean_bwd_dense.restype = ci
+        f32 = ctypes.c_float
+        L.fsa_class_fwd_workspace_bytes.argtypes = [i64, i64, i64, ci, i32, ci]
+        L.fsa_class_fwd_workspace_bytes.restype = i64
+        L.fsa_class_bwd_workspace_bytes.argtypes = [i64, i64, i64, ci, i32, ci, ci]
+        L.fsa_class_bwd_workspace_bytes.restype = i64
+        L.fsa_xent_fwd.argtypes = [vp, i64, vp, i64, ci, i64, i64, i64, f32, vp, vp, vp, vp, vp, i64, vp]
+        L.fsa_xent_fwd.restype = ci
+        L.fsa_xent_bwd.argtypes = [vp, vp, i64, vp, i64, ci, i64, i64, i64, f32, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.fsa_xent_bwd.restype = ci
+        L.fsa_distill_fwd.argtypes = [vp, i64, vp, i64, ci, i64, i64, i64, f32, f32, vp, vp, ci, i32, vp, vp, vp, vp, i64, vp]
+        L.fsa_distill_fwd.restype = ci
+        L.fsa_distill_bwd.argtypes = [vp, vp, i64, vp, i64, ci, i64, i64, i64, f32, f32, vp, vp, ci, i32, vp, vp, vp, vp, vp, i64, vp]
+        L.fsa_distill_bwd.restype = ci
         L.fsa_status_string.argtypes = [ci]
         L.fsa_status_string.restype = ctypes.c_char_p
         _lib, _host = L, _load_host(L)
@@ -695,3 +710,150 @@ def fsa_wmean_bwd(grad_out: torch.Tensor, ids1: torch.Tensor, w1: torch.Tensor,
     if rc != FSA_OK:
         raise FsaError(rc, "fsa_wmean_bwd")
     return grad_x
+
+
+# ----------------------------------------------------------------------------------------
+# losses over many classes
+# ----------------------------------------------------------------------------------------
+FSA_CLASS_DMAX = 256
+
+
+def _rows(t: torch.Tensor, name: str) -> int:
+    """Elements from one row of a matrix to the next; its rows are contiguous."""
+    if not t.is_cuda:
+        raise ValueError("%s must live on the GPU" % name)
+    if t.dim() != 2 or t.shape[1] < 1:
+        raise ValueError("%s must be a matrix, got %s" % (name, tuple(t.shape)))
+    if t.stride(1) != 1 and t.shape[1] > 1:
+        raise ValueError("%s must have contiguous rows" % name)
+    if t.shape[0] > 1:
+        if t.stride(0) < t.shape[1]:
+            raise ValueError("the rows of %s must not overlap" % name)
+        return t.stride(0)
+    return t.shape[1]
+
+
+def _class_operands(h: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, logits: Optional[torch.Tensor]):
+    """Checked leading arguments of the class losses: (pointers, strides and type, (T, V, D), K)."""
+    hs, ws = _rows(h, "h"), _rows(w, "w")
+    if h.dtype != w.dtype:
+        raise TypeError("h and w must have one type, got %s and %s" % (h.dtype, w.dtype))
+    (T, D), V = h.shape, w.shape[0]
+    if w.shape[1] != D:
+        raise ValueError("h and w must have rows of one length, got %d and %d" % (D, w.shape[1]))
+    if logits is None:
+        _need(ids, "targets", torch.int32)
+        _shape(ids, "targets", (T,))
+        K = 1
+    else:
+        _need(ids, "teacher_ids", torch.int32)
+        _need(logits, "teacher_logits")
+        _x_dtype(logits)
+        if ids.dim() != 2 or ids.shape[0] != T or ids.shape[1] < 1:
+            raise ValueError("teacher_ids must be [%d,K], got %s" % (T, tuple(ids.shape)))
+        _shape(logits, "teacher_logits", ids.shape)
+        K = ids.shape[1]
+    _same_device(h, (w, "w"), (ids, "targets" if logits is None else "teacher_ids"), (logits, "teacher_logits"))
+    return (_ptr(h), hs, _ptr(w), ws, _x_dtype(h), T, V, D), T, V, D, K
+
+
+def _class_workspace(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor, stream: Optional[torch.cuda.Stream]):
+    """The caller's workspace, or one of torch's for the call: memory that other streams get back only after `stream`."""
+    if workspace is not None:
+        check_workspace(workspace, like)
+        return workspace
+    ws = torch.empty(need, dtype=torch.uint8, device=like.device)
+    if stream is not None:
+        ws.record_stream(stream)
+    return ws
+
+
+def _class_fwd(name: str, h, w, ids, logits, scale: float, temperature: float, emit_mean: bool, workspace, stream):
+    lead, T, V, D, K = _class_operands(h, w, ids, logits)
+    L = lib()
+    loss = torch.empty((T,), dtype=torch.float32, device=h.device)
+    lse = torch.empty_like(loss)
+    mean = torch.empty((T, D), dtype=torch.float32, device=h.device) if emit_mean else None
+    ws = _class_workspace(workspace, L.fsa_class_fwd_workspace_bytes(T, V, D, lead[4], K, int(emit_mean)), h, stream)
+    tail = (_ptr(loss), _ptr(lse), _ptr(mean), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, h))
+    if logits is None:
+        rc = L.fsa_xent_fwd(*lead, scale, _ptr(ids), *tail)
+    else:
+        rc = L.fsa_distill_fwd(*lead, scale, temperature, _ptr(ids), _ptr(logits), _x_dtype(logits), K, *tail)
+    if rc != FSA_OK:
+        raise FsaError(rc, name)
+    return loss, lse, mean
+
+
+def _class_bwd(name: str, grad_loss, h, w, ids, logits, lse, mean, scale: float, temperature: float, want_h: bool, want_w: bool,
+               workspace, stream):
+    lead, T, V, D, K = _class_operands(h, w, ids, logits)
+    for t, n in ((grad_loss, "grad_loss"), (lse, "lse")):
+        _need(t, n, torch.float32)
+        _shape(t, n, (T,))
+    if mean is not None:
+        _need(mean, "mean", torch.float32)
+        _shape(mean, "mean", (T, D))
+    _same_device(h, (grad_loss, "grad_loss"), (lse, "lse"), (mean, "mean"))
+    L = lib()
+    grad_h = torch.empty((T, D), dtype=h.dtype, device=h.device) if want_h else None
+    grad_w = torch.empty((V, D), dtype=w.dtype, device=w.device) if want_w else None
+    need = L.fsa_class_bwd_workspace_bytes(T, V, D, lead[4], K, int(want_h and mean is None), int(want_w))
+    ws = _class_workspace(workspace, need, h, stream)
+    tail = (_ptr(lse), _ptr(mean), _ptr(grad_h), _ptr(grad_w), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, h))
+    if logits is None:
+        rc = L.fsa_xent_bwd(_ptr(grad_loss), *lead, scale, _ptr(ids), *tail)
+    else:
+        rc = L.fsa_distill_bwd(_ptr(grad_loss), *lead, scale, temperature, _ptr(ids), _ptr(logits), _x_dtype(logits), K, *tail)
+    if rc != FSA_OK:
+        raise FsaError(rc, name)
+    return grad_h, grad_w
+
+
+def fsa_xent_fwd(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, *, emit_mean: bool = False,
+                 workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                 ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+    """Softmax cross entropy of rows h [T,D] against the classes w [V,D], the scores never kept; targets [T] int32, a
+    negative one is none.  Returns (loss [T], lse [T], mean [T,D] | None), fp32.  `workspace`: see
+    fsa_class_fwd_workspace_bytes; torch's memory without one."""
+    return _class_fwd("fsa_xent_fwd", h, w, targets, None, float(scale), 1.0, bool(emit_mean), workspace, stream)
+
+
+def fsa_xent_bwd(grad_loss: torch.Tensor, h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,
+                 mean: Optional[torch.Tensor] = None, scale: float = 1.0, *, want_h: bool = True, want_w: bool = True,
+                 workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                 ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Gradients (grad_h | None, grad_w | None) of fsa_xent_fwd from grad_loss [T] and what it returned."""
+    return _class_bwd("fsa_xent_bwd", grad_loss, h, w, targets, None, lse, mean, float(scale), 1.0, bool(want_h), bool(want_w),
+                      workspace, stream)
+
+
+def fsa_distill_fwd(h: torch.Tensor, w: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor,
+                    temperature: float = 1.0, scale: float = 1.0, *, emit_mean: bool = False,
+                    workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                    ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+    """Divergence of the softmax of rows h [T,D] over the classes w [V,D] from a teacher's best classes: teacher_ids
+    [T,K] int32 (negative: an empty slot) and their logits [T,K], renormalised over those.  Returns as fsa_xent_fwd."""
+    return _class_fwd("fsa_distill_fwd", h, w, teacher_ids, teacher_logits, float(scale), float(temperature), bool(emit_mean),
+                      workspace, stream)
+
+
+def fsa_distill_bwd(grad_loss: torch.Tensor, h: torch.Tensor, w: torch.Tensor, teacher_ids: torch.Tensor,
+                    teacher_logits: torch.Tensor, lse: torch.Tensor, mean: Optional[torch.Tensor] = None,
+                    temperature: float = 1.0, scale: float = 1.0, *, want_h: bool = True, want_w: bool = True,
+                    workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                    ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Gradients (grad_h | None, grad_w | None) of fsa_distill_fwd; the teacher gets none."""
+    return _class_bwd("fsa_distill_bwd", grad_loss, h, w, teacher_ids, teacher_logits, lse, mean, float(scale), float(temperature),
+                      bool(want_h), bool(want_w), workspace, stream)
+
+
+def fsa_class_fwd_workspace_bytes(T: int, V: int, D: int, dtype: torch.dtype, K: int = 1, with_mean: bool = False) -> int:
+    """Workspace bytes of fsa_xent_fwd (K = 1) and fsa_distill_fwd; 0 for sizes that they refuse."""
+    return lib().fsa_class_fwd_workspace_bytes(T, V, D, _FLOAT_TYPE[dtype], K, int(with_mean))
+
+
+def fsa_class_bwd_workspace_bytes(T: int, V: int, D: int, dtype: torch.dtype, K: int = 1, with_mean: bool = False,
+                                  with_grad_w: bool = True) -> int:
+    """Workspace bytes of fsa_xent_bwd and fsa_distill_bwd; `with_mean`: grad_h is wanted and no mean given."""
+    return lib().fsa_class_bwd_workspace_bytes(T, V, D, _FLOAT_TYPE[dtype], K, int(with_mean), int(with_grad_w))

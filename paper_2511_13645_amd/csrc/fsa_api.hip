@@ -603,6 +603,7 @@ const char* fsa_status_string(int status) {
         case FSA_ERR_ALIGN: return "a pointer is not aligned to its element size";
         case FSA_ERR_HIP:   return "the HIP runtime refused the launch";
         case FSA_ERR_SCRATCH: return "the call needs more scratch memory than the library's fixed array holds";
+        case FSA_ERR_WORKSPACE: return "the workspace is smaller than the call needs";
         default:            return "unknown status";
     }
 }

@@ -1,0 +1,8 @@
+// Class losses on fp16 tables.
+#define FSA_CLASS_KIND 2
+#include "fsa_class_kernels.hip.h"
+
+namespace fsa {
+hipError_t class_forward_f16(const ClassArgs& a, hipStream_t stream) { return forward(a, stream); }
+hipError_t class_gradient_f16(const ClassArgs& a, hipStream_t stream) { return gradient(a, stream); }
+}  // namespace fsa

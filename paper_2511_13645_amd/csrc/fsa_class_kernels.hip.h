@@ -1,0 +1,815 @@
+// Device side of the class losses, one element type a translation unit (fsa_class_{f32,bf16,f16}.hip).
+//
+// Scores z[t,v] = scale * h[t].w[v] come from 32x32x16 matrix instructions, A = the streamed side (from LDS), B = the
+// held side (in registers).  Lane l of the result holds column l%32 (a held row) and rows 8*(i/4) + 4*(l/32) + i%4,
+// i = 0..15 (streamed rows).  Fed back as the B operand of the second product, register 8s+j of a lane is its k slot
+// (l/32, j) of step s, so with A read transposed at those same rows no lane ever exchanges a probability:
+//     acc[d, held] += sum over streamed rows of streamed[row, d] * P[row, held].
+//
+// fp32 rows are held as two fp16 planes, x * 2^e = hi + lo with 2^e that brings the largest finite |x| of the table to
+// [2^14, 2^15): 22 bits of every element down to 2^-16 of the largest and never an error over 2^-40 of it.  Products
+// take hi*hi + hi*lo + lo*hi; what is left out is below 2^-22 of a product, as is what the split rounds away.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "fsa_class.h"
+#include "fsa_internal.h"
+
+namespace fsa {
+
+struct ClassArgs {
+    ClassShape s;
+    const void* h; int64_t h_stride;                    // strides in elements
+    const void* w; int64_t w_stride;
+    float scale;                                        // what multiplies h.w (the temperature divided out)
+    const int32_t* ids;                                 // [T,K] targets or the teacher's classes
+    const void* teacher; int teacher_kind;              // [T,K] teacher logits, or null: one slot of weight one
+    float inv_temperature;
+    float* loss; float* lse; float* mean;               // forward outputs (mean nullable)
+    const float* grad_loss; const float* lse_in; const float* mean_in;
+    void* grad_h; void* grad_w;
+    ClassCut cut; ClassPlan plan; char* ws;
+    template <class T> __host__ __device__ T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
+};
+
+hipError_t class_forward_f32(const ClassArgs&, hipStream_t);
+hipError_t class_forward_bf16(const ClassArgs&, hipStream_t);
+hipError_t class_forward_f16(const ClassArgs&, hipStream_t);
+hipError_t class_gradient_f32(const ClassArgs&, hipStream_t);
+hipError_t class_gradient_bf16(const ClassArgs&, hipStream_t);
+hipError_t class_gradient_f16(const ClassArgs&, hipStream_t);
+
+#ifdef FSA_CLASS_KIND
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kKind = FSA_CLASS_KIND;                   // 0 fp32, 1 bfloat16, 2 fp16
+constexpr int NS = kKind == 0 ? 2 : 1;
+constexpr bool kHalf = kKind != 1;                      // planes hold fp16 (bfloat16 otherwise)
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+// fp16 probabilities are kept as p * 2^14: 22 binades below the largest stay normal numbers.
+constexpr float kLift = kHalf ? 14.0f : 0.0f;
+// The running reference of a row follows its maximum only when that is passed by this many binades, so that most tiles
+// leave the accumulators alone; 2^(14+1) is in range of fp16, bfloat16 has room.
+constexpr float kSlack = kHalf ? 1.0f : 8.0f;
+using Elem = typename std::conditional<kKind == 0, float, uint16_t>::type;
+
+__device__ __forceinline__ float as_float(uint16_t b) {
+    if constexpr (kHalf) return (float)__builtin_bit_cast(_Float16, b);
+    else return __builtin_bit_cast(float, (uint32_t)b << 16);
+}
+__device__ __forceinline__ float value(float x) { return x; }
+__device__ __forceinline__ float value(uint16_t x) { return as_float(x); }
+__device__ __forceinline__ uint32_t pack2(float a, float b) {     // nearest even
+    if constexpr (kHalf) { const f16x2 v = {(_Float16)a, (_Float16)b}; return __builtin_bit_cast(uint32_t, v); }
+    else { const bf16x2 v = {(__bf16)a, (__bf16)b}; return __builtin_bit_cast(uint32_t, v); }
+}
+__device__ __forceinline__ float low2(uint32_t p) { return as_float((uint16_t)(p & 0xffff)); }
+__device__ __forceinline__ float high2(uint32_t p) { return as_float((uint16_t)(p >> 16)); }
+
+__device__ __forceinline__ f32x16 matmul(u32x4 a, u32x4 b, f32x16 c) {
+    if constexpr (kHalf)
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// a and b of NS planes each: every product but lo*lo.
+__device__ __forceinline__ f32x16 matmul(const u32x4 (&a)[NS], const u32x4 (&b)[NS], f32x16 c) {
+    if constexpr (NS == 2) { c = matmul(a[1], b[0], c); c = matmul(a[0], b[1], c); }
+    return matmul(a[0], b[0], c);
+}
+
+// Planes of eight scaled elements.  An infinite element stays infinite (and its rest zero), NaN stays NaN.
+__device__ __forceinline__ void split8(const float (&x)[8], float unit, u32x4 (&out)[NS]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = x[2 * i] * unit, b = x[2 * i + 1] * unit;
+        out[0][i] = pack2(a, b);
+        if constexpr (NS == 2) {
+            float ra = a - low2(out[0][i]), rb = b - high2(out[0][i]);
+            if (__builtin_isinf(a)) ra = 0.0f;
+            if (__builtin_isinf(b)) rb = 0.0f;
+            out[1][i] = pack2(ra, rb);
+        }
+    }
+}
+
+// Eight elements of a row from column `col` on, zero behind its D: read wide, at whatever alignment the row has.
+struct Eight { typename std::conditional<kKind == 0, f32x4, u32x4>::type v[kKind == 0 ? 2 : 1]; };
+__device__ __forceinline__ Eight load8(const Elem* row, int64_t D, int col) {
+    Eight e;
+    if (col + 8 <= D) {
+        __builtin_memcpy(&e, row + col, sizeof(e));
+    } else {
+        Elem x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = col + i < D ? row[col + i] : (Elem)0;
+        __builtin_memcpy(&e, x, sizeof(e));
+    }
+    return e;
+}
+__device__ __forceinline__ void planes_of(const Eight& e, float unit, u32x4 (&out)[NS]) {
+    if constexpr (kKind == 0) {
+        float x[8];
+        __builtin_memcpy(x, &e, sizeof(x));
+        split8(x, unit, out);
+    } else out[0] = __builtin_bit_cast(u32x4, e.v[0]);
+}
+
+// Chunk (of 8 elements) c of row r lies at chunk c ^ turn(r) of its row: 8 rows of one chunk (the first product's reads)
+// and 4 rows of two neighbouring ones (the transposing reads) then lie on different banks.
+__device__ __forceinline__ int turn(int r) { return 2 * (r & 3) + ((r >> 2) & 1); }
+
+__device__ __forceinline__ u32x2 read_transposed(const uint16_t* p) {
+    using lds_s16x4 = __attribute__((address_space(3))) s16x4;
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// powers of two that bring the largest finite element of a table to [2^14, 2^15)
+// ---------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float unit_of(float peak) {
+    if (!(peak > 0.0f)) return 1.0f;
+    int e = 0;
+    frexpf(peak, &e);                                   // peak = m * 2^e, m in [0.5, 1)
+    e = 15 - e;
+    return ldexpf(1.0f, e < -126 ? -126 : e > 126 ? 126 : e);
+}
+__device__ __forceinline__ float finite_abs(float x) {
+    const float a = fabsf(x);
+    return a < __builtin_inff() ? a : 0.0f;
+}
+// Largest of n partial peaks, by the whole workgroup; `room` is a word of LDS per wave.
+__device__ __forceinline__ float block_peak(const float* peaks, int n, float* room) {
+    float m = 0.0f;
+    for (int i = threadIdx.x; i < n; i += kClassThreads) m = fmaxf(m, peaks[i]);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
+    __syncthreads();
+    return m;
+}
+struct Units { float w, h, g; };
+__device__ __forceinline__ Units units(const ClassArgs& a, float* room, bool grad) {
+    Units u{1.0f, 1.0f, 1.0f};
+    const float* p = a.at<const float>(a.plan.peaks);
+    if constexpr (kKind == 0) {
+        u.w = unit_of(block_peak(p, kPeaksTable, room));
+        u.h = unit_of(block_peak(p + kPeaksTable, kPeaksRows, room));
+    }
+    if constexpr (kHalf) if (grad) u.g = unit_of(block_peak(p + kPeaksTable + kPeaksRows, kPeaksGrad, room));
+    return u;
+}
+
+// Whether a row has a slot; the whole wave asks for one row.
+__device__ __forceinline__ bool row_lives(const ClassArgs& a, int64_t t, int lane) {
+    bool some = false;
+    for (int j = lane; j < a.s.K; j += 64) some |= a.ids[t * a.s.K + j] >= 0;
+    return __any(some);
+}
+
+__global__ __launch_bounds__(kClassThreads) void class_peaks_kernel(ClassArgs a, int table, int rows, int grad) {
+    __shared__ float room[kClassWaves];
+    float* out = a.at<float>(a.plan.peaks);
+    int b = blockIdx.x;
+    float m = 0.0f;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (b < table) {
+        const Elem* w = static_cast<const Elem*>(a.w);
+        if (a.w_stride == a.s.D) {
+            const int64_t n = a.s.V * a.s.D, step = (int64_t)table * kClassThreads;
+            const int64_t quads = (reinterpret_cast<uintptr_t>(w) & 15) == 0 ? n / 4 : 0;
+            for (int64_t i = (int64_t)b * kClassThreads + threadIdx.x; i < quads; i += step) {
+                const f32x4 x = reinterpret_cast<const f32x4*>(w)[i];
+                m = fmaxf(fmaxf(m, fmaxf(finite_abs(x[0]), finite_abs(x[1]))), fmaxf(finite_abs(x[2]), finite_abs(x[3])));
+            }
+            for (int64_t i = quads * 4 + (int64_t)b * kClassThreads + threadIdx.x; i < n; i += step) m = fmaxf(m, finite_abs(value(w[i])));
+        } else {
+            for (int64_t v = (int64_t)b * kClassWaves + wave; v < a.s.V; v += (int64_t)table * kClassWaves)
+                for (int d = lane; d < a.s.D; d += 64) m = fmaxf(m, finite_abs(value(w[v * a.w_stride + d])));
+        }
+    } else if ((b -= table) < rows) {
+        out += kPeaksTable;
+        for (int64_t t = (int64_t)b * kClassWaves + wave; t < a.s.T; t += (int64_t)rows * kClassWaves) {
+            if (!row_lives(a, t, lane)) continue;
+            for (int d = lane; d < a.s.D; d += 64) m = fmaxf(m, finite_abs(value(static_cast<const Elem*>(a.h)[t * a.h_stride + d])));
+        }
+    } else {
+        b -= rows;
+        out += kPeaksTable + kPeaksRows;
+        for (int64_t t = (int64_t)b * kClassWaves + wave; t < a.s.T; t += (int64_t)grad * kClassWaves)
+            if (row_lives(a, t, lane)) m = fmaxf(m, finite_abs(a.grad_loss[t]));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    if (lane == 0) room[wave] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) out[b] = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// rows: planes of h (rows without a slot are zero, whatever they hold), and for the gradient what a row brings along
+// ---------------------------------------------------------------------------------------------------------------
+// The teacher's weights of row t over its slots, in lanes 0..K-1 (K <= 64): a softmax over the slots that name a class.
+__device__ __forceinline__ float slot_weight(const ClassArgs& a, int64_t t, int lane, int& id, float& log_weight) {
+    id = -1;
+    float x = -__builtin_inff();
+    if (lane < a.s.K) {
+        const int64_t i = t * a.s.K + lane;
+        id = a.ids[i];
+        if (!a.teacher) x = 0.0f;
+        else if (a.teacher_kind == 0) x = static_cast<const float*>(a.teacher)[i];
+        else if (a.teacher_kind == 1) x = __builtin_bit_cast(float, (uint32_t)static_cast<const uint16_t*>(a.teacher)[i] << 16);
+        else x = (float)static_cast<const _Float16*>(a.teacher)[i];
+        x = id < 0 ? -__builtin_inff() : x * a.inv_temperature;
+    }
+    log_weight = 0.0f;
+    if (!a.teacher) return id >= 0 ? 1.0f : 0.0f;
+    float top = x;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    if (top == -__builtin_inff()) top = 0.0f;           // no slot, or none with any weight
+    const float e = id < 0 ? 0.0f : expf(x - top);
+    float sum = e;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    if (sum == 0.0f) { id = -1; return 0.0f; }          // teacher gives its classes no weight: as a row without slots
+    log_weight = x - top - logf(sum);
+    return e / sum;
+}
+
+// One workgroup per 32 rows, eight to a wave.
+template <int DP>
+__global__ __launch_bounds__(kClassThreads) void class_rows_kernel(ClassArgs a, int64_t padded, bool grad) {
+    __shared__ float room[kClassWaves];
+    __shared__ uint32_t signs;
+    if (threadIdx.x == 0) signs = 0;
+    const Units u = units(a, room, grad);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint16_t* planes = a.at<uint16_t>(a.plan.rows);
+    __syncthreads();
+    for (int q = wave; q < kBlock; q += kClassWaves) {
+        const int64_t t = (int64_t)blockIdx.x * kBlock + q;
+        int id = -1;
+        float log_weight, weight = 0.0f;
+        if (t < a.s.T) weight = slot_weight(a, t, lane, id, log_weight);
+        const bool lives = __any(id >= 0);
+        for (int c = lane; c < DP / 8; c += 64) {
+            u32x4 p[NS] = {};
+            if (lives && c * 8 < a.s.D)
+                planes_of(load8(static_cast<const Elem*>(a.h) + t * a.h_stride, a.s.D, c * 8), u.h, p);
+#pragma unroll
+            for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + ((int64_t)n * padded + t) * DP + c * 8) = p[n];
+        }
+        if (!grad) continue;
+        // P = |g| * softmax * units = 2^(scores*log2e + start), its sign apart
+        const float g = lives ? a.grad_loss[t] * u.g : 0.0f;
+        if (lane < a.s.K && t < a.s.T)
+            a.at<float>(a.plan.pull)[t * a.s.K + lane] = id >= 0 && id < a.s.V ? g * weight : 0.0f;
+        if (lane == 0) {
+            const float to_log2 = a.scale * kLog2e / u.h / u.w;
+            a.at<float>(a.plan.start)[t] = lives ? (log2f(fabsf(g)) - a.lse_in[t] * kLog2e) / to_log2 : -__builtin_inff();
+            if (g < 0.0f) atomicOr(&signs, 1u << q);
+        }
+    }
+    __syncthreads();
+    if (grad && threadIdx.x == 0) a.at<uint32_t>(a.plan.signs)[blockIdx.x] = signs;
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// the streamed side in LDS: ROWS rows of DP elements, NS planes
+// ---------------------------------------------------------------------------------------------------------------
+template <int DP, int ROWS>
+struct Tile {
+    static constexpr int kChunks = ROWS * DP / 8, kEach = kChunks / kClassThreads;
+    static constexpr int kPlane = ROWS * DP;            // elements
+    static_assert(kChunks % kClassThreads == 0, "threads share a tile evenly");
+
+    // Rows [first, first + ROWS) of the table, those behind its last row repeat it.
+    struct FromTable {
+        Eight e[kEach];
+        __device__ __forceinline__ void load(const Elem* w, int64_t stride, int64_t V, int64_t D, int64_t first) {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int q = i * kClassThreads + threadIdx.x, r = q / (DP / 8), c = q % (DP / 8);
+                const int64_t v = first + r < V ? first + r : V - 1;
+                e[i] = load8(w + v * stride, D, c * 8);
+            }
+        }
+        __device__ __forceinline__ void store(uint16_t* lds, float unit) const {
+#pragma unroll
+            for (int i = 0; i < kEach; ++i) {
+                const int q = i * kClassThreads + threadIdx.x, r = q / (DP / 8), c = q % (DP / 8);
+                u32x4 p[NS];
+                planes_of(e[i], unit, p);
+#pragma unroll
+                for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(lds + n * kPlane + r * DP + (c ^ turn(r)) * 8) = p[n];
+            }
+        }
+    };
+    // Rows [first, first + ROWS) of planes that have them all.
+    struct FromPlanes {
+        u32x4 p[NS][kEach];
+        __device__ __forceinline__ void load(const uint16_t* planes, int64_t padded, int64_t first) {
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const int q = i * kClassThreads + threadIdx.x;
+                    p[n][i] = *reinterpret_cast<const u32x4*>(planes + ((int64_t)n * padded + first) * DP + (int64_t)q * 8);
+                }
+        }
+        __device__ __forceinline__ void store(uint16_t* lds) const {
+#pragma unroll
+            for (int n = 0; n < NS; ++n)
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) {
+                    const int q = i * kClassThreads + threadIdx.x, r = q / (DP / 8), c = q % (DP / 8);
+                    *reinterpret_cast<u32x4*>(lds + n * kPlane + r * DP + (c ^ turn(r)) * 8) = p[n][i];
+                }
+        }
+    };
+
+    // A operand of the first product: block b, step ks of 16 elements.
+    static __device__ __forceinline__ void rows(const uint16_t* lds, int b, int ks, int lane, u32x4 (&out)[NS]) {
+        const int r = b * kBlock + (lane & 31), c = 2 * ks + (lane >> 5);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) out[n] = *reinterpret_cast<const u32x4*>(lds + n * kPlane + r * DP + (c ^ turn(r)) * 8);
+    }
+    // A operand of the second: elements 32*db.., step s of 16 rows of block b, the rows in the order of a result's registers.
+    static __device__ __forceinline__ void columns(const uint16_t* lds, int b, int s, int db, int lane, u32x4 (&out)[NS]) {
+        const int i = lane & 15, r = b * kBlock + 16 * s + 4 * (lane >> 5) + (i >> 2);
+        const int c = 4 * db + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            const uint16_t* p = lds + n * kPlane + r * DP + (c ^ turn(r)) * 8 + (i & 1) * 4;
+            const u32x2 a = read_transposed(p), z = read_transposed(p + 8 * DP);   // rows r and r + 8 turn alike
+            out[n] = u32x4{a[0], a[1], z[0], z[1]};
+        }
+    }
+};
+
+// P of a block as the second product's B operand, its two steps; planes of what fp16 or bfloat16 takes of it, nearest even.
+__device__ __forceinline__ void operand_of(const float (&p)[16], u32x4 (&out)[2][NS]) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = p[8 * s + j];
+        split8(x, 1.0f, out[s]);
+    }
+}
+
+// Row that register i of a result stands for, in its block.
+__device__ __forceinline__ int row_of(int i, int lane) { return 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3); }
+
+// ---------------------------------------------------------------------------------------------------------------
+// forward: a wave holds 32 rows of h, the table streams by
+// ---------------------------------------------------------------------------------------------------------------
+template <int DP, int WY, bool MEAN>
+__global__ __launch_bounds__(kClassThreads) void class_forward_kernel(ClassArgs a, int64_t padded) {
+    constexpr int NB = WY == 4 ? 4 : 2, MY = NB / WY, WX = kClassWaves / WY;   // blocks of a tile, a wave's own of them
+    using T = Tile<DP, NB * kBlock>;
+    __shared__ __align__(16) uint16_t lds[2][NS * T::kPlane];
+    __shared__ float room[kClassWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = wave % WX, y = wave / WX;
+    const int64_t part = blockIdx.x % a.cut.parts, group = blockIdx.x / a.cut.parts;
+    const Units u = units(a, room, false);
+    const float to_log2 = a.scale * kLog2e / u.h / u.w;
+    const int64_t first = a.cut.tiles * part / a.cut.parts, last = a.cut.tiles * (part + 1) / a.cut.parts;
+    const int64_t row = (group * WX + x) * kBlock + (lane & 31);               // of h, held by this lane
+    const bool live = (group * WX + x) * kBlock < padded;                      // wave-uniform
+
+    u32x4 held[DP / 16][NS];
+#pragma unroll
+    for (int ks = 0; ks < DP / 16; ++ks)
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+            held[ks][n] = live ? *reinterpret_cast<const u32x4*>(a.at<const uint16_t>(a.plan.rows) + ((int64_t)n * padded + row) * DP +
+                                                                  16 * ks + 8 * (lane >> 5))
+                               : u32x4{};
+
+    float ref = -1e30f, sum = 0.0f;                     // P = 2^(score - ref); ref = followed maximum - kLift
+    f32x16 acc[MEAN ? DP / 32 : 1];
+#pragma unroll
+    for (auto& f : acc) f = f32x16{};
+
+    const Elem* w = static_cast<const Elem*>(a.w);
+    typename T::FromTable next;
+    if (first < last) next.load(w, a.w_stride, a.s.V, a.s.D, first * NB * kBlock);
+    for (int64_t it = first; it < last; ++it) {
+        uint16_t* tile = lds[(it - first) & 1];         // the other one may still be read
+        next.store(tile, u.w);
+        __syncthreads();
+        if (it + 1 < last) next.load(w, a.w_stride, a.s.V, a.s.D, (it + 1) * NB * kBlock);
+        if (!live) continue;
+
+        f32x16 score[MY];
+#pragma unroll
+        for (int m = 0; m < MY; ++m) {
+            score[m] = f32x16{};
+#pragma unroll
+            for (int ks = 0; ks < DP / 16; ++ks) {
+                u32x4 f[NS];
+                T::rows(tile, y * MY + m, ks, lane, f);
+                score[m] = matmul(f, held[ks], score[m]);
+            }
+        }
+        if ((it + 1) * NB * kBlock > a.s.V) {           // the last tile: classes that there are not
+#pragma unroll
+            for (int m = 0; m < MY; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (it * NB * kBlock + (y * MY + m) * kBlock + row_of(i, lane) >= a.s.V) score[m][i] = -__builtin_inff();
+        }
+        float top = score[0][0];
+#pragma unroll
+        for (int m = 0; m < MY; ++m)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, score[m][i]);
+        top *= to_log2;
+        if (__any(top - ref > kLift + kSlack)) {
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float to = fmaxf(ref, top - kLift), by = exp2f(ref - to);
+            ref = to;
+            sum *= by;
+            if constexpr (MEAN)
+#pragma unroll
+                for (auto& f : acc) f *= by;
+        }
+#pragma unroll
+        for (int m = 0; m < MY; ++m) {
+            float p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(score[m][i], to_log2, -ref));
+            float s4[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s4[i] = (p[i] + p[i + 4]) + (p[i + 8] + p[i + 12]);
+            sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            if constexpr (MEAN) {
+                u32x4 b[2][NS];
+                operand_of(p, b);
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int db = 0; db < DP / 32; ++db) {
+                        u32x4 f[NS];
+                        T::columns(tile, y * MY + m, s, db, lane, f);
+                        acc[db] = matmul(f, b[s], acc[db]);
+                    }
+            }
+        }
+    }
+    if (!live) return;
+    sum += __shfl_xor(sum, 32);
+    const int64_t at = (part * WY + y) * padded + row;
+    if (lane < 32) {
+        a.at<float>(a.plan.top)[at] = ref;
+        a.at<float>(a.plan.sum)[at] = sum;
+    }
+    if constexpr (MEAN) {
+        float* out = a.at<float>(a.plan.mean_parts) + at * DP + 4 * (lane >> 5);
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4*>(out + 32 * db + 8 * i) =
+                    f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]};
+    }
+}
+
+// One workgroup per row: the parts joined, the row's slots scored again (fp32 sums of the elements themselves), its loss.
+__global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a, int64_t padded, int depth, int slices) {
+    __shared__ float room[kClassWaves], slot_q[64], slot_log[64], slot_loss[64];
+    __shared__ int slot_id[64];
+    const int64_t t = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const Units u = units(a, room, false);
+    if (wave == 0) {
+        int id;
+        float log_weight;
+        const float q = slot_weight(a, t, lane, id, log_weight);
+        if (lane < a.s.K) { slot_q[lane] = q; slot_log[lane] = log_weight; slot_id[lane] = id; slot_loss[lane] = 0.0f; }
+        const bool lives = __any(id >= 0);
+        if (lane == 0) room[0] = lives ? 1.0f : 0.0f;
+    }
+    __syncthreads();
+    const bool lives = room[0] != 0.0f;
+    __syncthreads();
+    if (!lives) {                                       // nothing of the row is used, whatever it holds
+        if (threadIdx.x == 0) { a.loss[t] = 0.0f; a.lse[t] = 0.0f; }
+        if (a.mean) for (int d = threadIdx.x; d < a.s.D; d += kClassThreads) a.mean[t * a.s.D + d] = 0.0f;
+        return;
+    }
+    const float* tops = a.at<const float>(a.plan.top);
+    const float* sums = a.at<const float>(a.plan.sum);
+    float top = -3e38f;
+    for (int p = threadIdx.x; p < slices; p += kClassThreads) top = fmaxf(top, tops[p * padded + t]);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
+    if (lane == 0) room[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
+    __syncthreads();
+    float sum = 0.0f;
+    for (int p = threadIdx.x; p < slices; p += kClassThreads) sum += sums[p * padded + t] * exp2f(tops[p * padded + t] - top);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+    if (lane == 0) room[wave] = sum;
+    __syncthreads();
+    sum = (room[0] + room[1]) + (room[2] + room[3]);
+    const float lse = (top + log2f(sum)) * kLn2;
+    if (a.mean) {
+        const float* parts = a.at<const float>(a.plan.mean_parts);
+        for (int d = threadIdx.x; d < a.s.D; d += kClassThreads) {
+            float e = 0.0f;
+            for (int p = 0; p < slices; ++p) e += parts[(p * padded + t) * depth + d] * exp2f(tops[p * padded + t] - top);
+            a.mean[t * a.s.D + d] = e / sum / u.w;
+        }
+    }
+    const Elem* h = static_cast<const Elem*>(a.h) + t * a.h_stride;
+    for (int j = wave; j < a.s.K; j += kClassWaves) {
+        const int id = slot_id[j];
+        const float q = slot_q[j];
+        if (id < 0 || q == 0.0f) continue;
+        float dot = 0.0f;
+        if (id < a.s.V)
+            for (int d = lane; d < a.s.D; d += 64) dot += value(h[d]) * value(static_cast<const Elem*>(a.w)[id * a.w_stride + d]);
+        else dot = __builtin_nanf("");                  // a class that there is not
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) dot += __shfl_xor(dot, d);
+        if (lane == 0) slot_loss[j] = q * (slot_log[j] + (lse - dot * a.scale));
+    }
+    __syncthreads();
+    if (wave == 0) {
+        float l = lane < a.s.K ? slot_loss[lane] : 0.0f;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
+        if (lane == 0) { a.loss[t] = l; a.lse[t] = lse; }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// gradients
+// ---------------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void store_elem(void* p, int64_t i, float x) {
+    if constexpr (kKind == 0) static_cast<float*>(p)[i] = x;
+    else static_cast<uint16_t*>(p)[i] = (uint16_t)(pack2(x, 0.0f) & 0xffff);
+}
+__device__ __forceinline__ void store4(void* p, int64_t i, f32x4 x) {
+    if constexpr (kKind == 0) __builtin_memcpy(static_cast<float*>(p) + i, &x, 16);
+    else {
+        const u32x2 v = {pack2(x[0], x[1]), pack2(x[2], x[3])};
+        __builtin_memcpy(static_cast<uint16_t*>(p) + i, &v, 8);
+    }
+}
+
+// grad_h[t] = g * scale * (mean[t] - sum_j q_j w[id_j]), one workgroup per row.
+__global__ __launch_bounds__(kClassThreads) void class_pull_kernel(ClassArgs a) {
+    __shared__ float slot_q[64];
+    __shared__ int slot_id[64], alive;
+    const int64_t t = blockIdx.x;
+    const int lane = threadIdx.x & 63;
+    if (threadIdx.x < 64) {
+        int id;
+        float log_weight;
+        const float q = slot_weight(a, t, lane, id, log_weight);
+        if (lane < a.s.K) { slot_q[lane] = q; slot_id[lane] = q != 0.0f && id < a.s.V ? id : -1; }
+        const bool some = __any(id >= 0);
+        if (lane == 0) alive = some;
+    }
+    __syncthreads();
+    const float g = alive ? a.grad_loss[t] * a.scale : 0.0f;
+    for (int d = threadIdx.x; d < a.s.D; d += kClassThreads) {
+        float e = alive ? a.mean_in[t * a.s.D + d] : 0.0f;
+        for (int j = 0; j < a.s.K; ++j)
+            if (slot_id[j] >= 0) e -= slot_q[j] * value(static_cast<const Elem*>(a.w)[slot_id[j] * a.w_stride + d]);
+        store_elem(a.grad_h, t * a.s.D + d, alive ? g * e : 0.0f);
+    }
+}
+
+// A wave holds 32 classes, the rows stream by:
+//   grad_w[v] = scale * sum_t g_t (p[t,v] - sum over t's slots j that name v of q_j) h[t]
+template <int DP, int WY>
+__global__ __launch_bounds__(kClassThreads) void class_gradient_kernel(ClassArgs a, int64_t padded) {
+    constexpr int NB = WY == 4 ? 4 : 2, MY = NB / WY, WX = kClassWaves / WY;
+    using T = Tile<DP, NB * kBlock>;
+    __shared__ __align__(16) uint16_t lds[2][NS * T::kPlane];
+    __shared__ __align__(16) float starts[2][NB * kBlock];
+    __shared__ float cells[kClassWaves][kBlock * kBlock];
+    __shared__ float room[kClassWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = wave % WX, y = wave / WX;
+    const int64_t part = blockIdx.x % a.cut.parts, group = blockIdx.x / a.cut.parts;
+    const Units u = units(a, room, true);
+    const float to_log2 = a.scale * kLog2e / u.h / u.w;
+    const int64_t first = a.cut.tiles * part / a.cut.parts, last = a.cut.tiles * (part + 1) / a.cut.parts;
+    const int64_t v0 = (group * WX + x) * kBlock, v = v0 + (lane & 31);
+    const bool live = v0 < a.s.V;                       // wave-uniform
+    const Elem* w = static_cast<const Elem*>(a.w) + (v < a.s.V ? v : a.s.V - 1) * a.w_stride;
+
+    u32x4 held[DP / 16][NS];
+#pragma unroll
+    for (int ks = 0; ks < DP / 16; ++ks) {
+        const int col = 16 * ks + 8 * (lane >> 5);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) held[ks][n] = u32x4{};
+        if (live && col < a.s.D) planes_of(load8(w, a.s.D, col), u.w, held[ks]);
+    }
+    f32x16 acc[DP / 32];
+#pragma unroll
+    for (auto& f : acc) f = f32x16{};
+    float* cell = cells[wave];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) cell[row_of(i, lane) * kBlock + (lane & 31)] = 0.0f;
+
+    const uint16_t* planes = a.at<const uint16_t>(a.plan.rows);
+    const float* start = a.at<const float>(a.plan.start);
+    const float* pull = a.at<const float>(a.plan.pull);
+    typename T::FromPlanes next;
+    float next_start = 0.0f;
+    auto fetch = [&](int64_t it) {
+        next.load(planes, padded, it * NB * kBlock);    // rows are padded to whole tiles
+        if (threadIdx.x < NB * kBlock) next_start = start[it * NB * kBlock + threadIdx.x];
+    };
+    if (first < last) fetch(first);
+    for (int64_t it = first; it < last; ++it) {
+        const int half = (it - first) & 1;
+        uint16_t* tile = lds[half];
+        next.store(tile);
+        if (threadIdx.x < NB * kBlock) starts[half][threadIdx.x] = next_start;
+        __syncthreads();
+        if (it + 1 < last) fetch(it + 1);
+        if (!live) continue;
+#pragma unroll
+        for (int m = 0; m < MY; ++m) {
+            const int b = y * MY + m;
+            const int64_t t0 = (it * NB + b) * kBlock;
+            if (t0 >= a.s.T) continue;
+            f32x16 score;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 s = *reinterpret_cast<const f32x4*>(&starts[half][b * kBlock + 8 * i + 4 * (lane >> 5)]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) score[4 * i + j] = s[j];
+            }
+#pragma unroll
+            for (int ks = 0; ks < DP / 16; ++ks) {
+                u32x4 f[NS];
+                T::rows(tile, b, ks, lane, f);
+                score = matmul(f, held[ks], score);
+            }
+            float p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(score[i] * to_log2);
+            const uint32_t signs = a.at<const uint32_t>(a.plan.signs)[t0 / kBlock];
+            if (signs) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) if (signs >> row_of(i, lane) & 1) p[i] = -p[i];
+            }
+            // slots of these rows that name one of these classes
+            const int n = (int)((a.s.T - t0 < kBlock ? a.s.T - t0 : kBlock) * a.s.K);
+            bool hit = false;
+            for (int e = lane; e < n; e += 64) {
+                const int64_t c = a.ids[t0 * a.s.K + e] - v0;
+                if (c >= 0 && c < kBlock) { atomicAdd(&cell[e / a.s.K * kBlock + (int)c], pull[t0 * a.s.K + e]); hit = true; }
+            }
+            if (__any(hit)) {
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float& c = cell[row_of(i, lane) * kBlock + (lane & 31)];
+                    p[i] -= c;
+                    c = 0.0f;
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+            u32x4 q[2][NS];
+            operand_of(p, q);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int db = 0; db < DP / 32; ++db) {
+                    u32x4 f[NS];
+                    T::columns(tile, b, s, db, lane, f);
+                    acc[db] = matmul(f, q[s], acc[db]);
+                }
+        }
+    }
+    if (!live) return;
+    const float back = a.scale / u.h / u.g;
+    if (a.cut.slices() > 1) {
+        const int64_t rows = ceil_div(a.s.V, kBlock) * kBlock;
+        float* out = a.at<float>(a.plan.grad_parts) + ((part * WY + y) * rows + v) * DP + 4 * (lane >> 5);
+#pragma unroll
+        for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<f32x4*>(out + 32 * db + 8 * i) =
+                    f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]} * back;
+        return;
+    }
+    if (v >= a.s.V) return;
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int d = 32 * db + 8 * i + 4 * (lane >> 5);
+            const f32x4 g = f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]} * back;
+            if (d + 4 <= a.s.D) store4(a.grad_w, v * a.s.D + d, g);
+            else
+                for (int j = 0; j < 4; ++j) if (d + j < a.s.D) store_elem(a.grad_w, v * a.s.D + d + j, g[j]);
+        }
+}
+
+// Parts of grad_w joined in part order.
+__global__ __launch_bounds__(kClassThreads) void class_join_kernel(ClassArgs a, int depth, int slices) {
+    const int64_t rows = ceil_div(a.s.V, kBlock) * kBlock, n = a.s.V * a.s.D;
+    const float* parts = a.at<const float>(a.plan.grad_parts);
+    for (int64_t i = (int64_t)blockIdx.x * kClassThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kClassThreads) {
+        const int64_t v = i / a.s.D, d = i % a.s.D;
+        float g = 0.0f;
+        for (int p = 0; p < slices; ++p) g += parts[(p * rows + v) * depth + d];
+        store_elem(a.grad_w, i, g);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------------------------------------------
+template <class F> hipError_t with_depth(int depth, F f) {
+    switch (depth) {
+        case 64: f(std::integral_constant<int, 64>{}); break;
+        case 128: f(std::integral_constant<int, 128>{}); break;
+        case 256: f(std::integral_constant<int, 256>{}); break;
+        default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
+hipError_t launch_rows(const ClassArgs& a, bool grad, hipStream_t stream) {
+    const int64_t padded = padded_rows(a.s.T);
+    const int table = kKind == 0 ? kPeaksTable : 0, rows = kKind == 0 ? kPeaksRows : 0, g = kHalf && grad ? kPeaksGrad : 0;
+    if (table + rows + g) class_peaks_kernel<<<table + rows + g, kClassThreads, 0, stream>>>(a, table, rows, g);
+    return with_depth(class_depth(a.s.D), [&](auto dp) {
+        if (padded) class_rows_kernel<dp()><<<padded / kBlock, kClassThreads, 0, stream>>>(a, padded, grad);
+    });
+}
+
+template <int DP, bool MEAN> void launch_forward_cut(const ClassArgs& a, int64_t padded, hipStream_t stream) {
+    const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
+    if (a.cut.wy == 1) class_forward_kernel<DP, 1, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    else if (a.cut.wy == 2) class_forward_kernel<DP, 2, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    else if constexpr (DP * NS <= 256) class_forward_kernel<DP, 4, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
+}
+
+hipError_t forward(ClassArgs a, hipStream_t stream) {
+    const int64_t padded = padded_rows(a.s.T);
+    a.cut = forward_cut(a.s);
+    if (hipError_t e = launch_rows(a, false, stream)) return e;
+    if (hipError_t e = with_depth(class_depth(a.s.D), [&](auto dp) {
+            if (a.mean) launch_forward_cut<dp(), true>(a, padded, stream);
+            else launch_forward_cut<dp(), false>(a, padded, stream);
+        })) return e;
+    class_finish_kernel<<<(unsigned)a.s.T, kClassThreads, 0, stream>>>(a, padded, class_depth(a.s.D), (int)a.cut.slices());
+    return hipGetLastError();
+}
+
+hipError_t gradient(ClassArgs a, hipStream_t stream) {
+    const int64_t padded = padded_rows(a.s.T);
+    if (a.grad_h && a.s.T) {
+        class_pull_kernel<<<(unsigned)a.s.T, kClassThreads, 0, stream>>>(a);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    if (!a.grad_w) return hipSuccess;
+    a.cut = gradient_cut(a.s);
+    if (hipError_t e = launch_rows(a, true, stream)) return e;
+    const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
+    if (hipError_t e = with_depth(class_depth(a.s.D), [&](auto dp) {
+            if (a.cut.wy == 1) class_gradient_kernel<dp(), 1><<<grid, kClassThreads, 0, stream>>>(a, padded);
+            else if (a.cut.wy == 2) class_gradient_kernel<dp(), 2><<<grid, kClassThreads, 0, stream>>>(a, padded);
+            else if constexpr (dp() * NS <= 256) class_gradient_kernel<dp(), 4><<<grid, kClassThreads, 0, stream>>>(a, padded);
+        })) return e;
+    if (a.cut.slices() > 1) {
+        const int64_t n = ceil_div(a.s.V * a.s.D, kClassThreads);
+        class_join_kernel<<<(unsigned)(n < 4096 ? n : 4096), kClassThreads, 0, stream>>>(a, class_depth(a.s.D), (int)a.cut.slices());
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+#endif
+
+}  // namespace fsa
