@@ -715,7 +715,7 @@ def fsa_wmean_bwd(grad_out: torch.Tensor, ids1: torch.Tensor, w1: torch.Tensor,
 # ----------------------------------------------------------------------------------------
 # losses over many classes
 # ----------------------------------------------------------------------------------------
-FSA_CLASS_DMAX = 256
+FSA_CLASS_DMAX = 1024
 
 
 def _rows(t: torch.Tensor, name: str) -> int:

@@ -12,8 +12,9 @@ namespace fsa {
 //              running mean of the table's rows under the softmax
 //   gradient   waves hold classes, the rows stream by: the scores again, their gradients, a class's gradient row
 // Each splits the streamed side over `parts` of the grid, joined in part order by a second launch.
-constexpr int kClassDepths[] = {64, 128, 256};          // depths that rows are padded to in LDS and registers
-constexpr int kClassMaxDepth = 256;
+//
+// Rows of up to 128 (fp32) or 256 elements are held by one wave each ("narrow"); longer ones by the four waves of a
+// workgroup, a quarter of the elements each ("wide"), whose partial scores meet in LDS.
 constexpr int kBlock = 32;                              // rows and classes come in blocks of one matrix instruction
 constexpr int kClassThreads = 256;
 constexpr int kClassWaves = kClassThreads / 64;
@@ -24,51 +25,61 @@ struct ClassShape {
     int K;                                              // slots a row
 };
 
-// How one launch is cut: wx waves of a workgroup side by side over held blocks, wy over streamed ones.
-struct ClassCut {
-    int wx, wy;
-    int64_t groups;                                     // workgroups over held blocks
-    int64_t tiles;                                      // streamed tiles of blocks_per_tile blocks
-    int64_t parts;                                      // shares of the streamed tiles in the grid
-    constexpr int64_t slices() const { return parts * wy; }       // partial results of every held row
-};
-
-inline int class_planes(int kind) { return kind == 0 ? 2 : 1; }          // 16-bit planes that hold an element
-inline int class_depth(int64_t D) {
-    for (int d : kClassDepths) if (D <= d) return d;
+constexpr int class_planes(int kind) { return kind == 0 ? 2 : 1; }       // 16-bit planes that hold an element
+constexpr bool narrow_depth(int depth, int kind) { return depth * class_planes(kind) <= 256; }
+inline int class_depth(int64_t D) {                     // what rows are padded to; 0: too long
+    constexpr int depths[] = {64, 128, 256, 384, 640, 1024};
+    for (int d : depths) if (D <= d) return d;
     return 0;
 }
 constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t padded_rows(int64_t T) { return ceil_div(T, 4 * kBlock) * 4 * kBlock; }
+
+// How one launch is cut: wx waves of a workgroup side by side over held blocks, wy over streamed ones (narrow).
+struct ClassCut {
+    int wx, wy;
+    int64_t groups;                                     // workgroups over held blocks
+    int64_t tiles;                                      // streamed tiles
+    int64_t parts;                                      // shares of the streamed tiles in the grid
+    constexpr int64_t slices() const { return parts * wy; }   // partial results of every held row
+};
+
 inline int blocks_per_tile(int wy) { return wy == 4 ? 4 : 2; }
 
-inline ClassCut cut_of(int64_t held, int64_t streamed, int depth, int planes, int64_t most_parts) {
+inline int64_t parts_for(int64_t groups, int64_t tiles, int64_t workgroups, int64_t most) {
+    int64_t want = ceil_div(workgroups, groups);
+    if (want >= 8) want = want / 8 * 8;                 // shares of one table range meet on one XCD's L2
+    if (want > most) want = most;
+    if (want > tiles) want = tiles;
+    return want < 1 ? 1 : want;
+}
+inline ClassCut cut_of(int64_t held, int64_t streamed, int depth, int kind, int64_t most_parts) {
     ClassCut c;
     const int64_t blocks = ceil_div(held, kBlock);
+    if (!narrow_depth(depth, kind)) {
+        c.wx = 1; c.wy = 1;
+        c.groups = blocks;
+        c.tiles = ceil_div(streamed, kBlock);
+        c.parts = parts_for(c.groups, c.tiles, 512, most_parts);
+        return c;
+    }
     c.wy = blocks >= 4 ? 1 : blocks >= 2 ? 2 : 4;
-    if (c.wy == 4 && depth * planes > 256) c.wy = 2;    // 128 rows of LDS tile would not fit twice
     c.wx = kClassWaves / c.wy;
     c.groups = ceil_div(blocks, c.wx);
     c.tiles = ceil_div(streamed, (int64_t)blocks_per_tile(c.wy) * kBlock);
-    int64_t want = ceil_div(1024, c.groups);            // workgroups of the launch: four to a CU
-    if (want >= 8) want = want / 8 * 8;                 // shares of one table range meet on one XCD's L2
-    c.parts = want < 1 ? 1 : want;
-    if (c.parts > most_parts) c.parts = most_parts;
-    if (c.parts > c.tiles) c.parts = c.tiles < 1 ? 1 : c.tiles;
+    c.parts = parts_for(c.groups, c.tiles, 1024, most_parts);
     return c;
 }
-inline ClassCut forward_cut(const ClassShape& s) {
-    return cut_of(s.T, s.V, class_depth(s.D), class_planes(s.kind), 1024);
-}
+inline ClassCut forward_cut(const ClassShape& s) { return cut_of(s.T, s.V, class_depth(s.D), s.kind, 1024); }
 inline ClassCut gradient_cut(const ClassShape& s) {
-    ClassCut c = cut_of(s.V, s.T, class_depth(s.D), class_planes(s.kind), 64);
+    ClassCut c = cut_of(s.V, s.T, class_depth(s.D), s.kind, 64);
     if (c.groups >= 512) c.parts = 1;                   // the classes fill the chip by themselves
     return c;
 }
 
 // Byte offsets into the caller's workspace.
 struct ClassPlan {
-    size_t peaks, rows, top, sum, mean_parts, loss, start, signs, pull, mean, grad_parts, bytes;
+    size_t peaks, rows, top, sum, mean_parts, norm, loss, start, signs, pull, mean, grad_parts, bytes;
 };
 constexpr int kPeaksTable = 512, kPeaksRows = 64, kPeaksGrad = 64, kPeaks = kPeaksTable + kPeaksRows + kPeaksGrad;
 
@@ -80,10 +91,12 @@ inline ClassPlan plan_of(const ClassShape& s, bool forward, bool want_mean, bool
     p.peaks = room(kPeaks * 4);
     p.rows = room(T * depth * 2 * class_planes(s.kind));
     if (forward) {
-        const size_t slices = forward_cut(s).slices();
-        p.top = room(slices * T * 4);
-        p.sum = room(slices * T * 4);
+        const bool narrow = narrow_depth((int)depth, s.kind);
+        const size_t slices = forward_cut(s).slices(), stats = narrow ? slices : slices * kClassWaves;
+        p.top = room(stats * T * 4);
+        p.sum = room(stats * T * 4);
         if (want_mean) p.mean_parts = room(slices * T * depth * 4);
+        if (want_mean && !narrow) p.norm = room(T * 4);
     }
     if (forward && want_mean) {                         // a backward that computes the mean again keeps it here
         p.mean = room((size_t)s.T * s.D * 4);

@@ -492,7 +492,7 @@ __global__ __launch_bounds__(kClassThreads) void class_forward_kernel(ClassArgs 
 }
 
 // One workgroup per row: the parts joined, the row's slots scored again (fp32 sums of the elements themselves), its loss.
-__global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a, int64_t padded, int depth, int slices) {
+__global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a, int64_t padded, int depth, int slices, bool wide) {
     __shared__ float room[kClassWaves], slot_q[64], slot_log[64], slot_loss[64];
     __shared__ int slot_id[64];
     const int64_t t = blockIdx.x;
@@ -510,8 +510,11 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
     const bool lives = room[0] != 0.0f;
     __syncthreads();
     if (!lives) {                                       // nothing of the row is used, whatever it holds
-        if (threadIdx.x == 0) { a.loss[t] = 0.0f; a.lse[t] = 0.0f; }
-        if (a.mean) for (int d = threadIdx.x; d < a.s.D; d += kClassThreads) a.mean[t * a.s.D + d] = 0.0f;
+        if (threadIdx.x == 0) {
+            a.loss[t] = 0.0f; a.lse[t] = 0.0f;
+            if (a.mean && wide) a.at<float>(a.plan.norm)[t] = __builtin_inff();
+        }
+        if (a.mean && !wide) for (int d = threadIdx.x; d < a.s.D; d += kClassThreads) a.mean[t * a.s.D + d] = 0.0f;
         return;
     }
     const float* tops = a.at<const float>(a.plan.top);
@@ -532,7 +535,9 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
     __syncthreads();
     sum = (room[0] + room[1]) + (room[2] + room[3]);
     const float lse = (top + log2f(sum)) * kLn2;
-    if (a.mean) {
+    if (a.mean && wide) {
+        if (threadIdx.x == 0) a.at<float>(a.plan.norm)[t] = top + log2f(sum) - kLift;
+    } else if (a.mean) {
         const float* parts = a.at<const float>(a.plan.mean_parts);
         for (int d = threadIdx.x; d < a.s.D; d += kClassThreads) {
             float e = 0.0f;
@@ -734,16 +739,235 @@ __global__ __launch_bounds__(kClassThreads) void class_gradient_kernel(ClassArgs
         }
 }
 
-// Parts of grad_w joined in part order.
-__global__ __launch_bounds__(kClassThreads) void class_join_kernel(ClassArgs a, int depth, int slices) {
-    const int64_t rows = ceil_div(a.s.V, kBlock) * kBlock, n = a.s.V * a.s.D;
-    const float* parts = a.at<const float>(a.plan.grad_parts);
-    for (int64_t i = (int64_t)blockIdx.x * kClassThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kClassThreads) {
-        const int64_t v = i / a.s.D, d = i % a.s.D;
-        float g = 0.0f;
-        for (int p = 0; p < slices; ++p) g += parts[(p * rows + v) * depth + d];
-        store_elem(a.grad_w, i, g);
+// ---------------------------------------------------------------------------------------------------------------
+// wide rows: the four waves of a workgroup hold a quarter of the elements each
+// ---------------------------------------------------------------------------------------------------------------
+// A wave's quarter of 32 streamed rows in LDS, its own: no other wave reads it.  Rows lie 8k + 2 chunks apart, every
+// second four of them one chunk on: the reads of 8 rows of one chunk and of 4 rows of two chunks fall on different banks.
+template <int Q>
+struct Quarter {
+    static constexpr int kChunks = Q / 8, kStride = ((kChunks + 1 + 5) / 8 * 8 + 2) * 8;   // elements from row to row
+    static constexpr int kPlane = kBlock * kStride, kEach = kBlock * kChunks / 64;
+    static_assert(kStride >= Q + 8 && (kBlock * kChunks) % 64 == 0, "a row and its shift fit, lanes share rows evenly");
+    static __device__ __forceinline__ int place(int r, int c) { return r * kStride + (c + ((r >> 2) & 1)) * 8; }
+    static __device__ __forceinline__ void rows(const uint16_t* lds, int ks, int lane, u32x4 (&out)[NS]) {
+#pragma unroll
+        for (int n = 0; n < NS; ++n)
+            out[n] = *reinterpret_cast<const u32x4*>(lds + n * kPlane + place(lane & 31, 2 * ks + (lane >> 5)));
     }
+    static __device__ __forceinline__ void columns(const uint16_t* lds, int s, int db, int lane, u32x4 (&out)[NS]) {
+        const int i = lane & 15, r = 16 * s + 4 * (lane >> 5) + (i >> 2), c = 4 * db + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) {
+            const uint16_t* p = lds + n * kPlane + place(r, c) + (i & 1) * 4;
+            const u32x2 a = read_transposed(p), z = read_transposed(p + 8 * kStride);
+            out[n] = u32x4{a[0], a[1], z[0], z[1]};
+        }
+    }
+};
+
+enum WideMode { kStats, kMean, kGradient };
+
+// kStats: running maximum and sum of every held row of h, one pair per wave (a quarter of the streamed classes each).
+// kMean: sum of the table's rows under 2^(score - norm).  kGradient: as the narrow kernel.
+template <int Q, WideMode MODE>
+__global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, int64_t padded) {
+    using S = Quarter<Q>;
+    constexpr int DEPTH = Q * kClassWaves;
+    __shared__ __align__(16) uint16_t quarters[kClassWaves][NS * S::kPlane];
+    constexpr int MEETS = MODE == kStats && Q * NS < 512 ? 2 : 1;      // one more barrier a tile where only one fits
+    __shared__ __align__(16) f32x4 partial[MEETS][kClassWaves][4][64];
+    __shared__ __align__(16) u32x2 shared_p[MODE == kStats ? 1 : NS][2][64][2];
+    __shared__ float cells[MODE == kGradient ? kBlock * kBlock : 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col0 = wave * Q;
+    const int64_t part = blockIdx.x % a.cut.parts, group = blockIdx.x / a.cut.parts;
+    const Units u = units(a, reinterpret_cast<float*>(partial), MODE == kGradient);
+    const float to_log2 = a.scale * kLog2e / u.h / u.w;
+    const int64_t first = a.cut.tiles * part / a.cut.parts, last = a.cut.tiles * (part + 1) / a.cut.parts;
+    const int64_t x0 = group * kBlock, x = x0 + (lane & 31);
+    const Elem* w = static_cast<const Elem*>(a.w);
+    const uint16_t* planes = a.at<const uint16_t>(a.plan.rows);
+    uint16_t* lds = quarters[wave];
+
+    u32x4 held[Q / 16][NS];
+#pragma unroll
+    for (int ks = 0; ks < Q / 16; ++ks) {
+        const int col = col0 + 16 * ks + 8 * (lane >> 5);
+        if constexpr (MODE == kGradient) {
+#pragma unroll
+            for (int n = 0; n < NS; ++n) held[ks][n] = u32x4{};
+            if (col < a.s.D) planes_of(load8(w + (x < a.s.V ? x : a.s.V - 1) * a.w_stride, a.s.D, col), u.w, held[ks]);
+        } else {
+#pragma unroll
+            for (int n = 0; n < NS; ++n) held[ks][n] = *reinterpret_cast<const u32x4*>(planes + ((int64_t)n * padded + x) * DEPTH + col);
+        }
+    }
+    if constexpr (MODE == kGradient) {
+        for (int i = threadIdx.x; i < kBlock * kBlock; i += kClassThreads) cells[i] = 0.0f;
+        __syncthreads();
+    }
+    const float norm = MODE == kMean && x < a.s.T ? a.at<const float>(a.plan.norm)[x] : __builtin_inff();
+    float ref = -1e30f, sum = 0.0f;
+    f32x16 acc[MODE == kStats ? 1 : Q / 32];
+#pragma unroll
+    for (auto& f : acc) f = f32x16{};
+
+    // the next tile's quarter: rows of the table as they are, or planes
+    struct { Eight e[MODE == kGradient ? 1 : S::kEach]; u32x4 p[MODE == kGradient ? NS : 1][MODE == kGradient ? S::kEach : 1]; } next;
+    f32x4 next_start = {};
+    auto fetch = [&](int64_t it) {
+#pragma unroll
+        for (int i = 0; i < S::kEach; ++i) {
+            const int q = i * 64 + lane, r = q / S::kChunks, c = q % S::kChunks;
+            const int64_t row = it * kBlock + r;
+            if constexpr (MODE == kGradient) {
+#pragma unroll
+                for (int n = 0; n < NS; ++n)
+                    next.p[n][i] = *reinterpret_cast<const u32x4*>(planes + ((int64_t)n * padded + row) * DEPTH + col0 + c * 8);
+            } else next.e[i] = load8(w + (row < a.s.V ? row : a.s.V - 1) * a.w_stride, a.s.D, col0 + c * 8);
+        }
+        if constexpr (MODE == kGradient)
+            next_start = *reinterpret_cast<const f32x4*>(a.at<const float>(a.plan.start) + it * kBlock + 8 * wave + 4 * (lane >> 5));
+    };
+    if (first < last) fetch(first);
+    for (int64_t it = first; it < last; ++it) {
+#pragma unroll
+        for (int i = 0; i < S::kEach; ++i) {
+            const int q = i * 64 + lane, r = q / S::kChunks, c = q % S::kChunks;
+            u32x4 p[NS];
+            if constexpr (MODE == kGradient) {
+#pragma unroll
+                for (int n = 0; n < NS; ++n) p[n] = next.p[n][i];
+            } else planes_of(next.e[i], u.w, p);
+#pragma unroll
+            for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(lds + n * S::kPlane + S::place(r, c)) = p[n];
+        }
+        const f32x4 start = next_start;
+        __builtin_amdgcn_wave_barrier();
+        if (it + 1 < last) fetch(it + 1);
+        f32x16 score = {};
+#pragma unroll
+        for (int ks = 0; ks < Q / 16; ++ks) {
+            u32x4 f[NS];
+            S::rows(lds, ks, lane, f);
+            score = matmul(f, held[ks], score);
+        }
+        auto& meet = partial[MEETS == 2 ? (it - first) & 1 : 0];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) meet[wave][i][lane] = f32x4{score[4 * i], score[4 * i + 1], score[4 * i + 2], score[4 * i + 3]};
+        const int64_t y0 = it * kBlock;
+        if constexpr (MODE == kGradient) {              // slots of these rows that name one of these classes
+            const int n = (int)((a.s.T - y0 < kBlock ? a.s.T - y0 : kBlock) * a.s.K);
+            for (int e = threadIdx.x; e < n; e += kClassThreads) {
+                const int64_t c = a.ids[y0 * a.s.K + e] - x0;
+                if (c >= 0 && c < kBlock) atomicAdd(&cells[e / a.s.K * kBlock + (int)c], a.at<const float>(a.plan.pull)[y0 * a.s.K + e]);
+            }
+        }
+        __syncthreads();
+        f32x4 z = (meet[0][wave][lane] + meet[1][wave][lane]) + (meet[2][wave][lane] + meet[3][wave][lane]);   // rows 8*wave + 4*(lane/32) + j
+        const int y = 8 * wave + 4 * (lane >> 5);
+        if (MODE != kGradient && y0 + kBlock > a.s.V)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (y0 + y + j >= a.s.V) z[j] = -__builtin_inff();
+        if constexpr (MODE == kStats) {
+            z *= to_log2;
+            const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
+            if (__any(top > ref + 8.0f)) {
+                const float to = fmaxf(ref, top);
+                sum *= exp2f(ref - to);
+                ref = to;
+            }
+            float e[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(z[j] - ref);
+            sum += (e[0] + e[1]) + (e[2] + e[3]);
+            if constexpr (MEETS == 1) __syncthreads();
+        } else {
+            float p[4];
+            if constexpr (MODE == kMean) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(z[j], to_log2, -norm));
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f((z[j] + start[j]) * to_log2);
+                const uint32_t signs = a.at<const uint32_t>(a.plan.signs)[it];
+                if (signs) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) if (signs >> (y + j) & 1) p[j] = -p[j];
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float& c = cells[(y + j) * kBlock + (lane & 31)];
+                    p[j] -= c;
+                    if (c != 0.0f) c = 0.0f;
+                }
+            }
+            const uint32_t p0 = pack2(p[0], p[1]), p1 = pack2(p[2], p[3]);
+            shared_p[0][wave >> 1][lane][wave & 1] = u32x2{p0, p1};
+            if constexpr (NS == 2)
+                shared_p[1][wave >> 1][lane][wave & 1] = u32x2{pack2(p[0] - low2(p0), p[1] - high2(p0)), pack2(p[2] - low2(p1), p[3] - high2(p1))};
+            __syncthreads();
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                u32x4 b[NS];
+#pragma unroll
+                for (int n = 0; n < NS; ++n) b[n] = *reinterpret_cast<const u32x4*>(&shared_p[n][s][lane][0]);
+#pragma unroll
+                for (int db = 0; db < Q / 32; ++db) {
+                    u32x4 f[NS];
+                    S::columns(lds, s, db, lane, f);
+                    acc[db] = matmul(f, b, acc[db]);
+                }
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    if constexpr (MODE == kStats) {                     // both halves of the wave hold a row's classes
+        const float other = __shfl_xor(ref, 32), to = fmaxf(ref, other);
+        sum = sum * exp2f(ref - to);
+        sum += __shfl_xor(sum, 32);
+        const int64_t at = (part * kClassWaves + wave) * padded + x;
+        if (lane < 32) {
+            a.at<float>(a.plan.top)[at] = to;
+            a.at<float>(a.plan.sum)[at] = sum;
+        }
+    } else {
+        const float back = MODE == kGradient ? a.scale / u.h / u.g : exp2f(-kLift) / u.w;
+        const int64_t rows = MODE == kGradient ? ceil_div(a.s.V, kBlock) * kBlock : padded;
+        const bool joined = MODE == kMean || a.cut.parts > 1;
+        float* out = a.at<float>(MODE == kGradient ? a.plan.grad_parts : a.plan.mean_parts);
+#pragma unroll
+        for (int db = 0; db < Q / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = col0 + 32 * db + 8 * i + 4 * (lane >> 5);
+                const f32x4 g = f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]} * back;
+                if (joined) *reinterpret_cast<f32x4*>(out + (part * rows + x) * DEPTH + d) = g;
+                else if (x < a.s.V) {
+                    if (d + 4 <= a.s.D) store4(a.grad_w, x * a.s.D + d, g);
+                    else
+                        for (int j = 0; j < 4; ++j) if (d + j < a.s.D) store_elem(a.grad_w, x * a.s.D + d + j, g[j]);
+                }
+            }
+    }
+}
+
+// Parts of a result of n rows, `rows` of them in a part, joined in part order.
+template <class Out>
+__global__ __launch_bounds__(kClassThreads) void class_join_kernel(const float* parts, Out* out, int64_t n, int64_t D, int64_t rows,
+                                                                    int depth, int slices) {
+    for (int64_t i = (int64_t)blockIdx.x * kClassThreads + threadIdx.x; i < n * D; i += (int64_t)gridDim.x * kClassThreads) {
+        const int64_t r = i / D, d = i % D;
+        float g = 0.0f;
+        for (int p = 0; p < slices; ++p) g += parts[(p * rows + r) * depth + d];
+        if constexpr (sizeof(Out) == 4) out[i] = g;
+        else store_elem(out, i, g);
+    }
+}
+template <class Out>
+void join(const float* parts, Out* out, int64_t n, int64_t D, int64_t rows, int depth, int slices, hipStream_t stream) {
+    const int64_t grid = ceil_div(n * D, kClassThreads);
+    class_join_kernel<Out><<<(unsigned)(grid < 4096 ? grid : 4096), kClassThreads, 0, stream>>>(parts, out, n, D, rows, depth, slices);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -754,6 +978,9 @@ template <class F> hipError_t with_depth(int depth, F f) {
         case 64: f(std::integral_constant<int, 64>{}); break;
         case 128: f(std::integral_constant<int, 128>{}); break;
         case 256: f(std::integral_constant<int, 256>{}); break;
+        case 384: f(std::integral_constant<int, 384>{}); break;
+        case 640: f(std::integral_constant<int, 640>{}); break;
+        case 1024: f(std::integral_constant<int, 1024>{}); break;
         default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
@@ -768,27 +995,42 @@ hipError_t launch_rows(const ClassArgs& a, bool grad, hipStream_t stream) {
     });
 }
 
-template <int DP, bool MEAN> void launch_forward_cut(const ClassArgs& a, int64_t padded, hipStream_t stream) {
+template <int DP, bool MEAN> void launch_forward(const ClassArgs& a, int64_t padded, hipStream_t stream) {
     const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
-    if (a.cut.wy == 1) class_forward_kernel<DP, 1, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    if constexpr (!narrow_depth(DP, kKind)) class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    else if (a.cut.wy == 1) class_forward_kernel<DP, 1, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
     else if (a.cut.wy == 2) class_forward_kernel<DP, 2, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
-    else if constexpr (DP * NS <= 256) class_forward_kernel<DP, 4, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    else class_forward_kernel<DP, 4, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
+}
+template <int DP> void launch_gradient(const ClassArgs& a, int64_t padded, hipStream_t stream) {
+    const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
+    if constexpr (!narrow_depth(DP, kKind)) class_wide_kernel<DP / kClassWaves, kGradient><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    else if (a.cut.wy == 1) class_gradient_kernel<DP, 1><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    else if (a.cut.wy == 2) class_gradient_kernel<DP, 2><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    else class_gradient_kernel<DP, 4><<<grid, kClassThreads, 0, stream>>>(a, padded);
 }
 
 hipError_t forward(ClassArgs a, hipStream_t stream) {
     const int64_t padded = padded_rows(a.s.T);
+    const int depth = class_depth(a.s.D);
+    const bool wide = !narrow_depth(depth, kKind);
     a.cut = forward_cut(a.s);
+    const int slices = (int)a.cut.slices();
     if (hipError_t e = launch_rows(a, false, stream)) return e;
-    if (hipError_t e = with_depth(class_depth(a.s.D), [&](auto dp) {
-            if (a.mean) launch_forward_cut<dp(), true>(a, padded, stream);
-            else launch_forward_cut<dp(), false>(a, padded, stream);
+    if (hipError_t e = with_depth(depth, [&](auto dp) {
+            if (a.mean && !wide) launch_forward<dp(), true>(a, padded, stream);
+            else launch_forward<dp(), false>(a, padded, stream);
         })) return e;
-    class_finish_kernel<<<(unsigned)a.s.T, kClassThreads, 0, stream>>>(a, padded, class_depth(a.s.D), (int)a.cut.slices());
+    class_finish_kernel<<<(unsigned)a.s.T, kClassThreads, 0, stream>>>(a, padded, depth, wide ? slices * kClassWaves : slices, wide);
+    if (!a.mean || !wide) return hipGetLastError();
+    if (hipError_t e = with_depth(depth, [&](auto dp) { launch_forward<dp(), true>(a, padded, stream); })) return e;
+    join(a.at<const float>(a.plan.mean_parts), a.mean, a.s.T, a.s.D, padded, depth, slices, stream);
     return hipGetLastError();
 }
 
 hipError_t gradient(ClassArgs a, hipStream_t stream) {
     const int64_t padded = padded_rows(a.s.T);
+    const int depth = class_depth(a.s.D);
     if (a.grad_h && a.s.T) {
         class_pull_kernel<<<(unsigned)a.s.T, kClassThreads, 0, stream>>>(a);
         if (hipError_t e = hipGetLastError()) return e;
@@ -796,16 +1038,10 @@ hipError_t gradient(ClassArgs a, hipStream_t stream) {
     if (!a.grad_w) return hipSuccess;
     a.cut = gradient_cut(a.s);
     if (hipError_t e = launch_rows(a, true, stream)) return e;
-    const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
-    if (hipError_t e = with_depth(class_depth(a.s.D), [&](auto dp) {
-            if (a.cut.wy == 1) class_gradient_kernel<dp(), 1><<<grid, kClassThreads, 0, stream>>>(a, padded);
-            else if (a.cut.wy == 2) class_gradient_kernel<dp(), 2><<<grid, kClassThreads, 0, stream>>>(a, padded);
-            else if constexpr (dp() * NS <= 256) class_gradient_kernel<dp(), 4><<<grid, kClassThreads, 0, stream>>>(a, padded);
-        })) return e;
-    if (a.cut.slices() > 1) {
-        const int64_t n = ceil_div(a.s.V * a.s.D, kClassThreads);
-        class_join_kernel<<<(unsigned)(n < 4096 ? n : 4096), kClassThreads, 0, stream>>>(a, class_depth(a.s.D), (int)a.cut.slices());
-    }
+    if (hipError_t e = with_depth(depth, [&](auto dp) { launch_gradient<dp()>(a, padded, stream); })) return e;
+    if (a.cut.slices() > 1)
+        join(a.at<const float>(a.plan.grad_parts), static_cast<Elem*>(a.grad_w), a.s.V, a.s.D, ceil_div(a.s.V, kBlock) * kBlock,
+             depth, (int)a.cut.slices(), stream);
     return hipGetLastError();
 }
 

@@ -47,7 +47,8 @@ def compare(fsa, op, dtype, h, w, ids, logits, g, temperature=1.0, scale=1.0):
 
 
 SIZES = [(1, 1, 1), (1, 47, 128), (2, 33, 3), (5, 1000, 64), (31, 64, 100), (32, 32, 32), (33, 129, 65), (64, 31, 128),
-         (65, 4097, 37), (127, 500, 256), (128, 2, 255), (129, 96, 129), (200, 3001, 96), (300, 65, 200), (513, 129, 16)]
+         (65, 4097, 37), (127, 500, 256), (128, 2, 255), (129, 96, 129), (200, 3001, 96), (300, 65, 200), (513, 129, 16),
+         (1, 1, 257), (33, 700, 602), (70, 95, 384), (65, 33, 1024), (129, 257, 640), (40, 1500, 385)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
@@ -59,7 +60,7 @@ def test_cross_entropy(fsa, dtype, T, V, D):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("T,V,D,K", [(1, 1, 8, 1), (3, 70, 20, 64), (40, 64, 64, 64), (65, 1000, 100, 10), (130, 2049, 128, 33),
-                                     (257, 200, 250, 5), (1, 5000, 128, 17)])
+                                     (257, 200, 250, 5), (1, 5000, 128, 17), (70, 300, 602, 50), (33, 64, 300, 64), (65, 40, 1001, 3)])
 def test_distillation(fsa, dtype, T, V, D, K):
     h, w, ids, logits, g = inputs("distill", dtype, T, V, D, K, seed=T + V + K)
     compare(fsa, "distill", dtype, h, w, ids, logits, g, temperature=2.0, scale=1.5)
