@@ -390,7 +390,7 @@ int fsa_wmean_bwd_ws(const float* grad_out, const float* grad_h1,
  * 22 bits.  Every result is a function of the arguments alone: no atomics whose order could change it (two slots of a row
  * that name one class aside).
  */
-enum { FSA_CLASS_TMAX = 1 << 23, FSA_CLASS_VMAX = 1 << 30, FSA_CLASS_DMAX = 1024 };
+enum { FSA_CLASS_TMAX = 1 << 23, FSA_CLASS_VMAX = 1 << 27, FSA_CLASS_DMAX = 1024 };
 
 int64_t fsa_class_fwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_mean);
 /* with_mean: grad_h is wanted and no mean is given; with_grad_w: grad_w is wanted.  0 for sizes that the calls refuse. */

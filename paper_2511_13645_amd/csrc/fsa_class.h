@@ -33,7 +33,7 @@ inline int class_depth(int64_t D) {                     // what rows are padded 
     return 0;
 }
 constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-inline int64_t padded_rows(int64_t T) { return ceil_div(T, 4 * kBlock) * 4 * kBlock; }
+constexpr int64_t padded_rows(int64_t T) { return ceil_div(T, 4 * kBlock) * 4 * kBlock; }
 
 // How one launch is cut: wx waves of a workgroup side by side over held blocks, wy over streamed ones (narrow).
 struct ClassCut {
@@ -77,13 +77,29 @@ inline ClassCut gradient_cut(const ClassShape& s) {
     return c;
 }
 
+// Slots of 32 rows are sorted by the classes that they name, for the gradient: `per` blocks of classes to a bucket, about
+// two buckets to a slot, so that a wave mostly learns from one word that no slot of these rows names one of its classes.
+struct ClassBuckets { int64_t per, count; };
+constexpr int kMostBuckets = 2 * kBlock * 64;
+constexpr ClassBuckets buckets_of(int64_t V, int K) {
+    const int64_t blocks = ceil_div(V, kBlock), per = ceil_div(blocks, 2 * kBlock * K);
+    return {per, ceil_div(blocks, per)};
+}
+
+// Whether the forward first lays the table out as planes of padded rows: one more pass over the table, against rows
+// that the kernel has to read off the 16-byte grid, or to split into planes, once for every workgroup beside it.
+inline bool forward_packs(const ClassShape& s, bool on_grid) {
+    return (s.kind == 0 || !on_grid) && forward_cut(s).groups > 2;
+}
+
 // Byte offsets into the caller's workspace.
 struct ClassPlan {
-    size_t peaks, rows, top, sum, mean_parts, norm, loss, start, signs, pull, mean, grad_parts, bytes;
+    size_t peaks, rows, table, top, sum, mean_parts, norm, loss, start, signs, buckets, slots, mean, grad_parts, bytes;
+    bool packed;                                        // the forward reads the table from planes made for the call
 };
 constexpr int kPeaksTable = 512, kPeaksRows = 64, kPeaksGrad = 64, kPeaks = kPeaksTable + kPeaksRows + kPeaksGrad;
 
-inline ClassPlan plan_of(const ClassShape& s, bool forward, bool want_mean, bool want_grad_w) {
+inline ClassPlan plan_of(const ClassShape& s, bool packed, bool forward, bool want_mean, bool want_grad_w) {
     ClassPlan p{};
     size_t at = 0;
     auto room = [&at](size_t n) { const size_t a = at; at += (n + 255) / 256 * 256; return a; };
@@ -93,6 +109,8 @@ inline ClassPlan plan_of(const ClassShape& s, bool forward, bool want_mean, bool
     if (forward) {
         const bool narrow = narrow_depth((int)depth, s.kind);
         const size_t slices = forward_cut(s).slices(), stats = narrow ? slices : slices * kClassWaves;
+        p.packed = packed;
+        if (packed) p.table = room(padded_rows(s.V) * depth * 2 * class_planes(s.kind));
         p.top = room(stats * T * 4);
         p.sum = room(stats * T * 4);
         if (want_mean) p.mean_parts = room(slices * T * depth * 4);
@@ -106,7 +124,8 @@ inline ClassPlan plan_of(const ClassShape& s, bool forward, bool want_mean, bool
         const ClassCut c = gradient_cut(s);
         p.start = room(T * 4);
         p.signs = room(T / kBlock * 4);
-        p.pull = room(T * s.K * 4);
+        p.buckets = room(T / kBlock * buckets_of(s.V, s.K).count * 4);
+        p.slots = room(T * s.K * 8);
         if (c.slices() > 1) p.grad_parts = room((size_t)c.slices() * ceil_div(s.V, kBlock) * kBlock * depth * 4);
     }
     p.bytes = at;

@@ -33,6 +33,12 @@ int take(fsa::ClassArgs& a, const void* h, int64_t h_stride, const void* w, int6
     return FSA_OK;
 }
 
+// Rows that all start on the 16-byte grid and end on it are read as they are.
+bool packs(const fsa::ClassArgs& a) {
+    const bool on_grid = aligned(a.w, 16) && a.w_stride * elem_bytes(a.s.kind) % 16 == 0 && a.s.D * elem_bytes(a.s.kind) % 16 == 0;
+    return fsa::forward_packs(a.s, on_grid);
+}
+
 int take_room(fsa::ClassArgs& a, void* workspace, int64_t bytes) {
     if (bytes < 0) return FSA_ERR_ARG;
     if ((size_t)bytes < a.plan.bytes || !workspace) return FSA_ERR_WORKSPACE;
@@ -56,7 +62,7 @@ int forward(fsa::ClassArgs& a, float* loss, float* lse, float* mean, void* works
     if (a.s.T > 0 && (!loss || !lse)) return FSA_ERR_NULL;
     if (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(mean, 4)) return FSA_ERR_ALIGN;
     if (a.s.T == 0) return FSA_OK;
-    a.plan = fsa::plan_of(a.s, true, mean != nullptr, false);
+    a.plan = fsa::plan_of(a.s, packs(a), true, mean != nullptr, false);
     if (int rc = take_room(a, workspace, bytes)) return rc;
     a.loss = loss; a.lse = lse; a.mean = mean;
     (void)hipGetLastError();                            // an error that the caller left pending is not this call's
@@ -70,7 +76,7 @@ int backward(fsa::ClassArgs& a, const float* grad_loss, const float* lse, const 
     if (!aligned(grad_loss, 4) || !aligned(lse, 4) || !aligned(mean, 4) || !aligned(grad_h, eb) || !aligned(grad_w, eb))
         return FSA_ERR_ALIGN;
     const bool again = grad_h && !mean && a.s.T > 0;
-    a.plan = fsa::plan_of(a.s, again, again, grad_w != nullptr);
+    a.plan = fsa::plan_of(a.s, again && packs(a), again, again, grad_w != nullptr);
     if (int rc = take_room(a, workspace, bytes)) return rc;
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -85,18 +91,23 @@ int backward(fsa::ClassArgs& a, const float* grad_loss, const float* lse, const 
     return status_of(gradient_of(a, st));
 }
 
+// The sizes alone do not say where the table lies: room for a table off the grid.
+int64_t room_for(const fsa::ClassShape& s, bool forward, bool with_mean, bool with_grad_w) {
+    return (int64_t)fsa::plan_of(s, forward && fsa::forward_packs(s, false), forward, with_mean, with_grad_w).bytes;
+}
+
 }  // namespace
 
 extern "C" {
 
 int64_t fsa_class_fwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_mean) {
     if (!known(dtype) || !sizes_ok(T, V, D, K)) return 0;
-    return (int64_t)fsa::plan_of({T, V, D, dtype, K}, true, with_mean != 0, false).bytes;
+    return room_for({T, V, D, dtype, K}, true, with_mean != 0, false);
 }
 
 int64_t fsa_class_bwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_mean, int with_grad_w) {
     if (!known(dtype) || !sizes_ok(T, V, D, K)) return 0;
-    return (int64_t)fsa::plan_of({T, V, D, dtype, K}, with_mean != 0, with_mean != 0, with_grad_w != 0).bytes;
+    return room_for({T, V, D, dtype, K}, with_mean != 0, with_mean != 0, with_grad_w != 0);
 }
 
 int fsa_xent_fwd(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,

@@ -151,26 +151,29 @@ __device__ __forceinline__ float finite_abs(float x) {
     return a < __builtin_inff() ? a : 0.0f;
 }
 // Largest of n partial peaks, by the whole workgroup; `room` is a word of LDS per wave.
+template <int WAVES>
 __device__ __forceinline__ float block_peak(const float* peaks, int n, float* room) {
     float m = 0.0f;
-    for (int i = threadIdx.x; i < n; i += kClassThreads) m = fmaxf(m, peaks[i]);
+    for (int i = threadIdx.x; i < n; i += WAVES * 64) m = fmaxf(m, peaks[i]);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
     if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = m;
     __syncthreads();
-    m = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) m = fmaxf(m, room[i]);
     __syncthreads();
     return m;
 }
 struct Units { float w, h, g; };
+template <int WAVES = kClassWaves>
 __device__ __forceinline__ Units units(const ClassArgs& a, float* room, bool grad) {
     Units u{1.0f, 1.0f, 1.0f};
     const float* p = a.at<const float>(a.plan.peaks);
     if constexpr (kKind == 0) {
-        u.w = unit_of(block_peak(p, kPeaksTable, room));
-        u.h = unit_of(block_peak(p + kPeaksTable, kPeaksRows, room));
+        u.w = unit_of(block_peak<WAVES>(p, kPeaksTable, room));
+        u.h = unit_of(block_peak<WAVES>(p + kPeaksTable, kPeaksRows, room));
     }
-    if constexpr (kHalf) if (grad) u.g = unit_of(block_peak(p + kPeaksTable + kPeaksRows, kPeaksGrad, room));
+    if constexpr (kHalf) if (grad) u.g = unit_of(block_peak<WAVES>(p + kPeaksTable + kPeaksRows, kPeaksGrad, room));
     return u;
 }
 
@@ -251,17 +254,38 @@ __device__ __forceinline__ float slot_weight(const ClassArgs& a, int64_t t, int 
     return e / sum;
 }
 
-// One workgroup per 32 rows, eight to a wave.
+// What the gradient knows of 32 rows' slots in one bucket: where they lie, how many, and whether any of the rows has a
+// negative gradient.
+struct SlotWord {
+    uint32_t w;
+    __device__ __forceinline__ int start() const { return w & 2047; }
+    __device__ __forceinline__ int count() const { return w >> 11 & 4095; }
+    __device__ __forceinline__ bool negative() const { return w >> 31; }
+};
+// A slot: its row of the 32 above 27 bits of class, and g * q with the units of the gradient.
+struct Slot { uint32_t key; float pull; };
+
+constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / 64, kRowsEach = kBlock / kRowWaves;
+
+// One workgroup per 32 rows, two to a wave.
 template <int DP>
-__global__ __launch_bounds__(kClassThreads) void class_rows_kernel(ClassArgs a, int64_t padded, bool grad) {
-    __shared__ float room[kClassWaves];
-    __shared__ uint32_t signs;
-    if (threadIdx.x == 0) signs = 0;
-    const Units u = units(a, room, grad);
+__global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, int64_t padded, bool grad) {
+    __shared__ float room[kRowWaves];
+    __shared__ uint32_t signs, counts[kMostBuckets], sums[kRowWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const ClassBuckets bk = buckets_of(a.s.V, a.s.K);
+    if (grad) {
+        if (threadIdx.x == 0) signs = 0;
+        for (int i = threadIdx.x; i < bk.count; i += kRowThreads) counts[i] = 0;
+    }
+    const Units u = units<kRowWaves>(a, room, grad);
     uint16_t* planes = a.at<uint16_t>(a.plan.rows);
     __syncthreads();
-    for (int q = wave; q < kBlock; q += kClassWaves) {
+    int ids[kRowsEach];
+    float pulls[kRowsEach];
+#pragma unroll
+    for (int k = 0; k < kRowsEach; ++k) {
+        const int q = wave * kRowsEach + k;
         const int64_t t = (int64_t)blockIdx.x * kBlock + q;
         int id = -1;
         float log_weight, weight = 0.0f;
@@ -277,16 +301,122 @@ __global__ __launch_bounds__(kClassThreads) void class_rows_kernel(ClassArgs a, 
         if (!grad) continue;
         // P = |g| * softmax * units = 2^(scores*log2e + start), its sign apart
         const float g = lives ? a.grad_loss[t] * u.g : 0.0f;
-        if (lane < a.s.K && t < a.s.T)
-            a.at<float>(a.plan.pull)[t * a.s.K + lane] = id >= 0 && id < a.s.V ? g * weight : 0.0f;
         if (lane == 0) {
             const float to_log2 = a.scale * kLog2e / u.h / u.w;
             a.at<float>(a.plan.start)[t] = lives ? (log2f(fabsf(g)) - a.lse_in[t] * kLog2e) / to_log2 : -__builtin_inff();
             if (g < 0.0f) atomicOr(&signs, 1u << q);
         }
+        ids[k] = id >= 0 && id < a.s.V && weight != 0.0f ? id : -1;
+        pulls[k] = g * weight;
+        if (ids[k] >= 0) atomicAdd(&counts[ids[k] / kBlock / bk.per], 1u);
+    }
+    if (!grad) return;
+    __syncthreads();
+    // counts to places, four buckets to a thread
+    static_assert(kMostBuckets <= 4 * kRowThreads, "a thread has four buckets");
+    uint32_t mine[4], before = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int i = 4 * threadIdx.x + j;
+        mine[j] = i < bk.count ? counts[i] : 0;
+        before += mine[j];
+    }
+    const uint32_t total = before;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const uint32_t o = __shfl_up(before, d);
+        if (lane >= d) before += o;
+    }
+    if (lane == 63) sums[wave] = before;
+    __syncthreads();
+    before -= total;
+    for (int i = 0; i < wave; ++i) before += sums[i];
+    uint32_t* words = a.at<uint32_t>(a.plan.buckets) + (int64_t)blockIdx.x * bk.count;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int i = 4 * threadIdx.x + j;
+        if (i < bk.count) {
+            words[i] = (mine[j] ? before : 0) | mine[j] << 11 | (signs ? 1u << 31 : 0);
+            counts[i] = before;
+        }
+        before += mine[j];
     }
     __syncthreads();
-    if (grad && threadIdx.x == 0) a.at<uint32_t>(a.plan.signs)[blockIdx.x] = signs;
+    Slot* slots = a.at<Slot>(a.plan.slots) + (int64_t)blockIdx.x * kBlock * a.s.K;
+#pragma unroll
+    for (int k = 0; k < kRowsEach; ++k)
+        if (ids[k] >= 0)
+            slots[atomicAdd(&counts[ids[k] / kBlock / bk.per], 1u)] = Slot{(uint32_t)(wave * kRowsEach + k) << 27 | (uint32_t)ids[k], pulls[k]};
+    if (threadIdx.x == 0) a.at<uint32_t>(a.plan.signs)[blockIdx.x] = signs;
+}
+
+// The slots that a wave's (or a wide workgroup's) 32 classes have in the streamed blocks, M blocks of a tile: words are
+// asked for two tiles ahead, slots one, so that nothing of it is waited for.
+template <int M>
+struct SlotFeed {
+    const uint32_t* words;                              // of this bucket, a block of rows apart
+    const Slot* slots;
+    int64_t buckets, block_slots, blocks;
+    uint32_t first_class;
+    SlotWord ahead[M], next[M], now[M];
+    Slot next_slot[M], slot[M];
+    __device__ __forceinline__ SlotFeed(const ClassArgs& a, int64_t padded, int64_t v0) {
+        const ClassBuckets bk = buckets_of(a.s.V, a.s.K);
+        const int64_t block = v0 / kBlock < ceil_div(a.s.V, kBlock) ? v0 / kBlock : 0;
+        words = a.at<const uint32_t>(a.plan.buckets) + block / bk.per;
+        slots = a.at<const Slot>(a.plan.slots);
+        buckets = bk.count; block_slots = (int64_t)kBlock * a.s.K; blocks = padded / kBlock;
+        first_class = (uint32_t)v0;
+    }
+    __device__ __forceinline__ void ask_words(int64_t block) {
+#pragma unroll
+        for (int m = 0; m < M; ++m) ahead[m].w = block + m < blocks ? words[(block + m) * buckets] : 0;
+    }
+    __device__ __forceinline__ void ask_slots(int64_t block, int lane) {
+#pragma unroll
+        for (int m = 0; m < M; ++m) {
+            next[m].w = __builtin_amdgcn_readfirstlane(ahead[m].w);
+            next_slot[m] = Slot{~0u, 0.0f};
+            if (lane < next[m].count()) next_slot[m] = slots[(block + m) * block_slots + next[m].start() + lane];
+        }
+    }
+    __device__ __forceinline__ void turn() {
+#pragma unroll
+        for (int m = 0; m < M; ++m) { now[m] = next[m]; slot[m] = next_slot[m]; }
+    }
+    // Adds what the slots of block m pull at to cells[row][class]; whether there was one (wave-uniform).
+    __device__ __forceinline__ bool gather(int m, int64_t block, int lane, float* cells) const {
+        if (now[m].count() == 0) return false;
+        bool hit = false;
+        Slot s = slot[m];
+        for (int e = lane;;) {
+            const uint32_t c = (s.key & 0x7ffffffu) - first_class;
+            if (e < now[m].count() && c < (uint32_t)kBlock) {
+                atomicAdd(&cells[(s.key >> 27) * kBlock + c], s.pull);
+                hit = true;
+            }
+            e += 64;
+            if (e - lane >= now[m].count()) break;
+            if (e < now[m].count()) s = slots[block * block_slots + now[m].start() + e];
+        }
+        return __any(hit);
+    }
+};
+
+// The table as planes of padded rows, zero behind its last row and element.
+template <int DP>
+__global__ __launch_bounds__(kClassThreads) void class_pack_kernel(ClassArgs a, int64_t rows) {
+    __shared__ float room[kClassWaves];
+    const Units u = units(a, room, false);
+    uint16_t* planes = a.at<uint16_t>(a.plan.table);
+    for (int64_t q = (int64_t)blockIdx.x * kClassThreads + threadIdx.x; q < rows * (DP / 8); q += (int64_t)gridDim.x * kClassThreads) {
+        const int64_t v = q / (DP / 8);
+        const int c = (int)(q % (DP / 8)) * 8;
+        u32x4 p[NS] = {};
+        if (v < a.s.V && c < a.s.D) planes_of(load8(static_cast<const Elem*>(a.w) + v * a.w_stride, a.s.D, c), u.w, p);
+#pragma unroll
+        for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + ((int64_t)n * rows + v) * DP + c) = p[n];
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -379,8 +509,8 @@ __device__ __forceinline__ int row_of(int i, int lane) { return 8 * (i >> 2) + 4
 // ---------------------------------------------------------------------------------------------------------------
 // forward: a wave holds 32 rows of h, the table streams by
 // ---------------------------------------------------------------------------------------------------------------
-template <int DP, int WY, bool MEAN>
-__global__ __launch_bounds__(kClassThreads) void class_forward_kernel(ClassArgs a, int64_t padded) {
+template <int DP, int WY, bool MEAN, bool PACKED>
+__global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_forward_kernel(ClassArgs a, int64_t padded) {
     constexpr int NB = WY == 4 ? 4 : 2, MY = NB / WY, WX = kClassWaves / WY;   // blocks of a tile, a wave's own of them
     using T = Tile<DP, NB * kBlock>;
     __shared__ __align__(16) uint16_t lds[2][NS * T::kPlane];
@@ -407,14 +537,19 @@ __global__ __launch_bounds__(kClassThreads) void class_forward_kernel(ClassArgs 
 #pragma unroll
     for (auto& f : acc) f = f32x16{};
 
-    const Elem* w = static_cast<const Elem*>(a.w);
-    typename T::FromTable next;
-    if (first < last) next.load(w, a.w_stride, a.s.V, a.s.D, first * NB * kBlock);
+    typename std::conditional<PACKED, typename T::FromPlanes, typename T::FromTable>::type next;
+    const int64_t table_rows = padded_rows(a.s.V);
+    auto fetch = [&](int64_t it) {
+        if constexpr (PACKED) next.load(a.at<const uint16_t>(a.plan.table), table_rows, it * NB * kBlock);
+        else next.load(static_cast<const Elem*>(a.w), a.w_stride, a.s.V, a.s.D, it * NB * kBlock);
+    };
+    if (first < last) fetch(first);
     for (int64_t it = first; it < last; ++it) {
         uint16_t* tile = lds[(it - first) & 1];         // the other one may still be read
-        next.store(tile, u.w);
+        if constexpr (PACKED) next.store(tile);
+        else next.store(tile, u.w);
         __syncthreads();
-        if (it + 1 < last) next.load(w, a.w_stride, a.s.V, a.s.D, (it + 1) * NB * kBlock);
+        if (it + 1 < last) fetch(it + 1);
         if (!live) continue;
 
         f32x16 score[MY];
@@ -609,7 +744,7 @@ __global__ __launch_bounds__(kClassThreads) void class_pull_kernel(ClassArgs a) 
 // A wave holds 32 classes, the rows stream by:
 //   grad_w[v] = scale * sum_t g_t (p[t,v] - sum over t's slots j that name v of q_j) h[t]
 template <int DP, int WY>
-__global__ __launch_bounds__(kClassThreads) void class_gradient_kernel(ClassArgs a, int64_t padded) {
+__global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_gradient_kernel(ClassArgs a, int64_t padded) {
     constexpr int NB = WY == 4 ? 4 : 2, MY = NB / WY, WX = kClassWaves / WY;
     using T = Tile<DP, NB * kBlock>;
     __shared__ __align__(16) uint16_t lds[2][NS * T::kPlane];
@@ -642,16 +777,22 @@ __global__ __launch_bounds__(kClassThreads) void class_gradient_kernel(ClassArgs
 
     const uint16_t* planes = a.at<const uint16_t>(a.plan.rows);
     const float* start = a.at<const float>(a.plan.start);
-    const float* pull = a.at<const float>(a.plan.pull);
     typename T::FromPlanes next;
     float next_start = 0.0f;
+    SlotFeed<MY> feed(a, padded, v0);
     auto fetch = [&](int64_t it) {
+        feed.ask_slots(it * NB + y * MY, lane);
+        feed.ask_words((it + 1) * NB + y * MY);
         next.load(planes, padded, it * NB * kBlock);    // rows are padded to whole tiles
         if (threadIdx.x < NB * kBlock) next_start = start[it * NB * kBlock + threadIdx.x];
     };
-    if (first < last) fetch(first);
+    if (first < last) {
+        feed.ask_words(first * NB + y * MY);
+        fetch(first);
+    }
     for (int64_t it = first; it < last; ++it) {
         const int half = (it - first) & 1;
+        feed.turn();
         uint16_t* tile = lds[half];
         next.store(tile);
         if (threadIdx.x < NB * kBlock) starts[half][threadIdx.x] = next_start;
@@ -679,19 +820,12 @@ __global__ __launch_bounds__(kClassThreads) void class_gradient_kernel(ClassArgs
             float p[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(score[i] * to_log2);
-            const uint32_t signs = a.at<const uint32_t>(a.plan.signs)[t0 / kBlock];
-            if (signs) {
+            if (feed.now[m].negative()) {
+                const uint32_t signs = a.at<const uint32_t>(a.plan.signs)[t0 / kBlock];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) if (signs >> row_of(i, lane) & 1) p[i] = -p[i];
             }
-            // slots of these rows that name one of these classes
-            const int n = (int)((a.s.T - t0 < kBlock ? a.s.T - t0 : kBlock) * a.s.K);
-            bool hit = false;
-            for (int e = lane; e < n; e += 64) {
-                const int64_t c = a.ids[t0 * a.s.K + e] - v0;
-                if (c >= 0 && c < kBlock) { atomicAdd(&cell[e / a.s.K * kBlock + (int)c], pull[t0 * a.s.K + e]); hit = true; }
-            }
-            if (__any(hit)) {
+            if (feed.gather(m, t0 / kBlock, lane, cell)) {
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -770,7 +904,7 @@ enum WideMode { kStats, kMean, kGradient };
 
 // kStats: running maximum and sum of every held row of h, one pair per wave (a quarter of the streamed classes each).
 // kMean: sum of the table's rows under 2^(score - norm).  kGradient: as the narrow kernel.
-template <int Q, WideMode MODE>
+template <int Q, WideMode MODE, bool PACKED>
 __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, int64_t padded) {
     using S = Quarter<Q>;
     constexpr int DEPTH = Q * kClassWaves;
@@ -813,29 +947,42 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
     for (auto& f : acc) f = f32x16{};
 
     // the next tile's quarter: rows of the table as they are, or planes
-    struct { Eight e[MODE == kGradient ? 1 : S::kEach]; u32x4 p[MODE == kGradient ? NS : 1][MODE == kGradient ? S::kEach : 1]; } next;
+    constexpr bool FROM_PLANES = MODE == kGradient || PACKED;
+    struct { Eight e[FROM_PLANES ? 1 : S::kEach]; u32x4 p[FROM_PLANES ? NS : 1][FROM_PLANES ? S::kEach : 1]; } next;
+    const uint16_t* streamed = MODE == kGradient ? planes : a.at<const uint16_t>(a.plan.table);
+    const int64_t streamed_rows = MODE == kGradient ? padded : padded_rows(a.s.V);
+    SlotFeed<1> feed(a, padded, MODE == kGradient ? x0 : 0);
     f32x4 next_start = {};
     auto fetch = [&](int64_t it) {
+        if constexpr (MODE == kGradient)
+            if (wave == 0) {                            // one wave looks after the slots of the workgroup's classes
+                feed.ask_slots(it, lane);
+                feed.ask_words(it + 1);
+            }
 #pragma unroll
         for (int i = 0; i < S::kEach; ++i) {
             const int q = i * 64 + lane, r = q / S::kChunks, c = q % S::kChunks;
             const int64_t row = it * kBlock + r;
-            if constexpr (MODE == kGradient) {
+            if constexpr (FROM_PLANES) {
 #pragma unroll
                 for (int n = 0; n < NS; ++n)
-                    next.p[n][i] = *reinterpret_cast<const u32x4*>(planes + ((int64_t)n * padded + row) * DEPTH + col0 + c * 8);
+                    next.p[n][i] = *reinterpret_cast<const u32x4*>(streamed + ((int64_t)n * streamed_rows + row) * DEPTH + col0 + c * 8);
             } else next.e[i] = load8(w + (row < a.s.V ? row : a.s.V - 1) * a.w_stride, a.s.D, col0 + c * 8);
         }
         if constexpr (MODE == kGradient)
             next_start = *reinterpret_cast<const f32x4*>(a.at<const float>(a.plan.start) + it * kBlock + 8 * wave + 4 * (lane >> 5));
     };
-    if (first < last) fetch(first);
+    if (first < last) {
+        if (MODE == kGradient && wave == 0) feed.ask_words(first);
+        fetch(first);
+    }
     for (int64_t it = first; it < last; ++it) {
+        if (MODE == kGradient && wave == 0) feed.turn();
 #pragma unroll
         for (int i = 0; i < S::kEach; ++i) {
             const int q = i * 64 + lane, r = q / S::kChunks, c = q % S::kChunks;
             u32x4 p[NS];
-            if constexpr (MODE == kGradient) {
+            if constexpr (FROM_PLANES) {
 #pragma unroll
                 for (int n = 0; n < NS; ++n) p[n] = next.p[n][i];
             } else planes_of(next.e[i], u.w, p);
@@ -856,13 +1003,7 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
 #pragma unroll
         for (int i = 0; i < 4; ++i) meet[wave][i][lane] = f32x4{score[4 * i], score[4 * i + 1], score[4 * i + 2], score[4 * i + 3]};
         const int64_t y0 = it * kBlock;
-        if constexpr (MODE == kGradient) {              // slots of these rows that name one of these classes
-            const int n = (int)((a.s.T - y0 < kBlock ? a.s.T - y0 : kBlock) * a.s.K);
-            for (int e = threadIdx.x; e < n; e += kClassThreads) {
-                const int64_t c = a.ids[y0 * a.s.K + e] - x0;
-                if (c >= 0 && c < kBlock) atomicAdd(&cells[e / a.s.K * kBlock + (int)c], a.at<const float>(a.plan.pull)[y0 * a.s.K + e]);
-            }
-        }
+        if (MODE == kGradient && wave == 0) feed.gather(0, it, lane, cells);
         __syncthreads();
         f32x4 z = (meet[0][wave][lane] + meet[1][wave][lane]) + (meet[2][wave][lane] + meet[3][wave][lane]);   // rows 8*wave + 4*(lane/32) + j
         const int y = 8 * wave + 4 * (lane >> 5);
@@ -991,20 +1132,23 @@ hipError_t launch_rows(const ClassArgs& a, bool grad, hipStream_t stream) {
     const int table = kKind == 0 ? kPeaksTable : 0, rows = kKind == 0 ? kPeaksRows : 0, g = kHalf && grad ? kPeaksGrad : 0;
     if (table + rows + g) class_peaks_kernel<<<table + rows + g, kClassThreads, 0, stream>>>(a, table, rows, g);
     return with_depth(class_depth(a.s.D), [&](auto dp) {
-        if (padded) class_rows_kernel<dp()><<<padded / kBlock, kClassThreads, 0, stream>>>(a, padded, grad);
+        if (padded) class_rows_kernel<dp()><<<padded / kBlock, kRowThreads, 0, stream>>>(a, padded, grad);
     });
 }
 
-template <int DP, bool MEAN> void launch_forward(const ClassArgs& a, int64_t padded, hipStream_t stream) {
+template <int DP, bool MEAN, bool PACKED> void launch_forward(const ClassArgs& a, int64_t padded, hipStream_t stream) {
     const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
-    if constexpr (!narrow_depth(DP, kKind)) class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats><<<grid, kClassThreads, 0, stream>>>(a, padded);
-    else if (a.cut.wy == 1) class_forward_kernel<DP, 1, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
-    else if (a.cut.wy == 2) class_forward_kernel<DP, 2, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
-    else class_forward_kernel<DP, 4, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    if constexpr (!narrow_depth(DP, kKind))
+        class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats, PACKED><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    else if (a.cut.wy == 1) class_forward_kernel<DP, 1, MEAN, PACKED><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    else if constexpr (!PACKED) {                       // (few rows never pack)
+        if (a.cut.wy == 2) class_forward_kernel<DP, 2, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
+        else class_forward_kernel<DP, 4, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    }
 }
 template <int DP> void launch_gradient(const ClassArgs& a, int64_t padded, hipStream_t stream) {
     const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
-    if constexpr (!narrow_depth(DP, kKind)) class_wide_kernel<DP / kClassWaves, kGradient><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    if constexpr (!narrow_depth(DP, kKind)) class_wide_kernel<DP / kClassWaves, kGradient, true><<<grid, kClassThreads, 0, stream>>>(a, padded);
     else if (a.cut.wy == 1) class_gradient_kernel<DP, 1><<<grid, kClassThreads, 0, stream>>>(a, padded);
     else if (a.cut.wy == 2) class_gradient_kernel<DP, 2><<<grid, kClassThreads, 0, stream>>>(a, padded);
     else class_gradient_kernel<DP, 4><<<grid, kClassThreads, 0, stream>>>(a, padded);
@@ -1017,13 +1161,22 @@ hipError_t forward(ClassArgs a, hipStream_t stream) {
     a.cut = forward_cut(a.s);
     const int slices = (int)a.cut.slices();
     if (hipError_t e = launch_rows(a, false, stream)) return e;
-    if (hipError_t e = with_depth(depth, [&](auto dp) {
-            if (a.mean && !wide) launch_forward<dp(), true>(a, padded, stream);
-            else launch_forward<dp(), false>(a, padded, stream);
-        })) return e;
+    auto run = [&](bool mean) {
+        return with_depth(depth, [&](auto dp) {
+            if (a.plan.packed) mean ? launch_forward<dp(), true, true>(a, padded, stream) : launch_forward<dp(), false, true>(a, padded, stream);
+            else mean ? launch_forward<dp(), true, false>(a, padded, stream) : launch_forward<dp(), false, false>(a, padded, stream);
+        });
+    };
+    if (a.plan.packed) {
+        const int64_t rows = padded_rows(a.s.V), grid = ceil_div(rows * depth / 8, kClassThreads);
+        if (hipError_t e = with_depth(depth, [&](auto dp) {
+                class_pack_kernel<dp()><<<(unsigned)(grid < 8192 ? grid : 8192), kClassThreads, 0, stream>>>(a, rows);
+            })) return e;
+    }
+    if (hipError_t e = run(a.mean && !wide)) return e;
     class_finish_kernel<<<(unsigned)a.s.T, kClassThreads, 0, stream>>>(a, padded, depth, wide ? slices * kClassWaves : slices, wide);
     if (!a.mean || !wide) return hipGetLastError();
-    if (hipError_t e = with_depth(depth, [&](auto dp) { launch_forward<dp(), true>(a, padded, stream); })) return e;
+    if (hipError_t e = run(true)) return e;
     join(a.at<const float>(a.plan.mean_parts), a.mean, a.s.T, a.s.D, padded, depth, slices, stream);
     return hipGetLastError();
 }
