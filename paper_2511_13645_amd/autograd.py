@@ -130,10 +130,17 @@ class _ClassLoss(torch.autograd.Function):
         return (*grads, None, None, None, None, None)
 
 
+def _class_loss(h, w, ids, logits, temperature, scale):
+    loss = binding.class_loss(h, w, ids, logits, temperature, scale)
+    if loss is None:
+        loss = _ClassLoss.apply(h, w, ids, logits, temperature, scale, h.requires_grad and torch.is_grad_enabled())
+    return loss
+
+
 def fused_cross_entropy(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, *, scale: float = 1.0) -> torch.Tensor:
     """Differentiable softmax cross entropy of rows h [T,D] against every class of w [V,D] (scores scale * h.w, never
     kept), one loss a row, fp32.  targets [T] int32; a negative one leaves its row out (loss 0, no gradient)."""
-    return _ClassLoss.apply(h, w, targets, None, 1.0, float(scale), h.requires_grad and torch.is_grad_enabled())
+    return _class_loss(h, w, targets, None, 1.0, float(scale))
 
 
 def fused_distillation(h: torch.Tensor, w: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, *,
@@ -141,5 +148,4 @@ def fused_distillation(h: torch.Tensor, w: torch.Tensor, teacher_ids: torch.Tens
     """Differentiable divergence of rows h [T,D] over every class of w [V,D] from a teacher of which the K best classes
     are known: teacher_ids [T,K] int32 (negative: an empty slot) and teacher_logits [T,K].  `temperature` divides both
     sides' scores; the loss is not multiplied by its square.  The teacher gets no gradient."""
-    return _ClassLoss.apply(h, w, teacher_ids, teacher_logits, float(temperature), float(scale),
-                            h.requires_grad and torch.is_grad_enabled())
+    return _class_loss(h, w, teacher_ids, teacher_logits, float(temperature), float(scale))

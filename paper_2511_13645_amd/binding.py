@@ -26,6 +26,7 @@ from . import build
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfsa_hip.so")
 HOST_PATH = build.host_lib()
+CLASS_HOST_PATH = build.class_host_lib()
 
 FSA_F32, FSA_BF16, FSA_F16 = 0, 1, 2
 FSA_I32, FSA_I64 = 0, 1
@@ -43,10 +44,13 @@ EXPORTS = ("fsa_sample_mean_fwd", "fsa_mean_replay_fwd", "fsa_mean_bwd", "fsa_me
            "fsa_xent_fwd", "fsa_xent_bwd", "fsa_distill_fwd", "fsa_distill_bwd")
 
 _lib: Optional[ctypes.CDLL] = None
+_class_host = None                              # the module _fsa_class_host, likewise
 _host = None                                    # the module _fsa_host, once the library is loaded; None without it
 _HOST_ENTRIES = ("fsa_sample_mean_fwd", "fsa_sample_wmean_fwd", "fsa_mean_replay_fwd", "fsa_mean_bwd", "fsa_mean_bwd_ws",
                  "fsa_mean_bwd_lp_ws", "fsa_wmean_bwd_ws", "fsa_mean_bwd_dense", "fsa_mean_bwd_dense_workspace_bytes",
                  "fsa_mean_bwd_dense_pays")              # entry points that _fsa_host calls
+_CLASS_HOST_ENTRIES = ("fsa_class_fwd_workspace_bytes", "fsa_class_bwd_workspace_bytes", "fsa_xent_fwd", "fsa_xent_bwd",
+                       "fsa_distill_fwd", "fsa_distill_bwd")             # the same of _fsa_class_host
 _PLAIN, _WORKSPACE, _LOW_PRECISION, _WEIGHTED = range(4)                # backward entry points, as _fsa_host.bwd counts them
 
 
@@ -58,7 +62,7 @@ class FsaError(RuntimeError):
 
 def lib() -> ctypes.CDLL:
     """Load the HIP library; fail loudly when it has not been built."""
-    global _lib, _host
+    global _lib, _host, _class_host
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError("HIP library missing: %s (build it with __graft_entry__.build())" % LIB_PATH)
@@ -125,21 +129,30 @@ def lib() -> ctypes.CDLL:
         L.fsa_distill_bwd.restype = ci
         L.fsa_status_string.argtypes = [ci]
         L.fsa_status_string.restype = ctypes.c_char_p
-        _lib, _host = L, _load_host(L)
+        _lib, _host, _class_host = L, _load_host(L), _load_class_host(L)
     return _lib
 
 
 def _load_host(L: ctypes.CDLL):
     """The module _fsa_host at HOST_PATH, or None and a warning: it saves host time and nothing else."""
+    return _load_module(L, "_fsa_host", HOST_PATH, _HOST_ENTRIES)
+
+
+def _load_class_host(L: ctypes.CDLL):
+    """The same for the class losses."""
+    return _load_module(L, "_fsa_class_host", CLASS_HOST_PATH, _CLASS_HOST_ENTRIES)
+
+
+def _load_module(L: ctypes.CDLL, name: str, path: str, entries: Sequence[str]):
     try:
-        spec = importlib.util.spec_from_loader("_fsa_host", importlib.machinery.ExtensionFileLoader("_fsa_host", HOST_PATH))
+        spec = importlib.util.spec_from_loader(name, importlib.machinery.ExtensionFileLoader(name, path))
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
-        module.bind(_raw_stream, {name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in _HOST_ENTRIES})
+        module.bind(_raw_stream, {e: ctypes.cast(getattr(L, e), ctypes.c_void_p).value for e in entries})
         return module
     except (ImportError, TypeError) as e:
         warnings.warn("calls go through Python only, which takes a few microseconds more: no %s (%s; build it with "
-                      "__graft_entry__.build())" % (HOST_PATH, e), RuntimeWarning, stacklevel=3)
+                      "__graft_entry__.build())" % (path, e), RuntimeWarning, stacklevel=4)
         return None
 
 
@@ -769,6 +782,10 @@ def _class_workspace(workspace: Optional[torch.Tensor], need: int, like: torch.T
 
 
 def _class_fwd(name: str, h, w, ids, logits, scale: float, temperature: float, emit_mean: bool, workspace, stream):
+    if _class_host is not None and stream is None and workspace is None:
+        r = _class_host.class_fwd(h, w, ids, logits, temperature, scale, emit_mean)
+        if _taken(r, name):
+            return r
     lead, T, V, D, K = _class_operands(h, w, ids, logits)
     L = lib()
     loss = torch.empty((T,), dtype=torch.float32, device=h.device)
@@ -808,6 +825,16 @@ def _class_bwd(name: str, grad_loss, h, w, ids, logits, lse, mean, scale: float,
     if rc != FSA_OK:
         raise FsaError(rc, name)
     return grad_h, grad_w
+
+
+def class_loss(h, w, ids, logits, temperature: float, scale: float) -> Optional[torch.Tensor]:
+    """The differentiable loss through the native host path, or None: then autograd.py's own function takes the call."""
+    lib()
+    if _class_host is not None:
+        r = _class_host.class_loss(h, w, ids, logits, temperature, scale)
+        if _taken(r, "fsa_xent_fwd" if logits is None else "fsa_distill_fwd"):
+            return r
+    return None
 
 
 def fsa_xent_fwd(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, *, emit_mean: bool = False,

@@ -26,13 +26,23 @@ HIPCC_FLAGS = [
 
 
 HOST_SOURCE = os.path.join(HERE, "csrc_host", "fsa_host.cpp")
+CLASS_HOST_SOURCE = os.path.join(HERE, "csrc_host", "fsa_class_host.cpp")
 
 
 def host_lib() -> str:
     """Where the host path for the running Python and torch lies.  It uses parts of both that other versions lay out
     otherwise, so a build for another one has another name and is never loaded."""
+    return _module("_fsa_host")
+
+
+def class_host_lib() -> str:
+    """The same for the class losses' host path."""
+    return _module("_fsa_class_host")
+
+
+def _module(name: str) -> str:
     import torch
-    return os.path.join(HERE, "_fsa_host.%s.torch-%s.so" % (sys.implementation.cache_tag, torch.__version__))
+    return os.path.join(HERE, "%s.%s.torch-%s.so" % (name, sys.implementation.cache_tag, torch.__version__))
 
 
 def hipcc() -> str:
@@ -72,14 +82,22 @@ def build_hip(extra_flags=(), verbose: bool = False, out: str = LIB) -> str:
 
 def build_host(extra_flags=(), verbose: bool = False, out: Optional[str] = None) -> str:
     """Compile the binding's host path (plain C++ against torch's headers and the CPython C API)."""
+    return _build_module(HOST_SOURCE, extra_flags, verbose, out or host_lib())
+
+
+def build_class_host(extra_flags=(), verbose: bool = False, out: Optional[str] = None) -> str:
+    """Compile the class losses' host path, a module of its own."""
+    return _build_module(CLASS_HOST_SOURCE, extra_flags, verbose, out or class_host_lib())
+
+
+def _build_module(source: str, extra_flags, verbose: bool, out: str) -> str:
     import torch
-    out = out or host_lib()
     base = os.path.dirname(torch.__file__)
     tmp = out + ".tmp.%d" % os.getpid()
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI),
            "-isystem", os.path.join(base, "include"), "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
-           "-isystem", sysconfig.get_paths()["include"], *extra_flags, HOST_SOURCE, "-o", tmp,
+           "-isystem", sysconfig.get_paths()["include"], *extra_flags, source, "-o", tmp,
            "-L" + os.path.join(base, "lib"), "-lc10", "-ltorch_cpu", "-ltorch_python"]
     if verbose:
         print(" ".join(cmd), flush=True)
@@ -89,11 +107,13 @@ def build_host(extra_flags=(), verbose: bool = False, out: Optional[str] = None)
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(host_lib()):
+    if not os.path.exists(LIB) or not os.path.exists(host_lib()) or not os.path.exists(class_host_lib()):
         return True
     newest = max(os.path.getmtime(os.path.join(CSRC, f)) for f in SOURCES + HEADERS)
     newest_host = max(os.path.getmtime(f) for f in (HOST_SOURCE, ABI_HEADER))
-    return os.path.getmtime(LIB) < newest or os.path.getmtime(host_lib()) < newest_host
+    newest_class = max(os.path.getmtime(f) for f in (CLASS_HOST_SOURCE, ABI_HEADER))
+    return (os.path.getmtime(LIB) < newest or os.path.getmtime(host_lib()) < newest_host or
+            os.path.getmtime(class_host_lib()) < newest_class)
 
 
 if __name__ == "__main__":
@@ -109,5 +129,6 @@ if __name__ == "__main__":
     if target == LIB:
         try:
             print(build_host(verbose=True))
+            print(build_class_host(verbose=True))
         except (OSError, subprocess.CalledProcessError) as e:
             print("the host path was not built, the binding goes without it: %s" % e, file=sys.stderr)

@@ -744,7 +744,7 @@ __global__ __launch_bounds__(kClassThreads) void class_pull_kernel(ClassArgs a) 
 // A wave holds 32 classes, the rows stream by:
 //   grad_w[v] = scale * sum_t g_t (p[t,v] - sum over t's slots j that name v of q_j) h[t]
 template <int DP, int WY>
-__global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_gradient_kernel(ClassArgs a, int64_t padded) {
+__global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) void class_gradient_kernel(ClassArgs a, int64_t padded) {
     constexpr int NB = WY == 4 ? 4 : 2, MY = NB / WY, WX = kClassWaves / WY;
     using T = Tile<DP, NB * kBlock>;
     __shared__ __align__(16) uint16_t lds[2][NS * T::kPlane];
