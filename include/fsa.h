@@ -372,16 +372,17 @@ int fsa_wmean_bwd_ws(const float* grad_out, const float* grad_h1,
  *                teacher_logits[t,j] / temperature: the divergence from a teacher of which the K best classes are known,
  *                renormalised over those.  Cross entropy is the case of one slot with weight one.
  * A negative target or ID is an empty slot and may appear anywhere; nothing that stands at it is used.  A row without a
- * slot (or whose teacher logits are all -inf) has loss 0, lse 0, mean 0, a zero gradient, and adds nothing to grad_w,
+ * slot (or whose teacher logits are all -inf) has loss 0, lse 0, a zero gradient, and adds nothing to grad_w,
  * whatever its h, lse and grad_loss hold, NaN included.  An ID of V or more is not read: the row's loss is NaN, the
  * gradients are as if its slot's class were none of the table's.  An ID named by two slots of a row counts twice.
  *   h [T,D], w [V,D]   fsa_dtype `dtype`, rows `h_stride` and `w_stride` elements apart (>= D), at any alignment of an
  *                      element;  0 <= T <= FSA_CLASS_TMAX, 1 <= V <= FSA_CLASS_VMAX, 1 <= D <= FSA_CLASS_DMAX
  *   scale, temperature finite and positive
  *   out_loss, out_lse  [T] fp32
- *   out_mean           [T,D] fp32, the mean of w's rows under p; may be NULL.  The gradient of h is made of it.
+ *   out_row_grad       [T,D] fp32, the gradient of every loss by its row, s * (sum_v p w[v] - sum_j q w[ids_j]); may be NULL
  *   grad_loss          [T] fp32: the gradient of every loss (its signs may differ)
- *   lse, mean          as the forward wrote them; mean may be NULL (the backward then computes it again)
+ *   lse, row_grad      as the forward wrote them; row_grad may be NULL (the backward then computes it again for grad_h,
+ *                      which is grad_loss times it)
  *   grad_h [T,D], grad_w [V,D]   `dtype`, contiguous, written whole; either may be NULL
  *   workspace          device memory of the call's *_workspace_bytes, 16-byte aligned (else FSA_ERR_WORKSPACE,
  *                      FSA_ERR_ALIGN); nothing in it is kept from one call to the next
@@ -392,28 +393,28 @@ int fsa_wmean_bwd_ws(const float* grad_out, const float* grad_h1,
  */
 enum { FSA_CLASS_TMAX = 1 << 23, FSA_CLASS_VMAX = 1 << 27, FSA_CLASS_DMAX = 1024 };
 
-int64_t fsa_class_fwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_mean);
-/* with_mean: grad_h is wanted and no mean is given; with_grad_w: grad_w is wanted.  0 for sizes that the calls refuse. */
-int64_t fsa_class_bwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_mean, int with_grad_w);
+int64_t fsa_class_fwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_row_grad);
+/* with_row_grad: grad_h is wanted and no row_grad is given; with_grad_w: grad_w is wanted.  0 for sizes that the calls refuse. */
+int64_t fsa_class_bwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_row_grad, int with_grad_w);
 
 int fsa_xent_fwd(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
                  int64_t T, int64_t V, int64_t D, float scale, const int32_t* targets,
-                 float* out_loss, float* out_lse, float* out_mean,
+                 float* out_loss, float* out_lse, float* out_row_grad,
                  void* workspace, int64_t workspace_bytes, void* stream);
 int fsa_xent_bwd(const float* grad_loss, const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
                  int64_t T, int64_t V, int64_t D, float scale, const int32_t* targets,
-                 const float* lse, const float* mean, void* grad_h, void* grad_w,
+                 const float* lse, const float* row_grad, void* grad_h, void* grad_w,
                  void* workspace, int64_t workspace_bytes, void* stream);
 /* teacher_ids [T,K] int32, teacher_logits [T,K] fsa_dtype `teacher_dtype`; 1 <= K <= FSA_KMAX */
 int fsa_distill_fwd(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
                     int64_t T, int64_t V, int64_t D, float scale, float temperature,
                     const int32_t* teacher_ids, const void* teacher_logits, int teacher_dtype, int32_t K,
-                    float* out_loss, float* out_lse, float* out_mean,
+                    float* out_loss, float* out_lse, float* out_row_grad,
                     void* workspace, int64_t workspace_bytes, void* stream);
 int fsa_distill_bwd(const float* grad_loss, const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
                     int64_t T, int64_t V, int64_t D, float scale, float temperature,
                     const int32_t* teacher_ids, const void* teacher_logits, int teacher_dtype, int32_t K,
-                    const float* lse, const float* mean, void* grad_h, void* grad_w,
+                    const float* lse, const float* row_grad, void* grad_h, void* grad_w,
                     void* workspace, int64_t workspace_bytes, void* stream);
 
 /* Static, never-freed description of a status code. */

@@ -108,25 +108,25 @@ def fused_sample_mean(x: torch.Tensor, indptr: torch.Tensor, indices: torch.Tens
 
 class _ClassLoss(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, h, w, ids, logits, temperature, scale, emit_mean):
+    def forward(ctx, h, w, ids, logits, temperature, scale, emit_row_grad):
         if logits is None:
-            loss, lse, mean = binding.fsa_xent_fwd(h, w, ids, scale, emit_mean=emit_mean)
+            loss, lse, row_grad = binding.fsa_xent_fwd(h, w, ids, scale, emit_row_grad=emit_row_grad)
         else:
-            loss, lse, mean = binding.fsa_distill_fwd(h, w, ids, logits, temperature, scale, emit_mean=emit_mean)
-        ctx.save_for_backward(h, w, ids, logits, lse, mean)
+            loss, lse, row_grad = binding.fsa_distill_fwd(h, w, ids, logits, temperature, scale, emit_row_grad=emit_row_grad)
+        ctx.save_for_backward(h, w, ids, logits, lse, row_grad)
         ctx.temperature, ctx.scale = temperature, scale
         return loss
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_loss):
-        h, w, ids, logits, lse, mean = ctx.saved_tensors
+        h, w, ids, logits, lse, row_grad = ctx.saved_tensors
         want = dict(want_h=ctx.needs_input_grad[0], want_w=ctx.needs_input_grad[1])
         g = grad_loss.contiguous()
         if logits is None:
-            grads = binding.fsa_xent_bwd(g, h, w, ids, lse, mean, ctx.scale, **want)
+            grads = binding.fsa_xent_bwd(g, h, w, ids, lse, row_grad, ctx.scale, **want)
         else:
-            grads = binding.fsa_distill_bwd(g, h, w, ids, logits, lse, mean, ctx.temperature, ctx.scale, **want)
+            grads = binding.fsa_distill_bwd(g, h, w, ids, logits, lse, row_grad, ctx.temperature, ctx.scale, **want)
         return (*grads, None, None, None, None, None)
 
 

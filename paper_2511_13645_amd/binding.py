@@ -781,43 +781,43 @@ def _class_workspace(workspace: Optional[torch.Tensor], need: int, like: torch.T
     return ws
 
 
-def _class_fwd(name: str, h, w, ids, logits, scale: float, temperature: float, emit_mean: bool, workspace, stream):
+def _class_fwd(name: str, h, w, ids, logits, scale: float, temperature: float, emit_row_grad: bool, workspace, stream):
     if _class_host is not None and stream is None and workspace is None:
-        r = _class_host.class_fwd(h, w, ids, logits, temperature, scale, emit_mean)
+        r = _class_host.class_fwd(h, w, ids, logits, temperature, scale, emit_row_grad)
         if _taken(r, name):
             return r
     lead, T, V, D, K = _class_operands(h, w, ids, logits)
     L = lib()
     loss = torch.empty((T,), dtype=torch.float32, device=h.device)
     lse = torch.empty_like(loss)
-    mean = torch.empty((T, D), dtype=torch.float32, device=h.device) if emit_mean else None
-    ws = _class_workspace(workspace, L.fsa_class_fwd_workspace_bytes(T, V, D, lead[4], K, int(emit_mean)), h, stream)
-    tail = (_ptr(loss), _ptr(lse), _ptr(mean), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, h))
+    row_grad = torch.empty((T, D), dtype=torch.float32, device=h.device) if emit_row_grad else None
+    ws = _class_workspace(workspace, L.fsa_class_fwd_workspace_bytes(T, V, D, lead[4], K, int(emit_row_grad)), h, stream)
+    tail = (_ptr(loss), _ptr(lse), _ptr(row_grad), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, h))
     if logits is None:
         rc = L.fsa_xent_fwd(*lead, scale, _ptr(ids), *tail)
     else:
         rc = L.fsa_distill_fwd(*lead, scale, temperature, _ptr(ids), _ptr(logits), _x_dtype(logits), K, *tail)
     if rc != FSA_OK:
         raise FsaError(rc, name)
-    return loss, lse, mean
+    return loss, lse, row_grad
 
 
-def _class_bwd(name: str, grad_loss, h, w, ids, logits, lse, mean, scale: float, temperature: float, want_h: bool, want_w: bool,
+def _class_bwd(name: str, grad_loss, h, w, ids, logits, lse, row_grad, scale: float, temperature: float, want_h: bool, want_w: bool,
                workspace, stream):
     lead, T, V, D, K = _class_operands(h, w, ids, logits)
     for t, n in ((grad_loss, "grad_loss"), (lse, "lse")):
         _need(t, n, torch.float32)
         _shape(t, n, (T,))
-    if mean is not None:
-        _need(mean, "mean", torch.float32)
-        _shape(mean, "mean", (T, D))
-    _same_device(h, (grad_loss, "grad_loss"), (lse, "lse"), (mean, "mean"))
+    if row_grad is not None:
+        _need(row_grad, "row_grad", torch.float32)
+        _shape(row_grad, "row_grad", (T, D))
+    _same_device(h, (grad_loss, "grad_loss"), (lse, "lse"), (row_grad, "row_grad"))
     L = lib()
     grad_h = torch.empty((T, D), dtype=h.dtype, device=h.device) if want_h else None
     grad_w = torch.empty((V, D), dtype=w.dtype, device=w.device) if want_w else None
-    need = L.fsa_class_bwd_workspace_bytes(T, V, D, lead[4], K, int(want_h and mean is None), int(want_w))
+    need = L.fsa_class_bwd_workspace_bytes(T, V, D, lead[4], K, int(want_h and row_grad is None), int(want_w))
     ws = _class_workspace(workspace, need, h, stream)
-    tail = (_ptr(lse), _ptr(mean), _ptr(grad_h), _ptr(grad_w), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, h))
+    tail = (_ptr(lse), _ptr(row_grad), _ptr(grad_h), _ptr(grad_w), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, h))
     if logits is None:
         rc = L.fsa_xent_bwd(_ptr(grad_loss), *lead, scale, _ptr(ids), *tail)
     else:
@@ -837,50 +837,50 @@ def class_loss(h, w, ids, logits, temperature: float, scale: float) -> Optional[
     return None
 
 
-def fsa_xent_fwd(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, *, emit_mean: bool = False,
+def fsa_xent_fwd(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, scale: float = 1.0, *, emit_row_grad: bool = False,
                  workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
                  ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
     """Softmax cross entropy of rows h [T,D] against the classes w [V,D], the scores never kept; targets [T] int32, a
-    negative one is none.  Returns (loss [T], lse [T], mean [T,D] | None), fp32.  `workspace`: see
+    negative one is none.  Returns (loss [T], lse [T], row_grad [T,D] | None), fp32.  `workspace`: see
     fsa_class_fwd_workspace_bytes; torch's memory without one."""
-    return _class_fwd("fsa_xent_fwd", h, w, targets, None, float(scale), 1.0, bool(emit_mean), workspace, stream)
+    return _class_fwd("fsa_xent_fwd", h, w, targets, None, float(scale), 1.0, bool(emit_row_grad), workspace, stream)
 
 
 def fsa_xent_bwd(grad_loss: torch.Tensor, h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,
-                 mean: Optional[torch.Tensor] = None, scale: float = 1.0, *, want_h: bool = True, want_w: bool = True,
+                 row_grad: Optional[torch.Tensor] = None, scale: float = 1.0, *, want_h: bool = True, want_w: bool = True,
                  workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
                  ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
     """Gradients (grad_h | None, grad_w | None) of fsa_xent_fwd from grad_loss [T] and what it returned."""
-    return _class_bwd("fsa_xent_bwd", grad_loss, h, w, targets, None, lse, mean, float(scale), 1.0, bool(want_h), bool(want_w),
+    return _class_bwd("fsa_xent_bwd", grad_loss, h, w, targets, None, lse, row_grad, float(scale), 1.0, bool(want_h), bool(want_w),
                       workspace, stream)
 
 
 def fsa_distill_fwd(h: torch.Tensor, w: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor,
-                    temperature: float = 1.0, scale: float = 1.0, *, emit_mean: bool = False,
+                    temperature: float = 1.0, scale: float = 1.0, *, emit_row_grad: bool = False,
                     workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
                     ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
     """Divergence of the softmax of rows h [T,D] over the classes w [V,D] from a teacher's best classes: teacher_ids
     [T,K] int32 (negative: an empty slot) and their logits [T,K], renormalised over those.  Returns as fsa_xent_fwd."""
-    return _class_fwd("fsa_distill_fwd", h, w, teacher_ids, teacher_logits, float(scale), float(temperature), bool(emit_mean),
+    return _class_fwd("fsa_distill_fwd", h, w, teacher_ids, teacher_logits, float(scale), float(temperature), bool(emit_row_grad),
                       workspace, stream)
 
 
 def fsa_distill_bwd(grad_loss: torch.Tensor, h: torch.Tensor, w: torch.Tensor, teacher_ids: torch.Tensor,
-                    teacher_logits: torch.Tensor, lse: torch.Tensor, mean: Optional[torch.Tensor] = None,
+                    teacher_logits: torch.Tensor, lse: torch.Tensor, row_grad: Optional[torch.Tensor] = None,
                     temperature: float = 1.0, scale: float = 1.0, *, want_h: bool = True, want_w: bool = True,
                     workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
                     ) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
     """Gradients (grad_h | None, grad_w | None) of fsa_distill_fwd; the teacher gets none."""
-    return _class_bwd("fsa_distill_bwd", grad_loss, h, w, teacher_ids, teacher_logits, lse, mean, float(scale), float(temperature),
+    return _class_bwd("fsa_distill_bwd", grad_loss, h, w, teacher_ids, teacher_logits, lse, row_grad, float(scale), float(temperature),
                       bool(want_h), bool(want_w), workspace, stream)
 
 
-def fsa_class_fwd_workspace_bytes(T: int, V: int, D: int, dtype: torch.dtype, K: int = 1, with_mean: bool = False) -> int:
+def fsa_class_fwd_workspace_bytes(T: int, V: int, D: int, dtype: torch.dtype, K: int = 1, with_row_grad: bool = False) -> int:
     """Workspace bytes of fsa_xent_fwd (K = 1) and fsa_distill_fwd; 0 for sizes that they refuse."""
-    return lib().fsa_class_fwd_workspace_bytes(T, V, D, _FLOAT_TYPE[dtype], K, int(with_mean))
+    return lib().fsa_class_fwd_workspace_bytes(T, V, D, _FLOAT_TYPE[dtype], K, int(with_row_grad))
 
 
-def fsa_class_bwd_workspace_bytes(T: int, V: int, D: int, dtype: torch.dtype, K: int = 1, with_mean: bool = False,
+def fsa_class_bwd_workspace_bytes(T: int, V: int, D: int, dtype: torch.dtype, K: int = 1, with_row_grad: bool = False,
                                   with_grad_w: bool = True) -> int:
-    """Workspace bytes of fsa_xent_bwd and fsa_distill_bwd; `with_mean`: grad_h is wanted and no mean given."""
-    return lib().fsa_class_bwd_workspace_bytes(T, V, D, _FLOAT_TYPE[dtype], K, int(with_mean), int(with_grad_w))
+    """Workspace bytes of fsa_xent_bwd and fsa_distill_bwd; `with_row_grad`: grad_h is wanted and no row_grad given."""
+    return lib().fsa_class_bwd_workspace_bytes(T, V, D, _FLOAT_TYPE[dtype], K, int(with_row_grad), int(with_grad_w))

@@ -13,8 +13,8 @@ namespace fsa {
 //   gradient   waves hold classes, the rows stream by: the scores again, their gradients, a class's gradient row
 // Each splits the streamed side over `parts` of the grid, joined in part order by a second launch.
 //
-// Rows of up to 128 (fp32) or 256 elements are held by one wave each ("narrow"); longer ones by the four waves of a
-// workgroup, a quarter of the elements each ("wide"), whose partial scores meet in LDS.
+// Rows of up to 256 elements are held by one wave each ("narrow"); longer ones by the four waves of a workgroup, a quarter
+// of the elements each ("wide"), whose partial scores meet in LDS.
 constexpr int kBlock = 32;                              // rows and classes come in blocks of one matrix instruction
 constexpr int kClassThreads = 256;
 constexpr int kClassWaves = kClassThreads / 64;
@@ -26,7 +26,7 @@ struct ClassShape {
 };
 
 constexpr int class_planes(int kind) { return kind == 0 ? 2 : 1; }       // 16-bit planes that hold an element
-constexpr bool narrow_depth(int depth, int kind) { return depth * class_planes(kind) <= 256; }
+constexpr bool narrow_depth(int depth) { return depth <= 256; }
 inline int class_depth(int64_t D) {                     // what rows are padded to; 0: too long
     constexpr int depths[] = {64, 128, 256, 384, 640, 1024};
     for (int d : depths) if (D <= d) return d;
@@ -44,7 +44,8 @@ struct ClassCut {
     constexpr int64_t slices() const { return parts * wy; }   // partial results of every held row
 };
 
-inline int blocks_per_tile(int wy) { return wy == 4 ? 4 : 2; }
+// Streamed blocks of a tile: two tiles and what else a workgroup keeps fit into LDS.
+constexpr int blocks_per_tile(int wy, int depth, int kind) { return depth * class_planes(kind) > 256 ? wy : wy == 4 ? 4 : 2; }
 
 inline int64_t parts_for(int64_t groups, int64_t tiles, int64_t workgroups, int64_t most) {
     int64_t want = ceil_div(workgroups, groups);
@@ -56,7 +57,7 @@ inline int64_t parts_for(int64_t groups, int64_t tiles, int64_t workgroups, int6
 inline ClassCut cut_of(int64_t held, int64_t streamed, int depth, int kind, int64_t most_parts) {
     ClassCut c;
     const int64_t blocks = ceil_div(held, kBlock);
-    if (!narrow_depth(depth, kind)) {
+    if (!narrow_depth(depth)) {
         c.wx = 1; c.wy = 1;
         c.groups = blocks;
         c.tiles = ceil_div(streamed, kBlock);
@@ -64,9 +65,10 @@ inline ClassCut cut_of(int64_t held, int64_t streamed, int depth, int kind, int6
         return c;
     }
     c.wy = blocks >= 4 ? 1 : blocks >= 2 ? 2 : 4;
+    if (c.wy == 4 && depth * class_planes(kind) > 256) c.wy = 2;
     c.wx = kClassWaves / c.wy;
     c.groups = ceil_div(blocks, c.wx);
-    c.tiles = ceil_div(streamed, (int64_t)blocks_per_tile(c.wy) * kBlock);
+    c.tiles = ceil_div(streamed, (int64_t)blocks_per_tile(c.wy, depth, kind) * kBlock);
     c.parts = parts_for(c.groups, c.tiles, 1024, most_parts);
     return c;
 }
@@ -94,34 +96,34 @@ inline bool forward_packs(const ClassShape& s, bool on_grid) {
 
 // Byte offsets into the caller's workspace.
 struct ClassPlan {
-    size_t peaks, rows, table, top, sum, mean_parts, norm, loss, start, signs, buckets, slots, mean, grad_parts, bytes;
+    size_t peaks, rows, table, top, sum, mean_parts, norm, loss, start, signs, buckets, slots, row_grad, grad_parts, bytes;
     bool packed;                                        // the forward reads the table from planes made for the call
 };
 constexpr int kPeaksTable = 512, kPeaksRows = 64, kPeaksGrad = 64, kPeaks = kPeaksTable + kPeaksRows + kPeaksGrad;
 
-inline ClassPlan plan_of(const ClassShape& s, bool packed, bool forward, bool want_mean, bool want_grad_w) {
+inline ClassPlan plan_of(const ClassShape& s, bool packed, bool forward, bool want_rows, bool want_grad_w) {
     ClassPlan p{};
     size_t at = 0;
     auto room = [&at](size_t n) { const size_t a = at; at += (n + 255) / 256 * 256; return a; };
     const size_t depth = class_depth(s.D), T = padded_rows(s.T);
     p.peaks = room(kPeaks * 4);
-    p.rows = room(T * depth * 2 * class_planes(s.kind));
     if (forward) {
-        const bool narrow = narrow_depth((int)depth, s.kind);
+        const bool narrow = narrow_depth((int)depth);
         const size_t slices = forward_cut(s).slices(), stats = narrow ? slices : slices * kClassWaves;
         p.packed = packed;
         if (packed) p.table = room(padded_rows(s.V) * depth * 2 * class_planes(s.kind));
         p.top = room(stats * T * 4);
         p.sum = room(stats * T * 4);
-        if (want_mean) p.mean_parts = room(slices * T * depth * 4);
-        if (want_mean && !narrow) p.norm = room(T * 4);
+        if (want_rows) p.mean_parts = room(slices * T * depth * 4);
+        if (want_rows && !narrow) p.norm = room(T * 4);
     }
-    if (forward && want_mean) {                         // a backward that computes the mean again keeps it here
-        p.mean = room((size_t)s.T * s.D * 4);
+    if (forward && want_rows) {                         // a backward that computes the rows' gradients again keeps them here
+        p.row_grad = room((size_t)s.T * s.D * 4);
         p.loss = room(2 * T * 4);
     }
     if (want_grad_w) {
         const ClassCut c = gradient_cut(s);
+        p.rows = room(T * depth * 2 * class_planes(s.kind));
         p.start = room(T * 4);
         p.signs = room(T / kBlock * 4);
         p.buckets = room(T / kBlock * buckets_of(s.V, s.K).count * 4);

@@ -58,98 +58,98 @@ hipError_t gradient_of(const fsa::ClassArgs& a, hipStream_t st) {
                                                                                       : fsa::class_gradient_f16(a, st);
 }
 
-int forward(fsa::ClassArgs& a, float* loss, float* lse, float* mean, void* workspace, int64_t bytes, void* stream) {
+int forward(fsa::ClassArgs& a, float* loss, float* lse, float* row_grad, void* workspace, int64_t bytes, void* stream) {
     if (a.s.T > 0 && (!loss || !lse)) return FSA_ERR_NULL;
-    if (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(mean, 4)) return FSA_ERR_ALIGN;
+    if (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(row_grad, 4)) return FSA_ERR_ALIGN;
     if (a.s.T == 0) return FSA_OK;
-    a.plan = fsa::plan_of(a.s, packs(a), true, mean != nullptr, false);
+    a.plan = fsa::plan_of(a.s, packs(a), true, row_grad != nullptr, false);
     if (int rc = take_room(a, workspace, bytes)) return rc;
-    a.loss = loss; a.lse = lse; a.mean = mean;
+    a.loss = loss; a.lse = lse; a.row_grad = row_grad;
     (void)hipGetLastError();                            // an error that the caller left pending is not this call's
     return status_of(forward_of(a, static_cast<hipStream_t>(stream)));
 }
 
-int backward(fsa::ClassArgs& a, const float* grad_loss, const float* lse, const float* mean, void* grad_h, void* grad_w,
+int backward(fsa::ClassArgs& a, const float* grad_loss, const float* lse, const float* row_grad, void* grad_h, void* grad_w,
              void* workspace, int64_t bytes, void* stream) {
     if (a.s.T > 0 && (!grad_loss || !lse)) return FSA_ERR_NULL;
     const int eb = elem_bytes(a.s.kind);
-    if (!aligned(grad_loss, 4) || !aligned(lse, 4) || !aligned(mean, 4) || !aligned(grad_h, eb) || !aligned(grad_w, eb))
+    if (!aligned(grad_loss, 4) || !aligned(lse, 4) || !aligned(row_grad, 4) || !aligned(grad_h, eb) || !aligned(grad_w, eb))
         return FSA_ERR_ALIGN;
-    const bool again = grad_h && !mean && a.s.T > 0;
+    const bool again = grad_h && !row_grad && a.s.T > 0;
     a.plan = fsa::plan_of(a.s, again && packs(a), again, again, grad_w != nullptr);
     if (int rc = take_room(a, workspace, bytes)) return rc;
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(stream);
-    a.grad_loss = grad_loss; a.lse_in = lse; a.mean_in = mean; a.grad_h = grad_h; a.grad_w = grad_w;
+    a.grad_loss = grad_loss; a.lse_in = lse; a.row_grad_in = row_grad; a.grad_h = grad_h; a.grad_w = grad_w;
     if (again) {                                        // losses and log-sum-exps of this run are not wanted
         fsa::ClassArgs f = a;
-        f.mean = a.at<float>(a.plan.mean);
+        f.row_grad = a.at<float>(a.plan.row_grad);
         f.loss = a.at<float>(a.plan.loss); f.lse = f.loss + fsa::padded_rows(a.s.T);
-        a.mean_in = f.mean;
+        a.row_grad_in = f.row_grad;
         if (hipError_t e = forward_of(f, st)) return status_of(e);
     }
     return status_of(gradient_of(a, st));
 }
 
 // The sizes alone do not say where the table lies: room for a table off the grid.
-int64_t room_for(const fsa::ClassShape& s, bool forward, bool with_mean, bool with_grad_w) {
-    return (int64_t)fsa::plan_of(s, forward && fsa::forward_packs(s, false), forward, with_mean, with_grad_w).bytes;
+int64_t room_for(const fsa::ClassShape& s, bool forward, bool with_row_grad, bool with_grad_w) {
+    return (int64_t)fsa::plan_of(s, forward && fsa::forward_packs(s, false), forward, with_row_grad, with_grad_w).bytes;
 }
 
 }  // namespace
 
 extern "C" {
 
-int64_t fsa_class_fwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_mean) {
+int64_t fsa_class_fwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_row_grad) {
     if (!known(dtype) || !sizes_ok(T, V, D, K)) return 0;
-    return room_for({T, V, D, dtype, K}, true, with_mean != 0, false);
+    return room_for({T, V, D, dtype, K}, true, with_row_grad != 0, false);
 }
 
-int64_t fsa_class_bwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_mean, int with_grad_w) {
+int64_t fsa_class_bwd_workspace_bytes(int64_t T, int64_t V, int64_t D, int dtype, int32_t K, int with_row_grad, int with_grad_w) {
     if (!known(dtype) || !sizes_ok(T, V, D, K)) return 0;
-    return room_for({T, V, D, dtype, K}, with_mean != 0, with_mean != 0, with_grad_w != 0);
+    return room_for({T, V, D, dtype, K}, with_row_grad != 0, with_row_grad != 0, with_grad_w != 0);
 }
 
 int fsa_xent_fwd(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
                  int64_t T, int64_t V, int64_t D, float scale, const int32_t* targets,
-                 float* out_loss, float* out_lse, float* out_mean,
+                 float* out_loss, float* out_lse, float* out_row_grad,
                  void* workspace, int64_t workspace_bytes, void* stream) {
     fsa::ClassArgs a{};
     if (int rc = take(a, h, h_stride, w, w_stride, dtype, T, V, D, scale, 1.0f, targets, nullptr, FSA_F32, 1)) return rc;
-    return forward(a, out_loss, out_lse, out_mean, workspace, workspace_bytes, stream);
+    return forward(a, out_loss, out_lse, out_row_grad, workspace, workspace_bytes, stream);
 }
 
 int fsa_xent_bwd(const float* grad_loss, const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
                  int64_t T, int64_t V, int64_t D, float scale, const int32_t* targets,
-                 const float* lse, const float* mean, void* grad_h, void* grad_w,
+                 const float* lse, const float* row_grad, void* grad_h, void* grad_w,
                  void* workspace, int64_t workspace_bytes, void* stream) {
     fsa::ClassArgs a{};
     if (int rc = take(a, h, h_stride, w, w_stride, dtype, T, V, D, scale, 1.0f, targets, nullptr, FSA_F32, 1)) return rc;
-    return backward(a, grad_loss, lse, mean, grad_h, grad_w, workspace, workspace_bytes, stream);
+    return backward(a, grad_loss, lse, row_grad, grad_h, grad_w, workspace, workspace_bytes, stream);
 }
 
 int fsa_distill_fwd(const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
                     int64_t T, int64_t V, int64_t D, float scale, float temperature,
                     const int32_t* teacher_ids, const void* teacher_logits, int teacher_dtype, int32_t K,
-                    float* out_loss, float* out_lse, float* out_mean,
+                    float* out_loss, float* out_lse, float* out_row_grad,
                     void* workspace, int64_t workspace_bytes, void* stream) {
     fsa::ClassArgs a{};
     if (T > 0 && !teacher_logits) return FSA_ERR_NULL;
     if (int rc = take(a, h, h_stride, w, w_stride, dtype, T, V, D, scale, temperature, teacher_ids, teacher_logits, teacher_dtype, K))
         return rc;
-    return forward(a, out_loss, out_lse, out_mean, workspace, workspace_bytes, stream);
+    return forward(a, out_loss, out_lse, out_row_grad, workspace, workspace_bytes, stream);
 }
 
 int fsa_distill_bwd(const float* grad_loss, const void* h, int64_t h_stride, const void* w, int64_t w_stride, int dtype,
                     int64_t T, int64_t V, int64_t D, float scale, float temperature,
                     const int32_t* teacher_ids, const void* teacher_logits, int teacher_dtype, int32_t K,
-                    const float* lse, const float* mean, void* grad_h, void* grad_w,
+                    const float* lse, const float* row_grad, void* grad_h, void* grad_w,
                     void* workspace, int64_t workspace_bytes, void* stream) {
     fsa::ClassArgs a{};
     if (T > 0 && !teacher_logits) return FSA_ERR_NULL;
     if (int rc = take(a, h, h_stride, w, w_stride, dtype, T, V, D, scale, temperature, teacher_ids, teacher_logits, teacher_dtype, K))
         return rc;
-    return backward(a, grad_loss, lse, mean, grad_h, grad_w, workspace, workspace_bytes, stream);
+    return backward(a, grad_loss, lse, row_grad, grad_h, grad_w, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -27,8 +27,8 @@ struct ClassArgs {
     const int32_t* ids;                                 // [T,K] targets or the teacher's classes
     const void* teacher; int teacher_kind;              // [T,K] teacher logits, or null: one slot of weight one
     float inv_temperature;
-    float* loss; float* lse; float* mean;               // forward outputs (mean nullable)
-    const float* grad_loss; const float* lse_in; const float* mean_in;
+    float* loss; float* lse; float* row_grad;           // forward outputs (row_grad nullable)
+    const float* grad_loss; const float* lse_in; const float* row_grad_in;
     void* grad_h; void* grad_w;
     ClassCut cut; ClassPlan plan; char* ws;
     template <class T> __host__ __device__ T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
@@ -55,7 +55,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kKind = FSA_CLASS_KIND;                   // 0 fp32, 1 bfloat16, 2 fp16
-constexpr int NS = kKind == 0 ? 2 : 1;
+constexpr int NS = class_planes(kKind);
 constexpr bool kHalf = kKind != 1;                      // planes hold fp16 (bfloat16 otherwise)
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 // fp16 probabilities are kept as p * 2^14: 22 binades below the largest stay normal numbers.
@@ -127,6 +127,21 @@ __device__ __forceinline__ void planes_of(const Eight& e, float unit, u32x4 (&ou
     } else out[0] = __builtin_bit_cast(u32x4, e.v[0]);
 }
 
+// Four elements of a row as numbers, zero behind its D.
+__device__ __forceinline__ f32x4 load4(const Elem* row, int64_t D, int col) {
+    f32x4 x = {};
+    if (col + 4 <= D) {
+        Elem e[4];
+        __builtin_memcpy(e, row + col, sizeof(e));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = value(e[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (col + j < D) x[j] = value(row[col + j]);
+    }
+    return x;
+}
+
 // Chunk (of 8 elements) c of row r lies at chunk c ^ turn(r) of its row: 8 rows of one chunk (the first product's reads)
 // and 4 rows of two neighbouring ones (the transposing reads) then lie on different banks.
 __device__ __forceinline__ int turn(int r) { return 2 * (r & 3) + ((r >> 2) & 1); }
@@ -134,6 +149,18 @@ __device__ __forceinline__ int turn(int r) { return 2 * (r & 3) + ((r >> 2) & 1)
 __device__ __forceinline__ u32x2 read_transposed(const uint16_t* p) {
     using lds_s16x4 = __attribute__((address_space(3))) s16x4;
     return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
+}
+
+__device__ __forceinline__ void store_elem(void* p, int64_t i, float x) {
+    if constexpr (kKind == 0) static_cast<float*>(p)[i] = x;
+    else static_cast<uint16_t*>(p)[i] = (uint16_t)(pack2(x, 0.0f) & 0xffff);
+}
+__device__ __forceinline__ void store4(void* p, int64_t i, f32x4 x) {
+    if constexpr (kKind == 0) __builtin_memcpy(static_cast<float*>(p) + i, &x, 16);
+    else {
+        const u32x2 v = {pack2(x[0], x[1]), pack2(x[2], x[3])};
+        __builtin_memcpy(static_cast<uint16_t*>(p) + i, &v, 8);
+    }
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -164,19 +191,43 @@ __device__ __forceinline__ float block_peak(const float* peaks, int n, float* ro
     __syncthreads();
     return m;
 }
-struct Units { float w, h, g; };
+// Units of the whole table (the forward streams it past rows), of all rows, and of the losses' gradients.
 template <int WAVES = kClassWaves>
-__device__ __forceinline__ Units units(const ClassArgs& a, float* room, bool grad) {
-    Units u{1.0f, 1.0f, 1.0f};
+__device__ __forceinline__ float table_unit(const ClassArgs& a, float* room) {
+    if constexpr (kKind != 0) return 1.0f;
+    return unit_of(block_peak<WAVES>(a.at<const float>(a.plan.peaks), kPeaksTable, room));
+}
+struct Units { float h, g; };
+template <int WAVES = kClassWaves>
+__device__ __forceinline__ Units row_units(const ClassArgs& a, float* room) {
+    Units u{1.0f, 1.0f};
     const float* p = a.at<const float>(a.plan.peaks);
-    if constexpr (kKind == 0) {
-        u.w = unit_of(block_peak<WAVES>(p, kPeaksTable, room));
-        u.h = unit_of(block_peak<WAVES>(p + kPeaksTable, kPeaksRows, room));
-    }
-    if constexpr (kHalf) if (grad) u.g = unit_of(block_peak<WAVES>(p + kPeaksTable + kPeaksRows, kPeaksGrad, room));
+    if constexpr (kKind == 0) u.h = unit_of(block_peak<WAVES>(p + kPeaksTable, kPeaksRows, room));
+    if constexpr (kHalf) u.g = unit_of(block_peak<WAVES>(p + kPeaksTable + kPeaksRows, kPeaksGrad, room));
     return u;
 }
+// A held side has a unit of its own: that of a wave's 32 rows (`peak` of every lane, the largest finite |x| it holds).
+__device__ __forceinline__ float peak_of(const Eight& e) {
+    float m = 0.0f;
+    if constexpr (kKind == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m = fmaxf(m, finite_abs(e.v[i][j]));
+    }
+    return m;
+}
+__device__ __forceinline__ float wave_max(float m) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
+    return m;
+}
 
+// Whether row t has a slot, asked by one lane.
+__device__ __forceinline__ bool lane_lives(const ClassArgs& a, int64_t t) {
+    for (int j = 0; j < a.s.K; ++j) if (a.ids[t * a.s.K + j] >= 0) return true;
+    return false;
+}
 // Whether a row has a slot; the whole wave asks for one row.
 __device__ __forceinline__ bool row_lives(const ClassArgs& a, int64_t t, int lane) {
     bool some = false;
@@ -224,7 +275,8 @@ __global__ __launch_bounds__(kClassThreads) void class_peaks_kernel(ClassArgs a,
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// rows: planes of h (rows without a slot are zero, whatever they hold), and for the gradient what a row brings along
+// backward, ahead of the products: planes of h (rows without a slot are zero, whatever they hold), what a row brings
+// along, the slots sorted, and the gradient of h
 // ---------------------------------------------------------------------------------------------------------------
 // The teacher's weights of row t over its slots, in lanes 0..K-1 (K <= 64): a softmax over the slots that name a class.
 __device__ __forceinline__ float slot_weight(const ClassArgs& a, int64_t t, int lane, int& id, float& log_weight) {
@@ -267,18 +319,31 @@ struct Slot { uint32_t key; float pull; };
 
 constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / 64, kRowsEach = kBlock / kRowWaves;
 
+// Row t of grad_h, by a wave: what the forward made of it, times the gradient of its loss.
+__device__ __forceinline__ void write_row_grad(const ClassArgs& a, int64_t t, float g, bool lives, int lane) {
+    for (int d = lane; d < a.s.D; d += 64)
+        store_elem(a.grad_h, t * a.s.D + d, lives ? g * a.row_grad_in[t * a.s.D + d] : 0.0f);
+}
+__global__ __launch_bounds__(kClassThreads) void class_row_grad_kernel(ClassArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int64_t t = (int64_t)blockIdx.x * kClassWaves + (threadIdx.x >> 6);
+    if (t >= a.s.T) return;
+    int id;
+    float log_weight;
+    slot_weight(a, t, lane, id, log_weight);
+    write_row_grad(a, t, a.grad_loss[t], __any(id >= 0), lane);
+}
+
 // One workgroup per 32 rows, two to a wave.
 template <int DP>
-__global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, int64_t padded, bool grad) {
+__global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, int64_t padded) {
     __shared__ float room[kRowWaves];
     __shared__ uint32_t signs, counts[kMostBuckets], sums[kRowWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const ClassBuckets bk = buckets_of(a.s.V, a.s.K);
-    if (grad) {
-        if (threadIdx.x == 0) signs = 0;
-        for (int i = threadIdx.x; i < bk.count; i += kRowThreads) counts[i] = 0;
-    }
-    const Units u = units<kRowWaves>(a, room, grad);
+    if (threadIdx.x == 0) signs = 0;
+    for (int i = threadIdx.x; i < bk.count; i += kRowThreads) counts[i] = 0;
+    const Units u = row_units<kRowWaves>(a, room);
     uint16_t* planes = a.at<uint16_t>(a.plan.rows);
     __syncthreads();
     int ids[kRowsEach];
@@ -298,19 +363,17 @@ __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, in
 #pragma unroll
             for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + ((int64_t)n * padded + t) * DP + c * 8) = p[n];
         }
-        if (!grad) continue;
-        // P = |g| * softmax * units = 2^(scores*log2e + start), its sign apart
-        const float g = lives ? a.grad_loss[t] * u.g : 0.0f;
+        const float loss_grad = lives ? a.grad_loss[t] : 0.0f, g = loss_grad * u.g;
+        if (a.grad_h && t < a.s.T) write_row_grad(a, t, loss_grad, lives, lane);
+        // P = |g| * softmax = 2^(score * log2e + start), its sign apart
         if (lane == 0) {
-            const float to_log2 = a.scale * kLog2e / u.h / u.w;
-            a.at<float>(a.plan.start)[t] = lives ? (log2f(fabsf(g)) - a.lse_in[t] * kLog2e) / to_log2 : -__builtin_inff();
+            a.at<float>(a.plan.start)[t] = lives ? log2f(fabsf(g)) - a.lse_in[t] * kLog2e : -__builtin_inff();
             if (g < 0.0f) atomicOr(&signs, 1u << q);
         }
         ids[k] = id >= 0 && id < a.s.V && weight != 0.0f ? id : -1;
         pulls[k] = g * weight;
         if (ids[k] >= 0) atomicAdd(&counts[ids[k] / kBlock / bk.per], 1u);
     }
-    if (!grad) return;
     __syncthreads();
     // counts to places, four buckets to a thread
     static_assert(kMostBuckets <= 4 * kRowThreads, "a thread has four buckets");
@@ -407,13 +470,13 @@ struct SlotFeed {
 template <int DP>
 __global__ __launch_bounds__(kClassThreads) void class_pack_kernel(ClassArgs a, int64_t rows) {
     __shared__ float room[kClassWaves];
-    const Units u = units(a, room, false);
+    const float unit = table_unit(a, room);
     uint16_t* planes = a.at<uint16_t>(a.plan.table);
     for (int64_t q = (int64_t)blockIdx.x * kClassThreads + threadIdx.x; q < rows * (DP / 8); q += (int64_t)gridDim.x * kClassThreads) {
         const int64_t v = q / (DP / 8);
         const int c = (int)(q % (DP / 8)) * 8;
         u32x4 p[NS] = {};
-        if (v < a.s.V && c < a.s.D) planes_of(load8(static_cast<const Elem*>(a.w) + v * a.w_stride, a.s.D, c), u.w, p);
+        if (v < a.s.V && c < a.s.D) planes_of(load8(static_cast<const Elem*>(a.w) + v * a.w_stride, a.s.D, c), unit, p);
 #pragma unroll
         for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + ((int64_t)n * rows + v) * DP + c) = p[n];
     }
@@ -506,31 +569,50 @@ __device__ __forceinline__ void operand_of(const float (&p)[16], u32x4 (&out)[2]
 // Row that register i of a result stands for, in its block.
 __device__ __forceinline__ int row_of(int i, int lane) { return 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3); }
 
+// Columns [col0, col0 + 16 KS) of a row as B operands, and their unit: that of what `join` makes of the lanes' peaks.
+template <int KS, class Join>
+__device__ __forceinline__ float hold(const Elem* row, int64_t D, int col0, int lane, bool lives, u32x4 (&held)[KS][NS], Join join) {
+    Eight e[KS];
+    float peak = 0.0f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        const int col = col0 + 16 * ks + 8 * (lane >> 5);
+        e[ks] = Eight{};
+        if (lives && col < D) e[ks] = load8(row, D, col);
+        peak = fmaxf(peak, peak_of(e[ks]));
+    }
+    const float unit = kKind == 0 ? unit_of(join(peak)) : 1.0f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) planes_of(e[ks], unit, held[ks]);
+    return unit;
+}
+
+// The same of row `row` of h, behind the last row of that.  Nothing of a row reaches another one but the unit, so only that
+// looks at whether rows have slots.
+template <int KS, class Join>
+__device__ __forceinline__ float hold_rows(const ClassArgs& a, int64_t row, int col0, int lane, u32x4 (&held)[KS][NS], Join join) {
+    const int64_t t = row < a.s.T ? row : a.s.T - 1;
+    const Elem* h = static_cast<const Elem*>(a.h) + t * a.h_stride;
+    return hold<KS>(h, a.s.D, col0, lane, kKind != 0 || lane_lives(a, t), held, join);
+}
 // ---------------------------------------------------------------------------------------------------------------
 // forward: a wave holds 32 rows of h, the table streams by
 // ---------------------------------------------------------------------------------------------------------------
 template <int DP, int WY, bool MEAN, bool PACKED>
 __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_forward_kernel(ClassArgs a, int64_t padded) {
-    constexpr int NB = WY == 4 ? 4 : 2, MY = NB / WY, WX = kClassWaves / WY;   // blocks of a tile, a wave's own of them
+    constexpr int NB = blocks_per_tile(WY, DP, kKind), MY = NB / WY, WX = kClassWaves / WY;   // blocks of a tile, a wave's own of them
     using T = Tile<DP, NB * kBlock>;
     __shared__ __align__(16) uint16_t lds[2][NS * T::kPlane];
     __shared__ float room[kClassWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = wave % WX, y = wave / WX;
     const int64_t part = blockIdx.x % a.cut.parts, group = blockIdx.x / a.cut.parts;
-    const Units u = units(a, room, false);
-    const float to_log2 = a.scale * kLog2e / u.h / u.w;
+    const float table = table_unit(a, room);
     const int64_t first = a.cut.tiles * part / a.cut.parts, last = a.cut.tiles * (part + 1) / a.cut.parts;
     const int64_t row = (group * WX + x) * kBlock + (lane & 31);               // of h, held by this lane
     const bool live = (group * WX + x) * kBlock < padded;                      // wave-uniform
 
     u32x4 held[DP / 16][NS];
-#pragma unroll
-    for (int ks = 0; ks < DP / 16; ++ks)
-#pragma unroll
-        for (int n = 0; n < NS; ++n)
-            held[ks][n] = live ? *reinterpret_cast<const u32x4*>(a.at<const uint16_t>(a.plan.rows) + ((int64_t)n * padded + row) * DP +
-                                                                  16 * ks + 8 * (lane >> 5))
-                               : u32x4{};
+    const float to_log2 = a.scale * kLog2e / hold_rows<DP / 16>(a, row, 0, lane, held, [](float peak) { return wave_max(peak); }) / table;
 
     float ref = -1e30f, sum = 0.0f;                     // P = 2^(score - ref); ref = followed maximum - kLift
     f32x16 acc[MEAN ? DP / 32 : 1];
@@ -547,7 +629,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
     for (int64_t it = first; it < last; ++it) {
         uint16_t* tile = lds[(it - first) & 1];         // the other one may still be read
         if constexpr (PACKED) next.store(tile);
-        else next.store(tile, u.w);
+        else next.store(tile, table);
         __syncthreads();
         if (it + 1 < last) fetch(it + 1);
         if (!live) continue;
@@ -626,126 +708,125 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
     }
 }
 
-// One workgroup per row: the parts joined, the row's slots scored again (fp32 sums of the elements themselves), its loss.
-__global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a, int64_t padded, int depth, int slices, bool wide) {
-    __shared__ float room[kClassWaves], slot_q[64], slot_log[64], slot_loss[64];
-    __shared__ int slot_id[64];
+// One workgroup per row.  LOSS: the parts joined, the row's slots scored again (fp32 sums of the elements themselves), its
+// loss.  ROWS: the gradient of its loss, scale * (mean of the table's rows - sum of its slots' q w), from parts that carry
+// their own reference (LOSS as well) or that are normalised already.
+// The workgroup is cut into groups of `lanes` lanes that cover four elements each; slots and parts go around them.
+constexpr int kMostSlices = 4096;
+template <bool LOSS, bool ROWS>
+__global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a, int64_t padded, int depth, int slices, int lanes) {
+    __shared__ float room[kClassWaves], slot_q[64], slot_log[64], slot_z[64];
+    __shared__ int slot_id[64], alive;
+    __shared__ float weight[LOSS && ROWS ? kMostSlices : 1];
+    __shared__ __align__(16) f32x4 gathered[ROWS ? kClassThreads : 1];
     const int64_t t = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Units u = units(a, room, false);
+    const float* tops = a.at<const float>(a.plan.top);
+    const float* sums = a.at<const float>(a.plan.sum);
+    float top = -3e38f, sum = 1.0f;
+    if constexpr (LOSS)
+        for (int p = threadIdx.x; p < slices; p += kClassThreads) top = fmaxf(top, tops[p * padded + t]);
+    const float table = LOSS && ROWS ? table_unit(a, room) : 1.0f;
     if (wave == 0) {
         int id;
         float log_weight;
         const float q = slot_weight(a, t, lane, id, log_weight);
-        if (lane < a.s.K) { slot_q[lane] = q; slot_log[lane] = log_weight; slot_id[lane] = id; slot_loss[lane] = 0.0f; }
+        if (lane < a.s.K) { slot_q[lane] = q; slot_log[lane] = log_weight; slot_id[lane] = q != 0.0f ? id : -1; slot_z[lane] = 0.0f; }
         const bool lives = __any(id >= 0);
-        if (lane == 0) room[0] = lives ? 1.0f : 0.0f;
+        if (lane == 0) alive = lives;
+    }
+    if constexpr (LOSS) {
+        top = wave_max(top);
+        if (lane == 0) room[wave] = top;
     }
     __syncthreads();
-    const bool lives = room[0] != 0.0f;
-    __syncthreads();
-    if (!lives) {                                       // nothing of the row is used, whatever it holds
-        if (threadIdx.x == 0) {
+    if (!alive) {                                       // nothing of the row is used, whatever it holds
+        if (LOSS && threadIdx.x == 0) {
             a.loss[t] = 0.0f; a.lse[t] = 0.0f;
-            if (a.mean && wide) a.at<float>(a.plan.norm)[t] = __builtin_inff();
+            if (!ROWS && a.row_grad) a.at<float>(a.plan.norm)[t] = __builtin_inff();
         }
-        if (a.mean && !wide) for (int d = threadIdx.x; d < a.s.D; d += kClassThreads) a.mean[t * a.s.D + d] = 0.0f;
+        if constexpr (ROWS)
+            for (int d = threadIdx.x; d < a.s.D; d += kClassThreads) a.row_grad[t * a.s.D + d] = 0.0f;
         return;
     }
-    const float* tops = a.at<const float>(a.plan.top);
-    const float* sums = a.at<const float>(a.plan.sum);
-    float top = -3e38f;
-    for (int p = threadIdx.x; p < slices; p += kClassThreads) top = fmaxf(top, tops[p * padded + t]);
+    const int groups = kClassThreads / lanes, group = threadIdx.x / lanes, l = threadIdx.x % lanes;
+    const Elem* w = static_cast<const Elem*>(a.w);
+    if constexpr (LOSS) {
+        top = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
+        __syncthreads();
+        sum = 0.0f;
+        for (int p = threadIdx.x; p < slices; p += kClassThreads) {
+            const float e = exp2f(tops[p * padded + t] - top);
+            sum += sums[p * padded + t] * e;
+            if constexpr (ROWS) weight[p] = e;
+        }
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    if (lane == 0) room[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
-    __syncthreads();
-    float sum = 0.0f;
-    for (int p = threadIdx.x; p < slices; p += kClassThreads) sum += sums[p * padded + t] * exp2f(tops[p * padded + t] - top);
+        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
+        if (lane == 0) room[wave] = sum;
+        const Elem* h = static_cast<const Elem*>(a.h) + t * a.h_stride;
+        for (int j = group; j < a.s.K; j += groups) {
+            const int id = slot_id[j];
+            if (id < 0) continue;
+            float dot = id < a.s.V ? 0.0f : __builtin_nanf("");     // a class that there is not
+            if (id < a.s.V)
+                for (int c = 4 * l; c < a.s.D; c += 4 * lanes) {
+                    const f32x4 x = load4(h, a.s.D, c), y = load4(w + id * a.w_stride, a.s.D, c);
+                    dot += (x[0] * y[0] + x[1] * y[1]) + (x[2] * y[2] + x[3] * y[3]);
+                }
+            for (int d = 1; d < lanes; d *= 2) dot += __shfl_xor(dot, d);
+            if (l == 0) slot_z[j] = dot;
+        }
+        __syncthreads();
+        sum = (room[0] + room[1]) + (room[2] + room[3]);
+        if (wave == 0) {
+            const float log2_sum = top + log2f(sum), lse = log2_sum * kLn2;
+            float loss = lane < a.s.K && slot_id[lane] >= 0 ? slot_q[lane] * (slot_log[lane] + (lse - slot_z[lane] * a.scale)) : 0.0f;
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    if (lane == 0) room[wave] = sum;
-    __syncthreads();
-    sum = (room[0] + room[1]) + (room[2] + room[3]);
-    const float lse = (top + log2f(sum)) * kLn2;
-    if (a.mean && wide) {
-        if (threadIdx.x == 0) a.at<float>(a.plan.norm)[t] = top + log2f(sum) - kLift;
-    } else if (a.mean) {
-        const float* parts = a.at<const float>(a.plan.mean_parts);
-        for (int d = threadIdx.x; d < a.s.D; d += kClassThreads) {
-            float e = 0.0f;
-            for (int p = 0; p < slices; ++p) e += parts[(p * padded + t) * depth + d] * exp2f(tops[p * padded + t] - top);
-            a.mean[t * a.s.D + d] = e / sum / u.w;
+            for (int d = 1; d < 64; d *= 2) loss += __shfl_xor(loss, d);
+            if (lane == 0) {
+                a.loss[t] = loss; a.lse[t] = lse;
+                if (!ROWS && a.row_grad) a.at<float>(a.plan.norm)[t] = log2_sum - kLift;
+            }
         }
     }
-    const Elem* h = static_cast<const Elem*>(a.h) + t * a.h_stride;
-    for (int j = wave; j < a.s.K; j += kClassWaves) {
-        const int id = slot_id[j];
-        const float q = slot_q[j];
-        if (id < 0 || q == 0.0f) continue;
-        float dot = 0.0f;
-        if (id < a.s.V)
-            for (int d = lane; d < a.s.D; d += 64) dot += value(h[d]) * value(static_cast<const Elem*>(a.w)[id * a.w_stride + d]);
-        else dot = __builtin_nanf("");                  // a class that there is not
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) dot += __shfl_xor(dot, d);
-        if (lane == 0) slot_loss[j] = q * (slot_log[j] + (lse - dot * a.scale));
-    }
-    __syncthreads();
-    if (wave == 0) {
-        float l = lane < a.s.K ? slot_loss[lane] : 0.0f;
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d);
-        if (lane == 0) { a.loss[t] = l; a.lse[t] = lse; }
+    if constexpr (ROWS) {
+        const float* parts = a.at<const float>(a.plan.mean_parts);
+        const float back = 1.0f / sum / table;
+        for (int c0 = 0; c0 < a.s.D; c0 += 4 * lanes) {
+            const int c = c0 + 4 * l;
+            f32x4 e = {};
+            if (c < a.s.D) {
+#pragma unroll 4
+                for (int p = group; p < slices; p += groups) {
+                    const f32x4 x = *reinterpret_cast<const f32x4*>(parts + (p * padded + t) * depth + c);
+                    e += LOSS ? x * weight[p] : x;
+                }
+                e *= back;
+#pragma unroll 4
+                for (int j = group; j < a.s.K; j += groups) {
+                    const int id = slot_id[j];
+                    if (id >= 0 && id < a.s.V) e -= slot_q[j] * load4(w + id * a.w_stride, a.s.D, c);
+                }
+            }
+            gathered[threadIdx.x] = e;
+            __syncthreads();
+            if (group == 0 && c < a.s.D) {
+                for (int g = 1; g < groups; ++g) e += gathered[g * lanes + l];
+                for (int j = 0; j < 4; ++j) if (c + j < a.s.D) a.row_grad[t * a.s.D + c + j] = a.scale * e[j];
+            }
+            __syncthreads();
+        }
     }
 }
 
 // ---------------------------------------------------------------------------------------------------------------
 // gradients
 // ---------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ void store_elem(void* p, int64_t i, float x) {
-    if constexpr (kKind == 0) static_cast<float*>(p)[i] = x;
-    else static_cast<uint16_t*>(p)[i] = (uint16_t)(pack2(x, 0.0f) & 0xffff);
-}
-__device__ __forceinline__ void store4(void* p, int64_t i, f32x4 x) {
-    if constexpr (kKind == 0) __builtin_memcpy(static_cast<float*>(p) + i, &x, 16);
-    else {
-        const u32x2 v = {pack2(x[0], x[1]), pack2(x[2], x[3])};
-        __builtin_memcpy(static_cast<uint16_t*>(p) + i, &v, 8);
-    }
-}
-
-// grad_h[t] = g * scale * (mean[t] - sum_j q_j w[id_j]), one workgroup per row.
-__global__ __launch_bounds__(kClassThreads) void class_pull_kernel(ClassArgs a) {
-    __shared__ float slot_q[64];
-    __shared__ int slot_id[64], alive;
-    const int64_t t = blockIdx.x;
-    const int lane = threadIdx.x & 63;
-    if (threadIdx.x < 64) {
-        int id;
-        float log_weight;
-        const float q = slot_weight(a, t, lane, id, log_weight);
-        if (lane < a.s.K) { slot_q[lane] = q; slot_id[lane] = q != 0.0f && id < a.s.V ? id : -1; }
-        const bool some = __any(id >= 0);
-        if (lane == 0) alive = some;
-    }
-    __syncthreads();
-    const float g = alive ? a.grad_loss[t] * a.scale : 0.0f;
-    for (int d = threadIdx.x; d < a.s.D; d += kClassThreads) {
-        float e = alive ? a.mean_in[t * a.s.D + d] : 0.0f;
-        for (int j = 0; j < a.s.K; ++j)
-            if (slot_id[j] >= 0) e -= slot_q[j] * value(static_cast<const Elem*>(a.w)[slot_id[j] * a.w_stride + d]);
-        store_elem(a.grad_h, t * a.s.D + d, alive ? g * e : 0.0f);
-    }
-}
-
 // A wave holds 32 classes, the rows stream by:
 //   grad_w[v] = scale * sum_t g_t (p[t,v] - sum over t's slots j that name v of q_j) h[t]
 template <int DP, int WY>
 __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) void class_gradient_kernel(ClassArgs a, int64_t padded) {
-    constexpr int NB = WY == 4 ? 4 : 2, MY = NB / WY, WX = kClassWaves / WY;
+    constexpr int NB = blocks_per_tile(WY, DP, kKind), MY = NB / WY, WX = kClassWaves / WY;
     using T = Tile<DP, NB * kBlock>;
     __shared__ __align__(16) uint16_t lds[2][NS * T::kPlane];
     __shared__ __align__(16) float starts[2][NB * kBlock];
@@ -753,21 +834,15 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
     __shared__ float room[kClassWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = wave % WX, y = wave / WX;
     const int64_t part = blockIdx.x % a.cut.parts, group = blockIdx.x / a.cut.parts;
-    const Units u = units(a, room, true);
-    const float to_log2 = a.scale * kLog2e / u.h / u.w;
+    const Units u = row_units(a, room);
     const int64_t first = a.cut.tiles * part / a.cut.parts, last = a.cut.tiles * (part + 1) / a.cut.parts;
     const int64_t v0 = (group * WX + x) * kBlock, v = v0 + (lane & 31);
     const bool live = v0 < a.s.V;                       // wave-uniform
-    const Elem* w = static_cast<const Elem*>(a.w) + (v < a.s.V ? v : a.s.V - 1) * a.w_stride;
 
     u32x4 held[DP / 16][NS];
-#pragma unroll
-    for (int ks = 0; ks < DP / 16; ++ks) {
-        const int col = 16 * ks + 8 * (lane >> 5);
-#pragma unroll
-        for (int n = 0; n < NS; ++n) held[ks][n] = u32x4{};
-        if (live && col < a.s.D) planes_of(load8(w, a.s.D, col), u.w, held[ks]);
-    }
+    const float to_log2 = a.scale * kLog2e / u.h /
+        hold<DP / 16>(static_cast<const Elem*>(a.w) + (v < a.s.V ? v : a.s.V - 1) * a.w_stride, a.s.D, 0, lane, true, held,
+                      [](float peak) { return wave_max(peak); });
     f32x16 acc[DP / 32];
 #pragma unroll
     for (auto& f : acc) f = f32x16{};
@@ -804,13 +879,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
             const int b = y * MY + m;
             const int64_t t0 = (it * NB + b) * kBlock;
             if (t0 >= a.s.T) continue;
-            f32x16 score;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const f32x4 s = *reinterpret_cast<const f32x4*>(&starts[half][b * kBlock + 8 * i + 4 * (lane >> 5)]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) score[4 * i + j] = s[j];
-            }
+            f32x16 score = {};
 #pragma unroll
             for (int ks = 0; ks < DP / 16; ++ks) {
                 u32x4 f[NS];
@@ -819,13 +888,18 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
             }
             float p[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(score[i] * to_log2);
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 s = *reinterpret_cast<const f32x4*>(&starts[half][b * kBlock + 8 * i + 4 * (lane >> 5)]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) p[4 * i + j] = __builtin_amdgcn_exp2f(fmaf(score[4 * i + j], to_log2, s[j]));
+            }
             if (feed.now[m].negative()) {
                 const uint32_t signs = a.at<const uint32_t>(a.plan.signs)[t0 / kBlock];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) if (signs >> row_of(i, lane) & 1) p[i] = -p[i];
             }
-            if (feed.gather(m, t0 / kBlock, lane, cell)) {
+            const bool hit = feed.gather(m, t0 / kBlock, lane, cell);
+            if (hit) {
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -845,6 +919,26 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
                     T::columns(tile, b, s, db, lane, f);
                     acc[db] = matmul(f, q[s], acc[db]);
                 }
+            // what a class's own rows pull at is most of its gradient: where there are some, what rounding took of it follows
+            if (NS == 1 && hit) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        p[8 * s + 2 * j] -= low2(q[s][0][j]);
+                        p[8 * s + 2 * j + 1] -= high2(q[s][0][j]);
+                    }
+                }
+                operand_of(p, q);
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int db = 0; db < DP / 32; ++db) {
+                        u32x4 f[NS];
+                        T::columns(tile, b, s, db, lane, f);
+                        acc[db] = matmul(f, q[s], acc[db]);
+                    }
+            }
         }
     }
     if (!live) return;
@@ -882,7 +976,7 @@ template <int Q>
 struct Quarter {
     static constexpr int kChunks = Q / 8, kStride = ((kChunks + 1 + 5) / 8 * 8 + 2) * 8;   // elements from row to row
     static constexpr int kPlane = kBlock * kStride, kEach = kBlock * kChunks / 64;
-    static_assert(kStride >= Q + 8 && (kBlock * kChunks) % 64 == 0, "a row and its shift fit, lanes share rows evenly");
+    static_assert(kStride >= Q + 16 && (kBlock * kChunks) % 64 == 0, "a row, its shift and a spare chunk fit, lanes share rows evenly");
     static __device__ __forceinline__ int place(int r, int c) { return r * kStride + (c + ((r >> 2) & 1)) * 8; }
     static __device__ __forceinline__ void rows(const uint16_t* lds, int ks, int lane, u32x4 (&out)[NS]) {
 #pragma unroll
@@ -911,12 +1005,16 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
     __shared__ __align__(16) uint16_t quarters[kClassWaves][NS * S::kPlane];
     constexpr int MEETS = MODE == kStats && Q * NS < 512 ? 2 : 1;      // one more barrier a tile where only one fits
     __shared__ __align__(16) f32x4 partial[MEETS][kClassWaves][4][64];
-    __shared__ __align__(16) u32x2 shared_p[MODE == kStats ? 1 : NS][2][64][2];
+    constexpr int PS = MODE == kStats ? 1 : MODE == kGradient ? 2 : NS;   // planes of P; 16-bit types use the second after a hit
+    __shared__ __align__(16) u32x2 shared_p[PS][2][64][2];
+    // the tile that last had a slot of these classes, in a corner of LDS that no row reaches
+    auto& hit = *reinterpret_cast<int64_t __attribute__((may_alias))*>(quarters[0] + S::kStride - 8);
     __shared__ float cells[MODE == kGradient ? kBlock * kBlock : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col0 = wave * Q;
     const int64_t part = blockIdx.x % a.cut.parts, group = blockIdx.x / a.cut.parts;
-    const Units u = units(a, reinterpret_cast<float*>(partial), MODE == kGradient);
-    const float to_log2 = a.scale * kLog2e / u.h / u.w;
+    float* room = reinterpret_cast<float*>(partial);
+    const Units u = MODE == kGradient ? row_units(a, room) : Units{1.0f, 1.0f};
+    const float table = MODE == kGradient ? 1.0f : table_unit(a, room);
     const int64_t first = a.cut.tiles * part / a.cut.parts, last = a.cut.tiles * (part + 1) / a.cut.parts;
     const int64_t x0 = group * kBlock, x = x0 + (lane & 31);
     const Elem* w = static_cast<const Elem*>(a.w);
@@ -924,20 +1022,21 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
     uint16_t* lds = quarters[wave];
 
     u32x4 held[Q / 16][NS];
-#pragma unroll
-    for (int ks = 0; ks < Q / 16; ++ks) {
-        const int col = col0 + 16 * ks + 8 * (lane >> 5);
-        if constexpr (MODE == kGradient) {
-#pragma unroll
-            for (int n = 0; n < NS; ++n) held[ks][n] = u32x4{};
-            if (col < a.s.D) planes_of(load8(w + (x < a.s.V ? x : a.s.V - 1) * a.w_stride, a.s.D, col), u.w, held[ks]);
-        } else {
-#pragma unroll
-            for (int n = 0; n < NS; ++n) held[ks][n] = *reinterpret_cast<const u32x4*>(planes + ((int64_t)n * padded + x) * DEPTH + col);
-        }
-    }
+    auto join = [&](float peak) {                       // one unit for the four quarters
+        peak = wave_max(peak);
+        if (lane == 0) room[wave] = peak;
+        __syncthreads();
+        peak = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
+        __syncthreads();
+        return peak;
+    };
+    const float held_unit = MODE == kGradient
+        ? hold<Q / 16>(w + (x < a.s.V ? x : a.s.V - 1) * a.w_stride, a.s.D, col0, lane, true, held, join)
+        : hold_rows<Q / 16>(a, x, col0, lane, held, join);
+    const float to_log2 = a.scale * kLog2e / u.h / held_unit / table;
     if constexpr (MODE == kGradient) {
         for (int i = threadIdx.x; i < kBlock * kBlock; i += kClassThreads) cells[i] = 0.0f;
+        if (threadIdx.x == 0) hit = -1;
         __syncthreads();
     }
     const float norm = MODE == kMean && x < a.s.T ? a.at<const float>(a.plan.norm)[x] : __builtin_inff();
@@ -985,7 +1084,7 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
             if constexpr (FROM_PLANES) {
 #pragma unroll
                 for (int n = 0; n < NS; ++n) p[n] = next.p[n][i];
-            } else planes_of(next.e[i], u.w, p);
+            } else planes_of(next.e[i], table, p);
 #pragma unroll
             for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(lds + n * S::kPlane + S::place(r, c)) = p[n];
         }
@@ -1003,7 +1102,8 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
 #pragma unroll
         for (int i = 0; i < 4; ++i) meet[wave][i][lane] = f32x4{score[4 * i], score[4 * i + 1], score[4 * i + 2], score[4 * i + 3]};
         const int64_t y0 = it * kBlock;
-        if (MODE == kGradient && wave == 0) feed.gather(0, it, lane, cells);
+        if (MODE == kGradient && wave == 0)
+            if (feed.gather(0, it, lane, cells) && lane == 0) hit = it;
         __syncthreads();
         f32x4 z = (meet[0][wave][lane] + meet[1][wave][lane]) + (meet[2][wave][lane] + meet[3][wave][lane]);   // rows 8*wave + 4*(lane/32) + j
         const int y = 8 * wave + 4 * (lane >> 5);
@@ -1030,23 +1130,27 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
                 for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(z[j], to_log2, -norm));
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f((z[j] + start[j]) * to_log2);
+                for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(z[j], to_log2, start[j]));
                 const uint32_t signs = a.at<const uint32_t>(a.plan.signs)[it];
                 if (signs) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j) if (signs >> (y + j) & 1) p[j] = -p[j];
                 }
+                if (hit == it) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    float& c = cells[(y + j) * kBlock + (lane & 31)];
-                    p[j] -= c;
-                    if (c != 0.0f) c = 0.0f;
+                    for (int j = 0; j < 4; ++j) {
+                        float& c = cells[(y + j) * kBlock + (lane & 31)];
+                        p[j] -= c;
+                        c = 0.0f;
+                    }
                 }
             }
             const uint32_t p0 = pack2(p[0], p[1]), p1 = pack2(p[2], p[3]);
             shared_p[0][wave >> 1][lane][wave & 1] = u32x2{p0, p1};
-            if constexpr (NS == 2)
-                shared_p[1][wave >> 1][lane][wave & 1] = u32x2{pack2(p[0] - low2(p0), p[1] - high2(p0)), pack2(p[2] - low2(p1), p[3] - high2(p1))};
+            const bool rest = MODE == kGradient && NS == 1 && hit == it;        // as in the narrow kernel
+            if (NS == 2 || rest)
+                shared_p[PS - 1][wave >> 1][lane][wave & 1] =
+                    u32x2{pack2(p[0] - low2(p0), p[1] - high2(p0)), pack2(p[2] - low2(p1), p[3] - high2(p1))};
             __syncthreads();
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -1058,6 +1162,15 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
                     u32x4 f[NS];
                     S::columns(lds, s, db, lane, f);
                     acc[db] = matmul(f, b, acc[db]);
+                }
+                if (rest) {
+                    b[0] = *reinterpret_cast<const u32x4*>(&shared_p[PS - 1][s][lane][0]);
+#pragma unroll
+                    for (int db = 0; db < Q / 32; ++db) {
+                        u32x4 f[NS];
+                        S::columns(lds, s, db, lane, f);
+                        acc[db] = matmul(f, b, acc[db]);
+                    }
                 }
             }
         }
@@ -1073,7 +1186,7 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
             a.at<float>(a.plan.sum)[at] = sum;
         }
     } else {
-        const float back = MODE == kGradient ? a.scale / u.h / u.g : exp2f(-kLift) / u.w;
+        const float back = MODE == kGradient ? a.scale / u.h / u.g : exp2f(-kLift) / table;
         const int64_t rows = MODE == kGradient ? ceil_div(a.s.V, kBlock) * kBlock : padded;
         const bool joined = MODE == kMean || a.cut.parts > 1;
         float* out = a.at<float>(MODE == kGradient ? a.plan.grad_parts : a.plan.mean_parts);
@@ -1093,22 +1206,17 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
     }
 }
 
-// Parts of a result of n rows, `rows` of them in a part, joined in part order.
-template <class Out>
-__global__ __launch_bounds__(kClassThreads) void class_join_kernel(const float* parts, Out* out, int64_t n, int64_t D, int64_t rows,
-                                                                    int depth, int slices) {
-    for (int64_t i = (int64_t)blockIdx.x * kClassThreads + threadIdx.x; i < n * D; i += (int64_t)gridDim.x * kClassThreads) {
-        const int64_t r = i / D, d = i % D;
+// Parts of grad_w joined in part order.
+__global__ __launch_bounds__(kClassThreads) void class_join_kernel(ClassArgs a, int depth, int slices) {
+    const int64_t rows = ceil_div(a.s.V, kBlock) * kBlock, n = a.s.V * a.s.D;
+    const float* parts = a.at<const float>(a.plan.grad_parts);
+    for (int64_t i = (int64_t)blockIdx.x * kClassThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kClassThreads) {
+        const int64_t v = i / a.s.D, d = i % a.s.D;
         float g = 0.0f;
-        for (int p = 0; p < slices; ++p) g += parts[(p * rows + r) * depth + d];
-        if constexpr (sizeof(Out) == 4) out[i] = g;
-        else store_elem(out, i, g);
+#pragma unroll 8
+        for (int p = 0; p < slices; ++p) g += parts[(p * rows + v) * depth + d];
+        store_elem(a.grad_w, i, g);
     }
-}
-template <class Out>
-void join(const float* parts, Out* out, int64_t n, int64_t D, int64_t rows, int depth, int slices, hipStream_t stream) {
-    const int64_t grid = ceil_div(n * D, kClassThreads);
-    class_join_kernel<Out><<<(unsigned)(grid < 4096 ? grid : 4096), kClassThreads, 0, stream>>>(parts, out, n, D, rows, depth, slices);
 }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -1127,74 +1235,75 @@ template <class F> hipError_t with_depth(int depth, F f) {
     return hipGetLastError();
 }
 
-hipError_t launch_rows(const ClassArgs& a, bool grad, hipStream_t stream) {
-    const int64_t padded = padded_rows(a.s.T);
-    const int table = kKind == 0 ? kPeaksTable : 0, rows = kKind == 0 ? kPeaksRows : 0, g = kHalf && grad ? kPeaksGrad : 0;
-    if (table + rows + g) class_peaks_kernel<<<table + rows + g, kClassThreads, 0, stream>>>(a, table, rows, g);
-    return with_depth(class_depth(a.s.D), [&](auto dp) {
-        if (padded) class_rows_kernel<dp()><<<padded / kBlock, kRowThreads, 0, stream>>>(a, padded, grad);
-    });
-}
-
 template <int DP, bool MEAN, bool PACKED> void launch_forward(const ClassArgs& a, int64_t padded, hipStream_t stream) {
     const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
-    if constexpr (!narrow_depth(DP, kKind))
+    if constexpr (!narrow_depth(DP))
         class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats, PACKED><<<grid, kClassThreads, 0, stream>>>(a, padded);
     else if (a.cut.wy == 1) class_forward_kernel<DP, 1, MEAN, PACKED><<<grid, kClassThreads, 0, stream>>>(a, padded);
     else if constexpr (!PACKED) {                       // (few rows never pack)
         if (a.cut.wy == 2) class_forward_kernel<DP, 2, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
-        else class_forward_kernel<DP, 4, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
+        else if constexpr (DP * NS <= 256) class_forward_kernel<DP, 4, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
     }
 }
 template <int DP> void launch_gradient(const ClassArgs& a, int64_t padded, hipStream_t stream) {
     const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
-    if constexpr (!narrow_depth(DP, kKind)) class_wide_kernel<DP / kClassWaves, kGradient, true><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    if constexpr (!narrow_depth(DP)) class_wide_kernel<DP / kClassWaves, kGradient, true><<<grid, kClassThreads, 0, stream>>>(a, padded);
     else if (a.cut.wy == 1) class_gradient_kernel<DP, 1><<<grid, kClassThreads, 0, stream>>>(a, padded);
     else if (a.cut.wy == 2) class_gradient_kernel<DP, 2><<<grid, kClassThreads, 0, stream>>>(a, padded);
-    else class_gradient_kernel<DP, 4><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    else if constexpr (DP * NS <= 256) class_gradient_kernel<DP, 4><<<grid, kClassThreads, 0, stream>>>(a, padded);
 }
 
 hipError_t forward(ClassArgs a, hipStream_t stream) {
     const int64_t padded = padded_rows(a.s.T);
     const int depth = class_depth(a.s.D);
-    const bool wide = !narrow_depth(depth, kKind);
+    const bool wide = !narrow_depth(depth), rows = a.row_grad != nullptr;
     a.cut = forward_cut(a.s);
     const int slices = (int)a.cut.slices();
-    if (hipError_t e = launch_rows(a, false, stream)) return e;
+    int lanes = 1;
+    while (lanes < 64 && 4 * lanes < a.s.D) lanes *= 2;
     auto run = [&](bool mean) {
         return with_depth(depth, [&](auto dp) {
             if (a.plan.packed) mean ? launch_forward<dp(), true, true>(a, padded, stream) : launch_forward<dp(), false, true>(a, padded, stream);
             else mean ? launch_forward<dp(), true, false>(a, padded, stream) : launch_forward<dp(), false, false>(a, padded, stream);
         });
     };
+    if constexpr (kKind == 0) class_peaks_kernel<<<kPeaksTable, kClassThreads, 0, stream>>>(a, kPeaksTable, 0, 0);
     if (a.plan.packed) {
-        const int64_t rows = padded_rows(a.s.V), grid = ceil_div(rows * depth / 8, kClassThreads);
+        const int64_t table = padded_rows(a.s.V), grid = ceil_div(table * depth / 8, kClassThreads);
         if (hipError_t e = with_depth(depth, [&](auto dp) {
-                class_pack_kernel<dp()><<<(unsigned)(grid < 8192 ? grid : 8192), kClassThreads, 0, stream>>>(a, rows);
+                class_pack_kernel<dp()><<<(unsigned)(grid < 8192 ? grid : 8192), kClassThreads, 0, stream>>>(a, table);
             })) return e;
     }
-    if (hipError_t e = run(a.mean && !wide)) return e;
-    class_finish_kernel<<<(unsigned)a.s.T, kClassThreads, 0, stream>>>(a, padded, depth, wide ? slices * kClassWaves : slices, wide);
-    if (!a.mean || !wide) return hipGetLastError();
+    if (hipError_t e = run(rows && !wide)) return e;
+    const unsigned T = (unsigned)a.s.T;
+    if (rows && !wide) class_finish_kernel<true, true><<<T, kClassThreads, 0, stream>>>(a, padded, depth, slices, lanes);
+    else class_finish_kernel<true, false><<<T, kClassThreads, 0, stream>>>(a, padded, depth, wide ? slices * kClassWaves : slices, lanes);
+    if (!rows || !wide) return hipGetLastError();
     if (hipError_t e = run(true)) return e;
-    join(a.at<const float>(a.plan.mean_parts), a.mean, a.s.T, a.s.D, padded, depth, slices, stream);
+    class_finish_kernel<false, true><<<T, kClassThreads, 0, stream>>>(a, padded, depth, slices, lanes);
     return hipGetLastError();
 }
 
 hipError_t gradient(ClassArgs a, hipStream_t stream) {
     const int64_t padded = padded_rows(a.s.T);
     const int depth = class_depth(a.s.D);
-    if (a.grad_h && a.s.T) {
-        class_pull_kernel<<<(unsigned)a.s.T, kClassThreads, 0, stream>>>(a);
-        if (hipError_t e = hipGetLastError()) return e;
+    if (!a.grad_w) {
+        if (a.grad_h && a.s.T) class_row_grad_kernel<<<(unsigned)ceil_div(a.s.T, kClassWaves), kClassThreads, 0, stream>>>(a);
+        return hipGetLastError();
     }
-    if (!a.grad_w) return hipSuccess;
     a.cut = gradient_cut(a.s);
-    if (hipError_t e = launch_rows(a, true, stream)) return e;
+    if constexpr (kHalf) {
+        const int rows = kKind == 0 ? kPeaksRows : 0;
+        class_peaks_kernel<<<rows + kPeaksGrad, kClassThreads, 0, stream>>>(a, 0, rows, kPeaksGrad);
+    }
+    if (hipError_t e = with_depth(depth, [&](auto dp) {
+            if (padded) class_rows_kernel<dp()><<<padded / kBlock, kRowThreads, 0, stream>>>(a, padded);
+        })) return e;
     if (hipError_t e = with_depth(depth, [&](auto dp) { launch_gradient<dp()>(a, padded, stream); })) return e;
-    if (a.cut.slices() > 1)
-        join(a.at<const float>(a.plan.grad_parts), static_cast<Elem*>(a.grad_w), a.s.V, a.s.D, ceil_div(a.s.V, kBlock) * kBlock,
-             depth, (int)a.cut.slices(), stream);
+    if (a.cut.slices() > 1) {
+        const int64_t n = ceil_div(a.s.V * a.s.D, kClassThreads);
+        class_join_kernel<<<(unsigned)(n < 4096 ? n : 4096), kClassThreads, 0, stream>>>(a, depth, (int)a.cut.slices());
+    }
     return hipGetLastError();
 }
 

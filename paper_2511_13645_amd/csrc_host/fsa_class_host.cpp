@@ -138,13 +138,13 @@ bool class_call(ClassCall& c, PyObject* const* a) {
     return stream_of(*h, &c.stream);
 }
 
-// (loss, lse, mean or nothing) of a call, or a status.
-int class_forward(const ClassCall& c, bool emit_mean, Tensor (&o)[3]) {
+// (loss, lse, row_grad or nothing) of a call, or a status.
+int class_forward(const ClassCall& c, bool emit_row_grad, Tensor (&o)[3]) {
     const auto f = at::TensorOptions().dtype(at::kFloat).device(c.h.device());
-    const int64_t need = abi.fsa_class_fwd_workspace_bytes(c.T, c.V, c.D, c.code, c.K, emit_mean);
+    const int64_t need = abi.fsa_class_fwd_workspace_bytes(c.T, c.V, c.D, c.code, c.K, emit_row_grad);
     o[0] = at::empty({c.T}, f);
     o[1] = at::empty({c.T}, f);
-    if (emit_mean) o[2] = at::empty({c.T, c.D}, f);
+    if (emit_row_grad) o[2] = at::empty({c.T, c.D}, f);
     const Tensor ws = at::empty({need}, f.dtype(at::kByte));       // (may go once the call is queued: same stream)
     if (!c.logits.defined())
         return abi.fsa_xent_fwd(data(c.h), c.h_stride, data(c.w), c.w_stride, c.code, c.T, c.V, c.D, c.scale, data<int32_t>(c.ids),
@@ -158,9 +158,9 @@ struct Refused : std::exception { int status; explicit Refused(int s) : status(s
 
 // The differentiable loss.  Its backward runs on the stream of its forward, which is the one that autograd then makes current.
 struct ClassLoss : torch::autograd::Function<ClassLoss> {
-    static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& h, const Tensor& w, const ClassCall& c, bool emit_mean) {
+    static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& h, const Tensor& w, const ClassCall& c, bool emit_row_grad) {
         Tensor o[3];
-        if (const int rc = class_forward(c, emit_mean, o)) throw Refused(rc);
+        if (const int rc = class_forward(c, emit_row_grad, o)) throw Refused(rc);
         ctx->save_for_backward({h, w, c.ids, c.logits, o[1], o[2]});
         auto& d = ctx->saved_data;
         d["temperature"] = (double)c.temperature;
@@ -170,7 +170,7 @@ struct ClassLoss : torch::autograd::Function<ClassLoss> {
     }
     static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
         const auto v = ctx->get_saved_variables();
-        const Tensor &h = v[0], &w = v[1], &ids = v[2], &logits = v[3], &lse = v[4], &mean = v[5];
+        const Tensor &h = v[0], &w = v[1], &ids = v[2], &logits = v[3], &lse = v[4], &row_grad = v[5];
         const bool again = c10::GradMode::is_enabled() && grads[0].requires_grad();
         torch::autograd::variable_list out(4);
         {
@@ -183,15 +183,15 @@ struct ClassLoss : torch::autograd::Function<ClassLoss> {
             const auto rows = at::TensorOptions().dtype(h.dtype()).device(h.device());
             if (want_h) out[0] = at::empty({T, D}, rows);
             if (want_w) out[1] = at::empty({V, D}, rows);
-            const int64_t need = abi.fsa_class_bwd_workspace_bytes(T, V, D, code, K, want_h && !mean.defined(), want_w);
+            const int64_t need = abi.fsa_class_bwd_workspace_bytes(T, V, D, code, K, want_h && !row_grad.defined(), want_w);
             const Tensor ws = at::empty({need}, rows.dtype(at::kByte));
             const float temperature = (float)ctx->saved_data["temperature"].toDouble(), scale = (float)ctx->saved_data["scale"].toDouble();
             void* stream = reinterpret_cast<void*>((intptr_t)ctx->saved_data["stream"].toInt());
             const int rc = !logits.defined()
                 ? abi.fsa_xent_bwd(data<float>(g), data(h), hs, data(w), wst, code, T, V, D, scale, data<int32_t>(ids),
-                                   data<float>(lse), data<float>(mean), data(out[0]), data(out[1]), data(ws), need, stream)
+                                   data<float>(lse), data<float>(row_grad), data(out[0]), data(out[1]), data(ws), need, stream)
                 : abi.fsa_distill_bwd(data<float>(g), data(h), hs, data(w), wst, code, T, V, D, scale, temperature, data<int32_t>(ids),
-                                      data(logits), float_code(logits), K, data<float>(lse), data<float>(mean), data(out[0]), data(out[1]),
+                                      data(logits), float_code(logits), K, data<float>(lse), data<float>(row_grad), data(out[0]), data(out[1]),
                                       data(ws), need, stream);
             TORCH_CHECK(rc == FSA_OK, "the backward of a class loss was refused (status ", rc, ")");
         }
@@ -205,7 +205,7 @@ struct ClassLoss : torch::autograd::Function<ClassLoss> {
     }
 };
 
-// (h, w, ids, logits | None, temperature, scale, emit_mean) -> (loss, lse, mean | None)
+// (h, w, ids, logits | None, temperature, scale, emit_row_grad) -> (loss, lse, row_grad | None)
 PyObject* class_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 7 || !PyBool_Check(a[6])) Py_RETURN_NONE;
     return or_none([&]() -> PyObject* {

@@ -48,7 +48,7 @@ def reference(h, w, ids, logits=None, temperature=1.0, scale=1.0, g=None):
     picked = z.gather(1, ids.clamp_min(0))
     loss = torch.where(q > 0, q * (q.clamp_min(1e-300).log() - picked + lse[:, None]), 0.0).sum(1)
     dense_q = torch.zeros_like(z).scatter_add_(1, ids.clamp_min(0), q)
-    r = {"loss": torch.where(some, loss, 0.0), "lse": torch.where(some, lse, 0.0), "mean": torch.where(some[:, None], p @ w, 0.0)}
+    r = {"loss": torch.where(some, loss, 0.0), "lse": torch.where(some, lse, 0.0), "row_grad": torch.where(some[:, None], (p - dense_q) @ w * s, 0.0)}
     if g is not None:
         g = torch.where(some, g.double(), 0.0)
         d = g[:, None] * (p - dense_q) * s
@@ -67,11 +67,11 @@ def bounds(dtype, x, g=None):
     b = {"lse": dlse, "loss": 2 * dlse + 16 * 2.0 ** -24 * (x["lse"].abs() + x["z"].abs().amax(1) + 64)}
     u, lift = U_P[dtype], (0.0 if dtype == "bf16" else 2.0 ** -39)
     delta = (dz + dlse + 2.0 ** -20)[:, None]
-    b["mean"] = (u + delta + (V + 16) * 2.0 ** -24) * (x["p"] @ w) + lift * 2 * w.sum(0)
+    both = x["p"] + x["q"]
+    b["row_grad"] = s * ((u + delta + (V + 80) * 2.0 ** -24) * (both @ w) + lift * 2 * w.sum(0))
     if g is not None:
         g = torch.where(x["some"], g.double().abs(), 0.0)
-        both = x["p"] + x["q"]
-        b["grad_h"] = s * g[:, None] * (b["mean"] + (D + 80) * 2.0 ** -24 * (both @ w))
+        b["grad_h"] = g[:, None] * (b["row_grad"] + s * 2.0 ** -24 * (both @ w))
         e = g[:, None] * both
         b["grad_w"] = s * ((u + (T + 80) * 2.0 ** -24) * (e.T @ h) + (e * delta).T @ h + lift * 2 * g.amax() * h.sum(0))
     return b

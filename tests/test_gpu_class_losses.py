@@ -23,27 +23,27 @@ def forward(fsa, op, h, w, ids, logits, temperature, scale, **kw):
     return fsa.fsa_distill_fwd(h, w, ids, logits, temperature, scale, **kw)
 
 
-def backward(fsa, op, g, h, w, ids, logits, lse, mean, temperature, scale, **kw):
+def backward(fsa, op, g, h, w, ids, logits, lse, row_grad, temperature, scale, **kw):
     if op == "xent":
-        return fsa.fsa_xent_bwd(g, h, w, ids, lse, mean, scale, **kw)
-    return fsa.fsa_distill_bwd(g, h, w, ids, logits, lse, mean, temperature, scale, **kw)
+        return fsa.fsa_xent_bwd(g, h, w, ids, lse, row_grad, scale, **kw)
+    return fsa.fsa_distill_bwd(g, h, w, ids, logits, lse, row_grad, temperature, scale, **kw)
 
 
 def compare(fsa, op, dtype, h, w, ids, logits, g, temperature=1.0, scale=1.0):
     """Forward and backward against the definition; returns what they gave."""
     ref, x = reference(h, w, ids, logits, temperature, scale, g)
     lim = bounds(dtype, x, g)
-    loss, lse, mean = forward(fsa, op, h, w, ids, logits, temperature, scale, emit_mean=True)
+    loss, lse, row_grad = forward(fsa, op, h, w, ids, logits, temperature, scale, emit_row_grad=True)
     alone, lse_alone, none = forward(fsa, op, h, w, ids, logits, temperature, scale)
     assert none is None
-    grad_h, grad_w = backward(fsa, op, g, h, w, ids, logits, lse, mean, temperature, scale)
+    grad_h, grad_w = backward(fsa, op, g, h, w, ids, logits, lse, row_grad, temperature, scale)
     assert grad_h.dtype == h.dtype and grad_w.dtype == w.dtype
-    for name, got, d in (("loss", loss, "f32"), ("lse", lse, "f32"), ("mean", mean, "f32"), ("grad_h", grad_h, dtype),
+    for name, got, d in (("loss", loss, "f32"), ("lse", lse, "f32"), ("row_grad", row_grad, "f32"), ("grad_h", grad_h, dtype),
                          ("grad_w", grad_w, dtype)):
         check(got, ref[name], lim[name], d, name)
     check(alone, ref["loss"], lim["loss"], "f32", "loss alone")
     check(lse_alone, ref["lse"], lim["lse"], "f32", "lse alone")
-    return loss, lse, mean, grad_h, grad_w
+    return loss, lse, row_grad, grad_h, grad_w
 
 
 SIZES = [(1, 1, 1), (1, 47, 128), (2, 33, 3), (5, 1000, 64), (31, 64, 100), (32, 32, 32), (33, 129, 65), (64, 31, 128),
