@@ -42,6 +42,13 @@ struct ClassCut {
     int64_t tiles;                                      // streamed tiles
     int64_t parts;                                      // shares of the streamed tiles in the grid
     constexpr int64_t slices() const { return parts * wy; }   // partial results of every held row
+    // A workgroup's place in the launch and its tiles [first, last).
+    struct Place { int part, group; int first, last; };
+    constexpr Place place(unsigned workgroup) const {
+        const unsigned p = (unsigned)parts, part = workgroup % p, each = (unsigned)tiles / p, more = (unsigned)tiles % p;
+        const unsigned first = part * each + (part < more ? part : more);
+        return {(int)part, (int)(workgroup / p), (int)first, (int)(first + each + (part < more ? 1 : 0))};
+    }
 };
 
 // Streamed blocks of a tile: two tiles and what else a workgroup keeps fit into LDS.
@@ -89,19 +96,18 @@ constexpr ClassBuckets buckets_of(int64_t V, int K) {
 }
 
 // Whether the forward first lays the table out as planes of padded rows: one more pass over the table, against rows
-// that the kernel has to read off the 16-byte grid, or to split into planes, once for every workgroup beside it.
-inline bool forward_packs(const ClassShape& s, bool on_grid) {
-    return (s.kind == 0 || !on_grid) && forward_cut(s).groups > 2;
-}
+// that the kernel has to read off the 16-byte grid, to pad, or to split into planes, once for every workgroup beside it.
+inline bool forward_packs(const ClassShape& s, bool straight) { return !straight && forward_cut(s).groups > 2; }
 
 // Byte offsets into the caller's workspace.
 struct ClassPlan {
     size_t peaks, rows, table, top, sum, mean_parts, norm, loss, start, signs, buckets, slots, row_grad, grad_parts, bytes;
-    bool packed;                                        // the forward reads the table from planes made for the call
+    bool packed;                                        // the forward reads the table from planes made for the call,
+    bool straight;                                      // or as it is: 16-bit rows of a depth, on the 16-byte grid
 };
 constexpr int kPeaksTable = 512, kPeaksRows = 64, kPeaksGrad = 64, kPeaks = kPeaksTable + kPeaksRows + kPeaksGrad;
 
-inline ClassPlan plan_of(const ClassShape& s, bool packed, bool forward, bool want_rows, bool want_grad_w) {
+inline ClassPlan plan_of(const ClassShape& s, bool straight, bool forward, bool want_rows, bool want_grad_w) {
     ClassPlan p{};
     size_t at = 0;
     auto room = [&at](size_t n) { const size_t a = at; at += (n + 255) / 256 * 256; return a; };
@@ -110,8 +116,9 @@ inline ClassPlan plan_of(const ClassShape& s, bool packed, bool forward, bool wa
     if (forward) {
         const bool narrow = narrow_depth((int)depth);
         const size_t slices = forward_cut(s).slices(), stats = narrow ? slices : slices * kClassWaves;
-        p.packed = packed;
-        if (packed) p.table = room(padded_rows(s.V) * depth * 2 * class_planes(s.kind));
+        p.straight = straight;
+        p.packed = forward_packs(s, straight);
+        if (p.packed) p.table = room(padded_rows(s.V) * depth * 2 * class_planes(s.kind));
         p.top = room(stats * T * 4);
         p.sum = room(stats * T * 4);
         if (want_rows) p.mean_parts = room(slices * T * depth * 4);

@@ -33,10 +33,9 @@ int take(fsa::ClassArgs& a, const void* h, int64_t h_stride, const void* w, int6
     return FSA_OK;
 }
 
-// Rows that all start on the 16-byte grid and end on it are read as they are.
-bool packs(const fsa::ClassArgs& a) {
-    const bool on_grid = aligned(a.w, 16) && a.w_stride * elem_bytes(a.s.kind) % 16 == 0 && a.s.D * elem_bytes(a.s.kind) % 16 == 0;
-    return fsa::forward_packs(a.s, on_grid);
+// Rows of a whole depth that all start on the 16-byte grid are read as they are.
+bool straight(const fsa::ClassArgs& a) {
+    return a.s.kind != FSA_F32 && a.s.D == fsa::class_depth(a.s.D) && aligned(a.w, 16) && a.w_stride % 8 == 0;
 }
 
 int take_room(fsa::ClassArgs& a, void* workspace, int64_t bytes) {
@@ -62,7 +61,7 @@ int forward(fsa::ClassArgs& a, float* loss, float* lse, float* row_grad, void* w
     if (a.s.T > 0 && (!loss || !lse)) return FSA_ERR_NULL;
     if (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(row_grad, 4)) return FSA_ERR_ALIGN;
     if (a.s.T == 0) return FSA_OK;
-    a.plan = fsa::plan_of(a.s, packs(a), true, row_grad != nullptr, false);
+    a.plan = fsa::plan_of(a.s, straight(a), true, row_grad != nullptr, false);
     if (int rc = take_room(a, workspace, bytes)) return rc;
     a.loss = loss; a.lse = lse; a.row_grad = row_grad;
     (void)hipGetLastError();                            // an error that the caller left pending is not this call's
@@ -76,7 +75,7 @@ int backward(fsa::ClassArgs& a, const float* grad_loss, const float* lse, const 
     if (!aligned(grad_loss, 4) || !aligned(lse, 4) || !aligned(row_grad, 4) || !aligned(grad_h, eb) || !aligned(grad_w, eb))
         return FSA_ERR_ALIGN;
     const bool again = grad_h && !row_grad && a.s.T > 0;
-    a.plan = fsa::plan_of(a.s, again && packs(a), again, again, grad_w != nullptr);
+    a.plan = fsa::plan_of(a.s, straight(a), again, again, grad_w != nullptr);
     if (int rc = take_room(a, workspace, bytes)) return rc;
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(stream);
@@ -93,7 +92,7 @@ int backward(fsa::ClassArgs& a, const float* grad_loss, const float* lse, const 
 
 // The sizes alone do not say where the table lies: room for a table off the grid.
 int64_t room_for(const fsa::ClassShape& s, bool forward, bool with_row_grad, bool with_grad_w) {
-    return (int64_t)fsa::plan_of(s, forward && fsa::forward_packs(s, false), forward, with_row_grad, with_grad_w).bytes;
+    return (int64_t)fsa::plan_of(s, false, forward, with_row_grad, with_grad_w).bytes;
 }
 
 }  // namespace

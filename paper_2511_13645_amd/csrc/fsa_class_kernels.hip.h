@@ -13,6 +13,8 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <type_traits>
+#include <utility>
 
 #include "fsa_class.h"
 #include "fsa_internal.h"
@@ -30,7 +32,7 @@ struct ClassArgs {
     float* loss; float* lse; float* row_grad;           // forward outputs (row_grad nullable)
     const float* grad_loss; const float* lse_in; const float* row_grad_in;
     void* grad_h; void* grad_w;
-    ClassCut cut; ClassPlan plan; char* ws;
+    ClassCut cut; ClassPlan plan; ClassBuckets buckets; char* ws;
     template <class T> __host__ __device__ T* at(size_t off) const { return reinterpret_cast<T*>(ws + off); }
 };
 
@@ -105,18 +107,40 @@ __device__ __forceinline__ void split8(const float (&x)[8], float unit, u32x4 (&
     }
 }
 
-// Eight elements of a row from column `col` on, zero behind its D: read wide, at whatever alignment the row has.
-struct Eight { typename std::conditional<kKind == 0, f32x4, u32x4>::type v[kKind == 0 ? 2 : 1]; };
+// 16 bytes of a row from byte `at` on, zero behind its end: one wide load at whatever alignment the row has, that of the
+// row's last 16 bytes shifted down where it ends before.
+__device__ __forceinline__ u32x4 load16(const Elem* row, int bytes, int at) {
+    const char* p = reinterpret_cast<const char*>(row);
+    u32x4 x = {};
+    if (at + 16 <= bytes) __builtin_memcpy(&x, p + at, 16);
+    else if (at < bytes && bytes >= 16) {
+        uint64_t lo, hi;
+        __builtin_memcpy(&lo, p + bytes - 16, 8);
+        __builtin_memcpy(&hi, p + bytes - 8, 8);
+        const int bits = 8 * (at + 16 - bytes);         // 16 ... 112
+        lo = bits >= 64 ? hi >> (bits - 64) : lo >> bits | hi << (64 - bits);
+        hi = bits >= 64 ? 0 : hi >> bits;
+        x = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+    } else if (at < bytes) {                            // rows of less than 16 bytes
+        uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+        for (int i = bytes / (int)sizeof(Elem) - 1; i >= at / (int)sizeof(Elem); --i) {
+            uint32_t e = 0;
+            __builtin_memcpy(&e, row + i, sizeof(Elem));
+            hi = hi << 8 * sizeof(Elem) | lo >> (64 - 8 * sizeof(Elem));
+            lo = lo << 8 * sizeof(Elem) | e;
+        }
+        x = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+    }
+    return x;
+}
+// Eight elements of a row from column `col` on.
+struct Eight { u32x4 v[kKind == 0 ? 2 : 1]; };
 __device__ __forceinline__ Eight load8(const Elem* row, int64_t D, int col) {
     Eight e;
-    if (col + 8 <= D) {
-        __builtin_memcpy(&e, row + col, sizeof(e));
-    } else {
-        Elem x[8];
+    const int bytes = (int)(D * sizeof(Elem));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = col + i < D ? row[col + i] : (Elem)0;
-        __builtin_memcpy(&e, x, sizeof(e));
-    }
+    for (int i = 0; i < (kKind == 0 ? 2 : 1); ++i) e.v[i] = load16(row, bytes, col * (int)sizeof(Elem) + 16 * i);
     return e;
 }
 __device__ __forceinline__ void planes_of(const Eight& e, float unit, u32x4 (&out)[NS]) {
@@ -124,7 +148,7 @@ __device__ __forceinline__ void planes_of(const Eight& e, float unit, u32x4 (&ou
         float x[8];
         __builtin_memcpy(x, &e, sizeof(x));
         split8(x, unit, out);
-    } else out[0] = __builtin_bit_cast(u32x4, e.v[0]);
+    } else out[0] = e.v[0];
 }
 
 // Four elements of a row as numbers, zero behind its D.
@@ -142,9 +166,12 @@ __device__ __forceinline__ f32x4 load4(const Elem* row, int64_t D, int col) {
     return x;
 }
 
-// Chunk (of 8 elements) c of row r lies at chunk c ^ turn(r) of its row: 8 rows of one chunk (the first product's reads)
-// and 4 rows of two neighbouring ones (the transposing reads) then lie on different banks.
-__device__ __forceinline__ int turn(int r) { return 2 * (r & 3) + ((r >> 2) & 1); }
+// Chunk (of 8 elements, 16 bytes) c of row r of a tile lies at chunk c ^ turn(r) of its row.  LDS serves 256 bytes at a time:
+// 16 rows of one chunk (the first product's reads) and 4 rows of four neighbouring ones (the transposing reads) then lie
+// on different banks.
+template <int DP> __device__ __forceinline__ int turn(int r) {
+    return DP == 64 ? 4 * ((r >> 1) & 1) + ((r >> 2) & 3) : 4 * (r & 3) + ((r >> 2) & 3);
+}
 
 __device__ __forceinline__ u32x2 read_transposed(const uint16_t* p) {
     using lds_s16x4 = __attribute__((address_space(3))) s16x4;
@@ -213,7 +240,7 @@ __device__ __forceinline__ float peak_of(const Eight& e) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) m = fmaxf(m, finite_abs(e.v[i][j]));
+            for (int j = 0; j < 4; ++j) m = fmaxf(m, finite_abs(__builtin_bit_cast(float, e.v[i][j])));
     }
     return m;
 }
@@ -340,7 +367,7 @@ __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, in
     __shared__ float room[kRowWaves];
     __shared__ uint32_t signs, counts[kMostBuckets], sums[kRowWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const ClassBuckets bk = buckets_of(a.s.V, a.s.K);
+    const ClassBuckets bk = a.buckets;
     if (threadIdx.x == 0) signs = 0;
     for (int i = threadIdx.x; i < bk.count; i += kRowThreads) counts[i] = 0;
     const Units u = row_units<kRowWaves>(a, room);
@@ -372,7 +399,7 @@ __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, in
         }
         ids[k] = id >= 0 && id < a.s.V && weight != 0.0f ? id : -1;
         pulls[k] = g * weight;
-        if (ids[k] >= 0) atomicAdd(&counts[ids[k] / kBlock / bk.per], 1u);
+        if (ids[k] >= 0) atomicAdd(&counts[(uint32_t)ids[k] / kBlock / (uint32_t)bk.per], 1u);
     }
     __syncthreads();
     // counts to places, four buckets to a thread
@@ -409,7 +436,7 @@ __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, in
 #pragma unroll
     for (int k = 0; k < kRowsEach; ++k)
         if (ids[k] >= 0)
-            slots[atomicAdd(&counts[ids[k] / kBlock / bk.per], 1u)] = Slot{(uint32_t)(wave * kRowsEach + k) << 27 | (uint32_t)ids[k], pulls[k]};
+            slots[atomicAdd(&counts[(uint32_t)ids[k] / kBlock / (uint32_t)bk.per], 1u)] = Slot{(uint32_t)(wave * kRowsEach + k) << 27 | (uint32_t)ids[k], pulls[k]};
     if (threadIdx.x == 0) a.at<uint32_t>(a.plan.signs)[blockIdx.x] = signs;
 }
 
@@ -424,9 +451,9 @@ struct SlotFeed {
     SlotWord ahead[M], next[M], now[M];
     Slot next_slot[M], slot[M];
     __device__ __forceinline__ SlotFeed(const ClassArgs& a, int64_t padded, int64_t v0) {
-        const ClassBuckets bk = buckets_of(a.s.V, a.s.K);
-        const int64_t block = v0 / kBlock < ceil_div(a.s.V, kBlock) ? v0 / kBlock : 0;
-        words = a.at<const uint32_t>(a.plan.buckets) + block / bk.per;
+        const ClassBuckets bk = a.buckets;
+        const uint32_t block = (uint32_t)(v0 < a.s.V ? v0 / kBlock : 0);
+        words = a.at<const uint32_t>(a.plan.buckets) + block / (uint32_t)bk.per;
         slots = a.at<const Slot>(a.plan.slots);
         buckets = bk.count; block_slots = (int64_t)kBlock * a.s.K; blocks = padded / kBlock;
         first_class = (uint32_t)v0;
@@ -509,21 +536,34 @@ struct Tile {
                 u32x4 p[NS];
                 planes_of(e[i], unit, p);
 #pragma unroll
-                for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(lds + n * kPlane + r * DP + (c ^ turn(r)) * 8) = p[n];
+                for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(lds + n * kPlane + r * DP + (c ^ turn<DP>(r)) * 8) = p[n];
             }
         }
     };
-    // Rows [first, first + ROWS) of planes that have them all.
+    // The same of 16-bit planes of rows of DP elements on the 16-byte grid, `rows` of them; a thread's share lies at fixed
+    // places from the tile's first row on.
     struct FromPlanes {
+        static constexpr int kStep = kClassThreads / (DP / 8);     // rows from one of a thread's chunks to the next
         u32x4 p[NS][kEach];
-        __device__ __forceinline__ void load(const uint16_t* planes, int64_t padded, int64_t first) {
+        __device__ __forceinline__ void load(const char* planes, int row_bytes, int64_t plane_bytes, int64_t rows, int64_t first) {
+            const uint32_t place = threadIdx.x / (DP / 8) * row_bytes + threadIdx.x % (DP / 8) * 16;
+            if (first + ROWS <= rows) {
 #pragma unroll
-            for (int n = 0; n < NS; ++n)
+                for (int n = 0; n < NS; ++n)
 #pragma unroll
-                for (int i = 0; i < kEach; ++i) {
-                    const int q = i * kClassThreads + threadIdx.x;
-                    p[n][i] = *reinterpret_cast<const u32x4*>(planes + ((int64_t)n * padded + first) * DP + (int64_t)q * 8);
-                }
+                    for (int i = 0; i < kEach; ++i)
+                        p[n][i] = *reinterpret_cast<const u32x4*>(planes + n * plane_bytes + (first + i * kStep) * row_bytes + place);
+            } else {
+                asm volatile("");                       // the last tile of a table as it is
+#pragma unroll
+                for (int n = 0; n < NS; ++n)
+#pragma unroll
+                    for (int i = 0; i < kEach; ++i) {
+                        int64_t r = first + i * kStep + threadIdx.x / (DP / 8);
+                        if (r >= rows) r = rows - 1;
+                        p[n][i] = *reinterpret_cast<const u32x4*>(planes + n * plane_bytes + r * row_bytes + threadIdx.x % (DP / 8) * 16);
+                    }
+            }
         }
         __device__ __forceinline__ void store(uint16_t* lds) const {
 #pragma unroll
@@ -531,7 +571,7 @@ struct Tile {
 #pragma unroll
                 for (int i = 0; i < kEach; ++i) {
                     const int q = i * kClassThreads + threadIdx.x, r = q / (DP / 8), c = q % (DP / 8);
-                    *reinterpret_cast<u32x4*>(lds + n * kPlane + r * DP + (c ^ turn(r)) * 8) = p[n][i];
+                    *reinterpret_cast<u32x4*>(lds + n * kPlane + r * DP + (c ^ turn<DP>(r)) * 8) = p[n][i];
                 }
         }
     };
@@ -540,7 +580,7 @@ struct Tile {
     static __device__ __forceinline__ void rows(const uint16_t* lds, int b, int ks, int lane, u32x4 (&out)[NS]) {
         const int r = b * kBlock + (lane & 31), c = 2 * ks + (lane >> 5);
 #pragma unroll
-        for (int n = 0; n < NS; ++n) out[n] = *reinterpret_cast<const u32x4*>(lds + n * kPlane + r * DP + (c ^ turn(r)) * 8);
+        for (int n = 0; n < NS; ++n) out[n] = *reinterpret_cast<const u32x4*>(lds + n * kPlane + r * DP + (c ^ turn<DP>(r)) * 8);
     }
     // A operand of the second: elements 32*db.., step s of 16 rows of block b, the rows in the order of a result's registers.
     static __device__ __forceinline__ void columns(const uint16_t* lds, int b, int s, int db, int lane, u32x4 (&out)[NS]) {
@@ -548,8 +588,9 @@ struct Tile {
         const int c = 4 * db + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-            const uint16_t* p = lds + n * kPlane + r * DP + (c ^ turn(r)) * 8 + (i & 1) * 4;
-            const u32x2 a = read_transposed(p), z = read_transposed(p + 8 * DP);   // rows r and r + 8 turn alike
+            const int t = c ^ turn<DP>(r);              // row r + 8 turns by 2 more
+            const uint16_t* p = lds + n * kPlane + r * DP + (i & 1) * 4;
+            const u32x2 a = read_transposed(p + t * 8), z = read_transposed(p + 8 * DP + (t ^ 2) * 8);
             out[n] = u32x4{a[0], a[1], z[0], z[1]};
         }
     }
@@ -595,21 +636,92 @@ __device__ __forceinline__ float hold_rows(const ClassArgs& a, int64_t row, int 
     const Elem* h = static_cast<const Elem*>(a.h) + t * a.h_stride;
     return hold<KS>(h, a.s.D, col0, lane, kKind != 0 || lane_lives(a, t), held, join);
 }
+// Two values of P, registers 2j and 2j + 1 of step s, into that step's B operand; planes of what fp16 or bfloat16 takes of
+// them, nearest even.
+__device__ __forceinline__ void put2(float a, float b, int j, u32x4 (&out)[NS]) {
+    out[0][j] = pack2(a, b);
+    if constexpr (NS == 2) out[1][j] = pack2(a - low2(out[0][j]), b - high2(out[0][j]));
+}
+
+template <int N> using number = std::integral_constant<int, N>;
+template <class F, int... I> __device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) { (f(number<I>{}), ...); }
+// f(number<0>), ..., f(number<N - 1>)
+template <int N, class F> __device__ __forceinline__ void each(F f) { each_of(f, std::make_integer_sequence<int, N>{}); }
+
+// One tile further: the scores of the tile `ahead` and the products of the tile `tile` with P, which element(m, i) makes of
+// the scores that `tile` had, a matrix instruction at a time.  Between two of them stand the reads for three further on
+// and a share of the exponentials, a block's own while the products before it run, so that the matrix unit, LDS and the
+// vector unit work side by side; the compiler's own order waited for every read.  ready(m, q) sees a block's operand.
+//
+// WITHIN: scores and products of one tile (ahead == tile); a block is exponentiated while the next one's scores, or the
+// products of the one before, run.  It keeps no scores from one tile to the next.
+template <int DP, int BLOCKS, int MY, bool PRODUCT, bool WITHIN, class Element, class Ready>
+__device__ __forceinline__ void advance(const uint16_t* ahead, const uint16_t* tile, int block0, int lane,
+                                        const u32x4 (&held)[DP / 16][NS], f32x16 (&score)[MY], f32x16* acc, Element element, Ready ready) {
+    constexpr int KS = DP / 16, DB = DP / 32;
+    constexpr int S = MY * KS, EACH = 2 * DB, ALL = S + (PRODUCT ? MY * EACH : 0), R = 4;
+    using T = Tile<DP, BLOCKS * kBlock>;
+    u32x4 ring[R][NS], q[2][2][NS];
+    float even = 0.0f;
+    auto load = [&](auto at) {
+        constexpr int k = at();
+        if constexpr (k < S) T::rows(ahead, block0 + (WITHIN ? k / KS : k % MY), WITHIN ? k % KS : k / MY, lane, ring[k % R]);
+        else if constexpr (k < ALL) T::columns(tile, block0 + (k - S) / EACH, (k - S) % EACH / DB, (k - S) % DB, lane, ring[k % R]);
+    };
+    auto elements = [&](auto block, auto from, auto to) {
+        constexpr int m = block(), first = from();
+        each<to() - first>([&](auto n) {
+            constexpr int i = first + n();
+            const float p = element(m, i);
+            if constexpr (i & 1) put2(even, p, i / 2 % 4, q[m & 1][i / 8]);
+            even = p;
+        });
+    };
+    each<R - 1>([&](auto k) { load(k); });
+    each<ALL>([&](auto at) {
+        constexpr int k = at();
+        load(number<k + R - 1>{});
+        if constexpr (k < S) {
+            constexpr int m = WITHIN ? k / KS : k % MY, ks = WITHIN ? k % KS : k / MY;
+            score[m] = matmul(ring[k % R], held[ks], ks == 0 ? f32x16{} : score[m]);
+            if constexpr (WITHIN) {
+                if constexpr (m == 1) elements(number<0>{}, number<16 * ks / KS>{}, number<16 * (ks + 1) / KS>{});
+                else if constexpr (MY == 1 && k == S - 1) elements(number<0>{}, number<0>{}, number<16>{});
+            } else if constexpr (PRODUCT) elements(number<0>{}, number<16 * k / S>{}, number<16 * (k + 1) / S>{});
+            else each<MY>([&](auto j) {                 // no products to hide other blocks' behind
+                elements(j, number<16 * k / S>{}, number<16 * (k + 1) / S>{});
+            });
+        } else {
+            constexpr int o = k - S, m = o / EACH;
+            acc[o % DB] = matmul(ring[k % R], q[m & 1][o % EACH / DB], acc[o % DB]);
+            if constexpr (m + 1 < MY) elements(number<m + 1>{}, number<16 * (o % EACH) / EACH>{}, number<16 * (o % EACH + 1) / EACH>{});
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (PRODUCT && k == S - 1) ready(0, q[0]);
+        if constexpr (PRODUCT && k >= S && (k - S) % EACH == EACH - 1 && (k - S) / EACH + 1 < MY) {
+            constexpr int m = (k - S) / EACH + 1;
+            ready(m, q[m & 1]);
+        }
+    });
+}
+
 // ---------------------------------------------------------------------------------------------------------------
 // forward: a wave holds 32 rows of h, the table streams by
 // ---------------------------------------------------------------------------------------------------------------
-template <int DP, int WY, bool MEAN, bool PACKED>
+template <int DP, int WY, bool MEAN, bool STRAIGHT>
 __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_forward_kernel(ClassArgs a, int64_t padded) {
     constexpr int NB = blocks_per_tile(WY, DP, kKind), MY = NB / WY, WX = kClassWaves / WY;   // blocks of a tile, a wave's own of them
     using T = Tile<DP, NB * kBlock>;
-    __shared__ __align__(16) uint16_t lds[2][NS * T::kPlane];
+    constexpr bool AHEAD = WY == 1;
+    constexpr int TILES = AHEAD ? 3 : 2;
+    __shared__ __align__(16) uint16_t lds[TILES][NS * T::kPlane];
     __shared__ float room[kClassWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = wave % WX, y = wave / WX;
-    const int64_t part = blockIdx.x % a.cut.parts, group = blockIdx.x / a.cut.parts;
+    const ClassCut::Place place = a.cut.place(blockIdx.x);
+    const int part = place.part, group = place.group, first = place.first, last = place.last;
     const float table = table_unit(a, room);
-    const int64_t first = a.cut.tiles * part / a.cut.parts, last = a.cut.tiles * (part + 1) / a.cut.parts;
-    const int64_t row = (group * WX + x) * kBlock + (lane & 31);               // of h, held by this lane
-    const bool live = (group * WX + x) * kBlock < padded;                      // wave-uniform
+    const int64_t row0 = ((int64_t)group * WX + x) * kBlock, row = row0 + (lane & 31);   // of h, held by this lane
+    const bool live = row0 < padded;                      // wave-uniform
 
     u32x4 held[DP / 16][NS];
     const float to_log2 = a.scale * kLog2e / hold_rows<DP / 16>(a, row, 0, lane, held, [](float peak) { return wave_max(peak); }) / table;
@@ -619,22 +731,23 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
 #pragma unroll
     for (auto& f : acc) f = f32x16{};
 
-    typename std::conditional<PACKED, typename T::FromPlanes, typename T::FromTable>::type next;
-    const int64_t table_rows = padded_rows(a.s.V);
-    auto fetch = [&](int64_t it) {
-        if constexpr (PACKED) next.load(a.at<const uint16_t>(a.plan.table), table_rows, it * NB * kBlock);
-        else next.load(static_cast<const Elem*>(a.w), a.w_stride, a.s.V, a.s.D, it * NB * kBlock);
+    // the table as planes (those of the call, or 16-bit rows as they are), or rows of any kind
+    typename std::conditional<STRAIGHT, typename T::FromPlanes, typename T::FromTable>::type next;
+    const char* planes = a.plan.packed ? a.ws + a.plan.table : static_cast<const char*>(a.w);
+    const int row_bytes = 2 * (a.plan.packed ? DP : (int)a.w_stride);
+    const int64_t table_rows = a.plan.packed ? padded_rows(a.s.V) : a.s.V;
+    auto fetch = [&](int it) {
+        if (it >= last) return;
+        if constexpr (STRAIGHT) next.load(planes, row_bytes, table_rows * row_bytes, table_rows, (int64_t)it * NB * kBlock);
+        else next.load(static_cast<const Elem*>(a.w), a.w_stride, a.s.V, a.s.D, (int64_t)it * NB * kBlock);
     };
-    if (first < last) fetch(first);
-    for (int64_t it = first; it < last; ++it) {
-        uint16_t* tile = lds[(it - first) & 1];         // the other one may still be read
-        if constexpr (PACKED) next.store(tile);
+    auto store = [&](uint16_t* tile) {
+        if constexpr (STRAIGHT) next.store(tile);
         else next.store(tile, table);
-        __syncthreads();
-        if (it + 1 < last) fetch(it + 1);
-        if (!live) continue;
-
-        f32x16 score[MY];
+    };
+    f32x16 score[MY];
+    float top;                                          // of this lane's scores of a tile
+    auto scores = [&](const uint16_t* tile) {
 #pragma unroll
         for (int m = 0; m < MY; ++m) {
             score[m] = f32x16{};
@@ -645,19 +758,51 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
                 score[m] = matmul(f, held[ks], score[m]);
             }
         }
-        if ((it + 1) * NB * kBlock > a.s.V) {           // the last tile: classes that there are not
+    };
+    auto find_top = [&](int it) {
+        if ((int64_t)(it + 1) * NB * kBlock > a.s.V) {  // the last tile: classes that there are not
+            asm volatile("");                           // a branch, not sixteen selects in every tile
+            const int left = (int)(a.s.V - (int64_t)it * NB * kBlock) - y * MY * kBlock;
 #pragma unroll
             for (int m = 0; m < MY; ++m)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (it * NB * kBlock + (y * MY + m) * kBlock + row_of(i, lane) >= a.s.V) score[m][i] = -__builtin_inff();
+                for (int i = 0; i < 16; ++i) if (m * kBlock + row_of(i, lane) >= left) score[m][i] = -__builtin_inff();
         }
-        float top = score[0][0];
+        top = score[0][0];
 #pragma unroll
         for (int m = 0; m < MY; ++m)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, score[m][i]);
         top *= to_log2;
+    };
+
+    // Ahead: a tile's scores are made while the tile before it is exponentiated and multiplied; its table rows lie in the
+    // next of three LDS tiles by then, those of the tile after it are on their way in registers.
+    int slot = 0;
+    fetch(first);
+    if constexpr (AHEAD) {
+        store(lds[0]);
+        fetch(first + 1);
+        __syncthreads();
+        if (live) {
+            scores(lds[0]);
+            find_top(first);
+        }
+    }
+    for (int it = first; it < last; ++it) {
+        uint16_t* tile = lds[slot];
+        slot = slot + 1 == TILES ? 0 : slot + 1;
+        uint16_t* ahead = lds[slot];
+        if constexpr (AHEAD) {
+            if (it + 1 < last) store(ahead);
+        } else store(tile);
+        __syncthreads();
+        fetch(it + (AHEAD ? 2 : 1));
+        if (!live) continue;
+        if constexpr (!AHEAD) {
+            scores(tile);
+            find_top(it);
+        }
         if (__any(top - ref > kLift + kSlack)) {
             top = fmaxf(top, __shfl_xor(top, 32));
             const float to = fmaxf(ref, top - kLift), by = exp2f(ref - to);
@@ -666,6 +811,20 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
             if constexpr (MEAN)
 #pragma unroll
                 for (auto& f : acc) f *= by;
+        }
+        if constexpr (AHEAD) {
+            f32x16 now[MY];
+#pragma unroll
+            for (int m = 0; m < MY; ++m) now[m] = score[m];
+            float some[2] = {};                         // (behind the last tile the scores are of no use, and unused)
+            advance<DP, NB, MY, MEAN, false>(ahead, tile, 0, lane, held, score, acc, [&](int m, int i) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(now[m][i], to_log2, -ref));
+                some[i & 1] += p;
+                return p;
+            }, [](int, u32x4 (&)[2][NS]) {});
+            sum += some[0] + some[1];
+            find_top(it + 1);
+            continue;
         }
 #pragma unroll
         for (int m = 0; m < MY; ++m) {
@@ -692,7 +851,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
     }
     if (!live) return;
     sum += __shfl_xor(sum, 32);
-    const int64_t at = (part * WY + y) * padded + row;
+    const int64_t at = (int64_t)(part * WY + y) * padded + row;
     if (lane < 32) {
         a.at<float>(a.plan.top)[at] = ref;
         a.at<float>(a.plan.sum)[at] = sum;
@@ -833,10 +992,10 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
     __shared__ float cells[kClassWaves][kBlock * kBlock];
     __shared__ float room[kClassWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = wave % WX, y = wave / WX;
-    const int64_t part = blockIdx.x % a.cut.parts, group = blockIdx.x / a.cut.parts;
+    const ClassCut::Place place = a.cut.place(blockIdx.x);
+    const int part = place.part, group = place.group, first = place.first, last = place.last;
     const Units u = row_units(a, room);
-    const int64_t first = a.cut.tiles * part / a.cut.parts, last = a.cut.tiles * (part + 1) / a.cut.parts;
-    const int64_t v0 = (group * WX + x) * kBlock, v = v0 + (lane & 31);
+    const int64_t v0 = ((int64_t)group * WX + x) * kBlock, v = v0 + (lane & 31);
     const bool live = v0 < a.s.V;                       // wave-uniform
 
     u32x4 held[DP / 16][NS];
@@ -850,102 +1009,108 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
 #pragma unroll
     for (int i = 0; i < 16; ++i) cell[row_of(i, lane) * kBlock + (lane & 31)] = 0.0f;
 
-    const uint16_t* planes = a.at<const uint16_t>(a.plan.rows);
     const float* start = a.at<const float>(a.plan.start);
     typename T::FromPlanes next;
     float next_start = 0.0f;
     SlotFeed<MY> feed(a, padded, v0);
-    auto fetch = [&](int64_t it) {
-        feed.ask_slots(it * NB + y * MY, lane);
-        feed.ask_words((it + 1) * NB + y * MY);
-        next.load(planes, padded, it * NB * kBlock);    // rows are padded to whole tiles
-        if (threadIdx.x < NB * kBlock) next_start = start[it * NB * kBlock + threadIdx.x];
+    auto fetch = [&](int it) {
+        if (it >= last) return;
+        next.load(a.ws + a.plan.rows, 2 * DP, padded * 2 * DP, padded, (int64_t)it * NB * kBlock);   // (padded to whole tiles)
+        if (threadIdx.x < NB * kBlock) next_start = start[(int64_t)it * NB * kBlock + threadIdx.x];
     };
-    if (first < last) {
-        feed.ask_words(first * NB + y * MY);
-        fetch(first);
-    }
-    for (int64_t it = first; it < last; ++it) {
-        const int half = (it - first) & 1;
-        feed.turn();
-        uint16_t* tile = lds[half];
-        next.store(tile);
-        if (threadIdx.x < NB * kBlock) starts[half][threadIdx.x] = next_start;
-        __syncthreads();
-        if (it + 1 < last) fetch(it + 1);
-        if (!live) continue;
+    auto store = [&](int slot) {
+        next.store(lds[slot]);
+        if (threadIdx.x < NB * kBlock) starts[slot][threadIdx.x] = next_start;
+    };
+    auto product = [&](const uint16_t* tile, int b, const u32x4 (&q)[2][NS]) {
 #pragma unroll
-        for (int m = 0; m < MY; ++m) {
-            const int b = y * MY + m;
-            const int64_t t0 = (it * NB + b) * kBlock;
-            if (t0 >= a.s.T) continue;
-            f32x16 score = {};
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int ks = 0; ks < DP / 16; ++ks) {
+            for (int db = 0; db < DP / 32; ++db) {
                 u32x4 f[NS];
-                T::rows(tile, b, ks, lane, f);
-                score = matmul(f, held[ks], score);
+                T::columns(tile, b, s, db, lane, f);
+                acc[db] = matmul(f, q[s], acc[db]);
             }
-            float p[16];
+    };
+    // Where rows of block t have negative gradients: their signs into P's operand, whose step s and word j hold registers
+    // 8s + 2j and 8s + 2j + 1.
+    auto sign = [&](int64_t block, u32x4 (&q)[2][NS]) {
+        const uint32_t signs = a.at<const uint32_t>(a.plan.signs)[block];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const f32x4 s = *reinterpret_cast<const f32x4*>(&starts[half][b * kBlock + 8 * i + 4 * (lane >> 5)]);
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) p[4 * i + j] = __builtin_amdgcn_exp2f(fmaf(score[4 * i + j], to_log2, s[j]));
+            for (int j = 0; j < 4; ++j) {
+                const int r = row_of(8 * s + 2 * j, lane);
+                const uint32_t flip = (signs >> r & 1) << 15 | (signs >> (r + 1)) << 31;
+#pragma unroll
+                for (int n = 0; n < NS; ++n) q[s][n][j] ^= flip;
             }
-            if (feed.now[m].negative()) {
-                const uint32_t signs = a.at<const uint32_t>(a.plan.signs)[t0 / kBlock];
+    };
+    // What slots pull at, subtracted by a product of its own, for 16-bit types in two roundings: it is most of the gradient
+    // of a class that rows name.
+    auto pull = [&](const uint16_t* tile, int b) {
+        float c[16];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) if (signs >> row_of(i, lane) & 1) p[i] = -p[i];
-            }
-            const bool hit = feed.gather(m, t0 / kBlock, lane, cell);
-            if (hit) {
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float& c = cell[row_of(i, lane) * kBlock + (lane & 31)];
-                    p[i] -= c;
-                    c = 0.0f;
-                }
-                __builtin_amdgcn_wave_barrier();
-            }
+        for (int i = 0; i < 16; ++i) {
+            float& at = cell[row_of(i, lane) * kBlock + (lane & 31)];
+            c[i] = -at;
+            at = 0.0f;
+        }
+#pragma unroll 1
+        for (int n = 0; n < 2 / NS; ++n) {
             u32x4 q[2][NS];
-            operand_of(p, q);
+            operand_of(c, q);
+            product(tile, b, q);
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int db = 0; db < DP / 32; ++db) {
-                    u32x4 f[NS];
-                    T::columns(tile, b, s, db, lane, f);
-                    acc[db] = matmul(f, q[s], acc[db]);
+                for (int j = 0; j < 4; ++j) {
+                    c[8 * s + 2 * j] -= low2(q[s][0][j]);
+                    c[8 * s + 2 * j + 1] -= high2(q[s][0][j]);
                 }
-            // what a class's own rows pull at is most of its gradient: where there are some, what rounding took of it follows
-            if (NS == 1 && hit) {
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        p[8 * s + 2 * j] -= low2(q[s][0][j]);
-                        p[8 * s + 2 * j + 1] -= high2(q[s][0][j]);
-                    }
-                }
-                operand_of(p, q);
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int db = 0; db < DP / 32; ++db) {
-                        u32x4 f[NS];
-                        T::columns(tile, b, s, db, lane, f);
-                        acc[db] = matmul(f, q[s], acc[db]);
-                    }
-            }
         }
+        __builtin_amdgcn_wave_barrier();
+    };
+
+    int slot = 0;
+    fetch(first);
+    if (first < last) {
+        feed.ask_words((int64_t)first * NB + y * MY);
+        feed.ask_slots((int64_t)first * NB + y * MY, lane);
+        feed.ask_words((int64_t)(first + 1) * NB + y * MY);
+    }
+    for (int it = first; it < last; ++it) {
+        const int at = slot;
+        const uint16_t* tile = lds[at];
+        slot ^= 1;
+        feed.turn();
+        store(at);                                      // the other tile may still be read
+        __syncthreads();
+        fetch(it + 1);
+        feed.ask_slots((int64_t)(it + 1) * NB + y * MY, lane);
+        feed.ask_words((int64_t)(it + 2) * NB + y * MY);
+        if (!live) continue;
+        const int64_t block0 = (int64_t)it * NB + y * MY;          // of rows
+        f32x16 score[MY];
+        f32x4 s = {};
+        advance<DP, NB, MY, true, true>(tile, tile, y * MY, lane, held, score, acc, [&](int m, int i) {
+            if (i % 4 == 0) s = *reinterpret_cast<const f32x4*>(&starts[at][(y * MY + m) * kBlock + 2 * i + 4 * (lane >> 5)]);
+            return __builtin_amdgcn_exp2f(fmaf(score[m][i], to_log2, s[i % 4]));
+        }, [&](int m, u32x4 (&q)[2][NS]) {
+            if (feed.now[m].negative()) sign(block0 + m, q);
+        });
+#pragma unroll
+        for (int m = 0; m < MY; ++m)
+            if (feed.gather(m, block0 + m, lane, cell)) {
+                __builtin_amdgcn_wave_barrier();
+                pull(tile, y * MY + m);
+            }
     }
     if (!live) return;
     const float back = a.scale / u.h / u.g;
     if (a.cut.slices() > 1) {
         const int64_t rows = ceil_div(a.s.V, kBlock) * kBlock;
-        float* out = a.at<float>(a.plan.grad_parts) + ((part * WY + y) * rows + v) * DP + 4 * (lane >> 5);
+        float* out = a.at<float>(a.plan.grad_parts) + ((int64_t)(part * WY + y) * rows + v) * DP + 4 * (lane >> 5);
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
@@ -970,14 +1135,19 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
 // ---------------------------------------------------------------------------------------------------------------
 // wide rows: the four waves of a workgroup hold a quarter of the elements each
 // ---------------------------------------------------------------------------------------------------------------
-// A wave's quarter of 32 streamed rows in LDS, its own: no other wave reads it.  Rows lie 8k + 2 chunks apart, every
-// second four of them one chunk on: the reads of 8 rows of one chunk and of 4 rows of two chunks fall on different banks.
+// A wave's quarter of 32 streamed rows in LDS, its own: no other wave reads it.  Rows of 32 chunks turn as in the narrow
+// kernels' tiles; others lie 4 or 12 chunks more than a multiple of 16 apart, every four of them one chunk further on,
+// which parts the same reads.
 template <int Q>
 struct Quarter {
-    static constexpr int kChunks = Q / 8, kStride = ((kChunks + 1 + 5) / 8 * 8 + 2) * 8;   // elements from row to row
-    static constexpr int kPlane = kBlock * kStride, kEach = kBlock * kChunks / 64;
-    static_assert(kStride >= Q + 16 && (kBlock * kChunks) % 64 == 0, "a row, its shift and a spare chunk fit, lanes share rows evenly");
-    static __device__ __forceinline__ int place(int r, int c) { return r * kStride + (c + ((r >> 2) & 1)) * 8; }
+    static constexpr int kChunks = Q / 8, kEach = kBlock * kChunks / 64;
+    static constexpr bool kTurns = kChunks == 32;
+    static constexpr int kStride = 8 * (kTurns ? 32 : kChunks + 3 <= 20 ? 20 : 28);       // elements from row to row
+    static constexpr int kPlane = kBlock * kStride;
+    static_assert(kStride >= Q && (kBlock * kChunks) % 64 == 0 && (kTurns || (kChunks + 3 <= 28)), "rows fit, lanes share them evenly");
+    static __device__ __forceinline__ int place(int r, int c) {
+        return r * kStride + (kTurns ? c ^ turn<Q>(r) : c + ((r >> 2) & 3)) * 8;
+    }
     static __device__ __forceinline__ void rows(const uint16_t* lds, int ks, int lane, u32x4 (&out)[NS]) {
 #pragma unroll
         for (int n = 0; n < NS; ++n)
@@ -987,8 +1157,8 @@ struct Quarter {
         const int i = lane & 15, r = 16 * s + 4 * (lane >> 5) + (i >> 2), c = 4 * db + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
 #pragma unroll
         for (int n = 0; n < NS; ++n) {
-            const uint16_t* p = lds + n * kPlane + place(r, c) + (i & 1) * 4;
-            const u32x2 a = read_transposed(p), z = read_transposed(p + 8 * kStride);
+            const uint16_t* p = lds + n * kPlane + (i & 1) * 4;
+            const u32x2 a = read_transposed(p + place(r, c)), z = read_transposed(p + place(r + 8, c));
             out[n] = u32x4{a[0], a[1], z[0], z[1]};
         }
     }
@@ -998,7 +1168,7 @@ enum WideMode { kStats, kMean, kGradient };
 
 // kStats: running maximum and sum of every held row of h, one pair per wave (a quarter of the streamed classes each).
 // kMean: sum of the table's rows under 2^(score - norm).  kGradient: as the narrow kernel.
-template <int Q, WideMode MODE, bool PACKED>
+template <int Q, WideMode MODE, bool STRAIGHT>
 __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, int64_t padded) {
     using S = Quarter<Q>;
     constexpr int DEPTH = Q * kClassWaves;
@@ -1007,16 +1177,15 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
     __shared__ __align__(16) f32x4 partial[MEETS][kClassWaves][4][64];
     constexpr int PS = MODE == kStats ? 1 : MODE == kGradient ? 2 : NS;   // planes of P; 16-bit types use the second after a hit
     __shared__ __align__(16) u32x2 shared_p[PS][2][64][2];
-    // the tile that last had a slot of these classes, in a corner of LDS that no row reaches
-    auto& hit = *reinterpret_cast<int64_t __attribute__((may_alias))*>(quarters[0] + S::kStride - 8);
+    __shared__ int hit;                             // the tile that last had a slot of these classes
     __shared__ float cells[MODE == kGradient ? kBlock * kBlock : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col0 = wave * Q;
-    const int64_t part = blockIdx.x % a.cut.parts, group = blockIdx.x / a.cut.parts;
+    const ClassCut::Place place = a.cut.place(blockIdx.x);
+    const int part = place.part, group = place.group, first = place.first, last = place.last;
     float* room = reinterpret_cast<float*>(partial);
     const Units u = MODE == kGradient ? row_units(a, room) : Units{1.0f, 1.0f};
     const float table = MODE == kGradient ? 1.0f : table_unit(a, room);
-    const int64_t first = a.cut.tiles * part / a.cut.parts, last = a.cut.tiles * (part + 1) / a.cut.parts;
-    const int64_t x0 = group * kBlock, x = x0 + (lane & 31);
+    const int64_t x0 = (int64_t)group * kBlock, x = x0 + (lane & 31);
     const Elem* w = static_cast<const Elem*>(a.w);
     const uint16_t* planes = a.at<const uint16_t>(a.plan.rows);
     uint16_t* lds = quarters[wave];
@@ -1046,13 +1215,14 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
     for (auto& f : acc) f = f32x16{};
 
     // the next tile's quarter: rows of the table as they are, or planes
-    constexpr bool FROM_PLANES = MODE == kGradient || PACKED;
+    constexpr bool FROM_PLANES = MODE == kGradient || STRAIGHT;
     struct { Eight e[FROM_PLANES ? 1 : S::kEach]; u32x4 p[FROM_PLANES ? NS : 1][FROM_PLANES ? S::kEach : 1]; } next;
-    const uint16_t* streamed = MODE == kGradient ? planes : a.at<const uint16_t>(a.plan.table);
-    const int64_t streamed_rows = MODE == kGradient ? padded : padded_rows(a.s.V);
+    const bool as_is = MODE != kGradient && !a.plan.packed;
+    const uint16_t* streamed = MODE == kGradient ? planes : as_is ? reinterpret_cast<const uint16_t*>(w) : a.at<const uint16_t>(a.plan.table);
+    const int64_t streamed_rows = MODE == kGradient ? padded : as_is ? a.s.V : padded_rows(a.s.V), streamed_stride = as_is ? a.w_stride : DEPTH;
     SlotFeed<1> feed(a, padded, MODE == kGradient ? x0 : 0);
     f32x4 next_start = {};
-    auto fetch = [&](int64_t it) {
+    auto fetch = [&](int it) {
         if constexpr (MODE == kGradient)
             if (wave == 0) {                            // one wave looks after the slots of the workgroup's classes
                 feed.ask_slots(it, lane);
@@ -1061,21 +1231,22 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
 #pragma unroll
         for (int i = 0; i < S::kEach; ++i) {
             const int q = i * 64 + lane, r = q / S::kChunks, c = q % S::kChunks;
-            const int64_t row = it * kBlock + r;
+            const int64_t row = (int64_t)it * kBlock + r;
             if constexpr (FROM_PLANES) {
 #pragma unroll
                 for (int n = 0; n < NS; ++n)
-                    next.p[n][i] = *reinterpret_cast<const u32x4*>(streamed + ((int64_t)n * streamed_rows + row) * DEPTH + col0 + c * 8);
+                    next.p[n][i] = *reinterpret_cast<const u32x4*>(streamed + ((int64_t)n * streamed_rows + (row < streamed_rows ? row : streamed_rows - 1)) *
+                                                                                 streamed_stride + col0 + c * 8);
             } else next.e[i] = load8(w + (row < a.s.V ? row : a.s.V - 1) * a.w_stride, a.s.D, col0 + c * 8);
         }
         if constexpr (MODE == kGradient)
-            next_start = *reinterpret_cast<const f32x4*>(a.at<const float>(a.plan.start) + it * kBlock + 8 * wave + 4 * (lane >> 5));
+            next_start = *reinterpret_cast<const f32x4*>(a.at<const float>(a.plan.start) + (int64_t)it * kBlock + 8 * wave + 4 * (lane >> 5));
     };
     if (first < last) {
         if (MODE == kGradient && wave == 0) feed.ask_words(first);
         fetch(first);
     }
-    for (int64_t it = first; it < last; ++it) {
+    for (int it = first; it < last; ++it) {
         if (MODE == kGradient && wave == 0) feed.turn();
 #pragma unroll
         for (int i = 0; i < S::kEach; ++i) {
@@ -1101,15 +1272,17 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
         auto& meet = partial[MEETS == 2 ? (it - first) & 1 : 0];
 #pragma unroll
         for (int i = 0; i < 4; ++i) meet[wave][i][lane] = f32x4{score[4 * i], score[4 * i + 1], score[4 * i + 2], score[4 * i + 3]};
-        const int64_t y0 = it * kBlock;
+        const int64_t y0 = (int64_t)it * kBlock;
         if (MODE == kGradient && wave == 0)
             if (feed.gather(0, it, lane, cells) && lane == 0) hit = it;
         __syncthreads();
         f32x4 z = (meet[0][wave][lane] + meet[1][wave][lane]) + (meet[2][wave][lane] + meet[3][wave][lane]);   // rows 8*wave + 4*(lane/32) + j
         const int y = 8 * wave + 4 * (lane >> 5);
-        if (MODE != kGradient && y0 + kBlock > a.s.V)
+        if (MODE != kGradient && y0 + kBlock > a.s.V) {
+            asm volatile("");
 #pragma unroll
             for (int j = 0; j < 4; ++j) if (y0 + y + j >= a.s.V) z[j] = -__builtin_inff();
+        }
         if constexpr (MODE == kStats) {
             z *= to_log2;
             const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
@@ -1180,7 +1353,7 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
         const float other = __shfl_xor(ref, 32), to = fmaxf(ref, other);
         sum = sum * exp2f(ref - to);
         sum += __shfl_xor(sum, 32);
-        const int64_t at = (part * kClassWaves + wave) * padded + x;
+        const int64_t at = (int64_t)(part * kClassWaves + wave) * padded + x;
         if (lane < 32) {
             a.at<float>(a.plan.top)[at] = to;
             a.at<float>(a.plan.sum)[at] = sum;
@@ -1196,7 +1369,7 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
             for (int i = 0; i < 4; ++i) {
                 const int d = col0 + 32 * db + 8 * i + 4 * (lane >> 5);
                 const f32x4 g = f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]} * back;
-                if (joined) *reinterpret_cast<f32x4*>(out + (part * rows + x) * DEPTH + d) = g;
+                if (joined) *reinterpret_cast<f32x4*>(out + ((int64_t)part * rows + x) * DEPTH + d) = g;
                 else if (x < a.s.V) {
                     if (d + 4 <= a.s.D) store4(a.grad_w, x * a.s.D + d, g);
                     else
@@ -1235,14 +1408,20 @@ template <class F> hipError_t with_depth(int depth, F f) {
     return hipGetLastError();
 }
 
-template <int DP, bool MEAN, bool PACKED> void launch_forward(const ClassArgs& a, int64_t padded, hipStream_t stream) {
+template <int DP, bool MEAN> void launch_forward(const ClassArgs& a, int64_t padded, hipStream_t stream) {
     const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
-    if constexpr (!narrow_depth(DP))
-        class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats, PACKED><<<grid, kClassThreads, 0, stream>>>(a, padded);
-    else if (a.cut.wy == 1) class_forward_kernel<DP, 1, MEAN, PACKED><<<grid, kClassThreads, 0, stream>>>(a, padded);
-    else if constexpr (!PACKED) {                       // (few rows never pack)
-        if (a.cut.wy == 2) class_forward_kernel<DP, 2, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
-        else if constexpr (DP * NS <= 256) class_forward_kernel<DP, 4, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    const bool straight = a.plan.packed || a.plan.straight;
+    if constexpr (!narrow_depth(DP)) {
+        if (straight) class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats, true><<<grid, kClassThreads, 0, stream>>>(a, padded);
+        else class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    } else if (a.cut.wy == 1) {
+        if (straight) class_forward_kernel<DP, 1, MEAN, true><<<grid, kClassThreads, 0, stream>>>(a, padded);
+        else class_forward_kernel<DP, 1, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    } else if (a.cut.wy == 2) {
+        class_forward_kernel<DP, 2, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    } else if constexpr (DP * NS <= 256) {
+        if (straight) class_forward_kernel<DP, 4, MEAN, true><<<grid, kClassThreads, 0, stream>>>(a, padded);
+        else class_forward_kernel<DP, 4, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
     }
 }
 template <int DP> void launch_gradient(const ClassArgs& a, int64_t padded, hipStream_t stream) {
@@ -1263,8 +1442,7 @@ hipError_t forward(ClassArgs a, hipStream_t stream) {
     while (lanes < 64 && 4 * lanes < a.s.D) lanes *= 2;
     auto run = [&](bool mean) {
         return with_depth(depth, [&](auto dp) {
-            if (a.plan.packed) mean ? launch_forward<dp(), true, true>(a, padded, stream) : launch_forward<dp(), false, true>(a, padded, stream);
-            else mean ? launch_forward<dp(), true, false>(a, padded, stream) : launch_forward<dp(), false, false>(a, padded, stream);
+            mean ? launch_forward<dp(), true>(a, padded, stream) : launch_forward<dp(), false>(a, padded, stream);
         });
     };
     if constexpr (kKind == 0) class_peaks_kernel<<<kPeaksTable, kClassThreads, 0, stream>>>(a, kPeaksTable, 0, 0);
@@ -1292,6 +1470,7 @@ hipError_t gradient(ClassArgs a, hipStream_t stream) {
         return hipGetLastError();
     }
     a.cut = gradient_cut(a.s);
+    a.buckets = buckets_of(a.s.V, a.s.K);
     if constexpr (kHalf) {
         const int rows = kKind == 0 ? kPeaksRows : 0;
         class_peaks_kernel<<<rows + kPeaksGrad, kClassThreads, 0, stream>>>(a, 0, rows, kPeaksGrad);
