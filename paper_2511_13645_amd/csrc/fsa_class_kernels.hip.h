@@ -301,6 +301,15 @@ __global__ __launch_bounds__(kClassThreads) void class_peaks_kernel(ClassArgs a,
     if (threadIdx.x == 0) out[b] = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
 }
 
+// Where chunk c of row r lies in planes of rows of DP elements, in elements.  Wide planes lie as a wave fetches them: by
+// tiles of 32 rows, quarters of the row, and 64 chunks an instruction (chunks lane%4 + 4 (i/2) of rows lane/4 + 16 (i%2)).
+template <int DP> __device__ __forceinline__ int64_t plane_place(int64_t r, int c) {
+    if constexpr (narrow_depth(DP)) return r * DP + c * 8;
+    constexpr int chunks = DP / kClassWaves / 8, each = kBlock * chunks / 64;
+    const int q = c / chunks, cc = c % chunks, rr = (int)(r % kBlock);
+    return (((r / kBlock * kClassWaves + q) * each + 2 * (cc / 4) + rr / 16) * 64 + rr % 16 * 4 + cc % 4) * 8;
+}
+
 // ---------------------------------------------------------------------------------------------------------------
 // backward, ahead of the products: planes of h (rows without a slot are zero, whatever they hold), what a row brings
 // along, the slots sorted, and the gradient of h
@@ -388,7 +397,7 @@ __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, in
             if (lives && c * 8 < a.s.D)
                 planes_of(load8(static_cast<const Elem*>(a.h) + t * a.h_stride, a.s.D, c * 8), u.h, p);
 #pragma unroll
-            for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + ((int64_t)n * padded + t) * DP + c * 8) = p[n];
+            for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + (int64_t)n * padded * DP + plane_place<DP>(t, c)) = p[n];
         }
         const float loss_grad = lives ? a.grad_loss[t] : 0.0f, g = loss_grad * u.g;
         if (a.grad_h && t < a.s.T) write_row_grad(a, t, loss_grad, lives, lane);
@@ -505,7 +514,7 @@ __global__ __launch_bounds__(kClassThreads) void class_pack_kernel(ClassArgs a, 
         u32x4 p[NS] = {};
         if (v < a.s.V && c < a.s.D) planes_of(load8(static_cast<const Elem*>(a.w) + v * a.w_stride, a.s.D, c), unit, p);
 #pragma unroll
-        for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + ((int64_t)n * rows + v) * DP + c) = p[n];
+        for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + (int64_t)n * rows * DP + plane_place<DP>(v, c / 8)) = p[n];
     }
 }
 
@@ -1141,6 +1150,10 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
 template <int Q>
 struct Quarter {
     static constexpr int kChunks = Q / 8, kEach = kBlock * kChunks / 64;
+    // Lane l fetches and stores chunks l%4 + 4 (i/2) of rows l/4 + 16 (i%2): 64 bytes of a row together, and places that
+    // follow from one by constants.
+    static __device__ __forceinline__ int row(int i, int lane) { return (lane >> 2) + 16 * (i & 1); }
+    static __device__ __forceinline__ int chunk(int i, int lane) { return (lane & 3) + 4 * (i >> 1); }
     static constexpr bool kTurns = kChunks == 32;
     static constexpr int kStride = 8 * (kTurns ? 32 : kChunks + 3 <= 20 ? 20 : 28);       // elements from row to row
     static constexpr int kPlane = kBlock * kStride;
@@ -1164,20 +1177,34 @@ struct Quarter {
     }
 };
 
+// Steps load(k, f), use(k, f) for k = 0 ... N - 1, every load three uses ahead of its own.
+template <int N, class Load, class Use> __device__ __forceinline__ void ahead_of(Load load, Use use) {
+    constexpr int R = 4;
+    u32x4 ring[R][NS];
+    each<R - 1>([&](auto k) { if constexpr (k() < N) load(k, ring[k()]); });
+    each<N>([&](auto k) {
+        if constexpr (k() + R - 1 < N) load(number<k() + R - 1>{}, ring[(k() + R - 1) % R]);
+        use(k, ring[k() % R]);
+        __builtin_amdgcn_sched_barrier(0);
+    });
+}
+
 enum WideMode { kStats, kMean, kGradient };
 
 // kStats: running maximum and sum of every held row of h, one pair per wave (a quarter of the streamed classes each).
 // kMean: sum of the table's rows under 2^(score - norm).  kGradient: as the narrow kernel.
 template <int Q, WideMode MODE, bool STRAIGHT>
-__global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, int64_t padded) {
+__global__ __launch_bounds__(kClassThreads, Q * NS <= 160 ? 2 : 1) void class_wide_kernel(ClassArgs a, int64_t padded) {
     using S = Quarter<Q>;
     constexpr int DEPTH = Q * kClassWaves;
     __shared__ __align__(16) uint16_t quarters[kClassWaves][NS * S::kPlane];
-    constexpr int MEETS = MODE == kStats && Q * NS < 512 ? 2 : 1;      // one more barrier a tile where only one fits
+    constexpr int MEETS = MODE == kStats && Q < 160 ? 2 : 1;          // one more barrier a tile where two cost a workgroup
     __shared__ __align__(16) f32x4 partial[MEETS][kClassWaves][4][64];
     constexpr int PS = MODE == kStats ? 1 : MODE == kGradient ? 2 : NS;   // planes of P; 16-bit types use the second after a hit
     __shared__ __align__(16) u32x2 shared_p[PS][2][64][2];
-    __shared__ int hit;                             // the tile that last had a slot of these classes
+    // the tile that last had a slot of these classes, where rows have a corner to spare in that
+    __shared__ int hit_alone;
+    int& hit = S::kTurns ? hit_alone : *reinterpret_cast<int __attribute__((may_alias))*>(quarters[0] + S::kStride - 8);
     __shared__ float cells[MODE == kGradient ? kBlock * kBlock : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col0 = wave * Q;
     const ClassCut::Place place = a.cut.place(blockIdx.x);
@@ -1219,7 +1246,9 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
     struct { Eight e[FROM_PLANES ? 1 : S::kEach]; u32x4 p[FROM_PLANES ? NS : 1][FROM_PLANES ? S::kEach : 1]; } next;
     const bool as_is = MODE != kGradient && !a.plan.packed;
     const uint16_t* streamed = MODE == kGradient ? planes : as_is ? reinterpret_cast<const uint16_t*>(w) : a.at<const uint16_t>(a.plan.table);
-    const int64_t streamed_rows = MODE == kGradient ? padded : as_is ? a.s.V : padded_rows(a.s.V), streamed_stride = as_is ? a.w_stride : DEPTH;
+    const int64_t plane = (MODE == kGradient ? padded : padded_rows(a.s.V)) * DEPTH;
+    const int lane_place = as_is ? S::row(0, lane) * (int)a.w_stride + S::chunk(0, lane) * 8 : lane * 8;
+    const int step_row = as_is ? 16 * (int)a.w_stride : 512, step_chunk = as_is ? 32 : 1024;
     SlotFeed<1> feed(a, padded, MODE == kGradient ? x0 : 0);
     f32x4 next_start = {};
     auto fetch = [&](int it) {
@@ -1228,15 +1257,21 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
                 feed.ask_slots(it, lane);
                 feed.ask_words(it + 1);
             }
+        const uint16_t* at = streamed + (as_is ? (int64_t)it * kBlock * a.w_stride + col0 : ((int64_t)it * kClassWaves + wave) * S::kEach * 512);
+        const int left = as_is ? (int)(a.s.V - 1 - (int64_t)it * kBlock) : kBlock;       // planes have whole tiles
 #pragma unroll
         for (int i = 0; i < S::kEach; ++i) {
-            const int q = i * 64 + lane, r = q / S::kChunks, c = q % S::kChunks;
-            const int64_t row = (int64_t)it * kBlock + r;
+            const int c = S::chunk(i, lane);
+            const int64_t row = (int64_t)it * kBlock + S::row(i, lane);
             if constexpr (FROM_PLANES) {
+                int place = lane_place + (i & 1) * step_row + (i >> 1) * step_chunk;
+                if (left < kBlock) {
+                    asm volatile("");                   // the last tile of a table as it is: rows behind its last one repeat it
+                    const int r = S::row(i, lane);
+                    place = (r < left ? r : left) * (int)a.w_stride + c * 8;
+                }
 #pragma unroll
-                for (int n = 0; n < NS; ++n)
-                    next.p[n][i] = *reinterpret_cast<const u32x4*>(streamed + ((int64_t)n * streamed_rows + (row < streamed_rows ? row : streamed_rows - 1)) *
-                                                                                 streamed_stride + col0 + c * 8);
+                for (int n = 0; n < NS; ++n) next.p[n][i] = *reinterpret_cast<const u32x4*>(at + n * plane + place);
             } else next.e[i] = load8(w + (row < a.s.V ? row : a.s.V - 1) * a.w_stride, a.s.D, col0 + c * 8);
         }
         if constexpr (MODE == kGradient)
@@ -1250,7 +1285,7 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
         if (MODE == kGradient && wave == 0) feed.turn();
 #pragma unroll
         for (int i = 0; i < S::kEach; ++i) {
-            const int q = i * 64 + lane, r = q / S::kChunks, c = q % S::kChunks;
+            const int r = S::row(i, lane), c = S::chunk(i, lane);
             u32x4 p[NS];
             if constexpr (FROM_PLANES) {
 #pragma unroll
@@ -1263,12 +1298,8 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
         __builtin_amdgcn_wave_barrier();
         if (it + 1 < last) fetch(it + 1);
         f32x16 score = {};
-#pragma unroll
-        for (int ks = 0; ks < Q / 16; ++ks) {
-            u32x4 f[NS];
-            S::rows(lds, ks, lane, f);
-            score = matmul(f, held[ks], score);
-        }
+        ahead_of<Q / 16>([&](auto k, u32x4 (&f)[NS]) { S::rows(lds, k(), lane, f); },
+                         [&](auto k, const u32x4 (&f)[NS]) { score = matmul(f, held[k()], score); });
         auto& meet = partial[MEETS == 2 ? (it - first) & 1 : 0];
 #pragma unroll
         for (int i = 0; i < 4; ++i) meet[wave][i][lane] = f32x4{score[4 * i], score[4 * i + 1], score[4 * i + 2], score[4 * i + 3]};
@@ -1325,26 +1356,21 @@ __global__ __launch_bounds__(kClassThreads) void class_wide_kernel(ClassArgs a, 
                 shared_p[PS - 1][wave >> 1][lane][wave & 1] =
                     u32x2{pack2(p[0] - low2(p0), p[1] - high2(p0)), pack2(p[2] - low2(p1), p[3] - high2(p1))};
             __syncthreads();
+            constexpr int DB = Q / 32;
+            u32x4 b[2][NS];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                u32x4 b[NS];
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-                for (int n = 0; n < NS; ++n) b[n] = *reinterpret_cast<const u32x4*>(&shared_p[n][s][lane][0]);
+                for (int n = 0; n < NS; ++n) b[s][n] = *reinterpret_cast<const u32x4*>(&shared_p[n][s][lane][0]);
+            auto products = [&] {
+                ahead_of<2 * DB>([&](auto k, u32x4 (&f)[NS]) { S::columns(lds, k() / DB, k() % DB, lane, f); },
+                                 [&](auto k, const u32x4 (&f)[NS]) { acc[k() % DB] = matmul(f, b[k() / DB], acc[k() % DB]); });
+            };
+            products();
+            if (rest) {
 #pragma unroll
-                for (int db = 0; db < Q / 32; ++db) {
-                    u32x4 f[NS];
-                    S::columns(lds, s, db, lane, f);
-                    acc[db] = matmul(f, b, acc[db]);
-                }
-                if (rest) {
-                    b[0] = *reinterpret_cast<const u32x4*>(&shared_p[PS - 1][s][lane][0]);
-#pragma unroll
-                    for (int db = 0; db < Q / 32; ++db) {
-                        u32x4 f[NS];
-                        S::columns(lds, s, db, lane, f);
-                        acc[db] = matmul(f, b, acc[db]);
-                    }
-                }
+                for (int s = 0; s < 2; ++s) b[s][0] = *reinterpret_cast<const u32x4*>(&shared_p[PS - 1][s][lane][0]);
+                products();
             }
         }
         __builtin_amdgcn_wave_barrier();
