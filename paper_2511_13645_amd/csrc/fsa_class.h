@@ -54,9 +54,15 @@ struct ClassCut {
 // Streamed blocks of a tile: two tiles and what else a workgroup keeps fit into LDS.
 constexpr int blocks_per_tile(int wy, int depth, int kind) { return depth * class_planes(kind) > 256 ? wy : wy == 4 ? 4 : 2; }
 
+// Workgroups that the chip's 256 CUs hold at a time: two to a CU where registers and LDS allow it.
+constexpr int64_t resident_workgroups(int depth, int kind) {
+    return depth * class_planes(kind) <= 128 || (!narrow_depth(depth) && depth <= 640 && class_planes(kind) == 1) ? 512 : 256;
+}
+// As many shares of the streamed side as make one round of workgroups; where that costs little a multiple of 8, so that the
+// workgroups of one share, dealt out to the 8 XCDs in turn, meet on one XCD's L2.
 inline int64_t parts_for(int64_t groups, int64_t tiles, int64_t workgroups, int64_t most) {
-    int64_t want = ceil_div(workgroups, groups);
-    if (want >= 8) want = want / 8 * 8;                 // shares of one table range meet on one XCD's L2
+    int64_t want = workgroups / groups;
+    if (want >= 8 && want / 8 * 8 * 8 >= want * 7) want = want / 8 * 8;
     if (want > most) want = most;
     if (want > tiles) want = tiles;
     return want < 1 ? 1 : want;
@@ -68,7 +74,7 @@ inline ClassCut cut_of(int64_t held, int64_t streamed, int depth, int kind, int6
         c.wx = 1; c.wy = 1;
         c.groups = blocks;
         c.tiles = ceil_div(streamed, kBlock);
-        c.parts = parts_for(c.groups, c.tiles, 512, most_parts);
+        c.parts = parts_for(c.groups, c.tiles, resident_workgroups(depth, kind), most_parts);
         return c;
     }
     c.wy = blocks >= 4 ? 1 : blocks >= 2 ? 2 : 4;
@@ -76,13 +82,12 @@ inline ClassCut cut_of(int64_t held, int64_t streamed, int depth, int kind, int6
     c.wx = kClassWaves / c.wy;
     c.groups = ceil_div(blocks, c.wx);
     c.tiles = ceil_div(streamed, (int64_t)blocks_per_tile(c.wy, depth, kind) * kBlock);
-    c.parts = parts_for(c.groups, c.tiles, 1024, most_parts);
+    c.parts = parts_for(c.groups, c.tiles, resident_workgroups(depth, kind), most_parts);
     return c;
 }
 inline ClassCut forward_cut(const ClassShape& s) { return cut_of(s.T, s.V, class_depth(s.D), s.kind, 1024); }
 inline ClassCut gradient_cut(const ClassShape& s) {
     ClassCut c = cut_of(s.V, s.T, class_depth(s.D), s.kind, 64);
-    if (c.groups >= 512) c.parts = 1;                   // the classes fill the chip by themselves
     return c;
 }
 
@@ -97,7 +102,10 @@ constexpr ClassBuckets buckets_of(int64_t V, int K) {
 
 // Whether the forward first lays the table out as planes of padded rows: one more pass over the table, against rows
 // that the kernel has to read off the 16-byte grid, to pad, or to split into planes, once for every workgroup beside it.
-inline bool forward_packs(const ClassShape& s, bool straight) { return !straight && forward_cut(s).groups > 2; }
+// Tables of a quarter of a million elements and less are not worth the launch.
+inline bool forward_packs(const ClassShape& s, bool straight) {
+    return !straight && forward_cut(s).groups > 2 && s.V * s.D > (1 << 18);
+}
 
 // Byte offsets into the caller's workspace.
 struct ClassPlan {

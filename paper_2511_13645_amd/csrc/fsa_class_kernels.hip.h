@@ -509,12 +509,19 @@ __global__ __launch_bounds__(kClassThreads) void class_pack_kernel(ClassArgs a, 
     const float unit = table_unit(a, room);
     uint16_t* planes = a.at<uint16_t>(a.plan.table);
     for (int64_t q = (int64_t)blockIdx.x * kClassThreads + threadIdx.x; q < rows * (DP / 8); q += (int64_t)gridDim.x * kClassThreads) {
-        const int64_t v = q / (DP / 8);
-        const int c = (int)(q % (DP / 8)) * 8;
+        int64_t v = q / (DP / 8);                       // chunk q of the planes, in their own order
+        int c = (int)(q % (DP / 8));
+        if constexpr (!narrow_depth(DP)) {
+            constexpr int chunks = DP / kClassWaves / 8, each = kBlock * chunks / 64;
+            const int lane = (int)(q % 64);
+            const int64_t load = q / 64, i = load % each, quarter = load / each % kClassWaves;
+            v = load / each / kClassWaves * kBlock + (lane >> 2) + 16 * (i & 1);
+            c = (int)(quarter * chunks + (lane & 3) + 4 * (i >> 1));
+        }
         u32x4 p[NS] = {};
-        if (v < a.s.V && c < a.s.D) planes_of(load8(static_cast<const Elem*>(a.w) + v * a.w_stride, a.s.D, c), unit, p);
+        if (v < a.s.V && c * 8 < a.s.D) planes_of(load8(static_cast<const Elem*>(a.w) + v * a.w_stride, a.s.D, c * 8), unit, p);
 #pragma unroll
-        for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + (int64_t)n * rows * DP + plane_place<DP>(v, c / 8)) = p[n];
+        for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + (int64_t)n * rows * DP + q * 8) = p[n];
     }
 }
 
@@ -861,9 +868,10 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
     if (!live) return;
     sum += __shfl_xor(sum, 32);
     const int64_t at = (int64_t)(part * WY + y) * padded + row;
-    if (lane < 32) {
-        a.at<float>(a.plan.top)[at] = ref;
-        a.at<float>(a.plan.sum)[at] = sum;
+    if (lane < 32) {                                    // a row's slices lie together
+        const int64_t stat = row * a.cut.slices() + part * WY + y;
+        a.at<float>(a.plan.top)[stat] = ref;
+        a.at<float>(a.plan.sum)[stat] = sum;
     }
     if constexpr (MEAN) {
         float* out = a.at<float>(a.plan.mean_parts) + at * DP + 4 * (lane >> 5);
@@ -889,11 +897,12 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
     __shared__ __align__(16) f32x4 gathered[ROWS ? kClassThreads : 1];
     const int64_t t = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const float* tops = a.at<const float>(a.plan.top);
-    const float* sums = a.at<const float>(a.plan.sum);
+    const float* tops = a.at<const float>(a.plan.top) + t * slices;
+    const float* sums = a.at<const float>(a.plan.sum) + t * slices;
     float top = -3e38f, sum = 1.0f;
     if constexpr (LOSS)
-        for (int p = threadIdx.x; p < slices; p += kClassThreads) top = fmaxf(top, tops[p * padded + t]);
+#pragma unroll 4
+        for (int p = threadIdx.x; p < slices; p += kClassThreads) top = fmaxf(top, tops[p]);
     const float table = LOSS && ROWS ? table_unit(a, room) : 1.0f;
     if (wave == 0) {
         int id;
@@ -923,9 +932,10 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
         top = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
         __syncthreads();
         sum = 0.0f;
+#pragma unroll 4
         for (int p = threadIdx.x; p < slices; p += kClassThreads) {
-            const float e = exp2f(tops[p * padded + t] - top);
-            sum += sums[p * padded + t] * e;
+            const float e = exp2f(tops[p] - top);
+            sum += sums[p] * e;
             if constexpr (ROWS) weight[p] = e;
         }
 #pragma unroll
@@ -1379,7 +1389,7 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 160 ? 2 : 1) void class_wi
         const float other = __shfl_xor(ref, 32), to = fmaxf(ref, other);
         sum = sum * exp2f(ref - to);
         sum += __shfl_xor(sum, 32);
-        const int64_t at = (int64_t)(part * kClassWaves + wave) * padded + x;
+        const int64_t at = x * (a.cut.parts * kClassWaves) + part * kClassWaves + wave;
         if (lane < 32) {
             a.at<float>(a.plan.top)[at] = to;
             a.at<float>(a.plan.sum)[at] = sum;
