@@ -375,8 +375,8 @@ int fsa_wmean_bwd_ws(const float* grad_out, const float* grad_h1,
  * slot (or whose teacher logits are all -inf) has loss 0, lse 0, a zero gradient, and adds nothing to grad_w,
  * whatever its h, lse and grad_loss hold, NaN included.  An ID of V or more is not read: the row's loss is NaN, the
  * gradients are as if its slot's class were none of the table's.  An ID named by two slots of a row counts twice.
- *   h [T,D], w [V,D]   fsa_dtype `dtype`, rows `h_stride` and `w_stride` elements apart (>= D), at any alignment of an
- *                      element;  0 <= T <= FSA_CLASS_TMAX, 1 <= V <= FSA_CLASS_VMAX, 1 <= D <= FSA_CLASS_DMAX
+ *   h [T,D], w [V,D]   fsa_dtype `dtype`, rows `h_stride` and `w_stride` elements apart (D to 2^24), at any alignment of
+ *                      an element;  0 <= T <= FSA_CLASS_TMAX, 1 <= V <= FSA_CLASS_VMAX, 1 <= D <= FSA_CLASS_DMAX
  *   scale, temperature finite and positive
  *   out_loss, out_lse  [T] fp32
  *   out_row_grad       [T,D] fp32, the gradient of every loss by its row, s * (sum_v p w[v] - sum_j q w[ids_j]); may be NULL

@@ -61,7 +61,7 @@ constexpr int64_t resident_workgroups(int depth, int kind) {
 // As many shares of the streamed side as make one round of workgroups; where that costs little a multiple of 8, so that the
 // workgroups of one share, dealt out to the 8 XCDs in turn, meet on one XCD's L2.
 inline int64_t parts_for(int64_t groups, int64_t tiles, int64_t workgroups, int64_t most) {
-    int64_t want = workgroups / groups;
+    int64_t want = groups > 0 ? workgroups / groups : 1;           // no rows: no workgroups either
     if (want >= 8 && want / 8 * 8 * 8 >= want * 7) want = want / 8 * 8;
     if (want > most) want = most;
     if (want > tiles) want = tiles;

@@ -14,6 +14,8 @@ bool sizes_ok(int64_t T, int64_t V, int64_t D, int32_t K) {
     return T >= 0 && T <= FSA_CLASS_TMAX && V >= 1 && V <= FSA_CLASS_VMAX && D >= 1 && D <= FSA_CLASS_DMAX && K >= 1 &&
            K <= FSA_KMAX;
 }
+constexpr int64_t kMostStride = 1 << 24;             // a block of 32 rows stays within 32-bit byte offsets
+
 bool positive(float x) { return std::isfinite(x) && x > 0.0f; }
 
 // What every entry point takes, checked; `a` is filled in but for outputs and workspace.
@@ -21,7 +23,8 @@ int take(fsa::ClassArgs& a, const void* h, int64_t h_stride, const void* w, int6
          int64_t D, float scale, float temperature, const int32_t* ids, const void* teacher, int teacher_dtype, int32_t K) {
     if (!w || (T > 0 && (!h || !ids))) return FSA_ERR_NULL;
     if (!known(dtype) || !known(teacher_dtype)) return FSA_ERR_DTYPE;
-    if (!sizes_ok(T, V, D, K) || h_stride < D || w_stride < D) return FSA_ERR_ARG;
+    if (!sizes_ok(T, V, D, K) || h_stride < D || w_stride < D || h_stride > kMostStride || w_stride > kMostStride)
+        return FSA_ERR_ARG;
     if (!positive(scale) || !positive(temperature) || !positive(scale / temperature) || !positive(1.0f / temperature)) return FSA_ERR_ARG;
     if (!aligned(h, elem_bytes(dtype)) || !aligned(w, elem_bytes(dtype)) || !aligned(ids, 4) ||
         !aligned(teacher, elem_bytes(teacher_dtype)))

@@ -227,7 +227,8 @@ __device__ __forceinline__ float table_unit(const ClassArgs& a, float* room) {
 struct Units { float h, g; };
 template <int WAVES = kClassWaves>
 __device__ __forceinline__ Units row_units(const ClassArgs& a, float* room) {
-    Units u{1.0f, 1.0f};
+    // bfloat16 has the range as it is: 24 binades keep products that its subnormals can still hold out of fp32's
+    Units u{1.0f, 0x1p24f};
     const float* p = a.at<const float>(a.plan.peaks);
     if constexpr (kKind == 0) u.h = unit_of(block_peak<WAVES>(p + kPeaksTable, kPeaksRows, room));
     if constexpr (kHalf) u.g = unit_of(block_peak<WAVES>(p + kPeaksTable + kPeaksRows, kPeaksGrad, room));
