@@ -56,7 +56,7 @@ constexpr int blocks_per_tile(int wy, int depth, int kind) { return depth * clas
 
 // Workgroups that the chip's 256 CUs hold at a time: two to a CU where registers and LDS allow it.
 constexpr int64_t resident_workgroups(int depth, int kind) {
-    return depth * class_planes(kind) <= 128 || (!narrow_depth(depth) && depth <= 640 && class_planes(kind) == 1) ? 512 : 256;
+    return depth * class_planes(kind) <= 128 || (!narrow_depth(depth) && depth * class_planes(kind) <= 768) ? 512 : 256;
 }
 // As many shares of the streamed side as make one round of workgroups; where that costs little a multiple of 8, so that the
 // workgroups of one share, dealt out to the 8 XCDs in turn, meet on one XCD's L2.

@@ -1156,8 +1156,8 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
 // wide rows: the four waves of a workgroup hold a quarter of the elements each
 // ---------------------------------------------------------------------------------------------------------------
 // A wave's quarter of 32 streamed rows in LDS, its own: no other wave reads it.  Rows of 32 chunks turn as in the narrow
-// kernels' tiles; others lie 4 or 12 chunks more than a multiple of 16 apart, every four of them one chunk further on,
-// which parts the same reads.
+// kernels' tiles; others, of 4 or 12 chunks more than a multiple of 16, lie close but for one chunk more after every four of
+// them, which parts the same reads.
 template <int Q>
 struct Quarter {
     static constexpr int kChunks = Q / 8, kEach = kBlock * kChunks / 64;
@@ -1166,11 +1166,11 @@ struct Quarter {
     static __device__ __forceinline__ int row(int i, int lane) { return (lane >> 2) + 16 * (i & 1); }
     static __device__ __forceinline__ int chunk(int i, int lane) { return (lane & 3) + 4 * (i >> 1); }
     static constexpr bool kTurns = kChunks == 32;
-    static constexpr int kStride = 8 * (kTurns ? 32 : kChunks + 3 <= 20 ? 20 : 28);       // elements from row to row
-    static constexpr int kPlane = kBlock * kStride;
-    static_assert(kStride >= Q && (kBlock * kChunks) % 64 == 0 && (kTurns || (kChunks + 3 <= 28)), "rows fit, lanes share them evenly");
+    static constexpr int kPlane = kBlock * Q + (kTurns ? 0 : 64);
+    static_assert(kTurns || kChunks % 16 == 4 || kChunks % 16 == 12, "rows part on banks");
+    static_assert((kBlock * kChunks) % 64 == 0 && kChunks % 4 == 0, "lanes share rows evenly");
     static __device__ __forceinline__ int place(int r, int c) {
-        return r * kStride + (kTurns ? c ^ turn<Q>(r) : c + ((r >> 2) & 3)) * 8;
+        return kTurns ? r * Q + (c ^ turn<Q>(r)) * 8 : r * Q + (r >> 2) * 8 + c * 8;
     }
     static __device__ __forceinline__ void rows(const uint16_t* lds, int ks, int lane, u32x4 (&out)[NS]) {
 #pragma unroll
@@ -1205,7 +1205,7 @@ enum WideMode { kStats, kMean, kGradient };
 // kStats: running maximum and sum of every held row of h, one pair per wave (a quarter of the streamed classes each).
 // kMean: sum of the table's rows under 2^(score - norm).  kGradient: as the narrow kernel.
 template <int Q, WideMode MODE, bool STRAIGHT>
-__global__ __launch_bounds__(kClassThreads, Q * NS <= 160 ? 2 : 1) void class_wide_kernel(ClassArgs a, int64_t padded) {
+__global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wide_kernel(ClassArgs a, int64_t padded) {
     using S = Quarter<Q>;
     constexpr int DEPTH = Q * kClassWaves;
     __shared__ __align__(16) uint16_t quarters[kClassWaves][NS * S::kPlane];
@@ -1213,9 +1213,7 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 160 ? 2 : 1) void class_wi
     __shared__ __align__(16) f32x4 partial[MEETS][kClassWaves][4][64];
     constexpr int PS = MODE == kStats ? 1 : MODE == kGradient ? 2 : NS;   // planes of P; 16-bit types use the second after a hit
     __shared__ __align__(16) u32x2 shared_p[PS][2][64][2];
-    // the tile that last had a slot of these classes, where rows have a corner to spare in that
-    __shared__ int hit_alone;
-    int& hit = S::kTurns ? hit_alone : *reinterpret_cast<int __attribute__((may_alias))*>(quarters[0] + S::kStride - 8);
+    __shared__ int hit;                                 // the tile that last had a slot of these classes
     __shared__ float cells[MODE == kGradient ? kBlock * kBlock : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col0 = wave * Q;
     const ClassCut::Place place = a.cut.place(blockIdx.x);
