@@ -100,11 +100,14 @@ constexpr ClassBuckets buckets_of(int64_t V, int K) {
     return {per, ceil_div(blocks, per)};
 }
 
-// Whether the forward first lays the table out as planes of padded rows: one more pass over the table, against rows
-// that the kernel has to read off the 16-byte grid, to pad, or to split into planes, once for every workgroup beside it.
-// Tables of a quarter of a million elements and less are not worth the launch.
+// Whether the forward first lays the table out as planes of padded rows: one more pass over the table, against rows that
+// the kernel has to read off the 16-byte grid, to pad, or to split into planes, once for every workgroup beside it (measured
+// on 2 to 9 of them: it pays from 3 on; wide rows of which two workgroups fit a CU hide that work, 3 of 67 rows x 493,386
+// x 336 fp32 1.54 ms without, 1.67 with).  Tables of a quarter of a million elements and less are not worth the launch.
 inline bool forward_packs(const ClassShape& s, bool straight) {
-    return !straight && forward_cut(s).groups > 2 && s.V * s.D > (1 << 18);
+    const int depth = class_depth(s.D);
+    const int64_t few = !narrow_depth(depth) && resident_workgroups(depth, s.kind) == 512 ? 4 : 2;
+    return !straight && forward_cut(s).groups > few && s.V * s.D > (1 << 18);
 }
 
 // Byte offsets into the caller's workspace.

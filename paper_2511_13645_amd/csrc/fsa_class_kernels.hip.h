@@ -1209,7 +1209,7 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
     using S = Quarter<Q>;
     constexpr int DEPTH = Q * kClassWaves;
     __shared__ __align__(16) uint16_t quarters[kClassWaves][NS * S::kPlane];
-    constexpr int MEETS = MODE == kStats && Q < 160 ? 2 : 1;          // one more barrier a tile where two cost a workgroup
+    constexpr int MEETS = MODE == kStats && Q * NS < 160 ? 2 : 1;         // one more barrier a tile where two cost a workgroup
     __shared__ __align__(16) f32x4 partial[MEETS][kClassWaves][4][64];
     constexpr int PS = MODE == kStats ? 1 : MODE == kGradient ? 2 : NS;   // planes of P; 16-bit types use the second after a hit
     __shared__ __align__(16) u32x2 shared_p[PS][2][64][2];
