@@ -251,18 +251,26 @@ __device__ __forceinline__ float wave_max(float m) {
     return m;
 }
 
-// Whether row t has a slot, asked by one lane.
+// Score of slot i of [T,K] before the softmax over a row's slots; -inf: an empty slot, or one that the teacher gives nothing.
+__device__ __forceinline__ float slot_score(const ClassArgs& a, int64_t i) {
+    if (a.ids[i] < 0) return -__builtin_inff();
+    if (!a.teacher) return 0.0f;
+    if (a.teacher_kind == 0) return static_cast<const float*>(a.teacher)[i] * a.inv_temperature;
+    if (a.teacher_kind == 1) return __builtin_bit_cast(float, (uint32_t)static_cast<const uint16_t*>(a.teacher)[i] << 16) * a.inv_temperature;
+    return (float)static_cast<const _Float16*>(a.teacher)[i] * a.inv_temperature;
+}
+// Whether row t has a slot of any weight, asked by one lane, and by a whole wave.
 __device__ __forceinline__ bool lane_lives(const ClassArgs& a, int64_t t) {
-    for (int j = 0; j < a.s.K; ++j) if (a.ids[t * a.s.K + j] >= 0) return true;
+    for (int j = 0; j < a.s.K; ++j) if (slot_score(a, t * a.s.K + j) != -__builtin_inff()) return true;
     return false;
 }
-// Whether a row has a slot; the whole wave asks for one row.
 __device__ __forceinline__ bool row_lives(const ClassArgs& a, int64_t t, int lane) {
-    bool some = false;
-    for (int j = lane; j < a.s.K; j += 64) some |= a.ids[t * a.s.K + j] >= 0;
-    return __any(some);
+    return __any(lane < a.s.K && slot_score(a, t * a.s.K + lane) != -__builtin_inff());
 }
 
+// Largest finite magnitudes, a part per workgroup, of the table, of the rows and of the losses' gradients (those of rows that
+// live).  One more read of an fp32 table, 1.28 GB in 0.35 ms: the price of 22-bit products at three matrix instructions instead
+// of six of three bfloat16 planes.
 __global__ __launch_bounds__(kClassThreads) void class_peaks_kernel(ClassArgs a, int table, int rows, int grad) {
     __shared__ float room[kClassWaves];
     float* out = a.at<float>(a.plan.peaks);
@@ -322,11 +330,7 @@ __device__ __forceinline__ float slot_weight(const ClassArgs& a, int64_t t, int 
     if (lane < a.s.K) {
         const int64_t i = t * a.s.K + lane;
         id = a.ids[i];
-        if (!a.teacher) x = 0.0f;
-        else if (a.teacher_kind == 0) x = static_cast<const float*>(a.teacher)[i];
-        else if (a.teacher_kind == 1) x = __builtin_bit_cast(float, (uint32_t)static_cast<const uint16_t*>(a.teacher)[i] << 16);
-        else x = (float)static_cast<const _Float16*>(a.teacher)[i];
-        x = id < 0 ? -__builtin_inff() : x * a.inv_temperature;
+        x = slot_score(a, i);
     }
     log_weight = 0.0f;
     if (!a.teacher) return id >= 0 ? 1.0f : 0.0f;
@@ -371,7 +375,7 @@ __global__ __launch_bounds__(kClassThreads) void class_row_grad_kernel(ClassArgs
     write_row_grad(a, t, a.grad_loss[t], __any(id >= 0), lane);
 }
 
-// One workgroup per 32 rows, two to a wave.
+// One workgroup per 32 rows, two to a wave.  Latency alone, 8 to 20 us: the chain from IDs over logits to the sorted slots.
 template <int DP>
 __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, int64_t padded) {
     __shared__ float room[kRowWaves];
@@ -503,7 +507,8 @@ struct SlotFeed {
     }
 };
 
-// The table as planes of padded rows, zero behind its last row and element.
+// The table as planes of padded rows, zero behind its last row and element.  Bound by memory: 2.5 M x 128 fp32, 1.28 GB in and
+// out each, 0.47 ms (5.4 TB/s).
 template <int DP>
 __global__ __launch_bounds__(kClassThreads) void class_pack_kernel(ClassArgs a, int64_t rows) {
     __shared__ float room[kClassWaves];
@@ -725,6 +730,15 @@ __device__ __forceinline__ void advance(const uint16_t* ahead, const uint16_t* t
 // ---------------------------------------------------------------------------------------------------------------
 // forward: a wave holds 32 rows of h, the table streams by
 // ---------------------------------------------------------------------------------------------------------------
+// Mathematics: p = 2^(score * log2e - ref), ref following a row's maximum; the sum of p and, for the gradient of the row,
+// the sum of p times the table's rows (whose quotient is their mean under the softmax), all in one pass.
+// What bounds it: two products of T V D multiply-adds on the matrix units beside an exponential a score, which takes 16
+// cycles for 64 of them, as long as half a product of 128 elements.  4096 rows x 2.5 M classes x 128 bfloat16: 5.04 ms, 1.04
+// PFLOP/s, matrix units busy 56 % of 9.0 M cycles at the 1.84 GHz that the card holds then; a large bfloat16 product of the
+// library runs at 1.29.  8 rows, one read of the table: 102 us, 6.1 TB/s.
+// Why this way: rows stay in registers and the table streams, because a row's statistics then never leave its lane (an
+// accumulator column) until the end; a wave has 32 of them, two waves fit a SIMD (one held 64 % as much: 8.1 ms).  Few rows: the
+// waves of a workgroup share the streamed blocks instead (WY).
 template <int DP, int WY, bool MEAN, bool STRAIGHT>
 __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_forward_kernel(ClassArgs a, int64_t padded) {
     constexpr int NB = blocks_per_tile(WY, DP, kKind), MY = NB / WY, WX = kClassWaves / WY;   // blocks of a tile, a wave's own of them
@@ -888,7 +902,8 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
 // One workgroup per row.  LOSS: the parts joined, the row's slots scored again (fp32 sums of the elements themselves), its
 // loss.  ROWS: the gradient of its loss, scale * (mean of the table's rows - sum of its slots' q w), from parts that carry
 // their own reference (LOSS as well) or that are normalised already.
-// The workgroup is cut into groups of `lanes` lanes that cover four elements each; slots and parts go around them.
+// The workgroup is cut into groups of `lanes` lanes that cover four elements each; slots and parts go around them.  Bound by
+// the latency of its reads: 4096 rows x 128 with 16 parts 20 us, 8 rows 6.
 constexpr int kMostSlices = 4096;
 template <bool LOSS, bool ROWS>
 __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a, int64_t padded, int depth, int slices, int lanes) {
@@ -1003,6 +1018,11 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
 // ---------------------------------------------------------------------------------------------------------------
 // A wave holds 32 classes, the rows stream by:
 //   grad_w[v] = scale * sum_t g_t (p[t,v] - sum over t's slots j that name v of q_j) h[t]
+// Scores are made again from the table and the rows, 2 T V D operations, because keeping them would move 6 bytes a score: 12
+// times what the classes and their gradients move at 128 elements.  A class's row is written once, by the wave that holds it,
+// or in parts that a second launch joins where there are fewer classes than waves.
+// 4096 x 2.5 M x 128 bfloat16: 5.4 ms, 0.97 PFLOP/s; what a slot adds costs by the slot (4096 x 169,343, 32 slots a row: 0.55
+// ms, 0.39 without).
 template <int DP, int WY>
 __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) void class_gradient_kernel(ClassArgs a, int64_t padded) {
     constexpr int NB = blocks_per_tile(WY, DP, kKind), MY = NB / WY, WX = kClassWaves / WY;
@@ -1202,6 +1222,13 @@ template <int N, class Load, class Use> __device__ __forceinline__ void ahead_of
 
 enum WideMode { kStats, kMean, kGradient };
 
+// Rows of more than 256 elements do not fit a wave's registers beside their accumulators.  Split over four waves, each adds
+// its quarter of every score; a wave then sums the four partial scores of a quarter of the streamed rows, so that every
+// exponential is taken once, and P goes back to all through LDS: 3 KB of LDS traffic a wave for 32 x 32 scores.  The forward is
+// two launches, statistics first: a common running maximum would cost the four waves another meeting a tile.
+// Bound by the meetings (two barriers a tile) and, for the statistics, by the table's way to the CUs, once for every 32 rows.
+// 1024 x 232,965 x 602 fp16: 0.62 + 0.94 + 1.00 ms (0.46, 0.61, 0.57 PFLOP/s); fp32, 257 rows: 0.59 + 0.77 + 1.14 ms, of which
+// one workgroup fits a CU, so that its meetings are waited for: 1.4 times the plain products in fp32, the furthest from the floor.
 // kStats: running maximum and sum of every held row of h, one pair per wave (a quarter of the streamed classes each).
 // kMean: sum of the table's rows under 2^(score - norm).  kGradient: as the narrow kernel.
 template <int Q, WideMode MODE, bool STRAIGHT>

@@ -398,3 +398,20 @@ def test_tables_beyond_32_bit_offsets(fsa, D, V):
     d = (p - (rows[None, :] == ids[:, None]).double()) * torch.where(live, g.double(), 0.0)[:, None]
     bound = 2 * 2.0 ** -8 * (d.abs().T @ h.double().abs())
     check(gw[rows], d.T @ h.double(), bound, "bf16", "grad_w")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("D", [80, 400])
+def test_rows_that_the_teacher_gives_nothing_hold_anything(fsa, dtype, D):
+    """A row whose slots all have logits of -inf is as one without slots: what it holds does not move another's units."""
+    h, w, ids, logits, g = inputs("distill", dtype, 40, 120, D, 4, holes=False)
+    dead = torch.zeros(40, dtype=torch.bool, device=h.device)
+    dead[[3, 33]] = True
+    logits[dead] = -math.inf
+    want = compare(fsa, "distill", dtype, h, w, ids, logits, g)
+    h[3], h[33] = torch.finfo(h.dtype).max, math.nan
+    g[3], g[33] = 3e38, math.nan
+    loss, lse, rg = fsa.fsa_distill_fwd(h, w, ids, logits, emit_row_grad=True)
+    gh, gw = fsa.fsa_distill_bwd(g, h, w, ids, logits, lse, rg)
+    for a, b, name in zip((loss, lse, rg, gh, gw), want, ("loss", "lse", "row_grad", "grad_h", "grad_w")):
+        assert torch.equal(a, b), name
