@@ -737,7 +737,7 @@ __device__ __forceinline__ void advance(const uint16_t* ahead, const uint16_t* t
 // PFLOP/s, matrix units busy 56 % of 9.0 M cycles at the 1.84 GHz that the card holds then; a large bfloat16 product of the
 // library runs at 1.29.  8 rows, one read of the table: 102 us, 6.1 TB/s.
 // Why this way: rows stay in registers and the table streams, because a row's statistics then never leave its lane (an
-// accumulator column) until the end; a wave has 32 of them, two waves fit a SIMD (one held 64 % as much: 8.1 ms).  Few rows: the
+// accumulator column) until the end; a wave has 32 of them, two waves fit a SIMD (with one: 8.1 ms against 5.6, before the order of advance()).  Few rows: the
 // waves of a workgroup share the streamed blocks instead (WY).
 template <int DP, int WY, bool MEAN, bool STRAIGHT>
 __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_forward_kernel(ClassArgs a, int64_t padded) {
@@ -1021,8 +1021,8 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
 // Scores are made again from the table and the rows, 2 T V D operations, because keeping them would move 6 bytes a score: 12
 // times what the classes and their gradients move at 128 elements.  A class's row is written once, by the wave that holds it,
 // or in parts that a second launch joins where there are fewer classes than waves.
-// 4096 x 2.5 M x 128 bfloat16: 5.4 ms, 0.97 PFLOP/s; what a slot adds costs by the slot (4096 x 169,343, 32 slots a row: 0.55
-// ms, 0.39 without).
+// 4096 x 2.5 M x 128 bfloat16: 5.4 ms, 0.97 PFLOP/s; what slots add costs by the slot (4096 x 169,343, 32 slots a row: 0.55
+// ms, where the classes alone would take 0.37 at that rate).
 template <int DP, int WY>
 __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) void class_gradient_kernel(ClassArgs a, int64_t padded) {
     constexpr int NB = blocks_per_tile(WY, DP, kKind), MY = NB / WY, WX = kClassWaves / WY;
