@@ -91,14 +91,19 @@ inline ClassCut gradient_cut(const ClassShape& s) {
     return c;
 }
 
-// Slots of 32 rows are sorted by the classes that they name, for the gradient: `per` blocks of classes to a bucket, about
-// two buckets to a slot, so that a wave mostly learns from one word that no slot of these rows names one of its classes.
+// Slots of 32 rows are sorted by the classes that they name, for the gradient: `per` blocks of classes to a bucket, 16 buckets
+// to a slot while they last, so that a wave mostly learns from one word that no slot of these rows names one of its classes.
 struct ClassBuckets { int64_t per, count; };
 constexpr int kMostBuckets = 2 * kBlock * 64;
 constexpr ClassBuckets buckets_of(int64_t V, int K) {
-    const int64_t blocks = ceil_div(V, kBlock), per = ceil_div(blocks, 2 * kBlock * K);
+    const int64_t blocks = ceil_div(V, kBlock), most = 16 * kBlock * K, per = ceil_div(blocks, most < kMostBuckets ? most : kMostBuckets);
     return {per, ceil_div(blocks, per)};
 }
+
+// Whether the gradient scores the slots of a row in a launch of its own, a workgroup a row, or where it sorts them, a wave to two
+// rows.  One slot: sorting takes 4 us longer for it (1024 rows x 128: 7.5 to 11.2), as much as a launch.  1024 rows x 47 x 100 fp32,
+// 10 slots: 23.6 us together, 12.0 and 8.9 apart; 257 rows x 602, 50 slots: 250 us together.
+constexpr bool slots_apart(const ClassShape& s) { return s.K > 1; }
 
 // Whether the forward first lays the table out as planes of padded rows: one more pass over the table, against rows that
 // the kernel has to read off the 16-byte grid, to pad, or to split into planes, once for every workgroup beside it (measured
@@ -112,7 +117,7 @@ inline bool forward_packs(const ClassShape& s, bool straight) {
 
 // Byte offsets into the caller's workspace.
 struct ClassPlan {
-    size_t peaks, rows, table, top, sum, mean_parts, norm, loss, start, signs, buckets, slots, row_grad, grad_parts, bytes;
+    size_t peaks, rows, table, top, sum, mean_parts, norm, loss, start, signs, buckets, slots, row_slots, row_grad, grad_parts, bytes;
     bool packed;                                        // the forward reads the table from planes made for the call,
     bool straight;                                      // or as it is: 16-bit rows of a depth, on the 16-byte grid
 };
@@ -146,6 +151,7 @@ inline ClassPlan plan_of(const ClassShape& s, bool straight, bool forward, bool 
         p.signs = room(T / kBlock * 4);
         p.buckets = room(T / kBlock * buckets_of(s.V, s.K).count * 4);
         p.slots = room(T * s.K * 8);
+        if (slots_apart(s)) p.row_slots = room(T * s.K * 8);
         if (c.slices() > 1) p.grad_parts = room((size_t)c.slices() * ceil_div(s.V, kBlock) * kBlock * depth * 4);
     }
     p.bytes = at;

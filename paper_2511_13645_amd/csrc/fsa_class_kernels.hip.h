@@ -355,7 +355,7 @@ struct SlotWord {
     __device__ __forceinline__ int count() const { return w >> 11 & 4095; }
     __device__ __forceinline__ bool negative() const { return w >> 31; }
 };
-// A slot: its row of the 32 above 27 bits of class, and g * q with the units of the gradient.
+// A slot: its row of the 32 above 27 bits of class, and g (q - p) with the units of the gradient, never zero.
 struct Slot { uint32_t key; float pull; };
 
 constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / 64, kRowsEach = kBlock / kRowWaves;
@@ -375,7 +375,104 @@ __global__ __launch_bounds__(kClassThreads) void class_row_grad_kernel(ClassArgs
     write_row_grad(a, t, a.grad_loss[t], __any(id >= 0), lane);
 }
 
-// One workgroup per 32 rows, two to a wave.  Latency alone, 8 to 20 us: the chain from IDs over logits to the sorted slots.
+__device__ __forceinline__ float probability(const ClassArgs& a, int64_t t, float dot) {
+    const float p = exp2f((dot * a.scale - a.lse_in[t]) * kLog2e);
+    return p > 1.0f ? 1.0f : p;                         // (NaN stays)
+}
+// p of the classes that lanes [from, to) name for row t (an ID behind the last class: 0), by the fp32 dot product of the elements
+// themselves; `lanes` of the wave to a class, four classes to a group of them at a time.
+__device__ __forceinline__ float slot_probability(const ClassArgs& a, int64_t t, int id, int lane, int lanes, int from, int to) {
+    const Elem *h = static_cast<const Elem*>(a.h) + t * a.h_stride, *w = static_cast<const Elem*>(a.w);
+    const int groups = 64 / lanes, group = lane / lanes, l = lane % lanes;
+    const bool known = id >= 0 && id < a.s.V;
+    float z = 0.0f;
+    for (int j = from; j < to; j += 4 * groups) {
+        const Elem* row[4];
+        float dot[4] = {};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = j + i * groups + group, of = __shfl(known ? id : -1, k & 63);
+            row[i] = of >= 0 && k < to ? w + of * a.w_stride : nullptr;
+        }
+        for (int c = 4 * l; c < a.s.D; c += 4 * lanes) {
+            const f32x4 x = load4(h, a.s.D, c);
+            f32x4 y[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i] = row[i] ? load4(row[i], a.s.D, c) : f32x4{};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dot[i] += (x[0] * y[i][0] + x[1] * y[i][1]) + (x[2] * y[i][2] + x[3] * y[i][3]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            for (int d = 1; d < lanes; d *= 2) dot[i] += __shfl_xor(dot[i], d);
+            const int k = j + i * groups;
+            const float mine = __shfl(dot[i], (lane - k) * lanes & 63);
+            if (lane >= k && lane < k + groups) z = mine;
+        }
+    }
+    return known ? probability(a, t, z) : 0.0f;
+}
+// The same of rows [t, t + N) of one slot each, the whole wave to a class, all rows at a time.
+template <int N> __device__ __forceinline__ void target_probability(const ClassArgs& a, int64_t t, int lane, float (&p)[N]) {
+    const Elem *h[N], *w[N];
+    float dot[N] = {};
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const int id = t + k < a.s.T ? a.ids[t + k] : -1;
+        h[k] = static_cast<const Elem*>(a.h) + (t + k) * a.h_stride;
+        w[k] = id >= 0 && id < a.s.V ? static_cast<const Elem*>(a.w) + id * a.w_stride : nullptr;
+    }
+    for (int c = 4 * lane; c < a.s.D; c += 256) {
+        f32x4 x[N] = {}, y[N] = {};
+#pragma unroll
+        for (int k = 0; k < N; ++k) if (w[k]) { x[k] = load4(h[k], a.s.D, c); y[k] = load4(w[k], a.s.D, c); }
+#pragma unroll
+        for (int k = 0; k < N; ++k) dot[k] += (x[k][0] * y[k][0] + x[k][1] * y[k][1]) + (x[k][2] * y[k][2] + x[k][3] * y[k][3]);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2)
+#pragma unroll
+        for (int k = 0; k < N; ++k) dot[k] += __shfl_xor(dot[k], d);
+#pragma unroll
+    for (int k = 0; k < N; ++k) p[k] = w[k] ? probability(a, t + k, dot[k]) : 0.0f;
+}
+
+// The slots of a row that the gradient sorts, in lanes 0..K-1, as their class (-1: none) and g (q - p): places of the classes that
+// a row names are left out of the products, which round p, because of a row that has learned its class only p - q is left.  A
+// class that several slots name is the first one's, with the weights in slot order, so that each place of [row][class] is written once.
+__device__ __forceinline__ Slot row_slot(const ClassArgs& a, int id, float weight, float p, float g, int lane) {
+    bool first = true;
+    float q = weight;
+    for (int j = 0; j < a.s.K && a.s.K > 1; ++j) {
+        const int other = __builtin_amdgcn_readlane(id, j);
+        const float more = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), j));
+        if (other == id && j < lane) first = false;
+        if (other == id && j > lane) q += more;
+    }
+    float pull = g * (q - p);
+    if (pull == 0.0f) pull = 0x1p-126f;                 // a place that is named is told from others by not being zero
+    return Slot{first && id >= 0 && id < a.s.V ? (uint32_t)id : ~0u, pull};
+}
+
+// Rows of more than one slot, ahead of the sorting: one workgroup per row, a quarter of its slots to a wave.  Bound by the reads of
+// the classes' rows: 4096 rows of 32 slots, 128 bfloat16 (33 MB of rows) 28 us.
+__global__ __launch_bounds__(kClassThreads) void class_slots_kernel(ClassArgs a, int lanes) {
+    __shared__ float room[kClassWaves];
+    const Units u = row_units(a, room);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t t = blockIdx.x;
+    const int each = (a.s.K + kClassWaves - 1) / kClassWaves, from = wave * each, to = from + each < a.s.K ? from + each : a.s.K;
+    int id;
+    float log_weight;
+    const float weight = slot_weight(a, t, lane, id, log_weight);
+    const bool lives = __any(id >= 0);
+    const float p = lives ? slot_probability(a, t, id, lane, lanes, from, to) : 0.0f;
+    const Slot s = row_slot(a, id, weight, p, lives ? a.grad_loss[t] * u.g : 0.0f, lane);
+    if (lane >= from && lane < to) a.at<Slot>(a.plan.row_slots)[t * a.s.K + lane] = s;
+}
+
+// One workgroup per 32 rows, two to a wave.  Latency alone, 11 to 24 us: the chain from IDs over logits or the classes' rows to
+// the sorted slots.
 template <int DP>
 __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, int64_t padded) {
     __shared__ float room[kRowWaves];
@@ -388,7 +485,8 @@ __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, in
     uint16_t* planes = a.at<uint16_t>(a.plan.rows);
     __syncthreads();
     int ids[kRowsEach];
-    float pulls[kRowsEach];
+    float pulls[kRowsEach], target[kRowsEach] = {};
+    if (!a.plan.row_slots) target_probability(a, (int64_t)blockIdx.x * kBlock + wave * kRowsEach, lane, target);
 #pragma unroll
     for (int k = 0; k < kRowsEach; ++k) {
         const int q = wave * kRowsEach + k;
@@ -411,8 +509,11 @@ __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, in
             a.at<float>(a.plan.start)[t] = lives ? log2f(fabsf(g)) - a.lse_in[t] * kLog2e : -__builtin_inff();
             if (g < 0.0f) atomicOr(&signs, 1u << q);
         }
-        ids[k] = id >= 0 && id < a.s.V && weight != 0.0f ? id : -1;
-        pulls[k] = g * weight;
+        Slot own{~0u, 0.0f};
+        if (!a.plan.row_slots) own = row_slot(a, id, weight, target[k], g, lane);
+        else if (t < a.s.T && lane < a.s.K) own = a.at<const Slot>(a.plan.row_slots)[t * a.s.K + lane];
+        ids[k] = (int)own.key;
+        pulls[k] = own.pull;
         if (ids[k] >= 0) atomicAdd(&counts[(uint32_t)ids[k] / kBlock / (uint32_t)bk.per], 1u);
     }
     __syncthreads();
@@ -488,7 +589,7 @@ struct SlotFeed {
 #pragma unroll
         for (int m = 0; m < M; ++m) { now[m] = next[m]; slot[m] = next_slot[m]; }
     }
-    // Adds what the slots of block m pull at to cells[row][class]; whether there was one (wave-uniform).
+    // What the slots of block m take, into cells[row][class]; whether there was one (wave-uniform).
     __device__ __forceinline__ bool gather(int m, int64_t block, int lane, float* cells) const {
         if (now[m].count() == 0) return false;
         bool hit = false;
@@ -496,7 +597,7 @@ struct SlotFeed {
         for (int e = lane;;) {
             const uint32_t c = (s.key & 0x7ffffffu) - first_class;
             if (e < now[m].count() && c < (uint32_t)kBlock) {
-                atomicAdd(&cells[(s.key >> 27) * kBlock + c], s.pull);
+                cells[(s.key >> 27) * kBlock + c] = s.pull;
                 hit = true;
             }
             e += 64;
@@ -1029,7 +1130,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
     using T = Tile<DP, NB * kBlock>;
     __shared__ __align__(16) uint16_t lds[2][NS * T::kPlane];
     __shared__ __align__(16) float starts[2][NB * kBlock];
-    __shared__ float cells[kClassWaves][kBlock * kBlock];
+    __shared__ float cells[kClassWaves][MY][kBlock * kBlock];
     __shared__ float room[kClassWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = wave % WX, y = wave / WX;
     const ClassCut::Place place = a.cut.place(blockIdx.x);
@@ -1045,9 +1146,8 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
     f32x16 acc[DP / 32];
 #pragma unroll
     for (auto& f : acc) f = f32x16{};
-    float* cell = cells[wave];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) cell[row_of(i, lane) * kBlock + (lane & 31)] = 0.0f;
+    float* cell = cells[wave][0];                       // what slots take of a tile's blocks, [row][class]
+    for (int i = lane; i < MY * kBlock * kBlock; i += 64) cell[i] = 0.0f;
 
     const float* start = a.at<const float>(a.plan.start);
     typename T::FromPlanes next;
@@ -1086,13 +1186,38 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
                 for (int n = 0; n < NS; ++n) q[s][n][j] ^= flip;
             }
     };
-    // What slots pull at, subtracted by a product of its own, for 16-bit types in two roundings: it is most of the gradient
-    // of a class that rows name.
-    auto pull = [&](const uint16_t* tile, int b) {
+    // Places that slots name are left out of the block's own product, whose rounding of p would be far above p - q of a row
+    // that has learned its class: p - q of them, made in fp32, is added by a product of its own, for 16-bit types in two
+    // roundings (of a row that has not learned its class it is most of what the class gets).
+    bool hit[MY];                                       // whether they are in a block of the tile, wave-uniform
+    uint32_t named[MY];                                 // registers of a lane whose places are named
+    auto gather = [&](int64_t block) {
+        feed.turn();
+#pragma unroll
+        for (int m = 0; m < MY; ++m) {
+            hit[m] = feed.gather(m, block + m, lane, cell + m * kBlock * kBlock);
+            if (!hit[m]) continue;
+            __builtin_amdgcn_wave_barrier();
+            named[m] = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) named[m] |= (cell[(m * kBlock + row_of(i, lane)) * kBlock + (lane & 31)] != 0.0f ? 1u : 0u) << i;
+        }
+    };
+    auto leave_out = [&](uint32_t named, u32x4 (&q)[2][NS]) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t two = named >> (8 * s + 2 * j), keep = ((two & 1) - 1 & 0xffffu) | ((two >> 1 & 1) - 1 & 0xffff0000u);
+#pragma unroll
+                for (int n = 0; n < NS; ++n) q[s][n][j] &= keep;
+            }
+    };
+    auto pull = [&](const uint16_t* tile, int m) {
         float c[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            float& at = cell[row_of(i, lane) * kBlock + (lane & 31)];
+            float& at = cell[(m * kBlock + row_of(i, lane)) * kBlock + (lane & 31)];
             c[i] = -at;
             at = 0.0f;
         }
@@ -1100,7 +1225,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
         for (int n = 0; n < 2 / NS; ++n) {
             u32x4 q[2][NS];
             operand_of(c, q);
-            product(tile, b, q);
+            product(tile, y * MY + m, q);
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -1118,12 +1243,12 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
         feed.ask_words((int64_t)first * NB + y * MY);
         feed.ask_slots((int64_t)first * NB + y * MY, lane);
         feed.ask_words((int64_t)(first + 1) * NB + y * MY);
+        if (live) gather((int64_t)first * NB + y * MY);
     }
     for (int it = first; it < last; ++it) {
         const int at = slot;
         const uint16_t* tile = lds[at];
         slot ^= 1;
-        feed.turn();
         store(at);                                      // the other tile may still be read
         __syncthreads();
         fetch(it + 1);
@@ -1138,13 +1263,12 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
             return __builtin_amdgcn_exp2f(fmaf(score[m][i], to_log2, s[i % 4]));
         }, [&](int m, u32x4 (&q)[2][NS]) {
             if (feed.now[m].negative()) sign(block0 + m, q);
+            if (hit[m]) leave_out(named[m], q);
         });
 #pragma unroll
         for (int m = 0; m < MY; ++m)
-            if (feed.gather(m, block0 + m, lane, cell)) {
-                __builtin_amdgcn_wave_barrier();
-                pull(tile, y * MY + m);
-            }
+            if (hit[m]) pull(tile, m);
+        if (it + 1 < last) gather(block0 + NB);         // what was asked for has come by now
     }
     if (!live) return;
     const float back = a.scale / u.h / u.g;
@@ -1380,7 +1504,7 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         float& c = cells[(y + j) * kBlock + (lane & 31)];
-                        p[j] -= c;
+                        if (c != 0.0f) p[j] = -c;       // p - q of a place that a slot names, as in the narrow kernel
                         c = 0.0f;
                     }
                 }
@@ -1470,6 +1594,13 @@ template <class F> hipError_t with_depth(int depth, F f) {
     return hipGetLastError();
 }
 
+// Lanes that share a row, four elements each.
+inline int row_lanes(int64_t D) {
+    int lanes = 1;
+    while (lanes < 64 && 4 * lanes < D) lanes *= 2;
+    return lanes;
+}
+
 template <int DP, bool MEAN> void launch_forward(const ClassArgs& a, int64_t padded, hipStream_t stream) {
     const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
     const bool straight = a.plan.packed || a.plan.straight;
@@ -1500,8 +1631,7 @@ hipError_t forward(ClassArgs a, hipStream_t stream) {
     const bool wide = !narrow_depth(depth), rows = a.row_grad != nullptr;
     a.cut = forward_cut(a.s);
     const int slices = (int)a.cut.slices();
-    int lanes = 1;
-    while (lanes < 64 && 4 * lanes < a.s.D) lanes *= 2;
+    const int lanes = row_lanes(a.s.D);
     auto run = [&](bool mean) {
         return with_depth(depth, [&](auto dp) {
             mean ? launch_forward<dp(), true>(a, padded, stream) : launch_forward<dp(), false>(a, padded, stream);
@@ -1537,6 +1667,7 @@ hipError_t gradient(ClassArgs a, hipStream_t stream) {
         const int rows = kKind == 0 ? kPeaksRows : 0;
         class_peaks_kernel<<<rows + kPeaksGrad, kClassThreads, 0, stream>>>(a, 0, rows, kPeaksGrad);
     }
+    if (a.plan.row_slots && a.s.T) class_slots_kernel<<<(unsigned)a.s.T, kClassThreads, 0, stream>>>(a, row_lanes(a.s.D));
     if (hipError_t e = with_depth(depth, [&](auto dp) {
             if (padded) class_rows_kernel<dp()><<<padded / kBlock, kRowThreads, 0, stream>>>(a, padded);
         })) return e;
