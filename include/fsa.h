@@ -388,7 +388,7 @@ int fsa_wmean_bwd_ws(const float* grad_out, const float* grad_h1,
  *                      FSA_ERR_ALIGN); nothing in it is kept from one call to the next
  * Sums, maxima and means are fp32.  Scores of 16-bit tables are fp32 sums of exact products; those of fp32 tables take
  * 22 bits of every element (see the kernels); probabilities enter the gradients rounded to the table's 16-bit type, or to
- * 22 bits, in grad_w less q where slots name their class (p - q is formed in fp32).  Every result is a function of the
+ * 22 bits, but for classes that a row's slots name: p - q of those is formed in fp32.  Every result is a function of the
  * arguments alone: no atomics whose order could change it.
  */
 enum { FSA_CLASS_TMAX = 1 << 23, FSA_CLASS_VMAX = 1 << 27, FSA_CLASS_DMAX = 1024 };

@@ -100,6 +100,10 @@ constexpr ClassBuckets buckets_of(int64_t V, int K) {
     return {per, ceil_div(blocks, per)};
 }
 
+constexpr int kWaveSlots = 2;                           // slots a row that a wave of the forward sorts itself: two to a lane pair
+// Whether 64 classes have more than 8 slots of 32 rows, on an average: for the forward with row gradients, which then reads the
+// (small) table as it is.
+constexpr bool crowded_tiles(const ClassShape& s) { return s.K > kWaveSlots && (int64_t)s.K * kBlock * 64 > 8 * s.V; }
 // Whether the gradient scores the slots of a row in a launch of its own, a workgroup a row, or where it sorts them, a wave to two
 // rows.  One slot: sorting takes 4 us longer for it (1024 rows x 128: 7.5 to 11.2), as much as a launch.  1024 rows x 47 x 100 fp32,
 // 10 slots: 23.6 us together, 12.0 and 8.9 apart; 257 rows x 602, 50 slots: 250 us together.
@@ -117,7 +121,7 @@ inline bool forward_packs(const ClassShape& s, bool straight) {
 
 // Byte offsets into the caller's workspace.
 struct ClassPlan {
-    size_t peaks, rows, table, top, sum, mean_parts, norm, loss, start, signs, buckets, slots, row_slots, row_grad, grad_parts, bytes;
+    size_t peaks, rows, table, top, sum, mean_parts, norm, pulls, named, named_starts, loss, start, signs, buckets, slots, row_slots, row_grad, grad_parts, bytes;
     bool packed;                                        // the forward reads the table from planes made for the call,
     bool straight;                                      // or as it is: 16-bit rows of a depth, on the 16-byte grid
 };
@@ -133,12 +137,17 @@ inline ClassPlan plan_of(const ClassShape& s, bool straight, bool forward, bool 
         const bool narrow = narrow_depth((int)depth);
         const size_t slices = forward_cut(s).slices(), stats = narrow ? slices : slices * kClassWaves;
         p.straight = straight;
-        p.packed = forward_packs(s, straight);
+        p.packed = forward_packs(s, straight) && !(want_rows && narrow && crowded_tiles(s));
         if (p.packed) p.table = room(padded_rows(s.V) * depth * 2 * class_planes(s.kind));
         p.top = room(stats * T * 4);
         p.sum = room(stats * T * 4);
         if (want_rows) p.mean_parts = room(slices * T * depth * 4);
         if (want_rows && !narrow) p.norm = room(T * 4);
+        if (want_rows && !narrow) p.pulls = room(T * s.K * 4);
+        if (want_rows && s.K > kWaveSlots) {
+            p.named = room(T * s.K * 4);
+            p.named_starts = room(T / kBlock * (forward_cut(s).parts + 1) * 4);
+        }
     }
     if (forward && want_rows) {                         // a backward that computes the rows' gradients again keeps them here
         p.row_grad = room((size_t)s.T * s.D * 4);

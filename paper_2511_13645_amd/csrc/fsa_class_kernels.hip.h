@@ -375,9 +375,23 @@ __global__ __launch_bounds__(kClassThreads) void class_row_grad_kernel(ClassArgs
     write_row_grad(a, t, a.grad_loss[t], __any(id >= 0), lane);
 }
 
-__device__ __forceinline__ float probability(const ClassArgs& a, int64_t t, float dot) {
-    const float p = exp2f((dot * a.scale - a.lse_in[t]) * kLog2e);
+__device__ __forceinline__ float probability(float score, float lse) {
+    const float p = exp2f((score - lse) * kLog2e);
     return p > 1.0f ? 1.0f : p;                         // (NaN stays)
+}
+// A class that several slots of a row name is the first one's, with the weights in slot order; false for the others, and for
+// slots that name no class of the table.  IDs and weights in lanes 0..K-1.
+__device__ __forceinline__ bool merge_slots(const ClassArgs& a, int id, float& q) {
+    const int lane = threadIdx.x & 63;
+    const float own = q;
+    bool first = id >= 0 && id < a.s.V;
+    for (int j = 0; j < a.s.K && a.s.K > 1; ++j) {
+        const int other = __builtin_amdgcn_readlane(id, j);
+        const float more = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, own), j));
+        if (other == id && j < lane) first = false;
+        if (other == id && j > lane) q += more;
+    }
+    return first;
 }
 // p of the classes that lanes [from, to) name for row t (an ID behind the last class: 0), by the fp32 dot product of the elements
 // themselves; `lanes` of the wave to a class, four classes to a group of them at a time.
@@ -410,7 +424,7 @@ __device__ __forceinline__ float slot_probability(const ClassArgs& a, int64_t t,
             if (lane >= k && lane < k + groups) z = mine;
         }
     }
-    return known ? probability(a, t, z) : 0.0f;
+    return known ? probability(z * a.scale, a.lse_in[t]) : 0.0f;
 }
 // The same of rows [t, t + N) of one slot each, the whole wave to a class, all rows at a time.
 template <int N> __device__ __forceinline__ void target_probability(const ClassArgs& a, int64_t t, int lane, float (&p)[N]) {
@@ -434,24 +448,16 @@ template <int N> __device__ __forceinline__ void target_probability(const ClassA
 #pragma unroll
         for (int k = 0; k < N; ++k) dot[k] += __shfl_xor(dot[k], d);
 #pragma unroll
-    for (int k = 0; k < N; ++k) p[k] = w[k] ? probability(a, t + k, dot[k]) : 0.0f;
+    for (int k = 0; k < N; ++k) p[k] = w[k] ? probability(dot[k] * a.scale, a.lse_in[t + k]) : 0.0f;
 }
 
 // The slots of a row that the gradient sorts, in lanes 0..K-1, as their class (-1: none) and g (q - p): places of the classes that
-// a row names are left out of the products, which round p, because of a row that has learned its class only p - q is left.  A
-// class that several slots name is the first one's, with the weights in slot order, so that each place of [row][class] is written once.
-__device__ __forceinline__ Slot row_slot(const ClassArgs& a, int id, float weight, float p, float g, int lane) {
-    bool first = true;
-    float q = weight;
-    for (int j = 0; j < a.s.K && a.s.K > 1; ++j) {
-        const int other = __builtin_amdgcn_readlane(id, j);
-        const float more = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), j));
-        if (other == id && j < lane) first = false;
-        if (other == id && j > lane) q += more;
-    }
-    float pull = g * (q - p);
-    if (pull == 0.0f) pull = 0x1p-126f;                 // a place that is named is told from others by not being zero
-    return Slot{first && id >= 0 && id < a.s.V ? (uint32_t)id : ~0u, pull};
+// a row names are left out of the products, which round p, because of a row that has learned its class only p - q is left.
+// Each place of [row][class] is one slot's.
+__device__ __forceinline__ Slot row_slot(const ClassArgs& a, int id, float q, float p, float g) {
+    const bool some = merge_slots(a, id, q);
+    const float pull = g * (q - p);
+    return Slot{some ? (uint32_t)id : ~0u, pull != 0.0f ? pull : 0x1p-126f};    // (a place that is named is told by not being zero)
 }
 
 // Rows of more than one slot, ahead of the sorting: one workgroup per row, a quarter of its slots to a wave.  Bound by the reads of
@@ -467,7 +473,7 @@ __global__ __launch_bounds__(kClassThreads) void class_slots_kernel(ClassArgs a,
     const float weight = slot_weight(a, t, lane, id, log_weight);
     const bool lives = __any(id >= 0);
     const float p = lives ? slot_probability(a, t, id, lane, lanes, from, to) : 0.0f;
-    const Slot s = row_slot(a, id, weight, p, lives ? a.grad_loss[t] * u.g : 0.0f, lane);
+    const Slot s = row_slot(a, id, weight, p, lives ? a.grad_loss[t] * u.g : 0.0f);
     if (lane >= from && lane < to) a.at<Slot>(a.plan.row_slots)[t * a.s.K + lane] = s;
 }
 
@@ -510,7 +516,7 @@ __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, in
             if (g < 0.0f) atomicOr(&signs, 1u << q);
         }
         Slot own{~0u, 0.0f};
-        if (!a.plan.row_slots) own = row_slot(a, id, weight, target[k], g, lane);
+        if (!a.plan.row_slots) own = row_slot(a, id, weight, target[k], g);
         else if (t < a.s.T && lane < a.s.K) own = a.at<const Slot>(a.plan.row_slots)[t * a.s.K + lane];
         ids[k] = (int)own.key;
         pulls[k] = own.pull;
@@ -730,6 +736,18 @@ __device__ __forceinline__ void operand_of(const float (&p)[16], u32x4 (&out)[2]
     }
 }
 
+// P's operand without the places that slots name: bit i of `named` is register i of this lane's result.
+__device__ __forceinline__ void leave_out(uint32_t named, u32x4 (&q)[2][NS]) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t two = named >> (8 * s + 2 * j), keep = ((two & 1) - 1 & 0xffffu) | ((two >> 1 & 1) - 1 & 0xffff0000u);
+#pragma unroll
+            for (int n = 0; n < NS; ++n) q[s][n][j] &= keep;
+        }
+}
+
 // Row that register i of a result stands for, in its block.
 __device__ __forceinline__ int row_of(int i, int lane) { return 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3); }
 
@@ -829,10 +847,137 @@ __device__ __forceinline__ void advance(const uint16_t* ahead, const uint16_t* t
 }
 
 // ---------------------------------------------------------------------------------------------------------------
+// classes that the held rows' slots name, for the forward
+// ---------------------------------------------------------------------------------------------------------------
+// Their places are left out of the sum of p w, which rounds p (theirs are added with p - q when the parts are joined).  A wave
+// asks for the next tile that has one with one comparison of scalars: looking at every tile's slots, or masking P between the
+// products, took the loop's registers and up to half of its speed.
+// Up to two slots a row lie in a register of the wave; more of them in a list for every 32 rows in the order of the classes, class *
+// 32 + row, that a launch ahead sorts.  Latency alone, 10 us (10 slots a row) to 21 (64).
+__global__ __launch_bounds__(kRowThreads) void class_named_kernel(ClassArgs a, int classes) {
+    __shared__ uint32_t keys[kBlock * 64];
+    __shared__ int count;
+    const int64_t t0 = (int64_t)blockIdx.x * kBlock;
+    int size = 2 * kRowThreads;                         // a power of two
+    while (size / 2 >= kBlock * a.s.K) size /= 2;
+    for (int e = threadIdx.x; e < size; e += kRowThreads) keys[e] = ~0u;
+    if (threadIdx.x == 0) count = 0;
+    __syncthreads();
+    for (int e = threadIdx.x; e < kBlock * a.s.K; e += kRowThreads) {
+        const int row = e / a.s.K;
+        const int id = t0 + row < a.s.T ? a.ids[t0 * a.s.K + e] : -1;
+        if (id >= 0 && id < a.s.V) { keys[e] = (uint32_t)id << 5 | (uint32_t)row; atomicAdd(&count, 1); }
+    }
+    for (int run = 2; run <= size; run *= 2)            // bitonic: runs of this length in turns up and down
+        for (int d = run / 2; d > 0; d /= 2) {
+            __syncthreads();
+            const int i = threadIdx.x / d * 2 * d + threadIdx.x % d;
+            if (i < size) {
+                const uint32_t x = keys[i], y = keys[i + d];
+                if ((x > y) == ((i & run) == 0)) { keys[i] = y; keys[i + d] = x; }
+            }
+        }
+    __syncthreads();
+    const int n = count;
+    uint32_t* list = a.at<uint32_t>(a.plan.named) + (int64_t)blockIdx.x * kBlock * a.s.K;
+    for (int e = threadIdx.x; e < n; e += kRowThreads) list[e] = keys[e];
+    uint32_t* starts = a.at<uint32_t>(a.plan.named_starts) + (int64_t)blockIdx.x * (a.cut.parts + 1);
+    for (int p = threadIdx.x; p <= a.cut.parts; p += kRowThreads) {
+        const int64_t from = p < a.cut.parts ? (int64_t)a.cut.place((unsigned)p).first * classes : a.s.V;
+        int lo = 0, hi = n;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if ((int64_t)(keys[mid] >> 5) < from) lo = mid + 1;
+            else hi = mid;
+        }
+        starts[p] = lo;
+    }
+}
+// What 32 rows name within a workgroup's part of the classes, tiles of CLASSES at a time.
+template <int CLASSES> struct Named {
+    static constexpr uint32_t kNone = 0x7fffffff;
+    const uint32_t* list;                               // null: a lane has a class of its own (negative: none)
+    uint32_t keys;                                      // that class, or 64 keys of the list
+    int at, end, most;                                  // wave-uniform, as
+    uint32_t next;                                      // the next tile that has one
+    int last;
+    __device__ __forceinline__ void load(int lane) { keys = (at & ~63) + lane < most ? list[(at & ~63) + lane] : 0; }
+    // From tile `from` on.
+    __device__ __forceinline__ void look(int from) {
+        if (list) next = at < end ? ((uint32_t)__builtin_amdgcn_readlane((int)keys, at & 63) >> 5) / CLASSES : kNone;
+        else {
+            const int tile = (int)keys >= 0 ? (int)(keys / CLASSES) : -1;
+            uint32_t m = tile >= from && tile < last ? tile : kNone;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) { const uint32_t o = __shfl_xor(m, d); m = o < m ? o : m; }
+            next = __builtin_amdgcn_readfirstlane(m);
+        }
+    }
+    __device__ __forceinline__ Named(const ClassArgs& a, int64_t block, int part, int first, int last_, int lane) : last(last_) {
+        most = kBlock * a.s.K;
+        if (a.plan.named) {
+            list = a.at<const uint32_t>(a.plan.named) + block * most;
+            const uint32_t* starts = a.at<const uint32_t>(a.plan.named_starts) + block * (a.cut.parts + 1) + part;
+            at = __builtin_amdgcn_readfirstlane(starts[0]);
+            end = __builtin_amdgcn_readfirstlane(starts[1]);
+            load(lane);
+        } else {
+            list = nullptr;
+            const int64_t t = block * kBlock + (lane & 31);
+            const int id = t < a.s.T && lane < most ? a.ids[t * a.s.K + (lane >> 5)] : -1;
+            keys = id < a.s.V ? id : -1;
+        }
+        look(first);
+    }
+    // f(whether a lane has one, its row and class of the tile) for up to 64 of tile `it`, the next, at a time.
+    template <class F> __device__ __forceinline__ void take_many(int it, int lane, F f) {
+        do {
+            const int now = __builtin_amdgcn_readfirstlane(at), i = (now & ~63) + lane;
+            const bool has = (keys >> 5) / CLASSES == (uint32_t)it && i >= now && i < end;
+            f(has, (int)(keys & 31), (int)((keys >> 5) % CLASSES));
+            at = now + __popcll(__ballot(has));
+            if ((at & 63) == 0 && at < end) load(lane);
+            look(it);
+        } while (next == (uint32_t)it);
+    }
+    // f(rows that name it, a bit each, class of the tile) for every class of tile `it`, the next; all of it in scalars, as the
+    // waves have no registers left.
+    template <class F> __device__ __forceinline__ void take(int it, int lane, F f) {
+        if (list) {
+            int now = __builtin_amdgcn_readfirstlane(at);
+            const int stop = __builtin_amdgcn_readfirstlane(end);
+            uint32_t key = __builtin_amdgcn_readlane((int)keys, now & 63), tile;
+            do {
+                const uint32_t cls = key >> 5;
+                uint32_t rows = 0;
+                do {
+                    rows |= 1u << (key & 31);
+                    if ((++now & 63) == 0 && now < stop) { at = now; load(lane); }
+                    key = __builtin_amdgcn_readlane((int)keys, now & 63);
+                } while (now < stop && key >> 5 == cls);
+                f(rows, (int)(cls % CLASSES));
+                tile = now < stop ? (key >> 5) / CLASSES : kNone;
+            } while (tile == (uint32_t)it);
+            at = now;
+            next = tile;
+        } else {
+            for (uint64_t some = __ballot((int)keys >= 0 && keys / CLASSES == (uint32_t)it); some;) {
+                const uint32_t cls = __builtin_amdgcn_readlane((int)keys, __builtin_ctzll(some));
+                const uint64_t same = __ballot(keys == cls);
+                f((uint32_t)(same | same >> 32), (int)(cls % CLASSES));
+                some &= ~same;
+            }
+            look(it + 1);
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------------------------------------------
 // forward: a wave holds 32 rows of h, the table streams by
 // ---------------------------------------------------------------------------------------------------------------
 // Mathematics: p = 2^(score * log2e - ref), ref following a row's maximum; the sum of p and, for the gradient of the row,
-// the sum of p times the table's rows (whose quotient is their mean under the softmax), all in one pass.
+// the sum of p times the table's rows but those that the row's slots name (theirs are added with p - q, formed in fp32, when
+// the parts are joined: of a row that has learned its class that difference is far below the rounding of p), all in one pass.
 // What bounds it: two products of T V D multiply-adds on the matrix units beside an exponential a score, which takes 16
 // cycles for 64 of them, as long as half a product of 128 elements.  4096 rows x 2.5 M classes x 128 bfloat16: 5.04 ms, 1.04
 // PFLOP/s, matrix units busy 56 % of 9.0 M cycles at the 1.84 GHz that the card holds then; a large bfloat16 product of the
@@ -840,7 +985,11 @@ __device__ __forceinline__ void advance(const uint16_t* ahead, const uint16_t* t
 // Why this way: rows stay in registers and the table streams, because a row's statistics then never leave its lane (an
 // accumulator column) until the end; a wave has 32 of them, two waves fit a SIMD (with one: 8.1 ms against 5.6, before the order of advance()).  Few rows: the
 // waves of a workgroup share the streamed blocks instead (WY).
-template <int DP, int WY, bool MEAN, bool STRAIGHT>
+//
+// Named classes: few of them are taken out of a tile's scores one after the other, 0.3 to 0.6 us each; CROWDED, the tile's operands
+// are masked for all of them, which costs every tile registers (1024 x 47 x 100 fp32, 10 slots: 47.9 us and 19.4; 4096 x 2.5 M x
+// 128 bfloat16: 5.3 ms and 6.4).
+template <int DP, int WY, bool MEAN, bool STRAIGHT, bool CROWDED = false>
 __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_forward_kernel(ClassArgs a, int64_t padded) {
     constexpr int NB = blocks_per_tile(WY, DP, kKind), MY = NB / WY, WX = kClassWaves / WY;   // blocks of a tile, a wave's own of them
     using T = Tile<DP, NB * kBlock>;
@@ -848,13 +997,14 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
     constexpr int TILES = AHEAD ? 3 : 2;
     __shared__ __align__(16) uint16_t lds[TILES][NS * T::kPlane];
     __shared__ float room[kClassWaves];
+    __shared__ uint32_t places[CROWDED ? kClassWaves : 1][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = wave % WX, y = wave / WX;
     const ClassCut::Place place = a.cut.place(blockIdx.x);
     const int part = place.part, group = place.group, first = place.first, last = place.last;
     const float table = table_unit(a, room);
+    if constexpr (CROWDED) places[wave][lane] = 0;
     const int64_t row0 = ((int64_t)group * WX + x) * kBlock, row = row0 + (lane & 31);   // of h, held by this lane
     const bool live = row0 < padded;                      // wave-uniform
-
     u32x4 held[DP / 16][NS];
     const float to_log2 = a.scale * kLog2e / hold_rows<DP / 16>(a, row, 0, lane, held, [](float peak) { return wave_max(peak); }) / table;
 
@@ -912,6 +1062,11 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
     // next of three LDS tiles by then, those of the tile after it are on their way in registers.
     int slot = 0;
     fetch(first);
+    using Places = Named<NB * kBlock>;
+    typename std::conditional<MEAN, Places, int>::type named = [&] {
+        if constexpr (MEAN) return Places(a, live ? row0 / kBlock : 0, part, first, last, lane);
+        else return 0;
+    }();
     if constexpr (AHEAD) {
         store(lds[0]);
         fetch(first + 1);
@@ -944,6 +1099,31 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
 #pragma unroll
                 for (auto& f : acc) f *= by;
         }
+        uint32_t out = 0;                               // bit 16 m + i: register i of block m is named
+        if constexpr (CROWDED) {
+            if (named.next == (uint32_t)it) {
+                named.take_many(it, lane, [&](bool has, int r, int c) {
+                    const int b = c / kBlock - y * MY;
+                    if (has && b >= 0 && b < MY)
+                        atomicOr(&places[wave][r + 32 * (c >> 2 & 1)], 1u << (16 * b + 4 * (c % kBlock >> 3) + (c & 3)));
+                });
+                __builtin_amdgcn_wave_barrier();
+                out = places[wave][lane];
+                places[wave][lane] = 0;
+                __builtin_amdgcn_wave_barrier();
+            }
+        } else if constexpr (MEAN)
+            if (named.next == (uint32_t)it)             // p of these to the sum, not to the product
+                named.take(it, lane, [&](uint32_t rows, int c) {
+                    const int b = c / kBlock - (WY == 1 ? 0 : __builtin_amdgcn_readfirstlane(y)) * MY, i = 4 * (c % kBlock >> 3) + (c & 3);
+                    const bool mine = lane >> 5 == (c >> 2 & 1) && rows >> (lane & 31) & 1;
+                    each<MY>([&](auto m) {
+                        if (b != m()) return;
+                        const float z = score[m()][i], p = __builtin_amdgcn_exp2f(fmaf(z, to_log2, -ref));
+                        if (mine) sum += p;
+                        score[m()][i] = mine ? -__builtin_inff() : z;
+                    });
+                });
         if constexpr (AHEAD) {
             f32x16 now[MY];
 #pragma unroll
@@ -953,7 +1133,9 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
                 const float p = __builtin_amdgcn_exp2f(fmaf(now[m][i], to_log2, -ref));
                 some[i & 1] += p;
                 return p;
-            }, [](int, u32x4 (&)[2][NS]) {});
+            }, [&](int m, u32x4 (&q)[2][NS]) {
+                if constexpr (CROWDED) leave_out(out >> 16 * m, q);
+            });
             sum += some[0] + some[1];
             find_top(it + 1);
             continue;
@@ -970,6 +1152,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
             if constexpr (MEAN) {
                 u32x4 b[2][NS];
                 operand_of(p, b);
+                if constexpr (CROWDED) leave_out(out >> 16 * m, b);
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -1001,14 +1184,14 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
 }
 
 // One workgroup per row.  LOSS: the parts joined, the row's slots scored again (fp32 sums of the elements themselves), its
-// loss.  ROWS: the gradient of its loss, scale * (mean of the table's rows - sum of its slots' q w), from parts that carry
-// their own reference (LOSS as well) or that are normalised already.
+// loss.  ROWS: the gradient of its loss, scale * (sum of p w over classes that no slot names + sum of (p - q) w over those), from
+// parts that carry their own reference (LOSS as well) or that are normalised already.
 // The workgroup is cut into groups of `lanes` lanes that cover four elements each; slots and parts go around them.  Bound by
 // the latency of its reads: 4096 rows x 128 with 16 parts 20 us, 8 rows 6.
 constexpr int kMostSlices = 4096;
 template <bool LOSS, bool ROWS>
 __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a, int64_t padded, int depth, int slices, int lanes) {
-    __shared__ float room[kClassWaves], slot_q[64], slot_log[64], slot_z[64];
+    __shared__ float room[kClassWaves], slot_z[64], slot_pull[64];
     __shared__ int slot_id[64], alive;
     __shared__ float weight[LOSS && ROWS ? kMostSlices : 1];
     __shared__ __align__(16) f32x4 gathered[ROWS ? kClassThreads : 1];
@@ -1021,11 +1204,13 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
 #pragma unroll 4
         for (int p = threadIdx.x; p < slices; p += kClassThreads) top = fmaxf(top, tops[p]);
     const float table = LOSS && ROWS ? table_unit(a, room) : 1.0f;
+    int id = -1;
+    float q = 0.0f, log_weight = 0.0f;                  // of lane's slot, in wave 0
     if (wave == 0) {
-        int id;
-        float log_weight;
-        const float q = slot_weight(a, t, lane, id, log_weight);
-        if (lane < a.s.K) { slot_q[lane] = q; slot_log[lane] = log_weight; slot_id[lane] = q != 0.0f ? id : -1; slot_z[lane] = 0.0f; }
+        q = slot_weight(a, t, lane, id, log_weight);
+        slot_id[lane] = id;
+        slot_z[lane] = 0.0f;
+        if constexpr (!LOSS) slot_pull[lane] = lane < a.s.K ? a.at<const float>(a.plan.pulls)[t * a.s.K + lane] : 0.0f;
         const bool lives = __any(id >= 0);
         if (lane == 0) alive = lives;
     }
@@ -1074,15 +1259,21 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
         __syncthreads();
         sum = (room[0] + room[1]) + (room[2] + room[3]);
         if (wave == 0) {
-            const float log2_sum = top + log2f(sum), lse = log2_sum * kLn2;
-            float loss = lane < a.s.K && slot_id[lane] >= 0 ? slot_q[lane] * (slot_log[lane] + (lse - slot_z[lane] * a.scale)) : 0.0f;
+            const float log2_sum = top + log2f(sum), lse = log2_sum * kLn2, z = slot_z[lane] * a.scale;
+            float loss = id >= 0 && q != 0.0f ? q * (log_weight + (lse - z)) : 0.0f;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) loss += __shfl_xor(loss, d);
             if (lane == 0) {
                 a.loss[t] = loss; a.lse[t] = lse;
                 if (!ROWS && a.row_grad) a.at<float>(a.plan.norm)[t] = log2_sum - kLift;
             }
+            if (ROWS || a.row_grad) {
+                const float pull = merge_slots(a, id, q) ? probability(z, lse) - q : 0.0f;
+                if constexpr (ROWS) slot_pull[lane] = pull;
+                else if (lane < a.s.K) a.at<float>(a.plan.pulls)[t * a.s.K + lane] = pull;
+            }
         }
+        if constexpr (ROWS) __syncthreads();
     }
     if constexpr (ROWS) {
         const float* parts = a.at<const float>(a.plan.mean_parts);
@@ -1099,8 +1290,8 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
                 e *= back;
 #pragma unroll 4
                 for (int j = group; j < a.s.K; j += groups) {
-                    const int id = slot_id[j];
-                    if (id >= 0 && id < a.s.V) e -= slot_q[j] * load4(w + id * a.w_stride, a.s.D, c);
+                    const float pull = slot_pull[j];    // 0 of an empty slot
+                    if (pull != 0.0f) e += pull * load4(w + slot_id[j] * a.w_stride, a.s.D, c);
                 }
             }
             gathered[threadIdx.x] = e;
@@ -1202,16 +1393,6 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
 #pragma unroll
             for (int i = 0; i < 16; ++i) named[m] |= (cell[(m * kBlock + row_of(i, lane)) * kBlock + (lane & 31)] != 0.0f ? 1u : 0u) << i;
         }
-    };
-    auto leave_out = [&](uint32_t named, u32x4 (&q)[2][NS]) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t two = named >> (8 * s + 2 * j), keep = ((two & 1) - 1 & 0xffffu) | ((two >> 1 & 1) - 1 & 0xffff0000u);
-#pragma unroll
-                for (int n = 0; n < NS; ++n) q[s][n][j] &= keep;
-            }
     };
     auto pull = [&](const uint16_t* tile, int m) {
         float c[16];
@@ -1395,6 +1576,11 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
         if (threadIdx.x == 0) hit = -1;
         __syncthreads();
     }
+    using Places = Named<kBlock>;
+    typename std::conditional<MODE == kMean, Places, int>::type named = [&] {
+        if constexpr (MODE == kMean) return Places(a, group, part, first, last, lane);
+        else return 0;
+    }();
     const float norm = MODE == kMean && x < a.s.T ? a.at<const float>(a.plan.norm)[x] : __builtin_inff();
     float ref = -1e30f, sum = 0.0f;
     f32x16 acc[MODE == kStats ? 1 : Q / 32];
@@ -1492,6 +1678,12 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
             if constexpr (MODE == kMean) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(z[j], to_log2, -norm));
+                if (named.next == (uint32_t)it)
+                    named.take(it, lane, [&](uint32_t rows, int c) {
+                        const bool mine = c >> 3 == wave && lane >> 5 == (c >> 2 & 1) && rows >> (lane & 31) & 1;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) if (mine && j == (c & 3)) p[j] = 0.0f;
+                    });
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(z[j], to_log2, start[j]));
@@ -1607,14 +1799,16 @@ template <int DP, bool MEAN> void launch_forward(const ClassArgs& a, int64_t pad
     if constexpr (!narrow_depth(DP)) {
         if (straight) class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats, true><<<grid, kClassThreads, 0, stream>>>(a, padded);
         else class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
-    } else if (a.cut.wy == 1) {
-        if (straight) class_forward_kernel<DP, 1, MEAN, true><<<grid, kClassThreads, 0, stream>>>(a, padded);
-        else class_forward_kernel<DP, 1, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
-    } else if (a.cut.wy == 2) {
-        class_forward_kernel<DP, 2, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
-    } else if constexpr (DP * NS <= 256) {
-        if (straight) class_forward_kernel<DP, 4, MEAN, true><<<grid, kClassThreads, 0, stream>>>(a, padded);
-        else class_forward_kernel<DP, 4, MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
+    } else {
+        const bool crowded = MEAN && crowded_tiles(a.s);
+        auto run = [&](auto wy) {
+            if (crowded) class_forward_kernel<DP, wy(), MEAN, false, MEAN><<<grid, kClassThreads, 0, stream>>>(a, padded);
+            else if (straight && wy() != 2) class_forward_kernel<DP, wy(), MEAN, wy() != 2><<<grid, kClassThreads, 0, stream>>>(a, padded);
+            else class_forward_kernel<DP, wy(), MEAN, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
+        };
+        if (a.cut.wy == 1) run(number<1>{});
+        else if (a.cut.wy == 2) run(number<2>{});
+        else if constexpr (DP * NS <= 256) run(number<4>{});
     }
 }
 template <int DP> void launch_gradient(const ClassArgs& a, int64_t padded, hipStream_t stream) {
@@ -1644,6 +1838,8 @@ hipError_t forward(ClassArgs a, hipStream_t stream) {
                 class_pack_kernel<dp()><<<(unsigned)(grid < 8192 ? grid : 8192), kClassThreads, 0, stream>>>(a, table);
             })) return e;
     }
+    if (a.plan.named)
+        class_named_kernel<<<(unsigned)(padded / kBlock), kRowThreads, 0, stream>>>(a, wide ? kBlock : blocks_per_tile(a.cut.wy, depth, kKind) * kBlock);
     if (hipError_t e = run(rows && !wide)) return e;
     const unsigned T = (unsigned)a.s.T;
     if (rows && !wide) class_finish_kernel<true, true><<<T, kClassThreads, 0, stream>>>(a, padded, depth, slices, lanes);

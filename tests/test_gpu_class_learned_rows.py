@@ -47,7 +47,7 @@ SIZES = [(3, 50, 64), (40, 47, 128), (64, 500, 256), (64, 500, 320), (33, 130, 6
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("T,V,D", SIZES)
-@pytest.mark.parametrize("name", ["grad_w"])
+@pytest.mark.parametrize("name", ["row_grad", "grad_w"])
 def test_cross_entropy_of_learned_rows(dtype, T, V, D, name):
     h, w, ids, g, scale = learned(dtype, T, V, D, T + D)
     for n, got, ref, lim, d in gradients(dtype, h, w, ids, None, g, scale):
@@ -58,7 +58,7 @@ def test_cross_entropy_of_learned_rows(dtype, T, V, D, name):
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("T,V,D", SIZES)
 @pytest.mark.parametrize("K", [3, 40])
-@pytest.mark.parametrize("name", ["grad_w"])
+@pytest.mark.parametrize("name", ["row_grad", "grad_w"])
 def test_students_that_agree_with_their_teacher(dtype, T, V, D, K, name):
     """The teacher's logits are the student's own scores of its K best classes; a few slots empty, a few named twice."""
     h, w, best, g, scale = learned(dtype, T, V, D, T + D + K)
@@ -87,7 +87,7 @@ def test_many_slots_that_name_one_class(dtype, D):
     ids[:, ::7] = best[:, None]
     logits = torch.randn((70, 40), generator=gen).cuda()
     for n, got, ref, lim, d in gradients(dtype, h, w, ids, logits, g, scale):
-        if n == "grad_w":
+        if n in ("grad_h", "grad_w"):
             check(got, ref, lim, d, n)
     loss, lse, row_grad = fsa.fsa_distill_fwd(h, w, ids, logits, 1.0, scale, emit_row_grad=True)
     first = fsa.fsa_distill_bwd(g, h, w, ids, logits, lse, row_grad, 1.0, scale)
