@@ -200,6 +200,8 @@ __device__ __forceinline__ float unit_of(float peak) {
     e = 15 - e;
     return ldexpf(1.0f, e < -126 ? -126 : e > 126 ? 126 : e);
 }
+// What scores of scaled tables are multiplied by, at least 2^-126: they are below 2^40, and -inf, a class that there is not, stays.
+__device__ __forceinline__ float not_zero(float x) { return fmaxf(x, 0x1p-126f); }
 __device__ __forceinline__ float finite_abs(float x) {
     const float a = fabsf(x);
     return a < __builtin_inff() ? a : 0.0f;
@@ -1006,7 +1008,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
     const int64_t row0 = ((int64_t)group * WX + x) * kBlock, row = row0 + (lane & 31);   // of h, held by this lane
     const bool live = row0 < padded;                      // wave-uniform
     u32x4 held[DP / 16][NS];
-    const float to_log2 = a.scale * kLog2e / hold_rows<DP / 16>(a, row, 0, lane, held, [](float peak) { return wave_max(peak); }) / table;
+    const float to_log2 = not_zero(a.scale * kLog2e / hold_rows<DP / 16>(a, row, 0, lane, held, [](float peak) { return wave_max(peak); }) / table);
 
     float ref = -1e30f, sum = 0.0f;                     // P = 2^(score - ref); ref = followed maximum - kLift
     f32x16 acc[MEAN ? DP / 32 : 1];
@@ -1331,9 +1333,9 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
     const bool live = v0 < a.s.V;                       // wave-uniform
 
     u32x4 held[DP / 16][NS];
-    const float to_log2 = a.scale * kLog2e / u.h /
+    const float to_log2 = not_zero(a.scale * kLog2e / u.h /
         hold<DP / 16>(static_cast<const Elem*>(a.w) + (v < a.s.V ? v : a.s.V - 1) * a.w_stride, a.s.D, 0, lane, true, held,
-                      [](float peak) { return wave_max(peak); });
+                      [](float peak) { return wave_max(peak); }));
     f32x16 acc[DP / 32];
 #pragma unroll
     for (auto& f : acc) f = f32x16{};
@@ -1570,7 +1572,7 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
     const float held_unit = MODE == kGradient
         ? hold<Q / 16>(w + (x < a.s.V ? x : a.s.V - 1) * a.w_stride, a.s.D, col0, lane, true, held, join)
         : hold_rows<Q / 16>(a, x, col0, lane, held, join);
-    const float to_log2 = a.scale * kLog2e / u.h / held_unit / table;
+    const float to_log2 = not_zero(a.scale * kLog2e / u.h / held_unit / table);
     if constexpr (MODE == kGradient) {
         for (int i = threadIdx.x; i < kBlock * kBlock; i += kClassThreads) cells[i] = 0.0f;
         if (threadIdx.x == 0) hit = -1;
