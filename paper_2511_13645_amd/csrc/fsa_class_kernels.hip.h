@@ -253,13 +253,13 @@ __device__ __forceinline__ float wave_max(float m) {
     return m;
 }
 
-// Score of slot i of [T,K] before the softmax over a row's slots; -inf: an empty slot, or one that the teacher gives nothing.
+// Logit of slot i of [T,K], before the temperature; -inf: an empty slot, or one that the teacher gives nothing.
 __device__ __forceinline__ float slot_score(const ClassArgs& a, int64_t i) {
     if (a.ids[i] < 0) return -__builtin_inff();
     if (!a.teacher) return 0.0f;
-    if (a.teacher_kind == 0) return static_cast<const float*>(a.teacher)[i] * a.inv_temperature;
-    if (a.teacher_kind == 1) return __builtin_bit_cast(float, (uint32_t)static_cast<const uint16_t*>(a.teacher)[i] << 16) * a.inv_temperature;
-    return (float)static_cast<const _Float16*>(a.teacher)[i] * a.inv_temperature;
+    if (a.teacher_kind == 0) return static_cast<const float*>(a.teacher)[i];
+    if (a.teacher_kind == 1) return __builtin_bit_cast(float, (uint32_t)static_cast<const uint16_t*>(a.teacher)[i] << 16);
+    return (float)static_cast<const _Float16*>(a.teacher)[i];
 }
 // Whether row t has a slot of any weight, asked by one lane, and by a whole wave.
 __device__ __forceinline__ bool lane_lives(const ClassArgs& a, int64_t t) {
@@ -340,12 +340,13 @@ __device__ __forceinline__ float slot_weight(const ClassArgs& a, int64_t t, int 
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
     if (top == -__builtin_inff()) top = 0.0f;           // no slot, or none with any weight
-    const float e = id < 0 ? 0.0f : expf(x - top);
+    x = (x - top) * a.inv_temperature;                  // differences alone: a logit over the temperature may be out of range
+    const float e = id < 0 ? 0.0f : expf(x);
     float sum = e;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
     if (sum == 0.0f) { id = -1; return 0.0f; }          // teacher gives its classes no weight: as a row without slots
-    log_weight = x - top - logf(sum);
+    log_weight = x - logf(sum);
     return e / sum;
 }
 

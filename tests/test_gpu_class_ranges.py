@@ -43,3 +43,20 @@ def test_very_small_tables(T, V, D, size):
     """Scores of nothing: every class is as likely, the loss is log V."""
     h, w, ids, _, g = inputs("xent", "f32", T, V, D, seed=9)
     compare("f32", h * size, w * size, ids, g=g, grads=size > 1e-30)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 300])
+@pytest.mark.parametrize("temperature", [0.25, 0.5, 1.0, 3.0])
+def test_teacher_logits_at_the_end_of_their_type(dtype, D, temperature):
+    """Logits that the temperature would take out of range: only their differences count.  A row of nothing but the lowest
+    number is one of equal weights, and one of nothing but the highest too."""
+    h, w, ids, logits, g = inputs("distill", dtype, 12, 90, D, 8, holes=False)
+    logits = logits.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    ends = torch.finfo(logits.dtype)
+    logits[0] = ends.min
+    logits[1] = ends.max
+    logits[2, 2:] = ends.min
+    logits[3, :3] = ends.max
+    logits[4, ::2] = -math.inf
+    compare(dtype, h, w, ids, logits, g, temperature)
