@@ -11,6 +11,7 @@ The library must have been built (``python -m paper_2511_13645_amd.build`` or
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import importlib.machinery
@@ -770,15 +771,18 @@ def _class_operands(h: torch.Tensor, w: torch.Tensor, ids: torch.Tensor, logits:
     return (_ptr(h), hs, _ptr(w), ws, _x_dtype(h), T, V, D), T, V, D, K
 
 
-def _class_workspace(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor, stream: Optional[torch.cuda.Stream]):
-    """The caller's workspace, or one of torch's for the call: memory that other streams get back only after `stream`."""
+def _allocating(stream: Optional[torch.cuda.Stream]):
+    """Allocations within are the call's stream's own: memory that another stream still works on is never handed out, and
+    what is dropped goes back to where only later work of that stream gets it."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _class_workspace(workspace: Optional[torch.Tensor], need: int, like: torch.Tensor):
+    """The caller's workspace, or one of torch's for the call."""
     if workspace is not None:
         check_workspace(workspace, like)
         return workspace
-    ws = torch.empty(need, dtype=torch.uint8, device=like.device)
-    if stream is not None:
-        ws.record_stream(stream)
-    return ws
+    return torch.empty(need, dtype=torch.uint8, device=like.device)
 
 
 def _class_fwd(name: str, h, w, ids, logits, scale: float, temperature: float, emit_row_grad: bool, workspace, stream):
@@ -788,10 +792,11 @@ def _class_fwd(name: str, h, w, ids, logits, scale: float, temperature: float, e
             return r
     lead, T, V, D, K = _class_operands(h, w, ids, logits)
     L = lib()
-    loss = torch.empty((T,), dtype=torch.float32, device=h.device)
-    lse = torch.empty_like(loss)
-    row_grad = torch.empty((T, D), dtype=torch.float32, device=h.device) if emit_row_grad else None
-    ws = _class_workspace(workspace, L.fsa_class_fwd_workspace_bytes(T, V, D, lead[4], K, int(emit_row_grad)), h, stream)
+    with _allocating(stream):
+        loss = torch.empty((T,), dtype=torch.float32, device=h.device)
+        lse = torch.empty_like(loss)
+        row_grad = torch.empty((T, D), dtype=torch.float32, device=h.device) if emit_row_grad else None
+        ws = _class_workspace(workspace, L.fsa_class_fwd_workspace_bytes(T, V, D, lead[4], K, int(emit_row_grad)), h)
     tail = (_ptr(loss), _ptr(lse), _ptr(row_grad), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, h))
     if logits is None:
         rc = L.fsa_xent_fwd(*lead, scale, _ptr(ids), *tail)
@@ -813,10 +818,11 @@ def _class_bwd(name: str, grad_loss, h, w, ids, logits, lse, row_grad, scale: fl
         _shape(row_grad, "row_grad", (T, D))
     _same_device(h, (grad_loss, "grad_loss"), (lse, "lse"), (row_grad, "row_grad"))
     L = lib()
-    grad_h = torch.empty((T, D), dtype=h.dtype, device=h.device) if want_h else None
-    grad_w = torch.empty((V, D), dtype=w.dtype, device=w.device) if want_w else None
     need = L.fsa_class_bwd_workspace_bytes(T, V, D, lead[4], K, int(want_h and row_grad is None), int(want_w))
-    ws = _class_workspace(workspace, need, h, stream)
+    with _allocating(stream):
+        grad_h = torch.empty((T, D), dtype=h.dtype, device=h.device) if want_h else None
+        grad_w = torch.empty((V, D), dtype=w.dtype, device=w.device) if want_w else None
+        ws = _class_workspace(workspace, need, h)
     tail = (_ptr(lse), _ptr(row_grad), _ptr(grad_h), _ptr(grad_w), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, h))
     if logits is None:
         rc = L.fsa_xent_bwd(_ptr(grad_loss), *lead, scale, _ptr(ids), *tail)
@@ -842,7 +848,8 @@ def fsa_xent_fwd(h: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, scale:
                  ) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
     """Softmax cross entropy of rows h [T,D] against the classes w [V,D], the scores never kept; targets [T] int32, a
     negative one is none.  Returns (loss [T], lse [T], row_grad [T,D] | None), fp32.  `workspace`: see
-    fsa_class_fwd_workspace_bytes; torch's memory without one."""
+    fsa_class_fwd_workspace_bytes; torch's memory without one.  With `stream`, results and workspace are that stream's, as of
+    calls within ``torch.cuda.stream(stream)``: inputs have to be ready there, and whoever uses results elsewhere orders that."""
     return _class_fwd("fsa_xent_fwd", h, w, targets, None, float(scale), 1.0, bool(emit_row_grad), workspace, stream)
 
 
