@@ -115,17 +115,18 @@ constexpr bool slots_apart(const ClassShape& s) { return s.K > 1; }
 // x 336 fp32 1.54 ms without, 1.67 with).  Tables of a quarter of a million elements and less are not worth the launch.
 inline bool forward_packs(const ClassShape& s, bool straight) {
     const int depth = class_depth(s.D);
+    if (!straight && !narrow_depth(depth) && s.kind == 0) return true;          // (no wave has a row whole, to make its unit of)
     const int64_t few = !narrow_depth(depth) && resident_workgroups(depth, s.kind) == 512 ? 4 : 2;
     return !straight && forward_cut(s).groups > few && s.V * s.D > (1 << 18);
 }
 
 // Byte offsets into the caller's workspace.
 struct ClassPlan {
-    size_t peaks, rows, table, top, sum, mean_parts, norm, pulls, named, named_starts, loss, start, signs, buckets, slots, row_slots, row_grad, grad_parts, bytes;
+    size_t peaks, rows, table, top, sum, mean_parts, norm, back, pulls, table_scales, scales, named, named_starts, loss, start, signs, buckets, slots, row_slots, row_grad, grad_parts, bytes;
     bool packed;                                        // the forward reads the table from planes made for the call,
     bool straight;                                      // or as it is: 16-bit rows of a depth, on the 16-byte grid
 };
-constexpr int kPeaksTable = 512, kPeaksRows = 64, kPeaksGrad = 64, kPeaks = kPeaksTable + kPeaksRows + kPeaksGrad;
+constexpr int kPeaks = 64;                              // workgroups that look for the gradients' largest
 
 inline ClassPlan plan_of(const ClassShape& s, bool straight, bool forward, bool want_rows, bool want_grad_w) {
     ClassPlan p{};
@@ -139,10 +140,12 @@ inline ClassPlan plan_of(const ClassShape& s, bool straight, bool forward, bool 
         p.straight = straight;
         p.packed = forward_packs(s, straight) && !(want_rows && narrow && crowded_tiles(s));
         if (p.packed) p.table = room(padded_rows(s.V) * depth * 2 * class_planes(s.kind));
+        if (p.packed && s.kind == 0) p.table_scales = room(padded_rows(s.V) * 4);
         p.top = room(stats * T * 4);
         p.sum = room(stats * T * 4);
         if (want_rows) p.mean_parts = room(slices * T * depth * 4);
         if (want_rows && !narrow) p.norm = room(T * 4);
+        if (want_rows && !narrow) p.back = room(T * 4);
         if (want_rows && !narrow) p.pulls = room(T * s.K * 4);
         if (want_rows && s.K > kWaveSlots) {
             p.named = room(T * s.K * 4);
@@ -157,6 +160,7 @@ inline ClassPlan plan_of(const ClassShape& s, bool straight, bool forward, bool 
         const ClassCut c = gradient_cut(s);
         p.rows = room(T * depth * 2 * class_planes(s.kind));
         p.start = room(T * 4);
+        if (s.kind == 0) p.scales = room(T * 4);
         p.signs = room(T / kBlock * 4);
         p.buckets = room(T / kBlock * buckets_of(s.V, s.K).count * 4);
         p.slots = room(T * s.K * 8);

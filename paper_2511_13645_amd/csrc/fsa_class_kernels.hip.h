@@ -6,9 +6,11 @@
 // (l/32, j) of step s, so with A read transposed at those same rows no lane ever exchanges a probability:
 //     acc[d, held] += sum over streamed rows of streamed[row, d] * P[row, held].
 //
-// fp32 rows are held as two fp16 planes, x * 2^e = hi + lo with 2^e that brings the largest finite |x| of the table to
-// [2^14, 2^15): 22 bits of every element down to 2^-16 of the largest and never an error over 2^-40 of it.  Products
-// take hi*hi + hi*lo + lo*hi; what is left out is below 2^-22 of a product, as is what the split rounds away.
+// fp32 rows are held as two fp16 planes, x * 2^e = hi + lo with 2^e that brings the largest finite |x| of the row to
+// [2^14, 2^15): 22 bits of every element down to 2^-16 of the row's largest and never an error over 2^-40 of it, whatever other rows
+// hold.  Products take hi*hi + hi*lo + lo*hi; what is left out is below 2^-22 of a product, as is what the split rounds away.
+// On the held side 2^-e is in the scores' multiplier, a lane's own.  Streamed rows have it beside their tile: s = 2^-e multiplies
+// a score, and the second product takes p s, so that what a running reference follows is p s as well.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -191,15 +193,29 @@ __device__ __forceinline__ void store4(void* p, int64_t i, f32x4 x) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// powers of two that bring the largest finite element of a table to [2^14, 2^15)
+// powers of two that bring the largest finite element of a row to [2^14, 2^15)
 // ---------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ float unit_of(float peak) {
-    if (!(peak > 0.0f)) return 1.0f;
+__device__ __forceinline__ int unit_exponent(float peak, int most) {
+    if (!(peak > 0.0f)) return 0;
     int e = 0;
     frexpf(peak, &e);                                   // peak = m * 2^e, m in [0.5, 1)
     e = 15 - e;
-    return ldexpf(1.0f, e < -126 ? -126 : e > 126 ? 126 : e);
+    return e < -126 ? -126 : e > most ? most : e;
 }
+__device__ __forceinline__ float unit_of(float peak, int most = 126) { return ldexpf(1.0f, unit_exponent(peak, most)); }
+// Streamed rows: at most 2^80, so that p, of p s, stays in range.  Rows whose largest element is below 2^-82 have fewer bits than 22.
+constexpr int kMostUnit = 80;
+// What a tile of streamed rows has beside it: s of every row and, in the forward, the binary logarithm of s 2^15 and its inverse
+// (2^15: the logarithms of rows with elements around one are small, and a score that one is added to loses nothing).
+__device__ __forceinline__ float log_scale(float s) { return (float)((int)(__builtin_bit_cast(uint32_t, s) >> 23) - 127 + 15); }
+template <int ROWS> struct Scales {
+    float s[ROWS], log[ROWS], inverse[ROWS];
+    __device__ __forceinline__ void put(int r, float scale) {
+        s[r] = scale;
+        log[r] = log_scale(scale);
+        inverse[r] = 0x1p-15f / scale;
+    }
+};
 // What scores of scaled tables are multiplied by, at least 2^-126: they are below 2^40, and -inf, a class that there is not, stays.
 __device__ __forceinline__ float not_zero(float x) { return fmaxf(x, 0x1p-126f); }
 __device__ __forceinline__ float finite_abs(float x) {
@@ -220,30 +236,24 @@ __device__ __forceinline__ float block_peak(const float* peaks, int n, float* ro
     __syncthreads();
     return m;
 }
-// Units of the whole table (the forward streams it past rows), of all rows, and of the losses' gradients.
+// Unit of the gradients: of |g| s over rows that live, for fp32 rows, or of |g|.
 template <int WAVES = kClassWaves>
-__device__ __forceinline__ float table_unit(const ClassArgs& a, float* room) {
-    if constexpr (kKind != 0) return 1.0f;
-    return unit_of(block_peak<WAVES>(a.at<const float>(a.plan.peaks), kPeaksTable, room));
-}
-struct Units { float h, g; };
-template <int WAVES = kClassWaves>
-__device__ __forceinline__ Units row_units(const ClassArgs& a, float* room) {
+__device__ __forceinline__ float grad_unit(const ClassArgs& a, float* room) {
     // bfloat16 has the range as it is: 24 binades keep products that its subnormals can still hold out of fp32's
-    Units u{1.0f, 0x1p24f};
-    const float* p = a.at<const float>(a.plan.peaks);
-    if constexpr (kKind == 0) u.h = unit_of(block_peak<WAVES>(p + kPeaksTable, kPeaksRows, room));
-    if constexpr (kHalf) u.g = unit_of(block_peak<WAVES>(p + kPeaksTable + kPeaksRows, kPeaksGrad, room));
-    return u;
+    if constexpr (!kHalf) return 0x1p24f;
+    return unit_of(block_peak<WAVES>(a.at<const float>(a.plan.peaks), kPeaks, room));
 }
-// A held side has a unit of its own: that of a wave's 32 rows (`peak` of every lane, the largest finite |x| it holds).
+// The largest finite |x| that a lane holds of a row.
 __device__ __forceinline__ float peak_of(const Eight& e) {
     float m = 0.0f;
     if constexpr (kKind == 0) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) m = fmaxf(m, finite_abs(__builtin_bit_cast(float, e.v[i][j])));
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t bits = e.v[i][j];        // (hipcc casts the vector's first element for e.v[i][j] itself)
+                m = fmaxf(m, finite_abs(__builtin_bit_cast(float, bits)));
+            }
     }
     return m;
 }
@@ -261,55 +271,27 @@ __device__ __forceinline__ float slot_score(const ClassArgs& a, int64_t i) {
     if (a.teacher_kind == 1) return __builtin_bit_cast(float, (uint32_t)static_cast<const uint16_t*>(a.teacher)[i] << 16);
     return (float)static_cast<const _Float16*>(a.teacher)[i];
 }
-// Whether row t has a slot of any weight, asked by one lane, and by a whole wave.
-__device__ __forceinline__ bool lane_lives(const ClassArgs& a, int64_t t) {
-    for (int j = 0; j < a.s.K; ++j) if (slot_score(a, t * a.s.K + j) != -__builtin_inff()) return true;
-    return false;
-}
+// Whether row t has a slot of any weight, asked by a whole wave.
 __device__ __forceinline__ bool row_lives(const ClassArgs& a, int64_t t, int lane) {
     return __any(lane < a.s.K && slot_score(a, t * a.s.K + lane) != -__builtin_inff());
 }
 
-// Largest finite magnitudes, a part per workgroup, of the table, of the rows and of the losses' gradients (those of rows that
-// live).  One more read of an fp32 table, 1.28 GB in 0.35 ms: the price of 22-bit products at three matrix instructions instead
-// of six of three bfloat16 planes.
-__global__ __launch_bounds__(kClassThreads) void class_peaks_kernel(ClassArgs a, int table, int rows, int grad) {
+// Largest |g| s of fp32 rows that live, or |g|, a part per workgroup.
+__global__ __launch_bounds__(kClassThreads) void class_peaks_kernel(ClassArgs a) {
     __shared__ float room[kClassWaves];
-    float* out = a.at<float>(a.plan.peaks);
-    int b = blockIdx.x;
-    float m = 0.0f;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (b < table) {
-        const Elem* w = static_cast<const Elem*>(a.w);
-        if (a.w_stride == a.s.D) {
-            const int64_t n = a.s.V * a.s.D, step = (int64_t)table * kClassThreads;
-            const int64_t quads = (reinterpret_cast<uintptr_t>(w) & 15) == 0 ? n / 4 : 0;
-            for (int64_t i = (int64_t)b * kClassThreads + threadIdx.x; i < quads; i += step) {
-                const f32x4 x = reinterpret_cast<const f32x4*>(w)[i];
-                m = fmaxf(fmaxf(m, fmaxf(finite_abs(x[0]), finite_abs(x[1]))), fmaxf(finite_abs(x[2]), finite_abs(x[3])));
-            }
-            for (int64_t i = quads * 4 + (int64_t)b * kClassThreads + threadIdx.x; i < n; i += step) m = fmaxf(m, finite_abs(value(w[i])));
-        } else {
-            for (int64_t v = (int64_t)b * kClassWaves + wave; v < a.s.V; v += (int64_t)table * kClassWaves)
-                for (int d = lane; d < a.s.D; d += 64) m = fmaxf(m, finite_abs(value(w[v * a.w_stride + d])));
-        }
-    } else if ((b -= table) < rows) {
-        out += kPeaksTable;
-        for (int64_t t = (int64_t)b * kClassWaves + wave; t < a.s.T; t += (int64_t)rows * kClassWaves) {
-            if (!row_lives(a, t, lane)) continue;
-            for (int d = lane; d < a.s.D; d += 64) m = fmaxf(m, finite_abs(value(static_cast<const Elem*>(a.h)[t * a.h_stride + d])));
-        }
-    } else {
-        b -= rows;
-        out += kPeaksTable + kPeaksRows;
-        for (int64_t t = (int64_t)b * kClassWaves + wave; t < a.s.T; t += (int64_t)grad * kClassWaves)
-            if (row_lives(a, t, lane)) m = fmaxf(m, finite_abs(a.grad_loss[t]));
+    float m = 0.0f;
+    for (int64_t t = (int64_t)blockIdx.x * kClassWaves + wave; t < a.s.T; t += (int64_t)gridDim.x * kClassWaves) {
+        if (!row_lives(a, t, lane)) continue;
+        float peak = 0.0f;
+        if constexpr (kKind == 0)
+            for (int d = lane; d < a.s.D; d += 64) peak = fmaxf(peak, finite_abs(value(static_cast<const Elem*>(a.h)[t * a.h_stride + d])));
+        const int e = kKind == 0 ? unit_exponent(wave_max(peak), kMostUnit) : 0;
+        m = fmaxf(m, fminf(ldexpf(finite_abs(a.grad_loss[t]), -e), 0x1.fffffep127f));
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) m = fmaxf(m, __shfl_xor(m, d));
     if (lane == 0) room[wave] = m;
     __syncthreads();
-    if (threadIdx.x == 0) out[b] = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
+    if (threadIdx.x == 0) a.at<float>(a.plan.peaks)[blockIdx.x] = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
 }
 
 // Where chunk c of row r lies in planes of rows of DP elements, in elements.  Wide planes lie as a wave fetches them: by
@@ -358,7 +340,7 @@ struct SlotWord {
     __device__ __forceinline__ int count() const { return w >> 11 & 4095; }
     __device__ __forceinline__ bool negative() const { return w >> 31; }
 };
-// A slot: its row of the 32 above 27 bits of class, and g (q - p) with the units of the gradient, never zero.
+// A slot: its row of the 32 above 27 bits of class, and g (q - p), sorted with the units of the gradient and never zero.
 struct Slot { uint32_t key; float pull; };
 
 constexpr int kRowThreads = 1024, kRowWaves = kRowThreads / 64, kRowsEach = kBlock / kRowWaves;
@@ -459,15 +441,12 @@ template <int N> __device__ __forceinline__ void target_probability(const ClassA
 // Each place of [row][class] is one slot's.
 __device__ __forceinline__ Slot row_slot(const ClassArgs& a, int id, float q, float p, float g) {
     const bool some = merge_slots(a, id, q);
-    const float pull = g * (q - p);
-    return Slot{some ? (uint32_t)id : ~0u, pull != 0.0f ? pull : 0x1p-126f};    // (a place that is named is told by not being zero)
+    return Slot{some ? (uint32_t)id : ~0u, g * (q - p)};
 }
 
 // Rows of more than one slot, ahead of the sorting: one workgroup per row, a quarter of its slots to a wave.  Bound by the reads of
 // the classes' rows: 4096 rows of 32 slots, 128 bfloat16 (33 MB of rows) 28 us.
 __global__ __launch_bounds__(kClassThreads) void class_slots_kernel(ClassArgs a, int lanes) {
-    __shared__ float room[kClassWaves];
-    const Units u = row_units(a, room);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t t = blockIdx.x;
     const int each = (a.s.K + kClassWaves - 1) / kClassWaves, from = wave * each, to = from + each < a.s.K ? from + each : a.s.K;
@@ -476,7 +455,7 @@ __global__ __launch_bounds__(kClassThreads) void class_slots_kernel(ClassArgs a,
     const float weight = slot_weight(a, t, lane, id, log_weight);
     const bool lives = __any(id >= 0);
     const float p = lives ? slot_probability(a, t, id, lane, lanes, from, to) : 0.0f;
-    const Slot s = row_slot(a, id, weight, p, lives ? a.grad_loss[t] * u.g : 0.0f);
+    const Slot s = row_slot(a, id, weight, p, lives ? a.grad_loss[t] : 0.0f);
     if (lane >= from && lane < to) a.at<Slot>(a.plan.row_slots)[t * a.s.K + lane] = s;
 }
 
@@ -490,7 +469,7 @@ __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, in
     const ClassBuckets bk = a.buckets;
     if (threadIdx.x == 0) signs = 0;
     for (int i = threadIdx.x; i < bk.count; i += kRowThreads) counts[i] = 0;
-    const Units u = row_units<kRowWaves>(a, room);
+    const float unit = grad_unit<kRowWaves>(a, room);
     uint16_t* planes = a.at<uint16_t>(a.plan.rows);
     __syncthreads();
     int ids[kRowsEach];
@@ -504,25 +483,41 @@ __global__ __launch_bounds__(kRowThreads) void class_rows_kernel(ClassArgs a, in
         float log_weight, weight = 0.0f;
         if (t < a.s.T) weight = slot_weight(a, t, lane, id, log_weight);
         const bool lives = __any(id >= 0);
-        for (int c = lane; c < DP / 8; c += 64) {
-            u32x4 p[NS] = {};
-            if (lives && c * 8 < a.s.D)
-                planes_of(load8(static_cast<const Elem*>(a.h) + t * a.h_stride, a.s.D, c * 8), u.h, p);
+        constexpr int kEach = (DP / 8 + 63) / 64;
+        Eight e[kEach];
+        float peak = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int c = lane + 64 * i;
+            e[i] = Eight{};
+            if (lives && c * 8 < a.s.D) e[i] = load8(static_cast<const Elem*>(a.h) + t * a.h_stride, a.s.D, c * 8);
+            peak = fmaxf(peak, peak_of(e[i]));
+        }
+        const int exponent = kKind == 0 ? unit_exponent(wave_max(peak), kMostUnit) : 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            const int c = lane + 64 * i;
+            if (c >= DP / 8) break;
+            u32x4 p[NS];
+            planes_of(e[i], ldexpf(1.0f, exponent), p);
 #pragma unroll
             for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + (int64_t)n * padded * DP + plane_place<DP>(t, c)) = p[n];
         }
-        const float loss_grad = lives ? a.grad_loss[t] : 0.0f, g = loss_grad * u.g;
+        const int up = (kKind == 0 ? (int)(__builtin_bit_cast(uint32_t, unit) >> 23) - 127 : 0) - exponent;       // the unit times s
+        const float loss_grad = lives ? a.grad_loss[t] : 0.0f, g = kKind == 0 ? ldexpf(loss_grad, up) : loss_grad * unit;
         if (a.grad_h && t < a.s.T) write_row_grad(a, t, loss_grad, lives, lane);
         // P = |g| * softmax = 2^(score * log2e + start), its sign apart
         if (lane == 0) {
             a.at<float>(a.plan.start)[t] = lives ? log2f(fabsf(g)) - a.lse_in[t] * kLog2e : -__builtin_inff();
+            if constexpr (kKind == 0) a.at<float>(a.plan.scales)[t] = ldexpf(1.0f, -exponent);
             if (g < 0.0f) atomicOr(&signs, 1u << q);
         }
         Slot own{~0u, 0.0f};
-        if (!a.plan.row_slots) own = row_slot(a, id, weight, target[k], g);
+        if (!a.plan.row_slots) own = row_slot(a, id, weight, target[k], loss_grad);
         else if (t < a.s.T && lane < a.s.K) own = a.at<const Slot>(a.plan.row_slots)[t * a.s.K + lane];
         ids[k] = (int)own.key;
-        pulls[k] = own.pull;
+        pulls[k] = kKind == 0 ? ldexpf(own.pull, up) : own.pull * unit;
+        if (pulls[k] == 0.0f) pulls[k] = 0x1p-126f;     // (a place that is named is told by not being zero)
         if (ids[k] >= 0) atomicAdd(&counts[(uint32_t)ids[k] / kBlock / (uint32_t)bk.per], 1u);
     }
     __syncthreads();
@@ -617,13 +612,51 @@ struct SlotFeed {
     }
 };
 
-// The table as planes of padded rows, zero behind its last row and element.  Bound by memory: 2.5 M x 128 fp32, 1.28 GB in and
-// out each, 0.47 ms (5.4 TB/s).
+// The table as planes of padded rows, zero behind its last row and element, and s of fp32 rows.  Bound by memory: 2.5 M x 128 fp32,
+// 1.28 GB in and out each, 0.47 ms (5.4 TB/s).
 template <int DP>
 __global__ __launch_bounds__(kClassThreads) void class_pack_kernel(ClassArgs a, int64_t rows) {
-    __shared__ float room[kClassWaves];
-    const float unit = table_unit(a, room);
     uint16_t* planes = a.at<uint16_t>(a.plan.table);
+    if constexpr (kKind == 0 && !narrow_depth(DP)) {    // tiles of 32 rows, a quarter to a wave, as its planes lie
+        constexpr int chunks = DP / kClassWaves / 8, each = kBlock * chunks / 64;
+        __shared__ float room[kClassWaves][kBlock];
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        for (int64_t tile = blockIdx.x; tile < rows / kBlock; tile += gridDim.x) {
+            Eight e[each];
+            float peak[2] = {}, unit[2];
+#pragma unroll
+            for (int i = 0; i < each; ++i) {
+                const int64_t v = tile * kBlock + (lane >> 2) + 16 * (i & 1);
+                const int c = wave * chunks + (lane & 3) + 4 * (i >> 1);
+                e[i] = Eight{};
+                if (v < a.s.V && c * 8 < a.s.D) e[i] = load8(static_cast<const Elem*>(a.w) + v * a.w_stride, a.s.D, c * 8);
+                peak[i & 1] = fmaxf(peak[i & 1], peak_of(e[i]));
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                peak[i] = fmaxf(peak[i], __shfl_xor(peak[i], 1));
+                peak[i] = fmaxf(peak[i], __shfl_xor(peak[i], 2));
+                if ((lane & 3) == 0) room[wave][(lane >> 2) + 16 * i] = peak[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = (lane >> 2) + 16 * i;
+                unit[i] = unit_of(fmaxf(fmaxf(room[0][r], room[1][r]), fmaxf(room[2][r], room[3][r])), kMostUnit);
+                if (wave == 0 && (lane & 3) == 0) a.at<float>(a.plan.table_scales)[tile * kBlock + r] = 1.0f / unit[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < each; ++i) {
+                u32x4 p[NS];
+                planes_of(e[i], unit[i & 1], p);
+#pragma unroll
+                for (int n = 0; n < NS; ++n)
+                    *reinterpret_cast<u32x4*>(planes + (int64_t)n * rows * DP + (((tile * kClassWaves + wave) * each + i) * 64 + lane) * 8) = p[n];
+            }
+        }
+        return;
+    }
     for (int64_t q = (int64_t)blockIdx.x * kClassThreads + threadIdx.x; q < rows * (DP / 8); q += (int64_t)gridDim.x * kClassThreads) {
         int64_t v = q / (DP / 8);                       // chunk q of the planes, in their own order
         int c = (int)(q % (DP / 8));
@@ -634,8 +667,18 @@ __global__ __launch_bounds__(kClassThreads) void class_pack_kernel(ClassArgs a, 
             v = load / each / kClassWaves * kBlock + (lane >> 2) + 16 * (i & 1);
             c = (int)(quarter * chunks + (lane & 3) + 4 * (i >> 1));
         }
-        u32x4 p[NS] = {};
-        if (v < a.s.V && c * 8 < a.s.D) planes_of(load8(static_cast<const Elem*>(a.w) + v * a.w_stride, a.s.D, c * 8), unit, p);
+        Eight e = {};
+        if (v < a.s.V && c * 8 < a.s.D) e = load8(static_cast<const Elem*>(a.w) + v * a.w_stride, a.s.D, c * 8);
+        float unit = 1.0f;
+        if constexpr (kKind == 0) {                     // DP / 8 neighbouring lanes have a row
+            float peak = peak_of(e);
+#pragma unroll
+            for (int d = 1; d < DP / 8; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
+            unit = unit_of(peak, kMostUnit);
+            if (c == 0) a.at<float>(a.plan.table_scales)[v] = 1.0f / unit;
+        }
+        u32x4 p[NS];
+        planes_of(e, unit, p);
 #pragma unroll
         for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(planes + (int64_t)n * rows * DP + q * 8) = p[n];
     }
@@ -661,10 +704,19 @@ struct Tile {
                 e[i] = load8(w + v * stride, D, c * 8);
             }
         }
-        __device__ __forceinline__ void store(uint16_t* lds, float unit) const {
+        // (DP / 8 neighbouring lanes have a row)
+        __device__ __forceinline__ void store(uint16_t* lds, Scales<ROWS>* scales) const {
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 const int q = i * kClassThreads + threadIdx.x, r = q / (DP / 8), c = q % (DP / 8);
+                float unit = 1.0f;
+                if constexpr (kKind == 0) {
+                    float peak = peak_of(e[i]);
+#pragma unroll
+                    for (int d = 1; d < DP / 8; d *= 2) peak = fmaxf(peak, __shfl_xor(peak, d));
+                    unit = unit_of(peak, kMostUnit);
+                    if (c == 0) scales->put(r, 1.0f / unit);
+                }
                 u32x4 p[NS];
                 planes_of(e[i], unit, p);
 #pragma unroll
@@ -754,16 +806,16 @@ __device__ __forceinline__ void leave_out(uint32_t named, u32x4 (&q)[2][NS]) {
 // Row that register i of a result stands for, in its block.
 __device__ __forceinline__ int row_of(int i, int lane) { return 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3); }
 
-// Columns [col0, col0 + 16 KS) of a row as B operands, and their unit: that of what `join` makes of the lanes' peaks.
+// Columns [col0, col0 + 16 KS) of a row as B operands, and the row's unit: that of what `join` makes of the peak of a lane's columns.
 template <int KS, class Join>
-__device__ __forceinline__ float hold(const Elem* row, int64_t D, int col0, int lane, bool lives, u32x4 (&held)[KS][NS], Join join) {
+__device__ __forceinline__ float hold(const Elem* row, int64_t D, int col0, int lane, u32x4 (&held)[KS][NS], Join join) {
     Eight e[KS];
     float peak = 0.0f;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         const int col = col0 + 16 * ks + 8 * (lane >> 5);
         e[ks] = Eight{};
-        if (lives && col < D) e[ks] = load8(row, D, col);
+        if (col < D) e[ks] = load8(row, D, col);
         peak = fmaxf(peak, peak_of(e[ks]));
     }
     const float unit = kKind == 0 ? unit_of(join(peak)) : 1.0f;
@@ -771,14 +823,11 @@ __device__ __forceinline__ float hold(const Elem* row, int64_t D, int col0, int 
     for (int ks = 0; ks < KS; ++ks) planes_of(e[ks], unit, held[ks]);
     return unit;
 }
-
-// The same of row `row` of h, behind the last row of that.  Nothing of a row reaches another one but the unit, so only that
-// looks at whether rows have slots.
-template <int KS, class Join>
-__device__ __forceinline__ float hold_rows(const ClassArgs& a, int64_t row, int col0, int lane, u32x4 (&held)[KS][NS], Join join) {
-    const int64_t t = row < a.s.T ? row : a.s.T - 1;
-    const Elem* h = static_cast<const Elem*>(a.h) + t * a.h_stride;
-    return hold<KS>(h, a.s.D, col0, lane, kKind != 0 || lane_lives(a, t), held, join);
+// The peak of a row that two lanes hold.
+__device__ __forceinline__ float both_halves(float peak) { return fmaxf(peak, __shfl_xor(peak, 32)); }
+// Row `row` of h, or its last one.
+__device__ __forceinline__ const Elem* held_row(const ClassArgs& a, int64_t row) {
+    return static_cast<const Elem*>(a.h) + (row < a.s.T ? row : a.s.T - 1) * a.h_stride;
 }
 // Two values of P, registers 2j and 2j + 1 of step s, into that step's B operand; planes of what fp16 or bfloat16 takes of
 // them, nearest even.
@@ -999,19 +1048,19 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
     constexpr bool AHEAD = WY == 1;
     constexpr int TILES = AHEAD ? 3 : 2;
     __shared__ __align__(16) uint16_t lds[TILES][NS * T::kPlane];
-    __shared__ float room[kClassWaves];
+    using Beside = Scales<NB * kBlock>;
+    __shared__ __align__(16) Beside scales[kKind == 0 ? TILES : 1];
     __shared__ uint32_t places[CROWDED ? kClassWaves : 1][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = wave % WX, y = wave / WX;
     const ClassCut::Place place = a.cut.place(blockIdx.x);
     const int part = place.part, group = place.group, first = place.first, last = place.last;
-    const float table = table_unit(a, room);
     if constexpr (CROWDED) places[wave][lane] = 0;
     const int64_t row0 = ((int64_t)group * WX + x) * kBlock, row = row0 + (lane & 31);   // of h, held by this lane
     const bool live = row0 < padded;                      // wave-uniform
     u32x4 held[DP / 16][NS];
-    const float to_log2 = not_zero(a.scale * kLog2e / hold_rows<DP / 16>(a, row, 0, lane, held, [](float peak) { return wave_max(peak); }) / table);
+    const float to_log2 = not_zero(a.scale * kLog2e / hold<DP / 16>(held_row(a, row), a.s.D, 0, lane, held, both_halves));
 
-    float ref = -1e30f, sum = 0.0f;                     // P = 2^(score - ref); ref = followed maximum - kLift
+    float ref = -3e38f, sum = 0.0f;                     // P = 2^(score - ref); ref = followed maximum - kLift
     f32x16 acc[MEAN ? DP / 32 : 1];
 #pragma unroll
     for (auto& f : acc) f = f32x16{};
@@ -1021,14 +1070,19 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
     const char* planes = a.plan.packed ? a.ws + a.plan.table : static_cast<const char*>(a.w);
     const int row_bytes = 2 * (a.plan.packed ? DP : (int)a.w_stride);
     const int64_t table_rows = a.plan.packed ? padded_rows(a.s.V) : a.s.V;
+    float next_scale = 1.0f;
     auto fetch = [&](int it) {
         if (it >= last) return;
         if constexpr (STRAIGHT) next.load(planes, row_bytes, table_rows * row_bytes, table_rows, (int64_t)it * NB * kBlock);
         else next.load(static_cast<const Elem*>(a.w), a.w_stride, a.s.V, a.s.D, (int64_t)it * NB * kBlock);
+        if constexpr (kKind == 0 && STRAIGHT)
+            if (threadIdx.x < NB * kBlock) next_scale = a.at<const float>(a.plan.table_scales)[(int64_t)it * NB * kBlock + threadIdx.x];
     };
-    auto store = [&](uint16_t* tile) {
-        if constexpr (STRAIGHT) next.store(tile);
-        else next.store(tile, table);
+    auto store = [&](int slot) {
+        if constexpr (STRAIGHT) {
+            next.store(lds[slot]);
+            if constexpr (kKind == 0) if (threadIdx.x < NB * kBlock) scales[slot].put(threadIdx.x, next_scale);
+        } else next.store(lds[slot], &scales[kKind == 0 ? slot : 0]);
     };
     f32x16 score[MY];
     float top;                                          // of this lane's scores of a tile
@@ -1044,7 +1098,20 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
             }
         }
     };
-    auto find_top = [&](int it) {
+    // fp32: the scores become binary logarithms of p s here (with a mean to make or not: the same sums), 16-bit scores those of p when
+    // they are exponentiated.
+    auto find_top = [&](int it, int slot) {
+        if constexpr (kKind == 0)
+#pragma unroll
+            for (int m = 0; m < MY; ++m)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const int r = (y * MY + m) * kBlock + row_of(i, lane);
+                    const f32x4 s = *reinterpret_cast<const f32x4*>(&scales[slot].s[r]) * to_log2;
+                    const f32x4 l = *reinterpret_cast<const f32x4*>(&scales[slot].log[r]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) score[m][i + j] = fmaf(score[m][i + j], s[j], l[j]);
+                }
         if ((int64_t)(it + 1) * NB * kBlock > a.s.V) {  // the last tile: classes that there are not
             asm volatile("");                           // a branch, not sixteen selects in every tile
             const int left = (int)(a.s.V - (int64_t)it * NB * kBlock) - y * MY * kBlock;
@@ -1058,8 +1125,9 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
         for (int m = 0; m < MY; ++m)
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, score[m][i]);
-        top *= to_log2;
+        if constexpr (kKind != 0) top *= to_log2;
     };
+    auto power = [&](float z) { return __builtin_amdgcn_exp2f(kKind == 0 ? z - ref : fmaf(z, to_log2, -ref)); };
 
     // Ahead: a tile's scores are made while the tile before it is exponentiated and multiplied; its table rows lie in the
     // next of three LDS tiles by then, those of the tile after it are on their way in registers.
@@ -1071,31 +1139,32 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
         else return 0;
     }();
     if constexpr (AHEAD) {
-        store(lds[0]);
+        store(0);
         fetch(first + 1);
         __syncthreads();
         if (live) {
             scores(lds[0]);
-            find_top(first);
+            find_top(first, 0);
         }
     }
     for (int it = first; it < last; ++it) {
-        uint16_t* tile = lds[slot];
+        const int at = slot;
+        uint16_t* tile = lds[at];
         slot = slot + 1 == TILES ? 0 : slot + 1;
         uint16_t* ahead = lds[slot];
         if constexpr (AHEAD) {
-            if (it + 1 < last) store(ahead);
-        } else store(tile);
+            if (it + 1 < last) store(slot);
+        } else store(at);
         __syncthreads();
         fetch(it + (AHEAD ? 2 : 1));
         if (!live) continue;
         if constexpr (!AHEAD) {
             scores(tile);
-            find_top(it);
+            find_top(it, at);
         }
         if (__any(top - ref > kLift + kSlack)) {
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float to = fmaxf(ref, top - kLift), by = exp2f(ref - to);
+            const float to = top - ref > kLift + kSlack ? top - kLift : ref, by = exp2f(ref - to);     // (of this row alone)
             ref = to;
             sum *= by;
             if constexpr (MEAN)
@@ -1122,8 +1191,8 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
                     const bool mine = lane >> 5 == (c >> 2 & 1) && rows >> (lane & 31) & 1;
                     each<MY>([&](auto m) {
                         if (b != m()) return;
-                        const float z = score[m()][i], p = __builtin_amdgcn_exp2f(fmaf(z, to_log2, -ref));
-                        if (mine) sum += p;
+                        const float z = score[m()][i], p = power(z);
+                        if (mine) sum += kKind == 0 ? p * scales[at].inverse[c] : p;
                         score[m()][i] = mine ? -__builtin_inff() : z;
                     });
                 });
@@ -1132,25 +1201,34 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
 #pragma unroll
             for (int m = 0; m < MY; ++m) now[m] = score[m];
             float some[2] = {};                         // (behind the last tile the scores are of no use, and unused)
+            f32x4 back[MEAN ? 1 : MY] = {};             // (of a block at a time where products follow, of all in turn otherwise)
             advance<DP, NB, MY, MEAN, false>(ahead, tile, 0, lane, held, score, acc, [&](int m, int i) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(now[m][i], to_log2, -ref));
-                some[i & 1] += p;
+                const float p = power(now[m][i]);
+                if constexpr (kKind == 0) {     // p of p s
+                    f32x4& b = back[MEAN ? 0 : m];
+                    if (i % 4 == 0) b = *reinterpret_cast<const f32x4*>(&scales[at].inverse[m * kBlock + row_of(i, lane)]);
+                    some[i & 1] = fmaf(p, b[i % 4], some[i & 1]);
+                } else some[i & 1] += p;
                 return p;
             }, [&](int m, u32x4 (&q)[2][NS]) {
                 if constexpr (CROWDED) leave_out(out >> 16 * m, q);
             });
             sum += some[0] + some[1];
-            find_top(it + 1);
+            find_top(it + 1, slot);
             continue;
         }
 #pragma unroll
         for (int m = 0; m < MY; ++m) {
             float p[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(score[m][i], to_log2, -ref));
-            float s4[4];
+            for (int i = 0; i < 16; ++i) p[i] = power(score[m][i]);
+            f32x4 s4 = {};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s4[i] = (p[i] + p[i + 4]) + (p[i + 8] + p[i + 12]);
+            for (int i = 0; i < 16; i += 4) {
+                f32x4 four{p[i], p[i + 1], p[i + 2], p[i + 3]};
+                if constexpr (kKind == 0) four *= *reinterpret_cast<const f32x4*>(&scales[at].inverse[(y * MY + m) * kBlock + row_of(i, lane)]);
+                s4 += four;
+            }
             sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
             if constexpr (MEAN) {
                 u32x4 b[2][NS];
@@ -1169,20 +1247,21 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
     }
     if (!live) return;
     sum += __shfl_xor(sum, 32);
-    const int64_t at = (int64_t)(part * WY + y) * padded + row;
+    const int64_t place_of = (int64_t)(part * WY + y) * padded + row;
     if (lane < 32) {                                    // a row's slices lie together
         const int64_t stat = row * a.cut.slices() + part * WY + y;
         a.at<float>(a.plan.top)[stat] = ref;
         a.at<float>(a.plan.sum)[stat] = sum;
     }
     if constexpr (MEAN) {
-        float* out = a.at<float>(a.plan.mean_parts) + at * DP + 4 * (lane >> 5);
+        float* out = a.at<float>(a.plan.mean_parts) + place_of * DP + 4 * (lane >> 5);
+        const float back = kKind == 0 ? 0x1p-15f : 1.0f;
 #pragma unroll
         for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 *reinterpret_cast<f32x4*>(out + 32 * db + 8 * i) =
-                    f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]};
+                    f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]} * back;
     }
 }
 
@@ -1206,7 +1285,6 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
     if constexpr (LOSS)
 #pragma unroll 4
         for (int p = threadIdx.x; p < slices; p += kClassThreads) top = fmaxf(top, tops[p]);
-    const float table = LOSS && ROWS ? table_unit(a, room) : 1.0f;
     int id = -1;
     float q = 0.0f, log_weight = 0.0f;                  // of lane's slot, in wave 0
     if (wave == 0) {
@@ -1268,7 +1346,11 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
             for (int d = 1; d < 64; d *= 2) loss += __shfl_xor(loss, d);
             if (lane == 0) {
                 a.loss[t] = loss; a.lse[t] = lse;
-                if (!ROWS && a.row_grad) a.at<float>(a.plan.norm)[t] = log2_sum - kLift;
+                // where means are made in a launch of their own: what they are relative to, for fp32 the reference of p s
+                if (!ROWS && a.row_grad) {
+                    a.at<float>(a.plan.norm)[t] = (kKind == 0 ? top : log2_sum) - kLift;
+                    a.at<float>(a.plan.back)[t] = kKind == 0 ? 1.0f / sum : 1.0f;
+                }
             }
             if (ROWS || a.row_grad) {
                 const float pull = merge_slots(a, id, q) ? probability(z, lse) - q : 0.0f;
@@ -1280,7 +1362,7 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
     }
     if constexpr (ROWS) {
         const float* parts = a.at<const float>(a.plan.mean_parts);
-        const float back = 1.0f / sum / table;
+        const float back = LOSS ? 1.0f / sum : a.at<const float>(a.plan.back)[t];
         for (int c0 = 0; c0 < a.s.D; c0 += 4 * lanes) {
             const int c = c0 + 4 * l;
             f32x4 e = {};
@@ -1318,25 +1400,30 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
 // or in parts that a second launch joins where there are fewer classes than waves.
 // 4096 x 2.5 M x 128 bfloat16: 5.4 ms, 0.97 PFLOP/s; what slots add costs by the slot (4096 x 169,343, 32 slots a row: 0.55
 // ms, where the classes alone would take 0.37 at that rate).
+// P = 2^(score * by + start), P s for fp32 rows: at most 2^15 there, which a row of enormous scores, whose log-sum-exp is rounded,
+// would exceed.
+template <bool BOUNDED> __device__ __forceinline__ float power_of(float score, float by, float start) {
+    const float e = fmaf(score, by, start);
+    return __builtin_amdgcn_exp2f(BOUNDED && e > 15.0f ? 15.0f : e);    // (NaN stays)
+}
 template <int DP, int WY>
 __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) void class_gradient_kernel(ClassArgs a, int64_t padded) {
     constexpr int NB = blocks_per_tile(WY, DP, kKind), MY = NB / WY, WX = kClassWaves / WY;
     using T = Tile<DP, NB * kBlock>;
     __shared__ __align__(16) uint16_t lds[2][NS * T::kPlane];
-    __shared__ __align__(16) float starts[2][NB * kBlock];
+    __shared__ __align__(16) float starts[2][NB * kBlock], scales[2][kKind == 0 ? NB * kBlock : 1];
     __shared__ float cells[kClassWaves][MY][kBlock * kBlock];
     __shared__ float room[kClassWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, x = wave % WX, y = wave / WX;
     const ClassCut::Place place = a.cut.place(blockIdx.x);
     const int part = place.part, group = place.group, first = place.first, last = place.last;
-    const Units u = row_units(a, room);
+    const float unit = grad_unit(a, room);
     const int64_t v0 = ((int64_t)group * WX + x) * kBlock, v = v0 + (lane & 31);
     const bool live = v0 < a.s.V;                       // wave-uniform
 
     u32x4 held[DP / 16][NS];
-    const float to_log2 = not_zero(a.scale * kLog2e / u.h /
-        hold<DP / 16>(static_cast<const Elem*>(a.w) + (v < a.s.V ? v : a.s.V - 1) * a.w_stride, a.s.D, 0, lane, true, held,
-                      [](float peak) { return wave_max(peak); }));
+    const float to_log2 = not_zero(a.scale * kLog2e /
+        hold<DP / 16>(static_cast<const Elem*>(a.w) + (v < a.s.V ? v : a.s.V - 1) * a.w_stride, a.s.D, 0, lane, held, both_halves));
     f32x16 acc[DP / 32];
 #pragma unroll
     for (auto& f : acc) f = f32x16{};
@@ -1345,16 +1432,22 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
 
     const float* start = a.at<const float>(a.plan.start);
     typename T::FromPlanes next;
-    float next_start = 0.0f;
+    float next_start = 0.0f, next_scale = 1.0f;
     SlotFeed<MY> feed(a, padded, v0);
     auto fetch = [&](int it) {
         if (it >= last) return;
         next.load(a.ws + a.plan.rows, 2 * DP, padded * 2 * DP, padded, (int64_t)it * NB * kBlock);   // (padded to whole tiles)
-        if (threadIdx.x < NB * kBlock) next_start = start[(int64_t)it * NB * kBlock + threadIdx.x];
+        if (threadIdx.x < NB * kBlock) {
+            next_start = start[(int64_t)it * NB * kBlock + threadIdx.x];
+            if constexpr (kKind == 0) next_scale = a.at<const float>(a.plan.scales)[(int64_t)it * NB * kBlock + threadIdx.x];
+        }
     };
     auto store = [&](int slot) {
         next.store(lds[slot]);
-        if (threadIdx.x < NB * kBlock) starts[slot][threadIdx.x] = next_start;
+        if (threadIdx.x < NB * kBlock) {
+            starts[slot][threadIdx.x] = next_start;
+            if constexpr (kKind == 0) scales[slot][threadIdx.x] = next_scale;
+        }
     };
     auto product = [&](const uint16_t* tile, int b, const u32x4 (&q)[2][NS]) {
 #pragma unroll
@@ -1441,10 +1534,14 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
         if (!live) continue;
         const int64_t block0 = (int64_t)it * NB + y * MY;          // of rows
         f32x16 score[MY];
-        f32x4 s = {};
+        f32x4 s = {}, by = {};
         advance<DP, NB, MY, true, true>(tile, tile, y * MY, lane, held, score, acc, [&](int m, int i) {
-            if (i % 4 == 0) s = *reinterpret_cast<const f32x4*>(&starts[at][(y * MY + m) * kBlock + 2 * i + 4 * (lane >> 5)]);
-            return __builtin_amdgcn_exp2f(fmaf(score[m][i], to_log2, s[i % 4]));
+            const int r = (y * MY + m) * kBlock + row_of(i, lane);
+            if (i % 4 == 0) {
+                s = *reinterpret_cast<const f32x4*>(&starts[at][r]);
+                if constexpr (kKind == 0) by = *reinterpret_cast<const f32x4*>(&scales[at][r]) * to_log2;
+            }
+            return power_of<kKind == 0>(score[m][i], kKind == 0 ? by[i % 4] : to_log2, s[i % 4]);
         }, [&](int m, u32x4 (&q)[2][NS]) {
             if (feed.now[m].negative()) sign(block0 + m, q);
             if (hit[m]) leave_out(named[m], q);
@@ -1455,7 +1552,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 && WY < 4 ? 2 : 1) vo
         if (it + 1 < last) gather(block0 + NB);         // what was asked for has come by now
     }
     if (!live) return;
-    const float back = a.scale / u.h / u.g;
+    const float back = a.scale / unit;
     if (a.cut.slices() > 1) {
         const int64_t rows = ceil_div(a.s.V, kBlock) * kBlock;
         float* out = a.at<float>(a.plan.grad_parts) + ((int64_t)(part * WY + y) * rows + v) * DP + 4 * (lane >> 5);
@@ -1554,26 +1651,24 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
     const ClassCut::Place place = a.cut.place(blockIdx.x);
     const int part = place.part, group = place.group, first = place.first, last = place.last;
     float* room = reinterpret_cast<float*>(partial);
-    const Units u = MODE == kGradient ? row_units(a, room) : Units{1.0f, 1.0f};
-    const float table = MODE == kGradient ? 1.0f : table_unit(a, room);
+    const float unit = MODE == kGradient ? grad_unit(a, room) : 1.0f;
     const int64_t x0 = (int64_t)group * kBlock, x = x0 + (lane & 31);
     const Elem* w = static_cast<const Elem*>(a.w);
     const uint16_t* planes = a.at<const uint16_t>(a.plan.rows);
     uint16_t* lds = quarters[wave];
 
     u32x4 held[Q / 16][NS];
-    auto join = [&](float peak) {                       // one unit for the four quarters
-        peak = wave_max(peak);
-        if (lane == 0) room[wave] = peak;
+    auto join = [&](float peak) {                       // of a row that four waves hold
+        peak = both_halves(peak);
+        if (lane < kBlock) room[wave * kBlock + lane] = peak;
         __syncthreads();
-        peak = fmaxf(fmaxf(room[0], room[1]), fmaxf(room[2], room[3]));
+#pragma unroll
+        for (int i = 0; i < kClassWaves; ++i) peak = fmaxf(peak, room[i * kBlock + (lane & 31)]);
         __syncthreads();
         return peak;
     };
-    const float held_unit = MODE == kGradient
-        ? hold<Q / 16>(w + (x < a.s.V ? x : a.s.V - 1) * a.w_stride, a.s.D, col0, lane, true, held, join)
-        : hold_rows<Q / 16>(a, x, col0, lane, held, join);
-    const float to_log2 = not_zero(a.scale * kLog2e / u.h / held_unit / table);
+    const Elem* own = MODE == kGradient ? w + (x < a.s.V ? x : a.s.V - 1) * a.w_stride : held_row(a, x);
+    const float to_log2 = not_zero(a.scale * kLog2e / hold<Q / 16>(own, a.s.D, col0, lane, held, join));
     if constexpr (MODE == kGradient) {
         for (int i = threadIdx.x; i < kBlock * kBlock; i += kClassThreads) cells[i] = 0.0f;
         if (threadIdx.x == 0) hit = -1;
@@ -1585,13 +1680,14 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
         else return 0;
     }();
     const float norm = MODE == kMean && x < a.s.T ? a.at<const float>(a.plan.norm)[x] : __builtin_inff();
-    float ref = -1e30f, sum = 0.0f;
+    float ref = -3e38f, sum = 0.0f;
     f32x16 acc[MODE == kStats ? 1 : Q / 32];
 #pragma unroll
     for (auto& f : acc) f = f32x16{};
 
     // the next tile's quarter: rows of the table as they are, or planes
     constexpr bool FROM_PLANES = MODE == kGradient || STRAIGHT;
+    static_assert(kKind != 0 || FROM_PLANES, "fp32 tables are laid out first: a wave has no row whole, to make its unit of");
     struct { Eight e[FROM_PLANES ? 1 : S::kEach]; u32x4 p[FROM_PLANES ? NS : 1][FROM_PLANES ? S::kEach : 1]; } next;
     const bool as_is = MODE != kGradient && !a.plan.packed;
     const uint16_t* streamed = MODE == kGradient ? planes : as_is ? reinterpret_cast<const uint16_t*>(w) : a.at<const uint16_t>(a.plan.table);
@@ -1599,7 +1695,8 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
     const int lane_place = as_is ? S::row(0, lane) * (int)a.w_stride + S::chunk(0, lane) * 8 : lane * 8;
     const int step_row = as_is ? 16 * (int)a.w_stride : 512, step_chunk = as_is ? 32 : 1024;
     SlotFeed<1> feed(a, padded, MODE == kGradient ? x0 : 0);
-    f32x4 next_start = {};
+    f32x4 next_start = {}, next_scale = {};
+    const float* scales = kKind == 0 ? a.at<const float>(MODE == kGradient ? a.plan.scales : a.plan.table_scales) : nullptr;
     auto fetch = [&](int it) {
         if constexpr (MODE == kGradient)
             if (wave == 0) {                            // one wave looks after the slots of the workgroup's classes
@@ -1625,6 +1722,7 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
         }
         if constexpr (MODE == kGradient)
             next_start = *reinterpret_cast<const f32x4*>(a.at<const float>(a.plan.start) + (int64_t)it * kBlock + 8 * wave + 4 * (lane >> 5));
+        if constexpr (kKind == 0) next_scale = *reinterpret_cast<const f32x4*>(scales + (int64_t)it * kBlock + 8 * wave + 4 * (lane >> 5));
     };
     if (first < last) {
         if (MODE == kGradient && wave == 0) feed.ask_words(first);
@@ -1639,11 +1737,11 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
             if constexpr (FROM_PLANES) {
 #pragma unroll
                 for (int n = 0; n < NS; ++n) p[n] = next.p[n][i];
-            } else planes_of(next.e[i], table, p);
+            } else planes_of(next.e[i], 1.0f, p);
 #pragma unroll
             for (int n = 0; n < NS; ++n) *reinterpret_cast<u32x4*>(lds + n * S::kPlane + S::place(r, c)) = p[n];
         }
-        const f32x4 start = next_start;
+        const f32x4 start = next_start, scale = next_scale;
         __builtin_amdgcn_wave_barrier();
         if (it + 1 < last) fetch(it + 1);
         f32x16 score = {};
@@ -1658,29 +1756,39 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
         __syncthreads();
         f32x4 z = (meet[0][wave][lane] + meet[1][wave][lane]) + (meet[2][wave][lane] + meet[3][wave][lane]);   // rows 8*wave + 4*(lane/32) + j
         const int y = 8 * wave + 4 * (lane >> 5);
+        f32x4 back = {1.0f, 1.0f, 1.0f, 1.0f};          // p of p s
+        if constexpr (kKind == 0 && MODE != kGradient) {        // to binary logarithms of p s 2^15, as in the narrow kernel
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float s = scale[j];
+                z[j] = fmaf(z[j], s * to_log2, log_scale(s));
+                back[j] = 0x1p-15f / s;
+            }
+        }
         if (MODE != kGradient && y0 + kBlock > a.s.V) {
             asm volatile("");
 #pragma unroll
             for (int j = 0; j < 4; ++j) if (y0 + y + j >= a.s.V) z[j] = -__builtin_inff();
         }
         if constexpr (MODE == kStats) {
-            z *= to_log2;
+            if constexpr (kKind != 0) z *= to_log2;
             const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
-            if (__any(top > ref + 8.0f)) {
-                const float to = fmaxf(ref, top);
+            constexpr float slack = kKind == 0 ? kSlack : 8.0f;    // (fp32: what the mean's P is relative to)
+            if (__any(top > ref + slack)) {
+                const float to = top > ref + slack ? top : ref;
                 sum *= exp2f(ref - to);
                 ref = to;
             }
             float e[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(z[j] - ref);
+            for (int j = 0; j < 4; ++j) e[j] = __builtin_amdgcn_exp2f(z[j] - ref) * back[j];
             sum += (e[0] + e[1]) + (e[2] + e[3]);
             if constexpr (MEETS == 1) __syncthreads();
         } else {
             float p[4];
             if constexpr (MODE == kMean) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(z[j], to_log2, -norm));
+                for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(kKind == 0 ? z[j] - norm : fmaf(z[j], to_log2, -norm));
                 if (named.next == (uint32_t)it)
                     named.take(it, lane, [&](uint32_t rows, int c) {
                         const bool mine = c >> 3 == wave && lane >> 5 == (c >> 2 & 1) && rows >> (lane & 31) & 1;
@@ -1689,7 +1797,7 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
                     });
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(fmaf(z[j], to_log2, start[j]));
+                for (int j = 0; j < 4; ++j) p[j] = power_of<kKind == 0>(z[j], kKind == 0 ? scale[j] * to_log2 : to_log2, start[j]);
                 const uint32_t signs = a.at<const uint32_t>(a.plan.signs)[it];
                 if (signs) {
 #pragma unroll
@@ -1740,7 +1848,7 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
             a.at<float>(a.plan.sum)[at] = sum;
         }
     } else {
-        const float back = MODE == kGradient ? a.scale / u.h / u.g : exp2f(-kLift) / table;
+        const float back = MODE == kGradient ? a.scale / unit : exp2f(kKind == 0 ? -kLift - 15.0f : -kLift);
         const int64_t rows = MODE == kGradient ? ceil_div(a.s.V, kBlock) * kBlock : padded;
         const bool joined = MODE == kMean || a.cut.parts > 1;
         float* out = a.at<float>(MODE == kGradient ? a.plan.grad_parts : a.plan.mean_parts);
@@ -1800,8 +1908,8 @@ template <int DP, bool MEAN> void launch_forward(const ClassArgs& a, int64_t pad
     const unsigned grid = (unsigned)(a.cut.groups * a.cut.parts);
     const bool straight = a.plan.packed || a.plan.straight;
     if constexpr (!narrow_depth(DP)) {
-        if (straight) class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats, true><<<grid, kClassThreads, 0, stream>>>(a, padded);
-        else class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
+        if (straight || kKind == 0) class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats, true><<<grid, kClassThreads, 0, stream>>>(a, padded);
+        else if constexpr (kKind != 0) class_wide_kernel<DP / kClassWaves, MEAN ? kMean : kStats, false><<<grid, kClassThreads, 0, stream>>>(a, padded);
     } else {
         const bool crowded = MEAN && crowded_tiles(a.s);
         auto run = [&](auto wy) {
@@ -1834,7 +1942,6 @@ hipError_t forward(ClassArgs a, hipStream_t stream) {
             mean ? launch_forward<dp(), true>(a, padded, stream) : launch_forward<dp(), false>(a, padded, stream);
         });
     };
-    if constexpr (kKind == 0) class_peaks_kernel<<<kPeaksTable, kClassThreads, 0, stream>>>(a, kPeaksTable, 0, 0);
     if (a.plan.packed) {
         const int64_t table = padded_rows(a.s.V), grid = ceil_div(table * depth / 8, kClassThreads);
         if (hipError_t e = with_depth(depth, [&](auto dp) {
@@ -1862,10 +1969,7 @@ hipError_t gradient(ClassArgs a, hipStream_t stream) {
     }
     a.cut = gradient_cut(a.s);
     a.buckets = buckets_of(a.s.V, a.s.K);
-    if constexpr (kHalf) {
-        const int rows = kKind == 0 ? kPeaksRows : 0;
-        class_peaks_kernel<<<rows + kPeaksGrad, kClassThreads, 0, stream>>>(a, 0, rows, kPeaksGrad);
-    }
+    if constexpr (kHalf) class_peaks_kernel<<<kPeaks, kClassThreads, 0, stream>>>(a);
     if (a.plan.row_slots && a.s.T) class_slots_kernel<<<(unsigned)a.s.T, kClassThreads, 0, stream>>>(a, row_lanes(a.s.D));
     if (hipError_t e = with_depth(depth, [&](auto dp) {
             if (padded) class_rows_kernel<dp()><<<padded / kBlock, kRowThreads, 0, stream>>>(a, padded);
