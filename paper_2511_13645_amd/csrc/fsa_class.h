@@ -104,6 +104,14 @@ constexpr int kWaveSlots = 2;                           // slots a row that a wa
 // Whether 64 classes have more than 8 slots of 32 rows, on an average: for the forward with row gradients, which then reads the
 // (small) table as it is.
 constexpr bool crowded_tiles(const ClassShape& s) { return s.K > kWaveSlots && (int64_t)s.K * kBlock * 64 > 8 * s.V; }
+// Whether workgroups of that forward look all their rows' slots through for every tile, or read them from a list that a launch
+// ahead sorts.  2 to 6 us a tile against 10 to 21 of the launch: 51 rows x 9896 x 144 bfloat16, 62 slots, 22.4 us against 16.1 and
+// 17.8; 1024 x 47 x 100 fp32, 10 slots, 18.9 against 19.4 and 9.5.
+inline bool looks_through(const ClassShape& s) {
+    const ClassCut c = forward_cut(s);
+    return (!narrow_depth(class_depth(s.D)) || crowded_tiles(s)) && c.tiles <= 4 * c.parts;
+}
+
 // Whether the gradient scores the slots of a row in a launch of its own, a workgroup a row, or where it sorts them, a wave to two
 // rows.  One slot: sorting takes 4 us longer for it (1024 rows x 128: 7.5 to 11.2), as much as a launch.  1024 rows x 47 x 100 fp32,
 // 10 slots: 23.6 us together, 12.0 and 8.9 apart; 257 rows x 602, 50 slots: 250 us together.
@@ -147,7 +155,7 @@ inline ClassPlan plan_of(const ClassShape& s, bool straight, bool forward, bool 
         if (want_rows && !narrow) p.norm = room(T * 4);
         if (want_rows && !narrow) p.back = room(T * 4);
         if (want_rows && !narrow) p.pulls = room(T * s.K * 4);
-        if (want_rows && s.K > kWaveSlots) {
+        if (want_rows && s.K > kWaveSlots && !looks_through(s)) {
             p.named = room(T * s.K * 4);
             p.named_starts = room(T / kBlock * (forward_cut(s).parts + 1) * 4);
         }

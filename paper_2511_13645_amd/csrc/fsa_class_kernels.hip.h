@@ -444,12 +444,12 @@ __device__ __forceinline__ Slot row_slot(const ClassArgs& a, int id, float q, fl
     return Slot{some ? (uint32_t)id : ~0u, g * (q - p)};
 }
 
-// Rows of more than one slot, ahead of the sorting: one workgroup per row, a quarter of its slots to a wave.  Bound by the reads of
+// Rows of more than one slot, ahead of the sorting: one workgroup per row, as many slots to a wave as it scores at a time.  Bound by the reads of
 // the classes' rows: 4096 rows of 32 slots, 128 bfloat16 (33 MB of rows) 28 us.
-__global__ __launch_bounds__(kClassThreads) void class_slots_kernel(ClassArgs a, int lanes) {
+__global__ __launch_bounds__(kRowThreads) void class_slots_kernel(ClassArgs a, int lanes) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t t = blockIdx.x;
-    const int each = (a.s.K + kClassWaves - 1) / kClassWaves, from = wave * each, to = from + each < a.s.K ? from + each : a.s.K;
+    const int each = 4 * (64 / lanes), from = wave * each, to = from + each < a.s.K ? from + each : a.s.K;
     int id;
     float log_weight;
     const float weight = slot_weight(a, t, lane, id, log_weight);
@@ -905,7 +905,7 @@ __device__ __forceinline__ void advance(const uint16_t* ahead, const uint16_t* t
 // asks for the next tile that has one with one comparison of scalars: looking at every tile's slots, or masking P between the
 // products, took the loop's registers and up to half of its speed.
 // Up to two slots a row lie in a register of the wave; more of them in a list for every 32 rows in the order of the classes, class *
-// 32 + row, that a launch ahead sorts.  Latency alone, 10 us (10 slots a row) to 21 (64).
+// 32 + row, that a launch ahead sorts, but for workgroups of few tiles, which look all of them through.  Latency alone, 10 us (10 slots a row) to 21 (64).
 __global__ __launch_bounds__(kRowThreads) void class_named_kernel(ClassArgs a, int classes) {
     __shared__ uint32_t keys[kBlock * 64];
     __shared__ int count;
@@ -922,7 +922,9 @@ __global__ __launch_bounds__(kRowThreads) void class_named_kernel(ClassArgs a, i
     }
     for (int run = 2; run <= size; run *= 2)            // bitonic: runs of this length in turns up and down
         for (int d = run / 2; d > 0; d /= 2) {
-            __syncthreads();
+            // (pairs up to 64 apart stay within the 128 keys of a wave)
+            if (d >= 64 || run == 2) __syncthreads();
+            else __builtin_amdgcn_wave_barrier();
             const int i = threadIdx.x / d * 2 * d + threadIdx.x % d;
             if (i < size) {
                 const uint32_t x = keys[i], y = keys[i + d];
@@ -973,6 +975,10 @@ template <int CLASSES> struct Named {
             at = __builtin_amdgcn_readfirstlane(starts[0]);
             end = __builtin_amdgcn_readfirstlane(starts[1]);
             load(lane);
+        } else if (a.s.K > kWaveSlots) {
+            list = nullptr;
+            next = first;
+            return;
         } else {
             list = nullptr;
             const int64_t t = block * kBlock + (lane & 31);
@@ -982,7 +988,18 @@ template <int CLASSES> struct Named {
         look(first);
     }
     // f(whether a lane has one, its row and class of the tile) for up to 64 of tile `it`, the next, at a time.
-    template <class F> __device__ __forceinline__ void take_many(int it, int lane, F f) {
+    template <class F> __device__ __forceinline__ void take_many(const ClassArgs& a, int64_t block, int it, int lane, F f) {
+        if (!list) {                                    // few tiles: every slot is looked at for each
+            const int64_t rows = a.s.T - block * kBlock;
+            const int n = (int)(rows < kBlock ? rows : kBlock) * a.s.K;
+#pragma unroll 4
+            for (int e = lane; e < n; e += 64) {
+                const int id = a.ids[block * most + e];
+                f(id >= 0 && id < a.s.V && id / CLASSES == it, e / a.s.K, id % CLASSES);
+            }
+            next = it + 1;
+            return;
+        }
         do {
             const int now = __builtin_amdgcn_readfirstlane(at), i = (now & ~63) + lane;
             const bool has = (keys >> 5) / CLASSES == (uint32_t)it && i >= now && i < end;
@@ -1174,7 +1191,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
         uint32_t out = 0;                               // bit 16 m + i: register i of block m is named
         if constexpr (CROWDED) {
             if (named.next == (uint32_t)it) {
-                named.take_many(it, lane, [&](bool has, int r, int c) {
+                named.take_many(a, row0 / kBlock, it, lane, [&](bool has, int r, int c) {
                     const int b = c / kBlock - y * MY;
                     if (has && b >= 0 && b < MY)
                         atomicOr(&places[wave][r + 32 * (c >> 2 & 1)], 1u << (16 * b + 4 * (c % kBlock >> 3) + (c & 3)));
@@ -1646,6 +1663,7 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
     constexpr int PS = MODE == kStats ? 1 : MODE == kGradient ? 2 : NS;   // planes of P; 16-bit types use the second after a hit
     __shared__ __align__(16) u32x2 shared_p[PS][2][64][2];
     __shared__ int hit;                                 // the tile that last had a slot of these classes
+    __shared__ uint32_t places[MODE == kMean ? kClassWaves : 1][64];
     __shared__ float cells[MODE == kGradient ? kBlock * kBlock : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col0 = wave * Q;
     const ClassCut::Place place = a.cut.place(blockIdx.x);
@@ -1674,6 +1692,7 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
         if (threadIdx.x == 0) hit = -1;
         __syncthreads();
     }
+    if constexpr (MODE == kMean) places[wave][lane] = 0;
     using Places = Named<kBlock>;
     typename std::conditional<MODE == kMean, Places, int>::type named = [&] {
         if constexpr (MODE == kMean) return Places(a, group, part, first, last, lane);
@@ -1789,7 +1808,17 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
             if constexpr (MODE == kMean) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(kKind == 0 ? z[j] - norm : fmaf(z[j], to_log2, -norm));
-                if (named.next == (uint32_t)it)
+                if (named.next == (uint32_t)it && a.s.K > kWaveSlots) {
+                    named.take_many(a, group, it, lane, [&](bool has, int r, int c) {
+                        if (has && c >> 3 == wave) atomicOr(&places[wave][r + 32 * (c >> 2 & 1)], 1u << (c & 3));
+                    });
+                    __builtin_amdgcn_wave_barrier();
+                    const uint32_t mine = places[wave][lane];
+                    places[wave][lane] = 0;
+                    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) if (mine >> j & 1) p[j] = 0.0f;
+                } else if (named.next == (uint32_t)it)
                     named.take(it, lane, [&](uint32_t rows, int c) {
                         const bool mine = c >> 3 == wave && lane >> 5 == (c >> 2 & 1) && rows >> (lane & 31) & 1;
 #pragma unroll
@@ -1970,7 +1999,10 @@ hipError_t gradient(ClassArgs a, hipStream_t stream) {
     a.cut = gradient_cut(a.s);
     a.buckets = buckets_of(a.s.V, a.s.K);
     if constexpr (kHalf) class_peaks_kernel<<<kPeaks, kClassThreads, 0, stream>>>(a);
-    if (a.plan.row_slots && a.s.T) class_slots_kernel<<<(unsigned)a.s.T, kClassThreads, 0, stream>>>(a, row_lanes(a.s.D));
+    if (a.plan.row_slots && a.s.T) {
+        const int lanes = row_lanes(a.s.D);
+        class_slots_kernel<<<(unsigned)a.s.T, 64 * (unsigned)ceil_div(a.s.K, 4 * (64 / lanes)), 0, stream>>>(a, lanes);
+    }
     if (hipError_t e = with_depth(depth, [&](auto dp) {
             if (padded) class_rows_kernel<dp()><<<padded / kBlock, kRowThreads, 0, stream>>>(a, padded);
         })) return e;
