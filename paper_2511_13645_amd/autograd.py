@@ -133,7 +133,9 @@ class _ClassLoss(torch.autograd.Function):
 def _class_loss(h, w, ids, logits, temperature, scale):
     loss = binding.class_loss(h, w, ids, logits, temperature, scale)
     if loss is None:
-        loss = _ClassLoss.apply(h, w, ids, logits, temperature, scale, h.requires_grad and torch.is_grad_enabled())
+        # with a gradient of w alone as well: the log-sum-exp that its backward takes is then as exact as both gradients need it
+        train = (h.requires_grad or w.requires_grad) and torch.is_grad_enabled()
+        loss = _ClassLoss.apply(h, w, ids, logits, temperature, scale, train)
     return loss
 
 

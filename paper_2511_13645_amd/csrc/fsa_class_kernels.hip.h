@@ -61,8 +61,9 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 constexpr int kKind = FSA_CLASS_KIND;                   // 0 fp32, 1 bfloat16, 2 fp16
 constexpr int NS = class_planes(kKind);
 constexpr bool kHalf = kKind != 1;                      // planes hold fp16 (bfloat16 otherwise)
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
-// fp16 probabilities are kept as p * 2^14: 22 binades below the largest stay normal numbers.
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr double kLog2eDouble = 1.44269504088896340736;
+// fp16 probabilities are kept as p * 2^14: 28 binades below the largest stay normal numbers.
 constexpr float kLift = kHalf ? 14.0f : 0.0f;
 // The running reference of a row follows its maximum only when that is passed by this many binades, so that most tiles
 // leave the accumulators alone; 2^(14+1) is in range of fp16, bfloat16 has room.
@@ -360,9 +361,13 @@ __global__ __launch_bounds__(kClassThreads) void class_row_grad_kernel(ClassArgs
     write_row_grad(a, t, a.grad_loss[t], __any(id >= 0), lane);
 }
 
-__device__ __forceinline__ float probability(float score, float lse) {
-    const float p = exp2f((score - lse) * kLog2e);
+// Scores of slots' classes are sums in 64 bits, few as they are: in fp32 the rounding of a score near 20 would be 1e-6 of p.
+__device__ __forceinline__ float probability(double score, double lse) {
+    const float p = exp2f((float)((score - lse) * kLog2eDouble));
     return p > 1.0f ? 1.0f : p;                         // (NaN stays)
+}
+__device__ __forceinline__ double dot4(f32x4 x, f32x4 y) {
+    return ((double)x[0] * y[0] + (double)x[1] * y[1]) + ((double)x[2] * y[2] + (double)x[3] * y[3]);
 }
 // A class that several slots of a row name is the first one's, with the weights in slot order; false for the others, and for
 // slots that name no class of the table.  IDs and weights in lanes 0..K-1.
@@ -378,16 +383,16 @@ __device__ __forceinline__ bool merge_slots(const ClassArgs& a, int id, float& q
     }
     return first;
 }
-// p of the classes that lanes [from, to) name for row t (an ID behind the last class: 0), by the fp32 dot product of the elements
+// p of the classes that lanes [from, to) name for row t (an ID behind the last class: 0), by the dot product of the elements
 // themselves; `lanes` of the wave to a class, four classes to a group of them at a time.
 __device__ __forceinline__ float slot_probability(const ClassArgs& a, int64_t t, int id, int lane, int lanes, int from, int to) {
     const Elem *h = static_cast<const Elem*>(a.h) + t * a.h_stride, *w = static_cast<const Elem*>(a.w);
     const int groups = 64 / lanes, group = lane / lanes, l = lane % lanes;
     const bool known = id >= 0 && id < a.s.V;
-    float z = 0.0f;
+    double z = 0.0;
     for (int j = from; j < to; j += 4 * groups) {
         const Elem* row[4];
-        float dot[4] = {};
+        double dot[4] = {};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int k = j + i * groups + group, of = __shfl(known ? id : -1, k & 63);
@@ -399,13 +404,13 @@ __device__ __forceinline__ float slot_probability(const ClassArgs& a, int64_t t,
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[i] = row[i] ? load4(row[i], a.s.D, c) : f32x4{};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) dot[i] += (x[0] * y[i][0] + x[1] * y[i][1]) + (x[2] * y[i][2] + x[3] * y[i][3]);
+            for (int i = 0; i < 4; ++i) dot[i] += dot4(x, y[i]);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             for (int d = 1; d < lanes; d *= 2) dot[i] += __shfl_xor(dot[i], d);
             const int k = j + i * groups;
-            const float mine = __shfl(dot[i], (lane - k) * lanes & 63);
+            const double mine = __shfl(dot[i], (lane - k) * lanes & 63);
             if (lane >= k && lane < k + groups) z = mine;
         }
     }
@@ -414,7 +419,7 @@ __device__ __forceinline__ float slot_probability(const ClassArgs& a, int64_t t,
 // The same of rows [t, t + N) of one slot each, the whole wave to a class, all rows at a time.
 template <int N> __device__ __forceinline__ void target_probability(const ClassArgs& a, int64_t t, int lane, float (&p)[N]) {
     const Elem *h[N], *w[N];
-    float dot[N] = {};
+    double dot[N] = {};
 #pragma unroll
     for (int k = 0; k < N; ++k) {
         const int id = t + k < a.s.T ? a.ids[t + k] : -1;
@@ -426,7 +431,7 @@ template <int N> __device__ __forceinline__ void target_probability(const ClassA
 #pragma unroll
         for (int k = 0; k < N; ++k) if (w[k]) { x[k] = load4(h[k], a.s.D, c); y[k] = load4(w[k], a.s.D, c); }
 #pragma unroll
-        for (int k = 0; k < N; ++k) dot[k] += (x[k][0] * y[k][0] + x[k][1] * y[k][1]) + (x[k][2] * y[k][2] + x[k][3] * y[k][3]);
+        for (int k = 0; k < N; ++k) dot[k] += dot4(x[k], y[k]);
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2)
@@ -901,7 +906,7 @@ __device__ __forceinline__ void advance(const uint16_t* ahead, const uint16_t* t
 // ---------------------------------------------------------------------------------------------------------------
 // classes that the held rows' slots name, for the forward
 // ---------------------------------------------------------------------------------------------------------------
-// Their places are left out of the sum of p w, which rounds p (theirs are added with p - q when the parts are joined).  A wave
+// Their places are left out of the sums of p and of p w (theirs are added when the parts are joined).  A wave
 // asks for the next tile that has one with one comparison of scalars: looking at every tile's slots, or masking P between the
 // products, took the loop's registers and up to half of its speed.
 // Up to two slots a row lie in a register of the wave; more of them in a list for every 32 rows in the order of the classes, class *
@@ -969,6 +974,11 @@ template <int CLASSES> struct Named {
     }
     __device__ __forceinline__ Named(const ClassArgs& a, int64_t block, int part, int first, int last_, int lane) : last(last_) {
         most = kBlock * a.s.K;
+        if (!a.row_grad) {                              // no gradients wanted: nothing is left out
+            list = nullptr;
+            next = kNone;
+            return;
+        }
         if (a.plan.named) {
             list = a.at<const uint32_t>(a.plan.named) + block * most;
             const uint32_t* starts = a.at<const uint32_t>(a.plan.named_starts) + block * (a.cut.parts + 1) + part;
@@ -1045,8 +1055,9 @@ template <int CLASSES> struct Named {
 // forward: a wave holds 32 rows of h, the table streams by
 // ---------------------------------------------------------------------------------------------------------------
 // Mathematics: p = 2^(score * log2e - ref), ref following a row's maximum; the sum of p and, for the gradient of the row,
-// the sum of p times the table's rows but those that the row's slots name (theirs are added with p - q, formed in fp32, when
-// the parts are joined: of a row that has learned its class that difference is far below the rounding of p), all in one pass.
+// the sum of p times the table's rows, both without the classes that the row's slots name (where gradients are wanted: theirs
+// are added, to p with its sum and with p - q, when the parts are joined: of a row that has learned its class 1 - p is far
+// below the roundings of p and of its score), all in one pass.
 // What bounds it: two products of T V D multiply-adds on the matrix units beside an exponential a score, which takes 16
 // cycles for 64 of them, as long as half a product of 128 elements.  4096 rows x 2.5 M classes x 128 bfloat16: 5.04 ms, 1.04
 // PFLOP/s, matrix units busy 56 % of 9.0 M cycles at the 1.84 GHz that the card holds then; a large bfloat16 product of the
@@ -1055,8 +1066,8 @@ template <int CLASSES> struct Named {
 // accumulator column) until the end; a wave has 32 of them, two waves fit a SIMD (with one: 8.1 ms against 5.6, before the order of advance()).  Few rows: the
 // waves of a workgroup share the streamed blocks instead (WY).
 //
-// Named classes: few of them are taken out of a tile's scores one after the other, 0.3 to 0.6 us each; CROWDED, the tile's operands
-// are masked for all of them, which costs every tile registers (1024 x 47 x 100 fp32, 10 slots: 47.9 us and 19.4; 4096 x 2.5 M x
+// Named classes: few of them are taken out of a tile's scores one after the other, 0.3 to 0.6 us each; CROWDED, all of them together,
+// which costs every tile registers (1024 x 47 x 100 fp32, 10 slots: 47.9 us and 19.4; 4096 x 2.5 M x
 // 128 bfloat16: 5.3 ms and 6.4).
 template <int DP, int WY, bool MEAN, bool STRAIGHT, bool CROWDED = false>
 __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_forward_kernel(ClassArgs a, int64_t padded) {
@@ -1188,7 +1199,6 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
 #pragma unroll
                 for (auto& f : acc) f *= by;
         }
-        uint32_t out = 0;                               // bit 16 m + i: register i of block m is named
         if constexpr (CROWDED) {
             if (named.next == (uint32_t)it) {
                 named.take_many(a, row0 / kBlock, it, lane, [&](bool has, int r, int c) {
@@ -1197,19 +1207,22 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
                         atomicOr(&places[wave][r + 32 * (c >> 2 & 1)], 1u << (16 * b + 4 * (c % kBlock >> 3) + (c & 3)));
                 });
                 __builtin_amdgcn_wave_barrier();
-                out = places[wave][lane];
+                const uint32_t out = places[wave][lane];        // bit 16 m + i: register i of block m is named
                 places[wave][lane] = 0;
                 __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int m = 0; m < MY; ++m)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) if (out >> (16 * m + i) & 1) score[m][i] = -__builtin_inff();
             }
         } else if constexpr (MEAN)
-            if (named.next == (uint32_t)it)             // p of these to the sum, not to the product
+            if (named.next == (uint32_t)it)
                 named.take(it, lane, [&](uint32_t rows, int c) {
                     const int b = c / kBlock - (WY == 1 ? 0 : __builtin_amdgcn_readfirstlane(y)) * MY, i = 4 * (c % kBlock >> 3) + (c & 3);
                     const bool mine = lane >> 5 == (c >> 2 & 1) && rows >> (lane & 31) & 1;
                     each<MY>([&](auto m) {
                         if (b != m()) return;
-                        const float z = score[m()][i], p = power(z);
-                        if (mine) sum += kKind == 0 ? p * scales[at].inverse[c] : p;
+                        const float z = score[m()][i];
                         score[m()][i] = mine ? -__builtin_inff() : z;
                     });
                 });
@@ -1227,9 +1240,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
                     some[i & 1] = fmaf(p, b[i % 4], some[i & 1]);
                 } else some[i & 1] += p;
                 return p;
-            }, [&](int m, u32x4 (&q)[2][NS]) {
-                if constexpr (CROWDED) leave_out(out >> 16 * m, q);
-            });
+            }, [](int, u32x4 (&)[2][NS]) {});
             sum += some[0] + some[1];
             find_top(it + 1, slot);
             continue;
@@ -1250,7 +1261,6 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
             if constexpr (MEAN) {
                 u32x4 b[2][NS];
                 operand_of(p, b);
-                if constexpr (CROWDED) leave_out(out >> 16 * m, b);
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -1282,7 +1292,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
     }
 }
 
-// One workgroup per row.  LOSS: the parts joined, the row's slots scored again (fp32 sums of the elements themselves), its
+// One workgroup per row.  LOSS: the parts joined, the row's slots scored again (sums in 64 bits of the elements themselves), its
 // loss.  ROWS: the gradient of its loss, scale * (sum of p w over classes that no slot names + sum of (p - q) w over those), from
 // parts that carry their own reference (LOSS as well) or that are normalised already.
 // The workgroup is cut into groups of `lanes` lanes that cover four elements each; slots and parts go around them.  Bound by
@@ -1290,7 +1300,8 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
 constexpr int kMostSlices = 4096;
 template <bool LOSS, bool ROWS>
 __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a, int64_t padded, int depth, int slices, int lanes) {
-    __shared__ float room[kClassWaves], slot_z[64], slot_pull[64];
+    __shared__ float room[kClassWaves], slot_pull[64];
+    __shared__ double slot_z[64];
     __shared__ int slot_id[64], alive;
     __shared__ float weight[LOSS && ROWS ? kMostSlices : 1];
     __shared__ __align__(16) f32x4 gathered[ROWS ? kClassThreads : 1];
@@ -1301,7 +1312,7 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
     float top = -3e38f, sum = 1.0f;
     if constexpr (LOSS)
 #pragma unroll 4
-        for (int p = threadIdx.x; p < slices; p += kClassThreads) top = fmaxf(top, tops[p]);
+        for (int p = threadIdx.x; p < slices; p += kClassThreads) if (sums[p] != 0.0f) top = fmaxf(top, tops[p]);    // (a reference may be a named class's)
     int id = -1;
     float q = 0.0f, log_weight = 0.0f;                  // of lane's slot, in wave 0
     if (wave == 0) {
@@ -1334,7 +1345,7 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
         sum = 0.0f;
 #pragma unroll 4
         for (int p = threadIdx.x; p < slices; p += kClassThreads) {
-            const float e = exp2f(tops[p] - top);
+            const float e = sums[p] != 0.0f ? exp2f(tops[p] - top) : 0.0f;
             sum += sums[p] * e;
             if constexpr (ROWS) weight[p] = e;
         }
@@ -1345,32 +1356,41 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
         for (int j = group; j < a.s.K; j += groups) {
             const int id = slot_id[j];
             if (id < 0) continue;
-            float dot = id < a.s.V ? 0.0f : __builtin_nanf("");     // a class that there is not
+            double dot = id < a.s.V ? 0.0 : __builtin_nan("");       // a class that there is not
             if (id < a.s.V)
                 for (int c = 4 * l; c < a.s.D; c += 4 * lanes) {
-                    const f32x4 x = load4(h, a.s.D, c), y = load4(w + id * a.w_stride, a.s.D, c);
-                    dot += (x[0] * y[0] + x[1] * y[1]) + (x[2] * y[2] + x[3] * y[3]);
+                    dot += dot4(load4(h, a.s.D, c), load4(w + id * a.w_stride, a.s.D, c));
                 }
             for (int d = 1; d < lanes; d *= 2) dot += __shfl_xor(dot, d);
             if (l == 0) slot_z[j] = dot;
         }
         __syncthreads();
-        sum = (room[0] + room[1]) + (room[2] + room[3]);
         if (wave == 0) {
-            const float log2_sum = top + log2f(sum), lse = log2_sum * kLn2, z = slot_z[lane] * a.scale;
-            float loss = id >= 0 && q != 0.0f ? q * (log_weight + (lse - z)) : 0.0f;
+            sum = (room[0] + room[1]) + (room[2] + room[3]);
+            // where gradients are wanted the named classes are not in the sums yet
+            const bool apart = ROWS || a.row_grad;
+            const double z = slot_z[lane] * a.scale, z2 = z * kLog2eDouble;
+            float pull = q;
+            const bool named = apart && merge_slots(a, id, pull);
+            double most = named && z2 > top ? z2 : (double)top;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) { const double o = __shfl_xor(most, d); most = o > most ? o : most; }
+            double own = named ? exp2(z2 - most) : 0.0;
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) own += __shfl_xor(own, d);
+            const double log2_sum = most + log2(sum * exp2(top - most) + own), lse = log2_sum / kLog2eDouble;
+            float loss = id >= 0 && q != 0.0f ? q * (log_weight + (float)(lse - z)) : 0.0f;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) loss += __shfl_xor(loss, d);
+            const float rest = (float)exp2(top - log2_sum);     // what the others' sums are relative to, as a share
             if (lane == 0) {
-                a.loss[t] = loss; a.lse[t] = lse;
-                // where means are made in a launch of their own: what they are relative to, for fp32 the reference of p s
-                if (!ROWS && a.row_grad) {
-                    a.at<float>(a.plan.norm)[t] = (kKind == 0 ? top : log2_sum) - kLift;
-                    a.at<float>(a.plan.back)[t] = kKind == 0 ? 1.0f / sum : 1.0f;
-                }
+                a.loss[t] = loss; a.lse[t] = (float)lse;
+                if constexpr (ROWS) room[0] = rest;
+                // where means are made in a launch of their own: what they are relative to
+                else if (a.row_grad) { a.at<float>(a.plan.norm)[t] = top - kLift; a.at<float>(a.plan.back)[t] = rest; }
             }
-            if (ROWS || a.row_grad) {
-                const float pull = merge_slots(a, id, q) ? probability(z, lse) - q : 0.0f;
+            if (apart) {
+                pull = named ? probability(z, lse) - pull : 0.0f;
                 if constexpr (ROWS) slot_pull[lane] = pull;
                 else if (lane < a.s.K) a.at<float>(a.plan.pulls)[t * a.s.K + lane] = pull;
             }
@@ -1379,7 +1399,7 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
     }
     if constexpr (ROWS) {
         const float* parts = a.at<const float>(a.plan.mean_parts);
-        const float back = LOSS ? 1.0f / sum : a.at<const float>(a.plan.back)[t];
+        const float back = LOSS ? room[0] : a.at<const float>(a.plan.back)[t];
         for (int c0 = 0; c0 < a.s.D; c0 += 4 * lanes) {
             const int c = c0 + 4 * l;
             f32x4 e = {};
@@ -1663,7 +1683,7 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
     constexpr int PS = MODE == kStats ? 1 : MODE == kGradient ? 2 : NS;   // planes of P; 16-bit types use the second after a hit
     __shared__ __align__(16) u32x2 shared_p[PS][2][64][2];
     __shared__ int hit;                                 // the tile that last had a slot of these classes
-    __shared__ uint32_t places[MODE == kMean ? kClassWaves : 1][64];
+    __shared__ uint32_t places[MODE != kGradient ? kClassWaves : 1][64];
     __shared__ float cells[MODE == kGradient ? kBlock * kBlock : 1];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col0 = wave * Q;
     const ClassCut::Place place = a.cut.place(blockIdx.x);
@@ -1692,10 +1712,10 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
         if (threadIdx.x == 0) hit = -1;
         __syncthreads();
     }
-    if constexpr (MODE == kMean) places[wave][lane] = 0;
+    if constexpr (MODE != kGradient) places[wave][lane] = 0;
     using Places = Named<kBlock>;
-    typename std::conditional<MODE == kMean, Places, int>::type named = [&] {
-        if constexpr (MODE == kMean) return Places(a, group, part, first, last, lane);
+    typename std::conditional<MODE != kGradient, Places, int>::type named = [&] {
+        if constexpr (MODE != kGradient) return Places(a, group, part, first, last, lane);
         else return 0;
     }();
     const float norm = MODE == kMean && x < a.s.T ? a.at<const float>(a.plan.norm)[x] : __builtin_inff();
@@ -1789,12 +1809,29 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
 #pragma unroll
             for (int j = 0; j < 4; ++j) if (y0 + y + j >= a.s.V) z[j] = -__builtin_inff();
         }
+        if constexpr (MODE != kGradient) {
+            if (named.next == (uint32_t)it && a.s.K > kWaveSlots) {
+                named.take_many(a, group, it, lane, [&](bool has, int r, int c) {
+                    if (has && c >> 3 == wave) atomicOr(&places[wave][r + 32 * (c >> 2 & 1)], 1u << (c & 3));
+                });
+                __builtin_amdgcn_wave_barrier();
+                const uint32_t mine = places[wave][lane];
+                places[wave][lane] = 0;
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (mine >> j & 1) z[j] = -__builtin_inff();
+            } else if (named.next == (uint32_t)it)
+                named.take(it, lane, [&](uint32_t rows, int c) {
+                    const bool mine = c >> 3 == wave && lane >> 5 == (c >> 2 & 1) && rows >> (lane & 31) & 1;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) if (mine && j == (c & 3)) z[j] = -__builtin_inff();
+                });
+        }
         if constexpr (MODE == kStats) {
             if constexpr (kKind != 0) z *= to_log2;
             const float top = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
-            constexpr float slack = kKind == 0 ? kSlack : 8.0f;    // (fp32: what the mean's P is relative to)
-            if (__any(top > ref + slack)) {
-                const float to = top > ref + slack ? top : ref;
+            if (__any(top > ref + kSlack)) {            // (what the mean's P is relative to)
+                const float to = top > ref + kSlack ? top : ref;
                 sum *= exp2f(ref - to);
                 ref = to;
             }
@@ -1808,22 +1845,6 @@ __global__ __launch_bounds__(kClassThreads, Q * NS <= 192 ? 2 : 1) void class_wi
             if constexpr (MODE == kMean) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) p[j] = __builtin_amdgcn_exp2f(kKind == 0 ? z[j] - norm : fmaf(z[j], to_log2, -norm));
-                if (named.next == (uint32_t)it && a.s.K > kWaveSlots) {
-                    named.take_many(a, group, it, lane, [&](bool has, int r, int c) {
-                        if (has && c >> 3 == wave) atomicOr(&places[wave][r + 32 * (c >> 2 & 1)], 1u << (c & 3));
-                    });
-                    __builtin_amdgcn_wave_barrier();
-                    const uint32_t mine = places[wave][lane];
-                    places[wave][lane] = 0;
-                    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) if (mine >> j & 1) p[j] = 0.0f;
-                } else if (named.next == (uint32_t)it)
-                    named.take(it, lane, [&](uint32_t rows, int c) {
-                        const bool mine = c >> 3 == wave && lane >> 5 == (c >> 2 & 1) && rows >> (lane & 31) & 1;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) if (mine && j == (c & 3)) p[j] = 0.0f;
-                    });
             } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) p[j] = power_of<kKind == 0>(z[j], kKind == 0 ? scale[j] * to_log2 : to_log2, start[j]);

@@ -229,7 +229,8 @@ PyObject* class_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
         Tensor loss;
         const int rc = without_gil([&] {
             try {
-                loss = ClassLoss::apply(c.h, c.w, c, c10::GradMode::is_enabled() && c.h.requires_grad());
+                // (with a gradient of w alone as well: the log-sum-exp that its backward takes is then as exact as both need it)
+                loss = ClassLoss::apply(c.h, c.w, c, c10::GradMode::is_enabled() && (c.h.requires_grad() || c.w.requires_grad()));
                 return (int)FSA_OK;
             } catch (const Refused& r) {
                 return r.status;

@@ -94,3 +94,15 @@ def test_many_slots_that_name_one_class(dtype, D):
     for _ in range(5):
         again = fsa.fsa_distill_bwd(g, h, w, ids, logits, lse, row_grad, 1.0, scale)
         assert all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T,V,D", SIZES)
+def test_losses_of_learned_rows(dtype, T, V, D):
+    """Where gradients are wanted, a loss of 1e-7 is right to a share of itself: that of a sum of V terms and of 2^20."""
+    from paper_2511_13645_amd import binding as fsa
+    h, w, ids, g, scale = learned(dtype, T, V, D, T + D + 1)
+    ref, x = reference(h, w, ids, None, 1.0, scale, g)
+    loss = fsa.fsa_xent_fwd(h, w, ids, scale, emit_row_grad=True)[0]
+    share = (V / 16 + 64 + 8 * x["z"].abs().amax(1)) * 2.0 ** -24 + 2.0 ** -20
+    check(loss, ref["loss"], share * ref["loss"] + 2.0 ** -48, "f32", "loss")
