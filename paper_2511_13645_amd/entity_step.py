@@ -61,7 +61,8 @@ def main() -> int:
     teacher = torch.randn((args.nodes, args.dim), generator=gen, device=dev) * args.dim ** -0.25
     table = torch.nn.Parameter((teacher + torch.randn(teacher.shape, generator=gen, device=dev)).mul_(0.3).to(dtype))
     layer = torch.nn.Linear(args.dim, args.dim, bias=False, device=dev, dtype=dtype)
-    opt = torch.optim.Adam([table, *layer.parameters()], lr=args.rate)
+    # Adam's squares of gradients below 2^-12 are zero in fp16, as is 1e-8: the step would be an infinity
+    opt = torch.optim.Adam([table, *layer.parameters()], lr=args.rate, eps=1e-4 if args.dtype == "f16" else 1e-8)
     n = args.steps + args.warmup
     seeds = synth.seed_batches(args.nodes, args.batch, n, seed=2).to(dev)
     times, losses = [], []
