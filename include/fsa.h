@@ -390,9 +390,10 @@ int fsa_wmean_bwd_ws(const float* grad_out, const float* grad_h1,
  * of every element down to 2^-16 of the row's largest finite one and never further off than 2^-40 of that, whatever other rows
  * hold (rows whose largest is below 2^-82 have fewer bits); an infinite element of an fp32 row makes its scores NaN.
  * Probabilities enter the gradients rounded to the table's 16-bit type, or to 22 bits, but for classes that a row's slots
- * name: their scores are 64-bit sums, they join loss and lse as such where out_row_grad is given, and p - q of them is fp32.  fp16 and fp32 end there at 2^-39 of the largest |grad_loss| (times its row's largest
- * element, for fp32) in grad_w, and at 2^-39 of the largest p (times its class's largest element) in a row's gradient;
- * bfloat16 takes |grad_loss| up to 2^64.  Scores of 16-bit tables are taken up to 2^22 in magnitude.
+ * name: their scores are 64-bit sums, they join loss and lse as such where out_row_grad is given, and p - q of them is fp32.
+ * fp16 and fp32 end at 2^-39 of the largest |grad_loss| (fp32: times its row's largest element) in grad_w, and at 2^-39 of
+ * the largest p (fp32: times its class's largest element) in a row's gradient; bfloat16 takes |grad_loss| up to 2^64.  Scores
+ * of 16-bit tables are taken up to 2^22 in magnitude.
  * Every result is a function of the arguments alone: no atomics whose order could change it.
  */
 enum { FSA_CLASS_TMAX = 1 << 23, FSA_CLASS_VMAX = 1 << 27, FSA_CLASS_DMAX = 1024 };

@@ -119,8 +119,8 @@ constexpr bool slots_apart(const ClassShape& s) { return s.K > 1; }
 
 // Whether the forward first lays the table out as planes of padded rows: one more pass over the table, against rows that
 // the kernel has to read off the 16-byte grid, to pad, or to split into planes, once for every workgroup beside it (measured
-// on 2 to 9 of them: it pays from 3 on; wide rows of which two workgroups fit a CU hide that work, 3 of 67 rows x 493,386
-// x 336 fp32 1.54 ms without, 1.67 with).  Tables of a quarter of a million elements and less are not worth the launch.
+// on 2 to 9 of them: it pays from 3 on, and from 5 on for wide 16-bit rows of which two workgroups fit a CU and hide that work).
+// Tables of a quarter of a million elements and less are not worth the launch.
 inline bool forward_packs(const ClassShape& s, bool straight) {
     const int depth = class_depth(s.D);
     if (!straight && !narrow_depth(depth) && s.kind == 0) return true;          // (no wave has a row whole, to make its unit of)

@@ -1059,9 +1059,10 @@ template <int CLASSES> struct Named {
 // are added, to p with its sum and with p - q, when the parts are joined: of a row that has learned its class 1 - p is far
 // below the roundings of p and of its score), all in one pass.
 // What bounds it: two products of T V D multiply-adds on the matrix units beside an exponential a score, which takes 16
-// cycles for 64 of them, as long as half a product of 128 elements.  4096 rows x 2.5 M classes x 128 bfloat16: 5.04 ms, 1.04
-// PFLOP/s, matrix units busy 56 % of 9.0 M cycles at the 1.84 GHz that the card holds then; a large bfloat16 product of the
-// library runs at 1.29.  8 rows, one read of the table: 102 us, 6.1 TB/s.
+// cycles for 64 of them, as long as half a product of 128 elements.  4096 rows x 2.5 M classes x 128 bfloat16: 5.06 to 5.4 ms,
+// 1.04 to 0.97 PFLOP/s as the card holds its clock, matrix units busy a little over half of the time; a large bfloat16 product of
+// the library runs at 1.29.  8 rows, one read of the table: 104 us, 6.0 TB/s.  fp32 rows of up to 64 elements and 16-bit ones of up
+// to 128 have no register left: 4 to 41 are spilled around the loop (fp32 64: 14 reads of them a tile).
 // Why this way: rows stay in registers and the table streams, because a row's statistics then never leave its lane (an
 // accumulator column) until the end; a wave has 32 of them, two waves fit a SIMD (with one: 8.1 ms against 5.6, before the order of advance()).  Few rows: the
 // waves of a workgroup share the streamed blocks instead (WY).
@@ -1296,7 +1297,7 @@ __global__ __launch_bounds__(kClassThreads, DP * NS <= 128 ? 2 : 1) void class_f
 // loss.  ROWS: the gradient of its loss, scale * (sum of p w over classes that no slot names + sum of (p - q) w over those), from
 // parts that carry their own reference (LOSS as well) or that are normalised already.
 // The workgroup is cut into groups of `lanes` lanes that cover four elements each; slots and parts go around them.  Bound by
-// the latency of its reads: 4096 rows x 128 with 16 parts 20 us, 8 rows 6.
+// the latency of its reads: 4096 rows x 128 with 16 parts 24 us, 8 rows 6.
 constexpr int kMostSlices = 4096;
 template <bool LOSS, bool ROWS>
 __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a, int64_t padded, int depth, int slices, int lanes) {
@@ -1435,7 +1436,7 @@ __global__ __launch_bounds__(kClassThreads) void class_finish_kernel(ClassArgs a
 // Scores are made again from the table and the rows, 2 T V D operations, because keeping them would move 6 bytes a score: 12
 // times what the classes and their gradients move at 128 elements.  A class's row is written once, by the wave that holds it,
 // or in parts that a second launch joins where there are fewer classes than waves.
-// 4096 x 2.5 M x 128 bfloat16: 5.4 ms, 0.97 PFLOP/s; what slots add costs by the slot (4096 x 169,343, 32 slots a row: 0.55
+// 4096 x 2.5 M x 128 bfloat16: 5.46 ms, 0.96 PFLOP/s; what slots add costs by the slot (4096 x 169,343, 32 slots a row: 0.59
 // ms, where the classes alone would take 0.37 at that rate).
 // P = 2^(score * by + start), P s for fp32 rows: at most 2^15 there, which a row of enormous scores, whose log-sum-exp is rounded,
 // would exceed.
@@ -1669,8 +1670,9 @@ enum WideMode { kStats, kMean, kGradient };
 // exponential is taken once, and P goes back to all through LDS: 3 KB of LDS traffic a wave for 32 x 32 scores.  The forward is
 // two launches, statistics first: a common running maximum would cost the four waves another meeting a tile.
 // Bound by the meetings (two barriers a tile) and, for the statistics, by the table's way to the CUs, once for every 32 rows.
-// 1024 x 232,965 x 602 fp16: 0.62 + 0.94 + 1.00 ms (0.46, 0.61, 0.57 PFLOP/s); fp32, 257 rows: 0.59 + 0.77 + 1.14 ms, of which
-// one workgroup fits a CU, so that its meetings are waited for: 1.4 times the plain products in fp32, the furthest from the floor.
+// 1024 x 232,965 x 602 fp16: 0.64 + 0.92 + 0.97 ms (0.45, 0.63, 0.59 PFLOP/s); fp32, 257 rows: 0.67 + 0.80 + 1.10 ms, of which
+// one workgroup fits a CU, so that its meetings are waited for: 1.35 times the plain products in fp32, the furthest from the floor.
+// fp32 rows of more than 640 elements spill up to 77 registers.
 // kStats: running maximum and sum of every held row of h, one pair per wave (a quarter of the streamed classes each).
 // kMean: sum of the table's rows under 2^(score - norm).  kGradient: as the narrow kernel.
 template <int Q, WideMode MODE, bool STRAIGHT>
