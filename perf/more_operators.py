@@ -1,0 +1,307 @@
+"""The block between a seed's sampled mean and its loss, and the update of the block's matrices -- as a list of cases with
+their inputs, one pass in plain form and through the public entry points, and what a pass cannot do without.
+
+  op        "norm"    s = x + residual (rounded to the type; x itself without a residual), y = s / sqrt(mean(s^2) + eps) * weight
+            "gated"   y = (act(x Wg^T) * (x Wu^T)) Wd^T
+            "orthogonal"   X = G / (|G| + eps), five times X = a X + (b A + c A^2) X with A = X X^T (of the transpose where G is tall)
+  path      "forward" outputs;  "train"  outputs and the gradients of all inputs from gradients of the outputs
+  rows, dim            T, D ("orthogonal": the matrix)
+  hidden, out          H, O ("gated")
+  batch                matrices of one size ("orthogonal")
+  residual             whether there is one ("norm")
+  activation           "silu", "gelu" (by the error function), "relu" ("gated")
+  dtype                of every tensor
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+DEVICE = "cuda:0"
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+EPS = 1e-6
+SMALL = 1e-7                                # added to a matrix's norm
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+STEPS = 5
+MOST_NORM = 65536 * 1024                    # elements of the largest listed cases,
+MOST_GATED = 16384 * 4096 * (2 * 1024 + 1024)   # products of theirs, forward,
+MOST_ORTHOGONAL = 1024 * 1024 * 4096        # and m^2 n of theirs
+
+own = False
+
+_PLAIN = {"op": "norm", "path": "train", "rows": 0, "dim": 0, "hidden": 0, "out": 0, "batch": 1, "residual": True,
+          "activation": "silu", "dtype": "f32"}
+
+
+def _case(**kw):
+    return {**_PLAIN, **kw}
+
+
+def listed():
+    return [
+        # one seed answered online, the social graph's width: all latency
+        _case(name="norm_1x602_f16", path="forward", rows=1, dim=602, dtype="f16"),
+        # the training step over the citation graph's nodes
+        _case(name="norm_1024x128_f32", rows=1024, dim=128),
+        # an odd last batch of the social graph
+        _case(name="norm_10007x602_f16", rows=10007, dim=602, dtype="f16"),
+        # wide rows of a large batch: bound by memory
+        _case(name="norm_65536x1024_bf16", rows=65536, dim=1024, dtype="bf16"),
+        # one seed through a wide block: every weight read once
+        _case(name="gated_1x1024_bf16", op="gated", path="forward", rows=1, dim=1024, hidden=4096, out=1024, dtype="bf16"),
+        # the block of the training step over the citation graph's nodes
+        _case(name="gated_1024x128_f32", op="gated", rows=1024, dim=128, hidden=512, out=128),
+        # node classification on the product graph: 100 features, 47 labels, nothing on a grid
+        _case(name="gated_4099x100_f16", op="gated", rows=4099, dim=100, hidden=333, out=47, activation="gelu", dtype="f16"),
+        # wide fp32 rows of the social graph
+        _case(name="gated_8192x602_f32", op="gated", rows=8192, dim=602, hidden=2048, out=602),
+        # a large batch through a wide block
+        _case(name="gated_16384x1024_bf16", op="gated", rows=16384, dim=1024, hidden=4096, out=1024, dtype="bf16"),
+        # the three matrices of the training step's block
+        _case(name="orthogonal_3x128x512_f32", op="orthogonal", path="forward", batch=3, rows=128, dim=512),
+        # a matrix off every grid
+        _case(name="orthogonal_602x2047_f16", op="orthogonal", path="forward", rows=602, dim=2047, dtype="f16"),
+        # a tall matrix of the wide block
+        _case(name="orthogonal_4096x1024_bf16", op="orthogonal", path="forward", rows=4096, dim=1024, dtype="bf16"),
+    ]
+
+
+def draw(rng):
+    """One more case of the same ranges; sizes over their logarithms, many of them odd."""
+    def log_int(lo, hi, grid=1):
+        n = int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+        return max(grid, n // grid * grid) if rng.random() < 0.5 else n
+
+    while True:
+        op = rng.choice(("norm", "gated", "gated", "orthogonal"))
+        dtype = rng.choice(("f32", "bf16", "f16"))
+        if op == "norm":
+            case = _case(path=rng.choice(("forward", "train", "train")), rows=log_int(1, 65536), dim=log_int(16, 4096, 16),
+                         residual=rng.random() < 0.8, dtype=dtype)
+            fits = case["rows"] * case["dim"] <= MOST_NORM
+        elif op == "gated":
+            path = rng.choice(("forward", "train", "train"))
+            case = _case(op=op, path=path, rows=log_int(1, 16384), dim=log_int(16, 1024, 16), hidden=log_int(32, 4096, 32),
+                         out=log_int(16, 1024, 16), activation=rng.choice(("silu", "silu", "gelu", "relu")), dtype=dtype)
+            fits = case["rows"] * case["hidden"] * (2 * case["dim"] + case["out"]) <= MOST_GATED
+        else:
+            case = _case(op=op, path="forward", batch=rng.choice((1, 1, 2, 3, 8)), rows=log_int(16, 4096, 16), dim=log_int(16, 4096, 16),
+                         dtype=dtype)
+            m, n = sorted((case["rows"], case["dim"]))
+            fits = case["batch"] * m * m * n <= MOST_ORTHOGONAL
+        if fits:
+            return case
+
+
+# ----------------------------------------------------------------------------------------
+# inputs
+# ----------------------------------------------------------------------------------------
+def prepare(case, seed):
+    gen = torch.Generator(device=DEVICE).manual_seed(int(seed))
+    dtype = DTYPES[case["dtype"]]
+    t, d, h, o = (case[x] for x in ("rows", "dim", "hidden", "out"))
+
+    def normal(*shape, unit=1.0):
+        return torch.randn(shape, generator=gen, device=DEVICE).mul_(unit)
+
+    s = {"case": dict(case)}
+    if case["op"] == "orthogonal":
+        # momentum of a gradient: a few strong directions over a floor of noise
+        b, k = case["batch"], min(t, d, 16)
+        strong = torch.bmm(normal(b, t, k) * torch.logspace(0, -2, k, device=DEVICE), normal(b, k, d)).mul_(4.0)
+        s["g"] = (strong + normal(b, t, d)).mul_(1e-3).to(dtype)
+        if b == 1:
+            s["g"] = s["g"][0]
+        return s
+    # gradients of a mean over the batch; in fp16 under a loss scale that brings the weights' gradients to about one
+    unit = t ** -0.5 if case["dtype"] == "f16" else 1.0 / t
+    if case["op"] == "norm":
+        spread = 0.25 + 2.0 * torch.rand((t, 1), generator=gen, device=DEVICE)      # rows grow with their degree
+        s["x"] = (normal(t, d) * spread).to(dtype)
+        if case["residual"]:
+            s["residual"] = (normal(t, d) * spread).to(dtype)
+        s["weight"] = (1.0 + normal(d, unit=0.2)).to(dtype)
+        s["grad_y"], s["grad_s"] = normal(t, d, unit=unit).to(dtype), normal(t, d, unit=unit).to(dtype)
+        wants = ("x", "residual", "weight")
+    else:
+        s["x"] = normal(t, d).to(dtype)
+        s["w_gate"], s["w_up"] = (normal(h, d, unit=1.5 * d ** -0.5).to(dtype) for _ in range(2))
+        s["w_down"] = normal(o, h, unit=h ** -0.5).to(dtype)
+        s["grad_y"] = normal(t, o, unit=unit).to(dtype)
+        wants = ("x", "w_gate", "w_up", "w_down")
+    if case["path"] == "train":
+        for name in wants:
+            if name in s:
+                s[name].requires_grad_(True)
+    return s
+
+
+# ----------------------------------------------------------------------------------------
+# one pass
+# ----------------------------------------------------------------------------------------
+def run(s):
+    return _own(s) if own else {"norm": _plain_norm, "gated": _plain_gated, "orthogonal": _plain_orthogonal}[s["case"]["op"]](s)
+
+
+def _own(s):
+    from paper_2511_13645_amd import binding
+    from paper_2511_13645_amd.autograd import fused_gated_feed_forward, fused_residual_norm
+    case = s["case"]
+    train = case["path"] == "train"
+    if case["op"] == "orthogonal":
+        return {"x": binding.fsa_orthogonalize(s["g"], COEFFICIENTS, STEPS, eps=SMALL)}
+    if case["op"] == "norm":
+        x, r, w = s["x"], s.get("residual"), s["weight"]
+        if not train:
+            y, total, _ = binding.fsa_norm_fwd(x, w, r, EPS)
+            return {"y": y, "s": total} if case["residual"] else {"y": y}
+        y, total = fused_residual_norm(x, w, r, eps=EPS)
+        if not case["residual"]:
+            gx, gw = torch.autograd.grad(y, (x, w), s["grad_y"])
+            return {"y": y.detach(), "grad_x": gx, "grad_weight": gw}
+        gx, gr, gw = torch.autograd.grad((y, total), (x, r, w), (s["grad_y"], s["grad_s"]))
+        return {"y": y.detach(), "s": total.detach(), "grad_x": gx, "grad_residual": gr, "grad_weight": gw}
+    weights = (s["w_gate"], s["w_up"], s["w_down"])
+    if not train:
+        return {"y": binding.fsa_gated_fwd(s["x"], *weights, activation=case["activation"])}
+    y = fused_gated_feed_forward(s["x"], *weights, activation=case["activation"])
+    grads = torch.autograd.grad(y, (s["x"], *weights), s["grad_y"])
+    return {"y": y.detach(), **dict(zip(("grad_x", "grad_gate", "grad_up", "grad_down"), grads))}
+
+
+@torch.no_grad()
+def _plain_norm(s):
+    case, dtype = s["case"], s["x"].dtype
+    total, w = s["x"].float(), s["weight"].float()
+    if case["residual"]:
+        rounded = (total + s["residual"].float()).to(dtype)
+        total = rounded.float()
+    scale = torch.rsqrt(total.square().mean(1, keepdim=True) + EPS)
+    unit = total * scale
+    out = {"y": (unit * w).to(dtype)}
+    if case["residual"]:
+        out["s"] = rounded
+    if case["path"] == "train":
+        g = s["grad_y"].float()
+        gw = g * w
+        gx = (gw - unit * (gw * unit).mean(1, keepdim=True)) * scale
+        if case["residual"]:
+            gx = gx + s["grad_s"].float()
+        out["grad_x"] = gx.to(dtype)
+        if case["residual"]:
+            out["grad_residual"] = out["grad_x"]
+        out["grad_weight"] = (g * unit).sum(0).to(dtype)
+    return out
+
+
+def _activation(name, g):
+    """act(g) and its derivative."""
+    if name == "silu":
+        p = torch.sigmoid(g)
+        return g * p, p * (1.0 + g * (1.0 - p))
+    if name == "gelu":
+        p = 0.5 * (1.0 + torch.erf(g * math.sqrt(0.5)))
+        return g * p, p + g * torch.exp(-0.5 * g * g) * (1.0 / math.sqrt(2.0 * math.pi))
+    return g.clamp_min(0.0), (g > 0).to(g.dtype)
+
+
+@torch.no_grad()
+def _plain_gated(s):
+    case, dtype = s["case"], s["x"].dtype
+    x, wg, wu, wd = (s[k].float() for k in ("x", "w_gate", "w_up", "w_down"))
+    g, u = torch.mm(x, wg.t()), torch.mm(x, wu.t())
+    act, slope = _activation(case["activation"], g)
+    h = act * u
+    out = {"y": torch.mm(h, wd.t()).to(dtype)}
+    if case["path"] == "train":
+        gy = s["grad_y"].float()
+        dh = torch.mm(gy, wd)
+        dg, du = dh * u * slope, dh * act
+        out["grad_x"] = torch.mm(dg, wg).add_(torch.mm(du, wu)).to(dtype)
+        out["grad_gate"], out["grad_up"] = torch.mm(dg.t(), x).to(dtype), torch.mm(du.t(), x).to(dtype)
+        out["grad_down"] = torch.mm(gy.t(), h).to(dtype)
+    return out
+
+
+@torch.no_grad()
+def _plain_orthogonal(s):
+    g = s["g"] if s["g"].dim() == 3 else s["g"][None]
+    tall = g.shape[1] > g.shape[2]
+    x = g.float()
+    x = x / (x.square().sum((1, 2), keepdim=True).sqrt() + SMALL)
+    if tall:
+        x = x.transpose(1, 2).contiguous()
+    a, b, c = COEFFICIENTS
+    for _ in range(STEPS):
+        gram = torch.matmul(x, x.transpose(1, 2).contiguous())
+        x = a * x + torch.matmul(b * gram + c * torch.matmul(gram, gram), x)
+    if tall:
+        x = x.transpose(1, 2)
+    return {"x": x.reshape(s["g"].shape).to(s["g"].dtype)}
+
+
+def exact(case, seed):
+    """In 64 bits: the gradients by torch's own differentiation of the definition, the orthogonalised matrix by its singular values."""
+    s = prepare(case, seed)
+    train = case["path"] == "train"
+    if case["op"] == "orthogonal":
+        g = s["g"].double()
+        if min(case["rows"], case["dim"]) > 512:                    # a decomposition would take too long: the products, one by one
+            x = g / (torch.linalg.vector_norm(g, dim=(-2, -1), keepdim=True) + SMALL)
+            wide = case["rows"] <= case["dim"]
+            a, b, c = COEFFICIENTS
+            for _ in range(STEPS):
+                gram = x @ x.mT.contiguous() if wide else x.mT.contiguous() @ x
+                first = gram @ x if wide else x @ gram
+                x = a * x + b * first + c * (gram @ first if wide else first @ gram)
+            return {"x": x}
+        # (on the host: the device's own decomposition of small matrices is no quicker)
+        u, sigma, vt = torch.linalg.svd(g.cpu(), full_matrices=False)
+        sigma = sigma / (sigma.square().sum(-1, keepdim=True).sqrt() + SMALL)
+        for _ in range(STEPS):
+            sigma = sum(k * sigma ** p for k, p in zip(COEFFICIENTS, (1, 3, 5)))
+        return {"x": ((u * sigma[..., None, :]) @ vt).to(DEVICE)}
+    d = {k: v.detach().double().requires_grad_(train and v.requires_grad) for k, v in s.items() if k != "case"}
+    if case["op"] == "norm":
+        total = d["x"]
+        if case["residual"]:
+            # the sum as the type holds it; its rounding passes gradients on
+            total = total + d["residual"]
+            total = total + (total.detach().to(s["x"].dtype).double() - total.detach())
+        y = total * torch.rsqrt(total.pow(2).mean(1, keepdim=True) + EPS) * d["weight"]
+        out = {"y": y.detach()}
+        outputs, grads = [y], [d["grad_y"]]
+        if case["residual"]:
+            out["s"] = total.detach()
+            outputs.append(total)
+            grads.append(d["grad_s"])
+        names = ["x", "residual", "weight"] if case["residual"] else ["x", "weight"]
+        keys = ["grad_" + n for n in names]
+    else:
+        act = {"silu": torch.nn.functional.silu, "gelu": torch.nn.functional.gelu, "relu": torch.relu}[case["activation"]]
+        y = (act(d["x"] @ d["w_gate"].mT) * (d["x"] @ d["w_up"].mT)) @ d["w_down"].mT
+        out = {"y": y.detach()}
+        outputs, grads = [y], [d["grad_y"]]
+        names, keys = ["x", "w_gate", "w_up", "w_down"], ["grad_x", "grad_gate", "grad_up", "grad_down"]
+    if train:
+        out.update(zip(keys, torch.autograd.grad(outputs, [d[n] for n in names], grads)))
+    return out
+
+
+# ----------------------------------------------------------------------------------------
+# what a pass cannot do without
+# ----------------------------------------------------------------------------------------
+def work(case):
+    t, d, h, o, b = (case[x] for x in ("rows", "dim", "hidden", "out", "batch"))
+    e = 4 if case["dtype"] == "f32" else 2
+    train = case["path"] == "train"
+    if case["op"] == "norm":
+        # in: x, residual; out: y, s; and in: gradients of both, out: that of x (the residual's is the same)
+        arrays = (4 if case["residual"] else 2) + ((3 if case["residual"] else 2) if train else 0)
+        return {"bytes": float(arrays * t * d * e + d * e * (2 if train else 1)), "flops": float(t * d * (14 if train else 5))}
+    if case["op"] == "gated":
+        nbytes = e * (t * d + t * o + h * (2 * d + o)) * (2 if train else 1)
+        return {"bytes": float(nbytes), "flops": 2.0 * t * h * (2 * d + o) * (3 if train else 1)}
+    m, n = sorted((t, d))                                           # gram matrix and polynomial are symmetric: half of each
+    return {"bytes": 2.0 * b * t * d * e, "flops": float(STEPS * b * (m * m * n + m ** 3 + 2 * m * m * n))}
