@@ -154,7 +154,7 @@ def _own(s):
     if case["op"] == "norm":
         x, r, w = s["x"], s.get("residual"), s["weight"]
         if not train:
-            y, total, _ = binding.fsa_norm_fwd(x, w, r, EPS)
+            y, total = binding.fsa_norm_fwd(x, w, r, EPS)
             return {"y": y, "s": total} if case["residual"] else {"y": y}
         y, total = fused_residual_norm(x, w, r, eps=EPS)
         if not case["residual"]:
