@@ -422,6 +422,82 @@ int fsa_distill_bwd(const float* grad_loss, const void* h, int64_t h_stride, con
                     const float* lse, const float* row_grad, void* grad_h, void* grad_w,
                     void* workspace, int64_t workspace_bytes, void* stream);
 
+/*
+ * The block between a mean and its loss: a norm of rows (with the residual's addition before it), a gated feed-forward
+ * block, and the orthogonalised update of a block's matrices.  Every sum and statistic is fp32 or more; every result is a function of
+ * the arguments alone (no atomics).  A workspace is device memory of the call's *_workspace_bytes, 16-byte aligned (else
+ * FSA_ERR_WORKSPACE, FSA_ERR_ALIGN); nothing in it is kept from one call to the next, and no two calls that may run at the
+ * same time share one.  Rows of a matrix argument lie `stride` elements apart, at any alignment of an element; the rows'
+ * elements are contiguous.  Outputs are contiguous and overlap no input.
+ */
+
+/*
+ * Root-mean-square norm.  s[t,:] = x[t,:] + residual[t,:], rounded to the type (the row that later layers add to), or x itself
+ * without a residual;  rstd[t] = 1 / sqrt(mean_d s[t,d]^2 + eps);  y[t,d] = s[t,d] * rstd[t] * weight[d].
+ *   x, residual [T,D]  fsa_dtype `dtype`; residual may be NULL, out_s then is too
+ *   weight [D]         fsa_dtype `weight_dtype`
+ *   eps                finite, not negative;  0 <= T <= FSA_NORM_TMAX, 1 <= D <= FSA_NORM_DMAX
+ *   out_y, out_s       [T,D] `dtype`
+ * Backward, with s as above (out_s, or x):  grad_x = grad_s + rstd * (grad_y w - s rstd^2 mean_d(grad_y w s)), which is the
+ * residual's gradient as well;  grad_weight = sum_t grad_y s rstd.
+ *   grad_y, grad_s     [T,D] `dtype`, contiguous; either may be NULL: none
+ *   grad_x [T,D] `dtype`, grad_weight [D] `weight_dtype`   written whole; either may be NULL
+ * A row of zeros has y 0 where eps > 0.  Squares are summed in fp32: elements of more than about 1e18 make rstd 0.
+ */
+enum { FSA_NORM_TMAX = 1 << 30, FSA_NORM_DMAX = 16384 };
+
+int fsa_norm_fwd(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride,
+                 const void* weight, int dtype, int weight_dtype, int64_t T, int64_t D, float eps,
+                 void* out_y, void* out_s, void* stream);
+int64_t fsa_norm_bwd_workspace_bytes(int64_t T, int64_t D, int dtype);
+int fsa_norm_bwd(const void* grad_y, const void* grad_s, const void* s, int64_t s_stride,
+                 const void* weight, int dtype, int weight_dtype, int64_t T, int64_t D, float eps,
+                 void* grad_x, void* grad_weight, void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Gated feed-forward block:  g = x Wg^T, u = x Wu^T  [T,H];  y = (act(g) * u) Wd^T  [T,O].
+ *   x [T,D], w_gate [H,D], w_up [H,D], w_down [O,H]   fsa_dtype `dtype`
+ *   activation         an fsa_activation
+ *   0 <= T <= FSA_GATED_TMAX; D, H, O from 1 to FSA_GATED_MOST
+ *   out_y [T,O]        `dtype`
+ * Backward, from grad_y [T,O] (rows grad_y_stride apart) and the forward's inputs; g and u are made again:
+ *   dh = grad_y Wd, dg = dh u act'(g), du = dh act(g);  grad_x = dg Wg + du Wu,  grad_gate = dg^T x,  grad_up = du^T x,
+ *   grad_down = grad_y^T (act(g) u).  Each in `dtype`, written whole (T == 0: the weights' are zero), and may be NULL.
+ * act * u, dg and du are rounded to a 16-bit type once between the products (fp16: act * u up to 65504; dg and du beside the power
+ * of two of the largest |grad_y|, up to 2^15 times that).  fp32 elements are taken whole; where an infinite one takes part,
+ * results may be NaN that would be infinite.  relu'(0) = 0.
+ */
+typedef enum { FSA_ACT_SILU = 0, FSA_ACT_GELU = 1, FSA_ACT_RELU = 2 } fsa_activation;   /* gelu: x * normal distribution */
+enum { FSA_GATED_TMAX = 1 << 26, FSA_GATED_MOST = 1 << 16 };
+
+int64_t fsa_gated_fwd_workspace_bytes(int64_t T, int64_t D, int64_t H, int64_t O, int dtype);
+int64_t fsa_gated_bwd_workspace_bytes(int64_t T, int64_t D, int64_t H, int64_t O, int dtype);
+int fsa_gated_fwd(const void* x, int64_t x_stride, const void* w_gate, int64_t gate_stride, const void* w_up, int64_t up_stride,
+                  const void* w_down, int64_t down_stride, int dtype, int activation, int64_t T, int64_t D, int64_t H, int64_t O,
+                  void* out_y, void* workspace, int64_t workspace_bytes, void* stream);
+int fsa_gated_bwd(const void* grad_y, int64_t grad_y_stride, const void* x, int64_t x_stride,
+                  const void* w_gate, int64_t gate_stride, const void* w_up, int64_t up_stride, const void* w_down, int64_t down_stride,
+                  int dtype, int activation, int64_t T, int64_t D, int64_t H, int64_t O,
+                  void* grad_x, void* grad_gate, void* grad_up, void* grad_down,
+                  void* workspace, int64_t workspace_bytes, void* stream);
+
+/*
+ * Orthogonalised matrices:  X = G / (|G|_F + eps);  for every step's (a, b, c):  A = X X^T, X = a X + (b A + c A A) X  (of the
+ * transpose where G has more rows than columns);  out = scale * X.  Singular vectors stay, singular values follow a s + b s^3 + c s^5.
+ *   g [B,M,N]          fsa_dtype `dtype`, matrices `batch_stride` and rows `stride` elements apart
+ *   coefficients       HOST [steps,3];  1 <= steps <= FSA_ORTHO_STEPS, each of a magnitude up to FSA_ORTHO_COEFFICIENT
+ *   eps, scale         finite, eps not negative;  0 <= B <= FSA_ORTHO_BMAX, 1 <= M, N <= FSA_ORTHO_MOST
+ *   out [B,M,N]        `dtype`
+ * X is held to 23 bits of every element down to 2^-24 or so, singular values up to about 2.  A matrix of zeros (with any eps) has zeros; one
+ * that holds an infinity or NaN is NaN throughout, whatever the others hold.
+ */
+enum { FSA_ORTHO_STEPS = 32, FSA_ORTHO_COEFFICIENT = 16, FSA_ORTHO_BMAX = 65535, FSA_ORTHO_MOST = 1 << 16 };
+
+int64_t fsa_orthogonalize_workspace_bytes(int64_t B, int64_t M, int64_t N, int dtype);
+int fsa_orthogonalize(const void* g, int64_t batch_stride, int64_t stride, int dtype, int64_t B, int64_t M, int64_t N,
+                      const float* coefficients, int32_t steps, float eps, float scale,
+                      void* out, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Static, never-freed description of a status code. */
 const char* fsa_status_string(int status);
 

@@ -151,3 +151,53 @@ def fused_distillation(h: torch.Tensor, w: torch.Tensor, teacher_ids: torch.Tens
     are known: teacher_ids [T,K] int32 (negative: an empty slot) and teacher_logits [T,K].  `temperature` divides both
     sides' scores; the loss is not multiplied by its square.  The teacher gets no gradient."""
     return _class_loss(h, w, teacher_ids, teacher_logits, float(temperature), float(scale))
+
+
+class _ResidualNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        y, s = binding.fsa_norm_fwd(x, weight, residual, eps)
+        ctx.save_for_backward(x if residual is None else s, weight)
+        ctx.eps = eps
+        ctx.set_materialize_grads(False)
+        return y if residual is None else (y, s)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_y, grad_s=None):
+        s, weight = ctx.saved_tensors
+        want_x, want_weight = ctx.needs_input_grad[0] or ctx.needs_input_grad[2], ctx.needs_input_grad[1]
+        grad_x, grad_weight = binding.fsa_norm_bwd(None if grad_y is None else grad_y.contiguous(),
+                                                   None if grad_s is None else grad_s.contiguous(), s, weight, ctx.eps,
+                                                   want_x=want_x, want_weight=want_weight)
+        return (grad_x if ctx.needs_input_grad[0] else None, grad_weight, grad_x if ctx.needs_input_grad[2] else None, None)
+
+
+def fused_residual_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, *, eps: float = 1e-6
+                        ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Differentiable root-mean-square norm of the rows s = x + residual [T,D], times weight [D].  Returns (y, s): what the next
+    layer takes and what its answer is added to.  Without a residual s is x itself."""
+    if residual is None:
+        return _ResidualNorm.apply(x, weight, None, float(eps)), x
+    return _ResidualNorm.apply(x, weight, residual, float(eps))
+
+
+class _GatedFeedForward(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, w_down, activation):
+        ctx.save_for_backward(x, w_gate, w_up, w_down)
+        ctx.activation = activation
+        return binding.fsa_gated_fwd(x, w_gate, w_up, w_down, activation=activation)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_y):
+        grads = binding.fsa_gated_bwd(grad_y.contiguous(), *ctx.saved_tensors, activation=ctx.activation, want=ctx.needs_input_grad[:4])
+        return (*grads, None)
+
+
+def fused_gated_feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
+                             activation: str = "silu") -> torch.Tensor:
+    """Differentiable gated feed-forward block (act(x w_gate^T) * (x w_up^T)) w_down^T of rows x [T,D]: w_gate, w_up [H,D],
+    w_down [O,H], one type.  No row of hidden elements is kept for the backward, which makes them again."""
+    return _GatedFeedForward.apply(x, w_gate, w_up, w_down, activation)

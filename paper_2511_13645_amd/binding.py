@@ -42,7 +42,10 @@ EXPORTS = ("fsa_sample_mean_fwd", "fsa_mean_replay_fwd", "fsa_mean_bwd", "fsa_me
            "fsa_mean_bwd_dense", "fsa_mean_bwd_dense_workspace_bytes", "fsa_mean_bwd_dense_pays",
            "fsa_sample_wmean_fwd", "fsa_wmean_replay_fwd", "fsa_wmean_bwd",
            "fsa_class_fwd_workspace_bytes", "fsa_class_bwd_workspace_bytes",
-           "fsa_xent_fwd", "fsa_xent_bwd", "fsa_distill_fwd", "fsa_distill_bwd")
+           "fsa_xent_fwd", "fsa_xent_bwd", "fsa_distill_fwd", "fsa_distill_bwd",
+           "fsa_norm_fwd", "fsa_norm_bwd", "fsa_norm_bwd_workspace_bytes",
+           "fsa_gated_fwd", "fsa_gated_bwd", "fsa_gated_fwd_workspace_bytes", "fsa_gated_bwd_workspace_bytes",
+           "fsa_orthogonalize", "fsa_orthogonalize_workspace_bytes")
 
 _lib: Optional[ctypes.CDLL] = None
 _class_host = None                              # the module _fsa_class_host, likewise
@@ -128,6 +131,23 @@ def lib() -> ctypes.CDLL:
         L.fsa_distill_fwd.restype = ci
         L.fsa_distill_bwd.argtypes = [vp, vp, i64, vp, i64, ci, i64, i64, i64, f32, f32, vp, vp, ci, i32, vp, vp, vp, vp, vp, i64, vp]
         L.fsa_distill_bwd.restype = ci
+        L.fsa_norm_fwd.argtypes = [vp, i64, vp, i64, vp, ci, ci, i64, i64, f32, vp, vp, vp]
+        L.fsa_norm_fwd.restype = ci
+        L.fsa_norm_bwd_workspace_bytes.argtypes = [i64, i64, ci]
+        L.fsa_norm_bwd_workspace_bytes.restype = i64
+        L.fsa_norm_bwd.argtypes = [vp, vp, vp, i64, vp, ci, ci, i64, i64, f32, vp, vp, vp, i64, vp]
+        L.fsa_norm_bwd.restype = ci
+        for name in ("fsa_gated_fwd_workspace_bytes", "fsa_gated_bwd_workspace_bytes"):
+            getattr(L, name).argtypes = [i64, i64, i64, i64, ci]
+            getattr(L, name).restype = i64
+        L.fsa_gated_fwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, ci, ci, i64, i64, i64, i64, vp, vp, i64, vp]
+        L.fsa_gated_fwd.restype = ci
+        L.fsa_gated_bwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, ci, ci, i64, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp]
+        L.fsa_gated_bwd.restype = ci
+        L.fsa_orthogonalize_workspace_bytes.argtypes = [i64, i64, i64, ci]
+        L.fsa_orthogonalize_workspace_bytes.restype = i64
+        L.fsa_orthogonalize.argtypes = [vp, i64, i64, ci, i64, i64, i64, vp, i32, f32, f32, vp, vp, i64, vp]
+        L.fsa_orthogonalize.restype = ci
         L.fsa_status_string.argtypes = [ci]
         L.fsa_status_string.restype = ctypes.c_char_p
         _lib, _host, _class_host = L, _load_host(L), _load_class_host(L)
@@ -891,3 +911,193 @@ def fsa_class_bwd_workspace_bytes(T: int, V: int, D: int, dtype: torch.dtype, K:
                                   with_grad_w: bool = True) -> int:
     """Workspace bytes of fsa_xent_bwd and fsa_distill_bwd; `with_row_grad`: grad_h is wanted and no row_grad given."""
     return lib().fsa_class_bwd_workspace_bytes(T, V, D, _FLOAT_TYPE[dtype], K, int(with_row_grad), int(with_grad_w))
+
+
+# ----------------------------------------------------------------------------------------
+# the block between a mean and its loss, and the update of its matrices
+# ----------------------------------------------------------------------------------------
+FSA_NORM_DMAX = 16384
+FSA_GATED_MOST = 1 << 16
+_ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
+ORTHOGONAL_COEFFICIENTS = (3.4445, -4.7750, 2.0315)     # singular values of 0.01 ... 1 go to 0.7 ... 1.2 in five steps
+
+
+@contextlib.contextmanager
+def _on(t: torch.Tensor, stream: Optional[torch.cuda.Stream]):
+    """What a call allocates and launches belongs to `t`'s device and, where given, to the call's stream."""
+    with contextlib.ExitStack() as stack:
+        if torch.cuda.current_device() != t.get_device():
+            stack.enter_context(torch.cuda.device(t.device))
+        stack.enter_context(_allocating(stream))
+        yield
+
+
+def _vector(t: torch.Tensor, name: str, n: int) -> None:
+    _need(t, name)
+    _x_dtype(t)
+    _shape(t, name, (n,))
+
+
+def _same_type(ref: torch.Tensor, ref_name: str, *named) -> None:
+    for t, name in named:
+        if t is not None and t.dtype != ref.dtype:
+            raise TypeError("%s and %s must have one type, got %s and %s" % (ref_name, name, ref.dtype, t.dtype))
+
+
+def fsa_norm_fwd(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-6, *,
+                 stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """Root-mean-square norm of rows s = x + residual [T,D] (rounded to their type), times weight [D] (of any of the three types).
+    Returns (y, s | None), s where there is a residual.  `stream`: see fsa_xent_fwd."""
+    xs = _rows(x, "x")
+    code = _x_dtype(x)
+    T, D = x.shape
+    _vector(weight, "weight", D)
+    rs = 0
+    if residual is not None:
+        rs = _rows(residual, "residual")
+        _same_type(x, "x", (residual, "residual"))
+        _shape(residual, "residual", x.shape)
+    _same_device(x, (weight, "weight"), (residual, "residual"))
+    with _on(x, stream):
+        y = torch.empty((T, D), dtype=x.dtype, device=x.device)
+        s = torch.empty_like(y) if residual is not None else None
+        rc = lib().fsa_norm_fwd(_ptr(x), xs, _ptr(residual), rs, _ptr(weight), code, _x_dtype(weight), T, D, float(eps),
+                                _ptr(y), _ptr(s), _stream(stream, x))
+    if rc != FSA_OK:
+        raise FsaError(rc, "fsa_norm_fwd")
+    return y, s
+
+
+def fsa_norm_bwd(grad_y: Optional[torch.Tensor], grad_s: Optional[torch.Tensor], s: torch.Tensor, weight: torch.Tensor,
+                 eps: float = 1e-6, *, want_x: bool = True, want_weight: bool = True, workspace: Optional[torch.Tensor] = None,
+                 stream: Optional[torch.cuda.Stream] = None) -> Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Gradients (grad_x | None, grad_weight | None) of fsa_norm_fwd; grad_x is the residual's as well.  s [T,D]: the sum that
+    the forward returned, or x where there was no residual.  grad_y, grad_s [T,D]: None for none.  `workspace`: see
+    fsa_norm_bwd_workspace_bytes; torch's memory without one."""
+    stride = _rows(s, "s")
+    code = _x_dtype(s)
+    T, D = s.shape
+    _vector(weight, "weight", D)
+    for g, name in ((grad_y, "grad_y"), (grad_s, "grad_s")):
+        if g is not None:
+            _need(g, name, s.dtype)
+            _shape(g, name, s.shape)
+    _same_device(s, (weight, "weight"), (grad_y, "grad_y"), (grad_s, "grad_s"))
+    L = lib()
+    with _on(s, stream):
+        grad_x = torch.empty((T, D), dtype=s.dtype, device=s.device) if want_x else None
+        grad_weight = torch.empty((D,), dtype=weight.dtype, device=s.device) if want_weight else None
+        ws = _class_workspace(workspace, L.fsa_norm_bwd_workspace_bytes(T, D, code) if want_weight else 0, s)
+        rc = L.fsa_norm_bwd(_ptr(grad_y), _ptr(grad_s), _ptr(s), stride, _ptr(weight), code, _x_dtype(weight), T, D, float(eps),
+                            _ptr(grad_x), _ptr(grad_weight), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, s))
+    if rc != FSA_OK:
+        raise FsaError(rc, "fsa_norm_bwd")
+    return grad_x, grad_weight
+
+
+def fsa_norm_bwd_workspace_bytes(T: int, D: int, dtype: torch.dtype) -> int:
+    """Workspace bytes of fsa_norm_bwd; 0 for sizes that it refuses."""
+    return lib().fsa_norm_bwd_workspace_bytes(T, D, _FLOAT_TYPE[dtype])
+
+
+def _gated_operands(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, activation: str):
+    """Checked arguments of the gated block: (pointers, strides, type, activation and sizes), (T, D, H, O)."""
+    act = _ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError("activation must be one of %s, got %r" % (", ".join(sorted(_ACTIVATIONS)), activation))
+    named = ((x, "x"), (w_gate, "w_gate"), (w_up, "w_up"), (w_down, "w_down"))
+    strides = [_rows(t, name) for t, name in named]
+    code = _x_dtype(x)
+    _same_type(x, "x", *named[1:])
+    _same_device(x, *named[1:])
+    (T, D), H, O = x.shape, w_gate.shape[0], w_down.shape[0]
+    if H < 1 or O < 1:
+        raise ValueError("w_gate and w_down must have rows")
+    _shape(w_gate, "w_gate", (H, D))
+    _shape(w_up, "w_up", (H, D))
+    _shape(w_down, "w_down", (O, H))
+    lead = [a for (t, _), stride in zip(named, strides) for a in (_ptr(t), stride)]
+    return (*lead, code, act, T, D, H, O), (T, D, H, O)
+
+
+def fsa_gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *, activation: str = "silu",
+                  workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Gated feed-forward block (act(x w_gate^T) * (x w_up^T)) w_down^T: x [T,D], w_gate and w_up [H,D], w_down [O,H], all of one
+    type; activation "silu", "gelu" (by the error function) or "relu".  `workspace`: see fsa_gated_fwd_workspace_bytes; torch's
+    memory without one.  `stream`: see fsa_xent_fwd."""
+    lead, (T, D, H, O) = _gated_operands(x, w_gate, w_up, w_down, activation)
+    L = lib()
+    with _on(x, stream):
+        y = torch.empty((T, O), dtype=x.dtype, device=x.device)
+        ws = _class_workspace(workspace, L.fsa_gated_fwd_workspace_bytes(T, D, H, O, lead[8]), x)
+        rc = L.fsa_gated_fwd(*lead, _ptr(y), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, x))
+    if rc != FSA_OK:
+        raise FsaError(rc, "fsa_gated_fwd")
+    return y
+
+
+def fsa_gated_bwd(grad_y: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
+                  activation: str = "silu", want: Sequence[bool] = (True, True, True, True),
+                  workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Gradients of fsa_gated_fwd by x, w_gate, w_up and w_down from grad_y [T,O]; None where not wanted."""
+    lead, (T, D, H, O) = _gated_operands(x, w_gate, w_up, w_down, activation)
+    gs = _rows(grad_y, "grad_y")
+    _same_type(x, "x", (grad_y, "grad_y"))
+    _shape(grad_y, "grad_y", (T, O))
+    _same_device(x, (grad_y, "grad_y"))
+    L = lib()
+    with _on(x, stream):
+        grads = tuple(torch.empty(t.shape, dtype=x.dtype, device=x.device) if w else None
+                      for t, w in zip((x, w_gate, w_up, w_down), want))
+        ws = _class_workspace(workspace, L.fsa_gated_bwd_workspace_bytes(T, D, H, O, lead[8]), x)
+        rc = L.fsa_gated_bwd(_ptr(grad_y), gs, *lead, *(_ptr(g) for g in grads), _ptr(ws), ws.numel() * ws.element_size(),
+                             _stream(stream, x))
+    if rc != FSA_OK:
+        raise FsaError(rc, "fsa_gated_bwd")
+    return grads
+
+
+def fsa_gated_fwd_workspace_bytes(T: int, D: int, H: int, O: int, dtype: torch.dtype) -> int:
+    """Workspace bytes of fsa_gated_fwd; 0 for sizes that it refuses."""
+    return lib().fsa_gated_fwd_workspace_bytes(T, D, H, O, _FLOAT_TYPE[dtype])
+
+
+def fsa_gated_bwd_workspace_bytes(T: int, D: int, H: int, O: int, dtype: torch.dtype) -> int:
+    """Workspace bytes of fsa_gated_bwd; 0 for sizes that it refuses."""
+    return lib().fsa_gated_bwd_workspace_bytes(T, D, H, O, _FLOAT_TYPE[dtype])
+
+
+def fsa_orthogonalize(g: torch.Tensor, coefficients: Sequence = ORTHOGONAL_COEFFICIENTS, steps: int = 5, *, eps: float = 1e-7,
+                      scale: float = 1.0, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
+                      ) -> torch.Tensor:
+    """`scale` times the orthogonalised matrix g [M,N], or matrices [B,M,N], by Newton-Schulz steps: X = g / (|g| + eps), then
+    X = a X + (b A + c A A) X with A = X X^T.  `coefficients`: (a, b, c) of every step, or one triple for each of `steps` steps.
+    `workspace`: see fsa_orthogonalize_workspace_bytes; torch's memory without one.  `stream`: see fsa_xent_fwd."""
+    if not g.is_cuda:
+        raise ValueError("g must live on the GPU")
+    if g.dim() not in (2, 3) or g.shape[-1] < 1 or g.shape[-2] < 1:
+        raise ValueError("g must be a matrix or a batch of matrices, got %s" % (tuple(g.shape),))
+    code = _x_dtype(g)
+    if len(coefficients) and not isinstance(coefficients[0], (tuple, list)):
+        coefficients = [tuple(coefficients)] * int(steps)
+    if any(len(c) != 3 for c in coefficients):
+        raise ValueError("coefficients must be triples")
+    B, (M, N) = (g.shape[0] if g.dim() == 3 else 1), g.shape[-2:]
+    if (g.stride(-1) != 1 and N > 1) or (M > 1 and g.stride(-2) < N):
+        raise ValueError("g must have contiguous rows that do not overlap")
+    stride = g.stride(-2) if M > 1 else N
+    host = (ctypes.c_float * max(1, 3 * len(coefficients)))(*(float(x) for c in coefficients for x in c))
+    L = lib()
+    with _on(g, stream):
+        out = torch.empty(g.shape, dtype=g.dtype, device=g.device)
+        ws = _class_workspace(workspace, L.fsa_orthogonalize_workspace_bytes(B, M, N, code), g)
+        rc = L.fsa_orthogonalize(_ptr(g), g.stride(0) if g.dim() == 3 else 0, stride, code, B, M, N, host, len(coefficients),
+                                 float(eps), float(scale), _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, g))
+    if rc != FSA_OK:
+        raise FsaError(rc, "fsa_orthogonalize")
+    return out
+
+
+def fsa_orthogonalize_workspace_bytes(B: int, M: int, N: int, dtype: torch.dtype) -> int:
+    """Workspace bytes of fsa_orthogonalize; 0 for sizes that it refuses."""
+    return lib().fsa_orthogonalize_workspace_bytes(B, M, N, _FLOAT_TYPE[dtype])

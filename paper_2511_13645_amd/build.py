@@ -13,8 +13,10 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfsa_hip.so")
 ABI_HEADER = os.path.normpath(os.path.join(HERE, "..", "include", "fsa.h"))
 SOURCES = ["fsa_api.hip", "fsa_fwd.hip", "fsa_bwd.hip", "fsa_bwd_sorted.hip", "fsa_bwd_owned.hip", "fsa_bwd_dense.hip", "fsa_wbwd.hip",
-           "fsa_class_api.hip", "fsa_class_f32.hip", "fsa_class_bf16.hip", "fsa_class_f16.hip"]
-HEADERS = ["fsa_device.hip.h", "fsa_atomic_rows.hip.h", "fsa_internal.h", "fsa_layout.h", "fsa_class.h", "fsa_class_kernels.hip.h", ABI_HEADER]
+           "fsa_class_api.hip", "fsa_class_f32.hip", "fsa_class_bf16.hip", "fsa_class_f16.hip",
+           "fsa_block_api.hip", "fsa_norm.hip", "fsa_gated_f32.hip", "fsa_gated_bf16.hip", "fsa_gated_f16.hip", "fsa_orthogonal.hip"]
+HEADERS = ["fsa_device.hip.h", "fsa_atomic_rows.hip.h", "fsa_internal.h", "fsa_layout.h", "fsa_class.h", "fsa_class_kernels.hip.h",
+           "fsa_block.h", "fsa_block_kernels.h", "fsa_product.hip.h", "fsa_gated_kernels.hip.h", ABI_HEADER]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

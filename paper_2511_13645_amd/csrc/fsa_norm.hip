@@ -1,0 +1,274 @@
+// Root-mean-square norm of rows, with the residual's addition before it, and its gradients.
+//
+//   s = x + residual (rounded to the type, as the next layers see it),  y = s * rstd * w,  rstd = (mean s^2 + eps)^-1/2
+//   ds = gs + rstd * (gy w - s^ * mean(gy w s^)),  s^ = s rstd,         dw = sum over rows of gy s^
+//
+// Bound by memory: every element is read once, held in registers by the lanes of its row, and written once; the backward makes
+// rstd again from the row that it reads anyway.  Sums over a row are fp32 and meet by shuffles (through LDS for rows of more than
+// 1024 elements); dw is summed by lane over the rows of a workgroup, written as one part a workgroup and joined in order
+// by a second launch, so that no order of atomics shows.
+#include "fsa_block_kernels.h"
+#include "fsa_product.hip.h"
+
+#include <type_traits>
+
+namespace fsa {
+namespace {
+
+template <int KIND> struct Row {
+    using Elem = typename std::conditional<KIND == 0, float, uint16_t>::type;
+    static constexpr int PER = KIND == 0 ? 4 : 8;       // elements of a 16-byte piece
+};
+
+template <int KIND> __device__ __forceinline__ float number_of(typename Row<KIND>::Elem e) {
+    if constexpr (KIND == 0) return e;
+    else return product::as_float<KIND == 2>(e);
+}
+
+// A piece of a row from element c on, zeros behind D.
+template <int KIND> __device__ __forceinline__ void load(const void* base, int64_t at, int c, int D, float (&out)[Row<KIND>::PER]) {
+    using Elem = typename Row<KIND>::Elem;
+    constexpr int PER = Row<KIND>::PER;
+    const Elem* p = static_cast<const Elem*>(base) + at + c;
+    Elem e[PER];
+    if (c + PER <= D) __builtin_memcpy(e, p, 16);
+    else {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) e[j] = c + j < D ? p[j] : Elem(0);
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) out[j] = number_of<KIND>(e[j]);
+}
+template <int KIND> __device__ __forceinline__ void store(void* base, int64_t at, int c, int D, const float (&x)[Row<KIND>::PER]) {
+    using Elem = typename Row<KIND>::Elem;
+    constexpr int PER = Row<KIND>::PER;
+    Elem* p = static_cast<Elem*>(base) + at + c;
+    Elem e[PER];
+    if constexpr (KIND == 0) __builtin_memcpy(e, x, sizeof(e));
+    else {
+        uint32_t w[PER / 2];
+#pragma unroll
+        for (int j = 0; j < PER / 2; ++j) w[j] = product::pack2<KIND == 2>(x[2 * j], x[2 * j + 1]);
+        __builtin_memcpy(e, w, sizeof(e));
+    }
+    if (c + PER <= D) __builtin_memcpy(p, e, 16);
+    else {
+#pragma unroll
+        for (int j = 0; j < PER; ++j) if (c + j < D) p[j] = e[j];
+    }
+}
+__device__ __forceinline__ float weight_at(const void* w, int kind, int c, int D) {
+    if (c >= D) return 0.0f;
+    if (kind == 0) return static_cast<const float*>(w)[c];
+    const uint32_t bits = static_cast<const uint16_t*>(w)[c];
+    return kind == 1 ? product::as_float<false>(bits) : product::as_float<true>(bits);
+}
+
+// Sum of x over the LANES lanes of a row, in every one of them.
+template <int LANES> __device__ __forceinline__ float row_sum(float x, float* lds) {
+#pragma unroll
+    for (int d = 1; d < (LANES < 64 ? LANES : 64); d *= 2) x += __shfl_xor(x, d, 64);
+    if constexpr (LANES > 64) {
+        constexpr int WAVES = LANES / 64;
+        __syncthreads();                                // (who still reads the last sum's)
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = 0.0f;
+        const int first = (threadIdx.x >> 6) / WAVES * WAVES;
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) x += lds[first + i];
+    }
+    return x;
+}
+
+template <int KIND, int LANES, int NV>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(NormArgs a) {
+    constexpr int PER = Row<KIND>::PER, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES;
+    __shared__ float lds[THREADS / 64];
+    const int lane = threadIdx.x % LANES, D = (int)a.D;
+    float w[NV][PER];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) w[v][j] = weight_at(a.weight, a.weight_kind, (v * LANES + lane) * PER + j, D);
+    // (every lane of a workgroup makes every turn: the sums of long rows meet at barriers)
+    for (int64_t t0 = (int64_t)blockIdx.x * ROWS; t0 < a.T; t0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t t = t0 + threadIdx.x / LANES;
+        const bool live = t < a.T;
+        float x[NV][PER];
+        float sum = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * LANES + lane) * PER;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) x[v][j] = 0.0f;
+            if (live && c < D) {
+                load<KIND>(a.x, t * a.x_stride, c, D, x[v]);
+                if (a.residual) {
+                    float r[PER];
+                    load<KIND>(a.residual, t * a.residual_stride, c, D, r);
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) x[v][j] += r[j];
+                    if constexpr (KIND != 0) {
+#pragma unroll
+                        for (int j = 0; j < PER; j += 2) {
+                            const uint32_t both = product::pack2<KIND == 2>(x[v][j], x[v][j + 1]);
+                            x[v][j] = product::as_float<KIND == 2>(both & 0xffff);
+                            x[v][j + 1] = product::as_float<KIND == 2>(both >> 16);
+                        }
+                    }
+                    store<KIND>(a.s, t * a.D, c, D, x[v]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < PER; ++j) sum = fmaf(x[v][j], x[v][j], sum);
+        }
+        const float rstd = 1.0f / sqrtf(row_sum<LANES>(sum, lds) / (float)D + a.eps);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * LANES + lane) * PER;
+            if (!live || c >= D) continue;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) x[v][j] = x[v][j] * rstd * w[v][j];
+            store<KIND>(a.y, t * a.D, c, D, x[v]);
+        }
+    }
+}
+
+template <int KIND, int LANES, int NV>
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(NormArgs a) {
+    constexpr int PER = Row<KIND>::PER, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES;
+    __shared__ float lds[THREADS / 64];
+    __shared__ float join[ROWS > 1 ? LANES * NV * PER : 1];
+    const int lane = threadIdx.x % LANES, D = (int)a.D;
+    float w[NV][PER], dw[NV][PER];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            w[v][j] = weight_at(a.weight, a.weight_kind, (v * LANES + lane) * PER + j, D);
+            dw[v][j] = 0.0f;
+        }
+    for (int64_t t0 = (int64_t)blockIdx.x * ROWS; t0 < a.T; t0 += (int64_t)gridDim.x * ROWS) {
+        const int64_t t = t0 + threadIdx.x / LANES;
+        const bool live = t < a.T;
+        float s[NV][PER], g[NV][PER], gs[NV][PER];
+        float sum = 0.0f, dot = 0.0f;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * LANES + lane) * PER;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) s[v][j] = g[v][j] = gs[v][j] = 0.0f;
+            if (live && c < D) {
+                load<KIND>(a.x, t * a.x_stride, c, D, s[v]);
+                if (a.grad_y) load<KIND>(a.grad_y, t * a.D, c, D, g[v]);
+                if (a.grad_s) load<KIND>(a.grad_s, t * a.D, c, D, gs[v]);
+            }
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                sum = fmaf(s[v][j], s[v][j], sum);
+                dot = fmaf(g[v][j] * w[v][j], s[v][j], dot);
+            }
+        }
+        const float rstd = 1.0f / sqrtf(row_sum<LANES>(sum, lds) / (float)D + a.eps);
+        const float mean = row_sum<LANES>(dot, lds) * rstd / (float)D;         // of gy w s^
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * LANES + lane) * PER;
+            if (!live || c >= D) continue;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const float unit = s[v][j] * rstd;
+                dw[v][j] = fmaf(g[v][j], unit, dw[v][j]);
+                s[v][j] = fmaf(rstd, fmaf(-unit, mean, g[v][j] * w[v][j]), gs[v][j]);
+            }
+            if (a.y) store<KIND>(a.y, t * a.D, c, D, s[v]);
+        }
+    }
+    if (!a.grad_weight) return;
+    // rows of a workgroup one after another, in LDS
+    float* out = a.parts + (int64_t)blockIdx.x * D;
+    if constexpr (ROWS == 1) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int j = 0; j < PER; ++j)
+                if (const int c = (v * LANES + lane) * PER + j; c < D) out[c] = dw[v][j];
+    } else {
+        // lanes of one wave that have the same columns join first
+#pragma unroll
+        for (int d = LANES; d < 64; d *= 2)
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int j = 0; j < PER; ++j) dw[v][j] += __shfl_xor(dw[v][j], d, 64);
+        for (int wave = 0; wave < THREADS / 64; ++wave) {
+            if ((int)(threadIdx.x >> 6) == wave && (int)(threadIdx.x & 63) < LANES)
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) {
+                        const int c = (v * LANES + lane) * PER + j;
+                        join[c] = wave == 0 ? dw[v][j] : join[c] + dw[v][j];
+                    }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < D; c += THREADS) out[c] = join[c];
+    }
+}
+
+// grad_weight from the workgroups' parts: 16 columns a workgroup, 16 lanes to each.
+__global__ __launch_bounds__(256) void norm_join_kernel(const float* parts, int64_t count, int64_t D, void* out, int kind) {
+    __shared__ float lds[16][17];
+    const int col = threadIdx.x & 15, share = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 16 + col;
+    float x = 0.0f;
+    if (c < D)
+        for (int64_t i = share; i < count; i += 16) x += parts[i * D + c];
+    lds[share][col] = x;
+    __syncthreads();
+    if (share != 0 || c >= D) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) x += lds[i][col];
+    if (kind == 0) static_cast<float*>(out)[c] = x;
+    else static_cast<uint16_t*>(out)[c] = (uint16_t)((kind == 1 ? product::pack2<false>(x, 0.0f) : product::pack2<true>(x, 0.0f)) & 0xffff);
+}
+
+template <int KIND, int LANES, int NV> hipError_t launch(const NormArgs& a, bool forward, hipStream_t st) {
+    const NormPlan p = norm_plan(a.D, KIND == 0 ? 4 : 2);
+    if (forward) {
+        const int64_t blocks = cut_into(a.T, p.rows), most = 256 * (p.threads > 256 ? 2 : 8);     // as many as the chip holds at a time
+        norm_fwd_kernel<KIND, LANES, NV><<<dim3((unsigned)(blocks < most ? blocks : most)), dim3(p.threads), 0, st>>>(a);
+        return hipGetLastError();
+    }
+    const int64_t parts = norm_parts(a.T, a.D, KIND == 0 ? 4 : 2);
+    norm_bwd_kernel<KIND, LANES, NV><<<dim3((unsigned)parts), dim3(p.threads), 0, st>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    if (a.grad_weight)
+        norm_join_kernel<<<dim3((unsigned)cut_into(a.D, 16)), dim3(256), 0, st>>>(a.parts, parts, a.D, a.grad_weight, a.weight_kind);
+    return hipGetLastError();
+}
+template <int KIND, int LANES> hipError_t by_pieces(const NormArgs& a, bool forward, hipStream_t st) {
+    const int pieces = norm_plan(a.D, KIND == 0 ? 4 : 2).pieces;
+    if constexpr (KIND == 0) if (pieces == 4) return launch<KIND, LANES, 4>(a, forward, st);
+    return pieces == 2 ? launch<KIND, LANES, 2>(a, forward, st) : launch<KIND, LANES, 1>(a, forward, st);
+}
+template <int KIND> hipError_t by_lanes(const NormArgs& a, bool forward, hipStream_t st) {
+    switch (norm_plan(a.D, KIND == 0 ? 4 : 2).lanes) {
+        case 4: return by_pieces<KIND, 4>(a, forward, st);
+        case 16: return by_pieces<KIND, 16>(a, forward, st);
+        case 64: return by_pieces<KIND, 64>(a, forward, st);
+        case 256: return by_pieces<KIND, 256>(a, forward, st);
+        default: return by_pieces<KIND, 1024>(a, forward, st);
+    }
+}
+hipError_t by_kind(const NormArgs& a, bool forward, hipStream_t st) {
+    return a.kind == 0 ? by_lanes<0>(a, forward, st) : a.kind == 1 ? by_lanes<1>(a, forward, st) : by_lanes<2>(a, forward, st);
+}
+
+}  // namespace
+
+hipError_t norm_forward(const NormArgs& a, hipStream_t st) { return by_kind(a, true, st); }
+hipError_t norm_backward(const NormArgs& a, hipStream_t st) { return by_kind(a, false, st); }
+
+}  // namespace fsa

@@ -1,0 +1,208 @@
+// Orthogonalised updates: X = G / (|G| + eps), then steps of X = a X + P X with A = X X^T, P = b A + c A^2.
+//
+// Singular values of X stay as they are paired with their vectors and are moved towards one by the steps' polynomial.  What bounds
+// it is the matrix cores: 2 m^2 n + m^3 multiplications a step.  X, A and P are two fp16 planes each, whose three products carry 23
+// bits: small singular values grow by up to a^steps, and with them what was rounded beside large ones, so that 16 bits of X
+// would leave nothing of directions a hundredth as strong as the strongest.
+#include "fsa_block_kernels.h"
+#include "fsa_product.hip.h"
+
+#include <type_traits>
+
+namespace fsa {
+namespace {
+
+using namespace product;
+
+template <int EDGE> using OrthoTile = Tile<2, true, EDGE, EDGE, EDGE == 128 ? 32 : 64, 2, 2>;
+template <int KIND> using ElemOf = typename std::conditional<KIND == 0, float, uint16_t>::type;
+constexpr float two_to(int e) { return e > 0 ? 2.0f * two_to(e - 1) : e < 0 ? 0.5f * two_to(e + 1) : 1.0f; }
+
+template <int KIND> __device__ __forceinline__ float number(ElemOf<KIND> e) {
+    if constexpr (KIND == 0) return e;
+    else return as_float<KIND == 2>(e);
+}
+
+// Squares of a matrix, summed in 64 bits: gradients of 1e-30 have norms too.
+template <int KIND> __global__ __launch_bounds__(256) void squares_kernel(OrthoArgs a) {
+    __shared__ double lds[4];
+    const ElemOf<KIND>* g = static_cast<const ElemOf<KIND>*>(a.g) + blockIdx.y * a.batch_stride;
+    double sum = 0.0;
+    const int64_t all = a.s.M * a.s.N;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const double x = number<KIND>(g[i / a.s.N * a.stride + i % a.s.N]);
+        sum = fma(x, x, sum);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        reinterpret_cast<double*>(a.ws + a.plan.squares)[blockIdx.y * kOrthoPeaks + blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+__device__ __forceinline__ float inverse_norm(const OrthoArgs& a, unsigned batch) {
+    double sum = reinterpret_cast<const double*>(a.ws + a.plan.squares)[batch * kOrthoPeaks + (threadIdx.x & 63)];
+    static_assert(kOrthoPeaks == 64, "one a lane");
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
+    const double norm = sqrt(sum) + (double)a.eps;
+    return norm > 0.0 ? (float)(1.0 / norm) : norm == 0.0 ? 0.0f : __builtin_nanf("");
+}
+
+// Planes of the first X, 64 x 64 of it a workgroup; of a tall matrix its transpose.
+template <int KIND> __global__ __launch_bounds__(256) void first_kernel(OrthoArgs a) {
+    __shared__ float tile[64][65];
+    const unsigned batch = blockIdx.z;
+    const float unit = inverse_norm(a, batch);
+    const bool tall = a.s.M > a.s.N;
+    const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;      // of the matrix as it is given
+    const ElemOf<KIND>* g = static_cast<const ElemOf<KIND>*>(a.g) + batch * a.batch_stride;
+    for (int i = threadIdx.x; i < 64 * 64; i += 256) {
+        const int64_t r = r0 + i / 64, c = c0 + i % 64;
+        tile[i / 64][i % 64] = r < a.s.M && c < a.s.N ? number<KIND>(g[r * a.stride + c]) * unit * two_to(kUnitX) : 0.0f;
+    }
+    __syncthreads();
+    const int64_t m = a.plan.m, n = a.plan.n, n8 = a.plan.n8, plane = m * n8;
+    uint16_t* x = reinterpret_cast<uint16_t*>(a.ws + a.plan.x[0]) + batch * 2 * plane;
+    for (int i = threadIdx.x; i < 64 * 16; i += 256) {
+        const int row = i / 16, col = i % 16 * 4;
+        const int64_t xm = (tall ? c0 : r0) + row, xn = (tall ? r0 : c0) + col;
+        if (xm >= m) continue;
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = tall ? tile[col + j][row] : tile[row][col + j];
+        store_planes<2, true>(x, plane, xm * n8 + xn, xn, n, v);
+    }
+}
+
+struct StepArgs {
+    const uint16_t *x, *sq, *poly;                      // planes of X, A, P; a matrix' planes are together
+    uint16_t* to;
+    void* out;                                          // of the last step, in the caller's type
+    int64_t m, n, m8, n8;
+    float a, b, c, scale;
+    unsigned mt, nt;
+    bool tall, grid;
+};
+
+// W elements of two planes from `at` on.
+template <int W> __device__ __forceinline__ void load_planes(const uint16_t* p, int64_t plane, int64_t at, int64_t n, int64_t end, float (&x)[W]) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) {
+        u32x2 hi = {}, lo = {};
+        if (n + i < end) {
+            hi = *reinterpret_cast<const u32x2*>(p + at + i);
+            lo = *reinterpret_cast<const u32x2*>(p + plane + at + i);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int s = j % 2 * 16;
+            x[i + j] = as_float<true>(hi[j / 2] >> s & 0xffff) + as_float<true>(lo[j / 2] >> s & 0xffff);
+        }
+    }
+}
+
+enum { kGram, kPoly, kUpdate };
+template <class T, int WHAT, int KIND> __global__ __launch_bounds__(T::THREADS) void step_kernel(StepArgs a) {
+    __shared__ __attribute__((aligned(256))) char lds[T::lds_bytes(1)];
+    unsigned mi, ni;
+    tile_of(blockIdx.x, a.mt, a.nt, mi, ni);
+    const int64_t m0 = (int64_t)mi * T::BM, n0 = (int64_t)ni * T::BN, batch = blockIdx.z;
+    const int64_t wide = a.m * a.n8, square = a.m * a.m8;
+    const uint16_t *x = a.x + batch * 2 * wide, *sq = a.sq + batch * 2 * square, *poly = a.poly + batch * 2 * square;
+    Sums<T, 1> acc = {};
+    const Side sx = {x, a.n8, wide}, sa = {sq, a.m8, square}, sp = {poly, a.m8, square};
+    if constexpr (WHAT == kGram) {
+        const Side b[1] = {sx};
+        accumulate<T, true, true, 1>(acc, lds, sx, b, m0, a.m, n0, a.m, 0, a.n);
+    } else if constexpr (WHAT == kPoly) {
+        const Side b[1] = {sa};
+        accumulate<T, true, true, 1>(acc, lds, sa, b, m0, a.m, n0, a.m, 0, a.m);
+    } else {
+        const Side b[1] = {sx};
+        accumulate<T, true, false, 1>(acc, lds, sp, b, m0, a.m, n0, a.n8, 0, a.m);
+    }
+    each_stretch<T>(m0, n0, [&](int i, int64_t m, int64_t n) {
+        if (m >= a.m) return;
+        constexpr int W = 4 * T::NJ;
+        float v[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) v[j] = acc[0][i][j / 4][j % 4];
+        if constexpr (WHAT == kGram) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[j] *= two_to(kUnitA - 2 * kUnitX);
+            store_planes<2, true>(a.to + batch * 2 * square, square, m * a.m8 + n, n, a.m, v);
+        } else if constexpr (WHAT == kPoly) {
+            float old[W];
+            load_planes<W>(sq, square, m * a.m8 + n, n, a.m8, old);
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[j] = fmaf(a.c * two_to(kUnitP - 2 * kUnitA), v[j], a.b * two_to(kUnitP - kUnitA) * old[j]);
+            store_planes<2, true>(a.to + batch * 2 * square, square, m * a.m8 + n, n, a.m, v);
+        } else {
+            float old[W];
+            load_planes<W>(x, wide, m * a.n8 + n, n, a.n8, old);
+#pragma unroll
+            for (int j = 0; j < W; ++j) v[j] = fmaf(two_to(-kUnitP), v[j], a.a * old[j]);
+            if (!a.out) store_planes<2, true>(a.to + batch * 2 * wide, wide, m * a.n8 + n, n, a.n, v);
+            else {
+                ElemOf<KIND>* out = static_cast<ElemOf<KIND>*>(a.out) + batch * a.m * a.n;
+                const float back = a.scale * two_to(-kUnitX);
+#pragma unroll
+                for (int j = 0; j < W; ++j) v[j] *= back;
+                if (!a.tall) store_row<KIND>(out, m * a.n, n, a.n, a.grid, v);
+                else {
+#pragma unroll
+                    for (int j = 0; j < W; ++j) {
+                        const float one[4] = {v[j], 0.0f, 0.0f, 0.0f};
+                        if (n + j < a.n) store_row<KIND>(out, (n + j) * a.m, m, m + 1, false, one);
+                    }
+                }
+            }
+        }
+    });
+}
+
+template <int WHAT, int KIND> hipError_t launch(StepArgs a, int64_t batch, int tile, hipStream_t st) {
+    a.mt = (unsigned)cut_into(a.m, tile);
+    a.nt = (unsigned)cut_into(WHAT == kUpdate ? a.n : a.m, tile);
+    const dim3 grid(a.mt * a.nt, 1, (unsigned)batch);
+    if (tile == 128) step_kernel<OrthoTile<128>, WHAT, KIND><<<grid, dim3(OrthoTile<128>::THREADS), 0, st>>>(a);
+    else step_kernel<OrthoTile<64>, WHAT, KIND><<<grid, dim3(OrthoTile<64>::THREADS), 0, st>>>(a);
+    return hipGetLastError();
+}
+
+template <int KIND> hipError_t run(const OrthoArgs& a, hipStream_t st) {
+    const OrthoPlan& p = a.plan;
+    squares_kernel<KIND><<<dim3(kOrthoPeaks, (unsigned)a.s.B), dim3(256), 0, st>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    first_kernel<KIND><<<dim3((unsigned)cut_into(a.s.M, 64), (unsigned)cut_into(a.s.N, 64), (unsigned)a.s.B), dim3(256), 0, st>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    StepArgs s{};
+    uint16_t* x[2] = {reinterpret_cast<uint16_t*>(a.ws + p.x[0]), reinterpret_cast<uint16_t*>(a.ws + p.x[1])};
+    uint16_t *sq = reinterpret_cast<uint16_t*>(a.ws + p.a), *poly = reinterpret_cast<uint16_t*>(a.ws + p.p);
+    s.sq = sq; s.poly = poly;
+    s.m = p.m; s.n = p.n; s.m8 = p.m8; s.n8 = p.n8;
+    s.scale = a.scale;
+    s.tall = a.s.M > a.s.N;
+    s.grid = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && p.n * (int64_t)sizeof(ElemOf<KIND>) % 16 == 0;
+    for (int i = 0; i < a.steps; ++i) {
+        s.a = a.coefficients[3 * i]; s.b = a.coefficients[3 * i + 1]; s.c = a.coefficients[3 * i + 2];
+        s.x = x[i % 2];
+        s.to = sq;
+        if (hipError_t e = launch<kGram, 0>(s, a.s.B, p.tile_square, st)) return e;
+        s.to = poly;
+        if (hipError_t e = launch<kPoly, 0>(s, a.s.B, p.tile_square, st)) return e;
+        s.to = x[(i + 1) % 2];
+        s.out = i + 1 == a.steps ? a.out : nullptr;
+        if (hipError_t e = launch<kUpdate, KIND>(s, a.s.B, p.tile_wide, st)) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t orthogonalize(const OrthoArgs& a, hipStream_t st) {
+    return a.s.kind == 0 ? run<0>(a, st) : a.s.kind == 1 ? run<1>(a, st) : run<2>(a, st);
+}
+
+}  // namespace fsa
