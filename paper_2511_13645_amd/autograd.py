@@ -184,20 +184,27 @@ def fused_residual_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optiona
 
 class _GatedFeedForward(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, w_gate, w_up, w_down, activation):
-        ctx.save_for_backward(x, w_gate, w_up, w_down)
+    def forward(ctx, x, w_gate, w_up, w_down, activation, keep):
+        gates = None
+        if keep and binding.fsa_gated_keep_pays(*x.shape, w_gate.shape[0], w_down.shape[0], x.dtype):
+            y, gates = binding.fsa_gated_fwd(x, w_gate, w_up, w_down, activation=activation, emit_gates=True)
+        else:
+            y = binding.fsa_gated_fwd(x, w_gate, w_up, w_down, activation=activation)
+        ctx.save_for_backward(x, w_gate, w_up, w_down, gates)
         ctx.activation = activation
-        return binding.fsa_gated_fwd(x, w_gate, w_up, w_down, activation=activation)
+        return y
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_y):
         grads = binding.fsa_gated_bwd(grad_y.contiguous(), *ctx.saved_tensors, activation=ctx.activation, want=ctx.needs_input_grad[:4])
-        return (*grads, None)
+        return (*grads, None, None)
 
 
 def fused_gated_feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
                              activation: str = "silu") -> torch.Tensor:
     """Differentiable gated feed-forward block (act(x w_gate^T) * (x w_up^T)) w_down^T of rows x [T,D]: w_gate, w_up [H,D],
-    w_down [O,H], one type.  No row of hidden elements is kept for the backward, which makes them again."""
-    return _GatedFeedForward.apply(x, w_gate, w_up, w_down, activation)
+    w_down [O,H], one type.  What is kept for the backward is its inputs, and the two hidden products where that is quicker than making them
+    again."""
+    keep = torch.is_grad_enabled() and any(t.requires_grad for t in (x, w_gate, w_up, w_down))
+    return _GatedFeedForward.apply(x, w_gate, w_up, w_down, activation, keep)

@@ -45,7 +45,7 @@ EXPORTS = ("fsa_sample_mean_fwd", "fsa_mean_replay_fwd", "fsa_mean_bwd", "fsa_me
            "fsa_xent_fwd", "fsa_xent_bwd", "fsa_distill_fwd", "fsa_distill_bwd",
            "fsa_norm_fwd", "fsa_norm_bwd", "fsa_norm_bwd_workspace_bytes",
            "fsa_gated_fwd", "fsa_gated_bwd", "fsa_gated_fwd_workspace_bytes", "fsa_gated_bwd_workspace_bytes",
-           "fsa_orthogonalize", "fsa_orthogonalize_workspace_bytes")
+           "fsa_gated_keep_pays", "fsa_orthogonalize", "fsa_orthogonalize_workspace_bytes")
 
 _lib: Optional[ctypes.CDLL] = None
 _class_host = None                              # the module _fsa_class_host, likewise
@@ -137,12 +137,12 @@ def lib() -> ctypes.CDLL:
         L.fsa_norm_bwd_workspace_bytes.restype = i64
         L.fsa_norm_bwd.argtypes = [vp, vp, vp, i64, vp, ci, ci, i64, i64, f32, vp, vp, vp, i64, vp]
         L.fsa_norm_bwd.restype = ci
-        for name in ("fsa_gated_fwd_workspace_bytes", "fsa_gated_bwd_workspace_bytes"):
+        for name in ("fsa_gated_fwd_workspace_bytes", "fsa_gated_bwd_workspace_bytes", "fsa_gated_keep_pays"):
             getattr(L, name).argtypes = [i64, i64, i64, i64, ci]
-            getattr(L, name).restype = i64
-        L.fsa_gated_fwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, ci, ci, i64, i64, i64, i64, vp, vp, i64, vp]
+            getattr(L, name).restype = ci if name == "fsa_gated_keep_pays" else i64
+        L.fsa_gated_fwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, ci, ci, i64, i64, i64, i64, vp, vp, vp, i64, vp]
         L.fsa_gated_fwd.restype = ci
-        L.fsa_gated_bwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, ci, ci, i64, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp]
+        L.fsa_gated_bwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, ci, ci, i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp]
         L.fsa_gated_bwd.restype = ci
         L.fsa_orthogonalize_workspace_bytes.argtypes = [i64, i64, i64, ci]
         L.fsa_orthogonalize_workspace_bytes.restype = i64
@@ -1021,40 +1021,51 @@ def _gated_operands(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w
 
 
 def fsa_gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *, activation: str = "silu",
-                  workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+                  emit_gates: bool = False, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Gated feed-forward block (act(x w_gate^T) * (x w_up^T)) w_down^T: x [T,D], w_gate and w_up [H,D], w_down [O,H], all of one
-    type; activation "silu", "gelu" (by the error function) or "relu".  `workspace`: see fsa_gated_fwd_workspace_bytes; torch's
-    memory without one.  `stream`: see fsa_xent_fwd."""
+    type; activation "silu", "gelu" (by the error function) or "relu".  Returns y [T,O], with `emit_gates` (y, gates): x w_gate^T and
+    x w_up^T [2,T,H] in fp32, which spare the backward making them again (fsa_gated_keep_pays).  `workspace`: see
+    fsa_gated_fwd_workspace_bytes; torch's memory without one.  `stream`: see fsa_xent_fwd."""
     lead, (T, D, H, O) = _gated_operands(x, w_gate, w_up, w_down, activation)
     L = lib()
     with _on(x, stream):
         y = torch.empty((T, O), dtype=x.dtype, device=x.device)
+        gates = torch.empty((2, T, H), dtype=torch.float32, device=x.device) if emit_gates else None
         ws = _class_workspace(workspace, L.fsa_gated_fwd_workspace_bytes(T, D, H, O, lead[8]), x)
-        rc = L.fsa_gated_fwd(*lead, _ptr(y), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, x))
+        rc = L.fsa_gated_fwd(*lead, _ptr(y), _ptr(gates), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, x))
     if rc != FSA_OK:
         raise FsaError(rc, "fsa_gated_fwd")
-    return y
+    return (y, gates) if emit_gates else y
 
 
-def fsa_gated_bwd(grad_y: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
-                  activation: str = "silu", want: Sequence[bool] = (True, True, True, True),
+def fsa_gated_bwd(grad_y: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
+                  gates: Optional[torch.Tensor] = None, *, activation: str = "silu", want: Sequence[bool] = (True, True, True, True),
                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
-    """Gradients of fsa_gated_fwd by x, w_gate, w_up and w_down from grad_y [T,O]; None where not wanted."""
+    """Gradients of fsa_gated_fwd by x, w_gate, w_up and w_down from grad_y [T,O]; None where not wanted.  `gates`: what the
+    forward emitted, or None."""
     lead, (T, D, H, O) = _gated_operands(x, w_gate, w_up, w_down, activation)
     gs = _rows(grad_y, "grad_y")
     _same_type(x, "x", (grad_y, "grad_y"))
     _shape(grad_y, "grad_y", (T, O))
-    _same_device(x, (grad_y, "grad_y"))
+    if gates is not None:
+        _need(gates, "gates", torch.float32)
+        _shape(gates, "gates", (2, T, H))
+    _same_device(x, (grad_y, "grad_y"), (gates, "gates"))
     L = lib()
     with _on(x, stream):
         grads = tuple(torch.empty(t.shape, dtype=x.dtype, device=x.device) if w else None
                       for t, w in zip((x, w_gate, w_up, w_down), want))
         ws = _class_workspace(workspace, L.fsa_gated_bwd_workspace_bytes(T, D, H, O, lead[8]), x)
-        rc = L.fsa_gated_bwd(_ptr(grad_y), gs, *lead, *(_ptr(g) for g in grads), _ptr(ws), ws.numel() * ws.element_size(),
+        rc = L.fsa_gated_bwd(_ptr(grad_y), gs, *lead, _ptr(gates), *(_ptr(g) for g in grads), _ptr(ws), ws.numel() * ws.element_size(),
                              _stream(stream, x))
     if rc != FSA_OK:
         raise FsaError(rc, "fsa_gated_bwd")
     return grads
+
+
+def fsa_gated_keep_pays(T: int, D: int, H: int, O: int, dtype: torch.dtype) -> bool:
+    """Whether a forward whose backward follows had better emit its gates."""
+    return bool(lib().fsa_gated_keep_pays(T, D, H, O, _FLOAT_TYPE[dtype]))
 
 
 def fsa_gated_fwd_workspace_bytes(T: int, D: int, H: int, O: int, dtype: torch.dtype) -> int:

@@ -10,6 +10,7 @@ namespace fsa {
 
 constexpr int64_t up_to(int64_t n, int64_t grid) { return (n + grid - 1) / grid * grid; }
 constexpr int64_t cut_into(int64_t n, int64_t piece) { return (n + piece - 1) / piece; }
+constexpr int64_t kChip = 256;                          // CUs
 
 // ---------------------------------------------------------------------------------------------------------------
 // norm
@@ -66,65 +67,164 @@ struct GatedShape {
     int kind;                                           // 0 fp32, 1 bfloat16, 2 fp16
 };
 constexpr int planes_of_kind(int kind) { return kind == 0 ? 3 : 1; }
-constexpr int kGatedPeaks = 64;                         // workgroups that look for the gradients' largest
+constexpr int kGatedPeaks = 256;                        // workgroups that look for the gradients' largest
 
-// One product's cut: tiles of `tile` x `tile`, the depth in `splits` shares.
-struct ProductCut {
-    int tile;
-    int64_t mt, nt, splits;
-};
-constexpr int64_t kChip = 256;                          // CUs
-inline ProductCut product_cut(int64_t M, int64_t N, int64_t K, int64_t products) {
-    ProductCut c{};
-    const int64_t wide = cut_into(M, 128) * cut_into(N, 128) * products;
-    c.tile = wide >= kChip ? 128 : 64;
-    c.mt = cut_into(M, c.tile);
-    c.nt = cut_into(N, c.tile);
-    const int64_t tiles = c.mt * c.nt * products > 0 ? c.mt * c.nt * products : 1, steps = cut_into(K, 64);    // (no rows: no tiles)
-    c.splits = 2 * kChip / tiles;
-    if (c.splits > steps / 4) c.splits = steps / 4;
-    if (c.splits < 1) c.splits = 1;
-    return c;
+
+// Tiles that a product may be cut into, with the rate that each reached (TFLOP/s of 16-bit products, 8192 x 4096 x 4096).
+struct TileChoice { int m, n; double rate; };
+constexpr int kTileKinds = 3;
+constexpr TileChoice kTilesOne[kTileKinds] = {{64, 64, 700}, {128, 128, 980}, {256, 256, 1300}};
+constexpr TileChoice kTilesThree[kTileKinds] = {{64, 64, 950}, {128, 64, 1150}, {256, 128, 1390}};
+constexpr const TileChoice& product_tile(int kind, int choice) { return kind == 0 ? kTilesThree[choice] : kTilesOne[choice]; }
+// The same of the pairs of products of the hidden rows: columns of each.
+constexpr TileChoice kPairsOne[kTileKinds] = {{64, 64, 700}, {128, 64, 900}, {256, 128, 1250}};
+constexpr TileChoice kPairsThree[kTileKinds] = {{64, 64, 900}, {128, 64, 1100}, {256, 64, 1300}};
+constexpr TileChoice kSlopesOne[kTileKinds] = {{64, 64, 700}, {128, 64, 900}, {128, 128, 1000}};
+constexpr const TileChoice& pair_tile(int kind, int choice, bool slopes) {
+    return kind == 0 ? kPairsThree[choice] : slopes ? kSlopesOne[choice] : kPairsOne[choice];
 }
-inline int pair_tile(int64_t T, int64_t H) { return cut_into(T, 128) * cut_into(H, 64) >= kChip ? 128 : 64; }
+constexpr double kTurn = 2.0;                           // us that a workgroup takes besides its products: first reads, writing out
+constexpr double kJoin = 4.0;                           // and a second launch
+
+// Products that one launch makes: `copies` of M x N over a depth K, in `splits` shares of the depth.
+constexpr int kMostJobs = 3;
+struct ProductJob {
+    int64_t M, N, K, copies, splits;
+    int64_t parts_bytes() const { return splits > 1 ? copies * splits * M * up_to(N, 8) * 4 : 0; }
+};
+struct ProductCut {
+    int choice, count;
+    ProductJob job[kMostJobs];
+};
+// When the last of the chip's CUs is done with `count` jobs' workgroups, `groups[j]` of length `length[j]`, the longest first, each
+// given to the CU that is free first.
+struct Load { int64_t cus; double at; };
+inline double makespan(int count, const int64_t* groups, const double* length) {
+    constexpr int kMost = 16;
+    Load load[kMost] = {{kChip, 0.0}};
+    int n = 1;                                          // loads in order, the least first
+    bool done[kMostJobs] = {};
+    for (int k = 0; k < count; ++k) {
+        int j = -1;
+        for (int i = 0; i < count; ++i) if (!done[i] && (j < 0 || length[i] > length[j])) j = i;
+        done[j] = true;
+        int64_t left = groups[j];
+        if (left > 64 * kChip) return ((double)left / kChip + 1.0) * length[j] + load[n - 1].at;    // (many: no end effects)
+        while (left > 0) {
+            Load take = load[0];
+            if (left < take.cus) { load[0].cus -= left; take.cus = left; }
+            else { --n; for (int i = 0; i < n; ++i) load[i] = load[i + 1]; }
+            left -= take.cus;
+            take.at += length[j];
+            int i = n;
+            for (; i > 0 && load[i - 1].at > take.at; --i) ;
+            if (i > 0 && load[i - 1].at == take.at) load[i - 1].cus += take.cus;
+            else if (n == kMost) return 1e30;           // (never: a job leaves at most two loads more than it found)
+            else { for (int q = n; q > i; --q) load[q] = load[q - 1]; load[i] = take; ++n; }
+        }
+    }
+    return load[n - 1].at;
+}
+// The tile and the shares that are estimated to take the least time: depths cut into shares of about one length, or one job's
+// alone in two; parts of a split product are written and read once more.
+inline ProductCut cut_products(int kind, ProductCut want) {
+    ProductCut best = want;
+    double least = 1e30;
+    const double each = kind == 0 ? 6.0 : 1.0;
+    for (int choice = 0; choice < kTileKinds; ++choice) {
+        const TileChoice& tile = product_tile(kind, choice);
+        const double depth_us = 2.0 * tile.m * tile.n * each / (tile.rate / kChip) * 1e-6;          // a workgroup's step of one
+        int64_t tiles[kMostJobs];
+        double work = 0.0;
+        for (int j = 0; j < want.count; ++j) {
+            tiles[j] = cut_into(want.job[j].M, tile.m) * cut_into(want.job[j].N, tile.n) * want.job[j].copies;
+            work += (double)tiles[j] * (double)want.job[j].K;
+        }
+        for (int way = 0; way < 5 + want.count; ++way) { // whole, shares of 1, 1/2, 1/3, 1/4 of a CU's work, one job's halves
+            ProductCut c = want;
+            c.choice = choice;
+            double share = way >= 1 && way < 5 ? work / (double)(kChip * way) : 1e30, bytes = 0.0, us[kMostJobs];
+            if (share < 256.0) share = 256.0;
+            int64_t groups[kMostJobs];
+            for (int j = 0; j < c.count; ++j) {
+                ProductJob& job = c.job[j];
+                const double n = (double)job.K / share + 0.5;
+                job.splits = way - 5 == j ? 2 : n > 64.0 ? 64 : n < 1.0 ? 1 : (int64_t)n;
+                groups[j] = tiles[j] * job.splits;
+                us[j] = (double)job.K / (double)job.splits * depth_us + kTurn;
+                bytes += (double)job.parts_bytes();
+            }
+            const double total = makespan(c.count, groups, us) + (bytes > 0.0 ? kJoin + bytes * 2.0 / 4e6 : 0.0);
+            if (total < least) { least = total; best = c; }
+        }
+    }
+    return best;
+}
+enum { kHiddenPass, kSlopesPass, kKeptPass };
+inline int cut_pairs(int kind, int64_t T, int64_t H, int64_t depth, int pass) {
+    int best = 0;
+    double least = 1e30;
+    for (int choice = 0; choice < kTileKinds; ++choice) {
+        const TileChoice& tile = pass == kKeptPass ? product_tile(kind, choice) : pair_tile(kind, choice, pass == kSlopesPass);
+        const double one = 2.0 * tile.m * tile.n * (double)depth * (kind == 0 ? 6.0 : 1.0) / (tile.rate / kChip) * 1e-6 + kTurn;
+        const double us = (double)cut_into(cut_into(T, tile.m) * cut_into(H, tile.n), kChip) * one;
+        if (us < least) { least = us; best = choice; }
+    }
+    return best;
+}
+
+// Whether h, dg and du are held with what their rounding to 16 bits leaves, as a second plane: their products take twice as long, which
+// is less than the launches of a pass up to about this many operations (1024 x 128 -> 512 -> 128, bfloat16: 4 us of 90).
+inline bool gated_fine(const GatedShape& s) { return s.kind != 0 && 6.0 * (double)s.T * (double)s.H * (double)(2 * s.D + s.O) < 4e9; }
+inline int gated_planes(const GatedShape& s) { return s.kind == 0 ? 3 : gated_fine(s) ? 2 : 1; }
+
+// Whether a forward whose backward follows keeps g and u, in fp32, rather than that they are made again: 16 bytes of traffic
+// an element against 4 D operations (of six products each in fp32).
+inline bool gated_keep_pays(const GatedShape& s) { return s.D >= (s.kind == 0 ? 160 : 512); }
 
 // Byte offsets into the caller's workspace.
 struct GatedPlan {
     size_t x, gate, up, down, grad_y;                   // laid out operands
     size_t h, dg, du, peaks, parts, bytes;
     int64_t D8, H8, O8;
-    ProductCut answer, dx, down_grad, gate_grad;
+    int planes;                                         // of h, dg and du
+    int pairs, slopes;                                  // choices of tiles
+    ProductCut products;
 };
-// `packs`: bits x, gate, up, down, grad_y of operands that are laid out.
-inline GatedPlan gated_plan(const GatedShape& s, bool backward, bool want_x, bool want_w, int packs) {
+// `packs`: bits x, gate, up, down, grad_y of operands that are laid out.  `kept`: the backward is given g and u.  Products of the
+// backward are cut as if all were wanted, so that room for them does not depend on which are.
+enum { kJobGates, kJobDown, kJobX };
+inline GatedPlan gated_plan(const GatedShape& s, bool backward, bool kept, int packs) {
     GatedPlan p{};
     size_t at = 0;
     auto room = [&at](int64_t n) { const size_t a = at; at += (size_t)up_to(n, 256); return a; };
     p.D8 = up_to(s.D, 8); p.H8 = up_to(s.H, 8); p.O8 = up_to(s.O, 8);
-    const int64_t planes = 2 * planes_of_kind(s.kind);  // bytes of an element's planes
+    p.planes = gated_planes(s);
+    const int64_t planes = 2 * planes_of_kind(s.kind), own = s.T * p.H8 * 2 * p.planes;             // bytes
     if (packs & 1) p.x = room(s.T * p.D8 * planes);
     if (packs & 2) p.gate = room(s.H * p.D8 * planes);
     if (packs & 4) p.up = room(s.H * p.D8 * planes);
     if (packs & 8) p.down = room(s.O * p.H8 * planes);
-    p.h = room(s.T * p.H8 * planes);
-    int64_t parts = 0;
-    auto product = [&](int64_t M, int64_t N, int64_t K, int64_t products) {
-        const ProductCut c = product_cut(M, N, K, products);
-        if (c.splits > 1) { const int64_t b = products * c.splits * M * up_to(N, 8) * 4; parts = parts > b ? parts : b; }
-        return c;
-    };
-    if (!backward) p.answer = product(s.T, s.O, s.H, 1);
-    else {
+    p.h = room(own);
+    const int64_t sums = s.kind != 0 ? p.planes : 1;    // products that make one, of h's, dg's or du's planes
+    ProductCut want{};
+    if (!backward) {
+        p.pairs = cut_pairs(s.kind, s.T, s.H, 2 * s.D, kHiddenPass);
+        want.job[want.count++] = {s.T, s.O, sums * s.H, 1, 1};
+    } else {
         if (packs & 16) p.grad_y = room(s.T * p.O8 * planes);
-        p.dg = room(s.T * p.H8 * planes);
-        p.du = room(s.T * p.H8 * planes);
+        p.dg = room(own);
+        p.du = room(own);
         p.peaks = room(kGatedPeaks * 4);
-        if (want_x) p.dx = product(s.T, s.D, 2 * s.H, 1);
-        if (want_w) {
-            p.down_grad = product(s.O, s.H, s.T, 1);
-            p.gate_grad = product(s.H, s.D, s.T, 2);
-        }
+        p.slopes = cut_pairs(s.kind, s.T, s.H, (kept ? 0 : 2 * s.D) + s.O, kept ? kKeptPass : kSlopesPass);
+        want.count = 3;
+        want.job[kJobGates] = {s.H, s.D, sums * s.T, 2, 1};
+        want.job[kJobDown] = {s.O, s.H, sums * s.T, 1, 1};
+        want.job[kJobX] = {s.T, s.D, 2 * sums * s.H, 1, 1};
     }
+    p.products = cut_products(s.kind, want);
+    int64_t parts = 0;
+    for (int j = 0; j < p.products.count; ++j) parts += up_to(p.products.job[j].parts_bytes(), 256);
     p.parts = room(parts);
     p.bytes = at;
     return p;
@@ -139,6 +239,7 @@ struct GatedArgs {
     int activation;
     Matrix x, gate, up, down, grad_y;
     void *y, *grad_x, *grad_gate, *grad_up, *grad_down; // contiguous
+    float* gates;                                       // [2,T,H] g and u: forward: written if not null; backward: read
     GatedPlan plan;
     int packs;
     char* ws;

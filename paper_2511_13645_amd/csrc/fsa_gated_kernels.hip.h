@@ -30,8 +30,30 @@ constexpr bool kHalf = kKind == 2;
 constexpr int BK = NP == 3 ? 32 : 64;
 using Elem = typename std::conditional<kKind == 0, float, uint16_t>::type;
 
-template <int EDGE> using ProductTile = Tile<NP, kHalf, EDGE, EDGE, BK, 2, 2>;
-template <int EDGE> using PairTile = Tile<NP, kHalf, EDGE, 64, BK, 2, 2>;
+// The tiles that fsa_block.h chooses from, in its order.
+template <int CHOICE> struct Tiles;
+template <> struct Tiles<0> {
+    using Product = Tile<NP, kHalf, 64, 64, BK, 2, 2>;
+    using Hidden = Product;
+    using Slopes = Product;
+};
+template <> struct Tiles<1> {
+    using Product = Tile<NP, kHalf, 128, NP == 1 ? 128 : 64, BK, NP == 1 ? 4 : 2, 2>;
+    using Hidden = Tile<NP, kHalf, 128, 64, BK, 2, 2>;
+    using Slopes = Hidden;
+};
+template <> struct Tiles<2> {
+    using Product = Tile<NP, kHalf, 256, NP == 1 ? 256 : 128, BK, NP == 1 ? 2 : 4, NP == 1 ? 4 : 2>;
+    using Hidden = Tile<NP, kHalf, 256, NP == 1 ? 128 : 64, BK, NP == 1 ? 2 : 4, NP == 1 ? 4 : 2>;
+    using Slopes = Tile<NP, kHalf, NP == 1 ? 128 : 256, NP == 1 ? 128 : 64, BK, 4, 2>;
+};
+template <int CHOICE> constexpr bool same_tiles() {
+    using C = Tiles<CHOICE>;
+    constexpr TileChoice p = product_tile(kKind, CHOICE), h = pair_tile(kKind, CHOICE, false), s = pair_tile(kKind, CHOICE, true);
+    return C::Product::BM == p.m && C::Product::BN == p.n && C::Hidden::BM == h.m && C::Hidden::BN == h.n && C::Slopes::BM == s.m &&
+           C::Slopes::BN == s.n;
+}
+static_assert(same_tiles<0>() && same_tiles<1>() && same_tiles<2>(), "as the plan has them");
 
 // ---------------------------------------------------------------------------------------------------------------
 // operands laid out as planes: rows of a multiple of 8 elements, zeros behind their end
@@ -41,22 +63,55 @@ struct PackList {
     uint16_t* to[5];
     int64_t first[6];                                   // pieces of 8 elements before each
     int count;
+    unsigned packers;                                   // workgroups that lay out; kGatedPeaks behind them look at grad_y
+    Matrix grad_y;
+    float* peaks;
 };
+__device__ __forceinline__ void load_piece(const Matrix& from, int64_t row, int64_t col, Elem (&e)[8]) {
+    const Elem* p = static_cast<const Elem*>(from.p) + row * from.stride + col;
+    if (col + 8 <= from.cols) __builtin_memcpy(e, p, sizeof(e));
+    else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = col + j < from.cols ? p[j] : Elem(0);
+    }
+}
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    return a <= 0x7fffffff ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
+// fp16: the largest finite |grad_y| of a workgroup's share.
+__device__ __forceinline__ void find_peak(const PackList& l) {
+    __shared__ float lds[4];
+    const unsigned share = blockIdx.x - l.packers;
+    const int64_t pieces = cut_into(l.grad_y.cols, 8), all = l.grad_y.rows * pieces;
+    float top = 0.0f;
+    for (int64_t i = (int64_t)share * 256 + threadIdx.x; i < all; i += kGatedPeaks * 256) {
+        const int64_t row = quotient(i, pieces);
+        Elem e[8];
+        load_piece(l.grad_y, row, (i - row * pieces) * 8, e);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float x = fabsf(as_float<true>((uint32_t)e[j]));
+            if (x < __builtin_inff()) top = fmaxf(top, x);
+        }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
+    __syncthreads();
+    if (threadIdx.x == 0) l.peaks[share] = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+}
 __global__ __launch_bounds__(256) void pack_kernel(PackList l) {
+    if constexpr (kHalf)
+        if (blockIdx.x >= l.packers) return find_peak(l);
     const int64_t all = l.first[l.count];
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)l.packers * 256) {
         int m = 0;
 #pragma unroll
         for (int j = 1; j < 5; ++j) if (j < l.count && i >= l.first[j]) m = j;
         const Matrix from = l.from[m];
-        const int64_t pieces = cut_into(from.cols, 8), at = i - l.first[m], row = at / pieces, col = at % pieces * 8;
-        const Elem* p = static_cast<const Elem*>(from.p) + row * from.stride + col;
+        const int64_t pieces = cut_into(from.cols, 8), at = i - l.first[m], row = quotient(at, pieces), col = (at - row * pieces) * 8;
         Elem e[8];
-        if (col + 8 <= from.cols) __builtin_memcpy(e, p, sizeof(e));
-        else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = col + j < from.cols ? p[j] : Elem(0);
-        }
+        load_piece(from, row, col, e);
         const int64_t plane = from.rows * pieces * 8;
         uint16_t* to = l.to[m] + (row * pieces * 8 + col);
         if constexpr (kKind == 0) {
@@ -73,28 +128,11 @@ __global__ __launch_bounds__(256) void pack_kernel(PackList l) {
     }
 }
 
-// ---------------------------------------------------------------------------------------------------------------
-// fp16: the power of two of the gradients
-// ---------------------------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void peaks_kernel(Matrix g, float* peaks) {
-    __shared__ float lds[4];
-    float top = 0.0f;
-    for (int64_t row = blockIdx.x; row < g.rows; row += gridDim.x)
-        for (int64_t c = threadIdx.x; c < g.cols; c += 256) {
-            const uint16_t e = static_cast<const uint16_t*>(g.p)[row * g.stride + c];
-            const float x = fabsf(as_float<true>(e));
-            if (x < __builtin_inff()) top = fmaxf(top, x);
-        }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
-    __syncthreads();
-    if (threadIdx.x == 0) peaks[blockIdx.x] = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
-}
 // 2^e with max * 2^e in [1, 2); what fp16 holds lies within 2^-24 ... 2^15.
 __device__ __forceinline__ int lift_of(const float* peaks) {
-    float top = peaks[threadIdx.x & 63];
-    static_assert(kGatedPeaks == 64, "one a lane");
+    const f32x4 four = reinterpret_cast<const f32x4*>(peaks)[threadIdx.x & 63];
+    static_assert(kGatedPeaks == 256, "four a lane");
+    float top = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3]));
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
     if (!(top > 0.0f)) return 0;
@@ -123,115 +161,245 @@ template <int ACT> __device__ __forceinline__ Gate gate_of(float g) {
 struct HiddenArgs {
     Side x, gate, up, down, grad_y;
     uint16_t *h, *dg, *du;                              // [T, H8] planes
+    float* gates;                                       // [2,T,H] or null
     int64_t T, D, H, O, H8;
     const float* peaks;
     unsigned mt, nt;
 };
 
-template <class T, int ACT> __global__ __launch_bounds__(T::THREADS) void hidden_kernel(HiddenArgs a) {
+// PLANES of h, dg and du: one more than an operand has where the rounding's rest is kept.
+template <class T, int ACT, int PLANES> __global__ __launch_bounds__(T::THREADS, T::waves(2)) void hidden_kernel(HiddenArgs a) {
     __shared__ __attribute__((aligned(256))) char lds[T::lds_bytes(2)];
     unsigned mi, ni;
     tile_of(blockIdx.x, a.mt, a.nt, mi, ni);
     const int64_t m0 = (int64_t)mi * T::BM, n0 = (int64_t)ni * T::BN;
-    Sums<T, 2> acc = {};
+    using Stream = OneStream<T, true, true, 2>;
+    Stream stream;
     const Side tables[2] = {a.gate, a.up};
-    accumulate<T, true, true, 2>(acc, lds, a.x, tables, m0, a.T, n0, a.H, 0, a.D);
+    stream.flow.start(a.x, tables, m0, a.T, n0, a.H, 0, a.D);
+    Ring<T, T::stage_bytes(2), Stream> ring{lds, stream};
+    ring.fill();
+    Sums<T, 2> acc = {};
+    accumulate<T, true, true, 2>(acc, ring, cut_into(a.D, T::BK));
+    ring.end();
     each_stretch<T>(m0, n0, [&](int i, int64_t m, int64_t n) {
         if (m >= a.T) return;
-        float h[4 * T::NJ];
+        constexpr int W = 4 * T::NJ;
+        float g[W], u[W];
 #pragma unroll
-        for (int j = 0; j < 4 * T::NJ; ++j) h[j] = gate_of<ACT>(acc[0][i][j / 4][j % 4]).value * acc[1][i][j / 4][j % 4];
-        store_planes<T::NP, T::HALF>(a.h, a.T * a.H8, m * a.H8 + n, n, a.H, h);
+        for (int j = 0; j < W; ++j) { g[j] = acc[0][i][j / 4][j % 4]; u[j] = acc[1][i][j / 4][j % 4]; }
+        if (a.gates) {
+            const bool grid = a.H % 4 == 0 && reinterpret_cast<uintptr_t>(a.gates) % 16 == 0;
+            store_row<0>(a.gates, m * a.H, n, a.H, grid, g);
+            store_row<0>(a.gates, (a.T + m) * a.H, n, a.H, grid, u);
+        }
+#pragma unroll
+        for (int j = 0; j < W; ++j) g[j] = gate_of<ACT>(g[j]).value * u[j];
+        store_planes<PLANES, T::HALF>(a.h, a.T * a.H8, m * a.H8 + n, n, a.H, g);
     });
 }
 
-template <class T, int ACT> __global__ __launch_bounds__(T::THREADS) void slopes_kernel(HiddenArgs a) {
-    __shared__ __attribute__((aligned(256))) char lds[T::lds_bytes(2)];
+template <int W> __device__ __forceinline__ void load_row(const float* p, int64_t n, int64_t N, float (&x)[W]) {
+#pragma unroll
+    for (int i = 0; i < W; i += 4) {
+        if (n + i + 4 <= N) __builtin_memcpy(x + i, p + n + i, 16);
+        else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[i + j] = n + i + j < N ? p[n + i + j] : 0.0f;
+        }
+    }
+}
+
+// What slopes without kept gates ask for: grad_y and w_down, then x and both tables.
+template <class T> struct SlopesStream {
+    using F = Flow<T, true, false, 1>;
+    using G = Flow<T, true, true, 2>;
+    static constexpr int ASKS = G::ASKS, SURE = F::SURE < G::SURE ? F::SURE : G::SURE;
+    static_assert(F::ASKS <= G::ASKS, "");
+    F down;
+    G gates;
+    bool at_gates = false;
+    __device__ __forceinline__ SlopesStream(const HiddenArgs& a, int64_t m0, int64_t n0) {
+        const Side table[1] = {a.down}, tables[2] = {a.gate, a.up};
+        down.start(a.grad_y, table, m0, a.T, n0, a.H8, 0, a.O);
+        gates.start(a.x, tables, m0, a.T, n0, a.H, 0, a.D);
+    }
+    __device__ __forceinline__ void ask(uint32_t stage, int piece) const {
+        if (at_gates) gates.ask(stage, piece);
+        else if (piece < F::ASKS) down.ask(stage, piece);
+    }
+    __device__ __forceinline__ void next() {
+        if (at_gates) gates.next();
+        else { down.next(); at_gates = down.left == 0; }
+    }
+};
+
+template <class T, int ACT, int PLANES, bool KEPT> __global__ __launch_bounds__(T::THREADS, T::waves(KEPT ? 1 : 2)) void slopes_kernel(HiddenArgs a) {
+    constexpr int PARTS = KEPT ? 1 : 2;
+    __shared__ __attribute__((aligned(256))) char lds[T::lds_bytes(PARTS)];
     unsigned mi, ni;
     tile_of(blockIdx.x, a.mt, a.nt, mi, ni);
     const int64_t m0 = (int64_t)mi * T::BM, n0 = (int64_t)ni * T::BN;
-    Sums<T, 2> acc = {};
+    Sums<T, PARTS> acc = {};
     Sums<T, 1> dh = {};
-    const Side tables[2] = {a.gate, a.up}, down[1] = {a.down};
-    accumulate<T, true, false, 1>(dh, lds, a.grad_y, down, m0, a.T, n0, a.H8, 0, a.O);
-    accumulate<T, true, true, 2>(acc, lds, a.x, tables, m0, a.T, n0, a.H, 0, a.D);
+    if constexpr (KEPT) {
+        using Stream = OneStream<T, true, false, 1>;
+        Stream stream;
+        const Side table[1] = {a.down};
+        stream.flow.start(a.grad_y, table, m0, a.T, n0, a.H8, 0, a.O);
+        Ring<T, T::stage_bytes(1), Stream> ring{lds, stream};
+        ring.fill();
+        accumulate<T, true, false, 1>(dh, ring, cut_into(a.O, T::BK));
+        ring.end();
+    } else {
+        SlopesStream<T> stream(a, m0, n0);
+        Ring<T, T::stage_bytes(2), SlopesStream<T>> ring{lds, stream};
+        ring.fill();
+        accumulate<T, true, false, 1>(dh, ring, cut_into(a.O, T::BK));
+        accumulate<T, true, true, 2>(acc, ring, cut_into(a.D, T::BK));
+        ring.end();
+    }
+    settle<T, 1>(dh);
     const float lift = kHalf ? power_of_two(lift_of(a.peaks)) : 1.0f;
     each_stretch<T>(m0, n0, [&](int i, int64_t m, int64_t n) {
         if (m >= a.T) return;
-        float h[4 * T::NJ], dg[4 * T::NJ], du[4 * T::NJ];
+        constexpr int W = 4 * T::NJ;
+        float g[W], u[W], dg[W], du[W];
+        if constexpr (KEPT) {
+            load_row(a.gates + m * a.H, n, a.H, g);
+            load_row(a.gates + (a.T + m) * a.H, n, a.H, u);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4 * T::NJ; ++j) {
-            const Gate g = gate_of<ACT>(acc[0][i][j / 4][j % 4]);
-            const float u = acc[1][i][j / 4][j % 4], d = kHalf ? dh[0][i][j / 4][j % 4] * lift : dh[0][i][j / 4][j % 4];
-            h[j] = g.value * u;
-            dg[j] = d * u * g.slope;
-            du[j] = d * g.value;
+            for (int j = 0; j < W; ++j) { g[j] = acc[0][i][j / 4][j % 4]; u[j] = acc[1][i][j / 4][j % 4]; }
         }
-        store_planes<T::NP, T::HALF>(a.h, a.T * a.H8, m * a.H8 + n, n, a.H, h);
-        store_planes<T::NP, T::HALF>(a.dg, a.T * a.H8, m * a.H8 + n, n, a.H, dg);
-        store_planes<T::NP, T::HALF>(a.du, a.T * a.H8, m * a.H8 + n, n, a.H, du);
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const Gate at = gate_of<ACT>(g[j]);
+            const float d = kHalf ? dh[0][i][j / 4][j % 4] * lift : dh[0][i][j / 4][j % 4];
+            g[j] = at.value * u[j];
+            dg[j] = d * u[j] * at.slope;
+            du[j] = d * at.value;
+        }
+        store_planes<PLANES, T::HALF>(a.h, a.T * a.H8, m * a.H8 + n, n, a.H, g);
+        store_planes<PLANES, T::HALF>(a.dg, a.T * a.H8, m * a.H8 + n, n, a.H, dg);
+        store_planes<PLANES, T::HALF>(a.du, a.T * a.H8, m * a.H8 + n, n, a.H, du);
     });
 }
 
 // ---------------------------------------------------------------------------------------------------------------
 // products that leave in the caller's type
 // ---------------------------------------------------------------------------------------------------------------
-struct ProductArgs {
-    Side a[2], b[2];
+// Up to three at a time, so that one's last workgroups run beside the next one's first, and small ones side by side.
+struct Job {
+    Side a[2][4], b[2][4];                              // of up to two results, the pairs of operands whose products make one
     void* out[2];
     int64_t M, N, K, out_ld;                            // K: depth of one pair
     int64_t M8, N8;                                     // ends of flat operands
-    bool together;                                      // one result, the sum of both pairs' products; else a result each
-    bool pairs, grid;
     float* parts;                                       // [results][splits][M][N8], where there are splits
-    const float* peaks;                                 // or null
-    unsigned mt, nt, splits;
+    int pairs, results, planned;                        // planned: which of the plan's
+    bool adeep, grid, lifted;                           // lifted: dg or du is in it
+    unsigned mt, nt, splits, first, first_join;         // workgroups before this job's
+};
+struct Jobs {
+    Job job[kMostJobs];
+    int count;
+    const float* peaks;
 };
 
-template <class T, bool ADEEP, bool BDEEP> __global__ __launch_bounds__(T::THREADS) void product_kernel(ProductArgs a) {
-    __shared__ __attribute__((aligned(256))) char lds[T::lds_bytes(1)];
+// A workgroup's place in a launch: its job, result, share of the depth and tile.
+struct Place {
+    const Job* job;
+    unsigned which, split;
     unsigned mi, ni;
-    tile_of(blockIdx.x, a.mt, a.nt, mi, ni);
-    const int64_t m0 = (int64_t)mi * T::BM, n0 = (int64_t)ni * T::BN;
-    const unsigned split = blockIdx.y, which = blockIdx.z;
+};
+__device__ __forceinline__ Place place_of(const Jobs& l, unsigned id) {
+    int j = 0;
+#pragma unroll
+    for (int i = 1; i < kMostJobs; ++i) if (i < l.count && id >= l.job[i].first) j = i;
+    const Job& a = l.job[j];
+    const unsigned tiles = a.mt * a.nt, at = id - a.first;
+    Place p{&a, at / tiles / a.splits, at / tiles % a.splits, 0, 0};
+    tile_of(at % tiles, a.mt, a.nt, p.mi, p.ni);
+    return p;
+}
+// What the products of a place ask for: its share of all its pairs' steps, one pair after the other.  Pairs lie alike, so that to
+// whoever multiplies they are one product.
+template <class T, bool ADEEP, bool BDEEP> struct ProductStream {
+    using F = Flow<T, ADEEP, BDEEP, 1>;
+    static constexpr int ASKS = F::ASKS, SURE = F::SURE;
+    const Job& a;
+    int64_t m0, n0, steps, last;                            // steps: in all; last: of the share, from the present pair's first
+    unsigned which;
+    int pair;
+    F flow;
+    __device__ __forceinline__ explicit ProductStream(const Place& p) : a(*p.job), m0((int64_t)p.mi * T::BM), n0((int64_t)p.ni * T::BN), which(p.which) {
+        const int64_t each = cut_into(a.K, T::BK), all = a.pairs * each, first = all * p.split / a.splits;
+        pair = (int)(first / each);
+        last = all * (p.split + 1) / a.splits;
+        steps = last - first;
+        last -= pair * each;
+        const Side b[1] = {a.b[which][pair]};
+        flow.start(a.a[which][pair], b, m0, ADEEP ? a.M : a.M8, n0, BDEEP ? a.N : a.N8, (first - pair * each) * T::BK, end());
+    }
+    __device__ __forceinline__ int64_t end() const { return last * T::BK < a.K ? last * T::BK : a.K; }
+    __device__ __forceinline__ void ask(uint32_t stage, int piece) const { flow.ask(stage, piece); }
+    __device__ __forceinline__ void next() {
+        flow.next();
+        if (flow.left > 0) return;
+        last -= cut_into(a.K, T::BK);
+        if (last <= 0) return;
+        ++pair;
+        flow.a.move(a.a[which][pair], m0, 0);
+        flow.b[0].move(a.b[which][pair], n0, 0);
+        flow.left = end();
+    }
+};
+
+template <class T, bool ADEEP, bool BDEEP> __device__ __forceinline__ void make_products(Sums<T, 1>& acc, char* lds, const Place& p) {
+    using Stream = ProductStream<T, ADEEP, BDEEP>;
+    Stream stream(p);
+    Ring<T, T::stage_bytes(1), Stream> ring{lds, stream};
+    ring.fill();
+    accumulate<T, ADEEP, BDEEP, 1>(acc, ring, stream.steps);
+    ring.end();
+    if constexpr (!BDEEP) settle<T, 1>(acc);
+}
+
+template <class T, bool FORWARD> __global__ __launch_bounds__(T::THREADS, T::waves(1)) void product_kernel(Jobs l) {
+    __shared__ __attribute__((aligned(256))) char lds[T::lds_bytes(1)];
+    const Place p = place_of(l, blockIdx.x);
+    const Job& a = *p.job;
     Sums<T, 1> acc = {};
-    // this split's steps of all pairs', one pair after the other
-    const int64_t steps = cut_into(a.K, T::BK), all = a.together ? 2 * steps : steps;
-    const int64_t first = all * split / a.splits, last = all * (split + 1) / a.splits;
-    auto add = [&](int pair, int64_t from, int64_t to) {
-        const Side b[1] = {a.b[pair]};
-        const int64_t end = to * T::BK < a.K ? to * T::BK : a.K;
-        accumulate<T, ADEEP, BDEEP, 1>(acc, lds, a.a[pair], b, m0, ADEEP ? a.M : a.M8, n0, BDEEP ? a.N : a.N8, from * T::BK, end);
-    };
-    if (!a.together) add(which, first, last);
-    else
-#pragma unroll 1
-        for (int pair = 0; pair < 2; ++pair) {
-            const int64_t from = first - pair * steps, to = last - pair * steps;
-            add(pair, from < 0 ? 0 : from, to < steps ? to : steps);
-        }
-    const float back = kHalf && a.peaks && a.splits == 1 ? power_of_two(-lift_of(a.peaks)) : 1.0f;
-    each_stretch<T>(m0, n0, [&](int i, int64_t m, int64_t n) {
+    if constexpr (FORWARD) make_products<T, true, true>(acc, lds, p);
+    else if (a.adeep) make_products<T, true, false>(acc, lds, p);
+    else make_products<T, false, false>(acc, lds, p);
+    const float back = kHalf && a.lifted && a.splits == 1 ? power_of_two(-lift_of(l.peaks)) : 1.0f;
+    each_stretch<T>((int64_t)p.mi * T::BM, (int64_t)p.ni * T::BN, [&](int i, int64_t m, int64_t n) {
         if (m >= a.M) return;
         float x[4 * T::NJ];
 #pragma unroll
         for (int j = 0; j < 4 * T::NJ; ++j) x[j] = kHalf ? acc[0][i][j / 4][j % 4] * back : acc[0][i][j / 4][j % 4];
-        if (a.splits > 1) store_row<0>(a.parts + (which * a.splits + split) * a.M * a.N8, m * a.N8, n, a.N8, true, x);
-        else store_row<kKind>(a.out[which], m * a.out_ld, n, a.N, a.grid, x);
+        if (a.splits > 1) store_row<0>(a.parts + (p.which * a.splits + p.split) * a.M * a.N8, m * a.N8, n, a.N8, true, x);
+        else store_row<kKind>(a.out[p.which], m * a.out_ld, n, a.N, a.grid, x);
     });
 }
 
-// Splits' parts joined in their order.
-__global__ __launch_bounds__(256) void join_kernel(ProductArgs a) {
-    const float back = kHalf && a.peaks ? power_of_two(-lift_of(a.peaks)) : 1.0f;
-    const int64_t pieces = a.N8 / 4, all = a.M * pieces;
-    const float* parts = a.parts + blockIdx.y * a.splits * a.M * a.N8;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        f32x4 sum = {};
-        for (unsigned s = 0; s < a.splits; ++s) sum += *reinterpret_cast<const f32x4*>(parts + s * a.M * a.N8 + i * 4);
-        const float x[4] = {sum[0] * back, sum[1] * back, sum[2] * back, sum[3] * back};
-        store_row<kKind>(a.out[blockIdx.y], i / pieces * a.out_ld, i % pieces * 4, a.N, a.grid, x);
-    }
+// Splits' parts joined in their order: 4 elements a lane, or one to each of 4 lanes' quarters of the parts.
+__global__ __launch_bounds__(256) void join_kernel(Jobs l) {
+    int which_job = 0;
+#pragma unroll
+    for (int j = 1; j < kMostJobs; ++j) if (j < l.count && blockIdx.x >= l.job[j].first_join) which_job = j;
+    const Job& a = l.job[which_job];
+    const float back = kHalf && a.lifted ? power_of_two(-lift_of(l.peaks)) : 1.0f;
+    const int64_t pieces = a.N8 / 4, all = a.M * pieces, at = (int64_t)(blockIdx.x - a.first_join) * 256 + threadIdx.x;
+    if (at >= all * a.results) return;
+    const int64_t which = at >= all ? 1 : 0, i = at - which * all, row = quotient(i, pieces);
+    const float* parts = a.parts + which * a.splits * a.M * a.N8 + i * 4;
+    f32x4 sum = {};
+#pragma unroll 4
+    for (unsigned s = 0; s < a.splits; ++s) sum += *reinterpret_cast<const f32x4*>(parts + s * a.M * a.N8);
+    const float x[4] = {sum[0] * back, sum[1] * back, sum[2] * back, sum[3] * back};
+    store_row<kKind>(a.out[which], row * a.out_ld, (i - row * pieces) * 4, a.N, a.grid, x);
 }
 
 // Gradients of weights over no rows at all.
@@ -244,40 +412,75 @@ __global__ __launch_bounds__(256) void zero_kernel(Elem* p, int64_t n) {
 // ---------------------------------------------------------------------------------------------------------------
 bool on_grid(const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (int64_t)sizeof(Elem) % 16 == 0; }
 
-template <class T, bool ADEEP, bool BDEEP> hipError_t launch_product(const ProductArgs& a, hipStream_t st) {
-    const unsigned results = a.pairs && !a.together ? 2 : 1;
-    product_kernel<T, ADEEP, BDEEP><<<dim3(a.mt * a.nt, a.splits, results), dim3(T::THREADS), 0, st>>>(a);
+template <class T, bool FORWARD> hipError_t launch_products(Jobs& l, hipStream_t st) {
+    unsigned groups = 0, joins = 0;
+    for (int j = 0; j < l.count; ++j) {
+        Job& a = l.job[j];
+        a.mt = (unsigned)cut_into(a.M, T::BM);
+        a.nt = (unsigned)cut_into(a.N, T::BN);
+        a.first = groups;
+        a.first_join = joins;
+        groups += a.mt * a.nt * a.splits * a.results;
+        if (a.splits > 1) joins += (unsigned)cut_into(a.M * (a.N8 / 4) * a.results, 256);
+    }
+    product_kernel<T, FORWARD><<<dim3(groups), dim3(T::THREADS), 0, st>>>(l);
     if (hipError_t e = hipGetLastError()) return e;
-    if (a.splits > 1) {
-        const int64_t blocks = cut_into(a.M * (a.N8 / 4), 256);
-        join_kernel<<<dim3((unsigned)(blocks < 4096 ? blocks : 4096), results), dim3(256), 0, st>>>(a);
+    if (joins) {
+        // (jobs without splits have no workgroup: the next job's start is theirs)
+        Jobs k = l;
+        k.count = 0;
+        for (int j = 0; j < l.count; ++j) if (l.job[j].splits > 1) k.job[k.count++] = l.job[j];
+        join_kernel<<<dim3(joins), dim3(256), 0, st>>>(k);
     }
     return hipGetLastError();
 }
-template <bool ADEEP, bool BDEEP> hipError_t run_product(ProductArgs a, const ProductCut& c, hipStream_t st) {
-    a.mt = (unsigned)c.mt; a.nt = (unsigned)c.nt; a.splits = (unsigned)c.splits;
-    a.M8 = up_to(a.M, 8); a.N8 = up_to(a.N, 8);
-    a.grid = on_grid(a.out[0], a.out_ld) && (!a.out[1] || on_grid(a.out[1], a.out_ld));
-    return c.tile == 128 ? launch_product<ProductTile<128>, ADEEP, BDEEP>(a, st) : launch_product<ProductTile<64>, ADEEP, BDEEP>(a, st);
+// `l` has everything but cuts and places.
+template <bool FORWARD> hipError_t run_products(const GatedArgs& g, Jobs& l, hipStream_t st) {
+    float* parts = reinterpret_cast<float*>(g.ws + g.plan.parts);
+    for (int j = 0; j < l.count; ++j) {
+        Job& a = l.job[j];
+        const ProductJob& plan = g.plan.products.job[a.planned];
+        a.splits = (unsigned)plan.splits;
+        a.M8 = up_to(a.M, 8); a.N8 = up_to(a.N, 8);
+        a.grid = on_grid(a.out[0], a.out_ld) && (a.results == 1 || on_grid(a.out[1], a.out_ld));
+        a.parts = parts;
+        parts += up_to(plan.parts_bytes(), 256) / 4;
+    }
+    const int choice = g.plan.products.choice;
+    return choice == 2 ? launch_products<Tiles<2>::Product, FORWARD>(l, st)
+         : choice == 1 ? launch_products<Tiles<1>::Product, FORWARD>(l, st) : launch_products<Tiles<0>::Product, FORWARD>(l, st);
 }
 
-template <class T, int ACT> hipError_t launch_pair(HiddenArgs a, bool forward, hipStream_t st) {
-    a.mt = (unsigned)cut_into(a.T, T::BM); a.nt = (unsigned)cut_into(a.H, T::BN);
-    if (forward) hidden_kernel<T, ACT><<<dim3(a.mt * a.nt), dim3(T::THREADS), 0, st>>>(a);
-    else slopes_kernel<T, ACT><<<dim3(a.mt * a.nt), dim3(T::THREADS), 0, st>>>(a);
+template <int CHOICE, int ACT, int PLANES> hipError_t launch_pair(HiddenArgs a, bool forward, hipStream_t st) {
+    using Hidden = typename Tiles<CHOICE>::Hidden;
+    using Slopes = typename Tiles<CHOICE>::Slopes;
+    using Kept = typename Tiles<CHOICE>::Product;
+    const int bm = forward ? Hidden::BM : a.gates ? Kept::BM : Slopes::BM, bn = forward ? Hidden::BN : a.gates ? Kept::BN : Slopes::BN;
+    a.mt = (unsigned)cut_into(a.T, bm);
+    a.nt = (unsigned)cut_into(a.H, bn);
+    const dim3 grid(a.mt * a.nt);
+    if (forward) hidden_kernel<Hidden, ACT, PLANES><<<grid, dim3(Hidden::THREADS), 0, st>>>(a);
+    else if (a.gates) slopes_kernel<Kept, ACT, PLANES, true><<<grid, dim3(Kept::THREADS), 0, st>>>(a);
+    else slopes_kernel<Slopes, ACT, PLANES, false><<<grid, dim3(Slopes::THREADS), 0, st>>>(a);
     return hipGetLastError();
 }
-template <int ACT> hipError_t by_edge(const HiddenArgs& a, bool forward, hipStream_t st) {
-    return pair_tile(a.T, a.H) == 128 ? launch_pair<PairTile<128>, ACT>(a, forward, st) : launch_pair<PairTile<64>, ACT>(a, forward, st);
+template <int CHOICE, int ACT> hipError_t by_planes(const HiddenArgs& a, int planes, bool forward, hipStream_t st) {
+    if constexpr (NP == 1) if (planes == 2) return launch_pair<CHOICE, ACT, 2>(a, forward, st);
+    return launch_pair<CHOICE, ACT, NP>(a, forward, st);
+}
+template <int ACT> hipError_t by_choice(const GatedPlan& p, const HiddenArgs& a, bool forward, hipStream_t st) {
+    const int choice = forward ? p.pairs : p.slopes;
+    return choice == 2 ? by_planes<2, ACT>(a, p.planes, forward, st)
+         : choice == 1 ? by_planes<1, ACT>(a, p.planes, forward, st) : by_planes<0, ACT>(a, p.planes, forward, st);
 }
 hipError_t run_pair(const GatedArgs& g, const HiddenArgs& a, bool forward, hipStream_t st) {
-    return g.activation == FSA_ACT_SILU ? by_edge<FSA_ACT_SILU>(a, forward, st)
-         : g.activation == FSA_ACT_GELU ? by_edge<FSA_ACT_GELU>(a, forward, st) : by_edge<FSA_ACT_RELU>(a, forward, st);
+    return g.activation == FSA_ACT_SILU ? by_choice<FSA_ACT_SILU>(g.plan, a, forward, st)
+         : g.activation == FSA_ACT_GELU ? by_choice<FSA_ACT_GELU>(g.plan, a, forward, st) : by_choice<FSA_ACT_RELU>(g.plan, a, forward, st);
 }
 
 struct Operands { Side x, gate, up, down, grad_y; };
 
-hipError_t lay_out(const GatedArgs& a, Operands& o, hipStream_t st) {
+hipError_t lay_out(const GatedArgs& a, Operands& o, bool peaks, hipStream_t st) {
     const Matrix* from[5] = {&a.x, &a.gate, &a.up, &a.down, &a.grad_y};
     Side* to[5] = {&o.x, &o.gate, &o.up, &o.down, &o.grad_y};
     const size_t at[5] = {a.plan.x, a.plan.gate, a.plan.up, a.plan.down, a.plan.grad_y};
@@ -295,9 +498,13 @@ hipError_t lay_out(const GatedArgs& a, Operands& o, hipStream_t st) {
         l.first[l.count + 1] = l.first[l.count] + from[i]->rows * (ld / 8);
         ++l.count;
     }
-    if (l.count == 0) return hipSuccess;
     const int64_t blocks = cut_into(l.first[l.count], 256);
-    pack_kernel<<<dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, st>>>(l);
+    l.packers = (unsigned)(blocks < 8192 ? blocks : 8192);
+    l.grad_y = a.grad_y;
+    l.peaks = reinterpret_cast<float*>(a.ws + a.plan.peaks);
+    const unsigned groups = l.packers + (peaks ? kGatedPeaks : 0);
+    if (groups == 0) return hipSuccess;
+    pack_kernel<<<dim3(groups), dim3(256), 0, st>>>(l);
     return hipGetLastError();
 }
 
@@ -307,29 +514,41 @@ HiddenArgs hidden_args(const GatedArgs& a, const Operands& o) {
     h.h = reinterpret_cast<uint16_t*>(a.ws + a.plan.h);
     h.dg = reinterpret_cast<uint16_t*>(a.ws + a.plan.dg);
     h.du = reinterpret_cast<uint16_t*>(a.ws + a.plan.du);
-    h.T = a.s.T; h.D = a.s.D; h.H = a.s.H; h.O = a.s.O;
-    h.H8 = a.plan.H8;
+    h.gates = a.gates;
+    h.T = a.s.T; h.D = a.s.D; h.H = a.s.H; h.O = a.s.O; h.H8 = a.plan.H8;
     h.peaks = reinterpret_cast<const float*>(a.ws + a.plan.peaks);
     return h;
 }
 
+// Pairs whose products' sum is that of all planes of `held` (h, dg or du) with `other`; fp32's planes belong to one pair.
+void add_pairs(Job& j, int result, int& pairs, const GatedPlan& p, Side held, const Side& other, bool held_first) {
+    for (int q = 0; q < (NP == 1 ? p.planes : 1); ++q) {
+        j.a[result][pairs] = held_first ? held : other;
+        j.b[result][pairs] = held_first ? other : held;
+        held.p += held.plane;
+        ++pairs;
+    }
+}
+
 hipError_t forward(const GatedArgs& a, hipStream_t st) {
     Operands o{};
-    if (hipError_t e = lay_out(a, o, st)) return e;
+    if (hipError_t e = lay_out(a, o, false, st)) return e;
     const HiddenArgs h = hidden_args(a, o);
     if (hipError_t e = run_pair(a, h, true, st)) return e;
-    ProductArgs p{};
-    p.a[0] = {h.h, h.H8, a.s.T * h.H8}; p.b[0] = o.down;
-    p.out[0] = a.y;
-    p.M = a.s.T; p.N = a.s.O; p.K = a.s.H; p.out_ld = a.s.O;
-    p.parts = reinterpret_cast<float*>(a.ws + a.plan.parts);
-    return run_product<true, true>(p, a.plan.answer, st);
+    Jobs l{};
+    l.count = 1;
+    Job& j = l.job[0];
+    add_pairs(j, 0, j.pairs, a.plan, {h.h, h.H8, a.s.T * h.H8}, o.down, true);
+    j.results = 1;
+    j.out[0] = a.y;
+    j.M = a.s.T; j.N = a.s.O; j.K = a.s.H; j.out_ld = a.s.O;
+    j.adeep = true;
+    return run_products<true>(a, l, st);
 }
 
 hipError_t backward(const GatedArgs& a, hipStream_t st) {
-    const bool want_w = a.grad_gate || a.grad_up || a.grad_down;
+    void* const outs[4] = {a.grad_gate, a.grad_up, a.grad_down, a.grad_x};
     if (a.s.T == 0) {
-        void* const outs[3] = {a.grad_gate, a.grad_up, a.grad_down};
         const int64_t sizes[3] = {a.s.H * a.s.D, a.s.H * a.s.D, a.s.O * a.s.H};
         for (int i = 0; i < 3; ++i)
             if (outs[i]) {
@@ -339,47 +558,46 @@ hipError_t backward(const GatedArgs& a, hipStream_t st) {
             }
         return hipSuccess;
     }
-    if (!want_w && !a.grad_x) return hipSuccess;
+    if (!outs[0] && !outs[1] && !outs[2] && !outs[3]) return hipSuccess;
     Operands o{};
-    if (hipError_t e = lay_out(a, o, st)) return e;
-    float* peaks = reinterpret_cast<float*>(a.ws + a.plan.peaks);
-    if (kHalf) {
-        peaks_kernel<<<dim3(kGatedPeaks), dim3(256), 0, st>>>(a.grad_y, peaks);
-        if (hipError_t e = hipGetLastError()) return e;
-    }
+    if (hipError_t e = lay_out(a, o, kHalf, st)) return e;
     const HiddenArgs h = hidden_args(a, o);
     if (hipError_t e = run_pair(a, h, false, st)) return e;
     const int64_t plane = a.s.T * h.H8;
     const Side hs = {h.h, h.H8, plane}, dg = {h.dg, h.H8, plane}, du = {h.du, h.H8, plane};
-    ProductArgs p{};
-    p.parts = reinterpret_cast<float*>(a.ws + a.plan.parts);
-    if (a.grad_x) {
-        p.a[0] = dg; p.a[1] = du; p.b[0] = o.gate; p.b[1] = o.up;
-        p.together = p.pairs = true;
-        p.out[0] = a.grad_x; p.out[1] = nullptr;
-        p.M = a.s.T; p.N = a.s.D; p.K = a.s.H; p.out_ld = a.s.D;
-        p.peaks = kHalf ? peaks : nullptr;
-        if (hipError_t e = run_product<true, false>(p, a.plan.dx, st)) return e;
-    }
-    p.together = p.pairs = false;
-    p.K = a.s.T;
-    if (a.grad_down) {
-        p.a[0] = o.grad_y; p.b[0] = hs;
-        p.out[0] = a.grad_down; p.out[1] = nullptr;
-        p.M = a.s.O; p.N = a.s.H; p.out_ld = a.s.H;
-        p.peaks = nullptr;
-        if (hipError_t e = run_product<false, false>(p, a.plan.down_grad, st)) return e;
-    }
+    Jobs l{};
+    l.peaks = h.peaks;
     if (a.grad_gate || a.grad_up) {
-        const bool both = a.grad_gate && a.grad_up;
-        p.pairs = both;
-        p.a[0] = a.grad_gate ? dg : du; p.a[1] = du; p.b[0] = p.b[1] = o.x;
-        p.out[0] = a.grad_gate ? a.grad_gate : a.grad_up; p.out[1] = both ? a.grad_up : nullptr;
-        p.M = a.s.H; p.N = a.s.D; p.out_ld = a.s.D;
-        p.peaks = kHalf ? peaks : nullptr;
-        if (hipError_t e = run_product<false, false>(p, a.plan.gate_grad, st)) return e;
+        Job& j = l.job[l.count++];
+        for (int i = 0; i < 2; ++i)
+            if (outs[i]) {
+                j.pairs = 0;
+                add_pairs(j, j.results, j.pairs, a.plan, i == 0 ? dg : du, o.x, true);
+                j.out[j.results++] = outs[i];
+            }
+        j.M = a.s.H; j.N = a.s.D; j.K = a.s.T; j.out_ld = a.s.D;
+        j.lifted = true;
+        j.planned = kJobGates;
     }
-    return hipSuccess;
+    if (a.grad_down) {
+        Job& j = l.job[l.count++];
+        j.planned = kJobDown;
+        add_pairs(j, 0, j.pairs, a.plan, hs, o.grad_y, false);
+        j.results = 1;
+        j.out[0] = a.grad_down;
+        j.M = a.s.O; j.N = a.s.H; j.K = a.s.T; j.out_ld = a.s.H;
+    }
+    if (a.grad_x) {
+        Job& j = l.job[l.count++];
+        add_pairs(j, 0, j.pairs, a.plan, dg, o.gate, true);
+        add_pairs(j, 0, j.pairs, a.plan, du, o.up, true);
+        j.results = 1;
+        j.out[0] = a.grad_x;
+        j.M = a.s.T; j.N = a.s.D; j.K = a.s.H; j.out_ld = a.s.D;
+        j.adeep = j.lifted = true;
+        j.planned = kJobX;
+    }
+    return run_products<false>(a, l, st);
 }
 
 }  // namespace

@@ -16,7 +16,7 @@ using namespace product;
 
 template <int EDGE> using OrthoTile = Tile<2, true, EDGE, EDGE, EDGE == 128 ? 32 : 64, 2, 2>;
 template <int KIND> using ElemOf = typename std::conditional<KIND == 0, float, uint16_t>::type;
-constexpr float two_to(int e) { return e > 0 ? 2.0f * two_to(e - 1) : e < 0 ? 0.5f * two_to(e + 1) : 1.0f; }
+template <int E> constexpr float kTwoTo = E > 0 ? (float)(1ull << (E > 0 ? E : 0)) : 1.0f / (float)(1ull << (E < 0 ? -E : 0));
 
 template <int KIND> __device__ __forceinline__ float number(ElemOf<KIND> e) {
     if constexpr (KIND == 0) return e;
@@ -28,10 +28,23 @@ template <int KIND> __global__ __launch_bounds__(256) void squares_kernel(OrthoA
     __shared__ double lds[4];
     const ElemOf<KIND>* g = static_cast<const ElemOf<KIND>*>(a.g) + blockIdx.y * a.batch_stride;
     double sum = 0.0;
-    const int64_t all = a.s.M * a.s.N;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const double x = number<KIND>(g[i / a.s.N * a.stride + i % a.s.N]);
-        sum = fma(x, x, sum);
+    // a wave's 64 pieces of 4 elements, row by row: few rows take several waves to one
+    const int64_t pieces = cut_into(a.s.N, 256), all = a.s.M * pieces, waves = (int64_t)gridDim.x * 4;
+    const int lane = threadIdx.x & 63;
+    for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < all; i += waves) {
+        const int64_t row = all <= 0x7fffffff ? (uint32_t)i / (uint32_t)pieces : i / pieces, c = (i - row * pieces) * 256 + lane * 4;
+        const ElemOf<KIND>* p = g + row * a.stride + c;
+        ElemOf<KIND> e[4] = {};
+        if (c + 4 <= a.s.N) __builtin_memcpy(e, p, sizeof(e));
+        else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j) if (c + j < a.s.N) e[j] = p[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const double x = number<KIND>(e[j]);
+            sum = fma(x, x, sum);
+        }
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
@@ -59,18 +72,18 @@ template <int KIND> __global__ __launch_bounds__(256) void first_kernel(OrthoArg
     const ElemOf<KIND>* g = static_cast<const ElemOf<KIND>*>(a.g) + batch * a.batch_stride;
     for (int i = threadIdx.x; i < 64 * 64; i += 256) {
         const int64_t r = r0 + i / 64, c = c0 + i % 64;
-        tile[i / 64][i % 64] = r < a.s.M && c < a.s.N ? number<KIND>(g[r * a.stride + c]) * unit * two_to(kUnitX) : 0.0f;
+        tile[i / 64][i % 64] = r < a.s.M && c < a.s.N ? number<KIND>(g[r * a.stride + c]) * unit * kTwoTo<kUnitX> : 0.0f;
     }
     __syncthreads();
     const int64_t m = a.plan.m, n = a.plan.n, n8 = a.plan.n8, plane = m * n8;
     uint16_t* x = reinterpret_cast<uint16_t*>(a.ws + a.plan.x[0]) + batch * 2 * plane;
-    for (int i = threadIdx.x; i < 64 * 16; i += 256) {
-        const int row = i / 16, col = i % 16 * 4;
+    for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+        const int row = i / 8, col = i % 8 * 8;
         const int64_t xm = (tall ? c0 : r0) + row, xn = (tall ? r0 : c0) + col;
         if (xm >= m) continue;
-        float v[4];
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = tall ? tile[col + j][row] : tile[row][col + j];
+        for (int j = 0; j < 8; ++j) v[j] = tall ? tile[col + j][row] : tile[row][col + j];
         store_planes<2, true>(x, plane, xm * n8 + xn, xn, n, v);
     }
 }
@@ -88,14 +101,14 @@ struct StepArgs {
 // W elements of two planes from `at` on.
 template <int W> __device__ __forceinline__ void load_planes(const uint16_t* p, int64_t plane, int64_t at, int64_t n, int64_t end, float (&x)[W]) {
 #pragma unroll
-    for (int i = 0; i < W; i += 4) {
-        u32x2 hi = {}, lo = {};
+    for (int i = 0; i < W; i += 8) {
+        u32x4 hi = {}, lo = {};
         if (n + i < end) {
-            hi = *reinterpret_cast<const u32x2*>(p + at + i);
-            lo = *reinterpret_cast<const u32x2*>(p + plane + at + i);
+            hi = *reinterpret_cast<const u32x4*>(p + at + i);
+            lo = *reinterpret_cast<const u32x4*>(p + plane + at + i);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 8; ++j) {
             const int s = j % 2 * 16;
             x[i + j] = as_float<true>(hi[j / 2] >> s & 0xffff) + as_float<true>(lo[j / 2] >> s & 0xffff);
         }
@@ -103,7 +116,7 @@ template <int W> __device__ __forceinline__ void load_planes(const uint16_t* p, 
 }
 
 enum { kGram, kPoly, kUpdate };
-template <class T, int WHAT, int KIND> __global__ __launch_bounds__(T::THREADS) void step_kernel(StepArgs a) {
+template <class T, int WHAT, int KIND> __global__ __launch_bounds__(T::THREADS, T::waves(1)) void step_kernel(StepArgs a) {
     __shared__ __attribute__((aligned(256))) char lds[T::lds_bytes(1)];
     unsigned mi, ni;
     tile_of(blockIdx.x, a.mt, a.nt, mi, ni);
@@ -112,16 +125,16 @@ template <class T, int WHAT, int KIND> __global__ __launch_bounds__(T::THREADS) 
     const uint16_t *x = a.x + batch * 2 * wide, *sq = a.sq + batch * 2 * square, *poly = a.poly + batch * 2 * square;
     Sums<T, 1> acc = {};
     const Side sx = {x, a.n8, wide}, sa = {sq, a.m8, square}, sp = {poly, a.m8, square};
-    if constexpr (WHAT == kGram) {
-        const Side b[1] = {sx};
-        accumulate<T, true, true, 1>(acc, lds, sx, b, m0, a.m, n0, a.m, 0, a.n);
-    } else if constexpr (WHAT == kPoly) {
-        const Side b[1] = {sa};
-        accumulate<T, true, true, 1>(acc, lds, sa, b, m0, a.m, n0, a.m, 0, a.m);
-    } else {
-        const Side b[1] = {sx};
-        accumulate<T, true, false, 1>(acc, lds, sp, b, m0, a.m, n0, a.n8, 0, a.m);
-    }
+    using Stream = OneStream<T, true, WHAT != kUpdate, 1>;
+    Stream stream;
+    const Side b[1] = {WHAT == kPoly ? sa : sx};
+    const int64_t depth = WHAT == kGram ? a.n : a.m;
+    stream.flow.start(WHAT == kGram ? sx : WHAT == kPoly ? sa : sp, b, m0, a.m, n0, WHAT == kUpdate ? a.n8 : a.m, 0, depth);
+    Ring<T, T::stage_bytes(1), Stream> ring{lds, stream};
+    ring.fill();
+    accumulate<T, true, WHAT != kUpdate, 1>(acc, ring, cut_into(depth, T::BK));
+    ring.end();
+    if constexpr (WHAT == kUpdate) settle<T, 1>(acc);
     each_stretch<T>(m0, n0, [&](int i, int64_t m, int64_t n) {
         if (m >= a.m) return;
         constexpr int W = 4 * T::NJ;
@@ -130,23 +143,23 @@ template <class T, int WHAT, int KIND> __global__ __launch_bounds__(T::THREADS) 
         for (int j = 0; j < W; ++j) v[j] = acc[0][i][j / 4][j % 4];
         if constexpr (WHAT == kGram) {
 #pragma unroll
-            for (int j = 0; j < W; ++j) v[j] *= two_to(kUnitA - 2 * kUnitX);
+            for (int j = 0; j < W; ++j) v[j] *= kTwoTo<kUnitA - 2 * kUnitX>;
             store_planes<2, true>(a.to + batch * 2 * square, square, m * a.m8 + n, n, a.m, v);
         } else if constexpr (WHAT == kPoly) {
             float old[W];
             load_planes<W>(sq, square, m * a.m8 + n, n, a.m8, old);
 #pragma unroll
-            for (int j = 0; j < W; ++j) v[j] = fmaf(a.c * two_to(kUnitP - 2 * kUnitA), v[j], a.b * two_to(kUnitP - kUnitA) * old[j]);
+            for (int j = 0; j < W; ++j) v[j] = fmaf(a.c * kTwoTo<kUnitP - 2 * kUnitA>, v[j], a.b * kTwoTo<kUnitP - kUnitA> * old[j]);
             store_planes<2, true>(a.to + batch * 2 * square, square, m * a.m8 + n, n, a.m, v);
         } else {
             float old[W];
             load_planes<W>(x, wide, m * a.n8 + n, n, a.n8, old);
 #pragma unroll
-            for (int j = 0; j < W; ++j) v[j] = fmaf(two_to(-kUnitP), v[j], a.a * old[j]);
+            for (int j = 0; j < W; ++j) v[j] = fmaf(kTwoTo<-kUnitP>, v[j], a.a * old[j]);
             if (!a.out) store_planes<2, true>(a.to + batch * 2 * wide, wide, m * a.n8 + n, n, a.n, v);
             else {
                 ElemOf<KIND>* out = static_cast<ElemOf<KIND>*>(a.out) + batch * a.m * a.n;
-                const float back = a.scale * two_to(-kUnitX);
+                const float back = a.scale * kTwoTo<-kUnitX>;
 #pragma unroll
                 for (int j = 0; j < W; ++j) v[j] *= back;
                 if (!a.tall) store_row<KIND>(out, m * a.n, n, a.n, a.grid, v);

@@ -56,18 +56,18 @@ def test_norm_backward(fsa):
 
 
 def _gated(fsa, **kw):
-    a = dict(x=FAKE, xs=64, g=FAKE, gs=64, u=FAKE, us=64, d=FAKE, ds=128, t=1, act=0, T=8, D=64, H=128, O=32, y=FAKE, ws=FAKE, n=1 << 40)
+    a = dict(x=FAKE, xs=64, g=FAKE, gs=64, u=FAKE, us=64, d=FAKE, ds=128, t=1, act=0, T=8, D=64, H=128, O=32, y=FAKE, k=None, ws=FAKE, n=1 << 40)
     a.update(kw)
     return fsa.lib().fsa_gated_fwd(a["x"], a["xs"], a["g"], a["gs"], a["u"], a["us"], a["d"], a["ds"], a["t"], a["act"], a["T"], a["D"],
-                                   a["H"], a["O"], a["y"], a["ws"], a["n"], None)
+                                   a["H"], a["O"], a["y"], a["k"], a["ws"], a["n"], None)
 
 
 def _gated_bwd(fsa, **kw):
-    a = dict(gy=FAKE, gys=32, x=FAKE, xs=64, g=FAKE, gs=64, u=FAKE, us=64, d=FAKE, ds=128, t=1, act=0, T=8, D=64, H=128, O=32,
+    a = dict(gy=FAKE, gys=32, x=FAKE, xs=64, g=FAKE, gs=64, u=FAKE, us=64, d=FAKE, ds=128, t=1, act=0, T=8, D=64, H=128, O=32, k=FAKE,
              gx=FAKE, gg=FAKE, gu=FAKE, gd=FAKE, ws=FAKE, n=1 << 40)
     a.update(kw)
     return fsa.lib().fsa_gated_bwd(a["gy"], a["gys"], a["x"], a["xs"], a["g"], a["gs"], a["u"], a["us"], a["d"], a["ds"], a["t"], a["act"],
-                                   a["T"], a["D"], a["H"], a["O"], a["gx"], a["gg"], a["gu"], a["gd"], a["ws"], a["n"], None)
+                                   a["T"], a["D"], a["H"], a["O"], a["k"], a["gx"], a["gg"], a["gu"], a["gd"], a["ws"], a["n"], None)
 
 
 @pytest.mark.parametrize("which", ["forward", "backward"])
@@ -76,7 +76,7 @@ def test_gated(fsa, which):
     for name in ("x", "g", "u", "d", "y" if which == "forward" else "gy"):
         assert call(fsa, **{name: None}) == NULL, name
         assert call(fsa, **{name: FAKE + 1}) == ALIGN, name
-    assert call(fsa, t=5) == DTYPE
+    assert call(fsa, t=5) == DTYPE and call(fsa, k=FAKE + 2) == ALIGN
     for bad in (dict(act=-1), dict(act=3), dict(T=-1), dict(T=(1 << 26) + 1), dict(D=0), dict(H=0), dict(O=0), dict(D=65537, xs=65537, gs=65537, us=65537),
                 dict(H=65537, ds=65537), dict(xs=63), dict(gs=63), dict(us=0), dict(ds=127), dict(xs=1 << 32)):
         assert call(fsa, **bad) == ARG, bad

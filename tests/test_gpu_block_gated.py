@@ -22,9 +22,12 @@ def _check(x, wg, wu, wd, gy, act, dtype):
     want = bb.gated(x, wg, wu, wd, gy, act, dtype)
     y = fsa.fsa_gated_fwd(x, wg, wu, wd, activation=act)
     bb.check("y", y, *want["y"])
-    got = fsa.fsa_gated_bwd(gy, x, wg, wu, wd, activation=act)
-    for name, g in zip(("grad_x", "grad_gate", "grad_up", "grad_down"), got):
-        bb.check(name, g, *want[name])
+    kept, gates = fsa.fsa_gated_fwd(x, wg, wu, wd, activation=act, emit_gates=True)
+    assert torch.equal(kept, y)
+    for given in (None, gates):
+        got = fsa.fsa_gated_bwd(gy, x, wg, wu, wd, given, activation=act)
+        for name, g in zip(("grad_x", "grad_gate", "grad_up", "grad_down"), got):
+            bb.check(name, g, *want[name])
 
 
 @pytest.mark.parametrize("dtype", TYPES)
