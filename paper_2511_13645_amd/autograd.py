@@ -177,9 +177,11 @@ def fused_residual_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optiona
                         ) -> Tuple[torch.Tensor, torch.Tensor]:
     """Differentiable root-mean-square norm of the rows s = x + residual [T,D], times weight [D].  Returns (y, s): what the next
     layer takes and what its answer is added to.  Without a residual s is x itself."""
-    if residual is None:
-        return _ResidualNorm.apply(x, weight, None, float(eps)), x
-    return _ResidualNorm.apply(x, weight, residual, float(eps))
+    r = binding.norm(x, weight, residual, float(eps))
+    if r is None:
+        r = _ResidualNorm.apply(x, weight, residual, float(eps))
+        r = (r, None) if residual is None else r
+    return r if residual is not None else (r[0], x)
 
 
 class _GatedFeedForward(torch.autograd.Function):
@@ -206,5 +208,8 @@ def fused_gated_feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.
     """Differentiable gated feed-forward block (act(x w_gate^T) * (x w_up^T)) w_down^T of rows x [T,D]: w_gate, w_up [H,D],
     w_down [O,H], one type.  What is kept for the backward is its inputs, and the two hidden products where that is quicker than making them
     again."""
+    y = binding.gated(x, w_gate, w_up, w_down, activation)
+    if y is not None:
+        return y
     keep = torch.is_grad_enabled() and any(t.requires_grad for t in (x, w_gate, w_up, w_down))
     return _GatedFeedForward.apply(x, w_gate, w_up, w_down, activation, keep)

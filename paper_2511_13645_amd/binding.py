@@ -28,6 +28,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libfsa_hip.so")
 HOST_PATH = build.host_lib()
 CLASS_HOST_PATH = build.class_host_lib()
+BLOCK_HOST_PATH = build.block_host_lib()
 
 FSA_F32, FSA_BF16, FSA_F16 = 0, 1, 2
 FSA_I32, FSA_I64 = 0, 1
@@ -49,12 +50,15 @@ EXPORTS = ("fsa_sample_mean_fwd", "fsa_mean_replay_fwd", "fsa_mean_bwd", "fsa_me
 
 _lib: Optional[ctypes.CDLL] = None
 _class_host = None                              # the module _fsa_class_host, likewise
+_block_host = None                              # and _fsa_block_host
 _host = None                                    # the module _fsa_host, once the library is loaded; None without it
 _HOST_ENTRIES = ("fsa_sample_mean_fwd", "fsa_sample_wmean_fwd", "fsa_mean_replay_fwd", "fsa_mean_bwd", "fsa_mean_bwd_ws",
                  "fsa_mean_bwd_lp_ws", "fsa_wmean_bwd_ws", "fsa_mean_bwd_dense", "fsa_mean_bwd_dense_workspace_bytes",
                  "fsa_mean_bwd_dense_pays")              # entry points that _fsa_host calls
 _CLASS_HOST_ENTRIES = ("fsa_class_fwd_workspace_bytes", "fsa_class_bwd_workspace_bytes", "fsa_xent_fwd", "fsa_xent_bwd",
                        "fsa_distill_fwd", "fsa_distill_bwd")             # the same of _fsa_class_host
+_BLOCK_HOST_ENTRIES = ("fsa_norm_fwd", "fsa_norm_bwd", "fsa_norm_bwd_workspace_bytes", "fsa_gated_fwd", "fsa_gated_bwd",
+                       "fsa_gated_fwd_workspace_bytes", "fsa_gated_bwd_workspace_bytes", "fsa_gated_keep_pays")      # and of _fsa_block_host
 _PLAIN, _WORKSPACE, _LOW_PRECISION, _WEIGHTED = range(4)                # backward entry points, as _fsa_host.bwd counts them
 
 
@@ -66,7 +70,7 @@ class FsaError(RuntimeError):
 
 def lib() -> ctypes.CDLL:
     """Load the HIP library; fail loudly when it has not been built."""
-    global _lib, _host, _class_host
+    global _lib, _host, _class_host, _block_host
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError("HIP library missing: %s (build it with __graft_entry__.build())" % LIB_PATH)
@@ -151,6 +155,7 @@ def lib() -> ctypes.CDLL:
         L.fsa_status_string.argtypes = [ci]
         L.fsa_status_string.restype = ctypes.c_char_p
         _lib, _host, _class_host = L, _load_host(L), _load_class_host(L)
+        _block_host = _load_block_host(L)
     return _lib
 
 
@@ -162,6 +167,11 @@ def _load_host(L: ctypes.CDLL):
 def _load_class_host(L: ctypes.CDLL):
     """The same for the class losses."""
     return _load_module(L, "_fsa_class_host", CLASS_HOST_PATH, _CLASS_HOST_ENTRIES)
+
+
+def _load_block_host(L: ctypes.CDLL):
+    """The same for the norm and the gated block."""
+    return _load_module(L, "_fsa_block_host", BLOCK_HOST_PATH, _BLOCK_HOST_ENTRIES)
 
 
 def _load_module(L: ctypes.CDLL, name: str, path: str, entries: Sequence[str]):
@@ -948,6 +958,10 @@ def fsa_norm_fwd(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
                  stream: Optional[torch.cuda.Stream] = None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """Root-mean-square norm of rows s = x + residual [T,D] (rounded to their type), times weight [D] (of any of the three types).
     Returns (y, s | None), s where there is a residual.  `stream`: see fsa_xent_fwd."""
+    if _block_host is not None and stream is None:
+        r = _block_host.norm_fwd(x, weight, residual, eps)
+        if _taken(r, "fsa_norm_fwd"):
+            return r
     xs = _rows(x, "x")
     code = _x_dtype(x)
     T, D = x.shape
@@ -966,6 +980,16 @@ def fsa_norm_fwd(x: torch.Tensor, weight: torch.Tensor, residual: Optional[torch
     if rc != FSA_OK:
         raise FsaError(rc, "fsa_norm_fwd")
     return y, s
+
+
+def norm(x, weight, residual, eps: float):
+    """The differentiable (y, s | None) through the native host path, or None: then autograd.py's own function takes the call."""
+    lib()
+    if _block_host is not None:
+        r = _block_host.norm(x, weight, residual, eps)
+        if _taken(r, "fsa_norm_fwd"):
+            return r
+    return None
 
 
 def fsa_norm_bwd(grad_y: Optional[torch.Tensor], grad_s: Optional[torch.Tensor], s: torch.Tensor, weight: torch.Tensor,
@@ -1026,6 +1050,10 @@ def fsa_gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_d
     type; activation "silu", "gelu" (by the error function) or "relu".  Returns y [T,O], with `emit_gates` (y, gates): x w_gate^T and
     x w_up^T [2,T,H] in fp32, which spare the backward making them again (fsa_gated_keep_pays).  `workspace`: see
     fsa_gated_fwd_workspace_bytes; torch's memory without one.  `stream`: see fsa_xent_fwd."""
+    if _block_host is not None and stream is None and workspace is None and not emit_gates:
+        r = _block_host.gated_fwd(x, w_gate, w_up, w_down, _ACTIVATIONS.get(activation))
+        if _taken(r, "fsa_gated_fwd"):
+            return r
     lead, (T, D, H, O) = _gated_operands(x, w_gate, w_up, w_down, activation)
     L = lib()
     with _on(x, stream):
@@ -1036,6 +1064,16 @@ def fsa_gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_d
     if rc != FSA_OK:
         raise FsaError(rc, "fsa_gated_fwd")
     return (y, gates) if emit_gates else y
+
+
+def gated(x, w_gate, w_up, w_down, activation: str):
+    """The differentiable block through the native host path, or None: then autograd.py's own function takes the call."""
+    lib()
+    if _block_host is not None:
+        r = _block_host.gated(x, w_gate, w_up, w_down, _ACTIVATIONS.get(activation))
+        if _taken(r, "fsa_gated_fwd"):
+            return r
+    return None
 
 
 def fsa_gated_bwd(grad_y: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,

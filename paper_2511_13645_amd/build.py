@@ -29,6 +29,7 @@ HIPCC_FLAGS = [
 
 HOST_SOURCE = os.path.join(HERE, "csrc_host", "fsa_host.cpp")
 CLASS_HOST_SOURCE = os.path.join(HERE, "csrc_host", "fsa_class_host.cpp")
+BLOCK_HOST_SOURCE = os.path.join(HERE, "csrc_host", "fsa_block_host.cpp")
 
 
 def host_lib() -> str:
@@ -40,6 +41,11 @@ def host_lib() -> str:
 def class_host_lib() -> str:
     """The same for the class losses' host path."""
     return _module("_fsa_class_host")
+
+
+def block_host_lib() -> str:
+    """The same for the host path of the norm and the gated block."""
+    return _module("_fsa_block_host")
 
 
 def _module(name: str) -> str:
@@ -92,6 +98,11 @@ def build_class_host(extra_flags=(), verbose: bool = False, out: Optional[str] =
     return _build_module(CLASS_HOST_SOURCE, extra_flags, verbose, out or class_host_lib())
 
 
+def build_block_host(extra_flags=(), verbose: bool = False, out: Optional[str] = None) -> str:
+    """Compile the host path of the norm and the gated block, a module of its own."""
+    return _build_module(BLOCK_HOST_SOURCE, extra_flags, verbose, out or block_host_lib())
+
+
 def _build_module(source: str, extra_flags, verbose: bool, out: str) -> str:
     import torch
     base = os.path.dirname(torch.__file__)
@@ -109,13 +120,14 @@ def _build_module(source: str, extra_flags, verbose: bool, out: str) -> str:
 
 
 def is_stale() -> bool:
-    if not os.path.exists(LIB) or not os.path.exists(host_lib()) or not os.path.exists(class_host_lib()):
+    if not all(os.path.exists(f) for f in (LIB, host_lib(), class_host_lib(), block_host_lib())):
         return True
     newest = max(os.path.getmtime(os.path.join(CSRC, f)) for f in SOURCES + HEADERS)
     newest_host = max(os.path.getmtime(f) for f in (HOST_SOURCE, ABI_HEADER))
     newest_class = max(os.path.getmtime(f) for f in (CLASS_HOST_SOURCE, ABI_HEADER))
+    newest_block = max(os.path.getmtime(f) for f in (BLOCK_HOST_SOURCE, ABI_HEADER))
     return (os.path.getmtime(LIB) < newest or os.path.getmtime(host_lib()) < newest_host or
-            os.path.getmtime(class_host_lib()) < newest_class)
+            os.path.getmtime(class_host_lib()) < newest_class or os.path.getmtime(block_host_lib()) < newest_block)
 
 
 if __name__ == "__main__":
@@ -132,5 +144,6 @@ if __name__ == "__main__":
         try:
             print(build_host(verbose=True))
             print(build_class_host(verbose=True))
+            print(build_block_host(verbose=True))
         except (OSError, subprocess.CalledProcessError) as e:
             print("the host path was not built, the binding goes without it: %s" % e, file=sys.stderr)

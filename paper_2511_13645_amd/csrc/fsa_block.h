@@ -251,18 +251,25 @@ struct GatedArgs {
 // X [m,n] with m <= n (the transpose of a tall matrix): two fp16 planes of X 2^13, likewise A = X X^T and P = b A + c A^2 of
 // which planes hold A 2^13 and P 2^10.
 constexpr int kMostSteps = 32;
-constexpr int kOrthoPeaks = 64;                         // workgroups a matrix that sum its squares
+constexpr int kOrthoPeaks = 256;                        // workgroups a matrix that sum its squares
 constexpr int kUnitX = 13, kUnitA = 13, kUnitP = 10;
 
 struct OrthoShape {
     int64_t B, M, N;
     int kind;
 };
+constexpr TileChoice kTilesTwo[kTileKinds] = {{64, 64, 860}, {128, 128, 1150}, {256, 256, 1400}};
 struct OrthoPlan {
-    size_t squares, x[2], a, p, bytes;
+    size_t squares, x[2], a, p, parts, bytes;
     int64_t m, n, m8, n8;
-    int tile_square, tile_wide;                         // of m x m and m x n results
+    int gram, poly, update;                             // choices of tiles
+    int64_t splits;                                     // of the gram matrix' depth: then half of its tiles are made, and joined
 };
+constexpr int64_t upper_tiles(int64_t m, int tile) { return cut_into(m, tile) * (cut_into(m, tile) + 1) / 2; }
+inline double ortho_us(int choice, int64_t tiles, int64_t depth) {
+    const TileChoice& t = kTilesTwo[choice];
+    return (double)cut_into(tiles, kChip) * (2.0 * t.m * t.n * 3.0 * (double)depth / (t.rate / kChip) * 1e-6 + kTurn);
+}
 inline OrthoPlan ortho_plan(const OrthoShape& s) {
     OrthoPlan p{};
     size_t at = 0;
@@ -270,12 +277,28 @@ inline OrthoPlan ortho_plan(const OrthoShape& s) {
     p.m = s.M < s.N ? s.M : s.N;
     p.n = s.M < s.N ? s.N : s.M;
     p.m8 = up_to(p.m, 8); p.n8 = up_to(p.n, 8);
-    p.tile_square = s.B * cut_into(p.m, 128) * cut_into(p.m, 128) >= kChip ? 128 : 64;
-    p.tile_wide = s.B * cut_into(p.m, 128) * cut_into(p.n, 128) >= kChip ? 128 : 64;
+    double gram = 1e30, poly = 1e30, update = 1e30;
+    for (int c = 0; c < kTileKinds; ++c) {
+        const int64_t mt = cut_into(p.m, kTilesTwo[c].m), nt = cut_into(p.n, kTilesTwo[c].n);
+        double us = ortho_us(c, s.B * mt * mt, p.m);
+        if (us < poly) { poly = us; p.poly = c; }
+        us = ortho_us(c, s.B * mt * nt, p.m);
+        if (us < update) { update = us; p.update = c; }
+        us = ortho_us(c, s.B * mt * mt, p.n);
+        if (us < gram) { gram = us; p.gram = c; p.splits = 1; }
+        const int64_t upper = s.B * upper_tiles(p.m, kTilesTwo[c].m);
+        for (int64_t splits = 2; splits <= 16 && p.n / splits >= 128; ++splits) {
+            const double bytes = (double)(upper * splits) * kTilesTwo[c].m * kTilesTwo[c].n * 4.0;
+            us = ortho_us(c, upper * splits, p.n / splits) + kJoin + bytes * 2.0 / 4e6;
+            if (us < gram) { gram = us; p.gram = c; p.splits = splits; }
+        }
+    }
     p.squares = room(s.B * kOrthoPeaks * 8);
     for (size_t& x : p.x) x = room(s.B * p.m * p.n8 * 4);
     p.a = room(s.B * p.m * p.m8 * 4);
     p.p = room(s.B * p.m * p.m8 * 4);
+    const TileChoice& t = kTilesTwo[p.gram];
+    p.parts = room(p.splits > 1 ? s.B * upper_tiles(p.m, t.m) * p.splits * t.m * t.n * 4 : 0);
     p.bytes = at;
     return p;
 }

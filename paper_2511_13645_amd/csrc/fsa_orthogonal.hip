@@ -14,7 +14,8 @@ namespace {
 
 using namespace product;
 
-template <int EDGE> using OrthoTile = Tile<2, true, EDGE, EDGE, EDGE == 128 ? 32 : 64, 2, 2>;
+// The tiles that fsa_block.h chooses from, in its order.
+template <int CHOICE> using OrthoTile = Tile<2, true, kTilesTwo[CHOICE].m, kTilesTwo[CHOICE].n, CHOICE == 0 ? 64 : 32, 2, CHOICE == 0 ? 2 : 4>;
 template <int KIND> using ElemOf = typename std::conditional<KIND == 0, float, uint16_t>::type;
 template <int E> constexpr float kTwoTo = E > 0 ? (float)(1ull << (E > 0 ? E : 0)) : 1.0f / (float)(1ull << (E < 0 ? -E : 0));
 
@@ -54,8 +55,9 @@ template <int KIND> __global__ __launch_bounds__(256) void squares_kernel(OrthoA
         reinterpret_cast<double*>(a.ws + a.plan.squares)[blockIdx.y * kOrthoPeaks + blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
 __device__ __forceinline__ float inverse_norm(const OrthoArgs& a, unsigned batch) {
-    double sum = reinterpret_cast<const double*>(a.ws + a.plan.squares)[batch * kOrthoPeaks + (threadIdx.x & 63)];
-    static_assert(kOrthoPeaks == 64, "one a lane");
+    const double* parts = reinterpret_cast<const double*>(a.ws + a.plan.squares) + batch * kOrthoPeaks + 4 * (threadIdx.x & 63);
+    static_assert(kOrthoPeaks == 256, "four a lane");
+    double sum = (parts[0] + parts[1]) + (parts[2] + parts[3]);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
     const double norm = sqrt(sum) + (double)a.eps;
@@ -91,12 +93,20 @@ template <int KIND> __global__ __launch_bounds__(256) void first_kernel(OrthoArg
 struct StepArgs {
     const uint16_t *x, *sq, *poly;                      // planes of X, A, P; a matrix' planes are together
     uint16_t* to;
+    float* parts;                                       // of a gram matrix with splits: tiles on and above the diagonal
     void* out;                                          // of the last step, in the caller's type
     int64_t m, n, m8, n8;
     float a, b, c, scale;
-    unsigned mt, nt;
+    unsigned mt, nt, splits;
     bool tall, grid;
 };
+
+// Tiles on and above the diagonal of a square of them, row by row.
+__device__ __forceinline__ void upper_tile(unsigned t, unsigned mt, unsigned& mi, unsigned& ni) {
+    mi = 0;
+    while (t >= mt - mi) { t -= mt - mi; ++mi; }
+    ni = mi + t;
+}
 
 // W elements of two planes from `at` on.
 template <int W> __device__ __forceinline__ void load_planes(const uint16_t* p, int64_t plane, int64_t at, int64_t n, int64_t end, float (&x)[W]) {
@@ -115,11 +125,13 @@ template <int W> __device__ __forceinline__ void load_planes(const uint16_t* p, 
     }
 }
 
-enum { kGram, kPoly, kUpdate };
+enum { kGram, kGramParts, kPoly, kUpdate };
 template <class T, int WHAT, int KIND> __global__ __launch_bounds__(T::THREADS, T::waves(1)) void step_kernel(StepArgs a) {
     __shared__ __attribute__((aligned(256))) char lds[T::lds_bytes(1)];
     unsigned mi, ni;
-    tile_of(blockIdx.x, a.mt, a.nt, mi, ni);
+    if constexpr (WHAT == kGramParts) upper_tile(blockIdx.x, a.mt, mi, ni);
+    else tile_of(blockIdx.x, a.mt, a.nt, mi, ni);
+    constexpr bool GRAM = WHAT == kGram || WHAT == kGramParts;
     const int64_t m0 = (int64_t)mi * T::BM, n0 = (int64_t)ni * T::BN, batch = blockIdx.z;
     const int64_t wide = a.m * a.n8, square = a.m * a.m8;
     const uint16_t *x = a.x + batch * 2 * wide, *sq = a.sq + batch * 2 * square, *poly = a.poly + batch * 2 * square;
@@ -128,11 +140,13 @@ template <class T, int WHAT, int KIND> __global__ __launch_bounds__(T::THREADS, 
     using Stream = OneStream<T, true, WHAT != kUpdate, 1>;
     Stream stream;
     const Side b[1] = {WHAT == kPoly ? sa : sx};
-    const int64_t depth = WHAT == kGram ? a.n : a.m;
-    stream.flow.start(WHAT == kGram ? sx : WHAT == kPoly ? sa : sp, b, m0, a.m, n0, WHAT == kUpdate ? a.n8 : a.m, 0, depth);
+    const int64_t depth = GRAM ? a.n : a.m, steps = cut_into(depth, T::BK);
+    const int64_t first = WHAT == kGramParts ? steps * blockIdx.y / a.splits : 0, last = WHAT == kGramParts ? steps * (blockIdx.y + 1) / a.splits : steps;
+    stream.flow.start(GRAM ? sx : WHAT == kPoly ? sa : sp, b, m0, a.m, n0, WHAT == kUpdate ? a.n8 : a.m, first * T::BK,
+                      last * T::BK < depth ? last * T::BK : depth);
     Ring<T, T::stage_bytes(1), Stream> ring{lds, stream};
     ring.fill();
-    accumulate<T, true, WHAT != kUpdate, 1>(acc, ring, cut_into(depth, T::BK));
+    accumulate<T, true, WHAT != kUpdate, 1>(acc, ring, last - first);
     ring.end();
     if constexpr (WHAT == kUpdate) settle<T, 1>(acc);
     each_stretch<T>(m0, n0, [&](int i, int64_t m, int64_t n) {
@@ -141,7 +155,10 @@ template <class T, int WHAT, int KIND> __global__ __launch_bounds__(T::THREADS, 
         float v[W];
 #pragma unroll
         for (int j = 0; j < W; ++j) v[j] = acc[0][i][j / 4][j % 4];
-        if constexpr (WHAT == kGram) {
+        if constexpr (WHAT == kGramParts) {
+            float* part = a.parts + ((batch * a.splits + blockIdx.y) * gridDim.x + blockIdx.x) * T::BM * T::BN;
+            store_row<0>(part, (m - m0) * T::BN, n - n0, T::BN, true, v);
+        } else if constexpr (WHAT == kGram) {
 #pragma unroll
             for (int j = 0; j < W; ++j) v[j] *= kTwoTo<kUnitA - 2 * kUnitX>;
             store_planes<2, true>(a.to + batch * 2 * square, square, m * a.m8 + n, n, a.m, v);
@@ -175,13 +192,53 @@ template <class T, int WHAT, int KIND> __global__ __launch_bounds__(T::THREADS, 
     });
 }
 
-template <int WHAT, int KIND> hipError_t launch(StepArgs a, int64_t batch, int tile, hipStream_t st) {
-    a.mt = (unsigned)cut_into(a.m, tile);
-    a.nt = (unsigned)cut_into(WHAT == kUpdate ? a.n : a.m, tile);
-    const dim3 grid(a.mt * a.nt, 1, (unsigned)batch);
-    if (tile == 128) step_kernel<OrthoTile<128>, WHAT, KIND><<<grid, dim3(OrthoTile<128>::THREADS), 0, st>>>(a);
-    else step_kernel<OrthoTile<64>, WHAT, KIND><<<grid, dim3(OrthoTile<64>::THREADS), 0, st>>>(a);
+// 64 x 64 of the gram matrix from its parts, and of its other half what mirrors them.
+__global__ __launch_bounds__(256) void mirror_kernel(StepArgs a, unsigned tile, unsigned tiles) {
+    __shared__ float sum[64][65];
+    const unsigned blocks = tile / 64, t = blockIdx.x / (blocks * blocks), at = blockIdx.x % (blocks * blocks), batch = blockIdx.z;
+    unsigned mi, ni;
+    upper_tile(t, a.mt, mi, ni);
+    const int64_t m0 = (int64_t)mi * tile + at / blocks * 64, n0 = (int64_t)ni * tile + at % blocks * 64;
+    if (m0 >= a.m || n0 >= a.m) return;
+    const int64_t size = (int64_t)tile * tile;
+    const float* part = a.parts + (batch * a.splits * tiles + t) * size + (at / blocks * 64) * tile + at % blocks * 64;
+    for (int i = threadIdx.x; i < 64 * 16; i += 256) {
+        const int row = i / 16, col = i % 16 * 4;
+        f32x4 x = {};
+        if (m0 + row < a.m) {
+#pragma unroll 4
+            for (unsigned s = 0; s < a.splits; ++s) x += *reinterpret_cast<const f32x4*>(part + s * tiles * size + row * tile + col);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[row][col + j] = x[j] * kTwoTo<kUnitA - 2 * kUnitX>;
+    }
+    __syncthreads();
+    const int64_t square = a.m * a.m8;
+    uint16_t* to = a.to + batch * 2 * square;
+    for (int i = threadIdx.x; i < 64 * 8; i += 256) {
+        const int row = i / 8, col = i % 8 * 8;
+        float v[8], w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { v[j] = sum[row][col + j]; w[j] = sum[col + j][row]; }
+        if (m0 + row < a.m) store_planes<2, true>(to, square, (m0 + row) * a.m8 + n0 + col, n0 + col, a.m, v);
+        if (mi != ni && n0 + row < a.m) store_planes<2, true>(to, square, (n0 + row) * a.m8 + m0 + col, m0 + col, a.m, w);
+    }
+}
+
+template <int CHOICE, int WHAT, int KIND> hipError_t launch_tiles(StepArgs a, int64_t batch, hipStream_t st) {
+    using T = OrthoTile<CHOICE>;
+    a.mt = (unsigned)cut_into(a.m, T::BM);
+    a.nt = (unsigned)cut_into(WHAT == kUpdate ? a.n : a.m, T::BN);
+    const unsigned tiles = WHAT == kGramParts ? (unsigned)upper_tiles(a.m, T::BM) : a.mt * a.nt;
+    step_kernel<T, WHAT, KIND><<<dim3(tiles, WHAT == kGramParts ? a.splits : 1, (unsigned)batch), dim3(T::THREADS), 0, st>>>(a);
+    if (hipError_t e = hipGetLastError()) return e;
+    if constexpr (WHAT == kGramParts)
+        mirror_kernel<<<dim3(tiles * (T::BM / 64) * (T::BM / 64), 1, (unsigned)batch), dim3(256), 0, st>>>(a, T::BM, tiles);
     return hipGetLastError();
+}
+template <int WHAT, int KIND> hipError_t launch(const StepArgs& a, int64_t batch, int choice, hipStream_t st) {
+    return choice == 2 ? launch_tiles<2, WHAT, KIND>(a, batch, st)
+         : choice == 1 ? launch_tiles<1, WHAT, KIND>(a, batch, st) : launch_tiles<0, WHAT, KIND>(a, batch, st);
 }
 
 template <int KIND> hipError_t run(const OrthoArgs& a, hipStream_t st) {
@@ -196,18 +253,20 @@ template <int KIND> hipError_t run(const OrthoArgs& a, hipStream_t st) {
     s.sq = sq; s.poly = poly;
     s.m = p.m; s.n = p.n; s.m8 = p.m8; s.n8 = p.n8;
     s.scale = a.scale;
+    s.parts = reinterpret_cast<float*>(a.ws + p.parts);
+    s.splits = (unsigned)p.splits;
     s.tall = a.s.M > a.s.N;
     s.grid = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && p.n * (int64_t)sizeof(ElemOf<KIND>) % 16 == 0;
     for (int i = 0; i < a.steps; ++i) {
         s.a = a.coefficients[3 * i]; s.b = a.coefficients[3 * i + 1]; s.c = a.coefficients[3 * i + 2];
         s.x = x[i % 2];
         s.to = sq;
-        if (hipError_t e = launch<kGram, 0>(s, a.s.B, p.tile_square, st)) return e;
+        if (hipError_t e = s.splits > 1 ? launch<kGramParts, 0>(s, a.s.B, p.gram, st) : launch<kGram, 0>(s, a.s.B, p.gram, st)) return e;
         s.to = poly;
-        if (hipError_t e = launch<kPoly, 0>(s, a.s.B, p.tile_square, st)) return e;
+        if (hipError_t e = launch<kPoly, 0>(s, a.s.B, p.poly, st)) return e;
         s.to = x[(i + 1) % 2];
         s.out = i + 1 == a.steps ? a.out : nullptr;
-        if (hipError_t e = launch<kUpdate, KIND>(s, a.s.B, p.tile_wide, st)) return e;
+        if (hipError_t e = launch<kUpdate, KIND>(s, a.s.B, p.update, st)) return e;
     }
     return hipSuccess;
 }
