@@ -18,7 +18,7 @@ constexpr int64_t kChip = 256;                          // CUs
 // A row is held by `lanes` lanes, at most 16 elements to each, in one of two or three lengths.
 constexpr int kNormLanes[] = {4, 16, 64, 256, 1024};
 constexpr int64_t kNormDmax = 16384;
-constexpr int kNormParts = 512;                         // workgroups of the backward, one part of grad_weight each
+constexpr int kNormParts = 1024;                        // workgroups of the backward, one part of grad_weight each
 
 struct NormPlan {
     int lanes, pieces;                                  // 16-byte pieces a lane
@@ -35,10 +35,10 @@ inline NormPlan norm_plan(int64_t D, int elem) {
     p.rows = p.threads / p.lanes;
     return p;
 }
-// Workgroups of the backward: at least two turns of rows each, so that a part of grad_weight is worth its writing.
+// Workgroups of the backward: about four turns of rows each, so that a part of grad_weight is worth its writing.
 inline int64_t norm_parts(int64_t T, int64_t D, int elem) {
     const int64_t turns = cut_into(T, norm_plan(D, elem).rows);
-    const int64_t want = cut_into(turns, 2);
+    const int64_t want = cut_into(turns, 4);
     return want < 1 ? 1 : want < kNormParts ? want : kNormParts;
 }
 
@@ -178,6 +178,9 @@ inline int cut_pairs(int kind, int64_t T, int64_t H, int64_t depth, int pass) {
 inline bool gated_fine(const GatedShape& s) { return s.kind != 0 && 6.0 * (double)s.T * (double)s.H * (double)(2 * s.D + s.O) < 4e9; }
 inline int gated_planes(const GatedShape& s) { return s.kind == 0 ? 3 : gated_fine(s) ? 2 : 1; }
 
+// A forward of few rows is bound by its reading of the tables: waves read them straight into registers, h is fp32.
+inline bool gated_few(const GatedShape& s) { return s.T <= (s.kind == 0 ? 32 : 16); }
+
 // Whether a forward whose backward follows keeps g and u, in fp32, rather than that they are made again: 16 bytes of traffic
 // an element against 4 D operations (of six products each in fp32).
 inline bool gated_keep_pays(const GatedShape& s) { return s.D >= (s.kind == 0 ? 160 : 512); }
@@ -205,7 +208,7 @@ inline GatedPlan gated_plan(const GatedShape& s, bool backward, bool kept, int p
     if (packs & 2) p.gate = room(s.H * p.D8 * planes);
     if (packs & 4) p.up = room(s.H * p.D8 * planes);
     if (packs & 8) p.down = room(s.O * p.H8 * planes);
-    p.h = room(own);
+    p.h = room(!backward && gated_few(s) && own < s.T * s.H * 4 ? s.T * s.H * 4 : own);
     const int64_t sums = s.kind != 0 ? p.planes : 1;    // products that make one, of h's, dg's or du's planes
     ProductCut want{};
     if (!backward) {

@@ -408,6 +408,179 @@ __global__ __launch_bounds__(256) void zero_kernel(Elem* p, int64_t n) {
 }
 
 // ---------------------------------------------------------------------------------------------------------------
+// few rows
+// ---------------------------------------------------------------------------------------------------------------
+// Up to 16 rows, 32 in fp32, against tables that are read once: 16 rows of a table a workgroup, its waves a
+// share of the depth each, from memory to registers at whatever alignment they have; the shares meet in LDS.  h stays fp32.
+// 1 x 1024 -> 4096 -> 1024 bfloat16: 5.2 + 8.1 us, tables read at 3.2 and 1.0 TB/s; chains of a cold read, a meeting and, for the
+// second, h from other XCDs bound it (8 or 4 rows a workgroup, for more of them, change nothing).  17 rows and more are as quick with the
+// tiles above (18.5 and 18.9 us), fp32 from 33 on (45 and 70).
+struct FewArgs {
+    Matrix x, gate, up, down;
+    float *h, *gates;                                   // h [T,H]
+    void* y;
+    int64_t T, D, H, O;
+    int activation;
+};
+constexpr int kFewWaves = 4, kFewAnswerWaves = 16;
+constexpr int kHeld = NP == 1 ? 2 : 3;                  // planes of h
+
+// Eight elements of a row as planes, zeros behind its end and of rows that there are not.
+template <int PLANES> __device__ __forceinline__ void few_planes(const float (&e)[8], u32x4 (&out)[PLANES]) {
+    uint32_t w[4][PLANES];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) split2<PLANES, kHalf>(e[2 * j], e[2 * j + 1], w[j]);
+#pragma unroll
+    for (int q = 0; q < PLANES; ++q) out[q] = u32x4{w[0][q], w[1][q], w[2][q], w[3][q]};
+}
+// WHOLE: all of the 32 columns that a wave reads are there, and no branch keeps loads from being on their way together.
+template <bool WHOLE, class E> __device__ __forceinline__ void few_elements(const E* p, int64_t col, int64_t cols, E (&e)[8]) {
+    if constexpr (WHOLE) __builtin_memcpy(e, p + col, sizeof(e));
+    else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = col + j < cols ? p[col + j] : E(0);
+    }
+}
+template <class E> __device__ __forceinline__ void few_operand(const E (&e)[8], u32x4 (&out)[NP]) {
+    if constexpr (sizeof(E) == 4) few_planes<NP>(e, out);
+    else __builtin_memcpy(&out[0], e, 16);
+}
+// A row of a matrix; behind its end its last one, of which no result is kept.
+__device__ __forceinline__ const Elem* few_row(const Matrix& m, int64_t row) {
+    return static_cast<const Elem*>(m.p) + (row < m.rows ? row : m.rows - 1) * m.stride;
+}
+// Calls f(whole, how many steps, first column) for a wave's share of the steps of 32 columns: four at a time, whose loads are
+// all asked for before the first product (few rows leave room for few waves), then one by one.
+template <class F> __device__ __forceinline__ void few_steps(int64_t cols, int wave, int waves, F f) {
+    using One = std::integral_constant<int, 1>;
+    const int64_t steps = cut_into(cols, 32), last = steps * (wave + 1) / waves, full = last * 32 <= cols ? last : last - 1;
+    int64_t s = steps * wave / waves;
+#pragma unroll 1
+    for (; s + 4 <= full; s += 4) f(std::true_type{}, std::integral_constant<int, 4>{}, s * 32);
+#pragma unroll 1
+    for (; s < full; ++s) f(std::true_type{}, One{}, s * 32);
+    if (s < last) f(std::false_type{}, One{}, s * 32);
+}
+
+// Products of a wave's fragments: rows of a table are the result's rows, 4 * (lane / 16) ..., its columns the rows of x.
+template <int PA, int PB> __device__ __forceinline__ f32x4 few_product(const u32x4 (&table)[PA], const u32x4 (&rows)[PB], f32x4 acc) {
+#pragma unroll
+    for (int rank = (PA > PB ? PA : PB) - 1; rank >= 0; --rank)
+#pragma unroll
+        for (int p = 0; p < PA; ++p)
+            if (rank - p >= 0 && rank - p < PB) acc = mfma<kHalf>(table[p], rows[rank - p], acc);
+    return acc;
+}
+
+__device__ __forceinline__ float gate_value(int activation, float g) {
+    return activation == FSA_ACT_SILU ? gate_of<FSA_ACT_SILU>(g).value
+         : activation == FSA_ACT_GELU ? gate_of<FSA_ACT_GELU>(g).value : gate_of<FSA_ACT_RELU>(g).value;
+}
+
+template <int MT> __global__ __launch_bounds__(64 * kFewWaves) void few_hidden_kernel(FewArgs a) {
+    __shared__ f32x4 lds[2 * MT * (kFewWaves - 1) * 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, q = lane >> 4;
+    const int64_t row = (int64_t)blockIdx.x * 16 + r16;
+    const Elem *gates = few_row(a.gate, row), *ups = few_row(a.up, row), *xs[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) xs[t] = few_row(a.x, 16 * t + r16);
+    f32x4 g[MT] = {}, u[MT] = {};
+    few_steps(a.D, wave, kFewWaves, [&](auto whole, auto count, int64_t first) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        constexpr int N = decltype(count)::value;
+        Elem ge[N][8], ue[N][8], xe[N][MT][8];
+#pragma unroll
+        for (int s = 0; s < N; ++s) {
+            const int64_t col = first + 32 * s + 8 * q;
+            few_elements<WHOLE>(gates, col, a.D, ge[s]);
+            few_elements<WHOLE>(ups, col, a.D, ue[s]);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) few_elements<WHOLE>(xs[t], col, a.D, xe[s][t]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < N; ++s) {
+            u32x4 gate[NP], up[NP], x[NP];
+            few_operand(ge[s], gate);
+            few_operand(ue[s], up);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                few_operand(xe[s][t], x);
+                g[t] = few_product(gate, x, g[t]);
+                u[t] = few_product(up, x, u[t]);
+            }
+        }
+    });
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+        if (wave > 0) { lds[((wave - 1) * MT + t) * 128 + lane] = g[t]; lds[((wave - 1) * MT + t) * 128 + 64 + lane] = u[t]; }
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+#pragma unroll
+        for (int w = 0; w < kFewWaves - 1; ++w) { g[t] += lds[(w * MT + t) * 128 + lane]; u[t] += lds[(w * MT + t) * 128 + 64 + lane]; }
+        const int64_t m = 16 * t + r16;
+        if (m >= a.T) continue;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t n = (int64_t)blockIdx.x * 16 + 4 * q + j;
+            if (n >= a.H) continue;
+            if (a.gates) { a.gates[m * a.H + n] = g[t][j]; a.gates[(a.T + m) * a.H + n] = u[t][j]; }
+            a.h[m * a.H + n] = gate_value(a.activation, g[t][j]) * u[t][j];
+        }
+    }
+}
+
+template <int MT> __global__ __launch_bounds__(64 * kFewAnswerWaves) void few_answer_kernel(FewArgs a) {
+    __shared__ f32x4 lds[MT * kFewAnswerWaves * 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, q = lane >> 4;
+    const Elem* downs = few_row(a.down, (int64_t)blockIdx.x * 16 + r16);
+    const float* hs[MT];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) hs[t] = a.h + (16 * t + r16 < a.T ? 16 * t + r16 : a.T - 1) * a.H;
+    f32x4 acc[MT] = {};
+    few_steps(a.H, wave, kFewAnswerWaves, [&](auto whole, auto count, int64_t first) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        constexpr int N = decltype(count)::value;
+        Elem de[N][8];
+        float he[N][MT][8];
+#pragma unroll
+        for (int s = 0; s < N; ++s) {
+            const int64_t col = first + 32 * s + 8 * q;
+            few_elements<WHOLE>(downs, col, a.H, de[s]);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) few_elements<WHOLE>(hs[t], col, a.H, he[s][t]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int s = 0; s < N; ++s) {
+            u32x4 down[NP], h[kHeld];
+            few_operand(de[s], down);
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                few_planes<kHeld>(he[s][t], h);
+                acc[t] = few_product(down, h, acc[t]);
+            }
+        }
+    });
+#pragma unroll
+    for (int t = 0; t < MT; ++t) lds[(wave * MT + t) * 64 + lane] = acc[t];
+    __syncthreads();
+    // a sum a thread: 256 of each 16 rows
+    for (int i = threadIdx.x; i < MT * 256; i += 64 * kFewAnswerWaves) {
+        const int t = i >> 8, at = i >> 2 & 63, j = i & 3;
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kFewAnswerWaves; ++w) sum += lds[(w * MT + t) * 64 + at][j];
+        const int64_t m = 16 * t + (at & 15), n = (int64_t)blockIdx.x * 16 + 4 * (at >> 4) + j;
+        if (m >= a.T || n >= a.O) continue;
+        const float one[4] = {sum, 0.0f, 0.0f, 0.0f};
+        store_row<kKind>(a.y, m * a.O, n, n + 1, false, one);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
 // launches
 // ---------------------------------------------------------------------------------------------------------------
 bool on_grid(const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (int64_t)sizeof(Elem) % 16 == 0; }
@@ -530,7 +703,19 @@ void add_pairs(Job& j, int result, int& pairs, const GatedPlan& p, Side held, co
     }
 }
 
+template <int MT> hipError_t launch_few(const FewArgs& f, hipStream_t st) {
+    few_hidden_kernel<MT><<<dim3((unsigned)cut_into(f.H, 16)), dim3(64 * kFewWaves), 0, st>>>(f);
+    if (hipError_t e = hipGetLastError()) return e;
+    few_answer_kernel<MT><<<dim3((unsigned)cut_into(f.O, 16)), dim3(64 * kFewAnswerWaves), 0, st>>>(f);
+    return hipGetLastError();
+}
+
 hipError_t forward(const GatedArgs& a, hipStream_t st) {
+    if (gated_few(a.s)) {
+        const FewArgs f{a.x, a.gate, a.up, a.down, reinterpret_cast<float*>(a.ws + a.plan.h), a.gates, a.y, a.s.T, a.s.D, a.s.H, a.s.O, a.activation};
+        if constexpr (kKind == 0) if (a.s.T > 16) return launch_few<2>(f, st);
+        return launch_few<1>(f, st);
+    }
     Operands o{};
     if (hipError_t e = lay_out(a, o, false, st)) return e;
     const HiddenArgs h = hidden_args(a, o);

@@ -217,21 +217,38 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(Nor
     }
 }
 
-// grad_weight from the workgroups' parts: 16 columns a workgroup, 16 lanes to each.
-__global__ __launch_bounds__(256) void norm_join_kernel(const float* parts, int64_t count, int64_t D, void* out, int kind) {
-    __shared__ float lds[16][17];
-    const int col = threadIdx.x & 15, share = threadIdx.x >> 4;
-    const int64_t c = (int64_t)blockIdx.x * 16 + col;
-    float x = 0.0f;
-    if (c < D)
-        for (int64_t i = share; i < count; i += 16) x += parts[i * D + c];
-    lds[share][col] = x;
-    __syncthreads();
-    if (share != 0 || c >= D) return;
+// grad_weight from the workgroups' parts: 64 columns a workgroup, a wave's 16 lanes 4 of them each, the parts in 64 shares.
+__global__ __launch_bounds__(1024) void norm_join_kernel(const float* parts, int64_t count, int64_t D, void* out, int kind) {
+    __shared__ float lds[64][65];
+    const int col = (threadIdx.x & 15) * 4, share = threadIdx.x >> 4;
+    const int64_t c = (int64_t)blockIdx.x * 64 + col;
+    float x[4] = {};
+    if (c + 4 <= D) {
+#pragma unroll 4
+        for (int64_t i = share; i < count; i += 64) {
+            float p[4];
+            __builtin_memcpy(p, parts + i * D + c, 16);
 #pragma unroll
-    for (int i = 1; i < 16; ++i) x += lds[i][col];
-    if (kind == 0) static_cast<float*>(out)[c] = x;
-    else static_cast<uint16_t*>(out)[c] = (uint16_t)((kind == 1 ? product::pack2<false>(x, 0.0f) : product::pack2<true>(x, 0.0f)) & 0xffff);
+            for (int j = 0; j < 4; ++j) x[j] += p[j];
+        }
+    } else
+        for (int64_t i = share; i < count; i += 64)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (c + j < D) x[j] += parts[i * D + c + j];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lds[share][col + j] = x[j];
+    __syncthreads();
+    // 16 lanes to a column, 4 shares each
+    const int own = threadIdx.x >> 4, part = threadIdx.x & 15;
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += lds[part * 4 + i][own];
+#pragma unroll
+    for (int d = 1; d < 16; d *= 2) sum += __shfl_xor(sum, d, 64);
+    const int64_t at = (int64_t)blockIdx.x * 64 + own;
+    if (part != 0 || at >= D) return;
+    if (kind == 0) static_cast<float*>(out)[at] = sum;
+    else static_cast<uint16_t*>(out)[at] = (uint16_t)((kind == 1 ? product::pack2<false>(sum, 0.0f) : product::pack2<true>(sum, 0.0f)) & 0xffff);
 }
 
 template <int KIND, int LANES, int NV> hipError_t launch(const NormArgs& a, bool forward, hipStream_t st) {
@@ -245,7 +262,7 @@ template <int KIND, int LANES, int NV> hipError_t launch(const NormArgs& a, bool
     norm_bwd_kernel<KIND, LANES, NV><<<dim3((unsigned)parts), dim3(p.threads), 0, st>>>(a);
     if (hipError_t e = hipGetLastError()) return e;
     if (a.grad_weight)
-        norm_join_kernel<<<dim3((unsigned)cut_into(a.D, 16)), dim3(256), 0, st>>>(a.parts, parts, a.D, a.grad_weight, a.weight_kind);
+        norm_join_kernel<<<dim3((unsigned)cut_into(a.D, 64)), dim3(1024), 0, st>>>(a.parts, parts, a.D, a.grad_weight, a.weight_kind);
     return hipGetLastError();
 }
 template <int KIND, int LANES> hipError_t by_pieces(const NormArgs& a, bool forward, hipStream_t st) {

@@ -11,6 +11,7 @@
 #include <c10/core/impl/DeviceGuardImplInterface.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/accumulate_grad.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -117,6 +118,29 @@ void once(const char* what, bool again, torch::autograd::variable_list& out) {
     auto node = std::make_shared<torch::autograd::DelayedError>(std::string(what) + " is differentiable once", (int)out.size());
     out = (*node)(std::move(out));
 }
+// A backward that is captured into a graph while a leaf that its gradient goes to has an eager graph alive: autograd would have the
+// leaf's stream wait for the captured one, which ends the capture and the process.  Raises instead.
+void refuse_capture(const char* what) {
+    const auto node = torch::autograd::get_current_node();
+    if (!node) return;
+    const auto own = node->stream();
+    bool other = false;
+    for (const auto& e : node->next_edges())
+        if (e.function && dynamic_cast<torch::autograd::AccumulateGrad*>(e.function.get())) {
+            const auto theirs = e.function->stream();
+            other = other || (own && theirs && *own != *theirs);
+        }
+    if (!other) return;
+    const PyGILState_STATE gil = PyGILState_Ensure();
+    PyObject *torch_c = PyImport_ImportModule("torch._C"), *r = torch_c ? PyObject_CallMethod(torch_c, "_cuda_isCurrentStreamCapturing", nullptr) : nullptr;
+    const bool capturing = r == Py_True;
+    Py_XDECREF(r);
+    Py_XDECREF(torch_c);
+    PyErr_Clear();
+    PyGILState_Release(gil);
+    TORCH_CHECK(!capturing, "the backward of ", what, " cannot be captured while an eager graph of the same parameters is alive "
+                "(one made on another stream): drop it, or what holds it, first");
+}
 bool differentiated(const torch::autograd::variable_list& grads) {
     if (!c10::GradMode::is_enabled()) return false;
     for (const Tensor& g : grads) if (g.defined() && g.requires_grad()) return true;
@@ -177,6 +201,7 @@ struct Norm : torch::autograd::Function<Norm> {
         return {o[0]};
     }
     static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+        refuse_capture("a norm");
         const auto v = ctx->get_saved_variables();
         const Tensor &s = v[0], &weight = v[1];
         const bool again = differentiated(grads);
@@ -295,6 +320,7 @@ struct Gated : torch::autograd::Function<Gated> {
         return y;
     }
     static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
+        refuse_capture("a gated block");
         const auto v = ctx->get_saved_variables();
         const bool again = differentiated(grads);
         torch::autograd::variable_list out(6);

@@ -1,0 +1,56 @@
+"""An optimizer whose update of a matrix is its momentum, orthogonalised: every direction that the gradients of a matrix point in is
+followed at about the same rate, strong and weak ones alike.
+
+Matrices go through ``binding.fsa_orthogonalize`` (those of one size and type in one call); whatever is no matrix has to go
+to another optimizer.
+"""
+from __future__ import annotations
+
+from typing import Iterable
+
+import torch
+
+from . import binding
+
+
+class OrthogonalMomentum(torch.optim.Optimizer):
+    """m = momentum * m + grad;  p -= rate * (decay * p + sqrt(max(1, rows / columns)) * orthogonalised(m)), or, with `nesterov`, of
+    grad + momentum * m.  The momentum is fp32 whatever the matrix's type."""
+
+    def __init__(self, params: Iterable, rate: float = 0.02, momentum: float = 0.95, *, nesterov: bool = True, decay: float = 0.0,
+                 steps: int = 5, coefficients=binding.ORTHOGONAL_COEFFICIENTS, eps: float = 1e-7):
+        if rate < 0.0 or not 0.0 <= momentum < 1.0 or decay < 0.0:
+            raise ValueError("rate and decay must not be negative, momentum must be in [0, 1)")
+        super().__init__(params, dict(rate=rate, momentum=momentum, nesterov=nesterov, decay=decay, steps=steps,
+                                      coefficients=coefficients, eps=eps))
+        for group in self.param_groups:
+            for p in group["params"]:
+                if p.dim() != 2:
+                    raise ValueError("only matrices have an orthogonalised update, got %s" % (tuple(p.shape),))
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            alike = {}
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                state = self.state[p]
+                grad = p.grad.float()
+                if "momentum" not in state:
+                    state["momentum"] = torch.zeros_like(grad, memory_format=torch.contiguous_format)
+                m = state["momentum"].mul_(group["momentum"]).add_(grad)
+                alike.setdefault((tuple(p.shape), p.device), []).append((p, grad.add(m, alpha=group["momentum"]) if group["nesterov"] else m))
+            for (shape, _), members in alike.items():
+                update = members[0][1][None] if len(members) == 1 else torch.stack([u for _, u in members])
+                update = binding.fsa_orthogonalize(update, group["coefficients"], group["steps"], eps=group["eps"],
+                                                   scale=max(1.0, shape[0] / shape[1]) ** 0.5)
+                for (p, _), u in zip(members, update):
+                    if group["decay"]:
+                        p.mul_(1.0 - group["rate"] * group["decay"])
+                    p.add_(u.to(p.dtype), alpha=-group["rate"])
+        return loss
