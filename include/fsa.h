@@ -460,9 +460,9 @@ int fsa_norm_bwd(const void* grad_y, const void* grad_s, const void* s, int64_t 
  *   activation         an fsa_activation
  *   0 <= T <= FSA_GATED_TMAX; D, H, O from 1 to FSA_GATED_MOST
  *   out_y [T,O]        `dtype`
- *   out_gates          [2,T,H] fp32, g and u, for a backward; may be NULL
- * Backward, from grad_y [T,O] (rows grad_y_stride apart), the forward's inputs and its gates; with gates NULL g and u are made again
- * (fsa_gated_keep_pays: 1 where keeping them is quicker):
+ *   out_kept           fsa_gated_kept_bytes of device memory, 16-byte aligned, for a backward of the same sizes and type; may be NULL
+ * Backward, from grad_y [T,O] (rows grad_y_stride apart), the forward's inputs and what it kept; with kept NULL g and u are made
+ * again (fsa_gated_keep_pays: 1 where keeping them is quicker):
  *   dh = grad_y Wd, dg = dh u act'(g), du = dh act(g);  grad_x = dg Wg + du Wu,  grad_gate = dg^T x,  grad_up = du^T x,
  *   grad_down = grad_y^T (act(g) u).  Each in `dtype`, written whole (T == 0: the weights' are zero), and may be NULL.
  * act * u, dg and du are rounded to a 16-bit type once between the products, or in small calls to two of its numbers (fp16: act * u up to 65504; dg and du beside the power
@@ -474,13 +474,14 @@ enum { FSA_GATED_TMAX = 1 << 26, FSA_GATED_MOST = 1 << 16 };
 
 int64_t fsa_gated_fwd_workspace_bytes(int64_t T, int64_t D, int64_t H, int64_t O, int dtype);
 int64_t fsa_gated_bwd_workspace_bytes(int64_t T, int64_t D, int64_t H, int64_t O, int dtype);
+int64_t fsa_gated_kept_bytes(int64_t T, int64_t D, int64_t H, int64_t O, int dtype);
 int fsa_gated_keep_pays(int64_t T, int64_t D, int64_t H, int64_t O, int dtype);
 int fsa_gated_fwd(const void* x, int64_t x_stride, const void* w_gate, int64_t gate_stride, const void* w_up, int64_t up_stride,
                   const void* w_down, int64_t down_stride, int dtype, int activation, int64_t T, int64_t D, int64_t H, int64_t O,
-                  void* out_y, float* out_gates, void* workspace, int64_t workspace_bytes, void* stream);
+                  void* out_y, void* out_kept, void* workspace, int64_t workspace_bytes, void* stream);
 int fsa_gated_bwd(const void* grad_y, int64_t grad_y_stride, const void* x, int64_t x_stride,
                   const void* w_gate, int64_t gate_stride, const void* w_up, int64_t up_stride, const void* w_down, int64_t down_stride,
-                  int dtype, int activation, int64_t T, int64_t D, int64_t H, int64_t O, const float* gates,
+                  int dtype, int activation, int64_t T, int64_t D, int64_t H, int64_t O, const void* kept,
                   void* grad_x, void* grad_gate, void* grad_up, void* grad_down,
                   void* workspace, int64_t workspace_bytes, void* stream);
 

@@ -187,12 +187,12 @@ def fused_residual_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optiona
 class _GatedFeedForward(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w_gate, w_up, w_down, activation, keep):
-        gates = None
+        kept = None
         if keep and binding.fsa_gated_keep_pays(*x.shape, w_gate.shape[0], w_down.shape[0], x.dtype):
-            y, gates = binding.fsa_gated_fwd(x, w_gate, w_up, w_down, activation=activation, emit_gates=True)
+            y, kept = binding.fsa_gated_fwd(x, w_gate, w_up, w_down, activation=activation, emit_kept=True)
         else:
             y = binding.fsa_gated_fwd(x, w_gate, w_up, w_down, activation=activation)
-        ctx.save_for_backward(x, w_gate, w_up, w_down, gates)
+        ctx.save_for_backward(x, w_gate, w_up, w_down, kept)
         ctx.activation = activation
         return y
 

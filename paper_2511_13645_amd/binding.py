@@ -46,7 +46,7 @@ EXPORTS = ("fsa_sample_mean_fwd", "fsa_mean_replay_fwd", "fsa_mean_bwd", "fsa_me
            "fsa_xent_fwd", "fsa_xent_bwd", "fsa_distill_fwd", "fsa_distill_bwd",
            "fsa_norm_fwd", "fsa_norm_bwd", "fsa_norm_bwd_workspace_bytes",
            "fsa_gated_fwd", "fsa_gated_bwd", "fsa_gated_fwd_workspace_bytes", "fsa_gated_bwd_workspace_bytes",
-           "fsa_gated_keep_pays", "fsa_orthogonalize", "fsa_orthogonalize_workspace_bytes")
+           "fsa_gated_keep_pays", "fsa_gated_kept_bytes", "fsa_orthogonalize", "fsa_orthogonalize_workspace_bytes")
 
 _lib: Optional[ctypes.CDLL] = None
 _class_host = None                              # the module _fsa_class_host, likewise
@@ -58,7 +58,7 @@ _HOST_ENTRIES = ("fsa_sample_mean_fwd", "fsa_sample_wmean_fwd", "fsa_mean_replay
 _CLASS_HOST_ENTRIES = ("fsa_class_fwd_workspace_bytes", "fsa_class_bwd_workspace_bytes", "fsa_xent_fwd", "fsa_xent_bwd",
                        "fsa_distill_fwd", "fsa_distill_bwd")             # the same of _fsa_class_host
 _BLOCK_HOST_ENTRIES = ("fsa_norm_fwd", "fsa_norm_bwd", "fsa_norm_bwd_workspace_bytes", "fsa_gated_fwd", "fsa_gated_bwd",
-                       "fsa_gated_fwd_workspace_bytes", "fsa_gated_bwd_workspace_bytes", "fsa_gated_keep_pays")      # and of _fsa_block_host
+                       "fsa_gated_fwd_workspace_bytes", "fsa_gated_bwd_workspace_bytes", "fsa_gated_keep_pays", "fsa_gated_kept_bytes")      # and of _fsa_block_host
 _PLAIN, _WORKSPACE, _LOW_PRECISION, _WEIGHTED = range(4)                # backward entry points, as _fsa_host.bwd counts them
 
 
@@ -141,7 +141,7 @@ def lib() -> ctypes.CDLL:
         L.fsa_norm_bwd_workspace_bytes.restype = i64
         L.fsa_norm_bwd.argtypes = [vp, vp, vp, i64, vp, ci, ci, i64, i64, f32, vp, vp, vp, i64, vp]
         L.fsa_norm_bwd.restype = ci
-        for name in ("fsa_gated_fwd_workspace_bytes", "fsa_gated_bwd_workspace_bytes", "fsa_gated_keep_pays"):
+        for name in ("fsa_gated_fwd_workspace_bytes", "fsa_gated_bwd_workspace_bytes", "fsa_gated_keep_pays", "fsa_gated_kept_bytes"):
             getattr(L, name).argtypes = [i64, i64, i64, i64, ci]
             getattr(L, name).restype = ci if name == "fsa_gated_keep_pays" else i64
         L.fsa_gated_fwd.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, ci, ci, i64, i64, i64, i64, vp, vp, vp, i64, vp]
@@ -1045,12 +1045,12 @@ def _gated_operands(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w
 
 
 def fsa_gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *, activation: str = "silu",
-                  emit_gates: bool = False, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+                  emit_kept: bool = False, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Gated feed-forward block (act(x w_gate^T) * (x w_up^T)) w_down^T: x [T,D], w_gate and w_up [H,D], w_down [O,H], all of one
-    type; activation "silu", "gelu" (by the error function) or "relu".  Returns y [T,O], with `emit_gates` (y, gates): x w_gate^T and
-    x w_up^T [2,T,H] in fp32, which spare the backward making them again (fsa_gated_keep_pays).  `workspace`: see
+    type; activation "silu", "gelu" (by the error function) or "relu".  Returns y [T,O], with `emit_kept` (y, kept): bytes
+    that spare a backward of the same operands making the hidden products again (fsa_gated_keep_pays).  `workspace`: see
     fsa_gated_fwd_workspace_bytes; torch's memory without one.  `stream`: see fsa_xent_fwd."""
-    if _block_host is not None and stream is None and workspace is None and not emit_gates:
+    if _block_host is not None and stream is None and workspace is None and not emit_kept:
         r = _block_host.gated_fwd(x, w_gate, w_up, w_down, _ACTIVATIONS.get(activation))
         if _taken(r, "fsa_gated_fwd"):
             return r
@@ -1058,12 +1058,12 @@ def fsa_gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_d
     L = lib()
     with _on(x, stream):
         y = torch.empty((T, O), dtype=x.dtype, device=x.device)
-        gates = torch.empty((2, T, H), dtype=torch.float32, device=x.device) if emit_gates else None
+        kept = torch.empty((L.fsa_gated_kept_bytes(T, D, H, O, lead[8]),), dtype=torch.uint8, device=x.device) if emit_kept else None
         ws = _class_workspace(workspace, L.fsa_gated_fwd_workspace_bytes(T, D, H, O, lead[8]), x)
-        rc = L.fsa_gated_fwd(*lead, _ptr(y), _ptr(gates), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, x))
+        rc = L.fsa_gated_fwd(*lead, _ptr(y), _ptr(kept), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, x))
     if rc != FSA_OK:
         raise FsaError(rc, "fsa_gated_fwd")
-    return (y, gates) if emit_gates else y
+    return (y, kept) if emit_kept else y
 
 
 def gated(x, w_gate, w_up, w_down, activation: str):
@@ -1077,24 +1077,24 @@ def gated(x, w_gate, w_up, w_down, activation: str):
 
 
 def fsa_gated_bwd(grad_y: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
-                  gates: Optional[torch.Tensor] = None, *, activation: str = "silu", want: Sequence[bool] = (True, True, True, True),
+                  kept: Optional[torch.Tensor] = None, *, activation: str = "silu", want: Sequence[bool] = (True, True, True, True),
                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
-    """Gradients of fsa_gated_fwd by x, w_gate, w_up and w_down from grad_y [T,O]; None where not wanted.  `gates`: what the
+    """Gradients of fsa_gated_fwd by x, w_gate, w_up and w_down from grad_y [T,O]; None where not wanted.  `kept`: what the
     forward emitted, or None."""
     lead, (T, D, H, O) = _gated_operands(x, w_gate, w_up, w_down, activation)
     gs = _rows(grad_y, "grad_y")
     _same_type(x, "x", (grad_y, "grad_y"))
     _shape(grad_y, "grad_y", (T, O))
-    if gates is not None:
-        _need(gates, "gates", torch.float32)
-        _shape(gates, "gates", (2, T, H))
-    _same_device(x, (grad_y, "grad_y"), (gates, "gates"))
     L = lib()
+    if kept is not None:
+        _need(kept, "kept", torch.uint8)
+        _shape(kept, "kept", (L.fsa_gated_kept_bytes(T, D, H, O, lead[8]),))
+    _same_device(x, (grad_y, "grad_y"), (kept, "kept"))
     with _on(x, stream):
         grads = tuple(torch.empty(t.shape, dtype=x.dtype, device=x.device) if w else None
                       for t, w in zip((x, w_gate, w_up, w_down), want))
         ws = _class_workspace(workspace, L.fsa_gated_bwd_workspace_bytes(T, D, H, O, lead[8]), x)
-        rc = L.fsa_gated_bwd(_ptr(grad_y), gs, *lead, _ptr(gates), *(_ptr(g) for g in grads), _ptr(ws), ws.numel() * ws.element_size(),
+        rc = L.fsa_gated_bwd(_ptr(grad_y), gs, *lead, _ptr(kept), *(_ptr(g) for g in grads), _ptr(ws), ws.numel() * ws.element_size(),
                              _stream(stream, x))
     if rc != FSA_OK:
         raise FsaError(rc, "fsa_gated_bwd")
@@ -1102,7 +1102,7 @@ def fsa_gated_bwd(grad_y: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w
 
 
 def fsa_gated_keep_pays(T: int, D: int, H: int, O: int, dtype: torch.dtype) -> bool:
-    """Whether a forward whose backward follows had better emit its gates."""
+    """Whether a forward whose backward follows had better emit what that can be given."""
     return bool(lib().fsa_gated_keep_pays(T, D, H, O, _FLOAT_TYPE[dtype]))
 
 

@@ -181,9 +181,25 @@ inline int gated_planes(const GatedShape& s) { return s.kind == 0 ? 3 : gated_fi
 // A forward of few rows is bound by its reading of the tables: waves read them straight into registers, h is fp32.
 inline bool gated_few(const GatedShape& s) { return s.T <= (s.kind == 0 ? 32 : 16); }
 
-// Whether a forward whose backward follows keeps g and u, in fp32, rather than that they are made again: 16 bytes of traffic
-// an element against 4 D operations (of six products each in fp32).
+// Whether a forward whose backward follows keeps g, u and h rather than that they are made again: some 16 bytes of traffic an
+// element (28 in fp32) against 4 D operations (of six products each in fp32), in a kernel of its own tiles.
 inline bool gated_keep_pays(const GatedShape& s) { return s.D >= (s.kind == 0 ? 160 : 512); }
+
+// What it keeps, as byte offsets: rows of H8 elements.  g and u are fp32, or the upper 24 bits of it, rounded, beside 16-bit tables: the
+// upper 16 in one array, the next 8 in another.  Those are 2^-17 of an element, where what is made of it is rounded to 2^-9 or 2^-12.
+struct KeptPlan { size_t g, u, g_low, u_low, h, bytes; };
+inline KeptPlan kept_plan(const GatedShape& s) {
+    KeptPlan k{};
+    size_t at = 0;
+    const int64_t n = s.T * up_to(s.H, 8);
+    auto room = [&at](int64_t bytes) { const size_t a = at; at += (size_t)up_to(bytes, 256); return a; };
+    k.g = room(n * (s.kind == 0 ? 4 : 2));
+    k.u = room(n * (s.kind == 0 ? 4 : 2));
+    if (s.kind != 0) { k.g_low = room(n); k.u_low = room(n); }
+    k.h = room(n * 2 * gated_planes(s));
+    k.bytes = at;
+    return k;
+}
 
 // Byte offsets into the caller's workspace.
 struct GatedPlan {
@@ -242,7 +258,7 @@ struct GatedArgs {
     int activation;
     Matrix x, gate, up, down, grad_y;
     void *y, *grad_x, *grad_gate, *grad_up, *grad_down; // contiguous
-    float* gates;                                       // [2,T,H] g and u: forward: written if not null; backward: read
+    char* kept;                                         // forward: written if not null; backward: read
     GatedPlan plan;
     int packs;
     char* ws;

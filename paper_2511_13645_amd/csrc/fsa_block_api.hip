@@ -128,18 +128,22 @@ int fsa_gated_keep_pays(int64_t T, int64_t D, int64_t H, int64_t O, int dtype) {
     return known(dtype) && gated_sizes(T, D, H, O) && fsa::gated_keep_pays({T, D, H, O, dtype}) ? 1 : 0;
 }
 
+int64_t fsa_gated_kept_bytes(int64_t T, int64_t D, int64_t H, int64_t O, int dtype) {
+    return known(dtype) && gated_sizes(T, D, H, O) ? (int64_t)fsa::kept_plan({T, D, H, O, dtype}).bytes : 0;
+}
+
 int fsa_gated_fwd(const void* x, int64_t x_stride, const void* w_gate, int64_t gate_stride, const void* w_up, int64_t up_stride,
                   const void* w_down, int64_t down_stride, int dtype, int activation, int64_t T, int64_t D, int64_t H, int64_t O,
-                  void* out_y, float* out_gates, void* workspace, int64_t workspace_bytes, void* stream) {
+                  void* out_y, void* out_kept, void* workspace, int64_t workspace_bytes, void* stream) {
     fsa::GatedArgs a{};
     if (T > 0 && !out_y) return FSA_ERR_NULL;
     if (int rc = gated_take(a, x, x_stride, w_gate, gate_stride, w_up, up_stride, w_down, down_stride, dtype, activation, T, D, H, O)) return rc;
-    if (!aligned(out_y, elem_bytes(dtype)) || !aligned(out_gates, 4)) return FSA_ERR_ALIGN;
+    if (!aligned(out_y, elem_bytes(dtype)) || !aligned(out_kept, 16)) return FSA_ERR_ALIGN;
     if (T == 0) return FSA_OK;
     a.packs = packs_of(a, false);
     a.plan = fsa::gated_plan(a.s, false, false, a.packs);
     if (int rc = take_room(workspace, workspace_bytes, a.plan.bytes)) return rc;
-    a.y = out_y; a.gates = out_gates; a.ws = static_cast<char*>(workspace);
+    a.y = out_y; a.kept = static_cast<char*>(out_kept); a.ws = static_cast<char*>(workspace);
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(stream);
     return status_of(dtype == FSA_F32 ? fsa::gated_forward_f32(a, st) : dtype == FSA_BF16 ? fsa::gated_forward_bf16(a, st)
@@ -148,7 +152,7 @@ int fsa_gated_fwd(const void* x, int64_t x_stride, const void* w_gate, int64_t g
 
 int fsa_gated_bwd(const void* grad_y, int64_t grad_y_stride, const void* x, int64_t x_stride,
                   const void* w_gate, int64_t gate_stride, const void* w_up, int64_t up_stride, const void* w_down, int64_t down_stride,
-                  int dtype, int activation, int64_t T, int64_t D, int64_t H, int64_t O, const float* gates,
+                  int dtype, int activation, int64_t T, int64_t D, int64_t H, int64_t O, const void* kept,
                   void* grad_x, void* grad_gate, void* grad_up, void* grad_down,
                   void* workspace, int64_t workspace_bytes, void* stream) {
     fsa::GatedArgs a{};
@@ -157,14 +161,14 @@ int fsa_gated_bwd(const void* grad_y, int64_t grad_y_stride, const void* x, int6
     if (!in(grad_y_stride, O, kMostStride)) return FSA_ERR_ARG;
     const int eb = elem_bytes(dtype);
     if (!aligned(grad_y, eb) || !aligned(grad_x, eb) || !aligned(grad_gate, eb) || !aligned(grad_up, eb) || !aligned(grad_down, eb) ||
-        !aligned(gates, 4))
+        !aligned(kept, 16))
         return FSA_ERR_ALIGN;
     a.grad_y = {grad_y, grad_y_stride, T, O};
-    a.gates = const_cast<float*>(gates);                // (read)
+    a.kept = static_cast<char*>(const_cast<void*>(kept));                     // (read)
     a.grad_x = grad_x; a.grad_gate = grad_gate; a.grad_up = grad_up; a.grad_down = grad_down;
     if (T > 0) {
         a.packs = packs_of(a, true);
-        a.plan = fsa::gated_plan(a.s, true, gates != nullptr, a.packs);
+        a.plan = fsa::gated_plan(a.s, true, kept != nullptr, a.packs);
         if (int rc = take_room(workspace, workspace_bytes, a.plan.bytes)) return rc;
         a.ws = static_cast<char*>(workspace);
     }

@@ -3,9 +3,11 @@
 //   g = x Wg^T, u = x Wu^T, h = act(g) u, y = h Wd^T;   dh = gy Wd, dg = dh u act'(g), du = dh act(g)
 //   dx = dg Wg + du Wu,  dWd = gy^T h,  dWg = dg^T x,  dWu = du^T x
 //
-// g and u are made side by side (one x, two tables), so that a lane has both of an element and h is all that is written.  The
-// backward makes them again beside dh rather than read copies: g and u in 16 bits would be rounded once more on the way to every
-// gradient, in fp32 they would be 16 bytes of traffic an element, which takes as long as 2 D products from D of about 1000 on.
+// g and u are made side by side (one x, two tables), so that a lane has both of an element and h is all that has to be written.  The
+// backward makes them again beside dh, in a kernel of three sums, or reads them where the forward kept them: in 16 bits they would be
+// rounded once more on the way to every gradient, so they are kept in 24 bits beside 16-bit tables.  16384 x 1024 -> 4096 bfloat16: the
+// forward takes 340 us instead of 265 and the slopes 316 instead of 680 (fp32 copies), since three sums only leave room for tiles of
+// 128 x 128, of which the reads are as much as L2 gives.
 // h, dg and du are rounded to the type once: each gradient is then off by its own rounding and one of a factor, as in any product of
 // tensors of that type.  fp32 has three planes and loses nothing.
 // fp16: dg and du are kept times the power of two that brings the largest |gy| to [1, 2), which the products take back, so that
@@ -161,11 +163,65 @@ template <int ACT> __device__ __forceinline__ Gate gate_of(float g) {
 struct HiddenArgs {
     Side x, gate, up, down, grad_y;
     uint16_t *h, *dg, *du;                              // [T, H8] planes
-    float* gates;                                       // [2,T,H] or null
+    char* kept;                                         // or null
+    KeptPlan at;                                        // of it
     int64_t T, D, H, O, H8;
     const float* peaks;
     unsigned mt, nt;
 };
+
+// W elements of g or u as they are kept (see KeptPlan), at element `at`, column n of a row of H8.
+template <int W> __device__ __forceinline__ void store_kept(char* p, char* low, int64_t at, int64_t n, int64_t H8, const float (&x)[W]) {
+#pragma unroll
+    for (int i = 0; i < W; i += 8) {
+        if (n + i >= H8) return;
+        if constexpr (kKind == 0) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 4)
+                *reinterpret_cast<f32x4*>(p + (at + i + j) * 4) = f32x4{x[i + j], x[i + j + 1], x[i + j + 2], x[i + j + 3]};
+        } else {
+            uint32_t word[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {               // to nearest 24 bits; infinities and NaN have no bits below those
+                const uint32_t bits = __builtin_bit_cast(uint32_t, x[i + j]);
+                word[j] = (bits & 0x7f800000u) == 0x7f800000u ? bits | (bits & 0xff ? 0x100u : 0u) : bits + 0x80u;
+            }
+            u32x4 high;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) high[j] = word[2 * j] >> 16 | (word[2 * j + 1] & 0xffff0000u);
+            u32x2 rest;
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+                rest[j] = (word[4 * j] >> 8 & 0xff) | (word[4 * j + 1] & 0xff00) | (word[4 * j + 2] & 0xff00) << 8 | (word[4 * j + 3] & 0xff00) << 16;
+            *reinterpret_cast<u32x4*>(p + (at + i) * 2) = high;
+            *reinterpret_cast<u32x2*>(low + at + i) = rest;
+        }
+    }
+}
+template <int W> __device__ __forceinline__ void load_kept(const char* p, const char* low, int64_t at, int64_t n, int64_t H8, float (&x)[W]) {
+#pragma unroll
+    for (int i = 0; i < W; i += 8) {
+        if (n + i >= H8) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[i + j] = 0.0f;
+        } else if constexpr (kKind == 0) {
+#pragma unroll
+            for (int j = 0; j < 8; j += 4) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(p + (at + i + j) * 4);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[i + j + k] = v[k];
+            }
+        } else {
+            const u32x4 high = *reinterpret_cast<const u32x4*>(p + (at + i) * 2);
+            const u32x2 rest = *reinterpret_cast<const u32x2*>(low + at + i);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint32_t up = j % 2 ? high[j / 2] & 0xffff0000u : high[j / 2] << 16;
+                x[i + j] = __builtin_bit_cast(float, up | (rest[j / 4] >> (j % 4 * 8) & 0xff) << 8);
+            }
+        }
+    }
+}
 
 // PLANES of h, dg and du: one more than an operand has where the rounding's rest is kept.
 template <class T, int ACT, int PLANES> __global__ __launch_bounds__(T::THREADS, T::waves(2)) void hidden_kernel(HiddenArgs a) {
@@ -188,26 +244,14 @@ template <class T, int ACT, int PLANES> __global__ __launch_bounds__(T::THREADS,
         float g[W], u[W];
 #pragma unroll
         for (int j = 0; j < W; ++j) { g[j] = acc[0][i][j / 4][j % 4]; u[j] = acc[1][i][j / 4][j % 4]; }
-        if (a.gates) {
-            const bool grid = a.H % 4 == 0 && reinterpret_cast<uintptr_t>(a.gates) % 16 == 0;
-            store_row<0>(a.gates, m * a.H, n, a.H, grid, g);
-            store_row<0>(a.gates, (a.T + m) * a.H, n, a.H, grid, u);
+        if (a.kept) {
+            store_kept(a.kept + a.at.g, a.kept + a.at.g_low, m * a.H8 + n, n, a.H8, g);
+            store_kept(a.kept + a.at.u, a.kept + a.at.u_low, m * a.H8 + n, n, a.H8, u);
         }
 #pragma unroll
         for (int j = 0; j < W; ++j) g[j] = gate_of<ACT>(g[j]).value * u[j];
         store_planes<PLANES, T::HALF>(a.h, a.T * a.H8, m * a.H8 + n, n, a.H, g);
     });
-}
-
-template <int W> __device__ __forceinline__ void load_row(const float* p, int64_t n, int64_t N, float (&x)[W]) {
-#pragma unroll
-    for (int i = 0; i < W; i += 4) {
-        if (n + i + 4 <= N) __builtin_memcpy(x + i, p + n + i, 16);
-        else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[i + j] = n + i + j < N ? p[n + i + j] : 0.0f;
-        }
-    }
 }
 
 // What slopes without kept gates ask for: grad_y and w_down, then x and both tables.
@@ -266,8 +310,8 @@ template <class T, int ACT, int PLANES, bool KEPT> __global__ __launch_bounds__(
         constexpr int W = 4 * T::NJ;
         float g[W], u[W], dg[W], du[W];
         if constexpr (KEPT) {
-            load_row(a.gates + m * a.H, n, a.H, g);
-            load_row(a.gates + (a.T + m) * a.H, n, a.H, u);
+            load_kept(a.kept + a.at.g, a.kept + a.at.g_low, m * a.H8 + n, n, a.H8, g);
+            load_kept(a.kept + a.at.u, a.kept + a.at.u_low, m * a.H8 + n, n, a.H8, u);
         } else {
 #pragma unroll
             for (int j = 0; j < W; ++j) { g[j] = acc[0][i][j / 4][j % 4]; u[j] = acc[1][i][j / 4][j % 4]; }
@@ -280,7 +324,7 @@ template <class T, int ACT, int PLANES, bool KEPT> __global__ __launch_bounds__(
             dg[j] = d * u[j] * at.slope;
             du[j] = d * at.value;
         }
-        store_planes<PLANES, T::HALF>(a.h, a.T * a.H8, m * a.H8 + n, n, a.H, g);
+        if constexpr (!KEPT) store_planes<PLANES, T::HALF>(a.h, a.T * a.H8, m * a.H8 + n, n, a.H, g);
         store_planes<PLANES, T::HALF>(a.dg, a.T * a.H8, m * a.H8 + n, n, a.H, dg);
         store_planes<PLANES, T::HALF>(a.du, a.T * a.H8, m * a.H8 + n, n, a.H, du);
     });
@@ -417,7 +461,7 @@ __global__ __launch_bounds__(256) void zero_kernel(Elem* p, int64_t n) {
 // tiles above (18.5 and 18.9 us), fp32 from 33 on (45 and 70).
 struct FewArgs {
     Matrix x, gate, up, down;
-    float *h, *gates;                                   // h [T,H]
+    float* h;                                           // [T,H]
     void* y;
     int64_t T, D, H, O;
     int activation;
@@ -526,7 +570,6 @@ template <int MT> __global__ __launch_bounds__(64 * kFewWaves) void few_hidden_k
         for (int j = 0; j < 4; ++j) {
             const int64_t n = (int64_t)blockIdx.x * 16 + 4 * q + j;
             if (n >= a.H) continue;
-            if (a.gates) { a.gates[m * a.H + n] = g[t][j]; a.gates[(a.T + m) * a.H + n] = u[t][j]; }
             a.h[m * a.H + n] = gate_value(a.activation, g[t][j]) * u[t][j];
         }
     }
@@ -628,12 +671,12 @@ template <int CHOICE, int ACT, int PLANES> hipError_t launch_pair(HiddenArgs a, 
     using Hidden = typename Tiles<CHOICE>::Hidden;
     using Slopes = typename Tiles<CHOICE>::Slopes;
     using Kept = typename Tiles<CHOICE>::Product;
-    const int bm = forward ? Hidden::BM : a.gates ? Kept::BM : Slopes::BM, bn = forward ? Hidden::BN : a.gates ? Kept::BN : Slopes::BN;
+    const int bm = forward ? Hidden::BM : a.kept ? Kept::BM : Slopes::BM, bn = forward ? Hidden::BN : a.kept ? Kept::BN : Slopes::BN;
     a.mt = (unsigned)cut_into(a.T, bm);
     a.nt = (unsigned)cut_into(a.H, bn);
     const dim3 grid(a.mt * a.nt);
     if (forward) hidden_kernel<Hidden, ACT, PLANES><<<grid, dim3(Hidden::THREADS), 0, st>>>(a);
-    else if (a.gates) slopes_kernel<Kept, ACT, PLANES, true><<<grid, dim3(Kept::THREADS), 0, st>>>(a);
+    else if (a.kept) slopes_kernel<Kept, ACT, PLANES, true><<<grid, dim3(Kept::THREADS), 0, st>>>(a);
     else slopes_kernel<Slopes, ACT, PLANES, false><<<grid, dim3(Slopes::THREADS), 0, st>>>(a);
     return hipGetLastError();
 }
@@ -684,10 +727,11 @@ hipError_t lay_out(const GatedArgs& a, Operands& o, bool peaks, hipStream_t st) 
 HiddenArgs hidden_args(const GatedArgs& a, const Operands& o) {
     HiddenArgs h{};
     h.x = o.x; h.gate = o.gate; h.up = o.up; h.down = o.down; h.grad_y = o.grad_y;
-    h.h = reinterpret_cast<uint16_t*>(a.ws + a.plan.h);
+    h.at = kept_plan(a.s);
+    h.h = reinterpret_cast<uint16_t*>(a.kept ? a.kept + h.at.h : a.ws + a.plan.h);
     h.dg = reinterpret_cast<uint16_t*>(a.ws + a.plan.dg);
     h.du = reinterpret_cast<uint16_t*>(a.ws + a.plan.du);
-    h.gates = a.gates;
+    h.kept = a.kept;
     h.T = a.s.T; h.D = a.s.D; h.H = a.s.H; h.O = a.s.O; h.H8 = a.plan.H8;
     h.peaks = reinterpret_cast<const float*>(a.ws + a.plan.peaks);
     return h;
@@ -711,8 +755,8 @@ template <int MT> hipError_t launch_few(const FewArgs& f, hipStream_t st) {
 }
 
 hipError_t forward(const GatedArgs& a, hipStream_t st) {
-    if (gated_few(a.s)) {
-        const FewArgs f{a.x, a.gate, a.up, a.down, reinterpret_cast<float*>(a.ws + a.plan.h), a.gates, a.y, a.s.T, a.s.D, a.s.H, a.s.O, a.activation};
+    if (gated_few(a.s) && !a.kept) {
+        const FewArgs f{a.x, a.gate, a.up, a.down, reinterpret_cast<float*>(a.ws + a.plan.h), a.y, a.s.T, a.s.D, a.s.H, a.s.O, a.activation};
         if constexpr (kKind == 0) if (a.s.T > 16) return launch_few<2>(f, st);
         return launch_few<1>(f, st);
     }

@@ -25,7 +25,7 @@ PyObject* raw_stream = nullptr;                            // device index -> cu
 
 // Addresses of the C ABI's entry points, set by bind(), with the types that fsa.h declares them with.
 #define FSA_HOST_ENTRIES(X) X(fsa_norm_fwd) X(fsa_norm_bwd) X(fsa_norm_bwd_workspace_bytes) X(fsa_gated_fwd) X(fsa_gated_bwd) \
-                            X(fsa_gated_fwd_workspace_bytes) X(fsa_gated_bwd_workspace_bytes) X(fsa_gated_keep_pays)
+                            X(fsa_gated_fwd_workspace_bytes) X(fsa_gated_bwd_workspace_bytes) X(fsa_gated_keep_pays) X(fsa_gated_kept_bytes)
 struct {
 #define FSA_HOST_MEMBER(name) decltype(&::name) name;
     FSA_HOST_ENTRIES(FSA_HOST_MEMBER)
@@ -299,22 +299,23 @@ bool gated_call(GatedCall& c, PyObject* const* a) {
     return here(c.t[0], &c.stream);
 }
 
-int gated_forward(const GatedCall& c, bool keep, Tensor& y, Tensor& gates) {
+int gated_forward(const GatedCall& c, bool keep, Tensor& y, Tensor& kept) {
     const auto like = at::TensorOptions().dtype(c.t[0].dtype()).device(c.t[0].device());
     y = at::empty({c.T, c.O}, like);
-    if (keep && abi.fsa_gated_keep_pays(c.T, c.D, c.H, c.O, c.code)) gates = at::empty({2, c.T, c.H}, like.dtype(at::kFloat));
+    if (keep && abi.fsa_gated_keep_pays(c.T, c.D, c.H, c.O, c.code))
+        kept = at::empty({abi.fsa_gated_kept_bytes(c.T, c.D, c.H, c.O, c.code)}, like.dtype(at::kByte));
     const int64_t need = abi.fsa_gated_fwd_workspace_bytes(c.T, c.D, c.H, c.O, c.code);
     const Tensor ws = at::empty({need}, like.dtype(at::kByte));            // (may go once the call is queued: same stream)
     return abi.fsa_gated_fwd(data(c.t[0]), c.stride[0], data(c.t[1]), c.stride[1], data(c.t[2]), c.stride[2], data(c.t[3]), c.stride[3],
-                             c.code, c.activation, c.T, c.D, c.H, c.O, data(y), data<float>(gates), data(ws), need, c.stream);
+                             c.code, c.activation, c.T, c.D, c.H, c.O, data(y), data(kept), data(ws), need, c.stream);
 }
 
 struct Gated : torch::autograd::Function<Gated> {
     static Tensor forward(torch::autograd::AutogradContext* ctx, const Tensor& x, const Tensor& gate, const Tensor& up, const Tensor& down,
                           const GatedCall& c, bool keep) {
-        Tensor y, gates;
-        if (const int rc = gated_forward(c, keep, y, gates)) throw Refused(rc);
-        ctx->save_for_backward({x, gate, up, down, gates});
+        Tensor y, kept;
+        if (const int rc = gated_forward(c, keep, y, kept)) throw Refused(rc);
+        ctx->save_for_backward({x, gate, up, down, kept});
         ctx->saved_data["activation"] = (int64_t)c.activation;
         ctx->saved_data["stream"] = (int64_t)reinterpret_cast<intptr_t>(c.stream);
         return y;
@@ -329,14 +330,14 @@ struct Gated : torch::autograd::Function<Gated> {
             GatedCall c;
             for (int i = 0; i < 4; ++i) c.t[i] = v[i];
             gated_sizes(c);
-            const Tensor g = grads[0].contiguous(), &gates = v[4];
+            const Tensor g = grads[0].contiguous(), &kept = v[4];
             const auto like = at::TensorOptions().dtype(g.dtype()).device(g.device());
             for (int i = 0; i < 4; ++i) if (ctx->needs_input_grad(i)) out[i] = at::empty(c.t[i].sizes(), like);
             const int64_t need = abi.fsa_gated_bwd_workspace_bytes(c.T, c.D, c.H, c.O, c.code);
             const Tensor ws = at::empty({need}, like.dtype(at::kByte));
             const int rc = abi.fsa_gated_bwd(data(g), rows_of(&g), data(c.t[0]), c.stride[0], data(c.t[1]), c.stride[1], data(c.t[2]), c.stride[2],
                                              data(c.t[3]), c.stride[3], c.code, (int)ctx->saved_data["activation"].toInt(), c.T, c.D, c.H, c.O,
-                                             data<float>(gates), data(out[0]), data(out[1]), data(out[2]), data(out[3]), data(ws), need,
+                                             data(kept), data(out[0]), data(out[1]), data(out[2]), data(out[3]), data(ws), need,
                                              reinterpret_cast<void*>((intptr_t)ctx->saved_data["stream"].toInt()));
             TORCH_CHECK(rc == FSA_OK, "the backward of a gated block was refused (status ", rc, ")");
         }
@@ -351,10 +352,10 @@ PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return or_none([&]() -> PyObject* {
         GatedCall c;
         if (!gated_call(c, a)) { if (PyErr_Occurred()) return nullptr; Py_RETURN_NONE; }
-        Tensor y, gates;
+        Tensor y, kept;
         const int rc = without_gil([&] {
             at::AutoGradMode off(false);
-            return gated_forward(c, false, y, gates);
+            return gated_forward(c, false, y, kept);
         });
         return rc != FSA_OK ? PyLong_FromLong(rc) : wrap(y);
     });

@@ -48,6 +48,8 @@ def gated(x, wg, wu, wd, gy, act, dtype):
     x, wg, wu, wd = (t.detach().double() for t in (x, wg, wu, wd))
     g, eg = product(x, wg)
     u, eu = product(x, wu)
+    if dtype != torch.float32:                               # what a forward keeps for its backward has 24 bits, 16 of them the number's
+        eg, eu = eg + 2.0 ** -17 * g.abs(), eu + 2.0 ** -17 * u.abs()
     a, slope, steep, bend = activation(act, g)
     # the functions themselves: exponential and reciprocal within 4 v of their value and (1 + |g|) v of the argument's
     # rounding; the error function within 4 v of one

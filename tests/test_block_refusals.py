@@ -76,7 +76,7 @@ def test_gated(fsa, which):
     for name in ("x", "g", "u", "d", "y" if which == "forward" else "gy"):
         assert call(fsa, **{name: None}) == NULL, name
         assert call(fsa, **{name: FAKE + 1}) == ALIGN, name
-    assert call(fsa, t=5) == DTYPE and call(fsa, k=FAKE + 2) == ALIGN
+    assert call(fsa, t=5) == DTYPE and call(fsa, k=FAKE + 4) == ALIGN
     for bad in (dict(act=-1), dict(act=3), dict(T=-1), dict(T=(1 << 26) + 1), dict(D=0), dict(H=0), dict(O=0), dict(D=65537, xs=65537, gs=65537, us=65537),
                 dict(H=65537, ds=65537), dict(xs=63), dict(gs=63), dict(us=0), dict(ds=127), dict(xs=1 << 32)):
         assert call(fsa, **bad) == ARG, bad

@@ -22,9 +22,9 @@ def _check(x, wg, wu, wd, gy, act, dtype):
     want = bb.gated(x, wg, wu, wd, gy, act, dtype)
     y = fsa.fsa_gated_fwd(x, wg, wu, wd, activation=act)
     bb.check("y", y, *want["y"])
-    kept, gates = fsa.fsa_gated_fwd(x, wg, wu, wd, activation=act, emit_gates=True)
-    assert torch.equal(kept, y)
-    for given in (None, gates):
+    again, kept = fsa.fsa_gated_fwd(x, wg, wu, wd, activation=act, emit_kept=True)
+    bb.check("y beside what is kept", again, *want["y"])
+    for given in (None, kept):
         got = fsa.fsa_gated_bwd(gy, x, wg, wu, wd, given, activation=act)
         for name, g in zip(("grad_x", "grad_gate", "grad_up", "grad_down"), got):
             bb.check(name, g, *want[name])
