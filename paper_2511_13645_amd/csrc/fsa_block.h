@@ -71,15 +71,16 @@ constexpr int kGatedPeaks = 256;                        // workgroups that look 
 
 
 // Tiles that a product may be cut into, with the rate that each reached (TFLOP/s of 16-bit products, 8192 x 4096 x 4096).
-struct TileChoice { int m, n; double rate; };
+// `alone`: ns a step of 1 of the depth takes a workgroup that no other keeps company, by its chain of requests, reads and products.
+struct TileChoice { int m, n; double rate, alone; };
 constexpr int kTileKinds = 3;
-constexpr TileChoice kTilesOne[kTileKinds] = {{64, 64, 700}, {128, 128, 980}, {256, 256, 1300}};
-constexpr TileChoice kTilesThree[kTileKinds] = {{64, 64, 950}, {128, 64, 1150}, {256, 128, 1390}};
+constexpr TileChoice kTilesOne[kTileKinds] = {{64, 64, 700, 8}, {128, 128, 980, 10}, {256, 256, 1300, 26}};
+constexpr TileChoice kTilesThree[kTileKinds] = {{64, 64, 950, 22}, {128, 64, 1150, 28}, {256, 128, 1390, 72}};
 constexpr const TileChoice& product_tile(int kind, int choice) { return kind == 0 ? kTilesThree[choice] : kTilesOne[choice]; }
 // The same of the pairs of products of the hidden rows: columns of each.
-constexpr TileChoice kPairsOne[kTileKinds] = {{64, 64, 700}, {128, 64, 900}, {256, 128, 1250}};
-constexpr TileChoice kPairsThree[kTileKinds] = {{64, 64, 900}, {128, 64, 1100}, {256, 64, 1300}};
-constexpr TileChoice kSlopesOne[kTileKinds] = {{64, 64, 700}, {128, 64, 900}, {128, 128, 1000}};
+constexpr TileChoice kPairsOne[kTileKinds] = {{64, 64, 700, 10}, {128, 64, 900, 10}, {256, 128, 1250, 26}};
+constexpr TileChoice kPairsThree[kTileKinds] = {{64, 64, 900, 35}, {128, 64, 1100, 45}, {256, 64, 1300, 72}};
+constexpr TileChoice kSlopesOne[kTileKinds] = {{64, 64, 700, 10}, {128, 64, 900, 10}, {128, 128, 1000, 16}};
 constexpr const TileChoice& pair_tile(int kind, int choice, bool slopes) {
     return kind == 0 ? kPairsThree[choice] : slopes ? kSlopesOne[choice] : kPairsOne[choice];
 }
@@ -143,8 +144,8 @@ inline ProductCut cut_products(int kind, ProductCut want) {
         for (int way = 0; way < 5 + want.count; ++way) { // whole, shares of 1, 1/2, 1/3, 1/4 of a CU's work, one job's halves
             ProductCut c = want;
             c.choice = choice;
-            double share = way >= 1 && way < 5 ? work / (double)(kChip * way) : 1e30, bytes = 0.0, us[kMostJobs];
-            if (share < 256.0) share = 256.0;
+            double share = way >= 1 && way < 5 ? work / (double)(kChip * way) : 1e30, bytes = 0.0, us[kMostJobs], longest = 0.0;
+            if (share < 128.0) share = 128.0;
             int64_t groups[kMostJobs];
             for (int j = 0; j < c.count; ++j) {
                 ProductJob& job = c.job[j];
@@ -152,9 +153,12 @@ inline ProductCut cut_products(int kind, ProductCut want) {
                 job.splits = way - 5 == j ? 2 : n > 64.0 ? 64 : n < 1.0 ? 1 : (int64_t)n;
                 groups[j] = tiles[j] * job.splits;
                 us[j] = (double)job.K / (double)job.splits * depth_us + kTurn;
+                const double alone = (double)job.K / (double)job.splits * tile.alone * 1e-3 + kTurn;
+                longest = alone > longest ? alone : longest;
                 bytes += (double)job.parts_bytes();
             }
-            const double total = makespan(c.count, groups, us) + (bytes > 0.0 ? kJoin + bytes * 2.0 / 4e6 : 0.0);
+            const double span = makespan(c.count, groups, us);
+            const double total = (span > longest ? span : longest) + (bytes > 0.0 ? kJoin + bytes * 2.0 / 4e6 : 0.0);
             if (total < least) { least = total; best = c; }
         }
     }
@@ -167,7 +171,8 @@ inline int cut_pairs(int kind, int64_t T, int64_t H, int64_t depth, int pass) {
     for (int choice = 0; choice < kTileKinds; ++choice) {
         const TileChoice& tile = pass == kKeptPass ? product_tile(kind, choice) : pair_tile(kind, choice, pass == kSlopesPass);
         const double one = 2.0 * tile.m * tile.n * (double)depth * (kind == 0 ? 6.0 : 1.0) / (tile.rate / kChip) * 1e-6 + kTurn;
-        const double us = (double)cut_into(cut_into(T, tile.m) * cut_into(H, tile.n), kChip) * one;
+        double us = (double)cut_into(cut_into(T, tile.m) * cut_into(H, tile.n), kChip) * one;
+        if (const double alone = (double)depth * tile.alone * 1e-3 + kTurn; alone > us) us = alone;
         if (us < least) { least = us; best = choice; }
     }
     return best;
@@ -181,9 +186,11 @@ inline int gated_planes(const GatedShape& s) { return s.kind == 0 ? 3 : gated_fi
 // A forward of few rows is bound by its reading of the tables: waves read them straight into registers, h is fp32.
 inline bool gated_few(const GatedShape& s) { return s.T <= (s.kind == 0 ? 32 : 16); }
 
-// Whether a forward whose backward follows keeps g, u and h rather than that they are made again: some 16 bytes of traffic an
-// element (28 in fp32) against 4 D operations (of six products each in fp32), in a kernel of its own tiles.
-inline bool gated_keep_pays(const GatedShape& s) { return s.D >= (s.kind == 0 ? 160 : 512); }
+// Whether a forward whose backward follows keeps g, u and h rather than that they are made again: some 10 bytes of traffic an
+// element (16 in fp32) against 4 D operations (of six products each in fp32), in a kernel of its own tiles.  Forward and backward
+// of T x D -> 4 D -> D, made again and kept, us: bfloat16, T 32768: D 256 371 and 400, 384 625 and 619, 768 2004 and 1758; fp32:
+// D 64 174 and 186, 128 511 and 489, 192 and 2048 rows 124 and 111.
+inline bool gated_keep_pays(const GatedShape& s) { return s.D >= (s.kind == 0 ? 128 : 384); }
 
 // What it keeps, as byte offsets: rows of H8 elements.  g and u are fp32, or the upper 24 bits of it, rounded, beside 16-bit tables: the
 // upper 16 in one array, the next 8 in another.  Those are 2^-17 of an element, where what is made of it is rounded to 2^-9 or 2^-12.
@@ -277,7 +284,7 @@ struct OrthoShape {
     int64_t B, M, N;
     int kind;
 };
-constexpr TileChoice kTilesTwo[kTileKinds] = {{64, 64, 860}, {128, 128, 1150}, {256, 256, 1400}};
+constexpr TileChoice kTilesTwo[kTileKinds] = {{64, 64, 860, 10}, {128, 128, 1150, 22}, {256, 256, 1400, 72}};
 struct OrthoPlan {
     size_t squares, x[2], a, p, parts, bytes;
     int64_t m, n, m8, n8;
@@ -287,7 +294,9 @@ struct OrthoPlan {
 constexpr int64_t upper_tiles(int64_t m, int tile) { return cut_into(m, tile) * (cut_into(m, tile) + 1) / 2; }
 inline double ortho_us(int choice, int64_t tiles, int64_t depth) {
     const TileChoice& t = kTilesTwo[choice];
-    return (double)cut_into(tiles, kChip) * (2.0 * t.m * t.n * 3.0 * (double)depth / (t.rate / kChip) * 1e-6 + kTurn);
+    const double alone = (double)depth * t.alone * 1e-3 + kTurn;
+    const double us = (double)cut_into(tiles, kChip) * (2.0 * t.m * t.n * 3.0 * (double)depth / (t.rate / kChip) * 1e-6 + kTurn);
+    return us > alone ? us : alone;
 }
 inline OrthoPlan ortho_plan(const OrthoShape& s) {
     OrthoPlan p{};

@@ -160,6 +160,7 @@ template <int ACT> __device__ __forceinline__ Gate gate_of(float g) {
     }
 }
 
+__device__ __forceinline__ int at_most(int most, int64_t n) { return n < most ? (int)n : most; }
 struct HiddenArgs {
     Side x, gate, up, down, grad_y;
     uint16_t *h, *dg, *du;                              // [T, H8] planes
@@ -170,11 +171,11 @@ struct HiddenArgs {
     unsigned mt, nt;
 };
 
-// W elements of g or u as they are kept (see KeptPlan), at element `at`, column n of a row of H8.
-template <int W> __device__ __forceinline__ void store_kept(char* p, char* low, int64_t at, int64_t n, int64_t H8, const float (&x)[W]) {
+// W elements of g or u as they are kept (see KeptPlan), at element `at`; `left` of the row's H8 are there from it on.
+template <int W> __device__ __forceinline__ void store_kept(char* p, char* low, int64_t at, int left, const float (&x)[W]) {
 #pragma unroll
     for (int i = 0; i < W; i += 8) {
-        if (n + i >= H8) return;
+        if (i >= left) return;
         if constexpr (kKind == 0) {
 #pragma unroll
             for (int j = 0; j < 8; j += 4)
@@ -182,46 +183,48 @@ template <int W> __device__ __forceinline__ void store_kept(char* p, char* low, 
         } else {
             uint32_t word[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {               // to nearest 24 bits; infinities and NaN have no bits below those
-                const uint32_t bits = __builtin_bit_cast(uint32_t, x[i + j]);
-                word[j] = (bits & 0x7f800000u) == 0x7f800000u ? bits | (bits & 0xff ? 0x100u : 0u) : bits + 0x80u;
-            }
+            for (int j = 0; j < 8; ++j)                 // to nearest 24 bits, which leaves infinities as they are
+                word[j] = x[i + j] != x[i + j] ? 0x7fc00000u : __builtin_bit_cast(uint32_t, x[i + j]) + 0x80u;
             u32x4 high;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) high[j] = word[2 * j] >> 16 | (word[2 * j + 1] & 0xffff0000u);
+            for (int j = 0; j < 4; ++j) high[j] = __builtin_amdgcn_perm(word[2 * j + 1], word[2 * j], 0x07060302u);
             u32x2 rest;
 #pragma unroll
             for (int j = 0; j < 2; ++j)
-                rest[j] = (word[4 * j] >> 8 & 0xff) | (word[4 * j + 1] & 0xff00) | (word[4 * j + 2] & 0xff00) << 8 | (word[4 * j + 3] & 0xff00) << 16;
+                rest[j] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(word[4 * j + 3], word[4 * j + 2], 0x0c0c0501u),
+                                                __builtin_amdgcn_perm(word[4 * j + 1], word[4 * j], 0x0c0c0501u), 0x05040100u);
             *reinterpret_cast<u32x4*>(p + (at + i) * 2) = high;
             *reinterpret_cast<u32x2*>(low + at + i) = rest;
         }
     }
 }
-template <int W> __device__ __forceinline__ void load_kept(const char* p, const char* low, int64_t at, int64_t n, int64_t H8, float (&x)[W]) {
+// The same elements on their way back.
+template <int W> struct KeptRow {
+    static constexpr int PER = kKind == 0 ? 4 : 8;
+    u32x4 high[W / PER];
+    u32x2 rest[kKind == 0 ? 1 : W / 8];
+    __device__ __forceinline__ void ask(const char* p, const char* low, int64_t at, int left) {
 #pragma unroll
-    for (int i = 0; i < W; i += 8) {
-        if (n + i >= H8) {
+        for (int i = 0; i < W; i += PER) {
+            high[i / PER] = u32x4{};
+            if constexpr (kKind != 0) rest[i / 8] = u32x2{};
+            if (i >= left) continue;
+            high[i / PER] = *reinterpret_cast<const u32x4*>(p + (at + i) * (16 / PER));
+            if constexpr (kKind != 0) rest[i / 8] = *reinterpret_cast<const u32x2*>(low + at + i);
+        }
+    }
+    __device__ __forceinline__ void get(float (&x)[W]) const {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[i + j] = 0.0f;
-        } else if constexpr (kKind == 0) {
-#pragma unroll
-            for (int j = 0; j < 8; j += 4) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(p + (at + i + j) * 4);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) x[i + j + k] = v[k];
-            }
-        } else {
-            const u32x4 high = *reinterpret_cast<const u32x4*>(p + (at + i) * 2);
-            const u32x2 rest = *reinterpret_cast<const u32x2*>(low + at + i);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint32_t up = j % 2 ? high[j / 2] & 0xffff0000u : high[j / 2] << 16;
-                x[i + j] = __builtin_bit_cast(float, up | (rest[j / 4] >> (j % 4 * 8) & 0xff) << 8);
+        for (int i = 0; i < W; ++i) {
+            const uint32_t word = high[i / PER][i % PER * 4 / PER];     // (a vector's element itself is not what a bit cast takes)
+            if constexpr (kKind == 0) x[i] = __builtin_bit_cast(float, word);
+            else {
+                const uint32_t up = i % 2 ? word & 0xffff0000u : word << 16;
+                x[i] = __builtin_bit_cast(float, up | (rest[i / 8][i % 8 / 4] >> (i % 4 * 8) & 0xff) << 8);
             }
         }
     }
-}
+};
 
 // PLANES of h, dg and du: one more than an operand has where the rounding's rest is kept.
 template <class T, int ACT, int PLANES> __global__ __launch_bounds__(T::THREADS, T::waves(2)) void hidden_kernel(HiddenArgs a) {
@@ -245,8 +248,9 @@ template <class T, int ACT, int PLANES> __global__ __launch_bounds__(T::THREADS,
 #pragma unroll
         for (int j = 0; j < W; ++j) { g[j] = acc[0][i][j / 4][j % 4]; u[j] = acc[1][i][j / 4][j % 4]; }
         if (a.kept) {
-            store_kept(a.kept + a.at.g, a.kept + a.at.g_low, m * a.H8 + n, n, a.H8, g);
-            store_kept(a.kept + a.at.u, a.kept + a.at.u_low, m * a.H8 + n, n, a.H8, u);
+            const int left = at_most(W, a.H8 - n);
+            store_kept(a.kept + a.at.g, a.kept + a.at.g_low, m * a.H8 + n, left, g);
+            store_kept(a.kept + a.at.u, a.kept + a.at.u_low, m * a.H8 + n, left, u);
         }
 #pragma unroll
         for (int j = 0; j < W; ++j) g[j] = gate_of<ACT>(g[j]).value * u[j];
@@ -305,13 +309,20 @@ template <class T, int ACT, int PLANES, bool KEPT> __global__ __launch_bounds__(
     }
     settle<T, 1>(dh);
     const float lift = kHalf ? power_of_two(lift_of(a.peaks)) : 1.0f;
+    constexpr int W = 4 * T::NJ;
+    KeptRow<W> kept_g, kept_u;                          // asked for a row ahead, before the one before is written
+    auto ask_kept = [&](int64_t m, int64_t n) {
+        const int left = m < a.T ? at_most(W, a.H8 - n) : 0;
+        kept_g.ask(a.kept + a.at.g, a.kept + a.at.g_low, m * a.H8 + n, left);
+        kept_u.ask(a.kept + a.at.u, a.kept + a.at.u_low, m * a.H8 + n, left);
+    };
+    if constexpr (KEPT) each_stretch<T>(m0, n0, [&](int i, int64_t m, int64_t n) { if (i == 0) ask_kept(m, n); });
     each_stretch<T>(m0, n0, [&](int i, int64_t m, int64_t n) {
-        if (m >= a.T) return;
-        constexpr int W = 4 * T::NJ;
         float g[W], u[W], dg[W], du[W];
         if constexpr (KEPT) {
-            load_kept(a.kept + a.at.g, a.kept + a.at.g_low, m * a.H8 + n, n, a.H8, g);
-            load_kept(a.kept + a.at.u, a.kept + a.at.u_low, m * a.H8 + n, n, a.H8, u);
+            kept_g.get(g);
+            kept_u.get(u);
+            if (i + 1 < T::MI) ask_kept(m + 16, n);
         } else {
 #pragma unroll
             for (int j = 0; j < W; ++j) { g[j] = acc[0][i][j / 4][j % 4]; u[j] = acc[1][i][j / 4][j % 4]; }
@@ -324,6 +335,7 @@ template <class T, int ACT, int PLANES, bool KEPT> __global__ __launch_bounds__(
             dg[j] = d * u[j] * at.slope;
             du[j] = d * at.value;
         }
+        if (m >= a.T) return;
         if constexpr (!KEPT) store_planes<PLANES, T::HALF>(a.h, a.T * a.H8, m * a.H8 + n, n, a.H, g);
         store_planes<PLANES, T::HALF>(a.dg, a.T * a.H8, m * a.H8 + n, n, a.H, dg);
         store_planes<PLANES, T::HALF>(a.du, a.T * a.H8, m * a.H8 + n, n, a.H, du);

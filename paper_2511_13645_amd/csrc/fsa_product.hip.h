@@ -392,8 +392,11 @@ template <bool HALF> __device__ __forceinline__ float as_float(uint32_t bits) { 
 }
 
 // Planes of two elements, one word each.  Three bfloat16 planes: the first is cut off rather than rounded, so that the largest
-// fp32 numbers stay finite.  Two planes: nearest.  What is not finite has no rest.
+// fp32 numbers stay finite.  Two planes: nearest.  What is not finite has no rest.  The rest is that of the number that was rounded:
+// a product that the compiler rounds to fp16 at once in one place and by way of fp32 in another may differ by a step near a tie,
+// so planes are made of fp32 numbers that are there as such.
 template <int NP, bool HALF> __device__ __forceinline__ void split2(float a, float b, uint32_t (&out)[NP]) {
+    if constexpr (NP > 1) asm("" : "+v"(a), "+v"(b));
     if constexpr (NP == 1) out[0] = pack2<HALF>(a, b);
     else if constexpr (NP == 2) {
         out[0] = pack2<HALF>(a, b);
@@ -412,23 +415,27 @@ template <int NP, bool HALF> __device__ __forceinline__ void split2(float a, flo
 }
 
 // Writes W (a multiple of 8) elements as planes at column n of row m: those at `N` and behind are written as zero up to the next
-// multiple of 8, which is as far as a reader of the planes looks.
+// multiple of 8, which is as far as a reader of the planes looks (they need not be zero in x: infinity times a zero is not).
 template <int NP, bool HALF, int W>
 __device__ __forceinline__ void store_planes(uint16_t* p, int64_t plane, int64_t at, int64_t n, int64_t N, const float (&x)[W]) {
-    const int64_t end = (N + 7) / 8 * 8;
-    if (n >= end) return;
-    uint32_t w[W / 2][NP];
-#pragma unroll
-    for (int i = 0; i < W / 2; ++i)
-        split2<NP, HALF>(n + 2 * i < N ? x[2 * i] : 0.0f, n + 2 * i + 1 < N ? x[2 * i + 1] : 0.0f, w[i]);
     static_assert(W % 8 == 0, "whole chunks");
+    const int left = N - n < W ? (int)(N - n) : W;
+    if (left <= 0) return;                              // (n is a multiple of 8)
 #pragma unroll
-    for (int q = 0; q < NP; ++q)
+    for (int i = 0; i < W; i += 8) {
+        if (i >= left) break;
+        uint32_t w[4][NP];
 #pragma unroll
-        for (int i = 0; i < W / 2; i += 4) {
-            if (n + 2 * i >= end) break;
-            *reinterpret_cast<u32x4*>(p + q * plane + at + 2 * i) = u32x4{w[i][q], w[i + 1][q], w[i + 2][q], w[i + 3][q]};
+        for (int j = 0; j < 4; ++j) {
+            const int k = i + 2 * j;
+            split2<NP, HALF>(x[k], x[k + 1], w[j]);
+            const uint32_t there = k + 1 < left ? 0xffffffffu : k < left ? 0xffffu : 0u;
+#pragma unroll
+            for (int q = 0; q < NP; ++q) w[j][q] &= there;
         }
+#pragma unroll
+        for (int q = 0; q < NP; ++q) *reinterpret_cast<u32x4*>(p + q * plane + at + i) = u32x4{w[0][q], w[1][q], w[2][q], w[3][q]};
+    }
 }
 
 // Writes W elements of row `row` (its first element at p) from column n on, those before N, in the caller's type.
