@@ -115,6 +115,7 @@ struct Refused : std::exception { int status; explicit Refused(int s) : status(s
 // A second derivative raises, as with torch's once_differentiable.
 void once(const char* what, bool again, torch::autograd::variable_list& out) {
     if (!again) return;
+    for (Tensor& t : out) if (t.defined()) t.requires_grad_(true);         // a node is put behind none but these
     auto node = std::make_shared<torch::autograd::DelayedError>(std::string(what) + " is differentiable once", (int)out.size());
     out = (*node)(std::move(out));
 }
