@@ -35,7 +35,8 @@ inline NormPlan norm_plan(int64_t D, int elem) {
     p.rows = p.threads / p.lanes;
     return p;
 }
-// Workgroups of the backward: about four turns of rows each, so that a part of grad_weight is worth its writing.
+// Workgroups of the backward: about four turns of rows each, so that a part of grad_weight is worth its writing, and no more than the
+// chip holds at a time.
 inline int64_t norm_parts(int64_t T, int64_t D, int elem) {
     const int64_t turns = cut_into(T, norm_plan(D, elem).rows);
     const int64_t want = cut_into(turns, 4);
@@ -188,8 +189,8 @@ inline bool gated_few(const GatedShape& s) { return s.T <= (s.kind == 0 ? 32 : 1
 
 // Whether a forward whose backward follows keeps g, u and h rather than that they are made again: some 10 bytes of traffic an
 // element (16 in fp32) against 4 D operations (of six products each in fp32), in a kernel of its own tiles.  Forward and backward
-// of T x D -> 4 D -> D, made again and kept, us: bfloat16, T 32768: D 256 371 and 400, 384 625 and 619, 768 2004 and 1758; fp32:
-// D 64 174 and 186, 128 511 and 489, 192 and 2048 rows 124 and 111.
+// of T x D -> 4 D -> D, made again and kept, us: bfloat16, T 32768: D 256 323 and 331, 384 605 and 598, 768 2000 and 1724; fp32:
+// D 64 178 and 185, 128 444 and 415, 512 4329 and 3696.
 inline bool gated_keep_pays(const GatedShape& s) { return s.D >= (s.kind == 0 ? 128 : 384); }
 
 // What it keeps, as byte offsets: rows of H8 elements.  g and u are fp32, or the upper 24 bits of it, rounded, beside 16-bit tables: the

@@ -7,6 +7,11 @@
 // rstd again from the row that it reads anyway.  Sums over a row are fp32 and meet by shuffles (through LDS for rows of more than
 // 1024 elements); dw is summed by lane over the rows of a workgroup, written as one part a workgroup and joined in order
 // by a second launch, so that no order of atomics shows.
+//
+// 65536 x 1024 bfloat16 with a residual: forward 98 us (5.5 TB/s), backward 120 (4.5 TB/s) and 5 that join dw.  Rows held as numbers
+// from the first on took 108 and 129, 10007 x 602 fp16 24.7 rather than 19.0: all of a row's reads are asked for before the first
+// is unpacked.  The backward's 120 registers leave room for 16 waves a CU, which is what 1024 workgroups need; the next row read ahead
+// takes 152 and is no quicker (122), 768, 1280 and 1536 workgroups take 136, 182 and 162 where 1024 take 129: two rounds, or too few reads.
 #include "fsa_block_kernels.h"
 #include "fsa_product.hip.h"
 
@@ -20,43 +25,44 @@ template <int KIND> struct Row {
     static constexpr int PER = KIND == 0 ? 4 : 8;       // elements of a 16-byte piece
 };
 
-template <int KIND> __device__ __forceinline__ float number_of(typename Row<KIND>::Elem e) {
-    if constexpr (KIND == 0) return e;
-    else return product::as_float<KIND == 2>(e);
-}
-
-// A piece of a row from element c on, zeros behind D.
-template <int KIND> __device__ __forceinline__ void load(const void* base, int64_t at, int c, int D, float (&out)[Row<KIND>::PER]) {
+// A piece of a row from element c on, zeros behind D, as it lies in memory: half as many registers for 16-bit rows as numbers take.
+template <int KIND> struct Piece {
     using Elem = typename Row<KIND>::Elem;
-    constexpr int PER = Row<KIND>::PER;
-    const Elem* p = static_cast<const Elem*>(base) + at + c;
-    Elem e[PER];
-    if (c + PER <= D) __builtin_memcpy(e, p, 16);
-    else {
+    static constexpr int PER = Row<KIND>::PER;
+    product::u32x4 raw;
+    __device__ __forceinline__ void read(const void* base, int64_t at, int c, int D) {
+        const Elem* p = static_cast<const Elem*>(base) + at + c;
+        if (c + PER <= D) __builtin_memcpy(&raw, p, 16);
+        else {
+            Elem e[PER];
 #pragma unroll
-        for (int j = 0; j < PER; ++j) e[j] = c + j < D ? p[j] : Elem(0);
+            for (int j = 0; j < PER; ++j) e[j] = c + j < D ? p[j] : Elem(0);
+            __builtin_memcpy(&raw, e, 16);
+        }
     }
+    __device__ __forceinline__ void write(void* base, int64_t at, int c, int D) const {
+        Elem* p = static_cast<Elem*>(base) + at + c;
+        if (c + PER <= D) __builtin_memcpy(p, &raw, 16);
+        else {
+            Elem e[PER];
+            __builtin_memcpy(e, &raw, 16);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) out[j] = number_of<KIND>(e[j]);
-}
-template <int KIND> __device__ __forceinline__ void store(void* base, int64_t at, int c, int D, const float (&x)[Row<KIND>::PER]) {
-    using Elem = typename Row<KIND>::Elem;
-    constexpr int PER = Row<KIND>::PER;
-    Elem* p = static_cast<Elem*>(base) + at + c;
-    Elem e[PER];
-    if constexpr (KIND == 0) __builtin_memcpy(e, x, sizeof(e));
-    else {
-        uint32_t w[PER / 2];
-#pragma unroll
-        for (int j = 0; j < PER / 2; ++j) w[j] = product::pack2<KIND == 2>(x[2 * j], x[2 * j + 1]);
-        __builtin_memcpy(e, w, sizeof(e));
+            for (int j = 0; j < PER; ++j) if (c + j < D) p[j] = e[j];
+        }
     }
-    if (c + PER <= D) __builtin_memcpy(p, e, 16);
-    else {
-#pragma unroll
-        for (int j = 0; j < PER; ++j) if (c + j < D) p[j] = e[j];
+    __device__ __forceinline__ float get(int j) const {
+        const uint32_t word = raw[j * 4 / PER];
+        if constexpr (KIND == 0) return __builtin_bit_cast(float, word);
+        else return product::as_float<KIND == 2>(j % 2 ? word >> 16 : word & 0xffff);
     }
-}
+    __device__ __forceinline__ void set(const float (&x)[PER]) {       // rounded to the type
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (KIND == 0) raw[i] = __builtin_bit_cast(uint32_t, x[i]);
+            else raw[i] = product::pack2<KIND == 2>(x[2 * i], x[2 * i + 1]);
+        }
+    }
+};
 __device__ __forceinline__ float weight_at(const void* w, int kind, int c, int D) {
     if (c >= D) return 0.0f;
     if (kind == 0) return static_cast<const float*>(w)[c];
@@ -95,42 +101,39 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(Nor
     for (int64_t t0 = (int64_t)blockIdx.x * ROWS; t0 < a.T; t0 += (int64_t)gridDim.x * ROWS) {
         const int64_t t = t0 + threadIdx.x / LANES;
         const bool live = t < a.T;
-        float x[NV][PER];
+        Piece<KIND> s[NV], r[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int c = (v * LANES + lane) * PER;
+            s[v].raw = r[v].raw = product::u32x4{};
+            if (!live || c >= D) continue;
+            s[v].read(a.x, t * a.x_stride, c, D);
+            if (a.residual) r[v].read(a.residual, t * a.residual_stride, c, D);
+        }
         float sum = 0.0f;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * LANES + lane) * PER;
+            if (a.residual) {
+                float x[PER];
 #pragma unroll
-            for (int j = 0; j < PER; ++j) x[v][j] = 0.0f;
-            if (live && c < D) {
-                load<KIND>(a.x, t * a.x_stride, c, D, x[v]);
-                if (a.residual) {
-                    float r[PER];
-                    load<KIND>(a.residual, t * a.residual_stride, c, D, r);
-#pragma unroll
-                    for (int j = 0; j < PER; ++j) x[v][j] += r[j];
-                    if constexpr (KIND != 0) {
-#pragma unroll
-                        for (int j = 0; j < PER; j += 2) {
-                            const uint32_t both = product::pack2<KIND == 2>(x[v][j], x[v][j + 1]);
-                            x[v][j] = product::as_float<KIND == 2>(both & 0xffff);
-                            x[v][j + 1] = product::as_float<KIND == 2>(both >> 16);
-                        }
-                    }
-                    store<KIND>(a.s, t * a.D, c, D, x[v]);
-                }
+                for (int j = 0; j < PER; ++j) x[j] = s[v].get(j) + r[v].get(j);
+                s[v].set(x);
+                if (live && c < D) s[v].write(a.s, t * a.D, c, D);
             }
 #pragma unroll
-            for (int j = 0; j < PER; ++j) sum = fmaf(x[v][j], x[v][j], sum);
+            for (int j = 0; j < PER; ++j) sum = fmaf(s[v].get(j), s[v].get(j), sum);
         }
         const float rstd = 1.0f / sqrtf(row_sum<LANES>(sum, lds) / (float)D + a.eps);
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * LANES + lane) * PER;
             if (!live || c >= D) continue;
+            float x[PER];
 #pragma unroll
-            for (int j = 0; j < PER; ++j) x[v][j] = x[v][j] * rstd * w[v][j];
-            store<KIND>(a.y, t * a.D, c, D, x[v]);
+            for (int j = 0; j < PER; ++j) x[j] = s[v].get(j) * rstd * w[v][j];
+            s[v].set(x);
+            s[v].write(a.y, t * a.D, c, D);
         }
     }
 }
@@ -151,38 +154,41 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(Nor
         }
     for (int64_t t0 = (int64_t)blockIdx.x * ROWS; t0 < a.T; t0 += (int64_t)gridDim.x * ROWS) {
         const int64_t t = t0 + threadIdx.x / LANES;
-        const bool live = t < a.T;
-        float s[NV][PER], g[NV][PER], gs[NV][PER];
-        float sum = 0.0f, dot = 0.0f;
+        struct { Piece<KIND> s[NV], g[NV], gs[NV]; } row;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * LANES + lane) * PER;
+            row.s[v].raw = row.g[v].raw = row.gs[v].raw = product::u32x4{};
+            if (t >= a.T || c >= D) continue;
+            row.s[v].read(a.x, t * a.x_stride, c, D);
+            if (a.grad_y) row.g[v].read(a.grad_y, t * a.D, c, D);
+            if (a.grad_s) row.gs[v].read(a.grad_s, t * a.D, c, D);
+        }
+        float sum = 0.0f, dot = 0.0f;
 #pragma unroll
-            for (int j = 0; j < PER; ++j) s[v][j] = g[v][j] = gs[v][j] = 0.0f;
-            if (live && c < D) {
-                load<KIND>(a.x, t * a.x_stride, c, D, s[v]);
-                if (a.grad_y) load<KIND>(a.grad_y, t * a.D, c, D, g[v]);
-                if (a.grad_s) load<KIND>(a.grad_s, t * a.D, c, D, gs[v]);
-            }
+        for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
-                sum = fmaf(s[v][j], s[v][j], sum);
-                dot = fmaf(g[v][j] * w[v][j], s[v][j], dot);
+                sum = fmaf(row.s[v].get(j), row.s[v].get(j), sum);
+                dot = fmaf(row.g[v].get(j) * w[v][j], row.s[v].get(j), dot);
             }
-        }
         const float rstd = 1.0f / sqrtf(row_sum<LANES>(sum, lds) / (float)D + a.eps);
         const float mean = row_sum<LANES>(dot, lds) * rstd / (float)D;         // of gy w s^
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * LANES + lane) * PER;
-            if (!live || c >= D) continue;
+            if (t >= a.T || c >= D) continue;
+            float x[PER];
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
-                const float unit = s[v][j] * rstd;
-                dw[v][j] = fmaf(g[v][j], unit, dw[v][j]);
-                s[v][j] = fmaf(rstd, fmaf(-unit, mean, g[v][j] * w[v][j]), gs[v][j]);
+                const float unit = row.s[v].get(j) * rstd;
+                dw[v][j] = fmaf(row.g[v].get(j), unit, dw[v][j]);
+                x[j] = fmaf(rstd, fmaf(-unit, mean, row.g[v].get(j) * w[v][j]), row.gs[v].get(j));
             }
-            if (a.y) store<KIND>(a.y, t * a.D, c, D, s[v]);
+            if (!a.y) continue;
+            Piece<KIND> out;
+            out.set(x);
+            out.write(a.y, t * a.D, c, D);
         }
     }
     if (!a.grad_weight) return;
