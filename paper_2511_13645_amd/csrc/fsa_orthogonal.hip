@@ -14,14 +14,28 @@ namespace {
 
 using namespace product;
 
-// The tiles that fsa_block.h chooses from, in its order.
-template <int CHOICE> using OrthoTile = Tile<2, true, kTilesTwo[CHOICE].m, kTilesTwo[CHOICE].n, CHOICE == 0 ? 64 : 32, 2, CHOICE == 0 ? 2 : 4>;
+// The tiles that fsa_block.h chooses from, in its order.  Steps of 64 of the depth where two stages of them fit: one 1024 x 1024 -> 4096
+// update takes 30 us rather than 37 with steps of 32, eight 600 x 2400 matrices 678 us rather than 745, though a CU then
+// holds one workgroup of 128 x 128 instead of two.  Four stages, two sets of fragments, depths begun at another place by each workgroup
+// and 8 waves to 64 x 64 changed nothing or cost (15.6 us of 1024 x 1024 x 1024: 13.2 to 16.2).
+template <int CHOICE> using OrthoTile = Tile<2, true, kTilesTwo[CHOICE].m, kTilesTwo[CHOICE].n, CHOICE <= 1 ? 64 : 32, 2, CHOICE == 0 ? 2 : 4>;
 template <int KIND> using ElemOf = typename std::conditional<KIND == 0, float, uint16_t>::type;
 template <int E> constexpr float kTwoTo = E > 0 ? (float)(1ull << (E > 0 ? E : 0)) : 1.0f / (float)(1ull << (E < 0 ? -E : 0));
 
 template <int KIND> __device__ __forceinline__ float number(ElemOf<KIND> e) {
     if constexpr (KIND == 0) return e;
     else return as_float<KIND == 2>(e);
+}
+
+// Elements c ... c + 3 of row r of a matrix, those that there are.
+template <int KIND> __device__ __forceinline__ void load_four(const ElemOf<KIND>* g, int64_t r, int64_t c, const OrthoArgs& a, ElemOf<KIND> (&e)[4]) {
+    if (r >= a.s.M) return;
+    const ElemOf<KIND>* p = g + r * a.stride + c;
+    if (c + 4 <= a.s.N) __builtin_memcpy(e, p, sizeof(e));
+    else {
+#pragma unroll
+        for (int j = 0; j < 3; ++j) if (c + j < a.s.N) e[j] = p[j];
+    }
 }
 
 // Squares of a matrix, summed in 64 bits: gradients of 1e-30 have norms too.
@@ -33,14 +47,9 @@ template <int KIND> __global__ __launch_bounds__(256) void squares_kernel(OrthoA
     const int64_t pieces = cut_into(a.s.N, 256), all = a.s.M * pieces, waves = (int64_t)gridDim.x * 4;
     const int lane = threadIdx.x & 63;
     for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < all; i += waves) {
-        const int64_t row = all <= 0x7fffffff ? (uint32_t)i / (uint32_t)pieces : i / pieces, c = (i - row * pieces) * 256 + lane * 4;
-        const ElemOf<KIND>* p = g + row * a.stride + c;
+        const int64_t row = all <= 0x7fffffff ? (uint32_t)i / (uint32_t)pieces : i / pieces;
         ElemOf<KIND> e[4] = {};
-        if (c + 4 <= a.s.N) __builtin_memcpy(e, p, sizeof(e));
-        else {
-#pragma unroll
-            for (int j = 0; j < 3; ++j) if (c + j < a.s.N) e[j] = p[j];
-        }
+        load_four<KIND>(g, row, (i - row * pieces) * 256 + lane * 4, a, e);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const double x = number<KIND>(e[j]);
@@ -68,14 +77,17 @@ __device__ __forceinline__ float inverse_norm(const OrthoArgs& a, unsigned batch
 template <int KIND> __global__ __launch_bounds__(256) void first_kernel(OrthoArgs a) {
     __shared__ float tile[64][65];
     const unsigned batch = blockIdx.z;
-    const float unit = inverse_norm(a, batch);
     const bool tall = a.s.M > a.s.N;
     const int64_t r0 = (int64_t)blockIdx.x * 64, c0 = (int64_t)blockIdx.y * 64;      // of the matrix as it is given
     const ElemOf<KIND>* g = static_cast<const ElemOf<KIND>*>(a.g) + batch * a.batch_stride;
-    for (int i = threadIdx.x; i < 64 * 64; i += 256) {
-        const int64_t r = r0 + i / 64, c = c0 + i % 64;
-        tile[i / 64][i % 64] = r < a.s.M && c < a.s.N ? number<KIND>(g[r * a.stride + c]) * unit * kTwoTo<kUnitX> : 0.0f;
-    }
+    ElemOf<KIND> e[4][4] = {};                          // 4 elements of each fourth of the rows, asked for before the norm is there
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load_four<KIND>(g, r0 + i * 16 + threadIdx.x / 16, c0 + threadIdx.x % 16 * 4, a, e[i]);
+    const float unit = inverse_norm(a, batch) * kTwoTo<kUnitX>;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) tile[i * 16 + threadIdx.x / 16][threadIdx.x % 16 * 4 + j] = number<KIND>(e[i][j]) * unit;
     __syncthreads();
     const int64_t m = a.plan.m, n = a.plan.n, n8 = a.plan.n8, plane = m * n8;
     uint16_t* x = reinterpret_cast<uint16_t*>(a.ws + a.plan.x[0]) + batch * 2 * plane;
