@@ -193,18 +193,23 @@ inline bool gated_few(const GatedShape& s) { return s.T <= (s.kind == 0 ? 32 : 1
 // D 64 178 and 185, 128 444 and 415, 512 4329 and 3696.
 inline bool gated_keep_pays(const GatedShape& s) { return s.D >= (s.kind == 0 ? 128 : 384); }
 
-// What it keeps, as byte offsets: rows of H8 elements.  g and u are fp32, or the upper 24 bits of it, rounded, beside 16-bit tables: the
-// upper 16 in one array, the next 8 in another.  Those are 2^-17 of an element, where what is made of it is rounded to 2^-9 or 2^-12.
+// What it keeps, as byte offsets.  h lies in rows of H8 elements, g and u in blocks of 16 x 32 (see kept_at), which is what a wave
+// writes or reads at a time.  g and u are fp32, or the upper 24 bits of it, rounded, beside 16-bit tables: the upper 16 in one
+// array, the next 8 in another.  Those are 2^-17 of an element, where what is made of it is rounded to 2^-9 or 2^-12.
 struct KeptPlan { size_t g, u, g_low, u_low, h, bytes; };
+constexpr int64_t kKeptRows = 16, kKeptCols = 32;
+constexpr int64_t kept_at(int64_t m, int64_t n, int64_t across) {           // element (m, n), `across` blocks side by side
+    return (m / kKeptRows * across + n / kKeptCols) * kKeptRows * kKeptCols + m % kKeptRows * kKeptCols + n % kKeptCols;
+}
 inline KeptPlan kept_plan(const GatedShape& s) {
     KeptPlan k{};
     size_t at = 0;
-    const int64_t n = s.T * up_to(s.H, 8);
+    const int64_t n = up_to(s.T, kKeptRows) * up_to(s.H, kKeptCols);
     auto room = [&at](int64_t bytes) { const size_t a = at; at += (size_t)up_to(bytes, 256); return a; };
     k.g = room(n * (s.kind == 0 ? 4 : 2));
     k.u = room(n * (s.kind == 0 ? 4 : 2));
     if (s.kind != 0) { k.g_low = room(n); k.u_low = room(n); }
-    k.h = room(n * 2 * gated_planes(s));
+    k.h = room(s.T * up_to(s.H, 8) * 2 * gated_planes(s));
     k.bytes = at;
     return k;
 }
