@@ -465,9 +465,10 @@ int fsa_norm_bwd(const void* grad_y, const void* grad_s, const void* s, int64_t 
  * again (fsa_gated_keep_pays: 1 where keeping them is quicker):
  *   dh = grad_y Wd, dg = dh u act'(g), du = dh act(g);  grad_x = dg Wg + du Wu,  grad_gate = dg^T x,  grad_up = du^T x,
  *   grad_down = grad_y^T (act(g) u).  Each in `dtype`, written whole (T == 0: the weights' are zero), and may be NULL.
- * act * u, dg and du are rounded to a 16-bit type once between the products, or in small calls to two of its numbers (fp16: act * u up to 65504; dg and du beside the power
- * of two of the largest |grad_y|, up to 2^15 times that).  fp32 elements are taken whole; where an infinite one takes part,
- * results may be NaN that would be infinite.  relu'(0) = 0.
+ * act * u, dg and du are rounded to a 16-bit type once between the products, or in small calls to two of its numbers (fp16:
+ * act * u up to 65504; dg and du beside the power of two of the largest |grad_y|, up to 2^15 times that).  What is kept of g and u
+ * beside 16-bit tables is 24 bits each.  fp32 elements are taken whole; where an infinite one takes part, results may be NaN
+ * that would be infinite.  relu'(0) = 0.
  */
 typedef enum { FSA_ACT_SILU = 0, FSA_ACT_GELU = 1, FSA_ACT_RELU = 2 } fsa_activation;   /* gelu: x * normal distribution */
 enum { FSA_GATED_TMAX = 1 << 26, FSA_GATED_MOST = 1 << 16 };

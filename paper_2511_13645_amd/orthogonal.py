@@ -23,10 +23,21 @@ class OrthogonalMomentum(torch.optim.Optimizer):
             raise ValueError("rate and decay must not be negative, momentum must be in [0, 1)")
         super().__init__(params, dict(rate=rate, momentum=momentum, nesterov=nesterov, decay=decay, steps=steps,
                                       coefficients=coefficients, eps=eps))
-        for group in self.param_groups:
-            for p in group["params"]:
-                if p.dim() != 2:
-                    raise ValueError("only matrices have an orthogonalised update, got %s" % (tuple(p.shape),))
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        for p in self.param_groups[-1]["params"]:
+            if p.dim() != 2:
+                self.param_groups.pop()
+                raise ValueError("only matrices have an orthogonalised update, got %s" % (tuple(p.shape),))
+
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)
+        # torch brings what is loaded to the parameters' type: the momentum stays fp32
+        names = [i for group in state_dict["param_groups"] for i in group["params"]]
+        for i, p in zip(names, (p for group in self.param_groups for p in group["params"])):
+            if "momentum" in state_dict["state"].get(i, ()):
+                self.state[p]["momentum"] = state_dict["state"][i]["momentum"].detach().to(p.device, torch.float32, copy=True)
 
     @torch.no_grad()
     def step(self, closure=None):

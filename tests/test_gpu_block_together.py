@@ -205,6 +205,38 @@ def test_the_optimizer_follows_its_formula(dtype):
         OrthogonalMomentum([torch.nn.Parameter(n(5))])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_optimizer_goes_on_from_a_checkpoint(dtype):
+    from paper_2511_13645_amd.orthogonal import OrthogonalMomentum
+    n = lambda *s: torch.randn(s, generator=gen, device=DEV)
+    results = []
+    for restart in (False, True):
+        gen = torch.Generator(device=DEV).manual_seed(4)
+        params = [torch.nn.Parameter(n(*s).to(dtype)) for s in ((40, 24), (24, 40))]
+        opt = OrthogonalMomentum(params, 0.1)
+        for i in range(4):
+            if restart and i == 2:
+                saved, opt = opt.state_dict(), OrthogonalMomentum(params, 0.7)
+                opt.load_state_dict(saved)
+                assert all(v["momentum"].dtype == torch.float32 for v in opt.state.values()) and len(opt.state) == 2
+            for p in params:
+                p.grad = n(*p.shape).to(dtype)
+            opt.step()
+        results.append([p.detach().clone() for p in params])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
+def test_the_optimizer_takes_matrices_alone():
+    from paper_2511_13645_amd.orthogonal import OrthogonalMomentum
+    p, q = torch.nn.Parameter(torch.ones((3, 2), device=DEV)), torch.nn.Parameter(torch.ones(3, device=DEV))
+    opt = OrthogonalMomentum([p])
+    with pytest.raises(ValueError, match="only matrices"):
+        opt.add_param_group(dict(params=[q]))
+    assert len(opt.param_groups) == 1
+    p.grad = torch.ones_like(p)
+    opt.step()
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 def test_the_training_step_with_blocks_runs(dtype):
     r = subprocess.run([sys.executable, "-m", "paper_2511_13645_amd.entity_step", "--nodes", "3000", "--dim", "64", "--batch", "256",
