@@ -85,6 +85,7 @@ constexpr TileChoice kSlopesOne[kTileKinds] = {{64, 64, 700, 10}, {128, 64, 900,
 constexpr const TileChoice& pair_tile(int kind, int choice, bool slopes) {
     return kind == 0 ? kPairsThree[choice] : slopes ? kSlopesOne[choice] : kPairsOne[choice];
 }
+constexpr int64_t kMostGroups = (1 << 23) - 1;          // workgroups of up to 512: a launch has less than 2^32 threads
 constexpr double kTurn = 2.0;                           // us that a workgroup takes besides its products: first reads, writing out
 constexpr double kJoin = 4.0;                           // and a second launch
 
@@ -92,7 +93,8 @@ constexpr double kJoin = 4.0;                           // and a second launch
 constexpr int kMostJobs = 3;
 struct ProductJob {
     int64_t M, N, K, copies, splits;
-    int64_t parts_bytes() const { return splits > 1 ? copies * splits * M * up_to(N, 8) * 4 : 0; }
+    int64_t joined() const { return splits > 1 ? copies * M * up_to(N, 8) : 0; }        // elements that a second launch joins
+    int64_t parts_bytes() const { return joined() * splits * 4; }
 };
 struct ProductCut {
     int choice, count;
@@ -147,17 +149,20 @@ inline ProductCut cut_products(int kind, ProductCut want) {
             c.choice = choice;
             double share = way >= 1 && way < 5 ? work / (double)(kChip * way) : 1e30, bytes = 0.0, us[kMostJobs], longest = 0.0;
             if (share < 128.0) share = 128.0;
-            int64_t groups[kMostJobs];
+            int64_t groups[kMostJobs], all = 0, joined = 0;
             for (int j = 0; j < c.count; ++j) {
                 ProductJob& job = c.job[j];
                 const double n = (double)job.K / share + 0.5;
                 job.splits = way - 5 == j ? 2 : n > 64.0 ? 64 : n < 1.0 ? 1 : (int64_t)n;
                 groups[j] = tiles[j] * job.splits;
+                all += groups[j];
                 us[j] = (double)job.K / (double)job.splits * depth_us + kTurn;
                 const double alone = (double)job.K / (double)job.splits * tile.alone * 1e-3 + kTurn;
                 longest = alone > longest ? alone : longest;
+                joined += job.joined();
                 bytes += (double)job.parts_bytes();
             }
+            if ((all > kMostGroups || joined / 4 > kMostGroups * 256) && (way > 0 || choice + 1 < kTileKinds)) continue;
             const double span = makespan(c.count, groups, us);
             const double total = (span > longest ? span : longest) + (bytes > 0.0 ? kJoin + bytes * 2.0 / 4e6 : 0.0);
             if (total < least) { least = total; best = c; }
@@ -174,6 +179,7 @@ inline int cut_pairs(int kind, int64_t T, int64_t H, int64_t depth, int pass) {
         const double one = 2.0 * tile.m * tile.n * (double)depth * (kind == 0 ? 6.0 : 1.0) / (tile.rate / kChip) * 1e-6 + kTurn;
         double us = (double)cut_into(cut_into(T, tile.m) * cut_into(H, tile.n), kChip) * one;
         if (const double alone = (double)depth * tile.alone * 1e-3 + kTurn; alone > us) us = alone;
+        if (cut_into(T, tile.m) * cut_into(H, tile.n) > kMostGroups && choice + 1 < kTileKinds) continue;
         if (us < least) { least = us; best = choice; }
     }
     return best;
