@@ -71,8 +71,9 @@ constexpr int planes_of_kind(int kind) { return kind == 0 ? 3 : 1; }
 constexpr int kGatedPeaks = 256;                        // workgroups that look for the gradients' largest
 
 
-// Tiles that a product may be cut into, with the rate that each reached (TFLOP/s of 16-bit products, 8192 x 4096 x 4096).
-// `alone`: ns a step of 1 of the depth takes a workgroup that no other keeps company, by its chain of requests, reads and products.
+// Tiles that a product may be cut into, with the rate that each reached (TFLOP/s of 16-bit products, 8192 x 4096 x 4096).  `alone`: ns
+// that 1 of the depth takes a workgroup that no other keeps company, by its chain of requests, reads and products.  What is made
+// of them by estimate: the plan that cut_products, cut_pairs or ortho_plan thinks the quickest, all sizes alike.
 struct TileChoice { int m, n; double rate, alone; };
 constexpr int kTileKinds = 3;
 constexpr TileChoice kTilesOne[kTileKinds] = {{64, 64, 700, 8}, {128, 128, 980, 10}, {256, 256, 1300, 26}};
@@ -185,8 +186,9 @@ inline int cut_pairs(int kind, int64_t T, int64_t H, int64_t depth, int pass) {
     return best;
 }
 
-// Whether h, dg and du are held with what their rounding to 16 bits leaves, as a second plane: their products take twice as long, which
-// is less than the launches of a pass up to about this many operations (1024 x 128 -> 512 -> 128, bfloat16: 4 us of 90).
+// Whether h, dg and du are held with what their rounding to 16 bits leaves, as a second plane: results are off by their own rounding
+// alone, and their products take twice as long, which is less than the launches of a pass up to about this many operations
+// (1024 x 128 -> 512 -> 128, bfloat16: 4 us of 90).
 inline bool gated_fine(const GatedShape& s) { return s.kind != 0 && 6.0 * (double)s.T * (double)s.H * (double)(2 * s.D + s.O) < 4e9; }
 inline int gated_planes(const GatedShape& s) { return s.kind == 0 ? 3 : gated_fine(s) ? 2 : 1; }
 

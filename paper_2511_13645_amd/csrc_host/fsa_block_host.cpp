@@ -16,6 +16,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <optional>
 
 namespace {
 
@@ -190,15 +191,15 @@ int norm_forward(const NormCall& c, Tensor (&o)[2]) {
 // Its backward runs on the stream of its forward, which is the one that autograd then makes current.
 struct Norm : torch::autograd::Function<Norm> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext* ctx, const Tensor& x, const Tensor& weight,
-                                                  const Tensor& residual, const NormCall& c) {
+                                                  const std::optional<Tensor>& residual, const NormCall& c) {
         Tensor o[2];
         if (const int rc = norm_forward(c, o)) throw Refused(rc);
-        ctx->save_for_backward({residual.defined() ? o[1] : x, weight});
+        ctx->save_for_backward({residual ? o[1] : x, weight});
         ctx->set_materialize_grads(false);
         auto& d = ctx->saved_data;
         d["eps"] = (double)c.eps;
         d["stream"] = (int64_t)reinterpret_cast<intptr_t>(c.stream);
-        if (residual.defined()) return {o[0], o[1]};
+        if (residual) return {o[0], o[1]};
         return {o[0]};
     }
     static torch::autograd::variable_list backward(torch::autograd::AutogradContext* ctx, torch::autograd::variable_list grads) {
@@ -256,7 +257,8 @@ PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         Tensor o[2];
         const int rc = without_gil([&] {
             try {
-                const auto r = Norm::apply(c.x, c.weight, c.residual, c);
+                // (an argument that is an undefined tensor is none that torch's function takes)
+                const auto r = Norm::apply(c.x, c.weight, c.residual.defined() ? std::optional<Tensor>(c.residual) : std::nullopt, c);
                 o[0] = r[0];
                 if (r.size() > 1) o[1] = r[1];
                 return (int)FSA_OK;

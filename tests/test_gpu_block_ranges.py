@@ -125,10 +125,15 @@ def test_both_host_paths_give_the_same(dtype, monkeypatch):
     def run():
         y, s = fused_residual_norm(x, w, r)
         z = fused_gated_feed_forward(y, wg, wu, wd, activation="gelu")
-        q, _ = fused_residual_norm(z, w)
+        q, same = fused_residual_norm(z, w)
+        assert same is z
         return [y, s, z, q, *torch.autograd.grad((q, s), (x, r, w, wg, wu, wd), (g, g))]
 
     native = run()
+    # no call of these is left to the Python code
+    assert all(fsa._block_host.norm(x, w, residual, 1e-6) is not None for residual in (None, r))
+    assert all(fsa._block_host.norm_fwd(x, w, residual, 1e-6) is not None for residual in (None, r))
+    assert fsa._block_host.gated(x, wg, wu, wd, 1) is not None and fsa._block_host.gated_fwd(x, wg, wu, wd, 1) is not None
     monkeypatch.setattr(fsa, "_block_host", None)
     assert all(torch.equal(a, b) for a, b in zip(native, run()))
 
