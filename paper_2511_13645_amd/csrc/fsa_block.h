@@ -77,11 +77,11 @@ constexpr int kGatedPeaks = 256;                        // workgroups that look 
 struct TileChoice { int m, n; double rate, alone; };
 constexpr int kTileKinds = 3;
 constexpr TileChoice kTilesOne[kTileKinds] = {{64, 64, 700, 8}, {128, 128, 980, 10}, {256, 256, 1300, 26}};
-constexpr TileChoice kTilesThree[kTileKinds] = {{64, 64, 950, 22}, {128, 64, 1150, 28}, {256, 128, 1390, 72}};
+constexpr TileChoice kTilesThree[kTileKinds] = {{64, 64, 950, 16}, {128, 64, 1150, 22}, {256, 128, 1390, 72}};
 constexpr const TileChoice& product_tile(int kind, int choice) { return kind == 0 ? kTilesThree[choice] : kTilesOne[choice]; }
 // The same of the pairs of products of the hidden rows: columns of each.
 constexpr TileChoice kPairsOne[kTileKinds] = {{64, 64, 700, 10}, {128, 64, 900, 10}, {256, 128, 1250, 26}};
-constexpr TileChoice kPairsThree[kTileKinds] = {{64, 64, 900, 35}, {128, 64, 1100, 45}, {256, 64, 1300, 72}};
+constexpr TileChoice kPairsThree[kTileKinds] = {{64, 64, 900, 25}, {128, 64, 1100, 45}, {256, 64, 1300, 72}};
 constexpr TileChoice kSlopesOne[kTileKinds] = {{64, 64, 700, 10}, {128, 64, 900, 10}, {128, 128, 1000, 16}};
 constexpr const TileChoice& pair_tile(int kind, int choice, bool slopes) {
     return kind == 0 ? kPairsThree[choice] : slopes ? kSlopesOne[choice] : kPairsOne[choice];

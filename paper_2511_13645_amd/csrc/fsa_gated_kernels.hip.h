@@ -35,15 +35,17 @@ constexpr bool kHalf = kKind == 2;
 constexpr int BK = NP == 3 ? 32 : 64;
 using Elem = typename std::conditional<kKind == 0, float, uint16_t>::type;
 
-// The tiles that fsa_block.h chooses from, in its order.
+// The tiles that fsa_block.h chooses from, in its order.  fp32's small ones have 8 waves and steps of 64 of the depth where two of them
+// fit, since they mostly have a CU to themselves: 64 rows of 1024 -> 4096 in tiles of 64 x 64 x 2 take 25 us, with 4 waves
+// 28 and with steps of 32 as well 33; 256 x 4096 -> 1024 in tiles of 128 x 64 18.6 rather than 24.4.
 template <int CHOICE> struct Tiles;
 template <> struct Tiles<0> {
-    using Product = Tile<NP, kHalf, 64, 64, BK, 2, 2>;
+    using Product = Tile<NP, kHalf, 64, 64, 64, NP == 3 ? 4 : 2, 2>;
     using Hidden = Product;
     using Slopes = Product;
 };
 template <> struct Tiles<1> {
-    using Product = Tile<NP, kHalf, 128, NP == 1 ? 128 : 64, BK, NP == 1 ? 4 : 2, 2>;
+    using Product = Tile<NP, kHalf, 128, NP == 1 ? 128 : 64, 64, 4, 2>;
     using Hidden = Tile<NP, kHalf, 128, 64, BK, 2, 2>;
     using Slopes = Hidden;
 };
@@ -439,12 +441,12 @@ template <class T, bool FORWARD> __global__ __launch_bounds__(T::THREADS, T::wav
     else make_products<T, false, false>(acc, lds, p);
     const float back = kHalf && a.lifted && a.splits == 1 ? power_of_two(-lift_of(l.peaks)) : 1.0f;
     each_stretch<T>((int64_t)p.mi * T::BM, (int64_t)p.ni * T::BN, [&](int i, int64_t m, int64_t n) {
-        if (m >= a.M) return;
         float x[4 * T::NJ];
 #pragma unroll
         for (int j = 0; j < 4 * T::NJ; ++j) x[j] = kHalf ? acc[0][i][j / 4][j % 4] * back : acc[0][i][j / 4][j % 4];
-        if (a.splits > 1) store_row<0>(a.parts + (p.which * a.splits + p.split) * a.M * a.N8, m * a.N8, n, a.N8, true, x);
-        else store_row<kKind>(a.out[p.which], m * a.out_ld, n, a.N, a.grid, x);
+        if (a.splits > 1) store_numbers(a.parts + ((p.which * a.splits + p.split) * a.M + m) * a.N8, m < a.M, n, a.N8, true, x);
+        else if constexpr (kKind == 0) store_numbers(static_cast<float*>(a.out[p.which]) + m * a.out_ld, m < a.M, n, a.N, a.grid, x);
+        else if (m < a.M) store_row<kKind>(a.out[p.which], m * a.out_ld, n, a.N, a.grid, x);
     });
 }
 

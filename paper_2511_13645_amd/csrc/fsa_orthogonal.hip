@@ -162,15 +162,16 @@ template <class T, int WHAT, int KIND> __global__ __launch_bounds__(T::THREADS, 
     ring.end();
     if constexpr (WHAT == kUpdate) settle<T, 1>(acc);
     each_stretch<T>(m0, n0, [&](int i, int64_t m, int64_t n) {
-        if (m >= a.m) return;
         constexpr int W = 4 * T::NJ;
         float v[W];
 #pragma unroll
         for (int j = 0; j < W; ++j) v[j] = acc[0][i][j / 4][j % 4];
         if constexpr (WHAT == kGramParts) {
             float* part = a.parts + ((batch * a.splits + blockIdx.y) * gridDim.x + blockIdx.x) * T::BM * T::BN;
-            store_row<0>(part, (m - m0) * T::BN, n - n0, T::BN, true, v);
-        } else if constexpr (WHAT == kGram) {
+            return store_numbers(part + (m - m0) * T::BN, m < a.m, n - n0, T::BN, true, v);
+        }
+        if (m >= a.m) return;
+        if constexpr (WHAT == kGram) {
 #pragma unroll
             for (int j = 0; j < W; ++j) v[j] *= kTwoTo<kUnitA - 2 * kUnitX>;
             store_planes<2, true>(a.to + batch * 2 * square, square, m * a.m8 + n, n, a.m, v);
