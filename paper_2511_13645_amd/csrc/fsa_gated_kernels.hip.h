@@ -480,7 +480,7 @@ __global__ __launch_bounds__(256) void zero_kernel(Elem* p, int64_t n) {
 // share of the depth each, from memory to registers at whatever alignment they have; the shares meet in LDS.  h stays fp32.
 // 1 x 1024 -> 4096 -> 1024 bfloat16: 5.2 + 8.1 us, tables read at 3.2 and 1.0 TB/s; chains of a cold read, a meeting and, for the
 // second, h from other XCDs bound it (8 or 4 rows a workgroup, for more of them, change nothing).  17 rows and more are as quick with the
-// tiles above (18.5 and 18.9 us), fp32 from 33 on (45 and 70).
+// tiles above (18.5 and 18.9 us); 32 rows of fp32 take 47 us and in tiles 60.
 struct FewArgs {
     Matrix x, gate, up, down;
     float* h;                                           // [T,H]
