@@ -114,7 +114,11 @@ inline double makespan(int count, const int64_t* groups, const double* length) {
         for (int i = 0; i < count; ++i) if (!done[i] && (j < 0 || length[i] > length[j])) j = i;
         done[j] = true;
         int64_t left = groups[j];
-        if (left > 64 * kChip) return ((double)left / kChip + 1.0) * length[j] + load[n - 1].at;    // (many: no end effects)
+        if (left > 64 * kChip) {                        // many: they even out what was before them
+            load[0] = {kChip, load[n - 1].at + ((double)left / kChip + 1.0) * length[j]};
+            n = 1;
+            continue;
+        }
         while (left > 0) {
             Load take = load[0];
             if (left < take.cus) { load[0].cus -= left; take.cus = left; }
