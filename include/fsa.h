@@ -456,7 +456,7 @@ int fsa_norm_bwd(const void* grad_y, const void* grad_s, const void* s, int64_t 
 
 /*
  * Gated feed-forward block:  g = x Wg^T, u = x Wu^T  [T,H];  y = (act(g) * u) Wd^T  [T,O].
- *   x [T,D], w_gate [H,D], w_up [H,D], w_down [O,H]   fsa_dtype `dtype`
+ *   x [T,D], w_gate [H,D], w_up [H,D], w_down [O,H]   fsa_dtype `dtype`, to which FSA_GATED_FINE may be added, in all calls alike
  *   activation         an fsa_activation
  *   0 <= T <= FSA_GATED_TMAX; D, H, O from 1 to FSA_GATED_MOST
  *   out_y [T,O]        `dtype`
@@ -465,13 +465,15 @@ int fsa_norm_bwd(const void* grad_y, const void* grad_s, const void* s, int64_t 
  * again (fsa_gated_keep_pays: 1 where keeping them is quicker):
  *   dh = grad_y Wd, dg = dh u act'(g), du = dh act(g);  grad_x = dg Wg + du Wu,  grad_gate = dg^T x,  grad_up = du^T x,
  *   grad_down = grad_y^T (act(g) u).  Each in `dtype`, written whole (T == 0: the weights' are zero), and may be NULL.
- * act * u, dg and du are rounded to a 16-bit type once between the products, or in small calls to two of its numbers (fp16:
+ * act * u, dg and du are rounded to a 16-bit type once between the products (a result is then off by its own rounding and a
+ * factor's, some sqrt 2 of its own alone); in calls of up to 16 rows or of less than 4e9 operations, and with FSA_GATED_FINE in
+ * any, to two of its numbers, which leaves the result's own, and takes up to twice as long in large calls.  (fp16:
  * act * u up to 65504; dg and du beside the power of two of the largest |grad_y|, up to 2^15 times that).  What is kept of g and u
  * beside 16-bit tables is 24 bits each.  fp32 elements are taken whole; where an infinite one takes part, results may be NaN
  * that would be infinite.  relu'(0) = 0.
  */
 typedef enum { FSA_ACT_SILU = 0, FSA_ACT_GELU = 1, FSA_ACT_RELU = 2 } fsa_activation;   /* gelu: x * normal distribution */
-enum { FSA_GATED_TMAX = 1 << 26, FSA_GATED_MOST = 1 << 16 };
+enum { FSA_GATED_TMAX = 1 << 26, FSA_GATED_MOST = 1 << 16, FSA_GATED_FINE = 0x100 };
 
 int64_t fsa_gated_fwd_workspace_bytes(int64_t T, int64_t D, int64_t H, int64_t O, int dtype);
 int64_t fsa_gated_bwd_workspace_bytes(int64_t T, int64_t D, int64_t H, int64_t O, int dtype);

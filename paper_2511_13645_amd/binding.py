@@ -928,6 +928,7 @@ def fsa_class_bwd_workspace_bytes(T: int, V: int, D: int, dtype: torch.dtype, K:
 # ----------------------------------------------------------------------------------------
 FSA_NORM_DMAX = 16384
 FSA_GATED_MOST = 1 << 16
+FSA_GATED_FINE = 0x100
 _ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 ORTHOGONAL_COEFFICIENTS = (3.4445, -4.7750, 2.0315)     # singular values of 0.01 ... 1 go to 0.7 ... 1.2 in five steps
 
@@ -1024,14 +1025,14 @@ def fsa_norm_bwd_workspace_bytes(T: int, D: int, dtype: torch.dtype) -> int:
     return lib().fsa_norm_bwd_workspace_bytes(T, D, _FLOAT_TYPE[dtype])
 
 
-def _gated_operands(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, activation: str):
+def _gated_operands(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, activation: str, fine: bool):
     """Checked arguments of the gated block: (pointers, strides, type, activation and sizes), (T, D, H, O)."""
     act = _ACTIVATIONS.get(activation)
     if act is None:
         raise ValueError("activation must be one of %s, got %r" % (", ".join(sorted(_ACTIVATIONS)), activation))
     named = ((x, "x"), (w_gate, "w_gate"), (w_up, "w_up"), (w_down, "w_down"))
     strides = [_rows(t, name) for t, name in named]
-    code = _x_dtype(x)
+    code = _x_dtype(x) | (FSA_GATED_FINE if fine else 0)
     _same_type(x, "x", *named[1:])
     _same_device(x, *named[1:])
     (T, D), H, O = x.shape, w_gate.shape[0], w_down.shape[0]
@@ -1045,16 +1046,20 @@ def _gated_operands(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w
 
 
 def fsa_gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *, activation: str = "silu",
-                  emit_kept: bool = False, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+                  emit_kept: bool = False, fine: bool = False, workspace: Optional[torch.Tensor] = None,
+                  stream: Optional[torch.cuda.Stream] = None):
     """Gated feed-forward block (act(x w_gate^T) * (x w_up^T)) w_down^T: x [T,D], w_gate and w_up [H,D], w_down [O,H], all of one
     type; activation "silu", "gelu" (by the error function) or "relu".  Returns y [T,O], with `emit_kept` (y, kept): bytes
-    that spare a backward of the same operands making the hidden products again (fsa_gated_keep_pays).  `workspace`: see
-    fsa_gated_fwd_workspace_bytes; torch's memory without one.  `stream`: see fsa_xent_fwd."""
+    that spare a backward of the same operands making the hidden products again (fsa_gated_keep_pays).  `fine`: 16-bit calls of any
+    size hold what lies between the products in two numbers of the type, as calls of up to 16 rows or 4e9 operations do:
+    results are off by their own rounding alone, and large calls take up to twice as long; given to a forward, it is to be given
+    to its backward and to the functions of sizes.  fp16: act * u of up to 65504.  `workspace`: see fsa_gated_fwd_workspace_bytes; torch's
+    memory without one.  `stream`: see fsa_xent_fwd."""
     if _block_host is not None and stream is None and workspace is None and not emit_kept:
-        r = _block_host.gated_fwd(x, w_gate, w_up, w_down, _ACTIVATIONS.get(activation))
+        r = _block_host.gated_fwd(x, w_gate, w_up, w_down, _ACTIVATIONS.get(activation), bool(fine))
         if _taken(r, "fsa_gated_fwd"):
             return r
-    lead, (T, D, H, O) = _gated_operands(x, w_gate, w_up, w_down, activation)
+    lead, (T, D, H, O) = _gated_operands(x, w_gate, w_up, w_down, activation, fine)
     L = lib()
     with _on(x, stream):
         y = torch.empty((T, O), dtype=x.dtype, device=x.device)
@@ -1066,11 +1071,11 @@ def fsa_gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_d
     return (y, kept) if emit_kept else y
 
 
-def gated(x, w_gate, w_up, w_down, activation: str):
+def gated(x, w_gate, w_up, w_down, activation: str, fine: bool):
     """The differentiable block through the native host path, or None: then autograd.py's own function takes the call."""
     lib()
     if _block_host is not None:
-        r = _block_host.gated(x, w_gate, w_up, w_down, _ACTIVATIONS.get(activation))
+        r = _block_host.gated(x, w_gate, w_up, w_down, _ACTIVATIONS.get(activation), bool(fine))
         if _taken(r, "fsa_gated_fwd"):
             return r
     return None
@@ -1078,10 +1083,10 @@ def gated(x, w_gate, w_up, w_down, activation: str):
 
 def fsa_gated_bwd(grad_y: torch.Tensor, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor,
                   kept: Optional[torch.Tensor] = None, *, activation: str = "silu", want: Sequence[bool] = (True, True, True, True),
-                  workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+                  fine: bool = False, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Gradients of fsa_gated_fwd by x, w_gate, w_up and w_down from grad_y [T,O]; None where not wanted.  `kept`: what the
-    forward emitted, or None."""
-    lead, (T, D, H, O) = _gated_operands(x, w_gate, w_up, w_down, activation)
+    forward emitted, or None.  `fine`: see there."""
+    lead, (T, D, H, O) = _gated_operands(x, w_gate, w_up, w_down, activation, fine)
     gs = _rows(grad_y, "grad_y")
     _same_type(x, "x", (grad_y, "grad_y"))
     _shape(grad_y, "grad_y", (T, O))
@@ -1106,14 +1111,14 @@ def fsa_gated_keep_pays(T: int, D: int, H: int, O: int, dtype: torch.dtype) -> b
     return bool(lib().fsa_gated_keep_pays(T, D, H, O, _FLOAT_TYPE[dtype]))
 
 
-def fsa_gated_fwd_workspace_bytes(T: int, D: int, H: int, O: int, dtype: torch.dtype) -> int:
+def fsa_gated_fwd_workspace_bytes(T: int, D: int, H: int, O: int, dtype: torch.dtype, fine: bool = False) -> int:
     """Workspace bytes of fsa_gated_fwd; 0 for sizes that it refuses."""
-    return lib().fsa_gated_fwd_workspace_bytes(T, D, H, O, _FLOAT_TYPE[dtype])
+    return lib().fsa_gated_fwd_workspace_bytes(T, D, H, O, _FLOAT_TYPE[dtype] | (FSA_GATED_FINE if fine else 0))
 
 
-def fsa_gated_bwd_workspace_bytes(T: int, D: int, H: int, O: int, dtype: torch.dtype) -> int:
+def fsa_gated_bwd_workspace_bytes(T: int, D: int, H: int, O: int, dtype: torch.dtype, fine: bool = False) -> int:
     """Workspace bytes of fsa_gated_bwd; 0 for sizes that it refuses."""
-    return lib().fsa_gated_bwd_workspace_bytes(T, D, H, O, _FLOAT_TYPE[dtype])
+    return lib().fsa_gated_bwd_workspace_bytes(T, D, H, O, _FLOAT_TYPE[dtype] | (FSA_GATED_FINE if fine else 0))
 
 
 def fsa_orthogonalize(g: torch.Tensor, coefficients: Sequence = ORTHOGONAL_COEFFICIENTS, steps: int = 5, *, eps: float = 1e-7,

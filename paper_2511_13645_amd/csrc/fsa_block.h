@@ -68,6 +68,7 @@ struct NormArgs {
 struct GatedShape {
     int64_t T, D, H, O;
     int kind;                                           // 0 fp32, 1 bfloat16, 2 fp16
+    bool fine = false;                                  // two planes between the products whatever the sizes
 };
 constexpr int planes_of_kind(int kind) { return kind == 0 ? 3 : 1; }
 constexpr int kGatedPeaks = 256;                        // workgroups that look for the gradients' largest
@@ -194,8 +195,12 @@ inline int cut_pairs(int kind, int64_t T, int64_t H, int64_t depth, int pass) {
 
 // Whether h, dg and du are held with what their rounding to 16 bits leaves, as a second plane: results are off by their own rounding
 // alone, and their products take twice as long, which is less than the launches of a pass up to about this many operations
-// (1024 x 128 -> 512 -> 128, bfloat16: 4 us of 90).
-inline bool gated_fine(const GatedShape& s) { return s.kind != 0 && 6.0 * (double)s.T * (double)s.H * (double)(2 * s.D + s.O) < 4e9; }
+// (1024 x 128 -> 512 -> 128, bfloat16: 4 us of 90).  Few rows are bound by the tables, and have h in two planes where nothing is kept:
+// an answer is as exact whether its gradient is wanted or not.  In larger calls it is the caller's choice.
+inline bool gated_few(const GatedShape& s);
+inline bool gated_fine(const GatedShape& s) {
+    return s.kind != 0 && (s.fine || gated_few(s) || 6.0 * (double)s.T * (double)s.H * (double)(2 * s.D + s.O) < 4e9);
+}
 inline int gated_planes(const GatedShape& s) { return s.kind == 0 ? 3 : gated_fine(s) ? 2 : 1; }
 
 // A forward of few rows is bound by its reading of the tables: waves read them straight into registers, h is fp32.

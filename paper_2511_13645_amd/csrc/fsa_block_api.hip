@@ -42,17 +42,22 @@ bool in_place(const fsa::Matrix& m, int dtype) {
     return dtype != FSA_F32 && aligned(m.p, 16) && m.stride % 8 == 0 && m.cols % 8 == 0 && m.stride <= (1 << 21);
 }
 constexpr int kAllPacked = 31;
+int type_of(int dtype) { return dtype & ~FSA_GATED_FINE; }
+fsa::GatedShape gated_shape(int64_t T, int64_t D, int64_t H, int64_t O, int dtype) {
+    return {T, D, H, O, type_of(dtype), (dtype & FSA_GATED_FINE) != 0};
+}
+bool gated_known(int64_t T, int64_t D, int64_t H, int64_t O, int dtype) { return known(type_of(dtype)) && gated_sizes(T, D, H, O); }
 
 int gated_take(fsa::GatedArgs& a, const void* x, int64_t x_stride, const void* gate, int64_t gate_stride, const void* up, int64_t up_stride,
                const void* down, int64_t down_stride, int dtype, int activation, int64_t T, int64_t D, int64_t H, int64_t O) {
     if (!gate || !up || !down || (T > 0 && !x)) return FSA_ERR_NULL;
-    if (!known(dtype)) return FSA_ERR_DTYPE;
+    if (!known(type_of(dtype))) return FSA_ERR_DTYPE;
     if (!gated_sizes(T, D, H, O) || !in(activation, FSA_ACT_SILU, FSA_ACT_RELU)) return FSA_ERR_ARG;
     if (!in(x_stride, D, kMostStride) || !in(gate_stride, D, kMostStride) || !in(up_stride, D, kMostStride) || !in(down_stride, H, kMostStride))
         return FSA_ERR_ARG;
-    const int eb = elem_bytes(dtype);
+    const int eb = elem_bytes(type_of(dtype));
     if (!aligned(x, eb) || !aligned(gate, eb) || !aligned(up, eb) || !aligned(down, eb)) return FSA_ERR_ALIGN;
-    a.s = {T, D, H, O, dtype};
+    a.s = gated_shape(T, D, H, O, dtype);
     a.activation = activation;
     a.x = {x, x_stride, T, D};
     a.gate = {gate, gate_stride, H, D};
@@ -116,20 +121,20 @@ int fsa_norm_bwd(const void* grad_y, const void* grad_s, const void* s, int64_t 
 
 // The sizes alone do not say where operands lie: room to lay all of them out.
 int64_t fsa_gated_fwd_workspace_bytes(int64_t T, int64_t D, int64_t H, int64_t O, int dtype) {
-    if (!known(dtype) || !gated_sizes(T, D, H, O)) return 0;
-    return (int64_t)fsa::gated_plan({T, D, H, O, dtype}, false, false, kAllPacked).bytes;
+    if (!gated_known(T, D, H, O, dtype)) return 0;
+    return (int64_t)fsa::gated_plan(gated_shape(T, D, H, O, dtype), false, false, kAllPacked).bytes;
 }
 int64_t fsa_gated_bwd_workspace_bytes(int64_t T, int64_t D, int64_t H, int64_t O, int dtype) {
-    if (!known(dtype) || !gated_sizes(T, D, H, O)) return 0;
-    return (int64_t)fsa::gated_plan({T, D, H, O, dtype}, true, false, kAllPacked).bytes;
+    if (!gated_known(T, D, H, O, dtype)) return 0;
+    return (int64_t)fsa::gated_plan(gated_shape(T, D, H, O, dtype), true, false, kAllPacked).bytes;
 }
 
 int fsa_gated_keep_pays(int64_t T, int64_t D, int64_t H, int64_t O, int dtype) {
-    return known(dtype) && gated_sizes(T, D, H, O) && fsa::gated_keep_pays({T, D, H, O, dtype}) ? 1 : 0;
+    return gated_known(T, D, H, O, dtype) && fsa::gated_keep_pays(gated_shape(T, D, H, O, dtype)) ? 1 : 0;
 }
 
 int64_t fsa_gated_kept_bytes(int64_t T, int64_t D, int64_t H, int64_t O, int dtype) {
-    return known(dtype) && gated_sizes(T, D, H, O) ? (int64_t)fsa::kept_plan({T, D, H, O, dtype}).bytes : 0;
+    return gated_known(T, D, H, O, dtype) ? (int64_t)fsa::kept_plan(gated_shape(T, D, H, O, dtype)).bytes : 0;
 }
 
 int fsa_gated_fwd(const void* x, int64_t x_stride, const void* w_gate, int64_t gate_stride, const void* w_up, int64_t up_stride,
@@ -138,7 +143,7 @@ int fsa_gated_fwd(const void* x, int64_t x_stride, const void* w_gate, int64_t g
     fsa::GatedArgs a{};
     if (T > 0 && !out_y) return FSA_ERR_NULL;
     if (int rc = gated_take(a, x, x_stride, w_gate, gate_stride, w_up, up_stride, w_down, down_stride, dtype, activation, T, D, H, O)) return rc;
-    if (!aligned(out_y, elem_bytes(dtype)) || !aligned(out_kept, 16)) return FSA_ERR_ALIGN;
+    if (!aligned(out_y, elem_bytes(a.s.kind)) || !aligned(out_kept, 16)) return FSA_ERR_ALIGN;
     if (T == 0) return FSA_OK;
     a.packs = packs_of(a, false);
     a.plan = fsa::gated_plan(a.s, false, false, a.packs);
@@ -146,8 +151,8 @@ int fsa_gated_fwd(const void* x, int64_t x_stride, const void* w_gate, int64_t g
     a.y = out_y; a.kept = static_cast<char*>(out_kept); a.ws = static_cast<char*>(workspace);
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(stream);
-    return status_of(dtype == FSA_F32 ? fsa::gated_forward_f32(a, st) : dtype == FSA_BF16 ? fsa::gated_forward_bf16(a, st)
-                                                                                         : fsa::gated_forward_f16(a, st));
+    return status_of(a.s.kind == FSA_F32 ? fsa::gated_forward_f32(a, st) : a.s.kind == FSA_BF16 ? fsa::gated_forward_bf16(a, st)
+                                                                                               : fsa::gated_forward_f16(a, st));
 }
 
 int fsa_gated_bwd(const void* grad_y, int64_t grad_y_stride, const void* x, int64_t x_stride,
@@ -159,7 +164,7 @@ int fsa_gated_bwd(const void* grad_y, int64_t grad_y_stride, const void* x, int6
     if (T > 0 && !grad_y) return FSA_ERR_NULL;
     if (int rc = gated_take(a, x, x_stride, w_gate, gate_stride, w_up, up_stride, w_down, down_stride, dtype, activation, T, D, H, O)) return rc;
     if (!in(grad_y_stride, O, kMostStride)) return FSA_ERR_ARG;
-    const int eb = elem_bytes(dtype);
+    const int eb = elem_bytes(a.s.kind);
     if (!aligned(grad_y, eb) || !aligned(grad_x, eb) || !aligned(grad_gate, eb) || !aligned(grad_up, eb) || !aligned(grad_down, eb) ||
         !aligned(kept, 16))
         return FSA_ERR_ALIGN;
@@ -174,8 +179,8 @@ int fsa_gated_bwd(const void* grad_y, int64_t grad_y_stride, const void* x, int6
     }
     (void)hipGetLastError();
     hipStream_t st = static_cast<hipStream_t>(stream);
-    return status_of(dtype == FSA_F32 ? fsa::gated_backward_f32(a, st) : dtype == FSA_BF16 ? fsa::gated_backward_bf16(a, st)
-                                                                                          : fsa::gated_backward_f16(a, st));
+    return status_of(a.s.kind == FSA_F32 ? fsa::gated_backward_f32(a, st) : a.s.kind == FSA_BF16 ? fsa::gated_backward_bf16(a, st)
+                                                                                                : fsa::gated_backward_f16(a, st));
 }
 
 int64_t fsa_orthogonalize_workspace_bytes(int64_t B, int64_t M, int64_t N, int dtype) {

@@ -276,7 +276,8 @@ PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
 struct GatedCall {
     Tensor t[4];                                           // x, w_gate, w_up, w_down
     int64_t stride[4], T, D, H, O;
-    int code, activation;
+    int code, activation;                                  // code: of the type, with FSA_GATED_FINE
+    bool fine = false;
     void* stream;
 };
 
@@ -284,12 +285,17 @@ void gated_sizes(GatedCall& c) {
     for (int i = 0; i < 4; ++i) c.stride[i] = rows_of(&c.t[i]);
     c.T = c.t[0].size(0); c.D = c.t[0].size(1); c.H = c.t[1].size(0); c.O = c.t[3].size(0);
     c.code = float_code(c.t[0]);
+    if (c.code >= 0 && c.fine) c.code |= FSA_GATED_FINE;
 }
 
-// (x, w_gate, w_up, w_down, activation's number)
-bool gated_call(GatedCall& c, PyObject* const* a) {
+// (x, w_gate, w_up, w_down, activation's number[, fine])
+bool gated_call(GatedCall& c, PyObject* const* a, Py_ssize_t n) {
     if (!PyLong_CheckExact(a[4])) return false;
     c.activation = (int)PyLong_AsLong(a[4]);
+    if (n > 5) {
+        if (!PyBool_Check(a[5])) return false;
+        c.fine = a[5] == Py_True;
+    }
     for (int i = 0; i < 4; ++i) {
         const Tensor* t = tensor_of(a[i]);
         if (!rows_of(t)) return false;
@@ -320,6 +326,7 @@ struct Gated : torch::autograd::Function<Gated> {
         if (const int rc = gated_forward(c, keep, y, kept)) throw Refused(rc);
         ctx->save_for_backward({x, gate, up, down, kept});
         ctx->saved_data["activation"] = (int64_t)c.activation;
+        ctx->saved_data["fine"] = c.fine;
         ctx->saved_data["stream"] = (int64_t)reinterpret_cast<intptr_t>(c.stream);
         return y;
     }
@@ -332,6 +339,7 @@ struct Gated : torch::autograd::Function<Gated> {
             at::AutoGradMode off(false);
             GatedCall c;
             for (int i = 0; i < 4; ++i) c.t[i] = v[i];
+            c.fine = ctx->saved_data["fine"].toBool();
             gated_sizes(c);
             const Tensor g = grads[0].contiguous(), &kept = v[4];
             const auto like = at::TensorOptions().dtype(g.dtype()).device(g.device());
@@ -349,12 +357,12 @@ struct Gated : torch::autograd::Function<Gated> {
     }
 };
 
-// (x, w_gate, w_up, w_down, activation's number) -> y
+// (x, w_gate, w_up, w_down, activation's number[, fine]) -> y
 PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 5) Py_RETURN_NONE;
+    if (n != 5 && n != 6) Py_RETURN_NONE;
     return or_none([&]() -> PyObject* {
         GatedCall c;
-        if (!gated_call(c, a)) { if (PyErr_Occurred()) return nullptr; Py_RETURN_NONE; }
+        if (!gated_call(c, a, n)) { if (PyErr_Occurred()) return nullptr; Py_RETURN_NONE; }
         Tensor y, kept;
         const int rc = without_gil([&] {
             at::AutoGradMode off(false);
@@ -366,10 +374,10 @@ PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 // The same with its gradients.
 PyObject* gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 5) Py_RETURN_NONE;
+    if (n != 5 && n != 6) Py_RETURN_NONE;
     return or_none([&]() -> PyObject* {
         GatedCall c;
-        if (!gated_call(c, a)) { if (PyErr_Occurred()) return nullptr; Py_RETURN_NONE; }
+        if (!gated_call(c, a, n)) { if (PyErr_Occurred()) return nullptr; Py_RETURN_NONE; }
         Tensor y;
         const int rc = without_gil([&] {
             try {
