@@ -187,10 +187,14 @@ def fused_residual_norm(x: torch.Tensor, weight: torch.Tensor, residual: Optiona
 class _GatedFeedForward(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w_gate, w_up, w_down, activation, fine, keep):
-        kept = None
-        if keep and binding.fsa_gated_keep_pays(*x.shape, w_gate.shape[0], w_down.shape[0], x.dtype):
-            y, kept = binding.fsa_gated_fwd(x, w_gate, w_up, w_down, activation=activation, emit_kept=True, fine=fine)
-        else:
+        kept = y = None
+        if keep or keep is None and binding.fsa_gated_keep_pays(*x.shape, w_gate.shape[0], w_down.shape[0], x.dtype):
+            try:
+                y, kept = binding.fsa_gated_fwd(x, w_gate, w_up, w_down, activation=activation, emit_kept=True, fine=fine)
+            except torch.cuda.OutOfMemoryError:              # no room for it: making it again needs none
+                if keep:
+                    raise
+        if y is None:
             y = binding.fsa_gated_fwd(x, w_gate, w_up, w_down, activation=activation, fine=fine)
         ctx.save_for_backward(x, w_gate, w_up, w_down, kept)
         ctx.activation, ctx.fine = activation, fine
@@ -205,13 +209,15 @@ class _GatedFeedForward(torch.autograd.Function):
 
 
 def fused_gated_feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
-                             activation: str = "silu", fine: bool = False) -> torch.Tensor:
+                             activation: str = "silu", fine: bool = False, keep: Optional[bool] = None) -> torch.Tensor:
     """Differentiable gated feed-forward block (act(x w_gate^T) * (x w_up^T)) w_down^T of rows x [T,D]: w_gate, w_up [H,D],
-    w_down [O,H], one type.  What is kept for the backward is its inputs, and the two hidden products where that is quicker than making them
-    again.  16-bit types: between the products numbers are rounded to the type once; with `fine` they are not, at up to twice the time of
+    w_down [O,H], one type.  What is kept for the backward is its inputs, and with `keep` the two hidden products and what is made of them, 8
+    bytes (fp32: 14) for every row and hidden element; without, its backward makes them again.  keep=None keeps them where that is
+    quicker and there is room.  16-bit types: between the products numbers are rounded to the type once; with `fine` they are not, at up to twice the time of
     a large call (binding.fsa_gated_fwd).  fp16: act(x w_gate^T) * (x w_up^T) of up to 65504."""
-    y = binding.gated(x, w_gate, w_up, w_down, activation, fine)
+    y = binding.gated(x, w_gate, w_up, w_down, activation, fine, keep)
     if y is not None:
         return y
-    keep = torch.is_grad_enabled() and any(t.requires_grad for t in (x, w_gate, w_up, w_down))
+    if not (torch.is_grad_enabled() and any(t.requires_grad for t in (x, w_gate, w_up, w_down))):
+        keep = False
     return _GatedFeedForward.apply(x, w_gate, w_up, w_down, activation, bool(fine), keep)

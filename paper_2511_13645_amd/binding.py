@@ -1071,11 +1071,11 @@ def fsa_gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_d
     return (y, kept) if emit_kept else y
 
 
-def gated(x, w_gate, w_up, w_down, activation: str, fine: bool):
+def gated(x, w_gate, w_up, w_down, activation: str, fine: bool, keep: Optional[bool]):
     """The differentiable block through the native host path, or None: then autograd.py's own function takes the call."""
     lib()
     if _block_host is not None:
-        r = _block_host.gated(x, w_gate, w_up, w_down, _ACTIVATIONS.get(activation), bool(fine))
+        r = _block_host.gated(x, w_gate, w_up, w_down, _ACTIVATIONS.get(activation), bool(fine), keep if keep is None else bool(keep))
         if _taken(r, "fsa_gated_fwd"):
             return r
     return None

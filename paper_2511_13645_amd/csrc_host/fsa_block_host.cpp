@@ -278,6 +278,7 @@ struct GatedCall {
     int64_t stride[4], T, D, H, O;
     int code, activation;                                  // code: of the type, with FSA_GATED_FINE
     bool fine = false;
+    enum Keep { kAsPays, kNever, kAlways } keep = kAsPays;    // what a backward would make again
     void* stream;
 };
 
@@ -288,13 +289,17 @@ void gated_sizes(GatedCall& c) {
     if (c.code >= 0 && c.fine) c.code |= FSA_GATED_FINE;
 }
 
-// (x, w_gate, w_up, w_down, activation's number[, fine])
+// (x, w_gate, w_up, w_down, activation's number[, fine[, keep: None, False or True]])
 bool gated_call(GatedCall& c, PyObject* const* a, Py_ssize_t n) {
     if (!PyLong_CheckExact(a[4])) return false;
     c.activation = (int)PyLong_AsLong(a[4]);
     if (n > 5) {
         if (!PyBool_Check(a[5])) return false;
         c.fine = a[5] == Py_True;
+    }
+    if (n > 6) {
+        if (a[6] != Py_None && !PyBool_Check(a[6])) return false;
+        c.keep = a[6] == Py_None ? GatedCall::kAsPays : a[6] == Py_True ? GatedCall::kAlways : GatedCall::kNever;
     }
     for (int i = 0; i < 4; ++i) {
         const Tensor* t = tensor_of(a[i]);
@@ -311,8 +316,13 @@ bool gated_call(GatedCall& c, PyObject* const* a, Py_ssize_t n) {
 int gated_forward(const GatedCall& c, bool keep, Tensor& y, Tensor& kept) {
     const auto like = at::TensorOptions().dtype(c.t[0].dtype()).device(c.t[0].device());
     y = at::empty({c.T, c.O}, like);
-    if (keep && abi.fsa_gated_keep_pays(c.T, c.D, c.H, c.O, c.code))
-        kept = at::empty({abi.fsa_gated_kept_bytes(c.T, c.D, c.H, c.O, c.code)}, like.dtype(at::kByte));
+    if (keep && c.keep != GatedCall::kNever && (c.keep == GatedCall::kAlways || abi.fsa_gated_keep_pays(c.T, c.D, c.H, c.O, c.code))) {
+        try {
+            kept = at::empty({abi.fsa_gated_kept_bytes(c.T, c.D, c.H, c.O, c.code)}, like.dtype(at::kByte));
+        } catch (const c10::OutOfMemoryError&) {           // no room for it: making it again needs none
+            if (c.keep == GatedCall::kAlways) throw;
+        }
+    }
     const int64_t need = abi.fsa_gated_fwd_workspace_bytes(c.T, c.D, c.H, c.O, c.code);
     const Tensor ws = at::empty({need}, like.dtype(at::kByte));            // (may go once the call is queued: same stream)
     return abi.fsa_gated_fwd(data(c.t[0]), c.stride[0], data(c.t[1]), c.stride[1], data(c.t[2]), c.stride[2], data(c.t[3]), c.stride[3],
@@ -372,9 +382,9 @@ PyObject* gated_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// The same with its gradients.
+// The same with its gradients (and `keep`).
 PyObject* gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 5 && n != 6) Py_RETURN_NONE;
+    if (n < 5 || n > 7) Py_RETURN_NONE;
     return or_none([&]() -> PyObject* {
         GatedCall c;
         if (!gated_call(c, a, n)) { if (PyErr_Occurred()) return nullptr; Py_RETURN_NONE; }
