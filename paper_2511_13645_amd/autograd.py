@@ -165,6 +165,7 @@ class _ResidualNorm(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_y, grad_s=None):
+        binding.refuse_capture("a norm")
         s, weight = ctx.saved_tensors
         want_x, want_weight = ctx.needs_input_grad[0] or ctx.needs_input_grad[2], ctx.needs_input_grad[1]
         grad_x, grad_weight = binding.fsa_norm_bwd(None if grad_y is None else grad_y.contiguous(),
@@ -203,6 +204,7 @@ class _GatedFeedForward(torch.autograd.Function):
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, grad_y):
+        binding.refuse_capture("a gated block")
         grads = binding.fsa_gated_bwd(grad_y.contiguous(), *ctx.saved_tensors, activation=ctx.activation, fine=ctx.fine,
                                       want=ctx.needs_input_grad[:4])
         return (*grads, None, None, None)

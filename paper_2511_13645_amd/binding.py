@@ -943,6 +943,20 @@ def _on(t: torch.Tensor, stream: Optional[torch.cuda.Stream]):
         yield
 
 
+def refuse_capture(what: str) -> None:
+    """Raises in a backward that is captured into a graph while a leaf that its gradient goes to has an eager graph alive, one made on
+    another stream: autograd would have that stream wait for the captured one, which ends the process.  Without the native host path, which
+    knows the streams of autograd's nodes, in any captured backward whose gradients go to leaves."""
+    if _block_host is not None:
+        _block_host.refuse_capture(what)
+        return
+    node = torch._C._current_autograd_node()
+    leaves = node is not None and any(n is not None and n.name() == "torch::autograd::AccumulateGrad" for n, _ in node.next_functions)
+    if leaves and torch.cuda.is_current_stream_capturing():
+        raise RuntimeError("the backward of %s cannot be captured without the native host path (an eager graph of the same parameters "
+                           "that is alive would end the process)" % what)
+
+
 def _vector(t: torch.Tensor, name: str, n: int) -> None:
     _need(t, name)
     _x_dtype(t)

@@ -143,6 +143,21 @@ void refuse_capture(const char* what) {
     TORCH_CHECK(!capturing, "the backward of ", what, " cannot be captured while an eager graph of the same parameters is alive "
                 "(one made on another stream): drop it, or what holds it, first");
 }
+// (what): the same for a backward that the Python code makes.
+PyObject* refuse_captured(PyObject*, PyObject* what) {
+    const char* name = PyUnicode_AsUTF8(what);
+    if (!name) return nullptr;
+    try {
+        refuse_capture(name);
+    } catch (const c10::Error& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what_without_backtrace());
+        return nullptr;
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+    Py_RETURN_NONE;
+}
 bool differentiated(const torch::autograd::variable_list& grads) {
     if (!c10::GradMode::is_enabled()) return false;
     for (const Tensor& g : grads) if (g.defined() && g.requires_grad()) return true;
@@ -426,6 +441,7 @@ PyMethodDef methods[] = {
     {"norm_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(norm_fwd)), METH_FASTCALL, nullptr},
     {"norm", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(norm)), METH_FASTCALL, nullptr},
     {"gated_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(gated_fwd)), METH_FASTCALL, nullptr},
+    {"refuse_capture", refuse_captured, METH_O, nullptr},
     {"gated", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(gated)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
