@@ -495,7 +495,7 @@ int fsa_gated_bwd(const void* grad_y, int64_t grad_y_stride, const void* x, int6
  *   coefficients       HOST [steps,3];  1 <= steps <= FSA_ORTHO_STEPS, each of a magnitude up to FSA_ORTHO_COEFFICIENT
  *   eps, scale         finite, eps not negative;  0 <= B <= FSA_ORTHO_BMAX, 1 <= M, N <= FSA_ORTHO_MOST
  *   out [B,M,N]        `dtype`
- * X is held to 23 bits of every element down to 2^-24 or so, singular values up to about 2.  A matrix of zeros (with any eps) has zeros; one
+ * X is held to 23 bits of every element down to 2^-15 and to 2^-38 below, singular values up to about 2.  A matrix of zeros (with any eps) has zeros; one
  * that holds an infinity or NaN is NaN throughout, whatever the others hold.
  */
 enum { FSA_ORTHO_STEPS = 32, FSA_ORTHO_COEFFICIENT = 16, FSA_ORTHO_BMAX = 65535, FSA_ORTHO_MOST = 1 << 16 };

@@ -63,14 +63,15 @@ template <int KIND> __global__ __launch_bounds__(256) void squares_kernel(OrthoA
     if (threadIdx.x == 0)
         reinterpret_cast<double*>(a.ws + a.plan.squares)[blockIdx.y * kOrthoPeaks + blockIdx.x] = (lds[0] + lds[1]) + (lds[2] + lds[3]);
 }
-__device__ __forceinline__ float inverse_norm(const OrthoArgs& a, unsigned batch) {
+// What brings a matrix to the planes of the first X, in 64 bits as well: 2^13 over a norm of 1e-36, or of 1e39, is no number of 32.
+__device__ __forceinline__ double first_unit(const OrthoArgs& a, unsigned batch) {
     const double* parts = reinterpret_cast<const double*>(a.ws + a.plan.squares) + batch * kOrthoPeaks + 4 * (threadIdx.x & 63);
     static_assert(kOrthoPeaks == 256, "four a lane");
     double sum = (parts[0] + parts[1]) + (parts[2] + parts[3]);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d, 64);
     const double norm = sqrt(sum) + (double)a.eps;
-    return norm > 0.0 ? (float)(1.0 / norm) : norm == 0.0 ? 0.0f : __builtin_nanf("");
+    return norm > 0.0 ? (double)kTwoTo<kUnitX> / norm : norm == 0.0 ? 0.0 : __builtin_nan("");
 }
 
 // Planes of the first X, 64 x 64 of it a workgroup; of a tall matrix its transpose.
@@ -83,11 +84,11 @@ template <int KIND> __global__ __launch_bounds__(256) void first_kernel(OrthoArg
     ElemOf<KIND> e[4][4] = {};                          // 4 elements of each fourth of the rows, asked for before the norm is there
 #pragma unroll
     for (int i = 0; i < 4; ++i) load_four<KIND>(g, r0 + i * 16 + threadIdx.x / 16, c0 + threadIdx.x % 16 * 4, a, e[i]);
-    const float unit = inverse_norm(a, batch) * kTwoTo<kUnitX>;
+    const double unit = first_unit(a, batch);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) tile[i * 16 + threadIdx.x / 16][threadIdx.x % 16 * 4 + j] = number<KIND>(e[i][j]) * unit;
+        for (int j = 0; j < 4; ++j) tile[i * 16 + threadIdx.x / 16][threadIdx.x % 16 * 4 + j] = (float)((double)number<KIND>(e[i][j]) * unit);
     __syncthreads();
     const int64_t m = a.plan.m, n = a.plan.n, n8 = a.plan.n8, plane = m * n8;
     uint16_t* x = reinterpret_cast<uint16_t*>(a.ws + a.plan.x[0]) + batch * 2 * plane;
