@@ -492,10 +492,12 @@ int fsa_gated_bwd(const void* grad_y, int64_t grad_y_stride, const void* x, int6
  * Orthogonalised matrices:  X = G / (|G|_F + eps);  for every step's (a, b, c):  A = X X^T, X = a X + (b A + c A A) X  (of the
  * transpose where G has more rows than columns);  out = scale * X.  Singular vectors stay, singular values follow a s + b s^3 + c s^5.
  *   g [B,M,N]          fsa_dtype `dtype`, matrices `batch_stride` and rows `stride` elements apart
- *   coefficients       HOST [steps,3];  1 <= steps <= FSA_ORTHO_STEPS, each of a magnitude up to FSA_ORTHO_COEFFICIENT
+ *   coefficients       HOST [steps,3];  1 <= steps <= FSA_ORTHO_STEPS, each of a magnitude up to FSA_ORTHO_COEFFICIENT, or up to 1024
+ *                      where singular values of 0 to 1 stay below 8 after every step
  *   eps, scale         finite, eps not negative;  0 <= B <= FSA_ORTHO_BMAX, 1 <= M, N <= FSA_ORTHO_MOST
  *   out [B,M,N]        `dtype`
- * X is held to 23 bits of every element down to 2^-15 and to 2^-38 below, singular values up to about 2.  A matrix of zeros (with any eps) has zeros; one
+ * X is held to 23 bits of every element down to 2^-15 and to 2^-38 below, singular values up to about 2, and to
+ * fewer bits below where the coefficients may take them further than 2.8.  A matrix of zeros (with any eps) has zeros; one
  * that holds an infinity or NaN is NaN throughout, whatever the others hold.
  */
 enum { FSA_ORTHO_STEPS = 32, FSA_ORTHO_COEFFICIENT = 16, FSA_ORTHO_BMAX = 65535, FSA_ORTHO_MOST = 1 << 16 };

@@ -1139,7 +1139,8 @@ def fsa_orthogonalize(g: torch.Tensor, coefficients: Sequence = ORTHOGONAL_COEFF
                       scale: float = 1.0, workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None
                       ) -> torch.Tensor:
     """`scale` times the orthogonalised matrix g [M,N], or matrices [B,M,N], by Newton-Schulz steps: X = g / (|g| + eps), then
-    X = a X + (b A + c A A) X with A = X X^T.  `coefficients`: (a, b, c) of every step, or one triple for each of `steps` steps.
+    X = a X + (b A + c A A) X with A = X X^T.  `coefficients`: (a, b, c) of every step, or one triple for each of `steps` steps; those
+    beyond 16 have to keep singular values of 0 to 1 below 8.
     `workspace`: see fsa_orthogonalize_workspace_bytes; torch's memory without one.  `stream`: see fsa_xent_fwd."""
     if not g.is_cuda:
         raise ValueError("g must live on the GPU")
@@ -1162,7 +1163,8 @@ def fsa_orthogonalize(g: torch.Tensor, coefficients: Sequence = ORTHOGONAL_COEFF
         rc = L.fsa_orthogonalize(_ptr(g), g.stride(0) if g.dim() == 3 else 0, stride, code, B, M, N, host, len(coefficients),
                                  float(eps), float(scale), _ptr(out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream, g))
     if rc != FSA_OK:
-        raise FsaError(rc, "fsa_orthogonalize")
+        far = any(abs(x) > 16 for x in host)
+        raise FsaError(rc, "fsa_orthogonalize" + (" (coefficients beyond 16 have to keep singular values of 0 to 1 below 8)" if far else ""))
     return out
 
 

@@ -300,10 +300,62 @@ struct GatedArgs {
 // orthogonalised updates
 // ---------------------------------------------------------------------------------------------------------------
 // X [m,n] with m <= n (the transpose of a tall matrix): two fp16 planes of X 2^13, likewise A = X X^T and P = b A + c A^2 of
-// which planes hold A 2^13 and P 2^10.
+// which planes hold A 2^13 and P 2^10; a step whose singular values may grow so far that one of them would not fit has it at a lower power.
 constexpr int kMostSteps = 32;
 constexpr int kOrthoPeaks = 256;                        // workgroups a matrix that sum its squares
-constexpr int kUnitX = 13, kUnitA = 13, kUnitP = 10;
+constexpr int kUnitX = 13, kUnitA = 13, kUnitP = 10, kLeastUnit = -110;
+constexpr double kMostHeld = 65504.0 / 1.02;            // of a plane, with room for what the sums are off by
+
+// No singular value of the first X is above one, and a step takes s to p(s) = a s + b s^3 + c s^5: what X, A = X X^T and P may have at
+// most follows from the coefficients alone, as the largest |b t + c t^2| and |p| over t = s^2 from 0 to the square of the largest s, at
+// an end or where their derivative is zero.  No element of a matrix is larger than its largest singular value.
+struct OrthoReach {
+    double poly, next;                                  // the largest |P| of a step, and the largest singular value after it
+};
+inline OrthoReach ortho_reach(const float* abc, double reach) {
+    const double a = abc[0], b = abc[1], c = abc[2], end = reach * reach;
+    OrthoReach r{0.0, 0.0};
+    auto at = [&](double t) {
+        if (!(t >= 0.0 && t <= end)) return;
+        const double poly = b * t + c * t * t, next = __builtin_sqrt(t) * (a + poly);
+        if (!(poly <= r.poly && -poly <= r.poly)) r.poly = poly < 0.0 ? -poly : poly;
+        if (!(next <= r.next && -next <= r.next)) r.next = next < 0.0 ? -next : next;
+    };
+    at(end);
+    if (c != 0.0) at(-b / (2.0 * c));
+    if (const double root = 9.0 * b * b - 20.0 * a * c; root >= 0.0) {      // a + 3 b t + 5 c t^2 = 0
+        const double q = -0.5 * (3.0 * b + (b < 0.0 ? -1.0 : 1.0) * __builtin_sqrt(root));
+        if (c != 0.0) at(q / (5.0 * c));
+        if (q != 0.0) at(a / q);
+    }
+    return r;
+}
+// The power of two at which planes hold what is `reach` at most.
+inline int ortho_unit(double reach, int most) {
+    int unit = most;
+    double held = reach;
+    for (int i = 0; i < most; ++i) held *= 2.0;
+    while (unit > kLeastUnit && !(held <= kMostHeld)) { held *= 0.5; --unit; }
+    return unit;
+}
+struct OrthoUnits { int x, a, p; };                     // of a step: of the X that it takes, and of its A and P
+// Coefficients above `plain` are taken where singular values stay below 8 after every step, which the usual units hold.
+inline bool ortho_units(const float* coefficients, int steps, double plain, OrthoUnits* units) {
+    double reach = 1.0;
+    bool small = true, near = true;
+    for (int i = 0; i < steps; ++i) {
+        const float* abc = coefficients + 3 * i;
+        for (int j = 0; j < 3; ++j) {
+            if (!(abc[j] <= 1024.0f && abc[j] >= -1024.0f)) return false;
+            small = small && abc[j] <= plain && abc[j] >= -plain;
+        }
+        const OrthoReach r = ortho_reach(abc, reach);
+        units[i] = {ortho_unit(reach, kUnitX), ortho_unit(reach * reach, kUnitA), ortho_unit(r.poly, kUnitP)};
+        reach = r.next;
+        near = near && reach <= 8.0;
+    }
+    return small || near;
+}
 
 struct OrthoShape {
     int64_t B, M, N;
@@ -361,6 +413,7 @@ struct OrthoArgs {
     int64_t batch_stride, stride;
     void* out;                                          // contiguous
     float coefficients[3 * kMostSteps];
+    OrthoUnits units[kMostSteps];
     int steps;
     float eps, scale;
     OrthoPlan plan;

@@ -197,10 +197,8 @@ int fsa_orthogonalize(const void* g, int64_t batch_stride, int64_t stride, int d
         !not_negative(eps) || !std::isfinite(scale) || !in(stride, N, kMostStride) || (B > 1 && batch_stride < 0))
         return FSA_ERR_ARG;
     fsa::OrthoArgs a{};
-    for (int i = 0; i < 3 * steps; ++i) {
-        if (!(std::fabs(coefficients[i]) <= (float)FSA_ORTHO_COEFFICIENT)) return FSA_ERR_ARG;
-        a.coefficients[i] = coefficients[i];
-    }
+    for (int i = 0; i < 3 * steps; ++i) a.coefficients[i] = coefficients[i];
+    if (!fsa::ortho_units(a.coefficients, steps, FSA_ORTHO_COEFFICIENT, a.units)) return FSA_ERR_ARG;
     if (!aligned(g, elem_bytes(dtype)) || !aligned(out, elem_bytes(dtype))) return FSA_ERR_ALIGN;
     if (B == 0) return FSA_OK;
     a.s = {B, M, N, dtype};

@@ -7,6 +7,7 @@
 #include "fsa_block_kernels.h"
 #include "fsa_product.hip.h"
 
+#include <cmath>
 #include <type_traits>
 
 namespace fsa {
@@ -109,7 +110,9 @@ struct StepArgs {
     float* parts;                                       // of a gram matrix with splits: tiles on and above the diagonal
     void* out;                                          // of the last step, in the caller's type
     int64_t m, n, m8, n8;
-    float a, b, c, scale;
+    // Units of the planes are powers of two: of a gram matrix in X's square, of A^2 and A in P's, of P X and X in X's, of the next X in this one's
+    // (which with coefficients that are known to keep singular values small are the usual ones), and the last X in the caller's.
+    float to_a, square, linear, product, keep, next, back;
     unsigned mt, nt, splits;
     bool tall, grid;
 };
@@ -174,25 +177,24 @@ template <class T, int WHAT, int KIND> __global__ __launch_bounds__(T::THREADS, 
         if (m >= a.m) return;
         if constexpr (WHAT == kGram) {
 #pragma unroll
-            for (int j = 0; j < W; ++j) v[j] *= kTwoTo<kUnitA - 2 * kUnitX>;
+            for (int j = 0; j < W; ++j) v[j] *= a.to_a;
             store_planes<2, true>(a.to + batch * 2 * square, square, m * a.m8 + n, n, a.m, v);
         } else if constexpr (WHAT == kPoly) {
             float old[W];
             load_planes<W>(sq, square, m * a.m8 + n, n, a.m8, old);
 #pragma unroll
-            for (int j = 0; j < W; ++j) v[j] = fmaf(a.c * kTwoTo<kUnitP - 2 * kUnitA>, v[j], a.b * kTwoTo<kUnitP - kUnitA> * old[j]);
+            for (int j = 0; j < W; ++j) v[j] = fmaf(a.square, v[j], a.linear * old[j]);
             store_planes<2, true>(a.to + batch * 2 * square, square, m * a.m8 + n, n, a.m, v);
         } else {
             float old[W];
             load_planes<W>(x, wide, m * a.n8 + n, n, a.n8, old);
 #pragma unroll
-            for (int j = 0; j < W; ++j) v[j] = fmaf(kTwoTo<-kUnitP>, v[j], a.a * old[j]);
+            for (int j = 0; j < W; ++j) v[j] = fmaf(a.product, v[j], a.keep * old[j]) * a.next;
             if (!a.out) store_planes<2, true>(a.to + batch * 2 * wide, wide, m * a.n8 + n, n, a.n, v);
             else {
                 ElemOf<KIND>* out = static_cast<ElemOf<KIND>*>(a.out) + batch * a.m * a.n;
-                const float back = a.scale * kTwoTo<-kUnitX>;
 #pragma unroll
-                for (int j = 0; j < W; ++j) v[j] *= back;
+                for (int j = 0; j < W; ++j) v[j] *= a.back;
                 if (!a.tall) store_row<KIND>(out, m * a.n, n, a.n, a.grid, v);
                 else {
 #pragma unroll
@@ -227,7 +229,7 @@ __global__ __launch_bounds__(kMirrorThreads) void mirror_kernel(StepArgs a, unsi
             for (unsigned s = 0; s < a.splits; ++s) x += *reinterpret_cast<const f32x4*>(part + s * tiles * size + row * tile + col);
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) sum[row][col + j] = x[j] * kTwoTo<kUnitA - 2 * kUnitX>;
+        for (int j = 0; j < 4; ++j) sum[row][col + j] = x[j] * a.to_a;
     }
     __syncthreads();
     const int64_t square = a.m * a.m8;
@@ -270,13 +272,20 @@ template <int KIND> hipError_t run(const OrthoArgs& a, hipStream_t st) {
     uint16_t *sq = reinterpret_cast<uint16_t*>(a.ws + p.a), *poly = reinterpret_cast<uint16_t*>(a.ws + p.p);
     s.sq = sq; s.poly = poly;
     s.m = p.m; s.n = p.n; s.m8 = p.m8; s.n8 = p.n8;
-    s.scale = a.scale;
     s.parts = reinterpret_cast<float*>(a.ws + p.parts);
     s.splits = (unsigned)p.splits;
     s.tall = a.s.M > a.s.N;
     s.grid = reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && p.n * (int64_t)sizeof(ElemOf<KIND>) % 16 == 0;
     for (int i = 0; i < a.steps; ++i) {
-        s.a = a.coefficients[3 * i]; s.b = a.coefficients[3 * i + 1]; s.c = a.coefficients[3 * i + 2];
+        const OrthoUnits& u = a.units[i];
+        const float* abc = a.coefficients + 3 * i;
+        s.to_a = ldexpf(1.0f, u.a - 2 * u.x);
+        s.square = ldexpf(abc[2], u.p - 2 * u.a);
+        s.linear = ldexpf(abc[1], u.p - u.a);
+        s.product = ldexpf(1.0f, -u.p);
+        s.keep = abc[0];
+        s.next = i + 1 < a.steps ? ldexpf(1.0f, a.units[i + 1].x - u.x) : 1.0f;
+        s.back = ldexpf(a.scale, -u.x);
         s.x = x[i % 2];
         s.to = sq;
         if (hipError_t e = s.splits > 1 ? launch<kGramParts, 0>(s, a.s.B, p.gram, st) : launch<kGram, 0>(s, a.s.B, p.gram, st)) return e;
