@@ -152,13 +152,30 @@ __device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast
 // ---------------------------------------------------------------------------------------------------------------
 struct Gate { float value, slope; };
 __device__ __forceinline__ float inverse(float x) { return kKind == 0 ? 1.0f / x : __builtin_amdgcn_rcpf(x); }
+// The normal distribution beside 16-bit types, from its density: what lies beyond |g| is the density times Mills' ratio, which a polynomial of
+// 1 / (1 + 0.35 |g|) meets within 2^-20 of itself (fitted for the least largest error up to 14, where the density is 1e-43).  1 + erf
+// leaves nothing of gates below -5 (of gelu(-5) it is 4 % off).  Forward of 16384 x 1024 -> 4096 bfloat16: 379 us, with the library's erfc
+// 423, with 1 + erf 404.
+__device__ __forceinline__ float distribution(float g, float density) {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.35f, fabsf(g), 1.0f));
+    float ratio = 0.122679926f;
+    ratio = fmaf(ratio, t, -0.506635785f);
+    ratio = fmaf(ratio, t, 0.603193879f);
+    ratio = fmaf(ratio, t, -0.0426689051f);
+    ratio = fmaf(ratio, t, 0.390936345f);
+    ratio = fmaf(ratio, t, 0.334271938f);
+    ratio = fmaf(ratio, t, 0.351605564f);
+    ratio = fmaf(ratio, t, -6.84674669e-05f);
+    const float beyond = density * ratio;
+    return g < 0.0f ? beyond : 1.0f - beyond;
+}
 template <int ACT> __device__ __forceinline__ Gate gate_of(float g) {
     if constexpr (ACT == FSA_ACT_SILU) {
         const float p = inverse(1.0f + (kKind == 0 ? expf(-g) : __expf(-g)));
         return {g * p, p * fmaf(g, 1.0f - p, 1.0f)};
     } else if constexpr (ACT == FSA_ACT_GELU) {
-        const float p = kKind == 0 ? 0.5f * erfcf(-0.70710678118654752440f * g) : fmaf(0.5f, erff(0.70710678118654752440f * g), 0.5f);
         const float bell = 0.39894228040143267794f * (kKind == 0 ? expf(-0.5f * g * g) : __expf(-0.5f * g * g));
+        const float p = kKind == 0 ? 0.5f * erfcf(-0.70710678118654752440f * g) : distribution(g, bell);
         return {g * p, fmaf(g, bell, p)};
     } else {
         return {g > 0.0f ? g : (g != g ? g : 0.0f), g > 0.0f ? 1.0f : 0.0f};
