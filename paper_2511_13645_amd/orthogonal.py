@@ -57,7 +57,8 @@ class OrthogonalMomentum(torch.optim.Optimizer):
                 m = state["momentum"].mul_(group["momentum"]).add_(grad)
                 alike.setdefault((tuple(p.shape), p.device), []).append((p, grad.add(m, alpha=group["momentum"]) if group["nesterov"] else m))
             for (shape, _), members in alike.items():
-                update = members[0][1][None] if len(members) == 1 else torch.stack([u for _, u in members])
+                # (a lone one lies as its gradient does, whose columns may be what is contiguous)
+                update = members[0][1].contiguous()[None] if len(members) == 1 else torch.stack([u for _, u in members])
                 update = binding.fsa_orthogonalize(update, group["coefficients"], group["steps"], eps=group["eps"],
                                                    scale=max(1.0, shape[0] / shape[1]) ** 0.5)
                 for (p, _), u in zip(members, update):
