@@ -15,7 +15,7 @@ from . import binding
 
 class OrthogonalMomentum(torch.optim.Optimizer):
     """m = momentum * m + grad;  p -= rate * (decay * p + sqrt(max(1, rows / columns)) * orthogonalised(m)), or, with `nesterov`, of
-    grad + momentum * m.  The momentum is fp32 whatever the matrix's type."""
+    grad + momentum * m.  The momentum is fp32 whatever the matrix's type, and so is the step, of which a 16-bit matrix is rounded once."""
 
     def __init__(self, params: Iterable, rate: float = 0.02, momentum: float = 0.95, *, nesterov: bool = True, decay: float = 0.0,
                  steps: int = 5, coefficients=binding.ORTHOGONAL_COEFFICIENTS, eps: float = 1e-7):
@@ -62,7 +62,11 @@ class OrthogonalMomentum(torch.optim.Optimizer):
                 update = binding.fsa_orthogonalize(update, group["coefficients"], group["steps"], eps=group["eps"],
                                                    scale=max(1.0, shape[0] / shape[1]) ** 0.5)
                 for (p, _), u in zip(members, update):
+                    # 16-bit parameters are rounded once: a decay by itself, mostly less than half of a step, would be rounded away
+                    wide = p.float() if p.dtype in (torch.bfloat16, torch.float16) else p
                     if group["decay"]:
-                        p.mul_(1.0 - group["rate"] * group["decay"])
-                    p.add_(u.to(p.dtype), alpha=-group["rate"])
+                        wide.mul_(1.0 - group["rate"] * group["decay"])
+                    wide.add_(u, alpha=-group["rate"])
+                    if wide is not p:
+                        p.copy_(wide)
         return loss

@@ -1,6 +1,8 @@
-"""Orthogonalised momentum: parameters may lie in memory as they like."""
+"""Orthogonalised momentum: parameters of 16-bit types are rounded once a step, and parameters may lie in memory as they like."""
 import pytest
 import torch
+
+import block_bounds as bb
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -8,6 +10,29 @@ DEV = "cuda:0"
 
 def _normal(*shape, seed=0):
     return torch.randn(shape, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV)
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+@pytest.mark.parametrize("decay", [0.0, 0.05])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+def test_a_step_rounds_once(dtype, decay, nesterov):
+    from paper_2511_13645_amd import binding as fsa
+    from paper_2511_13645_amd.orthogonal import OrthogonalMomentum
+    rate, scale = 0.1, (120 / 40) ** 0.5
+    p = torch.nn.Parameter((_normal(120, 40) * 2).to(dtype))
+    opt = OrthogonalMomentum([p], rate, 0.9, decay=decay, nesterov=nesterov)
+    m = torch.zeros((120, 40), device=DEV)
+    for step in range(3):
+        p.grad = _normal(120, 40, seed=step + 1).to(dtype)
+        m = m * 0.9 + p.grad.float()
+        u = fsa.fsa_orthogonalize(p.grad.float() + 0.9 * m if nesterov else m, scale=scale).double()
+        want = p.detach().double() * (1 - rate * decay) - rate * u
+        opt.step()
+        # half a step of the result, and fp32's own few on the way to it
+        size = p.detach().double().abs() + want.abs() + rate * u.abs()
+        # (the momentum and its orthogonalised matrix are fp32 too: they may differ by the order of an addition, 2^-23 of sizes of up to
+        # 4 and of what five steps make of it, 3.5^5)
+        assert ((p.detach().double() - want).abs() <= bb.rounding(want, dtype) + 4 * bb.V * size + rate * 600 * 4 * bb.V).all()
 
 
 @pytest.mark.parametrize("count", [1, 2])
