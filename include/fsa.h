@@ -467,9 +467,9 @@ int fsa_norm_bwd(const void* grad_y, const void* grad_s, const void* s, int64_t 
  *   grad_down = grad_y^T (act(g) u).  Each in `dtype`, written whole (T == 0: the weights' are zero), and may be NULL.
  * act * u, dg and du are rounded to a 16-bit type once between the products (a result is then off by its own rounding and a
  * factor's, some sqrt 2 of its own alone); in calls of up to 16 rows or of less than 4e9 operations, and with FSA_GATED_FINE in
- * any, to two of its numbers, which leaves the result's own, and takes up to twice as long in large calls.  (fp16:
- * act * u up to 65504; dg and du beside the power of two of the largest |grad_y|, up to 2^15 times that).  What is kept of g and u
- * beside 16-bit tables is 24 bits each.  fp32 elements are taken whole; where an infinite one takes part, results may be NaN
+ * any, to two of its numbers, which leaves the result's own, and takes up to twice as long in large calls.  fp16 has them
+ * beside powers of two that the longest rows of x, the tables and grad_y allow: none is too large for it, and those of less than 2^-28 of
+ * what there could be at most have fewer bits.  What is kept of g and u beside 16-bit tables is 24 bits each.  fp32 elements are taken whole; where an infinite one takes part, results may be NaN
  * that would be infinite.  relu'(0) = 0.
  */
 typedef enum { FSA_ACT_SILU = 0, FSA_ACT_GELU = 1, FSA_ACT_RELU = 2 } fsa_activation;   /* gelu: x * normal distribution */

@@ -1067,7 +1067,7 @@ def fsa_gated_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_d
     that spare a backward of the same operands making the hidden products again (fsa_gated_keep_pays).  `fine`: 16-bit calls of any
     size hold what lies between the products in two numbers of the type, as calls of up to 16 rows or 4e9 operations do:
     results are off by their own rounding alone, and large calls take up to twice as long; given to a forward, it is to be given
-    to its backward and to the functions of sizes.  fp16: act * u of up to 65504.  `workspace`: see fsa_gated_fwd_workspace_bytes; torch's
+    to its backward and to the functions of sizes.  `workspace`: see fsa_gated_fwd_workspace_bytes; torch's
     memory without one.  `stream`: see fsa_xent_fwd."""
     if _block_host is not None and stream is None and workspace is None and not emit_kept:
         r = _block_host.gated_fwd(x, w_gate, w_up, w_down, _ACTIVATIONS.get(activation), bool(fine))

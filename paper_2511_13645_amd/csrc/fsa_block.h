@@ -71,8 +71,10 @@ struct GatedShape {
     bool fine = false;                                  // two planes between the products whatever the sizes
 };
 constexpr int planes_of_kind(int kind) { return kind == 0 ? 3 : 1; }
-constexpr int kGatedPeaks = 256;                        // workgroups that look for the gradients' largest
-
+// fp16 holds h, dg and du beside powers of two that bring what they may be at most near the end of its range: a product of the largest
+// lengths of rows (x, both tables, grad_y) and columns (w_down), for which so many workgroups look.
+constexpr int kGatedPeaks = 256;
+enum { kPeakX, kPeakGate, kPeakUp, kPeakGradY, kPeakDown, kPeakKinds };
 
 // Tiles that a product may be cut into, with the rate that each reached (TFLOP/s of 16-bit products, 8192 x 4096 x 4096).  `alone`: ns
 // that 1 of the depth takes a workgroup that no other keeps company, by its chain of requests, reads and products.  What is made
@@ -257,6 +259,8 @@ inline GatedPlan gated_plan(const GatedShape& s, bool backward, bool kept, int p
     if (packs & 4) p.up = room(s.H * p.D8 * planes);
     if (packs & 8) p.down = room(s.O * p.H8 * planes);
     p.h = room(!backward && gated_few(s) && own < s.T * s.H * 4 ? s.T * s.H * 4 : own);
+    const int64_t few = gated_few(s) ? cut_into(s.H, 16) : 0;          // of few rows the largest |h| of each workgroup's
+    if (s.kind == 2 && !backward) p.peaks = room((few > kPeakKinds * kGatedPeaks ? few : kPeakKinds * kGatedPeaks) * 4);
     const int64_t sums = s.kind != 0 ? p.planes : 1;    // products that make one, of h's, dg's or du's planes
     ProductCut want{};
     if (!backward) {
@@ -266,7 +270,7 @@ inline GatedPlan gated_plan(const GatedShape& s, bool backward, bool kept, int p
         if (packs & 16) p.grad_y = room(s.T * p.O8 * planes);
         p.dg = room(own);
         p.du = room(own);
-        p.peaks = room(kGatedPeaks * 4);
+        p.peaks = room(kPeakKinds * kGatedPeaks * 4);
         p.slopes = cut_pairs(s.kind, s.T, s.H, (kept ? 0 : 2 * s.D) + s.O, kept ? kKeptPass : kSlopesPass);
         want.count = 3;
         want.job[kJobGates] = {s.H, s.D, sums * s.T, 2, 1};

@@ -13,8 +13,11 @@
 // TFLOP/s with their join.
 // h, dg and du are rounded to the type once: each gradient is then off by its own rounding and one of a factor, as in any product of
 // tensors of that type.  fp32 has three planes and loses nothing.
-// fp16: dg and du are kept times the power of two that brings the largest |gy| to [1, 2), which the products take back, so that
-// gradients of a small loss scale are not rounded among fp16's subnormal numbers.
+// fp16: h, dg and du are kept times powers of two, which the products take back, so that none is beyond fp16's largest number and the smallest
+// are not rounded among its subnormal ones.  A product of two rows is no larger than that of their lengths:  |h| <= |g| |u| <= |x|^2 |wg| |wu|
+// and |dg|, |du| <= 1.13 |gy| |wd| |x| max(|wu|, |wg|), of the longest rows (columns of wd), are brought to [2^14, 2^15).  Such bounds
+// lie some 2^4 to 2^8 above the largest element that random numbers have; numbers of up to 2^-28 of a bound are normal ones.  Looking for the
+// longest rows is a launch: 4 us of 64 x 256 -> 1024, 13 us (3.8 TB/s) of 16384 x 1024 -> 4096's forward of 380 and 21 of its backward of 900.
 #pragma once
 
 #include "fsa_block_kernels.h"
@@ -70,9 +73,9 @@ struct PackList {
     uint16_t* to[5];
     int64_t first[6];                                   // pieces of 8 elements before each
     int count;
-    unsigned packers;                                   // workgroups that lay out; kGatedPeaks behind them look at grad_y
-    Matrix grad_y;
-    float* peaks;
+    unsigned packers;                                   // workgroups that lay out; behind them kGatedPeaks a kind look for the longest rows
+    Matrix measured[kPeakKinds];
+    float* peaks;                                       // [kinds][kGatedPeaks], squares
 };
 __device__ __forceinline__ void load_piece(const Matrix& from, int64_t row, int64_t col, Elem (&e)[8]) {
     const Elem* p = static_cast<const Elem*>(from.p) + row * from.stride + col;
@@ -85,27 +88,93 @@ __device__ __forceinline__ void load_piece(const Matrix& from, int64_t row, int6
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
     return a <= 0x7fffffff ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
-// fp16: the largest finite |grad_y| of a workgroup's share.
+// fp16: the square of the longest row of a workgroup's share, among those that are finite; of this wave's rows.  A lane asks for kAhead pieces
+// before it adds them up, with no branch but whether they are there.
+constexpr int kAhead = 8;
+__device__ __forceinline__ float half_of(u32x4 raw, int j) { return as_float<true>(j % 2 ? raw[j / 2] >> 16 : raw[j / 2] & 0xffff); }
+__device__ __forceinline__ float longest_row(const Matrix& m, unsigned share) {
+    const int64_t whole = m.cols / 8;
+    int bits = 0;                                       // lanes to a row
+    while (bits < 6 && kAhead << bits < whole) ++bits;
+    const int lane = threadIdx.x & 63, rows = 64 >> bits, lanes = 1 << bits, own = lane & (lanes - 1);
+    float top = 0.0f;
+    for (int64_t r = ((int64_t)share * 4 + (threadIdx.x >> 6)) * rows; r < m.rows; r += (int64_t)kGatedPeaks * 4 * rows) {
+        const int64_t row = r + (lane >> bits);
+        float sum = 0.0f;
+        if (row < m.rows) {
+            const Elem* p = static_cast<const Elem*>(m.p) + row * m.stride;
+            for (int64_t at = own; at < whole; at += kAhead * lanes) {
+                u32x4 raw[kAhead] = {};
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) if (at + i * lanes < whole) __builtin_memcpy(&raw[i], p + (at + i * lanes) * 8, 16);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum = fmaf(half_of(raw[i], j), half_of(raw[i], j), sum);
+            }
+            if (own == 0)
+                for (int64_t c = whole * 8; c < m.cols; ++c) {
+                    const float x = as_float<true>((uint32_t)p[c]);
+                    sum = fmaf(x, x, sum);
+                }
+        }
+        for (int d = 1; d < lanes; d *= 2) sum += __shfl_xor(sum, d, 64);
+        if (sum < __builtin_inff()) top = fmaxf(top, sum);
+    }
+    return top;
+}
+// The same of columns, 32 a workgroup at a time: four lanes to a row's, 64 rows side by side; all of the workgroup calls.
+__device__ __forceinline__ float longest_column(const Matrix& m, unsigned share) {
+    __shared__ float lds[4][32];
+    const int lane = threadIdx.x & 63, line = threadIdx.x >> 2;
+    float top = 0.0f;
+    for (int64_t c0 = (int64_t)share * 32; c0 < m.cols; c0 += (int64_t)kGatedPeaks * 32) {
+        const int64_t col = c0 + 8 * (lane & 3);
+        const Elem* p = static_cast<const Elem*>(m.p) + col;
+        float sum[8] = {};
+        if (col + 8 <= m.cols) {
+            for (int64_t row = line; row < m.rows; row += kAhead * 64) {
+                u32x4 raw[kAhead] = {};
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) if (row + i * 64 < m.rows) __builtin_memcpy(&raw[i], p + (row + i * 64) * m.stride, 16);
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) sum[j] = fmaf(half_of(raw[i], j), half_of(raw[i], j), sum[j]);
+            }
+        } else if (col < m.cols) {
+            for (int64_t row = line; row < m.rows; row += 64)
+#pragma unroll
+                for (int j = 0; j < 7; ++j) {
+                    const float x = col + j < m.cols ? as_float<true>((uint32_t)p[row * m.stride + j]) : 0.0f;
+                    sum[j] = fmaf(x, x, sum[j]);
+                }
+        }
+#pragma unroll
+        for (int d = 4; d < 64; d *= 2)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += __shfl_xor(sum[j], d, 64);
+        if (lane < 4)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) lds[threadIdx.x >> 6][8 * lane + j] = sum[j];
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            const float all = (lds[0][threadIdx.x] + lds[1][threadIdx.x]) + (lds[2][threadIdx.x] + lds[3][threadIdx.x]);
+            if (all < __builtin_inff()) top = fmaxf(top, all);
+        }
+        __syncthreads();
+    }
+    return top;
+}
 __device__ __forceinline__ void find_peak(const PackList& l) {
     __shared__ float lds[4];
-    const unsigned share = blockIdx.x - l.packers;
-    const int64_t pieces = cut_into(l.grad_y.cols, 8), all = l.grad_y.rows * pieces;
-    float top = 0.0f;
-    for (int64_t i = (int64_t)share * 256 + threadIdx.x; i < all; i += kGatedPeaks * 256) {
-        const int64_t row = quotient(i, pieces);
-        Elem e[8];
-        load_piece(l.grad_y, row, (i - row * pieces) * 8, e);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float x = fabsf(as_float<true>((uint32_t)e[j]));
-            if (x < __builtin_inff()) top = fmaxf(top, x);
-        }
-    }
+    const unsigned kind = (blockIdx.x - l.packers) / kGatedPeaks, share = (blockIdx.x - l.packers) % kGatedPeaks;
+    float top = kind == kPeakDown ? longest_column(l.measured[kind], share) : longest_row(l.measured[kind], share);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = top;
     __syncthreads();
-    if (threadIdx.x == 0) l.peaks[share] = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+    if (threadIdx.x == 0) l.peaks[kind * kGatedPeaks + share] = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
 }
 __global__ __launch_bounds__(256) void pack_kernel(PackList l) {
     if constexpr (kHalf)
@@ -135,16 +204,33 @@ __global__ __launch_bounds__(256) void pack_kernel(PackList l) {
     }
 }
 
-// 2^e with max * 2^e in [1, 2); what fp16 holds lies within 2^-24 ... 2^15.
-__device__ __forceinline__ int lift_of(const float* peaks) {
-    const f32x4 four = reinterpret_cast<const f32x4*>(peaks)[threadIdx.x & 63];
-    static_assert(kGatedPeaks == 256, "four a lane");
-    float top = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3]));
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
-    if (!(top > 0.0f)) return 0;
-    return 127 - (int)(__builtin_bit_cast(uint32_t, top) >> 23);
+// e with bound * 2^e in [2^14, 2^15).
+__device__ __forceinline__ int lift_to_end(float bound) {
+    if (!(bound > 0.0f)) return 0;
+    const int e = 14 + 127 - (int)(__builtin_bit_cast(uint32_t, bound) >> 23);
+    return e < -110 ? -110 : e > 110 ? 110 : e;
 }
+enum { kNoLift, kLiftH, kLiftD };
+// The power of two beside which h, or dg and du are kept (see above); 1.02 for what the sums are off by.
+template <int OF> __device__ __forceinline__ int lift_of(const float* peaks) {
+    constexpr int KINDS = OF == kLiftH ? kPeakGradY : kPeakKinds;
+    static_assert(kGatedPeaks == 256, "four a lane");
+    float top[KINDS];
+#pragma unroll
+    for (int k = 0; k < KINDS; ++k) {
+        const f32x4 four = reinterpret_cast<const f32x4*>(peaks + k * kGatedPeaks)[threadIdx.x & 63];
+        top[k] = fmaxf(fmaxf(four[0], four[1]), fmaxf(four[2], four[3]));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2)
+#pragma unroll
+        for (int k = 0; k < KINDS; ++k) top[k] = fmaxf(top[k], __shfl_xor(top[k], d, 64));
+#pragma unroll
+    for (int k = 0; k < KINDS; ++k) top[k] = sqrtf(top[k]);
+    if constexpr (OF == kLiftH) return lift_to_end(1.02f * (top[kPeakX] * top[kPeakGate]) * (top[kPeakX] * top[kPeakUp]));
+    else return lift_to_end(1.02f * 1.13f * (top[kPeakGradY] * top[kPeakDown]) * (top[kPeakX] * fmaxf(top[kPeakGate], top[kPeakUp])));
+}
+__device__ __forceinline__ int lift_of(const float* peaks, int of) { return of == kLiftH ? lift_of<kLiftH>(peaks) : of == kLiftD ? lift_of<kLiftD>(peaks) : 0; }
 __device__ __forceinline__ float power_of_two(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
 
 // ---------------------------------------------------------------------------------------------------------------
@@ -263,6 +349,7 @@ template <class T, int ACT, int PLANES> __global__ __launch_bounds__(T::THREADS,
     stream.flow.start(a.x, tables, m0, a.T, n0, a.H, 0, a.D);
     Ring<T, T::stage_bytes(2), Stream> ring{lds, stream};
     ring.fill();
+    const float lift = kHalf ? power_of_two(lift_of<kLiftH>(a.peaks)) : 1.0f;       // (beside the first requests)
     Sums<T, 2> acc = {};
     accumulate<T, true, true, 2>(acc, ring, cut_into(a.D, T::BK));
     ring.end();
@@ -279,7 +366,10 @@ template <class T, int ACT, int PLANES> __global__ __launch_bounds__(T::THREADS,
             store_kept(a.kept + a.at.u, a.kept + a.at.u_low, at, left, u);
         }
 #pragma unroll
-        for (int j = 0; j < W; ++j) g[j] = gate_of<ACT>(g[j]).value * u[j];
+        for (int j = 0; j < W; ++j) {
+            g[j] = gate_of<ACT>(g[j]).value * u[j];
+            if constexpr (kHalf) g[j] *= lift;
+        }
         store_planes<PLANES, T::HALF>(a.h, a.T * a.H8, m * a.H8 + n, n, a.H, g);
     });
 }
@@ -316,6 +406,7 @@ template <class T, int ACT, int PLANES, bool KEPT> __global__ __launch_bounds__(
     const int64_t m0 = (int64_t)mi * T::BM, n0 = (int64_t)ni * T::BN;
     Sums<T, PARTS> acc = {};
     Sums<T, 1> dh = {};
+    float lift = 1.0f, lift_h = 1.0f;                   // found beside the first requests
     if constexpr (KEPT) {
         using Stream = OneStream<T, true, false, 1>;
         Stream stream;
@@ -323,18 +414,19 @@ template <class T, int ACT, int PLANES, bool KEPT> __global__ __launch_bounds__(
         stream.flow.start(a.grad_y, table, m0, a.T, n0, a.H8, 0, a.O);
         Ring<T, T::stage_bytes(1), Stream> ring{lds, stream};
         ring.fill();
+        if constexpr (kHalf) lift = power_of_two(lift_of<kLiftD>(a.peaks));
         accumulate<T, true, false, 1>(dh, ring, cut_into(a.O, T::BK));
         ring.end();
     } else {
         SlopesStream<T> stream(a, m0, n0);
         Ring<T, T::stage_bytes(2), SlopesStream<T>> ring{lds, stream};
         ring.fill();
+        if constexpr (kHalf) { lift = power_of_two(lift_of<kLiftD>(a.peaks)); lift_h = power_of_two(lift_of<kLiftH>(a.peaks)); }
         accumulate<T, true, false, 1>(dh, ring, cut_into(a.O, T::BK));
         accumulate<T, true, true, 2>(acc, ring, cut_into(a.D, T::BK));
         ring.end();
     }
     settle<T, 1>(dh);
-    const float lift = kHalf ? power_of_two(lift_of(a.peaks)) : 1.0f;
     constexpr int W = 4 * T::NJ;
     KeptRow<W> kept_g, kept_u;                          // asked for a row ahead, before the one before is written
     auto ask_kept = [&](int64_t m, int64_t n) {
@@ -358,7 +450,7 @@ template <class T, int ACT, int PLANES, bool KEPT> __global__ __launch_bounds__(
         for (int j = 0; j < W; ++j) {
             const Gate at = gate_of<ACT>(g[j]);
             const float d = kHalf ? dh[0][i][j / 4][j % 4] * lift : dh[0][i][j / 4][j % 4];
-            g[j] = at.value * u[j];
+            g[j] = kHalf ? at.value * u[j] * lift_h : at.value * u[j];
             dg[j] = d * u[j] * at.slope;
             du[j] = d * at.value;
         }
@@ -380,7 +472,8 @@ struct Job {
     int64_t M8, N8;                                     // ends of flat operands
     float* parts;                                       // [results][splits][M][N8], where there are splits
     int pairs, results, planned;                        // planned: which of the plan's
-    bool adeep, grid, lifted;                           // lifted: dg or du is in it
+    int lift;                                           // beside which of them one operand is kept
+    bool adeep, grid;
     unsigned mt, nt, splits, first, first_join;         // workgroups before this job's
 };
 struct Jobs {
@@ -438,11 +531,13 @@ template <class T, bool ADEEP, bool BDEEP> struct ProductStream {
     }
 };
 
-template <class T, bool ADEEP, bool BDEEP> __device__ __forceinline__ void make_products(Sums<T, 1>& acc, char* lds, const Place& p) {
+// `back`: what takes the operand's power of two from the result, found beside the first requests.
+template <class T, bool ADEEP, bool BDEEP> __device__ __forceinline__ void make_products(Sums<T, 1>& acc, char* lds, const Place& p, const float* peaks, float& back) {
     using Stream = ProductStream<T, ADEEP, BDEEP>;
     Stream stream(p);
     Ring<T, T::stage_bytes(1), Stream> ring{lds, stream};
     ring.fill();
+    if (kHalf && p.job->splits == 1) back = power_of_two(-lift_of(peaks, p.job->lift));
     accumulate<T, ADEEP, BDEEP, 1>(acc, ring, stream.steps);
     ring.end();
     if constexpr (!BDEEP) settle<T, 1>(acc);
@@ -453,10 +548,10 @@ template <class T, bool FORWARD> __global__ __launch_bounds__(T::THREADS, T::wav
     const Place p = place_of(l, blockIdx.x);
     const Job& a = *p.job;
     Sums<T, 1> acc = {};
-    if constexpr (FORWARD) make_products<T, true, true>(acc, lds, p);
-    else if (a.adeep) make_products<T, true, false>(acc, lds, p);
-    else make_products<T, false, false>(acc, lds, p);
-    const float back = kHalf && a.lifted && a.splits == 1 ? power_of_two(-lift_of(l.peaks)) : 1.0f;
+    float back = 1.0f;
+    if constexpr (FORWARD) make_products<T, true, true>(acc, lds, p, l.peaks, back);
+    else if (a.adeep) make_products<T, true, false>(acc, lds, p, l.peaks, back);
+    else make_products<T, false, false>(acc, lds, p, l.peaks, back);
     each_stretch<T>((int64_t)p.mi * T::BM, (int64_t)p.ni * T::BN, [&](int i, int64_t m, int64_t n) {
         float x[4 * T::NJ];
 #pragma unroll
@@ -473,7 +568,7 @@ __global__ __launch_bounds__(256) void join_kernel(Jobs l) {
 #pragma unroll
     for (int j = 1; j < kMostJobs; ++j) if (j < l.count && blockIdx.x >= l.job[j].first_join) which_job = j;
     const Job& a = l.job[which_job];
-    const float back = kHalf && a.lifted ? power_of_two(-lift_of(l.peaks)) : 1.0f;
+    const float back = kHalf ? power_of_two(-lift_of(l.peaks, a.lift)) : 1.0f;
     const int64_t pieces = a.N8 / 4, all = a.M * pieces, at = (int64_t)(blockIdx.x - a.first_join) * 256 + threadIdx.x;
     if (at >= all * a.results) return;
     const int64_t which = at >= all ? 1 : 0, i = at - which * all, row = quotient(i, pieces);
@@ -501,6 +596,7 @@ __global__ __launch_bounds__(256) void zero_kernel(Elem* p, int64_t n) {
 struct FewArgs {
     Matrix x, gate, up, down;
     float* h;                                           // [T,H]
+    float* peaks;                                       // fp16: the largest |h| of each workgroup
     void* y;
     int64_t T, D, H, O;
     int activation;
@@ -599,6 +695,7 @@ template <int MT> __global__ __launch_bounds__(64 * kFewWaves) void few_hidden_k
         if (wave > 0) { lds[((wave - 1) * MT + t) * 128 + lane] = g[t]; lds[((wave - 1) * MT + t) * 128 + 64 + lane] = u[t]; }
     __syncthreads();
     if (wave > 0) return;
+    float top = 0.0f;
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
 #pragma unroll
@@ -609,10 +706,42 @@ template <int MT> __global__ __launch_bounds__(64 * kFewWaves) void few_hidden_k
         for (int j = 0; j < 4; ++j) {
             const int64_t n = (int64_t)blockIdx.x * 16 + 4 * q + j;
             if (n >= a.H) continue;
-            a.h[m * a.H + n] = gate_value(a.activation, g[t][j]) * u[t][j];
+            const float h = gate_value(a.activation, g[t][j]) * u[t][j];
+            a.h[m * a.H + n] = h;
+            if (kHalf && fabsf(h) < __builtin_inff()) top = fmaxf(top, fabsf(h));
         }
     }
+    if constexpr (kHalf) {
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+        if (lane == 0) a.peaks[blockIdx.x] = top;
+    }
 }
+// The power of two beside which few rows' h is split into planes, from the largest of all workgroups: asked for first, and found once the first
+// tables' elements are on their way.
+struct NoLift {
+    static constexpr int lift = 0;
+    __device__ __forceinline__ explicit NoLift(const FewArgs&) {}
+    __device__ __forceinline__ void find() {}
+};
+struct FewLift {
+    static constexpr int N = 4;
+    float top[N];
+    int lift = 1000;
+    __device__ __forceinline__ explicit FewLift(const FewArgs& a) {
+        const int64_t count = cut_into(a.H, 16);
+#pragma unroll
+        for (int i = 0; i < N; ++i) top[i] = (int)(threadIdx.x & 63) + 64 * i < count ? a.peaks[(threadIdx.x & 63) + 64 * i] : 0.0f;
+        for (int64_t i = (threadIdx.x & 63) + 64 * N; i < count; i += 64) top[0] = fmaxf(top[0], a.peaks[i]);
+    }
+    __device__ __forceinline__ void find() {
+        if (lift != 1000) return;
+        float all = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) all = fmaxf(all, __shfl_xor(all, d, 64));
+        lift = __builtin_amdgcn_readfirstlane(lift_to_end(all));
+    }
+};
 
 template <int MT> __global__ __launch_bounds__(64 * kFewAnswerWaves) void few_answer_kernel(FewArgs a) {
     __shared__ f32x4 lds[MT * kFewAnswerWaves * 64];
@@ -622,6 +751,7 @@ template <int MT> __global__ __launch_bounds__(64 * kFewAnswerWaves) void few_an
 #pragma unroll
     for (int t = 0; t < MT; ++t) hs[t] = a.h + (16 * t + r16 < a.T ? 16 * t + r16 : a.T - 1) * a.H;
     f32x4 acc[MT] = {};
+    typename std::conditional<kHalf, FewLift, NoLift>::type lift(a);
     few_steps(a.H, wave, kFewAnswerWaves, [&](auto whole, auto count, int64_t first) {
         constexpr bool WHOLE = decltype(whole)::value;
         constexpr int N = decltype(count)::value;
@@ -635,12 +765,18 @@ template <int MT> __global__ __launch_bounds__(64 * kFewAnswerWaves) void few_an
             for (int t = 0; t < MT; ++t) few_elements<WHOLE>(hs[t], col, a.H, he[s][t]);
         }
         __builtin_amdgcn_sched_barrier(0);
+        lift.find();
+        const float up = power_of_two(lift.lift);
 #pragma unroll
         for (int s = 0; s < N; ++s) {
             u32x4 down[NP], h[kHeld];
             few_operand(de[s], down);
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
+                if constexpr (kHalf) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) he[s][t][j] *= up;
+                }
                 few_planes<kHeld>(he[s][t], h);
                 acc[t] = few_product(down, h, acc[t]);
             }
@@ -649,6 +785,8 @@ template <int MT> __global__ __launch_bounds__(64 * kFewAnswerWaves) void few_an
 #pragma unroll
     for (int t = 0; t < MT; ++t) lds[(wave * MT + t) * 64 + lane] = acc[t];
     __syncthreads();
+    lift.find();                                        // (a wave without a share has not)
+    const float back = power_of_two(-lift.lift);
     // a sum a thread: 256 of each 16 rows
     for (int i = threadIdx.x; i < MT * 256; i += 64 * kFewAnswerWaves) {
         const int t = i >> 8, at = i >> 2 & 63, j = i & 3;
@@ -657,7 +795,7 @@ template <int MT> __global__ __launch_bounds__(64 * kFewAnswerWaves) void few_an
         for (int w = 0; w < kFewAnswerWaves; ++w) sum += lds[(w * MT + t) * 64 + at][j];
         const int64_t m = 16 * t + (at & 15), n = (int64_t)blockIdx.x * 16 + 4 * (at >> 4) + j;
         if (m >= a.T || n >= a.O) continue;
-        const float one[4] = {sum, 0.0f, 0.0f, 0.0f};
+        const float one[4] = {kHalf ? sum * back : sum, 0.0f, 0.0f, 0.0f};
         store_row<kKind>(a.y, m * a.O, n, n + 1, false, one);
     }
 }
@@ -735,7 +873,8 @@ hipError_t run_pair(const GatedArgs& g, const HiddenArgs& a, bool forward, hipSt
 
 struct Operands { Side x, gate, up, down, grad_y; };
 
-hipError_t lay_out(const GatedArgs& a, Operands& o, bool peaks, hipStream_t st) {
+// Lays out what products cannot read in place, and looks for the first `kinds` of the longest rows.
+hipError_t lay_out(const GatedArgs& a, Operands& o, int kinds, hipStream_t st) {
     const Matrix* from[5] = {&a.x, &a.gate, &a.up, &a.down, &a.grad_y};
     Side* to[5] = {&o.x, &o.gate, &o.up, &o.down, &o.grad_y};
     const size_t at[5] = {a.plan.x, a.plan.gate, a.plan.up, a.plan.down, a.plan.grad_y};
@@ -755,9 +894,10 @@ hipError_t lay_out(const GatedArgs& a, Operands& o, bool peaks, hipStream_t st) 
     }
     const int64_t blocks = cut_into(l.first[l.count], 256);
     l.packers = (unsigned)(blocks < 8192 ? blocks : 8192);
-    l.grad_y = a.grad_y;
+    const Matrix* measured[kPeakKinds] = {&a.x, &a.gate, &a.up, &a.grad_y, &a.down};
+    for (int k = 0; k < kinds; ++k) l.measured[k] = *measured[k];
     l.peaks = reinterpret_cast<float*>(a.ws + a.plan.peaks);
-    const unsigned groups = l.packers + (peaks ? kGatedPeaks : 0);
+    const unsigned groups = l.packers + kinds * kGatedPeaks;
     if (groups == 0) return hipSuccess;
     pack_kernel<<<dim3(groups), dim3(256), 0, st>>>(l);
     return hipGetLastError();
@@ -795,22 +935,24 @@ template <int MT> hipError_t launch_few(const FewArgs& f, hipStream_t st) {
 
 hipError_t forward(const GatedArgs& a, hipStream_t st) {
     if (gated_few(a.s) && !a.kept) {
-        const FewArgs f{a.x, a.gate, a.up, a.down, reinterpret_cast<float*>(a.ws + a.plan.h), a.y, a.s.T, a.s.D, a.s.H, a.s.O, a.activation};
+        const FewArgs f{a.x, a.gate, a.up, a.down, reinterpret_cast<float*>(a.ws + a.plan.h), reinterpret_cast<float*>(a.ws + a.plan.peaks), a.y, a.s.T, a.s.D, a.s.H, a.s.O, a.activation};
         if constexpr (kKind == 0) if (a.s.T > 16) return launch_few<2>(f, st);
         return launch_few<1>(f, st);
     }
     Operands o{};
-    if (hipError_t e = lay_out(a, o, false, st)) return e;
+    if (hipError_t e = lay_out(a, o, kHalf ? kPeakGradY : 0, st)) return e;
     const HiddenArgs h = hidden_args(a, o);
     if (hipError_t e = run_pair(a, h, true, st)) return e;
     Jobs l{};
     l.count = 1;
+    l.peaks = h.peaks;
     Job& j = l.job[0];
     add_pairs(j, 0, j.pairs, a.plan, {h.h, h.H8, a.s.T * h.H8}, o.down, true);
     j.results = 1;
     j.out[0] = a.y;
     j.M = a.s.T; j.N = a.s.O; j.K = a.s.H; j.out_ld = a.s.O;
     j.adeep = true;
+    j.lift = kLiftH;
     return run_products<true>(a, l, st);
 }
 
@@ -828,7 +970,7 @@ hipError_t backward(const GatedArgs& a, hipStream_t st) {
     }
     if (!outs[0] && !outs[1] && !outs[2] && !outs[3]) return hipSuccess;
     Operands o{};
-    if (hipError_t e = lay_out(a, o, kHalf, st)) return e;
+    if (hipError_t e = lay_out(a, o, kHalf ? kPeakKinds : 0, st)) return e;
     const HiddenArgs h = hidden_args(a, o);
     if (hipError_t e = run_pair(a, h, false, st)) return e;
     const int64_t plane = a.s.T * h.H8;
@@ -844,12 +986,13 @@ hipError_t backward(const GatedArgs& a, hipStream_t st) {
                 j.out[j.results++] = outs[i];
             }
         j.M = a.s.H; j.N = a.s.D; j.K = a.s.T; j.out_ld = a.s.D;
-        j.lifted = true;
+        j.lift = kLiftD;
         j.planned = kJobGates;
     }
     if (a.grad_down) {
         Job& j = l.job[l.count++];
         j.planned = kJobDown;
+        j.lift = kLiftH;
         add_pairs(j, 0, j.pairs, a.plan, hs, o.grad_y, false);
         j.results = 1;
         j.out[0] = a.grad_down;
@@ -862,7 +1005,8 @@ hipError_t backward(const GatedArgs& a, hipStream_t st) {
         j.results = 1;
         j.out[0] = a.grad_x;
         j.M = a.s.T; j.N = a.s.D; j.K = a.s.H; j.out_ld = a.s.D;
-        j.adeep = j.lifted = true;
+        j.adeep = true;
+        j.lift = kLiftD;
         j.planned = kJobX;
     }
     return run_products<false>(a, l, st);
