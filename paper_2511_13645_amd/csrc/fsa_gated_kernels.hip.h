@@ -6,13 +6,14 @@
 // g and u are made side by side (one x, two tables), so that a lane has both of an element and h is all that has to be written.  The
 // backward makes them again beside dh, in a kernel of three sums, or reads them where the forward kept them: in 16 bits they would be
 // rounded once more on the way to every gradient, so they are kept in 24 bits beside 16-bit tables.  16384 x 1024 -> 4096 bfloat16: the
-// hidden pass takes 292 us instead of 253 and the slopes 241 instead of 623, since three sums only leave room for tiles of
+// hidden pass takes some 290 us instead of 253 and the slopes 240 instead of 623, since three sums only leave room for tiles of
 // 128 x 128, of which the reads are as much as L2 gives.  What bounds them kept is the matrix cores (212 and 106 us of it at the rate of
 // the largest tile) and then what they write and read (0.54 and 0.67 GB), the one after the other: all workgroups are at the same
-// part of their tile, and one told to begin later gains as little as it loses.  The products of the backward, 5/9 of the work, reach 1180
-// TFLOP/s with their join.
+// part of their tile, and one told to begin later gains as little as it loses.  The products of the backward, 5/9 of the work, reach 1160
+// TFLOP/s with their join (687 GFLOP in 563 and 30 us).
 // h, dg and du are rounded to the type once: each gradient is then off by its own rounding and one of a factor, as in any product of
-// tensors of that type.  fp32 has three planes and loses nothing.
+// tensors of that type (0.0023 for 0.0017).  Two planes of them leave its own alone and take 1990 us of such a pass where one takes 1240: in
+// small calls, and where the caller asks for them.  fp32 has three planes and loses nothing.
 // fp16: h, dg and du are kept times powers of two, which the products take back, so that none is beyond fp16's largest number and the smallest
 // are not rounded among its subnormal ones.  A product of two rows is no larger than that of their lengths:  |h| <= |g| |u| <= |x|^2 |wg| |wu|
 // and |dg|, |du| <= 1.13 |gy| |wd| |x| max(|wu|, |wg|), of the longest rows (columns of wd), are brought to [2^14, 2^15).  Such bounds

@@ -17,8 +17,9 @@ using namespace product;
 
 // The tiles that fsa_block.h chooses from, in its order.  Steps of 64 of the depth where two stages of them fit: one 1024 x 1024 -> 4096
 // update takes 30 us rather than 37 with steps of 32, eight 600 x 2400 matrices 678 us rather than 745, though a CU then
-// holds one workgroup of 128 x 128 instead of two.  Four stages, two sets of fragments, depths begun at another place by each workgroup
-// and 8 waves to 64 x 64 changed nothing or cost (15.6 us of 1024 x 1024 x 1024: 13.2 to 16.2).
+// holds one workgroup of 128 x 128 instead of two.  Tiles of 64 x 64 wait for all of a step's requests at its head.  With four stages A A of
+// 1024 x 1024 takes 12.8 us rather than 15.5, one workgroup a CU, but P X of 602 x 2047, of more, 20.2 rather than 14.2, since LDS then has room
+// for one alone; two sets of fragments (15.5 and 14.8) and 8 waves (15.8 and 14.2) are no gain.
 template <int CHOICE> using OrthoTile = Tile<2, true, kTilesTwo[CHOICE].m, kTilesTwo[CHOICE].n, CHOICE <= 1 ? 64 : 32, 2, CHOICE == 0 ? 2 : 4>;
 template <int KIND> using ElemOf = typename std::conditional<KIND == 0, float, uint16_t>::type;
 template <int E> constexpr float kTwoTo = E > 0 ? (float)(1ull << (E > 0 ? E : 0)) : 1.0f / (float)(1ull << (E < 0 ? -E : 0));
