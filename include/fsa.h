@@ -442,7 +442,7 @@ int fsa_distill_bwd(const float* grad_loss, const void* h, int64_t h_stride, con
  * residual's gradient as well;  grad_weight = sum_t grad_y s rstd.
  *   grad_y, grad_s     [T,D] `dtype`, contiguous; either may be NULL: none
  *   grad_x [T,D] `dtype`, grad_weight [D] `weight_dtype`   written whole; either may be NULL
- * A row of zeros has y 0 where eps > 0.  Squares are summed in fp32: elements of more than about 1e18 make rstd 0.
+ * A row of zeros has y 0 where eps > 0.  Rows of any magnitude: those whose squares fp32 cannot sum are taken beside a power of two.
  */
 enum { FSA_NORM_TMAX = 1 << 30, FSA_NORM_DMAX = 16384 };
 

@@ -10,7 +10,7 @@
 //
 // 65536 x 1024 bfloat16 with a residual: forward 98 us (5.5 TB/s), backward 120 (4.5 TB/s) and 5 that join dw.  Rows held as numbers
 // from the first on took 108 and 129, 10007 x 602 fp16 24.7 rather than 19.0: all of a row's reads are asked for before the first
-// is unpacked.  The backward's 120 registers leave room for 16 waves a CU, which is what 1024 workgroups need; the next row read ahead
+// is unpacked.  The backward's registers leave room for 16 waves a CU, which is what 1024 workgroups need; the next row read ahead
 // takes 152 and is no quicker (122), 768, 1280 and 1536 workgroups take 136, 182 and 162 where 1024 take 129: two rounds, or too few reads.
 #include "fsa_block_kernels.h"
 #include "fsa_product.hip.h"
@@ -87,6 +87,60 @@ template <int LANES> __device__ __forceinline__ float row_sum(float x, float* ld
     return x;
 }
 
+// Largest x over the lanes of a row.
+template <int LANES> __device__ __forceinline__ float row_most(float x, float* lds) {
+#pragma unroll
+    for (int d = 1; d < (LANES < 64 ? LANES : 64); d *= 2) x = fmaxf(x, __shfl_xor(x, d, 64));
+    if constexpr (LANES > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < LANES / 64; ++i) x = fmaxf(x, lds[i]);         // (a workgroup has one such row)
+    }
+    return x;
+}
+// rstd of a row whose squares are summed.  Squares that fp32 cannot hold (of elements beyond 2^60 or, where eps does not outweigh them, below
+// 2^-50; fp16 has none) are looked at again: the row's numbers are then times `unit`, the power of two that brings the largest to [1, 2), and rstd is that
+// of those numbers, since the row's own may be no number of fp32.
+struct Scale { float unit, rstd; };
+// What a branch that hardly a row takes makes of pieces is made there, and of nothing that would be held in registers on the way to it.
+template <int KIND, int NV> __device__ __forceinline__ void afresh(Piece<KIND> (&s)[NV]) {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) asm volatile("" : "+v"(s[v].raw));
+}
+template <int KIND, int LANES, int NV> __device__ __forceinline__ Scale scale_of(Piece<KIND> (&s)[NV], float sum, const NormArgs& a, float* lds) {
+    Scale r{1.0f, 1.0f / sqrtf(sum / (float)a.D + a.eps)};
+    if constexpr (KIND != 2) {
+        const bool odd = !(sum < 0x1p120f) || (sum < 0x1p-100f && a.eps < 0x1p-70f);
+        if (__builtin_expect(!__any(odd), 1)) return r;  // (all lanes of a row that several waves have find the same)
+        constexpr int PER = Row<KIND>::PER;
+        float most = 0.0f, again = 0.0f;
+        afresh(s);
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int j = 0; j < PER; ++j) most = fmaxf(most, fabsf(s[v].get(j)));
+        most = row_most<LANES>(most, lds);
+        if (odd && most > 0.0f && most < __builtin_inff()) {
+            const int e = 254 - (int)(__builtin_bit_cast(uint32_t, most) >> 23);       // (of subnormal numbers the lowest)
+            r.unit = __builtin_bit_cast(float, (uint32_t)(e < 1 ? 1 : e > 253 ? 253 : e) << 23);
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            float x[PER];
+#pragma unroll
+            for (int j = 0; j < PER; ++j) x[j] = s[v].get(j) * r.unit;
+            s[v].set(x);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) again = fmaf(x[j], x[j], again);
+        }
+        again = row_sum<LANES>(again, lds);
+        if (odd) r.rstd = 1.0f / sqrtf(again / (float)a.D + a.eps * r.unit * r.unit);
+    }
+    return r;
+}
+
 template <int KIND, int LANES, int NV>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(NormArgs a) {
     constexpr int PER = Row<KIND>::PER, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES;
@@ -124,7 +178,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(Nor
 #pragma unroll
             for (int j = 0; j < PER; ++j) sum = fmaf(s[v].get(j), s[v].get(j), sum);
         }
-        const float rstd = 1.0f / sqrtf(row_sum<LANES>(sum, lds) / (float)D + a.eps);
+        const float rstd = scale_of<KIND, LANES, NV>(s, row_sum<LANES>(sum, lds), a, lds).rstd;
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * LANES + lane) * PER;
@@ -139,7 +193,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_fwd_kernel(Nor
 }
 
 template <int KIND, int LANES, int NV>
-__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256, LANES < 256 ? 4 : 1) void norm_bwd_kernel(NormArgs a) {
     constexpr int PER = Row<KIND>::PER, THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES;
     __shared__ float lds[THREADS / 64];
     __shared__ float join[ROWS > 1 ? LANES * NV * PER : 1];
@@ -172,8 +226,19 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(Nor
                 sum = fmaf(row.s[v].get(j), row.s[v].get(j), sum);
                 dot = fmaf(row.g[v].get(j) * w[v][j], row.s[v].get(j), dot);
             }
-        const float rstd = 1.0f / sqrtf(row_sum<LANES>(sum, lds) / (float)D + a.eps);
-        const float mean = row_sum<LANES>(dot, lds) * rstd / (float)D;         // of gy w s^
+        sum = row_sum<LANES>(sum, lds);
+        dot = row_sum<LANES>(dot, lds);
+        const Scale r = scale_of<KIND, LANES, NV>(row.s, sum, a, lds);
+        if (KIND != 2 && __any(r.unit != 1.0f)) {
+            dot = 0.0f;
+            afresh(row.g);
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int j = 0; j < PER; ++j) dot = fmaf(row.g[v].get(j) * w[v][j], row.s[v].get(j), dot);
+            dot = row_sum<LANES>(dot, lds);
+        }
+        const float mean = dot * r.rstd / (float)D, rstd = r.rstd * r.unit;         // mean: of gy w s^
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int c = (v * LANES + lane) * PER;
@@ -181,7 +246,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_bwd_kernel(Nor
             float x[PER];
 #pragma unroll
             for (int j = 0; j < PER; ++j) {
-                const float unit = row.s[v].get(j) * rstd;
+                const float unit = row.s[v].get(j) * r.rstd;
                 dw[v][j] = fmaf(row.g[v].get(j), unit, dw[v][j]);
                 x[j] = fmaf(rstd, fmaf(-unit, mean, row.g[v].get(j) * w[v][j]), row.gs[v].get(j));
             }
