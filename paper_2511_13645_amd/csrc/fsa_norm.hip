@@ -101,8 +101,8 @@ template <int LANES> __device__ __forceinline__ float row_most(float x, float* l
     return x;
 }
 // rstd of a row whose squares are summed.  Squares that fp32 cannot hold (of elements beyond 2^60 or, where eps does not outweigh them, below
-// 2^-50; fp16 has none) are looked at again: the row's numbers are then times `unit`, the power of two that brings the largest to [1, 2), and rstd is that
-// of those numbers, since the row's own may be no number of fp32.
+// 2^-50; fp16 has none) are looked at again: the row's numbers are then times `unit`, the power of two that brings the largest to [1, 2) (or
+// to less beside a larger eps), and rstd is that of those numbers, since the row's own may be no number of fp32.
 struct Scale { float unit, rstd; };
 // What a branch that hardly a row takes makes of pieces is made there, and of nothing that would be held in registers on the way to it.
 template <int KIND, int NV> __device__ __forceinline__ void afresh(Piece<KIND> (&s)[NV]) {
@@ -121,7 +121,7 @@ template <int KIND, int LANES, int NV> __device__ __forceinline__ Scale scale_of
         for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int j = 0; j < PER; ++j) most = fmaxf(most, fabsf(s[v].get(j)));
-        most = row_most<LANES>(most, lds);
+        most = fmaxf(row_most<LANES>(most, lds), sqrtf(a.eps));        // (where that is the larger, its square is what counts)
         if (odd && most > 0.0f && most < __builtin_inff()) {
             const int e = 254 - (int)(__builtin_bit_cast(uint32_t, most) >> 23);       // (of subnormal numbers the lowest)
             r.unit = __builtin_bit_cast(float, (uint32_t)(e < 1 ? 1 : e > 253 ? 253 : e) << 23);

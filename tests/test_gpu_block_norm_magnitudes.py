@@ -50,7 +50,7 @@ def test_with_a_residual_and_an_eps(dtype, d):
     from paper_2511_13645_amd import binding as fsa
     x, w, gy = _inputs(6, d, dtype)
     r = _inputs(6, d, dtype)[2]
-    for unit, eps in ((2.0 ** 100, 1e-6), (2.0 ** -90, 2.0 ** -100), (2.0 ** -90, 1e-6), (2.0 ** 70, 1e30)):
+    for unit, eps in ((2.0 ** 100, 1e-6), (2.0 ** -90, 2.0 ** -100), (2.0 ** -90, 1e-6), (2.0 ** 70, 1e30), (2.0 ** -120, 2.0 ** -80), (2.0 ** -75, 2.0 ** -148)):
         a, b = (_times(v, torch.tensor(unit).log2().item()) for v in (x, r))
         want = bb.norm(a, b, w, gy, None, eps, dtype)
         y, s = fsa.fsa_norm_fwd(a, w, b, eps)
