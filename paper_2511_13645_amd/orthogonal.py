@@ -48,7 +48,7 @@ class OrthogonalMomentum(torch.optim.Optimizer):
         for group in self.param_groups:
             alike = {}
             for p in group["params"]:
-                if p.grad is None:
+                if p.grad is None or p.numel() == 0:
                     continue
                 state = self.state[p]
                 grad = p.grad.float()

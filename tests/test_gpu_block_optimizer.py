@@ -62,3 +62,13 @@ def test_gradients_that_autograd_makes_of_them():
     (_normal(7, 30) @ w).square().sum().backward()
     opt.step()
     assert w.isfinite().all() and not torch.equal(w.detach(), before)
+
+
+def test_matrices_without_elements_are_left():
+    from paper_2511_13645_amd.orthogonal import OrthogonalMomentum
+    params = [torch.nn.Parameter(torch.zeros(shape, device=DEV)) for shape in ((0, 5), (5, 0), (4, 5))]
+    opt = OrthogonalMomentum(params, 0.1)
+    for p in params:
+        p.grad = torch.ones_like(p)
+    opt.step()
+    assert params[2].abs().min().item() > 0
