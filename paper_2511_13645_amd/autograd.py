@@ -213,10 +213,10 @@ class _GatedFeedForward(torch.autograd.Function):
 def fused_gated_feed_forward(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, w_down: torch.Tensor, *,
                              activation: str = "silu", fine: bool = False, keep: Optional[bool] = None) -> torch.Tensor:
     """Differentiable gated feed-forward block (act(x w_gate^T) * (x w_up^T)) w_down^T of rows x [T,D]: w_gate, w_up [H,D],
-    w_down [O,H], one type.  What is kept for the backward is its inputs, and with `keep` the two hidden products and what is made of them, 8
-    bytes (fp32: 14) for every row and hidden element; without, its backward makes them again.  keep=None keeps them where that is
-    quicker and there is room.  16-bit types: between the products numbers are rounded to the type once; with `fine` they are not, at up to twice the time of
-    a large call (binding.fsa_gated_fwd)."""
+    w_down [O,H], one type.  What is kept for the backward is its inputs and, with `keep`, the two hidden products and what is made of them:
+    8 to 10 bytes (fp32: 14) for every row and hidden element.  Without, its backward makes them again.  keep=None keeps them where
+    that is quicker and there is room.  16-bit types: between the products numbers are rounded to the type once; with `fine` they are
+    not, at up to twice the time of a large call (binding.fsa_gated_fwd)."""
     y = binding.gated(x, w_gate, w_up, w_down, activation, fine, keep)
     if y is not None:
         return y
