@@ -943,15 +943,26 @@ def _on(t: torch.Tensor, stream: Optional[torch.cuda.Stream]):
         yield
 
 
+def _goes_to_a_leaf(node) -> bool:
+    """Whether a gradient goes to a leaf, straight or through nodes of one input alone, as casts and views are."""
+    for _ in range(8):
+        if node is None or node.name() == "torch::autograd::AccumulateGrad":
+            return node is not None
+        behind = [n for n, _ in node.next_functions if n is not None]
+        node = behind[0] if len(behind) == 1 else None
+    return False
+
+
 def refuse_capture(what: str) -> None:
     """Raises in a backward that is captured into a graph while a leaf that its gradient goes to has an eager graph alive, one made on
-    another stream: autograd would have that stream wait for the captured one, which ends the process.  Without the native host path, which
+    another stream (the block's own parameter, or what a cast or a view of it is made of): autograd would have that stream wait for the captured
+    one, which ends the process.  Without the native host path, which
     knows the streams of autograd's nodes, in any captured backward whose gradients go to leaves."""
     if _block_host is not None:
         _block_host.refuse_capture(what)
         return
     node = torch._C._current_autograd_node()
-    leaves = node is not None and any(n is not None and n.name() == "torch::autograd::AccumulateGrad" for n, _ in node.next_functions)
+    leaves = node is not None and any(_goes_to_a_leaf(n) for n, _ in node.next_functions)
     if leaves and torch.cuda.is_current_stream_capturing():
         raise RuntimeError("the backward of %s cannot be captured without the native host path (an eager graph of the same parameters "
                            "that is alive would end the process)" % what)

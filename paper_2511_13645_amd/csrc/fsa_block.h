@@ -343,7 +343,7 @@ inline int ortho_unit(double reach, int most) {
     return unit;
 }
 struct OrthoUnits { int x, a, p; };                     // of a step: of the X that it takes, and of its A and P
-// Coefficients above `plain` are taken where singular values stay below 8 after every step, which the usual units hold.
+// Coefficients above `plain` are taken where singular values stay below 8 after every step.
 inline bool ortho_units(const float* coefficients, int steps, double plain, OrthoUnits* units) {
     double reach = 1.0;
     bool small = true, near = true;

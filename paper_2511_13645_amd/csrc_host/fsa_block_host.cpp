@@ -120,6 +120,20 @@ void once(const char* what, bool again, torch::autograd::variable_list& out) {
     auto node = std::make_shared<torch::autograd::DelayedError>(std::string(what) + " is differentiable once", (int)out.size());
     out = (*node)(std::move(out));
 }
+// The leaf that a gradient goes to: straight, or through nodes that have one input alone, as casts and views do; nullptr for another way.
+torch::autograd::Node* leaf_of(torch::autograd::Node* node) {
+    for (int i = 0; node && i < 8; ++i) {
+        if (dynamic_cast<torch::autograd::AccumulateGrad*>(node)) return node;
+        torch::autograd::Node* next = nullptr;
+        for (const auto& e : node->next_edges()) {
+            if (!e.function) continue;
+            if (next) return nullptr;
+            next = e.function.get();
+        }
+        node = next;
+    }
+    return nullptr;
+}
 // A backward that is captured into a graph while a leaf that its gradient goes to has an eager graph alive: autograd would have the
 // leaf's stream wait for the captured one, which ends the capture and the process.  Raises instead.
 void refuse_capture(const char* what) {
@@ -128,8 +142,8 @@ void refuse_capture(const char* what) {
     const auto own = node->stream();
     bool other = false;
     for (const auto& e : node->next_edges())
-        if (e.function && dynamic_cast<torch::autograd::AccumulateGrad*>(e.function.get())) {
-            const auto theirs = e.function->stream();
+        if (torch::autograd::Node* leaf = leaf_of(e.function.get())) {
+            const auto theirs = leaf->stream();
             other = other || (own && theirs && *own != *theirs);
         }
     if (!other) return;

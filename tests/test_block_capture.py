@@ -26,7 +26,10 @@ def test_without_the_native_host_path(monkeypatch):
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
     with pytest.raises(RuntimeError, match="a test cannot be captured without the native host path"):
         run(x)
-    assert torch.equal(run(x * 1), torch.full((3,), 2.0))
+    for view in (lambda: x.double(), lambda: x.view(3, 1), lambda: x.half().float()[:2]):
+        with pytest.raises(RuntimeError, match="a test cannot be captured without the native host path"):
+            run(view())
+    assert torch.equal(run(x * x), torch.full((3,), 4.0))
 
 
 def test_both_functions_ask(monkeypatch):

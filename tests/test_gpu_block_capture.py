@@ -46,6 +46,45 @@ def test_beside_an_eager_graph(monkeypatch):
             assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("python", [False, True])
+def test_beside_an_eager_graph_of_what_a_cast_is_made_of(python, monkeypatch):
+    from paper_2511_13645_amd import binding as fsa
+    from paper_2511_13645_amd.autograd import fused_gated_feed_forward, fused_residual_norm
+    fsa.lib()
+    assert fsa._block_host is not None
+    if python:
+        monkeypatch.setattr(fsa, "norm", lambda *a: None)
+        monkeypatch.setattr(fsa, "gated", lambda *a: None)
+    gen = torch.Generator(device=DEV).manual_seed(0)
+    n = lambda *s: torch.randn(s, generator=gen, device=DEV)
+    x, g, both, wd = n(50, 32).bfloat16(), n(50, 32).bfloat16(), n(96, 32).requires_grad_(True), n(32, 48).requires_grad_(True)
+    w = n(32).requires_grad_(True)
+
+    def gated():
+        tables = both.bfloat16()
+        return fused_gated_feed_forward(x, tables[:48], tables[48:], wd.bfloat16())
+
+    for call, leaves in ((gated, (both, wd)), (lambda: fused_residual_norm(x, w.bfloat16())[0], (w,))):
+        eager = call()
+        want = torch.autograd.grad(call(), leaves, g)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with pytest.raises(RuntimeError, match="eager graph"):
+            with torch.cuda.graph(graph):
+                torch.autograd.grad(call(), leaves, g)
+        torch.cuda.synchronize()
+        del eager
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = torch.autograd.grad(call(), leaves, g)
+        for _ in range(3):
+            for v in got:
+                v.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_without_the_native_host_path(monkeypatch):
     from paper_2511_13645_amd import binding as fsa
     fsa.lib()
